@@ -413,6 +413,78 @@ int dadam_regions_from_stretches(const dadam_stretch* stretches, uint32_t n_stre
 int dadam_place_by_timing(void* arena, uint64_t arena_bytes, int32_t device, const uint64_t* nbytes, uint32_t n,
                           uint64_t device_total_bytes, uint64_t* offsets, dadam_placement* report);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * Around the step: gradient clipping before it, 4-bit gossip behind it
+ *
+ * All of these take their buffers in the call: HOST arrays of n_rows (messages that are read: n_cols) DEVICE pointers,
+ * caller-owned, 16-byte aligned and below address 2^52; nothing has to be bound.  Buffers of parameters have cfg.d elements of param_dtype,
+ * gradients cfg.d of grad_dtype, copies and sums cfg.d float32, messages dadam_mx4_info.bytes bytes.  What a call writes must not
+ * overlap anything else it reads or writes, but where "in place" is named.  Padding between tensors takes no part: it is
+ * neither used nor written.  The first such call on a handle allocates and uploads what tells padding from elements (4 bytes for every 512
+ * elements, 64 more where padding lies among them; nothing for one tensor of a multiple of 512) and the scratch of the norms; it may wait for the device, later calls allocate nothing and may be recorded into a graph.
+ * Errors of all: DADAM_EINVAL (null, address too high, value out of range, d above 2^36), DADAM_EALIGN, DADAM_EALIAS, DADAM_ESTATE (slot empty,
+ * host-only handle, n_rows != n_cols where named), DADAM_EHIP. */
+
+/* The global norm of every row's gradient over all tensors of the layout,
+ *     norms[i] = sqrt(sum_e grads[i][e]^2),
+ * to norms[n_rows], DEVICE memory, float32.  Squares and sums are taken in 64 bits, in an order that depends on the layout
+ * and n_rows only: the same inputs give the same bits, and no square overflows or vanishes.  A NaN makes the norm NaN,
+ * an infinity (without a NaN) makes it infinite; a norm above float32's range is infinite too.  Calls of dadam_grad_norm and dadam_clip_grads on one handle must not
+ * overlap in time: they share the handle's partial sums. */
+int dadam_grad_norm(dadam_handle* h, const void* const* grads, float* norms, void* hip_stream);
+
+/* Clipping by the global norm, as recipes for language models have it before Adam: the norms as above, and
+ *     out[i][e] = grads[i][e]                             if norms[i] <= max_norm (the same bits),
+ *                 grads[i][e] * (max_norm / norms[i])     otherwise,
+ * the quotient and the product in float32, rounded once to grad_dtype.  An infinite norm makes the factor 0 (finite elements
+ * become 0, infinite ones NaN), a NaN norm makes all elements NaN: a caller who would rather skip such a step looks at norms.
+ * out[i] may be grads[i] (in place; a row that needs no scaling is then not written).  max_norm is finite and >= 0. */
+int dadam_clip_grads(dadam_handle* h, const void* const* grads, void* const* out, float max_norm, float* norms,
+                     void* hip_stream);
+
+/* Messages: a vector in microscaled 4-bit floating point.  Block k is elements [32 k, 32 k + 32) of the packed vector, whatever
+ * tensors they belong to (pack with align_elems = 32 for blocks that no two tensors share).  Bytes 16 k .. 16 k + 15 of a message
+ * hold its codes, element 32 k + 2 j in the low half of byte j and 32 k + 2 j + 1 in the high half: a sign (8) and a magnitude
+ * 0, 1/2, 1, 3/2, 2, 3, 4, 6 (0 to 7).  Byte scale_offset + k holds the block's power of two: b stands for 2^(b - 127), 255 makes
+ * the whole block NaN.  (E2M1 elements and E8M0 scales of the OCP microscaling formats, blocks of 32.)  Codes of padding are 0. */
+#define DADAM_MX4_BLOCK 32u
+typedef struct {
+  uint64_t n_blocks;     /* ceil(d / 32) */
+  uint64_t scale_offset; /* 16 n_blocks */
+  uint64_t bytes;        /* 17 n_blocks, rounded up to 16 */
+} dadam_mx4_info;
+int dadam_mx4_get_info(const dadam_handle* h, dadam_mx4_info* out);
+
+/* What a worker sends.  For every row i, with u = x[i] - copy_in[i] in float32 (u = x[i] where copy_in is null) and, in every
+ * block, a = max |u| over its elements:
+ *     scale 2^e, e = max(floor(log2 a) - 2, -126);   q = u / 2^e to the nearest magnitude above, ties to the even code, at most 6
+ *     msg[i] = the codes and scales;   copy_out[i] = copy_in[i] + q 2^e   (q 2^e where copy_in is null)
+ * A block with an infinite or NaN u is sent as NaN (scale 255, codes 0).  copy_out may be null; copy_out[i] may be copy_in[i] (in place).
+ * Sending differences against a copy that sender and receivers move alike (start it at x^(0), or at 0) is what makes so coarse a
+ * message enough: what one round loses stays in the next round's difference. */
+int dadam_mx4_encode(dadam_handle* h, const void* const* x, const float* const* copy_in, float* const* copy_out,
+                     void* const* msg, void* hip_stream);
+
+/* out[i] = sum_k w[k] * value(msg[col[k]]) over row i of the slot's neighbour list, or out[i] += that with DADAM_MX4_ADD: the rows of W
+ * times vectors held in 4 bits.  msg has n_cols entries; those that no row lists are not read.  float32 sums in the order the row lists.
+ * The identity matrix decodes. */
+#define DADAM_MX4_ADD 1u
+int dadam_mx4_product(dadam_handle* h, uint32_t slot, const void* const* msg, float* const* out, uint32_t flags,
+                      void* hip_stream);
+
+/* The gossip update of a worker that keeps ONE vector for all its neighbours, sum[i] = sum_k w[k] copy[col[k]]:
+ *     sum[i] += sum_k w[k] * value(msg[col[k]]);      x_dst[i] = x_src[i] + gamma * (sum[i] - copy[i])
+ * with copy[i] the worker's own public copy, already moved by its own message (dadam_mx4_encode), and that message among msg.
+ * With a doubly stochastic W the replicas' mean does not move; 0 < gamma <= 1 (smaller for sparser graphs and coarser messages).  x_dst[i] may be x_src[i] (in place).
+ * float32, one rounding of x_dst to param_dtype. */
+int dadam_mx4_gossip(dadam_handle* h, uint32_t slot, const void* const* msg, float* const* sum, const float* const* copy,
+                     const void* const* x_src, void* const* x_dst, float gamma, void* hip_stream);
+
+/* One whole round where the handle holds every replica (n_rows == n_cols): dadam_mx4_encode of x_src against copy (in place) and
+ * dadam_mx4_gossip of the messages, in one pass and with the same bits, the messages never leaving the chip.  x_dst[i] may be x_src[i]. */
+int dadam_mx4_round(dadam_handle* h, uint32_t slot, const void* const* x_src, void* const* x_dst, float* const* copy,
+                    float* const* sum, float gamma, void* hip_stream);
+
 /* Text of the last error recorded on this handle ("" if none).  With h == NULL: the text of the
  * last dadam_init failure of the calling thread.  The pointer stays valid until the next call on
  * the same handle (thread). */

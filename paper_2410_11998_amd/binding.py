@@ -29,6 +29,7 @@ DADAM_F32, DADAM_BF16 = 0, 1
 DADAM_OK, DADAM_EINVAL, DADAM_EALIGN, DADAM_ETOPO, DADAM_EALIAS, DADAM_ESTATE, DADAM_EHIP = 0, -1, -2, -3, -4, -5, -6
 DADAM_FUSE_ACCUM, DADAM_FORCE_DIRECT, DADAM_FORCE_TILE = 1, 2, 4
 DADAM_WARN_NOT_COLUMN_STOCHASTIC = 1
+DADAM_MX4_BLOCK, DADAM_MX4_ADD = 32, 1
 DADAM_PLACE_TWO_REGIONS, DADAM_PLACE_ARENA_ELSEWHERE, DADAM_PLACE_TOO_LARGE = 1, 2, 4
 
 EXPORTS = [
@@ -36,6 +37,7 @@ EXPORTS = [
     "dadam_gossip_step_range", "dadam_accumulate", "dadam_mix", "dadam_mix_consensus", "dadam_mix_consensus_static", "dadam_set_lr", "dadam_get_plan_info",
     "dadam_slot_uses_tile_mode", "dadam_get_row_order", "dadam_pack_offsets", "dadam_spread_offsets", "dadam_place_offsets", "dadam_deal_offsets", "dadam_find_stretches", "dadam_regions_from_stretches",
     "dadam_place_by_timing",
+    "dadam_grad_norm", "dadam_clip_grads", "dadam_mx4_get_info", "dadam_mx4_encode", "dadam_mx4_product", "dadam_mx4_gossip", "dadam_mx4_round",
     "dadam_last_error",
     "dadam_destroy",
 ]
@@ -68,6 +70,10 @@ class dadam_plan_info(C.Structure):
                 ("mix_tile_elems", C.c_uint32), ("lds_bytes_mix", C.c_uint32), ("n_tiles_mix", C.c_uint64),
                 ("tile_waves", C.c_uint32), ("tile_vectors", C.c_uint32), ("mix_waves", C.c_uint32),
                 ("mix_vectors", C.c_uint32), ("streaming", C.c_uint32)]
+
+
+class dadam_mx4_info(C.Structure):
+    _fields_ = [("n_blocks", C.c_uint64), ("scale_offset", C.c_uint64), ("bytes", C.c_uint64)]
 
 
 PROBE_CHUNK_BYTES, PROBE_STEP_BYTES, MAX_STRETCHES = 1 << 30, 4 << 30, 6
@@ -117,6 +123,14 @@ def _load() -> C.CDLL:
     lib.dadam_get_row_order.argtypes = [H, C.c_uint32, C.POINTER(C.c_int32)]
     lib.dadam_deal_offsets.argtypes = [C.POINTER(C.c_uint64), C.c_uint32, C.c_uint64, C.c_uint64, C.c_uint64, C.c_uint64,
                                        C.c_uint32, C.POINTER(C.c_uint64)]
+    P = C.POINTER(C.c_void_p)
+    lib.dadam_grad_norm.argtypes = [H, P, C.c_void_p, C.c_void_p]
+    lib.dadam_clip_grads.argtypes = [H, P, P, C.c_float, C.c_void_p, C.c_void_p]
+    lib.dadam_mx4_get_info.argtypes = [H, C.POINTER(dadam_mx4_info)]
+    lib.dadam_mx4_encode.argtypes = [H, P, P, P, P, C.c_void_p]
+    lib.dadam_mx4_product.argtypes = [H, C.c_uint32, P, P, C.c_uint32, C.c_void_p]
+    lib.dadam_mx4_gossip.argtypes = [H, C.c_uint32, P, P, P, P, P, C.c_float, C.c_void_p]
+    lib.dadam_mx4_round.argtypes = [H, C.c_uint32, P, P, P, P, C.c_float, C.c_void_p]
     lib.dadam_last_error.argtypes = [H]
     lib.dadam_last_error.restype = C.c_char_p
     lib.dadam_destroy.argtypes = [H]
@@ -141,7 +155,7 @@ def _ptr_array(ptrs: Sequence[int]):
     return arr
 
 
-_SHAPE_OF_HANDLE = {}   # handle value -> (d, bytes per parameter, bytes per gradient): host-side size checks only
+_SHAPE_OF_HANDLE = {}   # handle value -> (d, bytes per parameter, bytes per gradient, rows, columns): host-side size checks only
 
 
 def _ptrs_of(tensors, h=None, elem_bytes: int = 0, what: str = "") -> Sequence[int]:
@@ -285,7 +299,7 @@ def dadam_init(n_rows: int, n_cols: int, d: int, offsets: Sequence[int], numels:
     rc = lib.dadam_init(C.byref(cfg), C.byref(h))
     if rc < 0:
         raise DadamError(rc, (lib.dadam_last_error(None) or b"").decode())
-    _SHAPE_OF_HANDLE[h.value] = (int(d), 2 if param_dtype == DADAM_BF16 else 4, 2 if grad_dtype == DADAM_BF16 else 4)
+    _SHAPE_OF_HANDLE[h.value] = (int(d), 2 if param_dtype == DADAM_BF16 else 4, 2 if grad_dtype == DADAM_BF16 else 4, int(n_rows), int(n_cols))
     return h
 
 
@@ -370,6 +384,110 @@ def dadam_get_plan_info(h) -> dadam_plan_info:
 
 def dadam_slot_uses_tile_mode(h, slot: int) -> bool:
     return _check(h, lib.dadam_slot_uses_tile_mode(h, slot)) == 1
+
+
+_TABLE_OF = {}   # number of pointers -> ctypes array type
+
+
+def _table(ptrs):
+    kind = _TABLE_OF.get(len(ptrs))
+    if kind is None:
+        kind = _TABLE_OF[len(ptrs)] = C.c_void_p * len(ptrs)
+    return kind(*ptrs)
+
+
+def pointer_table(buffers, count: int, length: int, elem_bytes: int, what: str):
+    """The host array of `count` device pointers that the calls below take, marshalled and size-checked once: from a sequence of tensors (or
+    integers taken as addresses), or from one tensor whose rows are the buffers.  None stays None, a table made before is
+    passed through.  The tensors must stay alive."""
+    if buffers is None:
+        return None
+    if len(buffers) < count:
+        raise ValueError(f"{what} holds {len(buffers)} buffers, the handle needs {count}")
+    if isinstance(buffers, C.Array):
+        return buffers
+    if hasattr(buffers, "data_ptr"):
+        stride = buffers.stride()
+        if len(stride) != 2 or (stride[1] != 1 and buffers.shape[1] > 1):
+            raise ValueError(f"{what} is one tensor: its rows must be the buffers, each contiguous")
+        if buffers.element_size() != elem_bytes:
+            raise ValueError(f"{what} has {buffers.element_size()}-byte elements, the handle expects {elem_bytes}")
+        if buffers.shape[1] < length:
+            raise ValueError(f"{what} holds {buffers.shape[1]} elements a buffer, the handle needs {length}")
+        first, step = buffers.data_ptr(), stride[0] * elem_bytes
+        return _table([first + k * step for k in range(count)])
+    ptrs = []
+    for k in range(count):
+        t = buffers[k]
+        if not isinstance(t, int):
+            if not t.is_contiguous():
+                raise ValueError(f"{what}[{k}] is not contiguous")
+            if t.element_size() != elem_bytes:
+                raise ValueError(f"{what}[{k}] has {t.element_size()}-byte elements, the handle expects {elem_bytes}")
+            if t.numel() < length:
+                raise ValueError(f"{what}[{k}] holds {t.numel()} elements, the handle needs {length}")
+            t = t.data_ptr()
+        ptrs.append(t)
+    return _table(ptrs)
+
+
+def _shape(h):
+    return _SHAPE_OF_HANDLE.get(getattr(h, "value", None), (0, 0, 0, 0, 0))
+
+
+def _message_bytes(d: int) -> int:
+    return -(-(-(-d // DADAM_MX4_BLOCK) * 17) // 16) * 16
+
+
+def _row_values(h, norms) -> int:
+    if isinstance(norms, int):
+        return norms
+    if norms.numel() < _shape(h)[3] or norms.element_size() != 4 or not norms.is_contiguous():
+        raise ValueError("norms must hold one float32 a row")
+    return norms.data_ptr()
+
+
+def dadam_grad_norm(h, grads, norms, stream: int = 0) -> None:
+    """norms: a device tensor of n_rows float32 (or an integer device address)."""
+    d, _, gb, rows, _ = _shape(h)
+    _check(h, lib.dadam_grad_norm(h, pointer_table(grads, rows, d, gb, "grads"), _row_values(h, norms), stream))
+
+
+def dadam_clip_grads(h, grads, out, max_norm: float, norms, stream: int = 0) -> None:
+    d, _, gb, rows, _ = _shape(h)
+    _check(h, lib.dadam_clip_grads(h, pointer_table(grads, rows, d, gb, "grads"), pointer_table(out, rows, d, gb, "out"), max_norm,
+                                   _row_values(h, norms), stream))
+
+
+def dadam_mx4_get_info(h) -> dadam_mx4_info:
+    info = dadam_mx4_info()
+    _check(h, lib.dadam_mx4_get_info(h, C.byref(info)))
+    return info
+
+
+def dadam_mx4_encode(h, x, copy_in, copy_out, msg, stream: int = 0) -> None:
+    """copy_in and copy_out may be None; messages are uint8 tensors."""
+    d, pb, _, rows, _ = _shape(h)
+    _check(h, lib.dadam_mx4_encode(h, pointer_table(x, rows, d, pb, "x"), pointer_table(copy_in, rows, d, 4, "copy_in"),
+                                   pointer_table(copy_out, rows, d, 4, "copy_out"), pointer_table(msg, rows, _message_bytes(d), 1, "msg"), stream))
+
+
+def dadam_mx4_product(h, slot: int, msg, out, flags: int = 0, stream: int = 0) -> None:
+    d, _, _, rows, cols = _shape(h)
+    _check(h, lib.dadam_mx4_product(h, slot, pointer_table(msg, cols, _message_bytes(d), 1, "msg"), pointer_table(out, rows, d, 4, "out"), flags, stream))
+
+
+def dadam_mx4_gossip(h, slot: int, msg, sum, copy, x_src, x_dst, gamma: float, stream: int = 0) -> None:
+    d, pb, _, rows, cols = _shape(h)
+    _check(h, lib.dadam_mx4_gossip(h, slot, pointer_table(msg, cols, _message_bytes(d), 1, "msg"), pointer_table(sum, rows, d, 4, "sum"),
+                                   pointer_table(copy, rows, d, 4, "copy"), pointer_table(x_src, rows, d, pb, "x_src"),
+                                   pointer_table(x_dst, rows, d, pb, "x_dst"), gamma, stream))
+
+
+def dadam_mx4_round(h, slot: int, x_src, x_dst, copy, sum, gamma: float, stream: int = 0) -> None:
+    d, pb, _, rows, _ = _shape(h)
+    _check(h, lib.dadam_mx4_round(h, slot, pointer_table(x_src, rows, d, pb, "x_src"), pointer_table(x_dst, rows, d, pb, "x_dst"),
+                                  pointer_table(copy, rows, d, 4, "copy"), pointer_table(sum, rows, d, 4, "sum"), gamma, stream))
 
 
 def dadam_destroy(h) -> None:

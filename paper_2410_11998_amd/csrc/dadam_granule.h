@@ -1,0 +1,118 @@
+// What the kernels of the operators around the step share: granules of 512 elements (a wavefront's share: lane l holds elements
+// 4 l .. 4 l + 3 and 256 + 4 l .. 256 + 4 l + 3, so that every access covers one contiguous run), the padding that cuts them, and
+// the addresses of a row's buffers.
+#ifndef DADAM_GRANULE_H_
+#define DADAM_GRANULE_H_
+
+#include "dadam_device.h"
+#include "dadam_operators.h"
+
+namespace dadam {
+namespace {
+
+template <typename T>
+__device__ __forceinline__ T* global_pointer(uint64_t address) {
+  typedef T __attribute__((address_space(1))) * Global;
+  return (T*)(Global)address;
+}
+// Buffer K of a row.
+template <typename T, int K>
+__device__ __forceinline__ T* buffer(const RowPointers& r) {
+  const uint64_t high = (r.high[K / 2] >> (16 * (K % 2))) & 0xFFFFu;
+  return global_pointer<T>(((high << 32) | r.low[K]) << 4);
+}
+__device__ __forceinline__ const uint8_t* buffer(const ColPointer& c) {
+  return global_pointer<const uint8_t>((((uint64_t)c.high << 32) | c.low) << 4);
+}
+
+__device__ __forceinline__ uint32_t wave_of_group() { return (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)); }
+
+// 1 + where the masks of a granule stand, 0 if no padding cuts it.
+__device__ __forceinline__ uint32_t cut_of(const Cuts& c, uint32_t granule) {
+  typedef const uint32_t __attribute__((address_space(4))) * Constant;
+  return c.index ? ((Constant)c.index)[granule] : 0u;
+}
+// Bits 0 to 3: which elements of a lane's group `half` belong to a tensor.
+__device__ __forceinline__ uint32_t group_bits(const Cuts& c, uint32_t cut, uint32_t half, uint32_t lane) {
+  if (cut == 0) return 0xFu;
+  return (c.masks[cut - 1 + half * (kGranuleBlocks / 2) + lane / 8] >> (4 * (lane % 8))) & 0xFu;
+}
+
+// A lane's group of four elements from e on (a multiple of 4), widened to float; elements that `bits` leaves out are not touched
+// and read as zero.
+template <typename T, bool NT>
+__device__ __forceinline__ void load_group(const void* base, uint64_t e, uint32_t bits, float (&v)[4]) {
+  if (bits == 0xFu) {
+    if constexpr (T::bytes == 4) {
+      const f4 x = vload<NT>(reinterpret_cast<const f4*>(at<float>(base, e)));
+      v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+    } else {
+      const u2 x = vload<NT>(reinterpret_cast<const u2*>(at<uint16_t>(base, e)));
+      v[0] = __uint_as_float(x.x << 16); v[1] = __uint_as_float(x.x & 0xFFFF0000u);
+      v[2] = __uint_as_float(x.y << 16); v[3] = __uint_as_float(x.y & 0xFFFF0000u);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = bits >> j & 1 ? load_elem<T>(base, e + j) : 0.0f;
+  }
+}
+
+template <typename T, bool NT>
+__device__ __forceinline__ void store_group(void* base, uint64_t e, uint32_t bits, const float (&v)[4]) {
+  if (bits == 0xFu) {
+    if constexpr (T::bytes == 4) {
+      const f4 x = {v[0], v[1], v[2], v[3]};
+      vstore<NT>(reinterpret_cast<f4*>(at<float>(base, e)), x);
+    } else {
+      const u2 x = {f32_to_bf16_bits(v[0]) | (f32_to_bf16_bits(v[1]) << 16), f32_to_bf16_bits(v[2]) | (f32_to_bf16_bits(v[3]) << 16)};
+      vstore<NT>(reinterpret_cast<u2*>(at<uint16_t>(base, e)), x);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (bits >> j & 1) store_elem<T>(base, e + j, v[j]);
+  }
+}
+
+}  // namespace
+
+// The part of a large argument block that a launch of at most kFewOperands rows (and sources) needs.
+template <typename Few, typename All>
+Few few_rows(const All& a) {
+  Few f;
+  memcpy((void*)f.row, (const void*)a.row, sizeof(f.row));
+  return f;
+}
+
+// The status of the launch itself; the runtime's copy of a failure is taken away (the call that reports it is this one).
+inline int enqueue_grid(KernelFn fn, uint32_t grid, uint32_t block, void* args, uint32_t lds, void* stream) {
+  if (grid == 0) return (int)hipSuccess;
+  void* list[] = {args};
+  const hipError_t e = hipLaunchKernel(fn, dim3(grid), dim3(block), list, lds, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) (void)hipGetLastError();
+  return (int)e;
+}
+
+inline constexpr uint32_t kMostThreads = 0xFFFFFFFFu;  // of one launch
+
+// Runs `launch` over granules [first, first + count) in pieces whose grid stays below 2^32 threads, `per` granules and `threads` a
+// workgroup, `groups` workgroups for each.
+template <typename Args, typename Launch>
+int in_pieces(Args& a, uint32_t per, uint32_t groups, uint32_t threads, Launch launch) {
+  const uint32_t most = kMostThreads / threads / groups;
+  uint64_t left = a.s.count;
+  int e = (int)hipSuccess;
+  while (left > 0 && e == (int)hipSuccess) {
+    const uint64_t works = (left + per - 1) / per;
+    const uint32_t now = works < most ? (uint32_t)works : most;
+    e = launch(now * groups);
+    const uint64_t done = (uint64_t)now * per < left ? (uint64_t)now * per : left;
+    a.s.first += (uint32_t)done;
+    left -= done;
+  }
+  return e;
+}
+
+}  // namespace dadam
+
+#endif  // DADAM_GRANULE_H_

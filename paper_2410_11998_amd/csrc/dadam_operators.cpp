@@ -1,0 +1,397 @@
+// Host side of the operators around the step (include/dadam.h, "Around the step"): validation, what a handle keeps for them on
+// the device, and launch set-up.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <memory>
+#include <new>
+#include <vector>
+
+#include "dadam_handle.h"
+#include "dadam_operators.h"
+
+namespace dadam {
+
+struct OperatorState {
+  uint32_t* cuts = nullptr;   // index and masks of Cuts, null if no padding cuts a granule
+  uint32_t n_index = 0;       // words of index, the masks stand behind
+  double* partials = nullptr; // per_row partial sums a row
+  uint32_t* arrived = nullptr;
+  uint32_t per_row = 1;
+};
+
+namespace {
+
+uint64_t granules_of(const dadam_handle* h) { return (h->cfg.d + kGranule - 1) / kGranule; }
+
+// Index and masks of the layout's granules (see Cuts); empty if all are whole.
+std::vector<uint32_t> build_cuts(const dadam_handle* h, uint32_t* n_index) {
+  const uint64_t n = granules_of(h);
+  std::vector<uint32_t> index(n, 0), masks;
+  // A granule is whole if one segment covers it; the others get a word of bits for each of their blocks, here side by side in order.
+  uint64_t covered = 0;  // granules before this one have their entry
+  auto cut = [&](uint64_t g) -> uint32_t* {
+    if (index[g] == 0) {
+      masks.resize(masks.size() + kGranuleBlocks, 0u);
+      index[g] = (uint32_t)(masks.size() - kGranuleBlocks) + 1;
+    }
+    return masks.data() + index[g] - 1;
+  };
+  for (size_t k = 0; k <= h->segs.size(); ++k) {
+    const bool end = k == h->segs.size();
+    const uint64_t lo = end ? n * kGranule : h->segs[k].lo, hi = end ? lo : h->segs[k].hi;
+    for (uint64_t g = covered; g < lo / kGranule; ++g) cut(g);  // nothing but padding, or begun by the segment before
+    covered = std::max(covered, lo / kGranule);
+    for (uint64_t g = lo / kGranule; !end && g * kGranule < hi; ++g) {
+      const uint64_t from = std::max(lo, g * kGranule), to = std::min(hi, (g + 1) * kGranule);
+      if (to - from == kGranule) {
+        covered = g + 1;
+        continue;
+      }
+      uint32_t* m = cut(g);
+      for (uint64_t e = from; e < to; ++e) m[e % kGranule / kMxBlock] |= 1u << e % kMxBlock;
+      if (to == (g + 1) * kGranule) covered = g + 1;
+    }
+  }
+  *n_index = (uint32_t)n;
+  if (masks.empty()) return {};
+  index.insert(index.end(), masks.begin(), masks.end());
+  return index;
+}
+
+void free_state(OperatorState* s) {
+  if (!s) return;
+  if (s->cuts) (void)hipFree(s->cuts);
+  if (s->partials) (void)hipFree(s->partials);
+  delete s;
+}
+
+constexpr uint64_t kMostElems = 1ull << 36;  // index and masks count in 32 bits
+
+// Segments with different decay that touch are one run of elements here: build_cuts sees every segment alone, and a granule that two
+// of them share gets masks whose bits add up to all elements, which costs a little and changes nothing.
+int make_state(dadam_handle* h) {
+  std::unique_ptr<OperatorState, void (*)(OperatorState*)> s(new OperatorState(), free_state);
+  const std::vector<uint32_t> cuts = build_cuts(h, &s->n_index);
+  // Workgroups of the norm, for all rows together: eight granules a wavefront, so that few have to report where there is little to
+  // read, up to four workgroups a compute unit.  us, 1024 / 2048 / 4096 workgroups: 8 rows of 355 million bfloat16 elements 872 / 898 /
+  // 922, norm and clipping of 4 rows of a million (256 workgroups by the rule: 14) 23 / 34 / 34.
+  s->per_row = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>((granules_of(h) + 31) / 32, 1024 / h->cfg.n_rows));
+  const size_t sums = (size_t)s->per_row * h->cfg.n_rows * sizeof(double);
+  const std::vector<char> zeros(sums + DADAM_MAX_ROWS * sizeof(uint32_t), 0);
+  hipError_t e = hipMalloc((void**)&s->partials, zeros.size());
+  if (e == hipSuccess) e = hipMemcpy(s->partials, zeros.data(), zeros.size(), hipMemcpyHostToDevice);
+  if (e == hipSuccess && !cuts.empty()) {
+    e = hipMalloc((void**)&s->cuts, cuts.size() * sizeof(uint32_t));
+    if (e == hipSuccess) e = hipMemcpy(s->cuts, cuts.data(), cuts.size() * sizeof(uint32_t), hipMemcpyHostToDevice);
+  }
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    return fail(h, DADAM_EHIP, "setting up the operators around the step failed: %s", hipGetErrorString(e));
+  }
+  s->arrived = reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(s->partials) + sums);
+  h->operators = s.release();
+  h->free_operators = free_state;
+  return DADAM_OK;
+}
+
+// One argument of a call: n buffers of `bytes` bytes.
+struct Table {
+  const void* const* p;
+  uint32_t n;
+  size_t bytes;
+  const char* name;
+  bool written;
+  int in_place_of;  // the table whose entry of the same number this one's may be, -1 none
+};
+
+struct Range {
+  uintptr_t lo, hi;
+  int table;
+  uint32_t index;
+};
+
+constexpr uintptr_t kHighest = (uintptr_t)1 << 52;
+
+// Every buffer is there, aligned and within reach; nothing that is written overlaps anything else, but the same entry of the table
+// it may be in place of.
+int check_tables(const dadam_handle* h, const Table* t, int n_tables) {
+  if (h->cfg.d > kMostElems) return fail(h, DADAM_EINVAL, "the operators around the step take up to 2^36 elements");
+  Range all[5 * DADAM_MAX_ROWS], open[5 * DADAM_MAX_ROWS];  // open: earlier ranges that reach beyond where the walk is
+  uint32_t n = 0, n_open = 0;
+  for (int k = 0; k < n_tables; ++k)
+    for (uint32_t i = 0; t[k].p && i < t[k].n; ++i) {
+      const uintptr_t at = (uintptr_t)t[k].p[i];
+      if (!at) return fail(h, DADAM_EINVAL, "%s[%u] is null", t[k].name, i);
+      if (at & 15u) return fail(h, DADAM_EALIGN, "%s[%u] is not 16-byte aligned", t[k].name, i);
+      if (at >= kHighest || t[k].bytes > kHighest - at) return fail(h, DADAM_EINVAL, "%s[%u] reaches above address 2^52", t[k].name, i);
+      all[n++] = {at, at + t[k].bytes, k, i};
+    }
+  std::sort(all, all + n, [](const Range& a, const Range& b) { return a.lo < b.lo; });
+  for (uint32_t q = 0; q < n; ++q) {
+    const Range& r = all[q];
+    n_open = (uint32_t)(std::remove_if(open, open + n_open, [&](const Range& o) { return o.hi <= r.lo; }) - open);
+    for (uint32_t k = 0; k < n_open; ++k) {
+      const Range& o = open[k];
+      if (!t[r.table].written && !t[o.table].written) continue;
+      const bool pair = t[r.table].in_place_of == o.table || t[o.table].in_place_of == r.table;
+      if (pair && r.lo == o.lo && r.index == o.index) continue;
+      return fail(h, DADAM_EALIAS, "%s[%u] overlaps %s[%u]", t[r.table].name, r.index, t[o.table].name, o.index);
+    }
+    open[n_open++] = r;
+  }
+  return DADAM_OK;
+}
+
+int check_norms(const dadam_handle* h, const float* norms) {
+  if (!norms) return fail(h, DADAM_EINVAL, "norms is null");
+  if ((uintptr_t)norms & 3u) return fail(h, DADAM_EALIGN, "norms is not 4-byte aligned");
+  return DADAM_OK;
+}
+
+int check_slot(const dadam_handle* h, uint32_t slot) {
+  if (slot >= DADAM_MAX_SLOTS) return fail(h, DADAM_EINVAL, "slot %u out of range", slot);
+  if (!h->slots[slot].set) return fail(h, DADAM_ESTATE, "slot %u has no topology", slot);
+  return DADAM_OK;
+}
+
+int check_gamma(const dadam_handle* h, float gamma) {
+  if (!(gamma > 0.f && gamma <= 1.f)) return fail(h, DADAM_EINVAL, "gamma must be in (0, 1]");
+  return DADAM_OK;
+}
+
+// A pointer as the kernels take it (see RowPointers).
+void put(RowPointers* r, int k, const void* p) {
+  const uint64_t v = (uint64_t)(uintptr_t)p >> 4;
+  r->low[k] = (uint32_t)v;
+  r->high[k / 2] |= (uint32_t)(v >> 32) << (16 * (k % 2));
+}
+void put(ColPointer* c, const void* p) {
+  const uint64_t v = (uint64_t)(uintptr_t)p >> 4;
+  c->low = (uint32_t)v;
+  c->high = (uint32_t)(v >> 32);
+}
+
+void fill_span(const dadam_handle* h, Span* s) {
+  const OperatorState* o = h->operators;
+  s->cuts = {o->cuts, o->cuts ? o->cuts + o->n_index : nullptr};
+  s->d = h->cfg.d;
+  s->n_granules = (uint32_t)granules_of(h);
+  s->first = 0;
+  s->count = s->n_granules;
+  s->row0 = 0;
+  s->n_rows = h->cfg.n_rows;
+  s->n_xcd = h->n_xcds;
+  s->streams = h->nontemporal;
+}
+
+uint64_t blocks_of(const dadam_handle* h) { return (h->cfg.d + kMxBlock - 1) / kMxBlock; }
+size_t message_bytes(const dadam_handle* h) { return (size_t)((blocks_of(h) * 17 + 15) / 16 * 16); }
+
+Lists lists_of(const Slot& s) { return {s.d_row_ptr, s.d_col, s.d_w}; }
+
+// Runs the launches of a call whose arguments have passed, with the handle's device current and its state made.
+template <typename Launch>
+int on_device(dadam_handle* h, Launch launch) {
+  DeviceGuard guard(h->cfg.device);
+  if (guard.err != hipSuccess) return fail(h, DADAM_EHIP, "hipSetDevice: %s", hipGetErrorString(guard.err));
+  if (!h->operators) {
+    const int rc = make_state(h);
+    if (rc) return rc;
+  }
+  const int e = launch();
+  if (e != (int)hipSuccess) return fail(h, DADAM_EHIP, "kernel launch failed: %s", hipGetErrorString((hipError_t)e));
+  return DADAM_OK;
+}
+
+int norm_impl(dadam_handle* h, const void* const* grads, void* const* out, float max_norm, float* norms, void* stream) {
+  const uint32_t R = h->cfg.n_rows;
+  const size_t gb = (size_t)h->cfg.d * dtype_bytes(h->cfg.grad_dtype);
+  const Table tables[2] = {{grads, R, gb, "grads", false, -1}, {out, out ? R : 0, gb, "out", true, 0}};
+  int rc = check_norms(h, norms);
+  if (!rc) rc = check_tables(h, tables, 2);
+  if (!rc && out)  // the norms lie outside the table's checks: they need not be 16-byte aligned
+    for (uint32_t i = 0; i < R && !rc; ++i)
+      if ((uintptr_t)norms < (uintptr_t)out[i] + gb && (uintptr_t)out[i] < (uintptr_t)(norms + R)) rc = fail(h, DADAM_EALIAS, "norms overlaps out[%u]", i);
+  for (uint32_t i = 0; i < R && !rc; ++i)
+    if ((uintptr_t)norms < (uintptr_t)grads[i] + gb && (uintptr_t)grads[i] < (uintptr_t)(norms + R)) rc = fail(h, DADAM_EALIAS, "norms overlaps grads[%u]", i);
+  if (!rc) rc = check_device(h);
+  if (rc) return rc;
+  return on_device(h, [&] {
+    NormArgs<kMaxRows> a;
+    memset((void*)&a, 0, sizeof(a));
+    for (uint32_t i = 0; i < R; ++i) {
+      put(&a.row[i], 0, grads[i]);
+      if (out) put(&a.row[i], 1, out[i]);
+    }
+    fill_span(h, &a.s);
+    a.partials = h->operators->partials;
+    a.arrived = h->operators->arrived;
+    a.per_row = h->operators->per_row;
+    a.norms = norms;
+    a.max_norm = max_norm;
+    int e = launch_norm((int)h->cfg.grad_dtype, a, stream);
+    if (e == (int)hipSuccess && out) e = launch_clip((int)h->cfg.grad_dtype, a, stream);
+    return e;
+  });
+}
+
+int mix_impl(dadam_handle* h, uint32_t slot, const void* const* msg, float* const* sum, MixMode mode, const float* const* copy,
+             const void* const* x_src, void* const* x_dst, float gamma, void* stream) {
+  const uint32_t R = h->cfg.n_rows, C = h->cfg.n_cols;
+  const size_t sb = (size_t)h->cfg.d * 4, xb = (size_t)h->cfg.d * dtype_bytes(h->cfg.param_dtype);
+  int rc = check_slot(h, slot);
+  const Table tables[5] = {{msg, C, message_bytes(h), "msg", false, -1},
+                           {(const void* const*)sum, R, sb, mode == kMixGossip ? "sum" : "out", true, -1},
+                           {(const void* const*)copy, R, sb, "copy", false, -1},
+                           {x_src, R, xb, "x_src", false, -1},
+                           {x_dst, R, xb, "x_dst", true, 3}};
+  if (!rc) rc = check_tables(h, tables, mode == kMixGossip ? 5 : 2);
+  if (!rc) rc = check_device(h);
+  if (rc) return rc;
+  return on_device(h, [&] {
+    int e = (int)hipSuccess;
+    for (uint32_t row0 = 0; row0 < R && e == (int)hipSuccess; row0 += kMessageRows) {
+      MixArgs<kMessageRows, kMaxRows> a;
+      memset((void*)&a, 0, sizeof(a));
+      fill_span(h, &a.s);
+      a.s.row0 = row0;
+      a.s.n_rows = std::min<uint32_t>(kMessageRows, R - row0);
+      for (uint32_t i = 0; i < a.s.n_rows; ++i) {
+        put(&a.row[i], 0, sum[row0 + i]);
+        if (mode != kMixGossip) continue;
+        put(&a.row[i], 1, copy[row0 + i]);
+        put(&a.row[i], 2, x_src[row0 + i]);
+        put(&a.row[i], 3, x_dst[row0 + i]);
+      }
+      for (uint32_t c = 0; c < C; ++c) put(&a.message[c], msg[c]);
+      a.lists = lists_of(h->slots[slot]);
+      a.scale_offset = 16 * blocks_of(h);
+      a.gamma = gamma;
+      e = launch_mix4((int)h->cfg.param_dtype, mode, C, a, stream);
+    }
+    return e;
+  });
+}
+
+// No exception leaves an entry point.
+template <typename Fn>
+int guarded(dadam_handle* h, Fn fn) {
+  try {
+    return fn();
+  } catch (const std::bad_alloc&) {
+    return fail(h, DADAM_EINVAL, "out of host memory");
+  }
+}
+
+}  // namespace
+}  // namespace dadam
+
+extern "C" {
+
+int dadam_grad_norm(dadam_handle* h, const void* const* grads, float* norms, void* hip_stream) {
+  if (!h) return DADAM_EINVAL;
+  if (!grads) return fail(h, DADAM_EINVAL, "grads is null");
+  return guarded(h, [&] { return norm_impl(h, grads, nullptr, 0.f, norms, hip_stream); });
+}
+
+int dadam_clip_grads(dadam_handle* h, const void* const* grads, void* const* out, float max_norm, float* norms, void* hip_stream) {
+  if (!h) return DADAM_EINVAL;
+  if (!grads || !out) return fail(h, DADAM_EINVAL, "grads or out is null");
+  if (!(max_norm >= 0.f) || !std::isfinite(max_norm)) return fail(h, DADAM_EINVAL, "max_norm must be finite and >= 0");
+  return guarded(h, [&] { return norm_impl(h, grads, out, max_norm, norms, hip_stream); });
+}
+
+int dadam_mx4_get_info(const dadam_handle* h, dadam_mx4_info* out) {
+  if (!h) return DADAM_EINVAL;
+  if (!out) return fail(h, DADAM_EINVAL, "out is null");
+  out->n_blocks = blocks_of(h);
+  out->scale_offset = 16 * out->n_blocks;
+  out->bytes = message_bytes(h);
+  return DADAM_OK;
+}
+
+int dadam_mx4_encode(dadam_handle* h, const void* const* x, const float* const* copy_in, float* const* copy_out, void* const* msg,
+                     void* hip_stream) {
+  if (!h) return DADAM_EINVAL;
+  if (!x || !msg) return fail(h, DADAM_EINVAL, "x or msg is null");
+  return guarded(h, [&] {
+    const uint32_t R = h->cfg.n_rows;
+    const size_t sb = (size_t)h->cfg.d * 4, xb = (size_t)h->cfg.d * dtype_bytes(h->cfg.param_dtype);
+    const Table tables[4] = {{x, R, xb, "x", false, -1},
+                             {(const void* const*)copy_in, R, sb, "copy_in", false, -1},
+                             {(const void* const*)copy_out, R, sb, "copy_out", true, 1},
+                             {msg, R, message_bytes(h), "msg", true, -1}};
+    int rc = check_tables(h, tables, 4);
+    if (!rc) rc = check_device(h);
+    if (rc) return rc;
+    return on_device(h, [&] {
+      EncodeArgs<kMaxRows> a;
+      memset((void*)&a, 0, sizeof(a));
+      for (uint32_t i = 0; i < R; ++i) {
+        put(&a.row[i], 0, x[i]);
+        if (copy_in) put(&a.row[i], 1, copy_in[i]);
+        if (copy_out) put(&a.row[i], 2, copy_out[i]);
+        put(&a.row[i], 3, msg[i]);
+      }
+      fill_span(h, &a.s);
+      a.scale_offset = 16 * blocks_of(h);
+      return launch_encode((int)h->cfg.param_dtype, a, hip_stream);
+    });
+  });
+}
+
+int dadam_mx4_product(dadam_handle* h, uint32_t slot, const void* const* msg, float* const* out, uint32_t flags, void* hip_stream) {
+  if (!h) return DADAM_EINVAL;
+  if (!msg || !out) return fail(h, DADAM_EINVAL, "msg or out is null");
+  if (flags & ~DADAM_MX4_ADD) return fail(h, DADAM_EINVAL, "unknown flags %u", flags);
+  return guarded(h, [&] {
+    return mix_impl(h, slot, msg, out, flags & DADAM_MX4_ADD ? kMixAdd : kMixStore, nullptr, nullptr, nullptr, 0.f, hip_stream);
+  });
+}
+
+int dadam_mx4_gossip(dadam_handle* h, uint32_t slot, const void* const* msg, float* const* sum, const float* const* copy,
+                     const void* const* x_src, void* const* x_dst, float gamma, void* hip_stream) {
+  if (!h) return DADAM_EINVAL;
+  if (!msg || !sum || !copy || !x_src || !x_dst) return fail(h, DADAM_EINVAL, "null table");
+  if (int rc = check_gamma(h, gamma)) return rc;
+  return guarded(h, [&] { return mix_impl(h, slot, msg, sum, kMixGossip, copy, x_src, x_dst, gamma, hip_stream); });
+}
+
+int dadam_mx4_round(dadam_handle* h, uint32_t slot, const void* const* x_src, void* const* x_dst, float* const* copy, float* const* sum,
+                    float gamma, void* hip_stream) {
+  if (!h) return DADAM_EINVAL;
+  if (!x_src || !x_dst || !copy || !sum) return fail(h, DADAM_EINVAL, "null table");
+  if (h->cfg.n_rows != h->cfg.n_cols) return fail(h, DADAM_ESTATE, "a round needs every replica in the handle (n_rows == n_cols)");
+  if (int rc = check_gamma(h, gamma)) return rc;
+  return guarded(h, [&] {
+    const uint32_t R = h->cfg.n_rows;
+    const size_t sb = (size_t)h->cfg.d * 4, xb = (size_t)h->cfg.d * dtype_bytes(h->cfg.param_dtype);
+    int rc = check_slot(h, slot);
+    const Table tables[4] = {{x_src, R, xb, "x_src", false, -1},
+                             {x_dst, R, xb, "x_dst", true, 0},
+                             {(const void* const*)copy, R, sb, "copy", true, -1},
+                             {(const void* const*)sum, R, sb, "sum", true, -1}};
+    if (!rc) rc = check_tables(h, tables, 4);
+    if (!rc) rc = check_device(h);
+    if (rc) return rc;
+    return on_device(h, [&] {
+      RoundArgs<kMaxRows> a;
+      memset((void*)&a, 0, sizeof(a));
+      for (uint32_t i = 0; i < R; ++i) {
+        put(&a.row[i], 0, x_src[i]);
+        put(&a.row[i], 1, x_dst[i]);
+        put(&a.row[i], 2, copy[i]);
+        put(&a.row[i], 3, sum[i]);
+      }
+      fill_span(h, &a.s);
+      a.lists = lists_of(h->slots[slot]);
+      a.gamma = gamma;
+      return launch_round((int)h->cfg.param_dtype, a, hip_stream);
+    });
+  });
+}
+
+}  // extern "C"

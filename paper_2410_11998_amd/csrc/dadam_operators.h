@@ -1,0 +1,101 @@
+// Internal interface between the host side of the operators around the step (dadam_operators.cpp: gradient norms and
+// clipping, microscaled 4-bit messages) and their kernels (dadam_norm.hip, dadam_mx4.hip).
+#ifndef DADAM_OPERATORS_H_
+#define DADAM_OPERATORS_H_
+
+#include <stdint.h>
+
+#include "dadam_internal.h"
+
+namespace dadam {
+
+constexpr uint32_t kMxBlock = DADAM_MX4_BLOCK;  // elements that share one power of two
+constexpr uint32_t kGranule = 512;              // elements a wavefront takes at a time: two groups of four a lane
+constexpr uint32_t kGranuleBlocks = kGranule / kMxBlock;
+
+// Up to four buffers of one row.  With 160 rows four plain addresses each would not fit the 4 KB of kernel arguments: these
+// are 16-byte aligned and below 2^52 (the host checks both), so 32 low and 16 high bits of address / 16 name them.
+struct RowPointers {
+  uint32_t low[4], high[2];
+};
+struct ColPointer {
+  uint32_t low, high;
+};
+
+// Which elements of a granule belong to a tensor.  index[granule]: 0 all of them, else 1 + where its kGranuleBlocks words of 32
+// bits stand in masks.  index == nullptr: every granule is whole.
+struct Cuts {
+  const uint32_t* index;
+  const uint32_t* masks;
+};
+
+// Neighbour lists of a slot (device).
+struct Lists {
+  const int32_t* row_ptr;
+  const int32_t* col;
+  const float* w;
+};
+
+// What all these launches have in common.  Granules [first, first + count) of rows [row0, row0 + n_rows).
+struct Span {
+  Cuts cuts;
+  uint64_t d;
+  uint32_t n_granules;        // of the whole vector
+  uint32_t first, count;
+  uint32_t row0, n_rows;
+  uint32_t n_xcd;
+  uint32_t streams;           // accesses carry the non-temporal hint
+};
+
+constexpr int kFewOperands = 16;  // rows and sources of the short argument block (see kFewRows)
+constexpr int kMessageRows = 96;  // rows of one launch that also carries the addresses of kMaxRows messages
+
+template <int N>
+struct NormArgs {
+  RowPointers row[N];  // 0 gradient, 1 scaled gradient
+  Span s;
+  double* partials;    // [row][per_row]
+  uint32_t* arrived;   // [row], zero between launches
+  float* norms;        // [row]
+  uint32_t per_row;    // workgroups that share a row
+  float max_norm;
+};
+
+template <int N>
+struct EncodeArgs {
+  RowPointers row[N];  // 0 x, 1 copy before (may be null), 2 copy behind (may be null), 3 message
+  Span s;
+  uint64_t scale_offset;
+};
+
+template <int N, int C>
+struct MixArgs {
+  RowPointers row[N];  // 0 sum or output, 1 copy, 2 x, 3 x behind
+  ColPointer message[C];
+  Span s;
+  Lists lists;
+  uint64_t scale_offset;
+  float gamma;
+};
+
+template <int N>
+struct RoundArgs {
+  RowPointers row[N];  // 0 x, 1 x behind, 2 copy, 3 sum
+  Span s;
+  Lists lists;
+  float gamma;
+};
+
+enum MixMode : int { kMixStore = 0, kMixAdd = 1, kMixGossip = 2 };
+
+// Launchers: enqueue on `stream`, return the hipError_t of the launch as int.  The large block is given; launches of few rows
+// and sources send the short one.
+int launch_norm(int gdt, const NormArgs<kMaxRows>& a, void* stream);
+int launch_clip(int gdt, const NormArgs<kMaxRows>& a, void* stream);
+int launch_encode(int xdt, const EncodeArgs<kMaxRows>& a, void* stream);
+int launch_mix4(int xdt, MixMode mode, uint32_t n_cols, const MixArgs<kMessageRows, kMaxRows>& a, void* stream);
+int launch_round(int xdt, const RoundArgs<kMaxRows>& a, void* stream);
+
+}  // namespace dadam
+
+#endif  // DADAM_OPERATORS_H_
