@@ -466,7 +466,8 @@ int dadam_mx4_encode(dadam_handle* h, const void* const* x, const float* const* 
                      void* const* msg, void* hip_stream);
 
 /* out[i] = sum_k w[k] * value(msg[col[k]]) over row i of the slot's neighbour list, or out[i] += that with DADAM_MX4_ADD: the rows of W
- * times vectors held in 4 bits.  msg has n_cols entries; those that no row lists are not read.  float32 sums in the order the row lists.
+ * times vectors held in 4 bits.  msg has n_cols entries; those that no row lists are not read.  float32 sums in the order the row lists;
+ * rows that list the same sources with the same weights share one sum, in order of the sources.
  * The identity matrix decodes. */
 #define DADAM_MX4_ADD 1u
 int dadam_mx4_product(dadam_handle* h, uint32_t slot, const void* const* msg, float* const* out, uint32_t flags,

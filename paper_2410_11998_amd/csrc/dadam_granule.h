@@ -32,10 +32,34 @@ __device__ __forceinline__ uint32_t cut_of(const Cuts& c, uint32_t granule) {
   typedef const uint32_t __attribute__((address_space(4))) * Constant;
   return c.index ? ((Constant)c.index)[granule] : 0u;
 }
-// Bits 0 to 3: which elements of a lane's group `half` belong to a tensor.
-__device__ __forceinline__ uint32_t group_bits(const Cuts& c, uint32_t cut, uint32_t half, uint32_t lane) {
-  if (cut == 0) return 0xFu;
-  return (c.masks[cut - 1 + half * (kGranuleBlocks / 2) + lane / 8] >> (4 * (lane % 8))) & 0xFu;
+// Bits 0 to 3: which elements of the group of four from e on (a multiple of 4) belong to a tensor.
+__device__ __forceinline__ uint32_t group_bits(const Cuts& c, uint64_t e) {
+  const uint32_t cut = c.index ? c.index[e / kGranule] : 0u;
+  return cut == 0 ? 0xFu : (c.masks[cut - 1 + e % kGranule / kMxBlock] >> (e % kMxBlock)) & 0xFu;
+}
+
+// Where a wavefront's unit of 512 elements (V = 2) or 256 (V = 1) lies: lane l holds V groups of four from `first` on, `step` apart; eight
+// lanes side by side hold a block of 32 elements.  In order: one run.  SPREAD: as streaming kernels have it (see lane_start, V vectors a
+// lane), the two halves of the wavefront work 8192 V elements apart, in blocks of twice that many elements that lie inside the vector.
+struct Unit {
+  uint64_t first;
+  uint32_t step;
+  bool whole;  // no padding in it
+};
+template <int V>
+constexpr uint32_t kUnitElems = 256 * V;
+template <int V, bool SPREAD>
+__device__ __forceinline__ Unit unit_place(uint32_t i, const Span& s, uint32_t lane) {
+  constexpr uint32_t kFar = 8192 * V, kUnits = 2 * kFar / kUnitElems<V>;
+  const uint64_t block = (uint64_t)(i & ~(kUnits - 1)) * kUnitElems<V>;
+  if (SPREAD && block + 2 * kFar <= s.d) {
+    const uint32_t at = (i % kUnits) * (kUnitElems<V> / 2);
+    const uint32_t granule = (uint32_t)((block + at) / kGranule);
+    const uint32_t near = V == 2 ? 4 * (lane & 15) + 8 * (lane & 16) : 4 * (lane & 31);
+    return {block + at + near + (lane >> 5) * kFar, 64, (cut_of(s.cuts, granule) | cut_of(s.cuts, granule + kFar / kGranule)) == 0};
+  }
+  const uint64_t first = (uint64_t)i * kUnitElems<V>;
+  return {first + 4 * lane, 256, cut_of(s.cuts, (uint32_t)(first / kGranule)) == 0};
 }
 
 // A lane's group of four elements from e on (a multiple of 4), widened to float; elements that `bits` leaves out are not touched

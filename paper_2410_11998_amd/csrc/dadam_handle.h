@@ -38,6 +38,11 @@ struct Slot {
   const int32_t *d_loop_col = nullptr, *d_loop_rows = nullptr;                              // loop kernel
   const float* d_loop_w = nullptr;
   const Loop* d_loops = nullptr;
+  std::vector<MixRow> mix_rows;       // see MixRow
+  std::vector<MixEntry> mix_entries;
+  bool mix_shared = false;            // some row shares its entries
+  const MixRow* d_mix_rows = nullptr;
+  const MixEntry* d_mix_entries = nullptr;
 };
 
 struct DeviceGuard {

@@ -60,6 +60,17 @@ struct Loop {
   int32_t first_entry, n_entries;  // in StepArgs::col / w
   int32_t first_row, n_rows;       // in StepArgs::row_order
 };
+// How the products with 4-bit messages walk a slot: its rows in an order in which rows that list the same sources with the same
+// weights follow each other (`same`: as the one before).  Their entries are filled up to a multiple of kMixAtOnce with the last one's
+// source and weight 0; rows that share them have them in order of the sources, the others as listed.
+struct MixRow {
+  int32_t row, first_entry, n_entries, same;
+};
+struct MixEntry {
+  int32_t col;
+  float w;
+};
+constexpr int kMixAtOnce = 4;
 constexpr int kMaxLoopWaves = 16;  // wavefronts of a loop kernel's workgroup
 
 // Pointer tables of the bound buffers of a handle with more than kInlineRows rows or sources: they do not

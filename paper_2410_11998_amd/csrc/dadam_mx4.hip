@@ -23,17 +23,14 @@ __device__ __forceinline__ uint32_t block_max(uint32_t m) {
   return m;
 }
 
-// The power of two that byte b of a message stands for: 2^(b - 127), NaN for 255.
-__device__ __forceinline__ float power_of(uint32_t b) {
-  return __uint_as_float(b == 0 ? 0x00400000u : b == 255 ? 0x7FC00000u : b << 23);
-}
-
-// The four values of 16 bits of codes, without their power of two.
-__device__ __forceinline__ void decode(uint32_t codes, float (&q)[4]) {
+// The four values of 16 bits of codes in a block of scale byte b.  The conversion takes the exponent of its scale operand as such a byte:
+// 2^(b - 127), 0 included, and NaN for 255.
+__device__ __forceinline__ void decode(uint32_t codes, uint32_t b, float (&value)[4]) {
   typedef float f2 __attribute__((ext_vector_type(2)));
-  const f2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 0);
-  const f2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 1);
-  q[0] = a.x; q[1] = a.y; q[2] = b.x; q[3] = b.y;
+  const float scale = __uint_as_float(b << 23);
+  const f2 x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0);
+  const f2 y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1);
+  value[0] = x.x; value[1] = x.y; value[2] = y.x; value[3] = y.y;
 }
 
 // A lane's group u of a block (padding: zeros) as 16 bits of codes, the block's scale byte, and the values these stand for.
@@ -47,167 +44,257 @@ __device__ __forceinline__ void encode(const float (&u)[4], uint32_t& codes, uin
   const uint32_t exponent = block_max(m) >> 23;  // floor(log2) + 127; 0: below 2^-126
   const bool finite = exponent != 255;
   scale = !finite ? 255u : exponent > 3 ? exponent - 2 : 1u;
-  const float power = power_of(scale);
+  const float power = __uint_as_float(scale << 23);
   codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, u[0], u[1], power, 0);
   codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, u[2], u[3], power, 1) & 0xFFFFu;
   if (!finite) codes = 0;
-  decode(codes, value);
-#pragma unroll
-  for (int j = 0; j < 4; ++j) value[j] *= power;
+  decode(codes, scale, value);
 }
 
-template <typename XT, int N>
-__global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_encode(const EncodeArgs<N> a) {
-  const uint32_t lane = threadIdx.x % kWave, wave = wave_of_group();
-  const uint32_t row = a.s.row0 + blockIdx.x % a.s.n_rows, i = a.s.first + blockIdx.x / a.s.n_rows * kMixWaves + wave;
-  if (i < a.s.n_granules) {
-    const RowPointers p = a.row[row];
-    const void* x = buffer<const void, 0>(p);
-    const void* before = buffer<const void, 1>(p);
-    void* behind = buffer<void, 2>(p);
-    uint8_t* message = buffer<uint8_t, 3>(p);
-    const uint32_t cut = cut_of(a.s.cuts, i);
+template <typename XT, bool WHOLE, bool NT>
+__device__ __forceinline__ void encode_unit(const Cuts& cuts, const Unit& t, const RowPointers& p, uint64_t scale_offset) {
+  const void* x = buffer<const void, 0>(p);
+  const void* before = buffer<const void, 1>(p);
+  void* behind = buffer<void, 2>(p);
+  uint8_t* message = buffer<uint8_t, 3>(p);
+  float u[2][4], copy[2][4] = {};
+  uint32_t bits[2];
 #pragma unroll
-    for (uint32_t half = 0; half < 2; ++half) {
-      const uint64_t e = (uint64_t)i * kGranule + half * 256 + 4 * lane;
-      const uint32_t bits = group_bits(a.s.cuts, cut, half, lane);
-      float u[4], copy[4] = {0.f, 0.f, 0.f, 0.f}, value[4];
-      load_group<XT, false>(x, e, bits, u);
+  for (uint32_t k = 0; k < 2; ++k) {
+    bits[k] = WHOLE ? 0xFu : group_bits(cuts, t.first + k * t.step);
+    load_group<XT, NT>(x, t.first + k * t.step, bits[k], u[k]);
+  }
+  if (before) {
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k) load_group<TF32, NT>(before, t.first + k * t.step, bits[k], copy[k]);
+  }
+#pragma unroll
+  for (uint32_t k = 0; k < 2; ++k) {
+    const uint64_t e = t.first + k * t.step;
+    if (before) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) u[k][j] -= copy[k][j];
+    }
+    uint32_t codes, scale;
+    float value[4];
+    encode(u[k], codes, scale, value);
+    if (WHOLE || e / 2 < scale_offset) {  // blocks end behind the vector where d is no multiple of 32, granules behind the blocks
+      *reinterpret_cast<uint16_t*>(message + e / 2) = (uint16_t)codes;
+      if (threadIdx.x % 8 == 0) message[scale_offset + e / kMxBlock] = (uint8_t)scale;
+    }
+    if (behind) {
       if (before) {
-        load_group<TF32, false>(before, e, bits, copy);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) u[j] -= copy[j];
+        for (int j = 0; j < 4; ++j) value[j] = copy[k][j] + value[j];
       }
-      uint32_t codes, scale;
-      encode(u, codes, scale, value);
-      if (e / 2 < a.scale_offset) {  // blocks end behind the vector where d is no multiple of 32, granules behind the blocks
-        *reinterpret_cast<uint16_t*>(message + e / 2) = (uint16_t)codes;
-        if (lane % 8 == 0) message[a.scale_offset + e / kMxBlock] = (uint8_t)scale;
-      }
-      if (behind) {
-        if (before) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) value[j] = copy[j] + value[j];
-        }
-        store_group<TF32, false>(behind, e, bits, value);
-      }
+      store_group<TF32, NT>(behind, e, bits[k], value);
     }
   }
 }
 
-template <typename XT, int MODE, int N, int C>
-__global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_mix(const MixArgs<N, C> a) {
-  const uint32_t lane = threadIdx.x % kWave, wave = wave_of_group();
-  const uint32_t row = blockIdx.x % a.s.n_rows, i = a.s.first + blockIdx.x / a.s.n_rows * kMixWaves + wave;
+template <typename XT, bool NT, int N>
+__global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_encode(const EncodeArgs<N> a) {
+  const uint32_t lane = threadIdx.x % kWave;
+  const uint32_t row = blockIdx.x % a.s.n_rows, i = a.s.first + blockIdx.x / a.s.n_rows * kMixWaves + wave_of_group();
   if (i < a.s.n_granules) {
-    const RowPointers p = a.row[row];
-    void* sum = buffer<void, 0>(p);
-    const void* copy = buffer<const void, 1>(p);
-    const void* x = buffer<const void, 2>(p);
-    void* behind = buffer<void, 3>(p);
-    const uint32_t cut = cut_of(a.s.cuts, i);
-    const uint64_t e0 = (uint64_t)i * kGranule + 4 * lane;
-    const uint32_t bits[2] = {group_bits(a.s.cuts, cut, 0, lane), group_bits(a.s.cuts, cut, 1, lane)};
-    float mixed[2][4] = {};
-    const int32_t first = a.lists.row_ptr[a.s.row0 + row], end = a.lists.row_ptr[a.s.row0 + row + 1];
-    for (int32_t k = first; k < end; ++k) {
-      const uint8_t* message = buffer(a.message[a.lists.col[k]]);
-      const float w = a.lists.w[k];
+    const Unit t = unit_place<2, NT>(i, a.s, lane);
+    if (t.whole) encode_unit<XT, true, NT>(a.s.cuts, t, a.row[row], a.scale_offset);
+    else encode_unit<XT, false, NT>(a.s.cuts, t, a.row[row], a.scale_offset);
+  }
+}
+
+__device__ __forceinline__ MixRow mix_row(const Lists& l, uint32_t position) {
+  typedef const MixRow __attribute__((address_space(4))) * Constant;
+  return *reinterpret_cast<const MixRow*>((const MixRow*)((Constant)l.rows + position));
+}
+__device__ __forceinline__ MixEntry mix_entry(const Lists& l, uint32_t at) {
+  typedef const MixEntry __attribute__((address_space(4))) * Constant;
+  return *reinterpret_cast<const MixEntry*>((const MixEntry*)((Constant)l.entries + at));
+}
+
+// The messages of a list times their weights, for a unit's two groups a lane.
+template <bool WHOLE, typename A>
+__device__ __forceinline__ void mix_unit(const A& a, const MixRow& r, const Unit& t, const uint32_t (&bits)[2], float (&mixed)[2][4]) {
+  uint64_t e[2];
 #pragma unroll
-      for (uint32_t half = 0; half < 2; ++half) {
-        const uint64_t e = e0 + half * 256;
-        if (bits[half] != 0) {
-          float q[4];
-          decode(*reinterpret_cast<const uint16_t*>(message + e / 2), q);
-          const float weight = w * power_of(message[a.scale_offset + e / kMxBlock]);
+  for (uint32_t k = 0; k < 2; ++k) {
+    // groups without an element may lie behind the message: their lanes look at its beginning instead
+    e[k] = WHOLE || bits[k] != 0 ? t.first + k * t.step : 0;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) mixed[half][j] = __builtin_fmaf(weight, q[j], mixed[half][j]);
-        }
+    for (int j = 0; j < 4; ++j) mixed[k][j] = 0.0f;
+  }
+  for (int32_t n = 0; n < r.n_entries; n += kMixAtOnce) {
+    uint32_t codes[kMixAtOnce][2], scale[kMixAtOnce][2];
+    float w[kMixAtOnce];
+#pragma unroll
+    for (int q = 0; q < kMixAtOnce; ++q) {
+      const MixEntry entry = mix_entry(a.lists, (uint32_t)(r.first_entry + n + q));
+      const uint8_t* message = buffer(a.message[entry.col]);
+      w[q] = entry.w;
+#pragma unroll
+      for (uint32_t k = 0; k < 2; ++k) {
+        codes[q][k] = *reinterpret_cast<const uint16_t*>(message + e[k] / 2);
+        scale[q][k] = message[a.scale_offset + e[k] / kMxBlock];
       }
     }
 #pragma unroll
-    for (uint32_t half = 0; half < 2; ++half) {
-      const uint64_t e = e0 + half * 256;
-      if constexpr (MODE != kMixStore) {
-        float s[4];
-        load_group<TF32, false>(sum, e, bits[half], s);
+    for (int q = 0; q < kMixAtOnce; ++q)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) mixed[half][j] = s[j] + mixed[half][j];
+      for (uint32_t k = 0; k < 2; ++k) {
+        float value[4];
+        decode(codes[q][k], scale[q][k], value);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mixed[k][j] = __builtin_fmaf(w[q], value[j], mixed[k][j]);
       }
+  }
+}
+
+template <typename XT, int MODE, bool WHOLE, bool NT, typename A>
+__device__ __forceinline__ void mix_positions(const A& a, const Unit& t, uint32_t from, uint32_t to) {
+  uint32_t bits[2];
+#pragma unroll
+  for (uint32_t k = 0; k < 2; ++k) bits[k] = WHOLE ? 0xFu : group_bits(a.s.cuts, t.first + k * t.step);
+  float mixed[2][4];
+  for (uint32_t p = from; p < to; ++p) {
+    const RowPointers rp = a.row[p];
+    void* sum = buffer<void, 0>(rp);
+    float s[2][4], c[2][4], x[2][4];
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k) {
+      const uint64_t e = t.first + k * t.step;
+      if constexpr (MODE != kMixStore) load_group<TF32, NT>(sum, e, bits[k], s[k]);
       if constexpr (MODE == kMixGossip) {
-        float c[4], v[4];
-        load_group<TF32, false>(copy, e, bits[half], c);
-        load_group<XT, false>(x, e, bits[half], v);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = __builtin_fmaf(a.gamma, mixed[half][j] - c[j], v[j]);
-        store_group<XT, false>(behind, e, bits[half], v);
+        load_group<TF32, NT>(buffer<const void, 1>(rp), e, bits[k], c[k]);
+        load_group<XT, NT>(buffer<const void, 2>(rp), e, bits[k], x[k]);
       }
-      store_group<TF32, false>(sum, e, bits[half], mixed[half]);
+    }
+    const MixRow r = mix_row(a.lists, p);
+    if (p == from || !r.same) mix_unit<WHOLE>(a, r, t, bits, mixed);
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k) {
+      const uint64_t e = t.first + k * t.step;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        s[k][j] = MODE == kMixStore ? mixed[k][j] : s[k][j] + mixed[k][j];
+        if constexpr (MODE == kMixGossip) x[k][j] = __builtin_fmaf(a.gamma, s[k][j] - c[k][j], x[k][j]);
+      }
+      store_group<TF32, NT>(sum, e, bits[k], s[k]);
+      if constexpr (MODE == kMixGossip) store_group<XT, NT>(buffer<void, 3>(rp), e, bits[k], x[k]);
     }
   }
 }
 
-// One workgroup takes 256 elements of all rows: its wavefronts deal the rows among themselves, park their messages in LDS,
-// and after one barrier take the neighbours' from there.  What a row holds in registers until then is its x, its copy and its sum.
-constexpr uint32_t kRoundElems = kWave * 4, kRoundMessage = kRoundElems / 2 + kRoundElems / kMxBlock;
+// A wavefront takes a unit of `rows_each` positions.  All of them for one unit run on one die, whose L2 then holds the unit's messages.
+template <typename XT, int MODE, bool NT, int N, int C>
+__global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_mix(const MixArgs<N, C> a) {
+  const uint32_t parts = (a.s.n_rows + a.rows_each - 1) / a.rows_each;
+  uint32_t piece, part;
+  const bool active = die_block_piece(blockIdx.x, parts, a.s.n_xcd, (a.s.count + kMixWaves - 1) / kMixWaves, kDieBlockTiles, piece, part);
+  const uint32_t i = a.s.first + piece * kMixWaves + wave_of_group();
+  if (active && i < a.s.n_granules) {
+    const uint32_t from = part * a.rows_each, to = from + a.rows_each < a.s.n_rows ? from + a.rows_each : a.s.n_rows;
+    const Unit t = unit_place<2, NT>(i, a.s, threadIdx.x % kWave);
+    if (t.whole) mix_positions<XT, MODE, true, NT>(a, t, from, to);
+    else mix_positions<XT, MODE, false, NT>(a, t, from, to);
+  }
+}
+
+// One workgroup takes a unit of all rows: its wavefronts deal the rows among themselves, park their messages in LDS,
+// and after one barrier take the neighbours' from there.  What a row holds in registers until then is its x and its copy.
+template <int V>
+constexpr uint32_t kRoundMessage = kUnitElems<V> / 2 + kUnitElems<V> / kMxBlock;  // bytes of a row's message of a unit, by lane
 constexpr uint32_t kRoundWaves = 16;
-template <typename XT, int ROWS, int N>
-__global__ __launch_bounds__(kWave * kRoundWaves) void k_mx4_round(const RoundArgs<N> a) {
-  extern __shared__ uint8_t lds[];  // of every row: 128 bytes of codes, 8 of scales
-  const uint32_t lane = threadIdx.x % kWave, wave = wave_of_group(), waves = blockDim.x / kWave;
-  const uint32_t tile = a.s.first * 2 + blockIdx.x;  // first, count and n_granules count granules, which are two tiles
-  const uint64_t e = (uint64_t)tile * kRoundElems + 4 * lane;
-  const uint32_t bits = group_bits(a.s.cuts, cut_of(a.s.cuts, tile / 2), tile % 2, lane);
-  float x[ROWS][4], copy[ROWS][4];
+
+template <typename XT, int ROWS, int V, bool WHOLE, bool NT, typename A>
+__device__ __forceinline__ void round_unit(const A& a, const Unit& t, uint32_t each, uint8_t* lds) {
+  const uint32_t lane = threadIdx.x % kWave, from = wave_of_group() * each;
+  uint32_t bits[V];
 #pragma unroll
-  for (int k = 0; k < ROWS; ++k) {
-    const uint32_t row = wave + k * waves;
-    if (row < a.s.n_rows) {
-      load_group<XT, false>(buffer<const void, 0>(a.row[row]), e, bits, x[k]);
-      load_group<TF32, false>(buffer<const void, 2>(a.row[row]), e, bits, copy[k]);
+  for (uint32_t k = 0; k < V; ++k) bits[k] = WHOLE ? 0xFu : group_bits(a.s.cuts, t.first + k * t.step);
+  float x[ROWS][V][4], copy[ROWS][V][4];
+#pragma unroll
+  for (uint32_t q = 0; q < ROWS; ++q) {
+    const uint32_t p = from + q;
+    if (q < each && p < a.s.n_rows) {
+#pragma unroll
+      for (uint32_t k = 0; k < V; ++k) {
+        load_group<XT, NT>(buffer<const void, 0>(a.row[p]), t.first + k * t.step, bits[k], x[q][k]);
+        load_group<TF32, NT>(buffer<const void, 2>(a.row[p]), t.first + k * t.step, bits[k], copy[q][k]);
+      }
     }
   }
 #pragma unroll
-  for (int k = 0; k < ROWS; ++k) {
-    const uint32_t row = wave + k * waves;
-    if (row < a.s.n_rows) {
-      float u[4], value[4];
-      uint32_t codes, scale;
+  for (uint32_t q = 0; q < ROWS; ++q) {
+    const uint32_t p = from + q;
+    if (q < each && p < a.s.n_rows) {
+      uint8_t* message = lds + mix_row(a.lists, p).row * kRoundMessage<V>;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) u[j] = x[k][j] - copy[k][j];
-      encode(u, codes, scale, value);
+      for (uint32_t k = 0; k < V; ++k) {
+        float u[4], value[4];
+        uint32_t codes, scale;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) copy[k][j] = copy[k][j] + value[j];
-      store_group<TF32, false>(buffer<void, 2>(a.row[row]), e, bits, copy[k]);
-      *reinterpret_cast<uint16_t*>(lds + row * kRoundMessage + 2 * lane) = (uint16_t)codes;
-      if (lane % 8 == 0) lds[row * kRoundMessage + kRoundElems / 2 + lane / 8] = (uint8_t)scale;
+        for (int j = 0; j < 4; ++j) u[j] = x[q][k][j] - copy[q][k][j];
+        encode(u, codes, scale, value);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) copy[q][k][j] = copy[q][k][j] + value[j];
+        store_group<TF32, NT>(buffer<void, 2>(a.row[p]), t.first + k * t.step, bits[k], copy[q][k]);
+        *reinterpret_cast<uint16_t*>(message + k * 128 + 2 * lane) = (uint16_t)codes;
+        if (lane % 8 == 0) message[128 * V + k * 8 + lane / 8] = (uint8_t)scale;
+      }
     }
   }
   __syncthreads();
+  float mixed[V][4];
 #pragma unroll
-  for (int k = 0; k < ROWS; ++k) {
-    const uint32_t row = wave + k * waves;
-    if (row < a.s.n_rows) {
-      float sum[4], mixed[4] = {};
-      load_group<TF32, false>(buffer<const void, 3>(a.row[row]), e, bits, sum);
-      const int32_t first = a.lists.row_ptr[row], end = a.lists.row_ptr[row + 1];
-      for (int32_t n = first; n < end; ++n) {
-        const uint8_t* message = lds + a.lists.col[n] * kRoundMessage;
-        float q[4];
-        decode(*reinterpret_cast<const uint16_t*>(message + 2 * lane), q);
-        const float weight = a.lists.w[n] * power_of(message[kRoundElems / 2 + lane / 8]);
+  for (uint32_t q = 0; q < ROWS; ++q) {
+    const uint32_t p = from + q;
+    if (q < each && p < a.s.n_rows) {
+      float s[V][4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) mixed[j] = __builtin_fmaf(weight, q[j], mixed[j]);
+      for (uint32_t k = 0; k < V; ++k) load_group<TF32, NT>(buffer<const void, 3>(a.row[p]), t.first + k * t.step, bits[k], s[k]);
+      const MixRow r = mix_row(a.lists, p);
+      if (q == 0 || !r.same) {
+#pragma unroll
+        for (uint32_t k = 0; k < V; ++k)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) mixed[k][j] = 0.0f;
+        for (int32_t n = 0; n < r.n_entries; n += kMixAtOnce) {
+#pragma unroll
+          for (int m = 0; m < kMixAtOnce; ++m) {
+            const MixEntry entry = mix_entry(a.lists, (uint32_t)(r.first_entry + n + m));
+            const uint8_t* message = lds + entry.col * kRoundMessage<V>;
+#pragma unroll
+            for (uint32_t k = 0; k < V; ++k) {
+              float value[4];
+              decode(*reinterpret_cast<const uint16_t*>(message + k * 128 + 2 * lane), message[128 * V + k * 8 + lane / 8], value);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) mixed[k][j] = __builtin_fmaf(entry.w, value[j], mixed[k][j]);
+            }
+          }
+        }
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        sum[j] = sum[j] + mixed[j];
-        x[k][j] = __builtin_fmaf(a.gamma, sum[j] - copy[k][j], x[k][j]);
+      for (uint32_t k = 0; k < V; ++k) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          s[k][j] = s[k][j] + mixed[k][j];
+          x[q][k][j] = __builtin_fmaf(a.gamma, s[k][j] - copy[q][k][j], x[q][k][j]);
+        }
+        store_group<TF32, NT>(buffer<void, 3>(a.row[p]), t.first + k * t.step, bits[k], s[k]);
+        store_group<XT, NT>(buffer<void, 1>(a.row[p]), t.first + k * t.step, bits[k], x[q][k]);
       }
-      store_group<TF32, false>(buffer<void, 3>(a.row[row]), e, bits, sum);
-      store_group<XT, false>(buffer<void, 1>(a.row[row]), e, bits, x[k]);
     }
   }
+}
+
+template <typename XT, int ROWS, int V, bool NT, int N>
+__global__ __launch_bounds__(kWave * kRoundWaves) void k_mx4_round(const RoundArgs<N> a) {
+  extern __shared__ uint8_t lds[];  // of every row: the codes of a unit, then its scales
+  const uint32_t waves = blockDim.x / kWave, each = (a.s.n_rows + waves - 1) / waves;
+  const uint32_t i = a.s.first * (kGranule / kUnitElems<V>) + die_block_order(blockIdx.x, gridDim.x, a.s.n_xcd, kDieBlockTiles);
+  const Unit t = unit_place<V, NT>(i, a.s, threadIdx.x % kWave);
+  if (t.whole) round_unit<XT, ROWS, V, true, NT>(a, t, each, lds);
+  else round_unit<XT, ROWS, V, false, NT>(a, t, each, lds);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -215,45 +302,48 @@ __global__ __launch_bounds__(kWave * kRoundWaves) void k_mx4_round(const RoundAr
 // ---------------------------------------------------------------------------------------------
 template <int N>
 int enqueue_encode(int xdt, EncodeArgs<N> a, void* stream) {
-  const KernelFn fn = xdt == DADAM_BF16 ? (KernelFn)k_mx4_encode<TBF16, N> : (KernelFn)k_mx4_encode<TF32, N>;
+  const bool nt = a.s.streams;
+  const KernelFn fn = xdt == DADAM_BF16 ? (nt ? (KernelFn)k_mx4_encode<TBF16, true, N> : (KernelFn)k_mx4_encode<TBF16, false, N>)
+                                        : (nt ? (KernelFn)k_mx4_encode<TF32, true, N> : (KernelFn)k_mx4_encode<TF32, false, N>);
   return in_pieces(a, kMixWaves, a.s.n_rows, kWave * kMixWaves, [&](uint32_t grid) { return enqueue_grid(fn, grid, kWave * kMixWaves, &a, 0, stream); });
 }
 
-template <int N, int C>
+template <int N, int C, bool NT>
 KernelFn mix_kernel(int xdt, MixMode mode) {
-  if (mode == kMixStore) return (KernelFn)k_mx4_mix<TF32, kMixStore, N, C>;
-  if (mode == kMixAdd) return (KernelFn)k_mx4_mix<TF32, kMixAdd, N, C>;
-  return xdt == DADAM_BF16 ? (KernelFn)k_mx4_mix<TBF16, kMixGossip, N, C> : (KernelFn)k_mx4_mix<TF32, kMixGossip, N, C>;
+  if (mode == kMixStore) return (KernelFn)k_mx4_mix<TF32, kMixStore, NT, N, C>;
+  if (mode == kMixAdd) return (KernelFn)k_mx4_mix<TF32, kMixAdd, NT, N, C>;
+  return xdt == DADAM_BF16 ? (KernelFn)k_mx4_mix<TBF16, kMixGossip, NT, N, C> : (KernelFn)k_mx4_mix<TF32, kMixGossip, NT, N, C>;
 }
 template <int N, int C>
 int enqueue_mix(int xdt, MixMode mode, MixArgs<N, C> a, void* stream) {
-  const KernelFn fn = mix_kernel<N, C>(xdt, mode);
-  return in_pieces(a, kMixWaves, a.s.n_rows, kWave * kMixWaves, [&](uint32_t grid) { return enqueue_grid(fn, grid, kWave * kMixWaves, &a, 0, stream); });
+  const KernelFn fn = a.s.streams ? mix_kernel<N, C, true>(xdt, mode) : mix_kernel<N, C, false>(xdt, mode);
+  const uint32_t parts = (a.s.n_rows + a.rows_each - 1) / a.rows_each;
+  return in_pieces(a, kMixWaves * a.s.n_xcd, parts * a.s.n_xcd, kWave * kMixWaves,
+                   [&](uint32_t grid) { return enqueue_grid(fn, grid, kWave * kMixWaves, &a, 0, stream); });
 }
 
-template <int N>
+// Rows a wavefront holds, and its groups a lane: what 128 registers have room for.
+template <int N, bool NT>
 KernelFn round_kernel(int xdt, uint32_t rows_per_wave) {
   const bool b = xdt == DADAM_BF16;
-#define DADAM_ROUND(ROWS) (b ? (KernelFn)k_mx4_round<TBF16, ROWS, N> : (KernelFn)k_mx4_round<TF32, ROWS, N>)
-  if (rows_per_wave <= 1) return DADAM_ROUND(1);
+#define DADAM_ROUND(ROWS, V) (b ? (KernelFn)k_mx4_round<TBF16, ROWS, V, NT, N> : (KernelFn)k_mx4_round<TF32, ROWS, V, NT, N>)
+  if (rows_per_wave <= 1) return DADAM_ROUND(1, 2);
   if constexpr (N > kFewOperands) {
-    if (rows_per_wave <= 2) return DADAM_ROUND(2);
-    if (rows_per_wave <= 4) return DADAM_ROUND(4);
-    return DADAM_ROUND(10);
+    if (rows_per_wave <= 2) return DADAM_ROUND(2, 2);
+    if (rows_per_wave <= 4) return DADAM_ROUND(4, 2);
+    return DADAM_ROUND(10, 1);
   }
 #undef DADAM_ROUND
   return nullptr;
 }
 template <int N>
 int enqueue_round(int xdt, RoundArgs<N> a, void* stream) {
-  const uint32_t waves = a.s.n_rows < kRoundWaves ? a.s.n_rows : kRoundWaves;
-  const KernelFn fn = round_kernel<N>(xdt, (a.s.n_rows + waves - 1) / waves);
+  const uint32_t waves = a.s.n_rows < kRoundWaves ? a.s.n_rows : kRoundWaves, each = (a.s.n_rows + waves - 1) / waves;
+  const KernelFn fn = a.s.streams ? round_kernel<N, true>(xdt, each) : round_kernel<N, false>(xdt, each);
   if (fn == nullptr) return (int)hipErrorInvalidDeviceFunction;
-  const uint32_t last = (uint32_t)((a.s.d + kRoundElems - 1) / kRoundElems);  // the last granule may hold one tile only
-  return in_pieces(a, 1, 2, kWave * waves, [&](uint32_t grid) {
-    const uint32_t from = a.s.first * 2;
-    return enqueue_grid(fn, from + grid > last ? last - from : grid, kWave * waves, &a, a.s.n_rows * kRoundMessage, stream);
-  });
+  const uint32_t units = each <= 4 ? 1 : 2;  // of a granule
+  const uint32_t lds = a.s.n_rows * (units == 1 ? kRoundMessage<2> : kRoundMessage<1>);
+  return in_pieces(a, 1, units, kWave * waves, [&](uint32_t grid) { return enqueue_grid(fn, grid, kWave * waves, &a, lds, stream); });
 }
 
 }  // namespace
@@ -269,7 +359,7 @@ int launch_mix4(int xdt, MixMode mode, uint32_t n_cols, const MixArgs<kMessageRo
   if (a.s.n_rows > (uint32_t)kFewOperands || n_cols > (uint32_t)kFewOperands) return enqueue_mix(xdt, mode, a, stream);
   auto f = few_rows<MixArgs<kFewOperands, kFewOperands>>(a);
   memcpy((void*)f.message, (const void*)a.message, sizeof(f.message));
-  f.s = a.s; f.lists = a.lists; f.scale_offset = a.scale_offset; f.gamma = a.gamma;
+  f.s = a.s; f.lists = a.lists; f.scale_offset = a.scale_offset; f.rows_each = a.rows_each; f.gamma = a.gamma;
   return enqueue_mix(xdt, mode, f, stream);
 }
 

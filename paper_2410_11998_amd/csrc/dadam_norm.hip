@@ -61,7 +61,7 @@ __global__ __launch_bounds__(kNormThreads) void k_grad_norm(const NormArgs<N> a)
   __shared__ double partial[kNormWaves];
   __shared__ uint32_t last;
   const uint32_t lane = threadIdx.x % kWave, wave = wave_of_group();
-  const uint32_t row = a.s.row0 + blockIdx.x % a.s.n_rows, part = blockIdx.x / a.s.n_rows;
+  const uint32_t row = blockIdx.x % a.s.n_rows, part = blockIdx.x / a.s.n_rows;
   const void* g = buffer<const void, 0>(a.row[row]);
   const uint32_t stride = a.per_row * kNormWaves, n = a.s.n_granules;
   constexpr uint32_t kAtOnce = 8 / kWholeVectors<GT>;
@@ -82,12 +82,14 @@ __global__ __launch_bounds__(kNormThreads) void k_grad_norm(const NormArgs<N> a)
 #pragma unroll
       for (uint32_t k = 0; k < kAtOnce; ++k) add_squares<GT>(raw[k], sums);
     } else {
+#pragma unroll 1
       for (uint32_t k = 0; k < kAtOnce; ++k) {
         const uint64_t i = i0 + (uint64_t)k * stride;
-        const uint32_t cut = i < n ? cut_of(a.s.cuts, (uint32_t)i) : 0;
+#pragma unroll 1
         for (uint32_t half = 0; half < 2 && i < n; ++half) {
           float v[4];
-          load_group<GT, NT>(g, i * kGranule + half * 256 + 4 * lane, group_bits(a.s.cuts, cut, half, lane), v);
+          const uint64_t e = i * kGranule + half * 256 + 4 * lane;
+          load_group<GT, NT>(g, e, group_bits(a.s.cuts, e), v);
 #pragma unroll
           for (int j = 0; j < 4; ++j) sums[j & 1] = with_square(sums[j & 1], v[j]);
         }
@@ -113,27 +115,36 @@ __global__ __launch_bounds__(kNormThreads) void k_grad_norm(const NormArgs<N> a)
   }
 }
 
+template <typename GT, bool WHOLE, bool NT>
+__device__ __forceinline__ void clip_unit(const Cuts& cuts, const Unit& u, const void* g, void* out, float factor) {
+  float v[2][4];
+  uint32_t bits[2];
+#pragma unroll
+  for (uint32_t k = 0; k < 2; ++k) {
+    bits[k] = WHOLE ? 0xFu : group_bits(cuts, u.first + k * u.step);
+    load_group<GT, NT>(g, u.first + k * u.step, bits[k], v[k]);
+  }
+#pragma unroll
+  for (uint32_t k = 0; k < 2; ++k) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[k][j] *= factor;
+    store_group<GT, NT>(out, u.first + k * u.step, bits[k], v[k]);
+  }
+}
+
 template <typename GT, bool NT, int N>
 __global__ __launch_bounds__(kNormThreads) void k_clip(const NormArgs<N> a) {
   const uint32_t lane = threadIdx.x % kWave, wave = wave_of_group();
-  const uint32_t row = a.s.row0 + blockIdx.x % a.s.n_rows, i = a.s.first + blockIdx.x / a.s.n_rows * kNormWaves + wave;
+  const uint32_t row = blockIdx.x % a.s.n_rows, i = a.s.first + blockIdx.x / a.s.n_rows * kNormWaves + wave;
   const void* g = buffer<const void, 0>(a.row[row]);
   void* out = buffer<void, 1>(a.row[row]);
   const float norm = a.norms[row];
   const bool scales = !(norm <= a.max_norm);  // NaN scales too: everything becomes NaN
   if (i < a.s.n_granules && (scales || g != out)) {
     const float factor = scales ? a.max_norm / norm : 1.0f;
-    const uint32_t cut = cut_of(a.s.cuts, i);
-#pragma unroll
-    for (uint32_t half = 0; half < 2; ++half) {
-      const uint64_t e = (uint64_t)i * kGranule + half * 256 + 4 * lane;
-      const uint32_t bits = group_bits(a.s.cuts, cut, half, lane);
-      float v[4];
-      load_group<GT, NT>(g, e, bits, v);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] *= factor;
-      store_group<GT, NT>(out, e, bits, v);
-    }
+    const Unit u = unit_place<2, NT>(i, a.s, lane);
+    if (u.whole) clip_unit<GT, true, NT>(a.s.cuts, u, g, out, factor);
+    else clip_unit<GT, false, NT>(a.s.cuts, u, g, out, factor);
   }
 }
 
@@ -146,7 +157,7 @@ NormArgs<N> shortened(const NormArgs<kMaxRows>& a) {
 
 template <typename Fn>
 int with_block(const NormArgs<kMaxRows>& a, Fn fn) {
-  if (a.s.row0 + a.s.n_rows <= (uint32_t)kFewOperands) {
+  if (a.s.n_rows <= (uint32_t)kFewOperands) {
     NormArgs<kFewOperands> f = shortened<kFewOperands>(a);
     return fn(f);
   }

@@ -181,7 +181,6 @@ void fill_span(const dadam_handle* h, Span* s) {
   s->n_granules = (uint32_t)granules_of(h);
   s->first = 0;
   s->count = s->n_granules;
-  s->row0 = 0;
   s->n_rows = h->cfg.n_rows;
   s->n_xcd = h->n_xcds;
   s->streams = h->nontemporal;
@@ -190,7 +189,14 @@ void fill_span(const dadam_handle* h, Span* s) {
 uint64_t blocks_of(const dadam_handle* h) { return (h->cfg.d + kMxBlock - 1) / kMxBlock; }
 size_t message_bytes(const dadam_handle* h) { return (size_t)((blocks_of(h) * 17 + 15) / 16 * 16); }
 
-Lists lists_of(const Slot& s) { return {s.d_row_ptr, s.d_col, s.d_w}; }
+// Rows of one position after the other that a wavefront takes: rows that share a sum have it formed once for as many of them as leave
+// the chip two rounds of wavefronts.
+constexpr uint64_t kRoundOfWaves = 256 * 32;
+uint32_t rows_each(const dadam_handle* h, const Slot& s, uint32_t n_rows) {
+  if (!s.mix_shared) return 1;
+  const uint64_t parts = (2 * kRoundOfWaves + granules_of(h) - 1) / granules_of(h);  // of the rows, at least
+  return (uint32_t)std::max<uint64_t>(1, n_rows / std::min<uint64_t>(parts, n_rows));
+}
 
 // Runs the launches of a call whose arguments have passed, with the handle's device current and its state made.
 template <typename Launch>
@@ -253,22 +259,24 @@ int mix_impl(dadam_handle* h, uint32_t slot, const void* const* msg, float* cons
   if (rc) return rc;
   return on_device(h, [&] {
     int e = (int)hipSuccess;
-    for (uint32_t row0 = 0; row0 < R && e == (int)hipSuccess; row0 += kMessageRows) {
+    const Slot& lists = h->slots[slot];
+    for (uint32_t p0 = 0; p0 < R && e == (int)hipSuccess; p0 += kMessageRows) {
       MixArgs<kMessageRows, kMaxRows> a;
       memset((void*)&a, 0, sizeof(a));
       fill_span(h, &a.s);
-      a.s.row0 = row0;
-      a.s.n_rows = std::min<uint32_t>(kMessageRows, R - row0);
-      for (uint32_t i = 0; i < a.s.n_rows; ++i) {
-        put(&a.row[i], 0, sum[row0 + i]);
+      a.s.n_rows = std::min<uint32_t>(kMessageRows, R - p0);
+      for (uint32_t p = 0; p < a.s.n_rows; ++p) {
+        const int32_t i = lists.mix_rows[p0 + p].row;
+        put(&a.row[p], 0, sum[i]);
         if (mode != kMixGossip) continue;
-        put(&a.row[i], 1, copy[row0 + i]);
-        put(&a.row[i], 2, x_src[row0 + i]);
-        put(&a.row[i], 3, x_dst[row0 + i]);
+        put(&a.row[p], 1, copy[i]);
+        put(&a.row[p], 2, x_src[i]);
+        put(&a.row[p], 3, x_dst[i]);
       }
       for (uint32_t c = 0; c < C; ++c) put(&a.message[c], msg[c]);
-      a.lists = lists_of(h->slots[slot]);
+      a.lists = {lists.d_mix_rows + p0, lists.d_mix_entries};
       a.scale_offset = 16 * blocks_of(h);
+      a.rows_each = rows_each(h, lists, a.s.n_rows);
       a.gamma = gamma;
       e = launch_mix4((int)h->cfg.param_dtype, mode, C, a, stream);
     }
@@ -380,14 +388,16 @@ int dadam_mx4_round(dadam_handle* h, uint32_t slot, const void* const* x_src, vo
     return on_device(h, [&] {
       RoundArgs<kMaxRows> a;
       memset((void*)&a, 0, sizeof(a));
-      for (uint32_t i = 0; i < R; ++i) {
-        put(&a.row[i], 0, x_src[i]);
-        put(&a.row[i], 1, x_dst[i]);
-        put(&a.row[i], 2, copy[i]);
-        put(&a.row[i], 3, sum[i]);
+      const Slot& lists = h->slots[slot];
+      for (uint32_t p = 0; p < R; ++p) {
+        const int32_t i = lists.mix_rows[p].row;
+        put(&a.row[p], 0, x_src[i]);
+        put(&a.row[p], 1, x_dst[i]);
+        put(&a.row[p], 2, copy[i]);
+        put(&a.row[p], 3, sum[i]);
       }
       fill_span(h, &a.s);
-      a.lists = lists_of(h->slots[slot]);
+      a.lists = {lists.d_mix_rows, lists.d_mix_entries};
       a.gamma = gamma;
       return launch_round((int)h->cfg.param_dtype, a, hip_stream);
     });

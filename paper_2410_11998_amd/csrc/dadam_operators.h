@@ -29,22 +29,21 @@ struct Cuts {
   const uint32_t* masks;
 };
 
-// Neighbour lists of a slot (device).
+// Neighbour lists of a slot (device), see MixRow: positions [first, first + the launch's rows) of its rows.
 struct Lists {
-  const int32_t* row_ptr;
-  const int32_t* col;
-  const float* w;
+  const MixRow* rows;
+  const MixEntry* entries;
 };
 
-// What all these launches have in common.  Granules [first, first + count) of rows [row0, row0 + n_rows).
+// What all these launches have in common: units [first, first + count) of n_rows rows.
 struct Span {
   Cuts cuts;
   uint64_t d;
-  uint32_t n_granules;        // of the whole vector
+  uint32_t n_granules;  // of the whole vector; as many units
   uint32_t first, count;
-  uint32_t row0, n_rows;
+  uint32_t n_rows;
   uint32_t n_xcd;
-  uint32_t streams;           // accesses carry the non-temporal hint
+  uint32_t streams;     // accesses carry the non-temporal hint, lanes lie apart (see unit_place)
 };
 
 constexpr int kFewOperands = 16;  // rows and sources of the short argument block (see kFewRows)
@@ -70,17 +69,18 @@ struct EncodeArgs {
 
 template <int N, int C>
 struct MixArgs {
-  RowPointers row[N];  // 0 sum or output, 1 copy, 2 x, 3 x behind
+  RowPointers row[N];  // by position: 0 sum or output, 1 copy, 2 x, 3 x behind
   ColPointer message[C];
   Span s;
   Lists lists;
   uint64_t scale_offset;
+  uint32_t rows_each;  // positions a wavefront takes one after the other
   float gamma;
 };
 
 template <int N>
 struct RoundArgs {
-  RowPointers row[N];  // 0 x, 1 x behind, 2 copy, 3 sum
+  RowPointers row[N];  // by position: 0 x, 1 x behind, 2 copy, 3 sum
   Span s;
   Lists lists;
   float gamma;

@@ -60,28 +60,28 @@ static void check_span(const Span& s) {
 static uint64_t address(const RowPointers& r, int k) {
   return (((uint64_t)((r.high[k / 2] >> (16 * (k % 2))) & 0xFFFF) << 32) | r.low[k]) << 4;
 }
-static void check_rows(const RowPointers* r, const Span& s, int n_tables, int first_table) {
+static void check_rows(const RowPointers* r, const Span& s, int n_tables, const MixRow* order = nullptr) {
   for (uint32_t i = 0; i < s.n_rows; ++i)
     for (int k = 0; k < n_tables; ++k)
-      if (address(r[i], k) != address_of(s.row0 + i, first_table + k)) ++bad;
+      if (address(r[i], k) != address_of(order ? (uint32_t)order[i].row : i, k)) ++bad;
 }
 int launch_norm(int, const NormArgs<kMaxRows>& a, void*) {
   check_span(a.s);
-  check_rows(a.row, a.s, 1, 0);
+  check_rows(a.row, a.s, 1);
   for (uint32_t k = 0; k < a.per_row * a.s.n_rows; ++k) bad += a.partials[k] != 0.0;
   for (uint32_t i = 0; i < a.s.n_rows; ++i) bad += a.arrived[i] != 0;
   return 0;
 }
-int launch_clip(int, const NormArgs<kMaxRows>& a, void*) { check_span(a.s); check_rows(a.row, a.s, 2, 0); return 0; }
-int launch_encode(int, const EncodeArgs<kMaxRows>& a, void*) { check_span(a.s); check_rows(a.row, a.s, 4, 0); return 0; }
+int launch_clip(int, const NormArgs<kMaxRows>& a, void*) { check_span(a.s); check_rows(a.row, a.s, 2); return 0; }
+int launch_encode(int, const EncodeArgs<kMaxRows>& a, void*) { check_span(a.s); check_rows(a.row, a.s, 4); return 0; }
 int launch_mix4(int, MixMode mode, uint32_t n_cols, const MixArgs<kMessageRows, kMaxRows>& a, void*) {
   check_span(a.s);
-  check_rows(a.row, a.s, mode == kMixGossip ? 4 : 1, 0);
+  check_rows(a.row, a.s, mode == kMixGossip ? 4 : 1, a.lists.rows);
   for (uint32_t c = 0; c < n_cols; ++c)
     if ((((uint64_t)a.message[c].high << 32) | a.message[c].low) << 4 != address_of(c, 5)) ++bad;
   return 0;
 }
-int launch_round(int, const RoundArgs<kMaxRows>& a, void*) { check_span(a.s); check_rows(a.row, a.s, 4, 0); return 0; }
+int launch_round(int, const RoundArgs<kMaxRows>& a, void*) { check_span(a.s); check_rows(a.row, a.s, 4, a.lists.rows); return 0; }
 }  // namespace dadam
 
 int main() {

@@ -288,7 +288,7 @@ def test_messages_of_infinities_and_nans():
 # ---------------------------------------------------------------------------------------------
 
 GRAPHS = [(1, 3, "share"), (1, 1, "identity"), (5, 5, "ring"), (16, 16, "exp"), (17, 17, "complete"), (100, 100, "exp"), (3, 40, "rect"),
-          (97, 160, "rect"), (40, 40, "complete")]
+          (97, 160, "rect"), (40, 40, "complete"), (16, 16, "aer"), (120, 120, "aer")]
 
 
 def csr_of(rows, cols, kind, seed=5):
@@ -304,7 +304,7 @@ def csr_of(rows, cols, kind, seed=5):
             w += list((p / p.sum()).astype(np.float32))
             ptr.append(len(col))
         return np.asarray(ptr, np.int32), np.asarray(col, np.int32), np.asarray(w, np.float32)
-    return graph_of(rows, kind)
+    return WL.aer(rows // 4, 1) if kind == "aer" else graph_of(rows, kind)
 
 
 def check_sums(c, msg, csr, old, got, where):
@@ -421,6 +421,77 @@ def test_replicas_agree_and_their_mean_stays():
             B.dadam_mx4_round(c.h, 0, x, x, copy, total, 0.5, stream())
         assert spread() < 1e-3 * at_first
         assert float((torch.stack(x).double().mean(0) - mean).abs().max()) < 1e-4
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,graph", [(1, "identity"), (3, "ring"), (16, "exp"), (17, "complete"), (40, "ring"), (70, "ring")])
+def test_layouts_that_stream(rows, graph, kind):
+    """23 million elements and more in all: accesses carry the streaming hint and the halves of a wavefront lie apart.  Long and short
+    tensors, gaps inside and at the ends of the blocks of such halves, an end that is no multiple of 32.  Every call against the oracle
+    on one row, the round against the two calls on every row."""
+    each = 23_500_000 // rows
+    offsets, sizes, at, rng = [], [], 5, np.random.default_rng(rows)
+    while at < each:
+        n = int(rng.choice([1, 700, 32768 * 3 + 17, 16384, 400_000]))
+        n = min(n, each - at)
+        offsets.append(at)
+        sizes.append(n)
+        at += n + int(rng.choice([0, 0, 3, 40, 2000]))
+    d = at + 3
+    stored = stored_of((offsets, sizes, d))
+    pad = torch.from_numpy(~stored).to(DEV)
+    csr = graph_of(rows, graph)
+    h = B.dadam_init(rows, rows, d, offsets, sizes, H.ABI_DT[kind], H.ABI_DT[kind])
+    assert B.dadam_get_plan_info(h).streaming == 1
+    B.dadam_set_topology(h, 0, *csr)
+    info = B.dadam_mx4_get_info(h)
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(rows)
+
+    def values(std, dtype=torch.float32):
+        out = []
+        for _ in range(rows):
+            t = (torch.randn(d, generator=gen, device=DEV) * std).to(dtype)
+            t[pad] = float("nan")
+            out.append(t)
+        return out
+    xt = H.TORCH_DT[kind]
+    x, copy, total = values(0.02, xt), values(0.02), values(0.02)
+    norms, clipped = torch.zeros(rows, device=DEV), values(1.0, xt)
+    B.dadam_clip_grads(h, x, clipped, 1.0, norms, stream())
+    msg = [torch.zeros(info.bytes, dtype=torch.uint8, device=DEV) for _ in range(rows)]
+    moved, mixed, again, behind = values(1.0), [t.clone() for t in total], [t.clone() for t in total], values(1.0, xt)
+    B.dadam_mx4_encode(h, x, copy, moved, msg, stream())
+    B.dadam_mx4_gossip(h, 0, msg, mixed, moved, x, behind, 0.4, stream())
+    out = values(1.0)
+    B.dadam_mx4_product(h, 0, msg, out, 0, stream())
+    one = [[t.clone() for t in copy], values(1.0, xt)]
+    B.dadam_mx4_round(h, 0, x, one[1], one[0], again, 0.4, stream())
+    torch.cuda.synchronize()
+    for i in range(rows):
+        for a, b in ((one[0][i], moved[i]), (one[1][i], behind[i]), (again[i], mixed[i])):
+            assert torch.equal(a.view(torch.int16 if a.element_size() == 2 else torch.int32), b.view(torch.int16 if b.element_size() == 2 else torch.int32)), i
+    for t in clipped + moved + mixed + behind + out:
+        assert torch.isnan(t[pad]).all() and not torch.isnan(t[~pad]).any()
+    i = rows // 2
+    xs, hs = host(x[i]), host(copy[i])
+    want, sent = O.encode(xs, hs, stored)
+    assert np.array_equal(msg[i].cpu().numpy()[:len(want)], want)
+    assert same(host(moved[i])[stored], (hs + sent.astype(np.float32))[stored])
+    n, scaled = O.clip(xs, stored, 1.0)
+    assert abs(float(norms[i]) - n) <= 2 * EPS * n
+    assert np.all((np.abs(host(clipped[i]) - scaled) <= np.abs(scaled) * (4 * EPS + (2.0 ** -8 if kind == "bf16" else 0)) + TINY)[stored])
+    entries = [int(c) for c in csr[1][csr[0][i]:csr[0][i + 1]]]
+    terms = [float(np.float32(1.0 / len(entries))) * O.decode(msg[c].cpu().numpy(), d) for c in entries]
+    ref, size, k = sum(terms), sum(np.abs(v) for v in terms), len(entries)
+    assert np.all((np.abs(host(out[i]) - ref) <= (k + 2) * EPS * size + (k + 2) * TINY)[stored])
+    base = host(total[i]).astype(np.float64)
+    assert np.all((np.abs(host(mixed[i]) - (base + ref)) <= (k + 2) * EPS * (size + np.abs(base)) + (k + 2) * TINY)[stored])
+    s, c, v = host(mixed[i]).astype(np.float64), host(moved[i]).astype(np.float64), xs.astype(np.float64)
+    ref = v + float(np.float32(0.4)) * (s - c)
+    bound = 0.41 * EPS * (np.abs(s) + np.abs(c)) + 1.01 * EPS * np.abs(ref) + TINY + (2.0 ** -8 * np.abs(ref) if kind == "bf16" else 0)
+    assert np.all((np.abs(host(behind[i]) - ref) <= bound)[stored])
+    B.dadam_destroy(h)
 
 
 # ---------------------------------------------------------------------------------------------
