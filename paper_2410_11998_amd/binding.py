@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 from typing import Optional, Sequence
 
 import numpy as np
@@ -123,7 +124,7 @@ def _load() -> C.CDLL:
     lib.dadam_get_row_order.argtypes = [H, C.c_uint32, C.POINTER(C.c_int32)]
     lib.dadam_deal_offsets.argtypes = [C.POINTER(C.c_uint64), C.c_uint32, C.c_uint64, C.c_uint64, C.c_uint64, C.c_uint64,
                                        C.c_uint32, C.POINTER(C.c_uint64)]
-    P = C.POINTER(C.c_void_p)
+    P = C.c_void_p   # a table: the address of its first pointer, or a ctypes array
     lib.dadam_grad_norm.argtypes = [H, P, C.c_void_p, C.c_void_p]
     lib.dadam_clip_grads.argtypes = [H, P, P, C.c_float, C.c_void_p, C.c_void_p]
     lib.dadam_mx4_get_info.argtypes = [H, C.POINTER(dadam_mx4_info)]
@@ -386,36 +387,28 @@ def dadam_slot_uses_tile_mode(h, slot: int) -> bool:
     return _check(h, lib.dadam_slot_uses_tile_mode(h, slot)) == 1
 
 
-_TABLE_OF = {}   # number of pointers -> ctypes array type
-
-
-def _table(ptrs):
-    kind = _TABLE_OF.get(len(ptrs))
-    if kind is None:
-        kind = _TABLE_OF[len(ptrs)] = C.c_void_p * len(ptrs)
-    return kind(*ptrs)
-
-
 def pointer_table(buffers, count: int, length: int, elem_bytes: int, what: str):
     """The host array of `count` device pointers that the calls below take, marshalled and size-checked once: from a sequence of tensors (or
     integers taken as addresses), or from one tensor whose rows are the buffers.  None stays None, a table made before is
     passed through.  The tensors must stay alive."""
     if buffers is None:
         return None
-    if len(buffers) < count:
-        raise ValueError(f"{what} holds {len(buffers)} buffers, the handle needs {count}")
-    if isinstance(buffers, C.Array):
-        return buffers
     if hasattr(buffers, "data_ptr"):
-        stride = buffers.stride()
-        if len(stride) != 2 or (stride[1] != 1 and buffers.shape[1] > 1):
+        shape, stride = buffers.shape, buffers.stride()
+        if len(stride) != 2 or (stride[1] != 1 and shape[1] > 1):
             raise ValueError(f"{what} is one tensor: its rows must be the buffers, each contiguous")
+        if shape[0] < count:
+            raise ValueError(f"{what} holds {shape[0]} buffers, the handle needs {count}")
         if buffers.element_size() != elem_bytes:
             raise ValueError(f"{what} has {buffers.element_size()}-byte elements, the handle expects {elem_bytes}")
-        if buffers.shape[1] < length:
-            raise ValueError(f"{what} holds {buffers.shape[1]} elements a buffer, the handle needs {length}")
+        if shape[1] < length:
+            raise ValueError(f"{what} holds {shape[1]} elements a buffer, the handle needs {length}")
         first, step = buffers.data_ptr(), stride[0] * elem_bytes
-        return _table([first + k * step for k in range(count)])
+        return array("Q", range(first, first + count * step, step)) if count > 1 and step > 0 else array("Q", (first,) * count)
+    if len(buffers) < count:
+        raise ValueError(f"{what} holds {len(buffers)} buffers, the handle needs {count}")
+    if isinstance(buffers, (array, C.Array)):
+        return buffers
     ptrs = []
     for k in range(count):
         t = buffers[k]
@@ -428,7 +421,12 @@ def pointer_table(buffers, count: int, length: int, elem_bytes: int, what: str):
                 raise ValueError(f"{what}[{k}] holds {t.numel()} elements, the handle needs {length}")
             t = t.data_ptr()
         ptrs.append(t)
-    return _table(ptrs)
+    return array("Q", ptrs)
+
+
+def _at(table):
+    """Where a table's pointers lie, for the call that holds the table."""
+    return table.buffer_info()[0] if isinstance(table, array) else table
 
 
 def _shape(h):
@@ -439,10 +437,10 @@ def _message_bytes(d: int) -> int:
     return -(-(-(-d // DADAM_MX4_BLOCK) * 17) // 16) * 16
 
 
-def _row_values(h, norms) -> int:
+def _row_values(norms, rows: int) -> int:
     if isinstance(norms, int):
         return norms
-    if norms.numel() < _shape(h)[3] or norms.element_size() != 4 or not norms.is_contiguous():
+    if norms.numel() < rows or norms.element_size() != 4 or not norms.is_contiguous():
         raise ValueError("norms must hold one float32 a row")
     return norms.data_ptr()
 
@@ -450,13 +448,14 @@ def _row_values(h, norms) -> int:
 def dadam_grad_norm(h, grads, norms, stream: int = 0) -> None:
     """norms: a device tensor of n_rows float32 (or an integer device address)."""
     d, _, gb, rows, _ = _shape(h)
-    _check(h, lib.dadam_grad_norm(h, pointer_table(grads, rows, d, gb, "grads"), _row_values(h, norms), stream))
+    g = pointer_table(grads, rows, d, gb, "grads")
+    _check(h, lib.dadam_grad_norm(h, _at(g), _row_values(norms, rows), stream))
 
 
 def dadam_clip_grads(h, grads, out, max_norm: float, norms, stream: int = 0) -> None:
     d, _, gb, rows, _ = _shape(h)
-    _check(h, lib.dadam_clip_grads(h, pointer_table(grads, rows, d, gb, "grads"), pointer_table(out, rows, d, gb, "out"), max_norm,
-                                   _row_values(h, norms), stream))
+    g, o = pointer_table(grads, rows, d, gb, "grads"), pointer_table(out, rows, d, gb, "out")
+    _check(h, lib.dadam_clip_grads(h, _at(g), _at(o), max_norm, _row_values(norms, rows), stream))
 
 
 def dadam_mx4_get_info(h) -> dadam_mx4_info:
@@ -468,26 +467,30 @@ def dadam_mx4_get_info(h) -> dadam_mx4_info:
 def dadam_mx4_encode(h, x, copy_in, copy_out, msg, stream: int = 0) -> None:
     """copy_in and copy_out may be None; messages are uint8 tensors."""
     d, pb, _, rows, _ = _shape(h)
-    _check(h, lib.dadam_mx4_encode(h, pointer_table(x, rows, d, pb, "x"), pointer_table(copy_in, rows, d, 4, "copy_in"),
-                                   pointer_table(copy_out, rows, d, 4, "copy_out"), pointer_table(msg, rows, _message_bytes(d), 1, "msg"), stream))
+    x, msg = pointer_table(x, rows, d, pb, "x"), pointer_table(msg, rows, _message_bytes(d), 1, "msg")
+    copy_in, copy_out = pointer_table(copy_in, rows, d, 4, "copy_in"), pointer_table(copy_out, rows, d, 4, "copy_out")
+    _check(h, lib.dadam_mx4_encode(h, _at(x), _at(copy_in), _at(copy_out), _at(msg), stream))
 
 
 def dadam_mx4_product(h, slot: int, msg, out, flags: int = 0, stream: int = 0) -> None:
     d, _, _, rows, cols = _shape(h)
-    _check(h, lib.dadam_mx4_product(h, slot, pointer_table(msg, cols, _message_bytes(d), 1, "msg"), pointer_table(out, rows, d, 4, "out"), flags, stream))
+    msg, out = pointer_table(msg, cols, _message_bytes(d), 1, "msg"), pointer_table(out, rows, d, 4, "out")
+    _check(h, lib.dadam_mx4_product(h, slot, _at(msg), _at(out), flags, stream))
 
 
 def dadam_mx4_gossip(h, slot: int, msg, sum, copy, x_src, x_dst, gamma: float, stream: int = 0) -> None:
     d, pb, _, rows, cols = _shape(h)
-    _check(h, lib.dadam_mx4_gossip(h, slot, pointer_table(msg, cols, _message_bytes(d), 1, "msg"), pointer_table(sum, rows, d, 4, "sum"),
-                                   pointer_table(copy, rows, d, 4, "copy"), pointer_table(x_src, rows, d, pb, "x_src"),
-                                   pointer_table(x_dst, rows, d, pb, "x_dst"), gamma, stream))
+    msg, sum = pointer_table(msg, cols, _message_bytes(d), 1, "msg"), pointer_table(sum, rows, d, 4, "sum")
+    copy, x_src = pointer_table(copy, rows, d, 4, "copy"), pointer_table(x_src, rows, d, pb, "x_src")
+    x_dst = pointer_table(x_dst, rows, d, pb, "x_dst")
+    _check(h, lib.dadam_mx4_gossip(h, slot, _at(msg), _at(sum), _at(copy), _at(x_src), _at(x_dst), gamma, stream))
 
 
 def dadam_mx4_round(h, slot: int, x_src, x_dst, copy, sum, gamma: float, stream: int = 0) -> None:
     d, pb, _, rows, _ = _shape(h)
-    _check(h, lib.dadam_mx4_round(h, slot, pointer_table(x_src, rows, d, pb, "x_src"), pointer_table(x_dst, rows, d, pb, "x_dst"),
-                                  pointer_table(copy, rows, d, 4, "copy"), pointer_table(sum, rows, d, 4, "sum"), gamma, stream))
+    x_src, x_dst = pointer_table(x_src, rows, d, pb, "x_src"), pointer_table(x_dst, rows, d, pb, "x_dst")
+    copy, sum = pointer_table(copy, rows, d, 4, "copy"), pointer_table(sum, rows, d, 4, "sum")
+    _check(h, lib.dadam_mx4_round(h, slot, _at(x_src), _at(x_dst), _at(copy), _at(sum), gamma, stream))
 
 
 def dadam_destroy(h) -> None:
@@ -495,7 +498,14 @@ def dadam_destroy(h) -> None:
     lib.dadam_destroy(h)
 
 
+_raw_stream = None   # torch's look-ups behind torch.cuda.current_stream(), which makes an object of the answer (1.5 us)
+
+
 def current_stream() -> int:
     """The HIP stream PyTorch is launching on, as an integer handle."""
-    import torch
-    return int(torch.cuda.current_stream().cuda_stream)
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        torch.cuda.current_stream()     # sets the device up
+        _raw_stream = (torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice)
+    return _raw_stream[0](_raw_stream[1]())

@@ -32,11 +32,12 @@ __device__ __forceinline__ uint32_t cut_of(const Cuts& c, uint32_t granule) {
   typedef const uint32_t __attribute__((address_space(4))) * Constant;
   return c.index ? ((Constant)c.index)[granule] : 0u;
 }
-// Bits 0 to 3: which elements of the group of four from e on (a multiple of 4) belong to a tensor.
-__device__ __forceinline__ uint32_t group_bits(const Cuts& c, uint64_t e) {
-  const uint32_t cut = c.index ? c.index[e / kGranule] : 0u;
-  return cut == 0 ? 0xFu : (c.masks[cut - 1 + e % kGranule / kMxBlock] >> (e % kMxBlock)) & 0xFu;
+// Which of the n elements from e on (multiples of n, 4 or 8; inside one granule of the vector) belong to a tensor.
+__device__ __forceinline__ uint32_t stored_bits(const Cuts& c, uint64_t e, int n) {
+  const uint32_t all = (1u << n) - 1, cut = c.index ? c.index[e / kGranule] : 0u;
+  return cut == 0 ? all : (c.masks[cut - 1 + e % kGranule / kMxBlock] >> (e % kMxBlock)) & all;
 }
+__device__ __forceinline__ uint32_t group_bits(const Cuts& c, uint64_t e) { return stored_bits(c, e, 4); }
 
 // Where a wavefront's unit of 512 elements (V = 2) or 256 (V = 1) lies: lane l holds V groups of four from `first` on, `step` apart; eight
 // lanes side by side hold a block of 32 elements.  In order: one run.  SPREAD: as streaming kernels have it (see lane_start, V vectors a
@@ -62,11 +63,11 @@ __device__ __forceinline__ Unit unit_place(uint32_t i, const Span& s, uint32_t l
   return {first + 4 * lane, 256, cut_of(s.cuts, (uint32_t)(first / kGranule)) == 0};
 }
 
-// A lane's group of four elements from e on (a multiple of 4), widened to float; elements that `bits` leaves out are not touched
-// and read as zero.
-template <typename T, bool NT>
-__device__ __forceinline__ void load_group(const void* base, uint64_t e, uint32_t bits, float (&v)[4]) {
-  if (bits == 0xFu) {
+// A lane's group of four elements from e on (a multiple of 4), widened to float.  Elements that `bits` leaves out read as zero: whole groups
+// are loaded wherever they end within the d elements of the buffer, so that no load waits for the masks.
+template <typename T, bool WHOLE, bool NT>
+__device__ __forceinline__ void load_group(const void* base, uint64_t e, uint32_t bits, uint64_t d, float (&v)[4]) {
+  if (WHOLE || e + 4 <= d) {
     if constexpr (T::bytes == 4) {
       const f4 x = vload<NT>(reinterpret_cast<const f4*>(at<float>(base, e)));
       v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
@@ -78,6 +79,10 @@ __device__ __forceinline__ void load_group(const void* base, uint64_t e, uint32_
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = bits >> j & 1 ? load_elem<T>(base, e + j) : 0.0f;
+  }
+  if constexpr (!WHOLE) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = bits >> j & 1 ? v[j] : 0.0f;
   }
 }
 

@@ -52,7 +52,7 @@ __device__ __forceinline__ void encode(const float (&u)[4], uint32_t& codes, uin
 }
 
 template <typename XT, bool WHOLE, bool NT>
-__device__ __forceinline__ void encode_unit(const Cuts& cuts, const Unit& t, const RowPointers& p, uint64_t scale_offset) {
+__device__ __forceinline__ void encode_unit(const Cuts& cuts, uint64_t d, const Unit& t, const RowPointers& p, uint64_t scale_offset) {
   const void* x = buffer<const void, 0>(p);
   const void* before = buffer<const void, 1>(p);
   void* behind = buffer<void, 2>(p);
@@ -62,11 +62,11 @@ __device__ __forceinline__ void encode_unit(const Cuts& cuts, const Unit& t, con
 #pragma unroll
   for (uint32_t k = 0; k < 2; ++k) {
     bits[k] = WHOLE ? 0xFu : group_bits(cuts, t.first + k * t.step);
-    load_group<XT, NT>(x, t.first + k * t.step, bits[k], u[k]);
+    load_group<XT, WHOLE, NT>(x, t.first + k * t.step, bits[k], d, u[k]);
   }
   if (before) {
 #pragma unroll
-    for (uint32_t k = 0; k < 2; ++k) load_group<TF32, NT>(before, t.first + k * t.step, bits[k], copy[k]);
+    for (uint32_t k = 0; k < 2; ++k) load_group<TF32, WHOLE, NT>(before, t.first + k * t.step, bits[k], d, copy[k]);
   }
 #pragma unroll
   for (uint32_t k = 0; k < 2; ++k) {
@@ -98,8 +98,8 @@ __global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_encode(const EncodeAr
   const uint32_t row = blockIdx.x % a.s.n_rows, i = a.s.first + blockIdx.x / a.s.n_rows * kMixWaves + wave_of_group();
   if (i < a.s.n_granules) {
     const Unit t = unit_place<2, NT>(i, a.s, lane);
-    if (t.whole) encode_unit<XT, true, NT>(a.s.cuts, t, a.row[row], a.scale_offset);
-    else encode_unit<XT, false, NT>(a.s.cuts, t, a.row[row], a.scale_offset);
+    if (t.whole) encode_unit<XT, true, NT>(a.s.cuts, a.s.d, t, a.row[row], a.scale_offset);
+    else encode_unit<XT, false, NT>(a.s.cuts, a.s.d, t, a.row[row], a.scale_offset);
   }
 }
 
@@ -162,10 +162,10 @@ __device__ __forceinline__ void mix_positions(const A& a, const Unit& t, uint32_
 #pragma unroll
     for (uint32_t k = 0; k < 2; ++k) {
       const uint64_t e = t.first + k * t.step;
-      if constexpr (MODE != kMixStore) load_group<TF32, NT>(sum, e, bits[k], s[k]);
+      if constexpr (MODE != kMixStore) load_group<TF32, WHOLE, NT>(sum, e, bits[k], a.s.d, s[k]);
       if constexpr (MODE == kMixGossip) {
-        load_group<TF32, NT>(buffer<const void, 1>(rp), e, bits[k], c[k]);
-        load_group<XT, NT>(buffer<const void, 2>(rp), e, bits[k], x[k]);
+        load_group<TF32, WHOLE, NT>(buffer<const void, 1>(rp), e, bits[k], a.s.d, c[k]);
+        load_group<XT, WHOLE, NT>(buffer<const void, 2>(rp), e, bits[k], a.s.d, x[k]);
       }
     }
     const MixRow r = mix_row(a.lists, p);
@@ -218,8 +218,8 @@ __device__ __forceinline__ void round_unit(const A& a, const Unit& t, uint32_t e
     if (q < each && p < a.s.n_rows) {
 #pragma unroll
       for (uint32_t k = 0; k < V; ++k) {
-        load_group<XT, NT>(buffer<const void, 0>(a.row[p]), t.first + k * t.step, bits[k], x[q][k]);
-        load_group<TF32, NT>(buffer<const void, 2>(a.row[p]), t.first + k * t.step, bits[k], copy[q][k]);
+        load_group<XT, WHOLE, NT>(buffer<const void, 0>(a.row[p]), t.first + k * t.step, bits[k], a.s.d, x[q][k]);
+        load_group<TF32, WHOLE, NT>(buffer<const void, 2>(a.row[p]), t.first + k * t.step, bits[k], a.s.d, copy[q][k]);
       }
     }
   }
@@ -251,7 +251,7 @@ __device__ __forceinline__ void round_unit(const A& a, const Unit& t, uint32_t e
     if (q < each && p < a.s.n_rows) {
       float s[V][4];
 #pragma unroll
-      for (uint32_t k = 0; k < V; ++k) load_group<TF32, NT>(buffer<const void, 3>(a.row[p]), t.first + k * t.step, bits[k], s[k]);
+      for (uint32_t k = 0; k < V; ++k) load_group<TF32, WHOLE, NT>(buffer<const void, 3>(a.row[p]), t.first + k * t.step, bits[k], a.s.d, s[k]);
       const MixRow r = mix_row(a.lists, p);
       if (q == 0 || !r.same) {
 #pragma unroll

@@ -33,24 +33,58 @@ __device__ __forceinline__ double row_sum(const double* partials, uint32_t count
 
 __device__ __forceinline__ double with_square(double sum, float v) { return __builtin_fma((double)v, (double)v, sum); }
 
-// A whole granule as 16-byte vectors, one (bfloat16) or two (float32) a lane: here it does not matter which lane has which element.
+// A granule goes as 16-byte vectors, one (bfloat16) or two (float32) a lane.  Bits of `stored` say which elements of a vector count.
 template <typename GT>
-constexpr int kWholeVectors = GT::bytes / 2;
+constexpr int kVectors = GT::bytes / 2;
 template <typename GT>
-__device__ __forceinline__ void add_squares(const u4 (&raw)[kWholeVectors<GT>], double (&sums)[2]) {
+constexpr int kVectorElems = 16 / GT::bytes;
+template <typename GT, bool WHOLE>
+__device__ __forceinline__ void add_squares(const u4& raw, uint32_t stored, double (&sums)[2]) {
+  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+  auto counted = [stored](uint32_t bits, int j) { return __uint_as_float(WHOLE || (stored >> j & 1) ? bits : 0u); };
 #pragma unroll
-  for (int k = 0; k < kWholeVectors<GT>; ++k) {
-    const uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if constexpr (GT::bytes == 4) {
-        sums[j & 1] = with_square(sums[j & 1], __uint_as_float(w[j]));
-      } else {
-        sums[0] = with_square(sums[0], __uint_as_float(w[j] << 16));
-        sums[1] = with_square(sums[1], __uint_as_float(w[j] & 0xFFFF0000u));
-      }
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (GT::bytes == 4) {
+      sums[j & 1] = with_square(sums[j & 1], counted(w[j], j));
+    } else {
+      sums[0] = with_square(sums[0], counted(w[j] << 16, 2 * j));
+      sums[1] = with_square(sums[1], counted(w[j] & 0xFFFF0000u, 2 * j + 1));
     }
   }
+}
+
+// kAtOnce granules, `stride` apart; all loads are in flight before the first use.  Not WHOLE: some have padding, end behind the vector or lie
+// there.
+template <typename GT, int AT_ONCE, bool WHOLE, bool NT>
+__device__ __forceinline__ void add_granules(const Span& s, const void* g, uint64_t i0, uint32_t stride, uint32_t lane, double (&sums)[2]) {
+  constexpr int V = kVectors<GT>, E = kVectorElems<GT>;
+  u4 raw[AT_ONCE][V];
+  uint32_t stored[AT_ONCE][V];
+#pragma unroll
+  for (uint32_t k = 0; k < AT_ONCE; ++k)
+#pragma unroll
+    for (uint32_t v = 0; v < V; ++v) {
+      const uint64_t i = i0 + (uint64_t)k * stride, e = i * kGranule + v * (kGranule / V) + E * lane;
+      const bool in = WHOLE || i < s.n_granules;
+      stored[k][v] = WHOLE ? 0u : in ? stored_bits(s.cuts, e, E) & (e < s.d ? ~0u : 0u) : 0u;
+      raw[k][v] = u4{0, 0, 0, 0};
+      if (WHOLE || (in && e + E <= s.d)) {
+        raw[k][v] = vload<NT>(reinterpret_cast<const u4*>(static_cast<const char*>(g) + e * GT::bytes));
+      } else if (in && e < s.d) {  // the vector's last elements
+        uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < E; ++j)
+          if (e + j < s.d) {
+            if constexpr (GT::bytes == 4) w[j] = at<uint32_t>(g, e)[j];
+            else w[j / 2] |= (uint32_t)at<uint16_t>(g, e)[j] << (16 * (j % 2));
+          }
+        raw[k][v] = u4{w[0], w[1], w[2], w[3]};
+      }
+    }
+#pragma unroll
+  for (uint32_t k = 0; k < AT_ONCE; ++k)
+#pragma unroll
+    for (uint32_t v = 0; v < V; ++v) add_squares<GT, WHOLE>(raw[k][v], stored[k][v], sums);
 }
 
 // per_row workgroups share a row, each wavefront takes every (per_row * 4)-th granule, kAtOnce of them at a time.  The workgroup
@@ -64,37 +98,16 @@ __global__ __launch_bounds__(kNormThreads) void k_grad_norm(const NormArgs<N> a)
   const uint32_t row = blockIdx.x % a.s.n_rows, part = blockIdx.x / a.s.n_rows;
   const void* g = buffer<const void, 0>(a.row[row]);
   const uint32_t stride = a.per_row * kNormWaves, n = a.s.n_granules;
-  constexpr uint32_t kAtOnce = 8 / kWholeVectors<GT>;
+  constexpr int kAtOnce = 8 / kVectors<GT>;
   double sums[2] = {0.0, 0.0};
   for (uint64_t i0 = part * kNormWaves + wave; i0 < n; i0 += (uint64_t)kAtOnce * stride) {
-    uint32_t cuts = i0 + (uint64_t)(kAtOnce - 1) * stride >= n;  // granules behind the end go one by one too
+    uint32_t cuts = i0 + (uint64_t)(kAtOnce - 1) * stride >= n;
     if (a.s.cuts.index && !cuts) {
 #pragma unroll
-      for (uint32_t k = 0; k < kAtOnce; ++k) cuts |= cut_of(a.s.cuts, (uint32_t)i0 + k * stride);
+      for (int k = 0; k < kAtOnce; ++k) cuts |= cut_of(a.s.cuts, (uint32_t)i0 + k * stride);
     }
-    if (cuts == 0) {
-      u4 raw[kAtOnce][kWholeVectors<GT>];
-#pragma unroll
-      for (uint32_t k = 0; k < kAtOnce; ++k)
-#pragma unroll
-        for (int v = 0; v < kWholeVectors<GT>; ++v)
-          raw[k][v] = vload<NT>(reinterpret_cast<const u4*>(static_cast<const char*>(g) + (i0 + k * stride) * (kGranule * GT::bytes) + v * 1024 + 16 * lane));
-#pragma unroll
-      for (uint32_t k = 0; k < kAtOnce; ++k) add_squares<GT>(raw[k], sums);
-    } else {
-#pragma unroll 1
-      for (uint32_t k = 0; k < kAtOnce; ++k) {
-        const uint64_t i = i0 + (uint64_t)k * stride;
-#pragma unroll 1
-        for (uint32_t half = 0; half < 2 && i < n; ++half) {
-          float v[4];
-          const uint64_t e = i * kGranule + half * 256 + 4 * lane;
-          load_group<GT, NT>(g, e, group_bits(a.s.cuts, e), v);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) sums[j & 1] = with_square(sums[j & 1], v[j]);
-        }
-      }
-    }
+    if (cuts == 0) add_granules<GT, kAtOnce, true, NT>(a.s, g, i0, stride, lane, sums);
+    else add_granules<GT, kAtOnce, false, NT>(a.s, g, i0, stride, lane, sums);
   }
   const double sum = group_sum(sums[0] + sums[1], partial, lane, wave);
   double* row_partials = a.partials + (uint64_t)row * a.per_row;
@@ -116,13 +129,13 @@ __global__ __launch_bounds__(kNormThreads) void k_grad_norm(const NormArgs<N> a)
 }
 
 template <typename GT, bool WHOLE, bool NT>
-__device__ __forceinline__ void clip_unit(const Cuts& cuts, const Unit& u, const void* g, void* out, float factor) {
+__device__ __forceinline__ void clip_unit(const Cuts& cuts, uint64_t d, const Unit& u, const void* g, void* out, float factor) {
   float v[2][4];
   uint32_t bits[2];
 #pragma unroll
   for (uint32_t k = 0; k < 2; ++k) {
     bits[k] = WHOLE ? 0xFu : group_bits(cuts, u.first + k * u.step);
-    load_group<GT, NT>(g, u.first + k * u.step, bits[k], v[k]);
+    load_group<GT, WHOLE, NT>(g, u.first + k * u.step, bits[k], d, v[k]);
   }
 #pragma unroll
   for (uint32_t k = 0; k < 2; ++k) {
@@ -143,8 +156,8 @@ __global__ __launch_bounds__(kNormThreads) void k_clip(const NormArgs<N> a) {
   if (i < a.s.n_granules && (scales || g != out)) {
     const float factor = scales ? a.max_norm / norm : 1.0f;
     const Unit u = unit_place<2, NT>(i, a.s, lane);
-    if (u.whole) clip_unit<GT, true, NT>(a.s.cuts, u, g, out, factor);
-    else clip_unit<GT, false, NT>(a.s.cuts, u, g, out, factor);
+    if (u.whole) clip_unit<GT, true, NT>(a.s.cuts, a.s.d, u, g, out, factor);
+    else clip_unit<GT, false, NT>(a.s.cuts, a.s.d, u, g, out, factor);
   }
 }
 

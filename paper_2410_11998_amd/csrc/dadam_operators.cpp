@@ -115,20 +115,12 @@ struct Range {
 
 constexpr uintptr_t kHighest = (uintptr_t)1 << 52;
 
-// Every buffer is there, aligned and within reach; nothing that is written overlaps anything else, but the same entry of the table
-// it may be in place of.
-int check_tables(const dadam_handle* h, const Table* t, int n_tables) {
-  if (h->cfg.d > kMostElems) return fail(h, DADAM_EINVAL, "the operators around the step take up to 2^36 elements");
+// Nothing that is written overlaps anything else, but the same entry of the table it may be in place of.
+int check_overlaps(const dadam_handle* h, const Table* t, int n_tables) {
   Range all[5 * DADAM_MAX_ROWS], open[5 * DADAM_MAX_ROWS];  // open: earlier ranges that reach beyond where the walk is
   uint32_t n = 0, n_open = 0;
   for (int k = 0; k < n_tables; ++k)
-    for (uint32_t i = 0; t[k].p && i < t[k].n; ++i) {
-      const uintptr_t at = (uintptr_t)t[k].p[i];
-      if (!at) return fail(h, DADAM_EINVAL, "%s[%u] is null", t[k].name, i);
-      if (at & 15u) return fail(h, DADAM_EALIGN, "%s[%u] is not 16-byte aligned", t[k].name, i);
-      if (at >= kHighest || t[k].bytes > kHighest - at) return fail(h, DADAM_EINVAL, "%s[%u] reaches above address 2^52", t[k].name, i);
-      all[n++] = {at, at + t[k].bytes, k, i};
-    }
+    for (uint32_t i = 0; t[k].p && i < t[k].n; ++i) all[n++] = {(uintptr_t)t[k].p[i], (uintptr_t)t[k].p[i] + t[k].bytes, k, i};
   std::sort(all, all + n, [](const Range& a, const Range& b) { return a.lo < b.lo; });
   for (uint32_t q = 0; q < n; ++q) {
     const Range& r = all[q];
@@ -143,6 +135,31 @@ int check_tables(const dadam_handle* h, const Table* t, int n_tables) {
     open[n_open++] = r;
   }
   return DADAM_OK;
+}
+
+// Every buffer is there, aligned and within reach, and does not overlap what it must not.
+int check_tables(const dadam_handle* h, const Table* t, int n_tables) {
+  if (h->cfg.d > kMostElems) return fail(h, DADAM_EINVAL, "the operators around the step take up to 2^36 elements");
+  bool apart = true;  // tables of increasing buffers, one table's behind the other's: nothing overlaps
+  uintptr_t lows[5], highs[5];
+  int n_used = 0;
+  for (int k = 0; k < n_tables; ++k) {
+    if (!t[k].p || t[k].n == 0) continue;
+    uintptr_t end = 0;
+    for (uint32_t i = 0; i < t[k].n; ++i) {
+      const uintptr_t at = (uintptr_t)t[k].p[i];
+      if (!at) return fail(h, DADAM_EINVAL, "%s[%u] is null", t[k].name, i);
+      if (at & 15u) return fail(h, DADAM_EALIGN, "%s[%u] is not 16-byte aligned", t[k].name, i);
+      if (at >= kHighest || t[k].bytes > kHighest - at) return fail(h, DADAM_EINVAL, "%s[%u] reaches above address 2^52", t[k].name, i);
+      apart &= at >= end;
+      end = at + t[k].bytes;
+    }
+    lows[n_used] = (uintptr_t)t[k].p[0];
+    highs[n_used++] = end;
+  }
+  for (int k = 0; k < n_used; ++k)
+    for (int m = 0; m < k; ++m) apart &= highs[k] <= lows[m] || highs[m] <= lows[k];
+  return apart ? DADAM_OK : check_overlaps(h, t, n_tables);
 }
 
 int check_norms(const dadam_handle* h, const float* norms) {
