@@ -40,7 +40,7 @@ struct Slot {
   const Loop* d_loops = nullptr;
   std::vector<MixRow> mix_rows;       // see MixRow
   std::vector<MixEntry> mix_entries;
-  bool mix_shared = false;            // some row shares its entries
+  uint32_t mix_groups = 0;            // different lists
   const MixRow* d_mix_rows = nullptr;
   const MixEntry* d_mix_entries = nullptr;
 };

@@ -806,13 +806,15 @@ void find_mix_rows(uint32_t R, Slot& s) {
     const int32_t first = (int32_t)s.mix_entries.size();
     if (rows.size() > 1) {
       for (const auto& e : sorted[i]) s.mix_entries.push_back({e.first, e.second});
-      s.mix_shared = true;
     } else {
       for (int32_t k = s.row_ptr[i]; k < s.row_ptr[i + 1]; ++k) s.mix_entries.push_back({s.col[k], s.w[k]});
     }
     const int32_t n = (int32_t)s.mix_entries.size() - first;
     while (s.mix_entries.size() % kMixAtOnce) s.mix_entries.push_back({s.mix_entries.back().col, 0.f});
-    for (int32_t row : rows) s.mix_rows.push_back({row, first, n, row != (int32_t)i});
+    const int32_t all = (int32_t)s.mix_entries.size() - first, step = kMixAtOnce * (rows.size() > 1 ? kMixParts : 1);
+    const int32_t part = rows.size() > 1 ? (all + step - 1) / step * kMixAtOnce : all;
+    for (int32_t row : rows) s.mix_rows.push_back({(int16_t)row, (int16_t)(row != (int32_t)i), first, n, part});
+    ++s.mix_groups;
   }
 }
 

@@ -62,15 +62,18 @@ struct Loop {
 };
 // How the products with 4-bit messages walk a slot: its rows in an order in which rows that list the same sources with the same
 // weights follow each other (`same`: as the one before).  Their entries are filled up to a multiple of kMixAtOnce with the last one's
-// source and weight 0; rows that share them have them in order of the sources, the others as listed.
+// source and weight 0; rows that share them have them in order of the sources, the others as listed.  The sum goes in parts of
+// `part` entries (a multiple of kMixAtOnce), each from zero on, that are then added in their order: four parts where rows share it, so that
+// four wavefronts can form it, one where not.
 struct MixRow {
-  int32_t row, first_entry, n_entries, same;
+  int16_t row, same;
+  int32_t first_entry, n_entries, part;
 };
 struct MixEntry {
   int32_t col;
   float w;
 };
-constexpr int kMixAtOnce = 4;
+constexpr int kMixAtOnce = 4, kMixParts = 4;
 constexpr int kMaxLoopWaves = 16;  // wavefronts of a loop kernel's workgroup
 
 // Pointer tables of the bound buffers of a handle with more than kInlineRows rows or sources: they do not

@@ -112,9 +112,9 @@ __device__ __forceinline__ MixEntry mix_entry(const Lists& l, uint32_t at) {
   return *reinterpret_cast<const MixEntry*>((const MixEntry*)((Constant)l.entries + at));
 }
 
-// The messages of a list times their weights, for a unit's two groups a lane.
+// Messages [first, end) of the lists times their weights, for a unit's two groups a lane.
 template <bool WHOLE, typename A>
-__device__ __forceinline__ void mix_unit(const A& a, const MixRow& r, const Unit& t, const uint32_t (&bits)[2], float (&mixed)[2][4]) {
+__device__ __forceinline__ void mix_unit(const A& a, int32_t first, int32_t end, const Unit& t, const uint32_t (&bits)[2], float (&mixed)[2][4]) {
   uint64_t e[2];
 #pragma unroll
   for (uint32_t k = 0; k < 2; ++k) {
@@ -123,12 +123,12 @@ __device__ __forceinline__ void mix_unit(const A& a, const MixRow& r, const Unit
 #pragma unroll
     for (int j = 0; j < 4; ++j) mixed[k][j] = 0.0f;
   }
-  for (int32_t n = 0; n < r.n_entries; n += kMixAtOnce) {
+  for (int32_t n = first; n < end; n += kMixAtOnce) {
     uint32_t codes[kMixAtOnce][2], scale[kMixAtOnce][2];
     float w[kMixAtOnce];
 #pragma unroll
     for (int q = 0; q < kMixAtOnce; ++q) {
-      const MixEntry entry = mix_entry(a.lists, (uint32_t)(r.first_entry + n + q));
+      const MixEntry entry = mix_entry(a.lists, (uint32_t)(n + q));
       const uint8_t* message = buffer(a.message[entry.col]);
       w[q] = entry.w;
 #pragma unroll
@@ -149,27 +149,22 @@ __device__ __forceinline__ void mix_unit(const A& a, const MixRow& r, const Unit
   }
 }
 
+// What one row does with its neighbours' sum.
 template <typename XT, int MODE, bool WHOLE, bool NT, typename A>
-__device__ __forceinline__ void mix_positions(const A& a, const Unit& t, uint32_t from, uint32_t to) {
-  uint32_t bits[2];
-#pragma unroll
-  for (uint32_t k = 0; k < 2; ++k) bits[k] = WHOLE ? 0xFu : group_bits(a.s.cuts, t.first + k * t.step);
-  float mixed[2][4];
-  for (uint32_t p = from; p < to; ++p) {
-    const RowPointers rp = a.row[p];
-    void* sum = buffer<void, 0>(rp);
-    float s[2][4], c[2][4], x[2][4];
+struct RowUpdate {
+  float s[2][4], c[2][4], x[2][4];
+  __device__ __forceinline__ void load(const A& a, uint32_t p, const Unit& t, const uint32_t (&bits)[2]) {
 #pragma unroll
     for (uint32_t k = 0; k < 2; ++k) {
       const uint64_t e = t.first + k * t.step;
-      if constexpr (MODE != kMixStore) load_group<TF32, WHOLE, NT>(sum, e, bits[k], a.s.d, s[k]);
+      if constexpr (MODE != kMixStore) load_group<TF32, WHOLE, NT>(buffer<const void, 0>(a.row[p]), e, bits[k], a.s.d, s[k]);
       if constexpr (MODE == kMixGossip) {
-        load_group<TF32, WHOLE, NT>(buffer<const void, 1>(rp), e, bits[k], a.s.d, c[k]);
-        load_group<XT, WHOLE, NT>(buffer<const void, 2>(rp), e, bits[k], a.s.d, x[k]);
+        load_group<TF32, WHOLE, NT>(buffer<const void, 1>(a.row[p]), e, bits[k], a.s.d, c[k]);
+        load_group<XT, WHOLE, NT>(buffer<const void, 2>(a.row[p]), e, bits[k], a.s.d, x[k]);
       }
     }
-    const MixRow r = mix_row(a.lists, p);
-    if (p == from || !r.same) mix_unit<WHOLE>(a, r, t, bits, mixed);
+  }
+  __device__ __forceinline__ void store(const A& a, uint32_t p, const Unit& t, const uint32_t (&bits)[2], const float (&mixed)[2][4]) {
 #pragma unroll
     for (uint32_t k = 0; k < 2; ++k) {
       const uint64_t e = t.first + k * t.step;
@@ -178,24 +173,103 @@ __device__ __forceinline__ void mix_positions(const A& a, const Unit& t, uint32_
         s[k][j] = MODE == kMixStore ? mixed[k][j] : s[k][j] + mixed[k][j];
         if constexpr (MODE == kMixGossip) x[k][j] = __builtin_fmaf(a.gamma, s[k][j] - c[k][j], x[k][j]);
       }
-      store_group<TF32, NT>(sum, e, bits[k], s[k]);
-      if constexpr (MODE == kMixGossip) store_group<XT, NT>(buffer<void, 3>(rp), e, bits[k], x[k]);
+      store_group<TF32, NT>(buffer<void, 0>(a.row[p]), e, bits[k], s[k]);
+      if constexpr (MODE == kMixGossip) store_group<XT, NT>(buffer<void, 3>(a.row[p]), e, bits[k], x[k]);
     }
+  }
+};
+
+// The whole sum of a list, part by part.
+template <bool WHOLE, typename A>
+__device__ __forceinline__ void mix_list(const A& a, const MixRow& r, const Unit& t, const uint32_t (&bits)[2], float (&mixed)[2][4]) {
+  mix_unit<WHOLE>(a, r.first_entry, r.first_entry + r.part, t, bits, mixed);
+  for (int32_t n = r.part; n < r.n_entries; n += r.part) {
+    float part[2][4];
+    mix_unit<WHOLE>(a, r.first_entry + n, r.first_entry + (n + r.part < r.n_entries ? n + r.part : r.n_entries), t, bits, part);
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) mixed[k][j] += part[k][j];
   }
 }
 
-// A wavefront takes a unit of `rows_each` positions.  All of them for one unit run on one die, whose L2 then holds the unit's messages.
+template <typename XT, int MODE, bool WHOLE, bool NT, typename A>
+__device__ __forceinline__ void mix_positions(const A& a, const Unit& t, uint32_t from, uint32_t to) {
+  uint32_t bits[2];
+#pragma unroll
+  for (uint32_t k = 0; k < 2; ++k) bits[k] = WHOLE ? 0xFu : group_bits(a.s.cuts, t.first + k * t.step);
+  float mixed[2][4];
+  for (uint32_t p = from; p < to; ++p) {
+    RowUpdate<XT, MODE, WHOLE, NT, A> row;
+    row.load(a, p, t, bits);
+    const MixRow r = mix_row(a.lists, p);
+    if (p == from || !r.same) mix_list<WHOLE>(a, r, t, bits, mixed);
+    row.store(a, p, t, bits, mixed);
+  }
+}
+
+// A wavefront takes a unit of rows_each positions, one after the other; a sum that rows share is formed once for those of them that follow
+// each other.  All positions of a unit run on one die, whose L2 then holds the unit's messages.
 template <typename XT, int MODE, bool NT, int N, int C>
 __global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_mix(const MixArgs<N, C> a) {
-  const uint32_t parts = (a.s.n_rows + a.rows_each - 1) / a.rows_each;
   uint32_t piece, part;
-  const bool active = die_block_piece(blockIdx.x, parts, a.s.n_xcd, (a.s.count + kMixWaves - 1) / kMixWaves, kDieBlockTiles, piece, part);
+  const bool active = die_block_piece(blockIdx.x, (a.s.n_rows + a.rows_each - 1) / a.rows_each, a.s.n_xcd, (a.s.count + kMixWaves - 1) / kMixWaves,
+                                      kDieBlockTiles, piece, part);
   const uint32_t i = a.s.first + piece * kMixWaves + wave_of_group();
   if (active && i < a.s.n_granules) {
     const uint32_t from = part * a.rows_each, to = from + a.rows_each < a.s.n_rows ? from + a.rows_each : a.s.n_rows;
     const Unit t = unit_place<2, NT>(i, a.s, threadIdx.x % kWave);
     if (t.whole) mix_positions<XT, MODE, true, NT>(a, t, from, to);
     else mix_positions<XT, MODE, false, NT>(a, t, from, to);
+  }
+}
+
+// Rows that share their sum: a workgroup takes a unit of `rows_each` positions.  For every run of rows with the same list its wavefronts
+// form a part of the sum each, add the parts up through LDS, all in the same order, and deal the rows among themselves.
+template <typename XT, int MODE, bool WHOLE, bool NT, typename A>
+__device__ __forceinline__ void mix_shared(const A& a, const Unit& t, uint32_t from, uint32_t to, f4 (&parts)[kMixParts][2][kWave]) {
+  static_assert(kMixParts == kMixWaves, "a part a wavefront");
+  const uint32_t lane = threadIdx.x % kWave, wave = wave_of_group();
+  uint32_t bits[2];
+#pragma unroll
+  for (uint32_t k = 0; k < 2; ++k) bits[k] = WHOLE ? 0xFu : group_bits(a.s.cuts, t.first + k * t.step);
+  while (from < to) {
+    const MixRow r = mix_row(a.lists, from);
+    uint32_t end = from + 1;
+    while (end < to && mix_row(a.lists, end).same) ++end;
+    float mixed[2][4];
+    const int32_t n = (int32_t)wave * r.part, last = n + r.part < r.n_entries ? n + r.part : r.n_entries;
+    mix_unit<WHOLE>(a, r.first_entry + n, r.first_entry + last, t, bits, mixed);
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k) parts[wave][k][lane] = f4{mixed[k][0], mixed[k][1], mixed[k][2], mixed[k][3]};
+    __syncthreads();
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k) {
+      f4 sum = parts[0][k][lane];
+      for (int32_t q = 1; q < kMixParts; ++q)
+        if (q * r.part < r.n_entries) sum += parts[q][k][lane];
+      mixed[k][0] = sum.x; mixed[k][1] = sum.y; mixed[k][2] = sum.z; mixed[k][3] = sum.w;
+    }
+    for (uint32_t p = from + wave; p < end; p += kMixWaves) {
+      RowUpdate<XT, MODE, WHOLE, NT, A> row;
+      row.load(a, p, t, bits);
+      row.store(a, p, t, bits, mixed);
+    }
+    __syncthreads();
+    from = end;
+  }
+}
+
+template <typename XT, int MODE, bool NT, int N, int C>
+__global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_shared(const MixArgs<N, C> a) {
+  __shared__ f4 parts[kMixParts][2][kWave];
+  uint32_t i, part;
+  const bool active = die_block_piece(blockIdx.x, (a.s.n_rows + a.rows_each - 1) / a.rows_each, a.s.n_xcd, a.s.count, kDieBlockTiles, i, part);
+  if (active) {
+    const uint32_t from = part * a.rows_each, to = from + a.rows_each < a.s.n_rows ? from + a.rows_each : a.s.n_rows;
+    const Unit t = unit_place<2, NT>(a.s.first + i, a.s, threadIdx.x % kWave);
+    if (t.whole) mix_shared<XT, MODE, true, NT>(a, t, from, to, parts);
+    else mix_shared<XT, MODE, false, NT>(a, t, from, to, parts);
   }
 }
 
@@ -258,19 +332,27 @@ __device__ __forceinline__ void round_unit(const A& a, const Unit& t, uint32_t e
         for (uint32_t k = 0; k < V; ++k)
 #pragma unroll
           for (int j = 0; j < 4; ++j) mixed[k][j] = 0.0f;
-        for (int32_t n = 0; n < r.n_entries; n += kMixAtOnce) {
+        for (int32_t from_n = 0; from_n < r.n_entries; from_n += r.part) {
+          const int32_t to_n = from_n + r.part < r.n_entries ? from_n + r.part : r.n_entries;
+          float part[V][4] = {};
+          for (int32_t n = from_n; n < to_n; n += kMixAtOnce) {
 #pragma unroll
-          for (int m = 0; m < kMixAtOnce; ++m) {
-            const MixEntry entry = mix_entry(a.lists, (uint32_t)(r.first_entry + n + m));
-            const uint8_t* message = lds + entry.col * kRoundMessage<V>;
+            for (int m = 0; m < kMixAtOnce; ++m) {
+              const MixEntry entry = mix_entry(a.lists, (uint32_t)(r.first_entry + n + m));
+              const uint8_t* message = lds + entry.col * kRoundMessage<V>;
 #pragma unroll
-            for (uint32_t k = 0; k < V; ++k) {
-              float value[4];
-              decode(*reinterpret_cast<const uint16_t*>(message + k * 128 + 2 * lane), message[128 * V + k * 8 + lane / 8], value);
+              for (uint32_t k = 0; k < V; ++k) {
+                float value[4];
+                decode(*reinterpret_cast<const uint16_t*>(message + k * 128 + 2 * lane), message[128 * V + k * 8 + lane / 8], value);
 #pragma unroll
-              for (int j = 0; j < 4; ++j) mixed[k][j] = __builtin_fmaf(entry.w, value[j], mixed[k][j]);
+                for (int j = 0; j < 4; ++j) part[k][j] = __builtin_fmaf(entry.w, value[j], part[k][j]);
+              }
             }
           }
+#pragma unroll
+          for (uint32_t k = 0; k < V; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mixed[k][j] = from_n == 0 ? part[k][j] : mixed[k][j] + part[k][j];
         }
       }
 #pragma unroll
@@ -309,28 +391,34 @@ int enqueue_encode(int xdt, EncodeArgs<N> a, void* stream) {
 }
 
 template <int N, int C, bool NT>
-KernelFn mix_kernel(int xdt, MixMode mode) {
-  if (mode == kMixStore) return (KernelFn)k_mx4_mix<TF32, kMixStore, NT, N, C>;
-  if (mode == kMixAdd) return (KernelFn)k_mx4_mix<TF32, kMixAdd, NT, N, C>;
-  return xdt == DADAM_BF16 ? (KernelFn)k_mx4_mix<TBF16, kMixGossip, NT, N, C> : (KernelFn)k_mx4_mix<TF32, kMixGossip, NT, N, C>;
+KernelFn mix_kernel(int xdt, MixMode mode, bool shared) {
+#define DADAM_MIX(XT, MODE) (shared ? (KernelFn)k_mx4_shared<XT, MODE, NT, N, C> : (KernelFn)k_mx4_mix<XT, MODE, NT, N, C>)
+  if (mode == kMixStore) return DADAM_MIX(TF32, kMixStore);
+  if (mode == kMixAdd) return DADAM_MIX(TF32, kMixAdd);
+  return xdt == DADAM_BF16 ? DADAM_MIX(TBF16, kMixGossip) : DADAM_MIX(TF32, kMixGossip);
+#undef DADAM_MIX
 }
 template <int N, int C>
 int enqueue_mix(int xdt, MixMode mode, MixArgs<N, C> a, void* stream) {
-  const KernelFn fn = a.s.streams ? mix_kernel<N, C, true>(xdt, mode) : mix_kernel<N, C, false>(xdt, mode);
-  const uint32_t parts = (a.s.n_rows + a.rows_each - 1) / a.rows_each;
-  return in_pieces(a, kMixWaves * a.s.n_xcd, parts * a.s.n_xcd, kWave * kMixWaves,
+  const bool shared = a.by_group;
+  const KernelFn fn = a.s.streams ? mix_kernel<N, C, true>(xdt, mode, shared) : mix_kernel<N, C, false>(xdt, mode, shared);
+  const uint32_t parts = (a.s.n_rows + a.rows_each - 1) / a.rows_each, units = shared ? 1 : kMixWaves;
+  return in_pieces(a, units * a.s.n_xcd, parts * a.s.n_xcd, kWave * kMixWaves,
                    [&](uint32_t grid) { return enqueue_grid(fn, grid, kWave * kMixWaves, &a, 0, stream); });
 }
 
 // Rows a wavefront holds, and its groups a lane: what 128 registers have room for.
 template <int N, bool NT>
-KernelFn round_kernel(int xdt, uint32_t rows_per_wave) {
+KernelFn round_kernel(int xdt, uint32_t each) {
   const bool b = xdt == DADAM_BF16;
 #define DADAM_ROUND(ROWS, V) (b ? (KernelFn)k_mx4_round<TBF16, ROWS, V, NT, N> : (KernelFn)k_mx4_round<TF32, ROWS, V, NT, N>)
-  if (rows_per_wave <= 1) return DADAM_ROUND(1, 2);
+  if (each <= 1) return DADAM_ROUND(1, 2);
+  if (each <= 2) return DADAM_ROUND(2, 2);
+  if (each <= 3) return DADAM_ROUND(3, 2);
   if constexpr (N > kFewOperands) {
-    if (rows_per_wave <= 2) return DADAM_ROUND(2, 2);
-    if (rows_per_wave <= 4) return DADAM_ROUND(4, 2);
+    if (each <= 4) return DADAM_ROUND(4, 2);
+    if (each <= 6) return DADAM_ROUND(6, 1);
+    if (each <= 8) return DADAM_ROUND(8, 1);
     return DADAM_ROUND(10, 1);
   }
 #undef DADAM_ROUND
@@ -338,7 +426,8 @@ KernelFn round_kernel(int xdt, uint32_t rows_per_wave) {
 }
 template <int N>
 int enqueue_round(int xdt, RoundArgs<N> a, void* stream) {
-  const uint32_t waves = a.s.n_rows < kRoundWaves ? a.s.n_rows : kRoundWaves, each = (a.s.n_rows + waves - 1) / waves;
+  const uint32_t least = (a.s.n_rows + kRoundWaves - 1) / kRoundWaves, most = a.s.n_rows < 3 ? a.s.n_rows : 3;
+  const uint32_t each = a.s.streams && least < most ? most : least, waves = (a.s.n_rows + each - 1) / each;
   const KernelFn fn = a.s.streams ? round_kernel<N, true>(xdt, each) : round_kernel<N, false>(xdt, each);
   if (fn == nullptr) return (int)hipErrorInvalidDeviceFunction;
   const uint32_t units = each <= 4 ? 1 : 2;  // of a granule
@@ -359,7 +448,7 @@ int launch_mix4(int xdt, MixMode mode, uint32_t n_cols, const MixArgs<kMessageRo
   if (a.s.n_rows > (uint32_t)kFewOperands || n_cols > (uint32_t)kFewOperands) return enqueue_mix(xdt, mode, a, stream);
   auto f = few_rows<MixArgs<kFewOperands, kFewOperands>>(a);
   memcpy((void*)f.message, (const void*)a.message, sizeof(f.message));
-  f.s = a.s; f.lists = a.lists; f.scale_offset = a.scale_offset; f.rows_each = a.rows_each; f.gamma = a.gamma;
+  f.s = a.s; f.lists = a.lists; f.scale_offset = a.scale_offset; f.rows_each = a.rows_each; f.by_group = a.by_group; f.gamma = a.gamma;
   return enqueue_mix(xdt, mode, f, stream);
 }
 

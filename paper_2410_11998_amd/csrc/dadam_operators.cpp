@@ -206,13 +206,24 @@ void fill_span(const dadam_handle* h, Span* s) {
 uint64_t blocks_of(const dadam_handle* h) { return (h->cfg.d + kMxBlock - 1) / kMxBlock; }
 size_t message_bytes(const dadam_handle* h) { return (size_t)((blocks_of(h) * 17 + 15) / 16 * 16); }
 
-// Rows of one position after the other that a wavefront takes: rows that share a sum have it formed once for as many of them as leave
-// the chip two rounds of wavefronts.
-constexpr uint64_t kRoundOfWaves = 256 * 32;
-uint32_t rows_each(const dadam_handle* h, const Slot& s, uint32_t n_rows) {
-  if (!s.mix_shared) return 1;
-  const uint64_t parts = (2 * kRoundOfWaves + granules_of(h) - 1) / granules_of(h);  // of the rows, at least
-  return (uint32_t)std::max<uint64_t>(1, n_rows / std::min<uint64_t>(parts, n_rows));
+// Who takes what of a launch of n_rows positions (MixArgs::by_group, rows_each).  Lists that fewer than four rows share on average: a wavefront
+// for every unit and row.  Otherwise products of 1536 granules and more: a wavefront takes a unit of all rows and forms the sum once; all
+// others: a workgroup does, its wavefronts share the list and the rows, and rows are split until there are 4096 workgroups.
+// us, by workgroup / by wavefront, complete graph, product of 100 rows of 4e6 elements 456 / 370, of 1e6 137 / 119, of 4e5 55 / 78, of 32 rows of 4e6 147 / 111,
+// of 2e6 48 / 53, of 4e5 15.5 / 22, of 8 rows of 2e6 18 / 13.5; gossip of 100 rows of 2e6 777 / 845, of 32 rows of 2e6 237 / 259, of 8 rows of 1e6 33 / 35.5.
+constexpr uint64_t kProductGranules = 1536, kSharedGroups = 4096;
+void share_rows(const dadam_handle* h, const Slot& s, MixMode mode, uint32_t n_rows, uint32_t* by_group, uint32_t* rows_each) {
+  const uint64_t granules = granules_of(h);
+  *by_group = 0;
+  *rows_each = 1;
+  if (h->cfg.n_rows < 4 * s.mix_groups) return;
+  if (mode != kMixGossip && granules >= kProductGranules) {
+    *rows_each = n_rows;
+    return;
+  }
+  const uint64_t parts = (kSharedGroups + granules - 1) / granules;
+  *by_group = 1;
+  *rows_each = std::min((uint32_t)((n_rows + parts - 1) / parts + kMixParts - 1) / kMixParts * kMixParts, n_rows);
 }
 
 // Runs the launches of a call whose arguments have passed, with the handle's device current and its state made.
@@ -277,11 +288,12 @@ int mix_impl(dadam_handle* h, uint32_t slot, const void* const* msg, float* cons
   return on_device(h, [&] {
     int e = (int)hipSuccess;
     const Slot& lists = h->slots[slot];
-    for (uint32_t p0 = 0; p0 < R && e == (int)hipSuccess; p0 += kMessageRows) {
+    const uint32_t launches = (R + kMessageRows - 1) / kMessageRows, rows = (R + launches - 1) / launches;
+    for (uint32_t p0 = 0; p0 < R && e == (int)hipSuccess; p0 += rows) {
       MixArgs<kMessageRows, kMaxRows> a;
       memset((void*)&a, 0, sizeof(a));
       fill_span(h, &a.s);
-      a.s.n_rows = std::min<uint32_t>(kMessageRows, R - p0);
+      a.s.n_rows = std::min(rows, R - p0);
       for (uint32_t p = 0; p < a.s.n_rows; ++p) {
         const int32_t i = lists.mix_rows[p0 + p].row;
         put(&a.row[p], 0, sum[i]);
@@ -293,7 +305,7 @@ int mix_impl(dadam_handle* h, uint32_t slot, const void* const* msg, float* cons
       for (uint32_t c = 0; c < C; ++c) put(&a.message[c], msg[c]);
       a.lists = {lists.d_mix_rows + p0, lists.d_mix_entries};
       a.scale_offset = 16 * blocks_of(h);
-      a.rows_each = rows_each(h, lists, a.s.n_rows);
+      share_rows(h, lists, mode, a.s.n_rows, &a.by_group, &a.rows_each);
       a.gamma = gamma;
       e = launch_mix4((int)h->cfg.param_dtype, mode, C, a, stream);
     }

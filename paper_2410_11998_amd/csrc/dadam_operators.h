@@ -74,7 +74,8 @@ struct MixArgs {
   Span s;
   Lists lists;
   uint64_t scale_offset;
-  uint32_t rows_each;  // positions a wavefront takes one after the other
+  uint32_t by_group;   // a workgroup takes a unit (k_mx4_shared), not a wavefront (k_mx4_mix)
+  uint32_t rows_each;  // positions it takes
   float gamma;
 };
 
