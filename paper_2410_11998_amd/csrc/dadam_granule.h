@@ -32,42 +32,67 @@ __device__ __forceinline__ uint32_t cut_of(const Cuts& c, uint32_t granule) {
   typedef const uint32_t __attribute__((address_space(4))) * Constant;
   return c.index ? ((Constant)c.index)[granule] : 0u;
 }
-// Which of the n elements from e on (multiples of n, 4 or 8; inside one granule of the vector) belong to a tensor.
-__device__ __forceinline__ uint32_t stored_bits(const Cuts& c, uint64_t e, int n) {
-  const uint32_t all = (1u << n) - 1, cut = c.index ? c.index[e / kGranule] : 0u;
-  return cut == 0 ? all : (c.masks[cut - 1 + e % kGranule / kMxBlock] >> (e % kMxBlock)) & all;
+// Which of the n elements from e on (multiples of n, 4 or 8) belong to a tensor; none behind the vector.
+__device__ __forceinline__ uint32_t stored_bits(const Cuts& c, uint64_t d, uint64_t e, int n) {
+  const uint32_t all = (1u << n) - 1, cut = c.index && e < d ? c.index[e / kGranule] : 0u;
+  return e >= d ? 0u : cut == 0 ? all : (c.masks[cut - 1 + e % kGranule / kMxBlock] >> (e % kMxBlock)) & all;
 }
-__device__ __forceinline__ uint32_t group_bits(const Cuts& c, uint64_t e) { return stored_bits(c, e, 4); }
 
-// Where a wavefront's unit of 512 elements (V = 2) or 256 (V = 1) lies: lane l holds V groups of four from `first` on, `step` apart; eight
-// lanes side by side hold a block of 32 elements.  In order: one run.  SPREAD: as streaming kernels have it (see lane_start, V vectors a
-// lane), the two halves of the wavefront work 8192 V elements apart, in blocks of twice that many elements that lie inside the vector.
-struct Unit {
-  uint64_t first;
+// Where a wavefront's unit of 512 elements (V = 2) or 256 (V = 1) lies: lane l holds V groups of four from a place of its own on, 64 or 256
+// elements apart; eight lanes side by side hold a block of 32 elements.  In order: one run.  SPREAD: as streaming kernels have it (see lane_start, V
+// vectors a lane), the two halves of the wavefront work 8192 V elements apart, in blocks of twice that many elements that lie inside
+// the vector.  A wavefront takes U units at a time, side by side; those behind the vector have no element.
+// Places count from `base`, the same for all lanes: addresses are then a scalar and 32 bits a lane.
+template <int V, int U>
+struct Units {
+  uint64_t base;     // a multiple of kGranule, below d
+  uint32_t left;     // elements from there to the end of the vector (2^31 - 1: so many or more)
+  uint32_t first[U];
   uint32_t step;
-  bool whole;  // no padding in it
+  bool whole;        // no padding in them
+  __device__ __forceinline__ uint32_t at(uint32_t k) const { return first[k / V] + k % V * step; }  // group k of the lane's U V
+  __device__ __forceinline__ Units<V, 1> one(uint32_t u) const { return {base, left, {first[u]}, step, whole}; }
+  __device__ __forceinline__ uint32_t bits(const Cuts& c, uint64_t d, uint32_t k) const { return stored_bits(c, d, base + at(k), 4); }
 };
 template <int V>
 constexpr uint32_t kUnitElems = 256 * V;
-template <int V, bool SPREAD>
-__device__ __forceinline__ Unit unit_place(uint32_t i, const Span& s, uint32_t lane) {
+template <int V, bool SPREAD, int U = 1>
+__device__ __forceinline__ Units<V, U> units_from(uint32_t i, const Span& s, uint32_t lane) {
   constexpr uint32_t kFar = 8192 * V, kUnits = 2 * kFar / kUnitElems<V>;
+  static_assert(kUnits % U == 0, "units side by side lie in one block");
   const uint64_t block = (uint64_t)(i & ~(kUnits - 1)) * kUnitElems<V>;
-  if (SPREAD && block + 2 * kFar <= s.d) {
-    const uint32_t at = (i % kUnits) * (kUnitElems<V> / 2);
-    const uint32_t granule = (uint32_t)((block + at) / kGranule);
-    const uint32_t near = V == 2 ? 4 * (lane & 15) + 8 * (lane & 16) : 4 * (lane & 31);
-    return {block + at + near + (lane >> 5) * kFar, 64, (cut_of(s.cuts, granule) | cut_of(s.cuts, granule + kFar / kGranule)) == 0};
+  const bool spread = SPREAD && block + 2 * kFar <= s.d;
+  Units<V, U> units;
+  units.base = spread ? block : (uint64_t)i * kUnitElems<V> / kGranule * kGranule;
+  units.left = s.d - units.base < 0x7FFFFFFFu ? (uint32_t)(s.d - units.base) : 0x7FFFFFFFu;
+  units.step = spread ? 64 : 256;
+  units.whole = true;
+  const uint32_t granule = (uint32_t)(units.base / kGranule);
+#pragma unroll
+  for (uint32_t u = 0; u < U; ++u) {
+    if (spread) {
+      const uint32_t at = (i % kUnits + u) * (kUnitElems<V> / 2);
+      units.first[u] = at + (V == 2 ? 4 * (lane & 15) + 8 * (lane & 16) : 4 * (lane & 31)) + (lane >> 5) * kFar;
+      units.whole &= (cut_of(s.cuts, granule + at / kGranule) | cut_of(s.cuts, granule + (at + kFar) / kGranule)) == 0;
+    } else {
+      const uint32_t at = (uint32_t)((uint64_t)i * kUnitElems<V> - units.base) + u * kUnitElems<V>;
+      units.first[u] = at + 4 * lane;
+      units.whole &= at < units.left && cut_of(s.cuts, granule + at / kGranule) == 0;
+    }
   }
-  const uint64_t first = (uint64_t)i * kUnitElems<V>;
-  return {first + 4 * lane, 256, cut_of(s.cuts, (uint32_t)(first / kGranule)) == 0};
+  return units;
 }
+// Where the elements of a buffer begin that units count from.
+template <typename T>
+__device__ __forceinline__ const void* based(const void* buffer, uint64_t base) { return static_cast<const char*>(buffer) + base * T::bytes; }
+template <typename T>
+__device__ __forceinline__ void* based(void* buffer, uint64_t base) { return static_cast<char*>(buffer) + base * T::bytes; }
 
-// A lane's group of four elements from e on (a multiple of 4), widened to float.  Elements that `bits` leaves out read as zero: whole groups
-// are loaded wherever they end within the d elements of the buffer, so that no load waits for the masks.
+// A lane's group of four elements at e (a multiple of 4), widened to float.  Elements that `bits` leaves out read as zero: whole groups
+// are loaded wherever they end within the buffer (`left` elements), so that no load waits for the masks.
 template <typename T, bool WHOLE, bool NT>
-__device__ __forceinline__ void load_group(const void* base, uint64_t e, uint32_t bits, uint64_t d, float (&v)[4]) {
-  if (WHOLE || e + 4 <= d) {
+__device__ __forceinline__ void load_group(const void* base, uint32_t e, uint32_t bits, uint32_t left, float (&v)[4]) {
+  if (WHOLE || e + 4 <= left) {
     if constexpr (T::bytes == 4) {
       const f4 x = vload<NT>(reinterpret_cast<const f4*>(at<float>(base, e)));
       v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
@@ -78,7 +103,7 @@ __device__ __forceinline__ void load_group(const void* base, uint64_t e, uint32_
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = bits >> j & 1 ? load_elem<T>(base, e + j) : 0.0f;
+    for (uint32_t j = 0; j < 4; ++j) v[j] = bits >> j & 1 ? load_elem<T>(at<typename T::elem>(base, e), j) : 0.0f;
   }
   if constexpr (!WHOLE) {
 #pragma unroll
@@ -87,7 +112,7 @@ __device__ __forceinline__ void load_group(const void* base, uint64_t e, uint32_
 }
 
 template <typename T, bool NT>
-__device__ __forceinline__ void store_group(void* base, uint64_t e, uint32_t bits, const float (&v)[4]) {
+__device__ __forceinline__ void store_group(void* base, uint32_t e, uint32_t bits, const float (&v)[4]) {
   if (bits == 0xFu) {
     if constexpr (T::bytes == 4) {
       const f4 x = {v[0], v[1], v[2], v[3]};
@@ -99,7 +124,7 @@ __device__ __forceinline__ void store_group(void* base, uint64_t e, uint32_t bit
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (bits >> j & 1) store_elem<T>(base, e + j, v[j]);
+      if (bits >> j & 1) store_elem<T>(at<typename T::elem>(base, e), j, v[j]);
   }
 }
 
@@ -134,10 +159,10 @@ int in_pieces(Args& a, uint32_t per, uint32_t groups, uint32_t threads, Launch l
   while (left > 0 && e == (int)hipSuccess) {
     const uint64_t works = (left + per - 1) / per;
     const uint32_t now = works < most ? (uint32_t)works : most;
+    a.s.count = (uint32_t)((uint64_t)now * per < left ? (uint64_t)now * per : left);  // kernels number the pieces of their launch
     e = launch(now * groups);
-    const uint64_t done = (uint64_t)now * per < left ? (uint64_t)now * per : left;
-    a.s.first += (uint32_t)done;
-    left -= done;
+    a.s.first += a.s.count;
+    left -= a.s.count;
   }
   return e;
 }

@@ -40,8 +40,8 @@ struct Slot {
   const Loop* d_loops = nullptr;
   std::vector<MixRow> mix_rows;       // see MixRow
   std::vector<MixEntry> mix_entries;
-  uint32_t mix_groups = 0;            // different lists
-  const MixRow* d_mix_rows = nullptr;
+  std::vector<MixRow> mix_firsts;     // the first row of every list
+  const MixRow *d_mix_rows = nullptr, *d_mix_firsts = nullptr;
   const MixEntry* d_mix_entries = nullptr;
 };
 

@@ -814,7 +814,7 @@ void find_mix_rows(uint32_t R, Slot& s) {
     const int32_t all = (int32_t)s.mix_entries.size() - first, step = kMixAtOnce * (rows.size() > 1 ? kMixParts : 1);
     const int32_t part = rows.size() > 1 ? (all + step - 1) / step * kMixAtOnce : all;
     for (int32_t row : rows) s.mix_rows.push_back({(int16_t)row, (int16_t)(row != (int32_t)i), first, n, part});
-    ++s.mix_groups;
+    s.mix_firsts.push_back({(int16_t)i, 0, first, n, part});
   }
 }
 
@@ -843,7 +843,7 @@ hipError_t upload_lists(const dadam_handle* h, Slot& s, const std::vector<int32_
   const bool has_loops = !s.loops.empty();
   const size_t l = has_loops ? add(s.loops) : 0, lc = has_loops ? add(loop_col) : 0, lww = has_loops ? add(loop_w) : 0,
                lr = has_loops ? add(loop_rows) : 0;
-  const size_t mix_rows = add(s.mix_rows), mix_entries = add(s.mix_entries);
+  const size_t mix_rows = add(s.mix_rows), mix_firsts = add(s.mix_firsts), mix_entries = add(s.mix_entries);
   hipError_t e = hipMalloc((void**)&s.d_lists, image.size());
   if (e == hipSuccess) e = hipMemcpy(s.d_lists, image.data(), image.size(), hipMemcpyHostToDevice);
   if (e != hipSuccess) return e;
@@ -856,6 +856,7 @@ hipError_t upload_lists(const dadam_handle* h, Slot& s, const std::vector<int32_
     s.d_loop_col = ints(lc); s.d_loop_w = floats(lww); s.d_loop_rows = ints(lr);
   }
   s.d_mix_rows = reinterpret_cast<const MixRow*>(s.d_lists + mix_rows);
+  s.d_mix_firsts = reinterpret_cast<const MixRow*>(s.d_lists + mix_firsts);
   s.d_mix_entries = reinterpret_cast<const MixEntry*>(s.d_lists + mix_entries);
   return hipSuccess;
 }

@@ -52,38 +52,41 @@ __device__ __forceinline__ void encode(const float (&u)[4], uint32_t& codes, uin
 }
 
 template <typename XT, bool WHOLE, bool NT>
-__device__ __forceinline__ void encode_unit(const Cuts& cuts, uint64_t d, const Unit& t, const RowPointers& p, uint64_t scale_offset) {
-  const void* x = buffer<const void, 0>(p);
-  const void* before = buffer<const void, 1>(p);
-  void* behind = buffer<void, 2>(p);
-  uint8_t* message = buffer<uint8_t, 3>(p);
+__device__ __forceinline__ void encode_unit(const Cuts& cuts, uint64_t d, const Units<2, 1>& t, const RowPointers& p, uint64_t scale_offset) {
+  const void* x = based<XT>(buffer<const void, 0>(p), t.base);
+  const bool differs = buffer<const void, 1>(p) != nullptr, moves = buffer<void, 2>(p) != nullptr;
+  const void* before = based<TF32>(buffer<const void, 1>(p), t.base);
+  void* behind = based<TF32>(buffer<void, 2>(p), t.base);
+  uint8_t* codes_to = buffer<uint8_t, 3>(p) + t.base / 2;
+  uint8_t* scales_to = buffer<uint8_t, 3>(p) + scale_offset + t.base / kMxBlock;
+  const uint32_t end = (uint32_t)(2 * scale_offset - t.base < 0x7FFFFFFFu ? 2 * scale_offset - t.base : 0x7FFFFFFFu);  // of the last block
   float u[2][4], copy[2][4] = {};
   uint32_t bits[2];
 #pragma unroll
   for (uint32_t k = 0; k < 2; ++k) {
-    bits[k] = WHOLE ? 0xFu : group_bits(cuts, t.first + k * t.step);
-    load_group<XT, WHOLE, NT>(x, t.first + k * t.step, bits[k], d, u[k]);
+    bits[k] = WHOLE ? 0xFu : t.bits(cuts, d, k);
+    load_group<XT, WHOLE, NT>(x, t.at(k), bits[k], t.left, u[k]);
   }
-  if (before) {
+  if (differs) {
 #pragma unroll
-    for (uint32_t k = 0; k < 2; ++k) load_group<TF32, WHOLE, NT>(before, t.first + k * t.step, bits[k], d, copy[k]);
+    for (uint32_t k = 0; k < 2; ++k) load_group<TF32, WHOLE, NT>(before, t.at(k), bits[k], t.left, copy[k]);
   }
 #pragma unroll
   for (uint32_t k = 0; k < 2; ++k) {
-    const uint64_t e = t.first + k * t.step;
-    if (before) {
+    const uint32_t e = t.at(k);
+    if (differs) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) u[k][j] -= copy[k][j];
     }
     uint32_t codes, scale;
     float value[4];
     encode(u[k], codes, scale, value);
-    if (WHOLE || e / 2 < scale_offset) {  // blocks end behind the vector where d is no multiple of 32, granules behind the blocks
-      *reinterpret_cast<uint16_t*>(message + e / 2) = (uint16_t)codes;
-      if (threadIdx.x % 8 == 0) message[scale_offset + e / kMxBlock] = (uint8_t)scale;
+    if (WHOLE || e < end) {  // blocks end behind the vector where d is no multiple of 32, granules behind the blocks
+      *reinterpret_cast<uint16_t*>(codes_to + e / 2) = (uint16_t)codes;
+      if (threadIdx.x % 8 == 0) scales_to[e / kMxBlock] = (uint8_t)scale;
     }
-    if (behind) {
-      if (before) {
+    if (moves) {
+      if (differs) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) value[j] = copy[k][j] + value[j];
       }
@@ -95,9 +98,11 @@ __device__ __forceinline__ void encode_unit(const Cuts& cuts, uint64_t d, const 
 template <typename XT, bool NT, int N>
 __global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_encode(const EncodeArgs<N> a) {
   const uint32_t lane = threadIdx.x % kWave;
-  const uint32_t row = blockIdx.x % a.s.n_rows, i = a.s.first + blockIdx.x / a.s.n_rows * kMixWaves + wave_of_group();
-  if (i < a.s.n_granules) {
-    const Unit t = unit_place<2, NT>(i, a.s, lane);
+  uint32_t piece, row;
+  const bool active = die_block_piece(blockIdx.x, a.s.n_rows, a.s.n_xcd, (a.s.count + kMixWaves - 1) / kMixWaves, kDieBlockTiles, piece, row, a.s.run);
+  const uint32_t i = a.s.first + piece * kMixWaves + wave_of_group();
+  if (active && i < a.s.n_granules) {
+    const Units<2, 1> t = units_from<2, NT>(i, a.s, lane);
     if (t.whole) encode_unit<XT, true, NT>(a.s.cuts, a.s.d, t, a.row[row], a.scale_offset);
     else encode_unit<XT, false, NT>(a.s.cuts, a.s.d, t, a.row[row], a.scale_offset);
   }
@@ -112,146 +117,205 @@ __device__ __forceinline__ MixEntry mix_entry(const Lists& l, uint32_t at) {
   return *reinterpret_cast<const MixEntry*>((const MixEntry*)((Constant)l.entries + at));
 }
 
-// Messages [first, end) of the lists times their weights, for a unit's two groups a lane.
-template <bool WHOLE, typename A>
-__device__ __forceinline__ void mix_unit(const A& a, int32_t first, int32_t end, const Unit& t, const uint32_t (&bits)[2], float (&mixed)[2][4]) {
-  uint64_t e[2];
+// Messages [first, end) of the lists times their weights, for a lane's G groups.
+template <bool WHOLE, int U, int G, typename A>
+__device__ __forceinline__ void mix_unit(const A& a, int32_t first, int32_t end, const Units<2, U>& t, const uint32_t (&bits)[G], float (&mixed)[G][4]) {
+  uint32_t e[G];
 #pragma unroll
-  for (uint32_t k = 0; k < 2; ++k) {
-    // groups without an element may lie behind the message: their lanes look at its beginning instead
-    e[k] = WHOLE || bits[k] != 0 ? t.first + k * t.step : 0;
+  for (uint32_t k = 0; k < G; ++k) {
+    // groups without an element may lie behind the message: their lanes look at what the units count from instead
+    e[k] = WHOLE || bits[k] != 0 ? t.at(k) : 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) mixed[k][j] = 0.0f;
   }
   for (int32_t n = first; n < end; n += kMixAtOnce) {
-    uint32_t codes[kMixAtOnce][2], scale[kMixAtOnce][2];
+    uint32_t codes[kMixAtOnce][G], scale[kMixAtOnce][G];
     float w[kMixAtOnce];
 #pragma unroll
     for (int q = 0; q < kMixAtOnce; ++q) {
       const MixEntry entry = mix_entry(a.lists, (uint32_t)(n + q));
-      const uint8_t* message = buffer(a.message[entry.col]);
       w[q] = entry.w;
+      if (n + q >= end) continue;
+      const uint8_t* message = buffer(a.message[entry.col]) + t.base / 2;
+      const uint8_t* scales = buffer(a.message[entry.col]) + a.scale_offset + t.base / kMxBlock;
 #pragma unroll
-      for (uint32_t k = 0; k < 2; ++k) {
+      for (uint32_t k = 0; k < G; ++k) {
         codes[q][k] = *reinterpret_cast<const uint16_t*>(message + e[k] / 2);
-        scale[q][k] = message[a.scale_offset + e[k] / kMxBlock];
+        scale[q][k] = scales[e[k] / kMxBlock];
       }
     }
 #pragma unroll
-    for (int q = 0; q < kMixAtOnce; ++q)
+    for (int q = 0; q < kMixAtOnce; ++q) {
+      if (n + q >= end) continue;
 #pragma unroll
-      for (uint32_t k = 0; k < 2; ++k) {
+      for (uint32_t k = 0; k < G; ++k) {
         float value[4];
         decode(codes[q][k], scale[q][k], value);
 #pragma unroll
         for (int j = 0; j < 4; ++j) mixed[k][j] = __builtin_fmaf(w[q], value[j], mixed[k][j]);
       }
+    }
   }
 }
 
 // What one row does with its neighbours' sum.
-template <typename XT, int MODE, bool WHOLE, bool NT, typename A>
+template <typename XT, int MODE, int U, bool WHOLE, bool NT, typename A>
 struct RowUpdate {
-  float s[2][4], c[2][4], x[2][4];
-  __device__ __forceinline__ void load(const A& a, uint32_t p, const Unit& t, const uint32_t (&bits)[2]) {
+  static constexpr int G = 2 * U;
+  float s[G][4], c[G][4], x[G][4];
+  __device__ __forceinline__ void load(const A& a, uint32_t p, const Units<2, U>& t, const uint32_t (&bits)[G]) {
 #pragma unroll
-    for (uint32_t k = 0; k < 2; ++k) {
-      const uint64_t e = t.first + k * t.step;
-      if constexpr (MODE != kMixStore) load_group<TF32, WHOLE, NT>(buffer<const void, 0>(a.row[p]), e, bits[k], a.s.d, s[k]);
+    for (uint32_t k = 0; k < G; ++k) {
+      const uint32_t e = t.at(k);
+      if constexpr (MODE != kMixStore) load_group<TF32, WHOLE, NT>(based<TF32>(buffer<const void, 0>(a.row[p]), t.base), e, bits[k], t.left, s[k]);
       if constexpr (MODE == kMixGossip) {
-        load_group<TF32, WHOLE, NT>(buffer<const void, 1>(a.row[p]), e, bits[k], a.s.d, c[k]);
-        load_group<XT, WHOLE, NT>(buffer<const void, 2>(a.row[p]), e, bits[k], a.s.d, x[k]);
+        load_group<TF32, WHOLE, NT>(based<TF32>(buffer<const void, 1>(a.row[p]), t.base), e, bits[k], t.left, c[k]);
+        load_group<XT, WHOLE, NT>(based<XT>(buffer<const void, 2>(a.row[p]), t.base), e, bits[k], t.left, x[k]);
       }
     }
   }
-  __device__ __forceinline__ void store(const A& a, uint32_t p, const Unit& t, const uint32_t (&bits)[2], const float (&mixed)[2][4]) {
+  __device__ __forceinline__ void store(const A& a, uint32_t p, const Units<2, U>& t, const uint32_t (&bits)[G], const float (&mixed)[G][4]) {
 #pragma unroll
-    for (uint32_t k = 0; k < 2; ++k) {
-      const uint64_t e = t.first + k * t.step;
+    for (uint32_t k = 0; k < G; ++k) {
+      const uint32_t e = t.at(k);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         s[k][j] = MODE == kMixStore ? mixed[k][j] : s[k][j] + mixed[k][j];
         if constexpr (MODE == kMixGossip) x[k][j] = __builtin_fmaf(a.gamma, s[k][j] - c[k][j], x[k][j]);
       }
-      store_group<TF32, NT>(buffer<void, 0>(a.row[p]), e, bits[k], s[k]);
-      if constexpr (MODE == kMixGossip) store_group<XT, NT>(buffer<void, 3>(a.row[p]), e, bits[k], x[k]);
+      store_group<TF32, NT>(based<TF32>(buffer<void, 0>(a.row[p]), t.base), e, bits[k], s[k]);
+      if constexpr (MODE == kMixGossip) store_group<XT, NT>(based<XT>(buffer<void, 3>(a.row[p]), t.base), e, bits[k], x[k]);
     }
   }
 };
 
 // The whole sum of a list, part by part.
-template <bool WHOLE, typename A>
-__device__ __forceinline__ void mix_list(const A& a, const MixRow& r, const Unit& t, const uint32_t (&bits)[2], float (&mixed)[2][4]) {
-  mix_unit<WHOLE>(a, r.first_entry, r.first_entry + r.part, t, bits, mixed);
+template <bool WHOLE, int U, int G, typename A>
+__device__ __forceinline__ void mix_list(const A& a, const MixRow& r, const Units<2, U>& t, const uint32_t (&bits)[G], float (&mixed)[G][4]) {
+  mix_unit<WHOLE>(a, r.first_entry, r.first_entry + (r.part < r.n_entries ? r.part : r.n_entries), t, bits, mixed);
   for (int32_t n = r.part; n < r.n_entries; n += r.part) {
-    float part[2][4];
+    float part[G][4];
     mix_unit<WHOLE>(a, r.first_entry + n, r.first_entry + (n + r.part < r.n_entries ? n + r.part : r.n_entries), t, bits, part);
 #pragma unroll
-    for (uint32_t k = 0; k < 2; ++k)
+    for (uint32_t k = 0; k < G; ++k)
 #pragma unroll
       for (int j = 0; j < 4; ++j) mixed[k][j] += part[k][j];
   }
 }
 
+template <typename XT, int MODE, bool WHOLE, bool NT, int U, typename A>
+__device__ __forceinline__ void mix_position(const A& a, const Units<2, U>& t, uint32_t p) {
+  constexpr int G = 2 * U;
+  uint32_t bits[G];
+#pragma unroll
+  for (uint32_t k = 0; k < G; ++k) bits[k] = WHOLE ? 0xFu : t.bits(a.s.cuts, a.s.d, k);
+  float mixed[G][4];
+  RowUpdate<XT, MODE, U, WHOLE, NT, A> row;
+  row.load(a, p, t, bits);
+  mix_list<WHOLE>(a, mix_row(a.lists, p), t, bits, mixed);
+  row.store(a, p, t, bits, mixed);
+}
+
+// A wavefront takes kMixUnits units of one row.  All rows of a unit run on one die, whose L2 then holds the unit's messages; where handles stream
+// a die walks runs of units row after row.  Two units where nothing but messages is read: their loads are then twice as many (us, one unit /
+// two, ring of 8 of 3e7 elements 268 / 216, exp. graph of 16 of 2e7 420 / 333, four 430; adding 315 / 390, 458 / 512: their registers leave too few wavefronts).
+template <int MODE>
+constexpr uint32_t kMixUnits = MODE == kMixStore ? 2 : 1;
+template <typename XT, int MODE, bool NT, int N, int C>
+__global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_mix(const MixArgs<N, C> a) {
+  constexpr uint32_t U = kMixUnits<MODE>;
+  uint32_t piece, p;
+  const bool active = die_block_piece(blockIdx.x, a.s.n_rows, a.s.n_xcd, (a.s.count + kMixWaves * U - 1) / (kMixWaves * U), kDieBlockTiles, piece, p, a.s.run);
+  const uint32_t i = a.s.first + (piece * kMixWaves + wave_of_group()) * U;
+  if (active && i < a.s.n_granules) {
+    const Units<2, U> t = units_from<2, NT, U>(i, a.s, threadIdx.x % kWave);
+    if (t.whole) mix_position<XT, MODE, true, NT>(a, t, p);
+    else mix_position<XT, MODE, false, NT>(a, t, p);
+  }
+}
+
+// Rows that share their sum, products of many granules: a wavefront takes a unit of all rows and forms the sums once.  (Two or four units, so that
+// more of a row is written at a time, change nothing for 32 rows and lose 10 to 30 % for 100.)
 template <typename XT, int MODE, bool WHOLE, bool NT, typename A>
-__device__ __forceinline__ void mix_positions(const A& a, const Unit& t, uint32_t from, uint32_t to) {
+__device__ __forceinline__ void mix_rows(const A& a, const Units<2, 1>& t) {
   uint32_t bits[2];
 #pragma unroll
-  for (uint32_t k = 0; k < 2; ++k) bits[k] = WHOLE ? 0xFu : group_bits(a.s.cuts, t.first + k * t.step);
+  for (uint32_t k = 0; k < 2; ++k) bits[k] = WHOLE ? 0xFu : t.bits(a.s.cuts, a.s.d, k);
   float mixed[2][4];
-  for (uint32_t p = from; p < to; ++p) {
-    RowUpdate<XT, MODE, WHOLE, NT, A> row;
+  for (uint32_t p = 0; p < a.s.n_rows; ++p) {
+    RowUpdate<XT, MODE, 1, WHOLE, NT, A> row;
     row.load(a, p, t, bits);
     const MixRow r = mix_row(a.lists, p);
-    if (p == from || !r.same) mix_list<WHOLE>(a, r, t, bits, mixed);
+    if (p == 0 || !r.same) mix_list<WHOLE>(a, r, t, bits, mixed);
     row.store(a, p, t, bits, mixed);
   }
 }
 
-// A wavefront takes a unit of rows_each positions, one after the other; a sum that rows share is formed once for those of them that follow
-// each other.  All positions of a unit run on one die, whose L2 then holds the unit's messages.
-template <typename XT, int MODE, bool NT, int N, int C>
-__global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_mix(const MixArgs<N, C> a) {
-  uint32_t piece, part;
-  const bool active = die_block_piece(blockIdx.x, (a.s.n_rows + a.rows_each - 1) / a.rows_each, a.s.n_xcd, (a.s.count + kMixWaves - 1) / kMixWaves,
-                                      kDieBlockTiles, piece, part);
+template <int MODE, bool NT, int N, int C>
+__global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_products(const MixArgs<N, C> a) {
+  const uint32_t pieces = (a.s.count + kMixWaves - 1) / kMixWaves;
+  const uint32_t i = a.s.first + die_block_order(blockIdx.x, pieces, a.s.n_xcd, kDieBlockTiles) * kMixWaves + wave_of_group();
+  if (i < a.s.n_granules) {
+    const Units<2, 1> t = units_from<2, NT>(i, a.s, threadIdx.x % kWave);
+    if (t.whole) mix_rows<TF32, MODE, true, NT>(a, t);
+    else mix_rows<TF32, MODE, false, NT>(a, t);
+  }
+}
+
+// The other rows of products that share their sum, from the row that has it.
+template <bool WHOLE, bool NT, typename A>
+__device__ __forceinline__ void copy_unit(const A& a, const Units<2, 1>& t, const RowPointers& p) {
+  uint32_t bits[2];
+  float v[2][4];
+#pragma unroll
+  for (uint32_t k = 0; k < 2; ++k) {
+    bits[k] = WHOLE ? 0xFu : t.bits(a.s.cuts, a.s.d, k);
+    load_group<TF32, WHOLE, false>(based<TF32>(buffer<const void, 1>(p), t.base), t.at(k), bits[k], t.left, v[k]);
+  }
+#pragma unroll
+  for (uint32_t k = 0; k < 2; ++k) store_group<TF32, NT>(based<TF32>(buffer<void, 0>(p), t.base), t.at(k), bits[k], v[k]);
+}
+template <bool NT, int N, int C>
+__global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_copy(const MixArgs<N, C> a) {
+  uint32_t piece, p;
+  const bool active = die_block_piece(blockIdx.x, a.s.n_rows, a.s.n_xcd, (a.s.count + kMixWaves - 1) / kMixWaves, kDieBlockTiles, piece, p, a.s.run);
   const uint32_t i = a.s.first + piece * kMixWaves + wave_of_group();
   if (active && i < a.s.n_granules) {
-    const uint32_t from = part * a.rows_each, to = from + a.rows_each < a.s.n_rows ? from + a.rows_each : a.s.n_rows;
-    const Unit t = unit_place<2, NT>(i, a.s, threadIdx.x % kWave);
-    if (t.whole) mix_positions<XT, MODE, true, NT>(a, t, from, to);
-    else mix_positions<XT, MODE, false, NT>(a, t, from, to);
+    const Units<2, 1> t = units_from<2, NT>(i, a.s, threadIdx.x % kWave);
+    if (t.whole) copy_unit<true, NT>(a, t, a.row[p]);
+    else copy_unit<false, NT>(a, t, a.row[p]);
   }
 }
 
 // Rows that share their sum: a workgroup takes a unit of `rows_each` positions.  For every run of rows with the same list its wavefronts
 // form a part of the sum each, add the parts up through LDS, all in the same order, and deal the rows among themselves.
 template <typename XT, int MODE, bool WHOLE, bool NT, typename A>
-__device__ __forceinline__ void mix_shared(const A& a, const Unit& t, uint32_t from, uint32_t to, f4 (&parts)[kMixParts][2][kWave]) {
+__device__ __forceinline__ void mix_shared(const A& a, const Units<2, 1>& t, uint32_t from, uint32_t to, f4 (&parts)[kMixParts][2][kWave]) {
   static_assert(kMixParts == kMixWaves, "a part a wavefront");
   const uint32_t lane = threadIdx.x % kWave, wave = wave_of_group();
-  uint32_t bits[2];
+  constexpr int G = 2;
+  uint32_t bits[G];
 #pragma unroll
-  for (uint32_t k = 0; k < 2; ++k) bits[k] = WHOLE ? 0xFu : group_bits(a.s.cuts, t.first + k * t.step);
+  for (uint32_t k = 0; k < G; ++k) bits[k] = WHOLE ? 0xFu : t.bits(a.s.cuts, a.s.d, k);
   while (from < to) {
     const MixRow r = mix_row(a.lists, from);
     uint32_t end = from + 1;
     while (end < to && mix_row(a.lists, end).same) ++end;
-    float mixed[2][4];
+    float mixed[G][4];
     const int32_t n = (int32_t)wave * r.part, last = n + r.part < r.n_entries ? n + r.part : r.n_entries;
     mix_unit<WHOLE>(a, r.first_entry + n, r.first_entry + last, t, bits, mixed);
 #pragma unroll
-    for (uint32_t k = 0; k < 2; ++k) parts[wave][k][lane] = f4{mixed[k][0], mixed[k][1], mixed[k][2], mixed[k][3]};
+    for (uint32_t k = 0; k < G; ++k) parts[wave][k][lane] = f4{mixed[k][0], mixed[k][1], mixed[k][2], mixed[k][3]};
     __syncthreads();
 #pragma unroll
-    for (uint32_t k = 0; k < 2; ++k) {
+    for (uint32_t k = 0; k < G; ++k) {
       f4 sum = parts[0][k][lane];
       for (int32_t q = 1; q < kMixParts; ++q)
         if (q * r.part < r.n_entries) sum += parts[q][k][lane];
       mixed[k][0] = sum.x; mixed[k][1] = sum.y; mixed[k][2] = sum.z; mixed[k][3] = sum.w;
     }
     for (uint32_t p = from + wave; p < end; p += kMixWaves) {
-      RowUpdate<XT, MODE, WHOLE, NT, A> row;
+      RowUpdate<XT, MODE, 1, WHOLE, NT, A> row;
       row.load(a, p, t, bits);
       row.store(a, p, t, bits, mixed);
     }
@@ -264,10 +328,10 @@ template <typename XT, int MODE, bool NT, int N, int C>
 __global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_shared(const MixArgs<N, C> a) {
   __shared__ f4 parts[kMixParts][2][kWave];
   uint32_t i, part;
-  const bool active = die_block_piece(blockIdx.x, (a.s.n_rows + a.rows_each - 1) / a.rows_each, a.s.n_xcd, a.s.count, kDieBlockTiles, i, part);
+  const bool active = die_block_piece(blockIdx.x, (a.s.n_rows + a.rows_each - 1) / a.rows_each, a.s.n_xcd, a.s.count, kDieBlockTiles, i, part, a.s.run);
   if (active) {
     const uint32_t from = part * a.rows_each, to = from + a.rows_each < a.s.n_rows ? from + a.rows_each : a.s.n_rows;
-    const Unit t = unit_place<2, NT>(a.s.first + i, a.s, threadIdx.x % kWave);
+    const Units<2, 1> t = units_from<2, NT>(a.s.first + i, a.s, threadIdx.x % kWave);
     if (t.whole) mix_shared<XT, MODE, true, NT>(a, t, from, to, parts);
     else mix_shared<XT, MODE, false, NT>(a, t, from, to, parts);
   }
@@ -280,11 +344,11 @@ constexpr uint32_t kRoundMessage = kUnitElems<V> / 2 + kUnitElems<V> / kMxBlock;
 constexpr uint32_t kRoundWaves = 16;
 
 template <typename XT, int ROWS, int V, bool WHOLE, bool NT, typename A>
-__device__ __forceinline__ void round_unit(const A& a, const Unit& t, uint32_t each, uint8_t* lds) {
+__device__ __forceinline__ void round_unit(const A& a, const Units<V, 1>& t, uint32_t each, uint8_t* lds) {
   const uint32_t lane = threadIdx.x % kWave, from = wave_of_group() * each;
   uint32_t bits[V];
 #pragma unroll
-  for (uint32_t k = 0; k < V; ++k) bits[k] = WHOLE ? 0xFu : group_bits(a.s.cuts, t.first + k * t.step);
+  for (uint32_t k = 0; k < V; ++k) bits[k] = WHOLE ? 0xFu : t.bits(a.s.cuts, a.s.d, k);
   float x[ROWS][V][4], copy[ROWS][V][4];
 #pragma unroll
   for (uint32_t q = 0; q < ROWS; ++q) {
@@ -292,8 +356,8 @@ __device__ __forceinline__ void round_unit(const A& a, const Unit& t, uint32_t e
     if (q < each && p < a.s.n_rows) {
 #pragma unroll
       for (uint32_t k = 0; k < V; ++k) {
-        load_group<XT, WHOLE, NT>(buffer<const void, 0>(a.row[p]), t.first + k * t.step, bits[k], a.s.d, x[q][k]);
-        load_group<TF32, WHOLE, NT>(buffer<const void, 2>(a.row[p]), t.first + k * t.step, bits[k], a.s.d, copy[q][k]);
+        load_group<XT, WHOLE, NT>(based<XT>(buffer<const void, 0>(a.row[p]), t.base), t.at(k), bits[k], t.left, x[q][k]);
+        load_group<TF32, WHOLE, NT>(based<TF32>(buffer<const void, 2>(a.row[p]), t.base), t.at(k), bits[k], t.left, copy[q][k]);
       }
     }
   }
@@ -311,7 +375,7 @@ __device__ __forceinline__ void round_unit(const A& a, const Unit& t, uint32_t e
         encode(u, codes, scale, value);
 #pragma unroll
         for (int j = 0; j < 4; ++j) copy[q][k][j] = copy[q][k][j] + value[j];
-        store_group<TF32, NT>(buffer<void, 2>(a.row[p]), t.first + k * t.step, bits[k], copy[q][k]);
+        store_group<TF32, NT>(based<TF32>(buffer<void, 2>(a.row[p]), t.base), t.at(k), bits[k], copy[q][k]);
         *reinterpret_cast<uint16_t*>(message + k * 128 + 2 * lane) = (uint16_t)codes;
         if (lane % 8 == 0) message[128 * V + k * 8 + lane / 8] = (uint8_t)scale;
       }
@@ -325,7 +389,7 @@ __device__ __forceinline__ void round_unit(const A& a, const Unit& t, uint32_t e
     if (q < each && p < a.s.n_rows) {
       float s[V][4];
 #pragma unroll
-      for (uint32_t k = 0; k < V; ++k) load_group<TF32, WHOLE, NT>(buffer<const void, 3>(a.row[p]), t.first + k * t.step, bits[k], a.s.d, s[k]);
+      for (uint32_t k = 0; k < V; ++k) load_group<TF32, WHOLE, NT>(based<TF32>(buffer<const void, 3>(a.row[p]), t.base), t.at(k), bits[k], t.left, s[k]);
       const MixRow r = mix_row(a.lists, p);
       if (q == 0 || !r.same) {
 #pragma unroll
@@ -338,6 +402,7 @@ __device__ __forceinline__ void round_unit(const A& a, const Unit& t, uint32_t e
           for (int32_t n = from_n; n < to_n; n += kMixAtOnce) {
 #pragma unroll
             for (int m = 0; m < kMixAtOnce; ++m) {
+              if (n + m >= to_n) continue;
               const MixEntry entry = mix_entry(a.lists, (uint32_t)(r.first_entry + n + m));
               const uint8_t* message = lds + entry.col * kRoundMessage<V>;
 #pragma unroll
@@ -362,8 +427,8 @@ __device__ __forceinline__ void round_unit(const A& a, const Unit& t, uint32_t e
           s[k][j] = s[k][j] + mixed[k][j];
           x[q][k][j] = __builtin_fmaf(a.gamma, s[k][j] - copy[q][k][j], x[q][k][j]);
         }
-        store_group<TF32, NT>(buffer<void, 3>(a.row[p]), t.first + k * t.step, bits[k], s[k]);
-        store_group<XT, NT>(buffer<void, 1>(a.row[p]), t.first + k * t.step, bits[k], x[q][k]);
+        store_group<TF32, NT>(based<TF32>(buffer<void, 3>(a.row[p]), t.base), t.at(k), bits[k], s[k]);
+        store_group<XT, NT>(based<XT>(buffer<void, 1>(a.row[p]), t.base), t.at(k), bits[k], x[q][k]);
       }
     }
   }
@@ -374,7 +439,7 @@ __global__ __launch_bounds__(kWave * kRoundWaves) void k_mx4_round(const RoundAr
   extern __shared__ uint8_t lds[];  // of every row: the codes of a unit, then its scales
   const uint32_t waves = blockDim.x / kWave, each = (a.s.n_rows + waves - 1) / waves;
   const uint32_t i = a.s.first * (kGranule / kUnitElems<V>) + die_block_order(blockIdx.x, gridDim.x, a.s.n_xcd, kDieBlockTiles);
-  const Unit t = unit_place<V, NT>(i, a.s, threadIdx.x % kWave);
+  const Units<V, 1> t = units_from<V, NT>(i, a.s, threadIdx.x % kWave);
   if (t.whole) round_unit<XT, ROWS, V, true, NT>(a, t, each, lds);
   else round_unit<XT, ROWS, V, false, NT>(a, t, each, lds);
 }
@@ -387,12 +452,15 @@ int enqueue_encode(int xdt, EncodeArgs<N> a, void* stream) {
   const bool nt = a.s.streams;
   const KernelFn fn = xdt == DADAM_BF16 ? (nt ? (KernelFn)k_mx4_encode<TBF16, true, N> : (KernelFn)k_mx4_encode<TBF16, false, N>)
                                         : (nt ? (KernelFn)k_mx4_encode<TF32, true, N> : (KernelFn)k_mx4_encode<TF32, false, N>);
-  return in_pieces(a, kMixWaves, a.s.n_rows, kWave * kMixWaves, [&](uint32_t grid) { return enqueue_grid(fn, grid, kWave * kMixWaves, &a, 0, stream); });
+  return in_pieces(a, kMixWaves * a.s.n_xcd, a.s.n_rows * a.s.n_xcd, kWave * kMixWaves,
+                   [&](uint32_t grid) { return enqueue_grid(fn, grid, kWave * kMixWaves, &a, 0, stream); });
 }
 
 template <int N, int C, bool NT>
-KernelFn mix_kernel(int xdt, MixMode mode, bool shared) {
-#define DADAM_MIX(XT, MODE) (shared ? (KernelFn)k_mx4_shared<XT, MODE, NT, N, C> : (KernelFn)k_mx4_mix<XT, MODE, NT, N, C>)
+KernelFn mix_kernel(int xdt, MixMode mode, uint32_t work) {
+  if (work == kMixCopy) return (KernelFn)k_mx4_copy<NT, N, C>;
+  if (work == kMixAllRows) return mode == kMixStore ? (KernelFn)k_mx4_products<kMixStore, NT, N, C> : (KernelFn)k_mx4_products<kMixAdd, NT, N, C>;
+#define DADAM_MIX(XT, MODE) (work == kMixByGroup ? (KernelFn)k_mx4_shared<XT, MODE, NT, N, C> : (KernelFn)k_mx4_mix<XT, MODE, NT, N, C>)
   if (mode == kMixStore) return DADAM_MIX(TF32, kMixStore);
   if (mode == kMixAdd) return DADAM_MIX(TF32, kMixAdd);
   return xdt == DADAM_BF16 ? DADAM_MIX(TBF16, kMixGossip) : DADAM_MIX(TF32, kMixGossip);
@@ -400,11 +468,20 @@ KernelFn mix_kernel(int xdt, MixMode mode, bool shared) {
 }
 template <int N, int C>
 int enqueue_mix(int xdt, MixMode mode, MixArgs<N, C> a, void* stream) {
-  const bool shared = a.by_group;
-  const KernelFn fn = a.s.streams ? mix_kernel<N, C, true>(xdt, mode, shared) : mix_kernel<N, C, false>(xdt, mode, shared);
-  const uint32_t parts = (a.s.n_rows + a.rows_each - 1) / a.rows_each, units = shared ? 1 : kMixWaves;
-  return in_pieces(a, units * a.s.n_xcd, parts * a.s.n_xcd, kWave * kMixWaves,
-                   [&](uint32_t grid) { return enqueue_grid(fn, grid, kWave * kMixWaves, &a, 0, stream); });
+  const KernelFn fn = a.s.streams ? mix_kernel<N, C, true>(xdt, mode, a.work) : mix_kernel<N, C, false>(xdt, mode, a.work);
+  const uint32_t X = a.s.n_xcd;  // kernels that walk rows have as many workgroups on every die
+  uint32_t units = kMixWaves, groups = 1;
+  if (a.work == kMixByRow) {
+    units = kMixWaves * (mode == kMixStore ? kMixUnits<kMixStore> : kMixUnits<kMixAdd>) * X;
+    groups = a.s.n_rows * X;
+  } else if (a.work == kMixCopy) {
+    units = kMixWaves * X;
+    groups = a.s.n_rows * X;
+  } else if (a.work == kMixByGroup) {
+    units = X;
+    groups = (a.s.n_rows + a.rows_each - 1) / a.rows_each * X;
+  }
+  return in_pieces(a, units, groups, kWave * kMixWaves, [&](uint32_t grid) { return enqueue_grid(fn, grid, kWave * kMixWaves, &a, 0, stream); });
 }
 
 // Rows a wavefront holds, and its groups a lane: what 128 registers have room for.
@@ -448,7 +525,7 @@ int launch_mix4(int xdt, MixMode mode, uint32_t n_cols, const MixArgs<kMessageRo
   if (a.s.n_rows > (uint32_t)kFewOperands || n_cols > (uint32_t)kFewOperands) return enqueue_mix(xdt, mode, a, stream);
   auto f = few_rows<MixArgs<kFewOperands, kFewOperands>>(a);
   memcpy((void*)f.message, (const void*)a.message, sizeof(f.message));
-  f.s = a.s; f.lists = a.lists; f.scale_offset = a.scale_offset; f.rows_each = a.rows_each; f.by_group = a.by_group; f.gamma = a.gamma;
+  f.s = a.s; f.lists = a.lists; f.scale_offset = a.scale_offset; f.rows_each = a.rows_each; f.work = a.work; f.gamma = a.gamma;
   return enqueue_mix(xdt, mode, f, stream);
 }
 

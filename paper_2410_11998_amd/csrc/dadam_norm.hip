@@ -65,12 +65,11 @@ __device__ __forceinline__ void add_granules(const Span& s, const void* g, uint6
 #pragma unroll
     for (uint32_t v = 0; v < V; ++v) {
       const uint64_t i = i0 + (uint64_t)k * stride, e = i * kGranule + v * (kGranule / V) + E * lane;
-      const bool in = WHOLE || i < s.n_granules;
-      stored[k][v] = WHOLE ? 0u : in ? stored_bits(s.cuts, e, E) & (e < s.d ? ~0u : 0u) : 0u;
+      stored[k][v] = WHOLE ? 0u : stored_bits(s.cuts, s.d, e, E);
       raw[k][v] = u4{0, 0, 0, 0};
-      if (WHOLE || (in && e + E <= s.d)) {
+      if (WHOLE || e + E <= s.d) {
         raw[k][v] = vload<NT>(reinterpret_cast<const u4*>(static_cast<const char*>(g) + e * GT::bytes));
-      } else if (in && e < s.d) {  // the vector's last elements
+      } else if (e < s.d) {  // the vector's last elements
         uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
         for (int j = 0; j < E; ++j)
@@ -129,33 +128,35 @@ __global__ __launch_bounds__(kNormThreads) void k_grad_norm(const NormArgs<N> a)
 }
 
 template <typename GT, bool WHOLE, bool NT>
-__device__ __forceinline__ void clip_unit(const Cuts& cuts, uint64_t d, const Unit& u, const void* g, void* out, float factor) {
+__device__ __forceinline__ void clip_unit(const Cuts& cuts, uint64_t d, const Units<2, 1>& u, const void* g, void* out, float factor) {
   float v[2][4];
   uint32_t bits[2];
 #pragma unroll
   for (uint32_t k = 0; k < 2; ++k) {
-    bits[k] = WHOLE ? 0xFu : group_bits(cuts, u.first + k * u.step);
-    load_group<GT, WHOLE, NT>(g, u.first + k * u.step, bits[k], d, v[k]);
+    bits[k] = WHOLE ? 0xFu : u.bits(cuts, d, k);
+    load_group<GT, WHOLE, NT>(based<GT>(g, u.base), u.at(k), bits[k], u.left, v[k]);
   }
 #pragma unroll
   for (uint32_t k = 0; k < 2; ++k) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[k][j] *= factor;
-    store_group<GT, NT>(out, u.first + k * u.step, bits[k], v[k]);
+    store_group<GT, NT>(based<GT>(out, u.base), u.at(k), bits[k], v[k]);
   }
 }
 
 template <typename GT, bool NT, int N>
 __global__ __launch_bounds__(kNormThreads) void k_clip(const NormArgs<N> a) {
-  const uint32_t lane = threadIdx.x % kWave, wave = wave_of_group();
-  const uint32_t row = blockIdx.x % a.s.n_rows, i = a.s.first + blockIdx.x / a.s.n_rows * kNormWaves + wave;
+  const uint32_t lane = threadIdx.x % kWave;
+  uint32_t piece, row;
+  const bool active = die_block_piece(blockIdx.x, a.s.n_rows, a.s.n_xcd, (a.s.count + kNormWaves - 1) / kNormWaves, kDieBlockTiles, piece, row, a.s.run);
+  const uint32_t i = a.s.first + piece * kNormWaves + wave_of_group();
   const void* g = buffer<const void, 0>(a.row[row]);
   void* out = buffer<void, 1>(a.row[row]);
   const float norm = a.norms[row];
   const bool scales = !(norm <= a.max_norm);  // NaN scales too: everything becomes NaN
-  if (i < a.s.n_granules && (scales || g != out)) {
+  if (active && i < a.s.n_granules && (scales || g != out)) {
     const float factor = scales ? a.max_norm / norm : 1.0f;
-    const Unit u = unit_place<2, NT>(i, a.s, lane);
+    const Units<2, 1> u = units_from<2, NT>(i, a.s, lane);
     if (u.whole) clip_unit<GT, true, NT>(a.s.cuts, a.s.d, u, g, out, factor);
     else clip_unit<GT, false, NT>(a.s.cuts, a.s.d, u, g, out, factor);
   }
@@ -195,7 +196,7 @@ int enqueue_norm(int gdt, NormArgs<N>& a, void* stream) {
 }
 template <int N>
 int enqueue_clip(int gdt, NormArgs<N>& a, void* stream) {
-  return in_pieces(a, kNormWaves, a.s.n_rows, kNormThreads, [&](uint32_t grid) { return enqueue_grid(clip_kernel<N>(gdt, a.s.streams), grid, kNormThreads, &a, 0, stream); });
+  return in_pieces(a, kNormWaves * a.s.n_xcd, a.s.n_rows * a.s.n_xcd, kNormThreads, [&](uint32_t grid) { return enqueue_grid(clip_kernel<N>(gdt, a.s.streams), grid, kNormThreads, &a, 0, stream); });
 }
 
 }  // namespace

@@ -201,29 +201,39 @@ void fill_span(const dadam_handle* h, Span* s) {
   s->n_rows = h->cfg.n_rows;
   s->n_xcd = h->n_xcds;
   s->streams = h->nontemporal;
+  s->run = s->streams ? kDieRunPieces : 1;
 }
 
 uint64_t blocks_of(const dadam_handle* h) { return (h->cfg.d + kMxBlock - 1) / kMxBlock; }
 size_t message_bytes(const dadam_handle* h) { return (size_t)((blocks_of(h) * 17 + 15) / 16 * 16); }
 
-// Who takes what of a launch of n_rows positions (MixArgs::by_group, rows_each).  Lists that fewer than four rows share on average: a wavefront
+// Who takes what of a launch of n_rows positions (MixArgs::work, rows_each).  Lists that fewer than four rows share on average: a wavefront
 // for every unit and row.  Otherwise products of 1536 granules and more: a wavefront takes a unit of all rows and forms the sum once; all
 // others: a workgroup does, its wavefronts share the list and the rows, and rows are split until there are 4096 workgroups.
 // us, by workgroup / by wavefront, complete graph, product of 100 rows of 4e6 elements 456 / 370, of 1e6 137 / 119, of 4e5 55 / 78, of 32 rows of 4e6 147 / 111,
 // of 2e6 48 / 53, of 4e5 15.5 / 22, of 8 rows of 2e6 18 / 13.5; gossip of 100 rows of 2e6 777 / 845, of 32 rows of 2e6 237 / 259, of 8 rows of 1e6 33 / 35.5.
 constexpr uint64_t kProductGranules = 1536, kSharedGroups = 4096;
-void share_rows(const dadam_handle* h, const Slot& s, MixMode mode, uint32_t n_rows, uint32_t* by_group, uint32_t* rows_each) {
+bool shares_rows(const dadam_handle* h, const Slot& s) { return h->cfg.n_rows >= 4 * s.mix_firsts.size(); }
+void share_rows(const dadam_handle* h, const Slot& s, MixMode mode, uint32_t n_rows, uint32_t* work, uint32_t* rows_each) {
   const uint64_t granules = granules_of(h);
-  *by_group = 0;
+  *work = kMixByRow;
   *rows_each = 1;
-  if (h->cfg.n_rows < 4 * s.mix_groups) return;
+  if (!shares_rows(h, s)) return;
   if (mode != kMixGossip && granules >= kProductGranules) {
-    *rows_each = n_rows;
+    *work = kMixAllRows;
     return;
   }
   const uint64_t parts = (kSharedGroups + granules - 1) / granules;
-  *by_group = 1;
+  *work = kMixByGroup;
   *rows_each = std::min((uint32_t)((n_rows + parts - 1) / parts + kMixParts - 1) / kMixParts * kMixParts, n_rows);
+}
+
+// Products of 1e8 elements in all rows whose rows share sums: one row of every list is formed, and the others are copied from it, a die taking
+// a run of 256 pieces of one row after the other, with what it copies in its L2.  (A wavefront that writes all rows has as many places of
+// memory in use at a time as there are wavefronts on the chip.)  us, a wavefront for all rows / copies, complete graph: 32 rows of 2.6e7 951 / 731, 12 of 3e7 349 /
+// 309, 100 of 4e6 373 / 330, of 1e6 129 / 110; 8 rows of 8e6 45 / 59.  Runs of 32 / 128 / 1024 pieces: the first 802 / 759 / 1050.
+bool copies_rows(const dadam_handle* h, const Slot& s, MixMode mode) {
+  return mode == kMixStore && h->cfg.d * h->cfg.n_rows >= kManyElems && shares_rows(h, s) && granules_of(h) >= kProductGranules;
 }
 
 // Runs the launches of a call whose arguments have passed, with the handle's device current and its state made.
@@ -286,30 +296,55 @@ int mix_impl(dadam_handle* h, uint32_t slot, const void* const* msg, float* cons
   if (!rc) rc = check_device(h);
   if (rc) return rc;
   return on_device(h, [&] {
-    int e = (int)hipSuccess;
     const Slot& lists = h->slots[slot];
-    const uint32_t launches = (R + kMessageRows - 1) / kMessageRows, rows = (R + launches - 1) / launches;
-    for (uint32_t p0 = 0; p0 < R && e == (int)hipSuccess; p0 += rows) {
-      MixArgs<kMessageRows, kMaxRows> a;
-      memset((void*)&a, 0, sizeof(a));
-      fill_span(h, &a.s);
-      a.s.n_rows = std::min(rows, R - p0);
-      for (uint32_t p = 0; p < a.s.n_rows; ++p) {
-        const int32_t i = lists.mix_rows[p0 + p].row;
-        put(&a.row[p], 0, sum[i]);
-        if (mode != kMixGossip) continue;
-        put(&a.row[p], 1, copy[i]);
-        put(&a.row[p], 2, x_src[i]);
-        put(&a.row[p], 3, x_dst[i]);
+    const bool copies = copies_rows(h, lists, mode);
+    // Positions [0, count) of `rows` in as few launches as the argument block allows, of about the same number each.
+    MixArgs<kMessageRows, kMaxRows> a;
+    memset((void*)&a, 0, sizeof(a));
+    fill_span(h, &a.s);
+    for (uint32_t c = 0; c < C; ++c) put(&a.message[c], msg[c]);
+    a.scale_offset = 16 * blocks_of(h);
+    a.gamma = gamma;
+    auto in_launches = [&](uint32_t count, auto fill) {
+      const uint32_t launches = (count + kMessageRows - 1) / kMessageRows, each = launches ? (count + launches - 1) / launches : 0;
+      int e = (int)hipSuccess;
+      for (uint32_t p0 = 0; p0 < count && e == (int)hipSuccess; p0 += each) {
+        memset((void*)a.row, 0, sizeof(a.row));
+        a.s.n_rows = std::min(each, count - p0);
+        for (uint32_t p = 0; p < a.s.n_rows; ++p) fill(&a.row[p], p0 + p);
+        fill(nullptr, p0);
+        e = launch_mix4((int)h->cfg.param_dtype, mode, C, a, stream);
       }
-      for (uint32_t c = 0; c < C; ++c) put(&a.message[c], msg[c]);
-      a.lists = {lists.d_mix_rows + p0, lists.d_mix_entries};
-      a.scale_offset = 16 * blocks_of(h);
-      share_rows(h, lists, mode, a.s.n_rows, &a.by_group, &a.rows_each);
-      a.gamma = gamma;
-      e = launch_mix4((int)h->cfg.param_dtype, mode, C, a, stream);
+      return e;
+    };
+    const std::vector<MixRow>& rows = copies ? lists.mix_firsts : lists.mix_rows;
+    int e = in_launches((uint32_t)rows.size(), [&](RowPointers* r, uint32_t p) {
+      if (!r) {
+        a.lists = {(copies ? lists.d_mix_firsts : lists.d_mix_rows) + p, lists.d_mix_entries};
+        a.work = kMixByRow;
+        if (!copies) share_rows(h, lists, mode, a.s.n_rows, &a.work, &a.rows_each);
+        return;
+      }
+      const int32_t i = rows[p].row;
+      put(r, 0, sum[i]);
+      if (mode != kMixGossip) return;
+      put(r, 1, copy[i]);
+      put(r, 2, x_src[i]);
+      put(r, 3, x_dst[i]);
+    });
+    if (e != (int)hipSuccess || !copies) return e;
+    std::vector<std::pair<int32_t, int32_t>> pairs;  // (copy, of)
+    int32_t of = 0;
+    for (const MixRow& r : lists.mix_rows) {
+      if (r.same) pairs.push_back({r.row, of});
+      else of = r.row;
     }
-    return e;
+    a.work = kMixCopy;
+    return in_launches((uint32_t)pairs.size(), [&](RowPointers* r, uint32_t p) {
+      if (!r) return;
+      put(r, 0, sum[pairs[p].first]);
+      put(r, 1, sum[pairs[p].second]);
+    });
   });
 }
 

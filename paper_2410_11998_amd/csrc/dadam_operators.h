@@ -43,6 +43,7 @@ struct Span {
   uint32_t first, count;
   uint32_t n_rows;
   uint32_t n_xcd;
+  uint32_t run;
   uint32_t streams;     // accesses carry the non-temporal hint, lanes lie apart (see unit_place)
 };
 
@@ -74,8 +75,8 @@ struct MixArgs {
   Span s;
   Lists lists;
   uint64_t scale_offset;
-  uint32_t by_group;   // a workgroup takes a unit (k_mx4_shared), not a wavefront (k_mx4_mix)
-  uint32_t rows_each;  // positions it takes
+  uint32_t work;       // MixWork
+  uint32_t rows_each;  // kMixByGroup: positions a workgroup takes
   float gamma;
 };
 
@@ -87,6 +88,9 @@ struct RoundArgs {
   float gamma;
 };
 
+// Who does what of a launch: a wavefront a row, a workgroup several rows that share their sum, a wavefront all rows; or rows are copies of
+// others (row 0 the copy, 1 what it is of).
+enum MixWork : uint32_t { kMixByRow = 0, kMixByGroup = 1, kMixAllRows = 2, kMixCopy = 3 };
 enum MixMode : int { kMixStore = 0, kMixAdd = 1, kMixGossip = 2 };
 
 // Launchers: enqueue on `stream`, return the hipError_t of the launch as int.  The large block is given; launches of few rows
