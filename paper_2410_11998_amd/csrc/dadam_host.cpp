@@ -813,8 +813,9 @@ void find_mix_rows(uint32_t R, Slot& s) {
     while (s.mix_entries.size() % kMixAtOnce) s.mix_entries.push_back({s.mix_entries.back().col, 0.f});
     const int32_t all = (int32_t)s.mix_entries.size() - first, step = kMixAtOnce * (rows.size() > 1 ? kMixParts : 1);
     const int32_t part = rows.size() > 1 ? (all + step - 1) / step * kMixAtOnce : all;
-    for (int32_t row : rows) s.mix_rows.push_back({(int16_t)row, (int16_t)(row != (int32_t)i), first, n, part});
-    s.mix_firsts.push_back({(int16_t)i, 0, first, n, part});
+    const int16_t group = (int16_t)s.mix_firsts.size();
+    for (int32_t row : rows) s.mix_rows.push_back({(int16_t)row, group, first, n, part});
+    s.mix_firsts.push_back({(int16_t)i, group, first, n, part});
   }
 }
 

@@ -61,12 +61,12 @@ struct Loop {
   int32_t first_row, n_rows;       // in StepArgs::row_order
 };
 // How the products with 4-bit messages walk a slot: its rows in an order in which rows that list the same sources with the same
-// weights follow each other (`same`: as the one before).  Their entries are filled up to a multiple of kMixAtOnce with the last one's
+// weights follow each other (`group`: number of the list).  Their entries are filled up to a multiple of kMixAtOnce with the last one's
 // source and weight 0; rows that share them have them in order of the sources, the others as listed.  The sum goes in parts of
 // `part` entries (a multiple of kMixAtOnce), each from zero on, that are then added in their order: four parts where rows share it, so that
 // four wavefronts can form it, one where not.
 struct MixRow {
-  int16_t row, same;
+  int16_t row, group;
   int32_t first_entry, n_entries, part;
 };
 struct MixEntry {

@@ -242,11 +242,13 @@ __device__ __forceinline__ void mix_rows(const A& a, const Units<2, 1>& t) {
 #pragma unroll
   for (uint32_t k = 0; k < 2; ++k) bits[k] = WHOLE ? 0xFu : t.bits(a.s.cuts, a.s.d, k);
   float mixed[2][4];
+  int32_t group = -1;
   for (uint32_t p = 0; p < a.s.n_rows; ++p) {
     RowUpdate<XT, MODE, 1, WHOLE, NT, A> row;
     row.load(a, p, t, bits);
     const MixRow r = mix_row(a.lists, p);
-    if (p == 0 || !r.same) mix_list<WHOLE>(a, r, t, bits, mixed);
+    if (r.group != group) mix_list<WHOLE>(a, r, t, bits, mixed);
+    group = r.group;
     row.store(a, p, t, bits, mixed);
   }
 }
@@ -300,7 +302,7 @@ __device__ __forceinline__ void mix_shared(const A& a, const Units<2, 1>& t, uin
   while (from < to) {
     const MixRow r = mix_row(a.lists, from);
     uint32_t end = from + 1;
-    while (end < to && mix_row(a.lists, end).same) ++end;
+    while (end < to && mix_row(a.lists, end).group == r.group) ++end;
     float mixed[G][4];
     const int32_t n = (int32_t)wave * r.part, last = n + r.part < r.n_entries ? n + r.part : r.n_entries;
     mix_unit<WHOLE>(a, r.first_entry + n, r.first_entry + last, t, bits, mixed);
@@ -343,6 +345,30 @@ template <int V>
 constexpr uint32_t kRoundMessage = kUnitElems<V> / 2 + kUnitElems<V> / kMxBlock;  // bytes of a row's message of a unit, by lane
 constexpr uint32_t kRoundWaves = 16;
 
+// Entries [first, end) of the lists, from the messages in LDS.
+template <int V, typename A>
+__device__ __forceinline__ void mix_parked(const A& a, int32_t first, int32_t end, const uint8_t* lds, uint32_t lane, float (&part)[V][4]) {
+#pragma unroll
+  for (uint32_t k = 0; k < V; ++k)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) part[k][j] = 0.0f;
+  for (int32_t n = first; n < end; n += kMixAtOnce) {
+#pragma unroll
+    for (int m = 0; m < kMixAtOnce; ++m) {
+      if (n + m >= end) continue;
+      const MixEntry entry = mix_entry(a.lists, (uint32_t)(n + m));
+      const uint8_t* message = lds + entry.col * kRoundMessage<V>;
+#pragma unroll
+      for (uint32_t k = 0; k < V; ++k) {
+        float value[4];
+        decode(*reinterpret_cast<const uint16_t*>(message + k * 128 + 2 * lane), message[128 * V + k * 8 + lane / 8], value);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) part[k][j] = __builtin_fmaf(entry.w, value[j], part[k][j]);
+      }
+    }
+  }
+}
+
 template <typename XT, int ROWS, int V, bool WHOLE, bool NT, typename A>
 __device__ __forceinline__ void round_unit(const A& a, const Units<V, 1>& t, uint32_t each, uint8_t* lds) {
   const uint32_t lane = threadIdx.x % kWave, from = wave_of_group() * each;
@@ -382,7 +408,23 @@ __device__ __forceinline__ void round_unit(const A& a, const Units<V, 1>& t, uin
     }
   }
   __syncthreads();
+  // Lists that many rows share: a part of a sum to a wavefront, through LDS.  (Every wavefront its own sum: complete graph on 61 rows of 2e6 in
+  // bfloat16 715 us.)
+  f4* parts = reinterpret_cast<f4*>(lds + a.s.n_rows * kRoundMessage<V> + (a.s.n_rows * kRoundMessage<V> & 8));
+  if (a.n_groups != 0) {
+    for (uint32_t task = wave_of_group(); task < a.n_groups * kMixParts; task += blockDim.x / kWave) {
+      const Lists firsts = {a.firsts, a.lists.entries};
+      const MixRow r = mix_row(firsts, task / kMixParts);
+      const int32_t n = (int32_t)(task % kMixParts) * r.part;
+      float part[V][4];
+      mix_parked<V>(a, r.first_entry + n, r.first_entry + (n + r.part < r.n_entries ? n + r.part : r.n_entries), lds, lane, part);
+#pragma unroll
+      for (uint32_t k = 0; k < V; ++k) parts[(task * V + k) * kWave + lane] = f4{part[k][0], part[k][1], part[k][2], part[k][3]};
+    }
+    __syncthreads();
+  }
   float mixed[V][4];
+  int32_t group = -1;
 #pragma unroll
   for (uint32_t q = 0; q < ROWS; ++q) {
     const uint32_t p = from + q;
@@ -391,33 +433,23 @@ __device__ __forceinline__ void round_unit(const A& a, const Units<V, 1>& t, uin
 #pragma unroll
       for (uint32_t k = 0; k < V; ++k) load_group<TF32, WHOLE, NT>(based<TF32>(buffer<const void, 3>(a.row[p]), t.base), t.at(k), bits[k], t.left, s[k]);
       const MixRow r = mix_row(a.lists, p);
-      if (q == 0 || !r.same) {
+      if (r.group != group) {
+        group = r.group;
+        for (int32_t n = 0; n < r.n_entries; n += r.part) {
+          float part[V][4];
+          if (a.n_groups != 0) {
 #pragma unroll
-        for (uint32_t k = 0; k < V; ++k)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) mixed[k][j] = 0.0f;
-        for (int32_t from_n = 0; from_n < r.n_entries; from_n += r.part) {
-          const int32_t to_n = from_n + r.part < r.n_entries ? from_n + r.part : r.n_entries;
-          float part[V][4] = {};
-          for (int32_t n = from_n; n < to_n; n += kMixAtOnce) {
-#pragma unroll
-            for (int m = 0; m < kMixAtOnce; ++m) {
-              if (n + m >= to_n) continue;
-              const MixEntry entry = mix_entry(a.lists, (uint32_t)(r.first_entry + n + m));
-              const uint8_t* message = lds + entry.col * kRoundMessage<V>;
-#pragma unroll
-              for (uint32_t k = 0; k < V; ++k) {
-                float value[4];
-                decode(*reinterpret_cast<const uint16_t*>(message + k * 128 + 2 * lane), message[128 * V + k * 8 + lane / 8], value);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) part[k][j] = __builtin_fmaf(entry.w, value[j], part[k][j]);
-              }
+            for (uint32_t k = 0; k < V; ++k) {
+              const f4 v = parts[((r.group * kMixParts + n / r.part) * V + k) * kWave + lane];
+              part[k][0] = v.x; part[k][1] = v.y; part[k][2] = v.z; part[k][3] = v.w;
             }
+          } else {
+            mix_parked<V>(a, r.first_entry + n, r.first_entry + (n + r.part < r.n_entries ? n + r.part : r.n_entries), lds, lane, part);
           }
 #pragma unroll
           for (uint32_t k = 0; k < V; ++k)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) mixed[k][j] = from_n == 0 ? part[k][j] : mixed[k][j] + part[k][j];
+            for (int j = 0; j < 4; ++j) mixed[k][j] = n == 0 ? part[k][j] : mixed[k][j] + part[k][j];
         }
       }
 #pragma unroll
@@ -436,7 +468,7 @@ __device__ __forceinline__ void round_unit(const A& a, const Units<V, 1>& t, uin
 
 template <typename XT, int ROWS, int V, bool NT, int N>
 __global__ __launch_bounds__(kWave * kRoundWaves) void k_mx4_round(const RoundArgs<N> a) {
-  extern __shared__ uint8_t lds[];  // of every row: the codes of a unit, then its scales
+  extern __shared__ __align__(16) uint8_t lds[];  // of every row: the codes of a unit, then its scales; then parts of shared sums
   const uint32_t waves = blockDim.x / kWave, each = (a.s.n_rows + waves - 1) / waves;
   const uint32_t i = a.s.first * (kGranule / kUnitElems<V>) + die_block_order(blockIdx.x, gridDim.x, a.s.n_xcd, kDieBlockTiles);
   const Units<V, 1> t = units_from<V, NT>(i, a.s, threadIdx.x % kWave);
@@ -508,7 +540,8 @@ int enqueue_round(int xdt, RoundArgs<N> a, void* stream) {
   const KernelFn fn = a.s.streams ? round_kernel<N, true>(xdt, each) : round_kernel<N, false>(xdt, each);
   if (fn == nullptr) return (int)hipErrorInvalidDeviceFunction;
   const uint32_t units = each <= 4 ? 1 : 2;  // of a granule
-  const uint32_t lds = a.s.n_rows * (units == 1 ? kRoundMessage<2> : kRoundMessage<1>);
+  const uint32_t messages = a.s.n_rows * (units == 1 ? kRoundMessage<2> : kRoundMessage<1>);
+  const uint32_t lds = messages + (messages & 8) + a.n_groups * kMixParts * (2 / units) * kWave * 16;
   return in_pieces(a, 1, units, kWave * waves, [&](uint32_t grid) { return enqueue_grid(fn, grid, kWave * waves, &a, lds, stream); });
 }
 
@@ -532,7 +565,7 @@ int launch_mix4(int xdt, MixMode mode, uint32_t n_cols, const MixArgs<kMessageRo
 int launch_round(int xdt, const RoundArgs<kMaxRows>& a, void* stream) {
   if (a.s.n_rows > (uint32_t)kFewOperands) return enqueue_round(xdt, a, stream);
   auto f = few_rows<RoundArgs<kFewOperands>>(a);
-  f.s = a.s; f.lists = a.lists; f.gamma = a.gamma;
+  f.s = a.s; f.lists = a.lists; f.firsts = a.firsts; f.n_groups = a.n_groups; f.gamma = a.gamma;
   return enqueue_round(xdt, f, stream);
 }
 

@@ -228,6 +228,9 @@ void share_rows(const dadam_handle* h, const Slot& s, MixMode mode, uint32_t n_r
   *rows_each = std::min((uint32_t)((n_rows + parts - 1) / parts + kMixParts - 1) / kMixParts * kMixParts, n_rows);
 }
 
+// Rounds whose wavefronts form shared sums together: up to kRoundGroups lists (their parts lie in LDS) of kRoundEntries entries and more on average.
+constexpr size_t kRoundGroups = 4, kRoundEntries = 12;
+
 // Products of 1e8 elements in all rows whose rows share sums: one row of every list is formed, and the others are copied from it, a die taking
 // a run of 256 pieces of one row after the other, with what it copies in its L2.  (A wavefront that writes all rows has as many places of
 // memory in use at a time as there are wavefronts on the chip.)  us, a wavefront for all rows / copies, complete graph: 32 rows of 2.6e7 951 / 731, 12 of 3e7 349 /
@@ -334,11 +337,8 @@ int mix_impl(dadam_handle* h, uint32_t slot, const void* const* msg, float* cons
     });
     if (e != (int)hipSuccess || !copies) return e;
     std::vector<std::pair<int32_t, int32_t>> pairs;  // (copy, of)
-    int32_t of = 0;
-    for (const MixRow& r : lists.mix_rows) {
-      if (r.same) pairs.push_back({r.row, of});
-      else of = r.row;
-    }
+    for (const MixRow& r : lists.mix_rows)
+      if (r.row != lists.mix_firsts[r.group].row) pairs.push_back({r.row, lists.mix_firsts[r.group].row});
     a.work = kMixCopy;
     return in_launches((uint32_t)pairs.size(), [&](RowPointers* r, uint32_t p) {
       if (!r) return;
@@ -462,6 +462,9 @@ int dadam_mx4_round(dadam_handle* h, uint32_t slot, const void* const* x_src, vo
       }
       fill_span(h, &a.s);
       a.lists = {lists.d_mix_rows, lists.d_mix_entries};
+      a.firsts = lists.d_mix_firsts;
+      a.n_groups = shares_rows(h, lists) && lists.mix_firsts.size() <= kRoundGroups && lists.mix_entries.size() >= kRoundEntries * lists.mix_firsts.size()
+                       ? (uint32_t)lists.mix_firsts.size() : 0;
       a.gamma = gamma;
       return launch_round((int)h->cfg.param_dtype, a, hip_stream);
     });

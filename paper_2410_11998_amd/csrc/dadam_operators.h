@@ -85,6 +85,8 @@ struct RoundArgs {
   RowPointers row[N];  // by position: 0 x, 1 x behind, 2 copy, 3 sum
   Span s;
   Lists lists;
+  const MixRow* firsts;  // the first row of every list
+  uint32_t n_groups;     // lists whose sums the wavefronts of a workgroup form together, 0: every wavefront its own
   float gamma;
 };
 
