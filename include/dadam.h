@@ -36,7 +36,7 @@
  *     frees or copies them and never synchronises a stream.  The library owns only metadata on host and
  *     device: the segment table, the CSR slots and, for layouts of many short tensors with at most seven
  *     elements between two of them, a byte of device memory for every four elements of one buffer, up
- *     to 64 MB (d of 2^28).  (One set-up call is the exception and says so: dadam_place_by_timing
+ *     to 64 MB (d of 2^28); for handles that call what is described under "Around the step", what that needs.  (One set-up call is the exception and says so: dadam_place_by_timing
  *     overwrites the empty arena it is given and returns when its measurements are done.)
  *   - Launching entry points enqueue work on the given HIP stream (a hipStream_t passed as
  *     void*; NULL = the default stream) and return at once.  The caller keeps every buffer alive

@@ -156,7 +156,7 @@ def _ptr_array(ptrs: Sequence[int]):
     return arr
 
 
-_SHAPE_OF_HANDLE = {}   # handle value -> (d, bytes per parameter, bytes per gradient, rows, columns): host-side size checks only
+_SHAPE_OF_HANDLE = {}   # handle value -> (d, bytes per parameter, bytes per gradient, rows, columns, on a device): host-side checks only
 
 
 def _ptrs_of(tensors, h=None, elem_bytes: int = 0, what: str = "") -> Sequence[int]:
@@ -300,7 +300,7 @@ def dadam_init(n_rows: int, n_cols: int, d: int, offsets: Sequence[int], numels:
     rc = lib.dadam_init(C.byref(cfg), C.byref(h))
     if rc < 0:
         raise DadamError(rc, (lib.dadam_last_error(None) or b"").decode())
-    _SHAPE_OF_HANDLE[h.value] = (int(d), 2 if param_dtype == DADAM_BF16 else 4, 2 if grad_dtype == DADAM_BF16 else 4, int(n_rows), int(n_cols))
+    _SHAPE_OF_HANDLE[h.value] = (int(d), 2 if param_dtype == DADAM_BF16 else 4, 2 if grad_dtype == DADAM_BF16 else 4, int(n_rows), int(n_cols), device >= 0)
     return h
 
 
@@ -387,7 +387,7 @@ def dadam_slot_uses_tile_mode(h, slot: int) -> bool:
     return _check(h, lib.dadam_slot_uses_tile_mode(h, slot)) == 1
 
 
-def pointer_table(buffers, count: int, length: int, elem_bytes: int, what: str):
+def pointer_table(buffers, count: int, length: int, elem_bytes: int, what: str, on_device: bool = False):
     """The host array of `count` device pointers that the calls below take, marshalled and size-checked once: from a sequence of tensors (or
     integers taken as addresses), or from one tensor whose rows are the buffers.  None stays None, a table made before is
     passed through.  The tensors must stay alive."""
@@ -401,6 +401,8 @@ def pointer_table(buffers, count: int, length: int, elem_bytes: int, what: str):
             raise ValueError(f"{what} holds {shape[0]} buffers, the handle needs {count}")
         if buffers.element_size() != elem_bytes:
             raise ValueError(f"{what} has {buffers.element_size()}-byte elements, the handle expects {elem_bytes}")
+        if on_device and not buffers.is_cuda:
+            raise ValueError(f"{what} is not on a GPU")
         if shape[1] < length:
             raise ValueError(f"{what} holds {shape[1]} elements a buffer, the handle needs {length}")
         first, step = buffers.data_ptr(), stride[0] * elem_bytes
@@ -419,6 +421,8 @@ def pointer_table(buffers, count: int, length: int, elem_bytes: int, what: str):
                 raise ValueError(f"{what}[{k}] has {t.element_size()}-byte elements, the handle expects {elem_bytes}")
             if t.numel() < length:
                 raise ValueError(f"{what}[{k}] holds {t.numel()} elements, the handle needs {length}")
+            if on_device and not t.is_cuda:
+                raise ValueError(f"{what}[{k}] is not on a GPU")
             t = t.data_ptr()
         ptrs.append(t)
     return array("Q", ptrs)
@@ -430,32 +434,34 @@ def _at(table):
 
 
 def _shape(h):
-    return _SHAPE_OF_HANDLE.get(getattr(h, "value", None), (0, 0, 0, 0, 0))
+    return _SHAPE_OF_HANDLE.get(getattr(h, "value", None), (0, 0, 0, 0, 0, False))
 
 
 def _message_bytes(d: int) -> int:
     return -(-(-(-d // DADAM_MX4_BLOCK) * 17) // 16) * 16
 
 
-def _row_values(norms, rows: int) -> int:
+def _row_values(norms, rows: int, on_device: bool) -> int:
     if isinstance(norms, int):
         return norms
     if norms.numel() < rows or norms.element_size() != 4 or not norms.is_contiguous():
         raise ValueError("norms must hold one float32 a row")
+    if on_device and not norms.is_cuda:
+        raise ValueError("norms is not on a GPU")
     return norms.data_ptr()
 
 
 def dadam_grad_norm(h, grads, norms, stream: int = 0) -> None:
     """norms: a device tensor of n_rows float32 (or an integer device address)."""
-    d, _, gb, rows, _ = _shape(h)
-    g = pointer_table(grads, rows, d, gb, "grads")
-    _check(h, lib.dadam_grad_norm(h, _at(g), _row_values(norms, rows), stream))
+    d, _, gb, rows, _, gpu = _shape(h)
+    g = pointer_table(grads, rows, d, gb, "grads", gpu)
+    _check(h, lib.dadam_grad_norm(h, _at(g), _row_values(norms, rows, gpu), stream))
 
 
 def dadam_clip_grads(h, grads, out, max_norm: float, norms, stream: int = 0) -> None:
-    d, _, gb, rows, _ = _shape(h)
-    g, o = pointer_table(grads, rows, d, gb, "grads"), pointer_table(out, rows, d, gb, "out")
-    _check(h, lib.dadam_clip_grads(h, _at(g), _at(o), max_norm, _row_values(norms, rows), stream))
+    d, _, gb, rows, _, gpu = _shape(h)
+    g, o = pointer_table(grads, rows, d, gb, "grads", gpu), pointer_table(out, rows, d, gb, "out", gpu)
+    _check(h, lib.dadam_clip_grads(h, _at(g), _at(o), max_norm, _row_values(norms, rows, gpu), stream))
 
 
 def dadam_mx4_get_info(h) -> dadam_mx4_info:
@@ -466,30 +472,30 @@ def dadam_mx4_get_info(h) -> dadam_mx4_info:
 
 def dadam_mx4_encode(h, x, copy_in, copy_out, msg, stream: int = 0) -> None:
     """copy_in and copy_out may be None; messages are uint8 tensors."""
-    d, pb, _, rows, _ = _shape(h)
-    x, msg = pointer_table(x, rows, d, pb, "x"), pointer_table(msg, rows, _message_bytes(d), 1, "msg")
-    copy_in, copy_out = pointer_table(copy_in, rows, d, 4, "copy_in"), pointer_table(copy_out, rows, d, 4, "copy_out")
+    d, pb, _, rows, _, gpu = _shape(h)
+    x, msg = pointer_table(x, rows, d, pb, "x", gpu), pointer_table(msg, rows, _message_bytes(d), 1, "msg", gpu)
+    copy_in, copy_out = pointer_table(copy_in, rows, d, 4, "copy_in", gpu), pointer_table(copy_out, rows, d, 4, "copy_out", gpu)
     _check(h, lib.dadam_mx4_encode(h, _at(x), _at(copy_in), _at(copy_out), _at(msg), stream))
 
 
 def dadam_mx4_product(h, slot: int, msg, out, flags: int = 0, stream: int = 0) -> None:
-    d, _, _, rows, cols = _shape(h)
-    msg, out = pointer_table(msg, cols, _message_bytes(d), 1, "msg"), pointer_table(out, rows, d, 4, "out")
+    d, _, _, rows, cols, gpu = _shape(h)
+    msg, out = pointer_table(msg, cols, _message_bytes(d), 1, "msg", gpu), pointer_table(out, rows, d, 4, "out", gpu)
     _check(h, lib.dadam_mx4_product(h, slot, _at(msg), _at(out), flags, stream))
 
 
 def dadam_mx4_gossip(h, slot: int, msg, sum, copy, x_src, x_dst, gamma: float, stream: int = 0) -> None:
-    d, pb, _, rows, cols = _shape(h)
-    msg, sum = pointer_table(msg, cols, _message_bytes(d), 1, "msg"), pointer_table(sum, rows, d, 4, "sum")
-    copy, x_src = pointer_table(copy, rows, d, 4, "copy"), pointer_table(x_src, rows, d, pb, "x_src")
-    x_dst = pointer_table(x_dst, rows, d, pb, "x_dst")
+    d, pb, _, rows, cols, gpu = _shape(h)
+    msg, sum = pointer_table(msg, cols, _message_bytes(d), 1, "msg", gpu), pointer_table(sum, rows, d, 4, "sum", gpu)
+    copy, x_src = pointer_table(copy, rows, d, 4, "copy", gpu), pointer_table(x_src, rows, d, pb, "x_src", gpu)
+    x_dst = pointer_table(x_dst, rows, d, pb, "x_dst", gpu)
     _check(h, lib.dadam_mx4_gossip(h, slot, _at(msg), _at(sum), _at(copy), _at(x_src), _at(x_dst), gamma, stream))
 
 
 def dadam_mx4_round(h, slot: int, x_src, x_dst, copy, sum, gamma: float, stream: int = 0) -> None:
-    d, pb, _, rows, _ = _shape(h)
-    x_src, x_dst = pointer_table(x_src, rows, d, pb, "x_src"), pointer_table(x_dst, rows, d, pb, "x_dst")
-    copy, sum = pointer_table(copy, rows, d, 4, "copy"), pointer_table(sum, rows, d, 4, "sum")
+    d, pb, _, rows, _, gpu = _shape(h)
+    x_src, x_dst = pointer_table(x_src, rows, d, pb, "x_src", gpu), pointer_table(x_dst, rows, d, pb, "x_dst", gpu)
+    copy, sum = pointer_table(copy, rows, d, 4, "copy", gpu), pointer_table(sum, rows, d, 4, "sum", gpu)
     _check(h, lib.dadam_mx4_round(h, slot, _at(x_src), _at(x_dst), _at(copy), _at(sum), gamma, stream))
 
 

@@ -2,8 +2,11 @@
 //
 //   n_i = sqrt(sum_e g_i[e]^2),   out_i = g_i  or  g_i (max_norm / n_i)
 //
-// One pass over g for the norm (bound by reading it), one more to scale it.  A float32 square is exact in 64 bits (24 + 24 of 53), so
-// sums in double lose next to nothing whatever their order, and nothing overflows or vanishes on the way.
+// One pass over g for the norm, bound by reading it (8 rows of 355 million bfloat16 elements 831 us, 6.8 TB/s; 1e8 float32 elements 64.7 us, 6.2), one more
+// to scale it (355 million float32 elements with both passes 680 us, 6.3 TB/s of the three streams).  A float32 square is exact in 64 bits (24 + 24 of
+// 53), so sums in double lose next to nothing whatever their order, and nothing overflows or vanishes on the way; conversion and
+// product take 6 of the vector units' issue slots an element, of the 16 that reading bfloat16 leaves.  Tried and dropped: clipping in reverse order, for what the norm's pass left in
+// the 256 MB cache (704 against 681 us), and adding the partial sums up in every workgroup that clips (no counter; 683 to 820).
 #include <hip/hip_runtime.h>
 
 #include <cstring>
@@ -13,14 +16,19 @@
 namespace dadam {
 namespace {
 
-constexpr uint32_t kNormThreads = 256, kNormWaves = kNormThreads / kWave;
+constexpr uint32_t kClipThreads = 256, kClipWaves = kClipThreads / kWave;
+constexpr uint32_t kNormThreads = kWave * kNormWaves;
 
-__device__ __forceinline__ double group_sum(double sum, double (&partial)[kNormWaves], uint32_t lane, uint32_t wave) {
+template <uint32_t WAVES>
+__device__ __forceinline__ double group_sum(double sum, double (&partial)[WAVES], uint32_t lane, uint32_t wave) {
 #pragma unroll
   for (int off = kWave / 2; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
   if (lane == 0) partial[wave] = sum;
   __syncthreads();
-  return (partial[0] + partial[1]) + (partial[2] + partial[3]);
+  sum = partial[0];
+#pragma unroll
+  for (uint32_t w = 1; w < WAVES; ++w) sum += partial[w];
+  return sum;
 }
 
 // The sum of a row's partial sums, the same in every workgroup that forms it.
@@ -117,7 +125,7 @@ __global__ __launch_bounds__(kNormThreads) void k_grad_norm(const NormArgs<N> a)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     last = __hip_atomic_fetch_add(a.arrived + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == a.per_row;
   }
-  __syncthreads();
+  __syncthreads();  // (also: everybody has read the partial sums, which the next sum overwrites)
   if (last) {
     const double all = row_sum(row_partials, a.per_row, partial, lane, wave);
     if (threadIdx.x == 0) {
@@ -145,11 +153,11 @@ __device__ __forceinline__ void clip_unit(const Cuts& cuts, uint64_t d, const Un
 }
 
 template <typename GT, bool NT, int N>
-__global__ __launch_bounds__(kNormThreads) void k_clip(const NormArgs<N> a) {
+__global__ __launch_bounds__(kClipThreads) void k_clip(const NormArgs<N> a) {
   const uint32_t lane = threadIdx.x % kWave;
   uint32_t piece, row;
-  const bool active = die_block_piece(blockIdx.x, a.s.n_rows, a.s.n_xcd, (a.s.count + kNormWaves - 1) / kNormWaves, kDieBlockTiles, piece, row, a.s.run);
-  const uint32_t i = a.s.first + piece * kNormWaves + wave_of_group();
+  const bool active = die_block_piece(blockIdx.x, a.s.n_rows, a.s.n_xcd, (a.s.count + kClipWaves - 1) / kClipWaves, kDieBlockTiles, piece, row, a.s.run);
+  const uint32_t i = a.s.first + piece * kClipWaves + wave_of_group();
   const void* g = buffer<const void, 0>(a.row[row]);
   void* out = buffer<void, 1>(a.row[row]);
   const float norm = a.norms[row];
@@ -159,6 +167,59 @@ __global__ __launch_bounds__(kNormThreads) void k_clip(const NormArgs<N> a) {
     const Units<2, 1> u = units_from<2, NT>(i, a.s, lane);
     if (u.whole) clip_unit<GT, true, NT>(a.s.cuts, a.s.d, u, g, out, factor);
     else clip_unit<GT, false, NT>(a.s.cuts, a.s.d, u, g, out, factor);
+  }
+}
+
+// Rows of at most kSmallGranules granules: one workgroup takes a row, holds it in registers (64 floats a lane at most) and does both.  One launch and one
+// pass.  us, two launches / this: 16 rows of 13624 10.7 / 6.7, of 60000 10.6 / 9.2, one of 60000 bfloat16 11.0 / 10.6; 115 of 189 17.9 / 12.3.
+constexpr uint32_t kSmallWaves = 16;
+template <typename GT, int EACH, int N>
+__global__ __launch_bounds__(kWave * kSmallWaves) void k_clip_small(const NormArgs<N> a) {
+  __shared__ double partial[kSmallWaves];
+  const uint32_t lane = threadIdx.x % kWave, wave = wave_of_group();
+  const RowPointers p = a.row[blockIdx.x];
+  float v[EACH][2][4];
+  uint32_t bits[EACH][2];
+  double sums[2] = {0.0, 0.0};
+#pragma unroll
+  for (uint32_t q = 0; q < EACH; ++q) {
+    const uint32_t i = wave + q * kSmallWaves;
+    if (i < a.s.n_granules) {
+      const Units<2, 1> u = units_from<2, false>(i, a.s, lane);
+#pragma unroll
+      for (uint32_t k = 0; k < 2; ++k) {
+        bits[q][k] = u.bits(a.s.cuts, a.s.d, k);
+        load_group<GT, false, false>(based<GT>(buffer<const void, 0>(p), u.base), u.at(k), bits[q][k], u.left, v[q][k]);
+      }
+    }
+  }
+#pragma unroll
+  for (uint32_t q = 0; q < EACH; ++q)
+    if (wave + q * kSmallWaves < a.s.n_granules) {
+#pragma unroll
+      for (uint32_t k = 0; k < 2; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sums[j & 1] = with_square(sums[j & 1], v[q][k][j]);
+    }
+  const double sum = group_sum(sums[0] + sums[1], partial, lane, wave);
+  const float norm = (float)__builtin_sqrt(sum);
+  if (threadIdx.x == 0) a.norms[blockIdx.x] = norm;
+  const bool scales = !(norm <= a.max_norm);
+  if (scales || buffer<const void, 0>(p) != buffer<void, 1>(p)) {
+    const float factor = scales ? a.max_norm / norm : 1.0f;
+#pragma unroll
+    for (uint32_t q = 0; q < EACH; ++q) {
+      const uint32_t i = wave + q * kSmallWaves;
+      if (i < a.s.n_granules) {
+        const Units<2, 1> u = units_from<2, false>(i, a.s, lane);
+#pragma unroll
+        for (uint32_t k = 0; k < 2; ++k) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[q][k][j] *= factor;
+          store_group<GT, false>(based<GT>(buffer<void, 1>(p), u.base), u.at(k), bits[q][k], v[q][k]);
+        }
+      }
+    }
   }
 }
 
@@ -196,11 +257,22 @@ int enqueue_norm(int gdt, NormArgs<N>& a, void* stream) {
 }
 template <int N>
 int enqueue_clip(int gdt, NormArgs<N>& a, void* stream) {
-  return in_pieces(a, kNormWaves * a.s.n_xcd, a.s.n_rows * a.s.n_xcd, kNormThreads, [&](uint32_t grid) { return enqueue_grid(clip_kernel<N>(gdt, a.s.streams), grid, kNormThreads, &a, 0, stream); });
+  return in_pieces(a, kClipWaves * a.s.n_xcd, a.s.n_rows * a.s.n_xcd, kClipThreads, [&](uint32_t grid) { return enqueue_grid(clip_kernel<N>(gdt, a.s.streams), grid, kClipThreads, &a, 0, stream); });
+}
+
+template <int N>
+int enqueue_small(int gdt, NormArgs<N>& a, void* stream) {
+  const bool few = a.s.n_granules <= kSmallGranules / 2;
+  const KernelFn fn = gdt == DADAM_BF16 ? (few ? (KernelFn)k_clip_small<TBF16, kSmallGranules / kSmallWaves / 2, N> : (KernelFn)k_clip_small<TBF16, kSmallGranules / kSmallWaves, N>)
+                                        : (few ? (KernelFn)k_clip_small<TF32, kSmallGranules / kSmallWaves / 2, N> : (KernelFn)k_clip_small<TF32, kSmallGranules / kSmallWaves, N>);
+  return enqueue_grid(fn, a.s.n_rows, kWave * kSmallWaves, &a, 0, stream);
 }
 
 }  // namespace
 
+int launch_clip_small(int gdt, const NormArgs<kMaxRows>& a, void* stream) {
+  return with_block(a, [&](auto& block) { return enqueue_small(gdt, block, stream); });
+}
 int launch_norm(int gdt, const NormArgs<kMaxRows>& a, void* stream) {
   return with_block(a, [&](auto& block) { return enqueue_norm(gdt, block, stream); });
 }

@@ -75,10 +75,10 @@ constexpr uint64_t kMostElems = 1ull << 36;  // index and masks count in 32 bits
 int make_state(dadam_handle* h) {
   std::unique_ptr<OperatorState, void (*)(OperatorState*)> s(new OperatorState(), free_state);
   const std::vector<uint32_t> cuts = build_cuts(h, &s->n_index);
-  // Workgroups of the norm, for all rows together: eight granules a wavefront, so that few have to report where there is little to
-  // read, up to four workgroups a compute unit.  us, 1024 / 2048 / 4096 workgroups: 8 rows of 355 million bfloat16 elements 872 / 898 /
-  // 922, norm and clipping of 4 rows of a million (256 workgroups by the rule: 14) 23 / 34 / 34.
-  s->per_row = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>((granules_of(h) + 31) / 32, 1024 / h->cfg.n_rows));
+  // Workgroups of the norm, sixteen wavefronts each, for all rows together: one a compute unit, four granules a wavefront and more, so that few
+  // have to report.  us, 256 / 512 workgroups: 1e8 float32 elements 64.7 / 64.3, 9 rows of 3.9e6 bfloat16 18.3 / 20.4, 87 of 5.8e5 22.6 / 25.3; two / four / eight
+  // granules: 4e6 elements 10.1 / 8.0 / 8.7, 3 rows of 707 small tensors 8.3 / 8.0 / 10.2.  (1024 workgroups of four wavefronts: the first 73, the second 23.)
+  s->per_row = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>((granules_of(h) + 4 * kNormWaves - 1) / (4 * kNormWaves), 256 / h->cfg.n_rows));
   const size_t sums = (size_t)s->per_row * h->cfg.n_rows * sizeof(double);
   const std::vector<char> zeros(sums + DADAM_MAX_ROWS * sizeof(uint32_t), 0);
   hipError_t e = hipMalloc((void**)&s->partials, zeros.size());
@@ -279,6 +279,7 @@ int norm_impl(dadam_handle* h, const void* const* grads, void* const* out, float
     a.per_row = h->operators->per_row;
     a.norms = norms;
     a.max_norm = max_norm;
+    if (out && a.s.n_granules <= kSmallGranules) return launch_clip_small((int)h->cfg.grad_dtype, a, stream);
     int e = launch_norm((int)h->cfg.grad_dtype, a, stream);
     if (e == (int)hipSuccess && out) e = launch_clip((int)h->cfg.grad_dtype, a, stream);
     return e;

@@ -48,6 +48,8 @@ struct Span {
 };
 
 constexpr int kFewOperands = 16;  // rows and sources of the short argument block (see kFewRows)
+constexpr uint32_t kNormWaves = 16;       // of a workgroup of k_grad_norm
+constexpr uint32_t kSmallGranules = 128;  // see k_clip_small
 constexpr int kMessageRows = 96;  // rows of one launch that also carries the addresses of kMaxRows messages
 
 template <int N>
@@ -99,6 +101,7 @@ enum MixMode : int { kMixStore = 0, kMixAdd = 1, kMixGossip = 2 };
 // and sources send the short one.
 int launch_norm(int gdt, const NormArgs<kMaxRows>& a, void* stream);
 int launch_clip(int gdt, const NormArgs<kMaxRows>& a, void* stream);
+int launch_clip_small(int gdt, const NormArgs<kMaxRows>& a, void* stream);  // norms and clipping of up to kSmallGranules granules
 int launch_encode(int xdt, const EncodeArgs<kMaxRows>& a, void* stream);
 int launch_mix4(int xdt, MixMode mode, uint32_t n_cols, const MixArgs<kMessageRows, kMaxRows>& a, void* stream);
 int launch_round(int xdt, const RoundArgs<kMaxRows>& a, void* stream);

@@ -73,6 +73,7 @@ int launch_norm(int, const NormArgs<kMaxRows>& a, void*) {
   return 0;
 }
 int launch_clip(int, const NormArgs<kMaxRows>& a, void*) { check_span(a.s); check_rows(a.row, a.s, 2); return 0; }
+int launch_clip_small(int gdt, const NormArgs<kMaxRows>& a, void* stream) { return launch_norm(gdt, a, stream) | launch_clip(gdt, a, stream); }
 int launch_encode(int, const EncodeArgs<kMaxRows>& a, void*) { check_span(a.s); check_rows(a.row, a.s, 4); return 0; }
 int launch_mix4(int, MixMode mode, uint32_t n_cols, const MixArgs<kMessageRows, kMaxRows>& a, void*) {
   check_span(a.s);

@@ -36,12 +36,14 @@ def layout_of(kind):
     if kind == "many":                      # most granules cut, over several workgroups
         L = WL.pack([("t%d" % k, (1 + (k * 97) % 700,)) for k in range(300)])
         return list(L.offsets), list(L.numels), L.d
+    if kind == "empty":                     # no tensor has an element
+        return [0, 40], [0, 0], 100
     if kind == "gaps":                      # odd beginnings, whole granules of padding, an empty tensor, an end that is no multiple of 4
         return [3, 70, 701, 5000, 5000, 9001], [60, 500, 1024, 0, 2049, 1002], 10007
     raise ValueError(kind)
 
 
-LAYOUTS = [1, 2, 31, 33, 255, 512, 515, 4096, 100003, "odd", "many", "gaps"]
+LAYOUTS = [1, 2, 31, 33, 255, 512, 515, 4096, 100003, "odd", "many", "gaps", "empty"]
 
 
 def stored_of(layout):
@@ -321,7 +323,7 @@ def check_sums(c, msg, csr, old, got, where):
     return sums, bounds
 
 
-@pytest.mark.parametrize("layout", [1, 33, 515, "odd", "many", "gaps", 40961])
+@pytest.mark.parametrize("layout", [1, 33, 515, "odd", "many", "gaps", "empty", 40961])
 @pytest.mark.parametrize("graph", GRAPHS)
 def test_products_and_gossip(graph, layout):
     rows, cols, kind = graph
@@ -534,6 +536,18 @@ def test_on_another_stream_and_in_a_graph():
             for a, b in zip(got, want):
                 assert same(host(a), host(b))
             (torch.ones(1 << 20, device=DEV) * 2).sum().item()
+
+
+def test_buffers_that_are_not_on_a_gpu_are_refused():
+    with Case(100, 1, csr=WL.identity(1)) as c:
+        on, off, norms = torch.zeros(1, 100, device=DEV), torch.zeros(1, 100), torch.zeros(1, device=DEV)
+        for bad in (off, [off[0]]):
+            with pytest.raises(ValueError, match="not on a GPU"):
+                B.dadam_grad_norm(c.h, bad, norms)
+        with pytest.raises(ValueError, match="not on a GPU"):
+            B.dadam_grad_norm(c.h, on, off[0, :1])
+        with pytest.raises(ValueError, match="not on a GPU"):
+            B.dadam_mx4_round(c.h, 0, on, on, on.clone(), off, 0.5)
 
 
 def test_rows_of_one_tensor():
