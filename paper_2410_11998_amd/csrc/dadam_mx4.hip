@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstring>
+#include <type_traits>
 
 #include "dadam_granule.h"
 
@@ -95,14 +96,15 @@ __device__ __forceinline__ void encode_unit(const Cuts& cuts, uint64_t d, const 
   }
 }
 
-template <typename XT, bool NT, int N>
+template <typename XT, int S, int N>
 __global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_encode(const EncodeArgs<N> a) {
+  constexpr bool NT = S == kStreamsHinted;
   const uint32_t lane = threadIdx.x % kWave;
   uint32_t piece, row;
   const bool active = die_block_piece(blockIdx.x, a.s.n_rows, a.s.n_xcd, (a.s.count + kMixWaves - 1) / kMixWaves, kDieBlockTiles, piece, row, a.s.run);
   const uint32_t i = a.s.first + piece * kMixWaves + wave_of_group();
   if (active && i < a.s.n_granules) {
-    const Units<2, 1> t = units_from<2, NT>(i, a.s, lane);
+    const Units<2, 1> t = units_from<2, S != kStreamsNot>(i, a.s, lane);
     if (t.whole) encode_unit<XT, true, NT>(a.s.cuts, a.s.d, t, a.row[row], a.scale_offset);
     else encode_unit<XT, false, NT>(a.s.cuts, a.s.d, t, a.row[row], a.scale_offset);
   }
@@ -221,14 +223,15 @@ __device__ __forceinline__ void mix_position(const A& a, const Units<2, U>& t, u
 // two, ring of 8 of 3e7 elements 268 / 216, exp. graph of 16 of 2e7 420 / 333, four 430; adding 315 / 390, 458 / 512: their registers leave too few wavefronts).
 template <int MODE>
 constexpr uint32_t kMixUnits = MODE == kMixStore ? 2 : 1;
-template <typename XT, int MODE, bool NT, int N, int C>
+template <typename XT, int MODE, int S, int N, int C>
 __global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_mix(const MixArgs<N, C> a) {
+  constexpr bool NT = S == kStreamsHinted;
   constexpr uint32_t U = kMixUnits<MODE>;
   uint32_t piece, p;
   const bool active = die_block_piece(blockIdx.x, a.s.n_rows, a.s.n_xcd, (a.s.count + kMixWaves * U - 1) / (kMixWaves * U), kDieBlockTiles, piece, p, a.s.run);
   const uint32_t i = a.s.first + (piece * kMixWaves + wave_of_group()) * U;
   if (active && i < a.s.n_granules) {
-    const Units<2, U> t = units_from<2, NT, U>(i, a.s, threadIdx.x % kWave);
+    const Units<2, U> t = units_from<2, S != kStreamsNot, U>(i, a.s, threadIdx.x % kWave);
     if (t.whole) mix_position<XT, MODE, true, NT>(a, t, p);
     else mix_position<XT, MODE, false, NT>(a, t, p);
   }
@@ -253,12 +256,13 @@ __device__ __forceinline__ void mix_rows(const A& a, const Units<2, 1>& t) {
   }
 }
 
-template <int MODE, bool NT, int N, int C>
+template <int MODE, int S, int N, int C>
 __global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_products(const MixArgs<N, C> a) {
+  constexpr bool NT = S == kStreamsHinted;
   const uint32_t pieces = (a.s.count + kMixWaves - 1) / kMixWaves;
   const uint32_t i = a.s.first + die_block_order(blockIdx.x, pieces, a.s.n_xcd, kDieBlockTiles) * kMixWaves + wave_of_group();
   if (i < a.s.n_granules) {
-    const Units<2, 1> t = units_from<2, NT>(i, a.s, threadIdx.x % kWave);
+    const Units<2, 1> t = units_from<2, S != kStreamsNot>(i, a.s, threadIdx.x % kWave);
     if (t.whole) mix_rows<TF32, MODE, true, NT>(a, t);
     else mix_rows<TF32, MODE, false, NT>(a, t);
   }
@@ -277,13 +281,14 @@ __device__ __forceinline__ void copy_unit(const A& a, const Units<2, 1>& t, cons
 #pragma unroll
   for (uint32_t k = 0; k < 2; ++k) store_group<TF32, NT>(based<TF32>(buffer<void, 0>(p), t.base), t.at(k), bits[k], v[k]);
 }
-template <bool NT, int N, int C>
+template <int S, int N, int C>
 __global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_copy(const MixArgs<N, C> a) {
+  constexpr bool NT = S == kStreamsHinted;
   uint32_t piece, p;
   const bool active = die_block_piece(blockIdx.x, a.s.n_rows, a.s.n_xcd, (a.s.count + kMixWaves - 1) / kMixWaves, kDieBlockTiles, piece, p, a.s.run);
   const uint32_t i = a.s.first + piece * kMixWaves + wave_of_group();
   if (active && i < a.s.n_granules) {
-    const Units<2, 1> t = units_from<2, NT>(i, a.s, threadIdx.x % kWave);
+    const Units<2, 1> t = units_from<2, S != kStreamsNot>(i, a.s, threadIdx.x % kWave);
     if (t.whole) copy_unit<true, NT>(a, t, a.row[p]);
     else copy_unit<false, NT>(a, t, a.row[p]);
   }
@@ -326,14 +331,15 @@ __device__ __forceinline__ void mix_shared(const A& a, const Units<2, 1>& t, uin
   }
 }
 
-template <typename XT, int MODE, bool NT, int N, int C>
+template <typename XT, int MODE, int S, int N, int C>
 __global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_shared(const MixArgs<N, C> a) {
+  constexpr bool NT = S == kStreamsHinted;
   __shared__ f4 parts[kMixParts][2][kWave];
   uint32_t i, part;
   const bool active = die_block_piece(blockIdx.x, (a.s.n_rows + a.rows_each - 1) / a.rows_each, a.s.n_xcd, a.s.count, kDieBlockTiles, i, part, a.s.run);
   if (active) {
     const uint32_t from = part * a.rows_each, to = from + a.rows_each < a.s.n_rows ? from + a.rows_each : a.s.n_rows;
-    const Units<2, 1> t = units_from<2, NT>(a.s.first + i, a.s, threadIdx.x % kWave);
+    const Units<2, 1> t = units_from<2, S != kStreamsNot>(a.s.first + i, a.s, threadIdx.x % kWave);
     if (t.whole) mix_shared<XT, MODE, true, NT>(a, t, from, to, parts);
     else mix_shared<XT, MODE, false, NT>(a, t, from, to, parts);
   }
@@ -466,12 +472,13 @@ __device__ __forceinline__ void round_unit(const A& a, const Units<V, 1>& t, uin
   }
 }
 
-template <typename XT, int ROWS, int V, bool NT, int N>
+template <typename XT, int ROWS, int V, int S, int N>
 __global__ __launch_bounds__(kWave * kRoundWaves) void k_mx4_round(const RoundArgs<N> a) {
+  constexpr bool NT = S == kStreamsHinted;
   extern __shared__ __align__(16) uint8_t lds[];  // of every row: the codes of a unit, then its scales; then parts of shared sums
   const uint32_t waves = blockDim.x / kWave, each = (a.s.n_rows + waves - 1) / waves;
   const uint32_t i = a.s.first * (kGranule / kUnitElems<V>) + die_block_order(blockIdx.x, gridDim.x, a.s.n_xcd, kDieBlockTiles);
-  const Units<V, 1> t = units_from<V, NT>(i, a.s, threadIdx.x % kWave);
+  const Units<V, 1> t = units_from<V, S != kStreamsNot>(i, a.s, threadIdx.x % kWave);
   if (t.whole) round_unit<XT, ROWS, V, true, NT>(a, t, each, lds);
   else round_unit<XT, ROWS, V, false, NT>(a, t, each, lds);
 }
@@ -479,20 +486,28 @@ __global__ __launch_bounds__(kWave * kRoundWaves) void k_mx4_round(const RoundAr
 // ---------------------------------------------------------------------------------------------
 // launches
 // ---------------------------------------------------------------------------------------------
+// pick(std::integral_constant<int, S>) for the Streams of a launch
+template <typename Pick>
+KernelFn for_streams(uint32_t streams, Pick pick) {
+  if (streams == kStreamsHinted) return pick(std::integral_constant<int, kStreamsHinted>());
+  if (streams == kStreamsApart) return pick(std::integral_constant<int, kStreamsApart>());
+  return pick(std::integral_constant<int, kStreamsNot>());
+}
+
 template <int N>
 int enqueue_encode(int xdt, EncodeArgs<N> a, void* stream) {
-  const bool nt = a.s.streams;
-  const KernelFn fn = xdt == DADAM_BF16 ? (nt ? (KernelFn)k_mx4_encode<TBF16, true, N> : (KernelFn)k_mx4_encode<TBF16, false, N>)
-                                        : (nt ? (KernelFn)k_mx4_encode<TF32, true, N> : (KernelFn)k_mx4_encode<TF32, false, N>);
+  const KernelFn fn = for_streams(a.s.streams, [&](auto s) {
+    return xdt == DADAM_BF16 ? (KernelFn)k_mx4_encode<TBF16, decltype(s)::value, N> : (KernelFn)k_mx4_encode<TF32, decltype(s)::value, N>;
+  });
   return in_pieces(a, kMixWaves * a.s.n_xcd, a.s.n_rows * a.s.n_xcd, kWave * kMixWaves,
                    [&](uint32_t grid) { return enqueue_grid(fn, grid, kWave * kMixWaves, &a, 0, stream); });
 }
 
-template <int N, int C, bool NT>
+template <int N, int C, int S>
 KernelFn mix_kernel(int xdt, MixMode mode, uint32_t work) {
-  if (work == kMixCopy) return (KernelFn)k_mx4_copy<NT, N, C>;
-  if (work == kMixAllRows) return mode == kMixStore ? (KernelFn)k_mx4_products<kMixStore, NT, N, C> : (KernelFn)k_mx4_products<kMixAdd, NT, N, C>;
-#define DADAM_MIX(XT, MODE) (work == kMixByGroup ? (KernelFn)k_mx4_shared<XT, MODE, NT, N, C> : (KernelFn)k_mx4_mix<XT, MODE, NT, N, C>)
+  if (work == kMixCopy) return (KernelFn)k_mx4_copy<S, N, C>;
+  if (work == kMixAllRows) return mode == kMixStore ? (KernelFn)k_mx4_products<kMixStore, S, N, C> : (KernelFn)k_mx4_products<kMixAdd, S, N, C>;
+#define DADAM_MIX(XT, MODE) (work == kMixByGroup ? (KernelFn)k_mx4_shared<XT, MODE, S, N, C> : (KernelFn)k_mx4_mix<XT, MODE, S, N, C>)
   if (mode == kMixStore) return DADAM_MIX(TF32, kMixStore);
   if (mode == kMixAdd) return DADAM_MIX(TF32, kMixAdd);
   return xdt == DADAM_BF16 ? DADAM_MIX(TBF16, kMixGossip) : DADAM_MIX(TF32, kMixGossip);
@@ -500,7 +515,7 @@ KernelFn mix_kernel(int xdt, MixMode mode, uint32_t work) {
 }
 template <int N, int C>
 int enqueue_mix(int xdt, MixMode mode, MixArgs<N, C> a, void* stream) {
-  const KernelFn fn = a.s.streams ? mix_kernel<N, C, true>(xdt, mode, a.work) : mix_kernel<N, C, false>(xdt, mode, a.work);
+  const KernelFn fn = for_streams(a.s.streams, [&](auto s) { return mix_kernel<N, C, decltype(s)::value>(xdt, mode, a.work); });
   const uint32_t X = a.s.n_xcd;  // kernels that walk rows have as many workgroups on every die
   uint32_t units = kMixWaves, groups = 1;
   if (a.work == kMixByRow) {
@@ -517,10 +532,10 @@ int enqueue_mix(int xdt, MixMode mode, MixArgs<N, C> a, void* stream) {
 }
 
 // Rows a wavefront holds, and its groups a lane: what 128 registers have room for.
-template <int N, bool NT>
+template <int N, int S>
 KernelFn round_kernel(int xdt, uint32_t each) {
   const bool b = xdt == DADAM_BF16;
-#define DADAM_ROUND(ROWS, V) (b ? (KernelFn)k_mx4_round<TBF16, ROWS, V, NT, N> : (KernelFn)k_mx4_round<TF32, ROWS, V, NT, N>)
+#define DADAM_ROUND(ROWS, V) (b ? (KernelFn)k_mx4_round<TBF16, ROWS, V, S, N> : (KernelFn)k_mx4_round<TF32, ROWS, V, S, N>)
   if (each <= 1) return DADAM_ROUND(1, 2);
   if (each <= 2) return DADAM_ROUND(2, 2);
   if (each <= 3) return DADAM_ROUND(3, 2);
@@ -537,7 +552,7 @@ template <int N>
 int enqueue_round(int xdt, RoundArgs<N> a, void* stream) {
   const uint32_t least = (a.s.n_rows + kRoundWaves - 1) / kRoundWaves, most = a.s.n_rows < 3 ? a.s.n_rows : 3;
   const uint32_t each = a.s.streams && least < most ? most : least, waves = (a.s.n_rows + each - 1) / each;
-  const KernelFn fn = a.s.streams ? round_kernel<N, true>(xdt, each) : round_kernel<N, false>(xdt, each);
+  const KernelFn fn = for_streams(a.s.streams, [&](auto s) { return round_kernel<N, decltype(s)::value>(xdt, each); });
   if (fn == nullptr) return (int)hipErrorInvalidDeviceFunction;
   const uint32_t units = each <= 4 ? 1 : 2;  // of a granule
   const uint32_t messages = a.s.n_rows * (units == 1 ? kRoundMessage<2> : kRoundMessage<1>);

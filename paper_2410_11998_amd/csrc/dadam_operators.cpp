@@ -191,7 +191,15 @@ void put(ColPointer* c, const void* p) {
   c->high = (uint32_t)(v >> 32);
 }
 
-void fill_span(const dadam_handle* h, Span* s) {
+bool lines_are_whole(const Table* t, int n_tables) {
+  uintptr_t bits = 0;
+  for (int k = 0; k < n_tables; ++k)
+    for (uint32_t i = 0; t[k].p && i < t[k].n; ++i) bits |= (uintptr_t)t[k].p[i];
+  return bits % 128 == 0;
+}
+
+// whole: all buffers that are streamed begin on a line, or cut lines do not matter (see Streams).
+void fill_span(const dadam_handle* h, bool whole, Span* s) {
   const OperatorState* o = h->operators;
   s->cuts = {o->cuts, o->cuts ? o->cuts + o->n_index : nullptr};
   s->d = h->cfg.d;
@@ -200,7 +208,7 @@ void fill_span(const dadam_handle* h, Span* s) {
   s->count = s->n_granules;
   s->n_rows = h->cfg.n_rows;
   s->n_xcd = h->n_xcds;
-  s->streams = h->nontemporal;
+  s->streams = !h->nontemporal ? kStreamsNot : whole ? kStreamsHinted : kStreamsApart;
   s->run = s->streams ? kDieRunPieces : 1;
 }
 
@@ -273,7 +281,7 @@ int norm_impl(dadam_handle* h, const void* const* grads, void* const* out, float
       put(&a.row[i], 0, grads[i]);
       if (out) put(&a.row[i], 1, out[i]);
     }
-    fill_span(h, &a.s);
+    fill_span(h, true, &a.s);
     a.partials = h->operators->partials;
     a.arrived = h->operators->arrived;
     a.per_row = h->operators->per_row;
@@ -305,7 +313,7 @@ int mix_impl(dadam_handle* h, uint32_t slot, const void* const* msg, float* cons
     // Positions [0, count) of `rows` in as few launches as the argument block allows, of about the same number each.
     MixArgs<kMessageRows, kMaxRows> a;
     memset((void*)&a, 0, sizeof(a));
-    fill_span(h, &a.s);
+    fill_span(h, (mode != kMixGossip && !(mode == kMixAdd && shares_rows(h, lists))) || lines_are_whole(tables + 1, mode == kMixGossip ? 4 : 1), &a.s);
     for (uint32_t c = 0; c < C; ++c) put(&a.message[c], msg[c]);
     a.scale_offset = 16 * blocks_of(h);
     a.gamma = gamma;
@@ -409,7 +417,7 @@ int dadam_mx4_encode(dadam_handle* h, const void* const* x, const float* const* 
         if (copy_out) put(&a.row[i], 2, copy_out[i]);
         put(&a.row[i], 3, msg[i]);
       }
-      fill_span(h, &a.s);
+      fill_span(h, lines_are_whole(tables, 3), &a.s);
       a.scale_offset = 16 * blocks_of(h);
       return launch_encode((int)h->cfg.param_dtype, a, hip_stream);
     });
@@ -461,7 +469,7 @@ int dadam_mx4_round(dadam_handle* h, uint32_t slot, const void* const* x_src, vo
         put(&a.row[p], 2, copy[i]);
         put(&a.row[p], 3, sum[i]);
       }
-      fill_span(h, &a.s);
+      fill_span(h, lines_are_whole(tables, 4), &a.s);
       a.lists = {lists.d_mix_rows, lists.d_mix_entries};
       a.firsts = lists.d_mix_firsts;
       a.n_groups = shares_rows(h, lists) && lists.mix_firsts.size() <= kRoundGroups && lists.mix_entries.size() >= kRoundEntries * lists.mix_firsts.size()

@@ -425,12 +425,13 @@ def test_replicas_agree_and_their_mean_stays():
         assert float((torch.stack(x).double().mean(0) - mean).abs().max()) < 1e-4
 
 
+@pytest.mark.parametrize("shift", [0, 16])
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,graph", [(1, "identity"), (3, "ring"), (16, "exp"), (17, "complete"), (40, "ring"), (70, "ring")])
-def test_layouts_that_stream(rows, graph, kind):
+def test_layouts_that_stream(rows, graph, kind, shift):
     """23 million elements and more in all: accesses carry the streaming hint and the halves of a wavefront lie apart.  Long and short
     tensors, gaps inside and at the ends of the blocks of such halves, an end that is no multiple of 32.  Every call against the oracle
-    on one row, the round against the two calls on every row."""
+    on one row, the round against the two calls on every row.  shift: bytes by which buffers miss the beginning of a line."""
     each = 23_500_000 // rows
     offsets, sizes, at, rng = [], [], 5, np.random.default_rng(rows)
     while at < each:
@@ -453,26 +454,36 @@ def test_layouts_that_stream(rows, graph, kind):
     def values(std, dtype=torch.float32):
         out = []
         for _ in range(rows):
-            t = (torch.randn(d, generator=gen, device=DEV) * std).to(dtype)
+            room = torch.empty(d + 16, dtype=dtype, device=DEV)
+            t = room[shift // room.element_size():][:d]
+            t.copy_(torch.randn(d, generator=gen, device=DEV) * std)
             t[pad] = float("nan")
             out.append(t)
+        return out
+
+    def copies(tensors):
+        out = values(1.0, tensors[0].dtype)
+        for a, b in zip(out, tensors):
+            a.copy_(b)
         return out
     xt = H.TORCH_DT[kind]
     x, copy, total = values(0.02, xt), values(0.02), values(0.02)
     norms, clipped = torch.zeros(rows, device=DEV), values(1.0, xt)
     B.dadam_clip_grads(h, x, clipped, 1.0, norms, stream())
     msg = [torch.zeros(info.bytes, dtype=torch.uint8, device=DEV) for _ in range(rows)]
-    moved, mixed, again, behind = values(1.0), [t.clone() for t in total], [t.clone() for t in total], values(1.0, xt)
+    moved, mixed, again, behind = values(1.0), copies(total), copies(total), values(1.0, xt)
     B.dadam_mx4_encode(h, x, copy, moved, msg, stream())
     B.dadam_mx4_gossip(h, 0, msg, mixed, moved, x, behind, 0.4, stream())
     out = values(1.0)
     B.dadam_mx4_product(h, 0, msg, out, 0, stream())
-    one = [[t.clone() for t in copy], values(1.0, xt)]
+    added = copies(total)
+    B.dadam_mx4_product(h, 0, msg, added, B.DADAM_MX4_ADD, stream())
+    one = [copies(copy), values(1.0, xt)]
     B.dadam_mx4_round(h, 0, x, one[1], one[0], again, 0.4, stream())
     torch.cuda.synchronize()
     for i in range(rows):
-        for a, b in ((one[0][i], moved[i]), (one[1][i], behind[i]), (again[i], mixed[i])):
-            assert torch.equal(a.view(torch.int16 if a.element_size() == 2 else torch.int32), b.view(torch.int16 if b.element_size() == 2 else torch.int32)), i
+        for a, b in ((one[0][i], moved[i]), (one[1][i], behind[i]), (again[i], mixed[i]), (added[i], mixed[i])):
+            assert torch.equal(a.nan_to_num(nan=7.0), b.nan_to_num(nan=7.0)), i
     for t in clipped + moved + mixed + behind + out:
         assert torch.isnan(t[pad]).all() and not torch.isnan(t[~pad]).any()
     i = rows // 2
