@@ -15,47 +15,49 @@
 namespace dadam {
 
 struct OperatorState {
-  uint32_t* cuts = nullptr;   // index and masks of Cuts, null if no padding cuts a granule
-  uint32_t n_index = 0;       // words of index, the masks stand behind
-  double* partials = nullptr; // per_row partial sums a row
+  char* memory = nullptr;      // one allocation: partial sums, counters, index and masks
+  double* partials = nullptr;  // per_row partial sums a row
   uint32_t* arrived = nullptr;
   uint32_t per_row = 1;
+  Cuts cuts{};
 };
 
 namespace {
 
 uint64_t granules_of(const dadam_handle* h) { return (h->cfg.d + kGranule - 1) / kGranule; }
 
-// Index and masks of the layout's granules (see Cuts); empty if all are whole.
-std::vector<uint32_t> build_cuts(const dadam_handle* h, uint32_t* n_index) {
+// Index and masks of the layout's granules (see Cuts), the masks behind the granules_of(h) words of the index; empty if all granules are whole.
+// A granule is whole if one segment covers it; the others get a word of bits for each of their blocks.  Segments that touch (they differ in decay)
+// may cover a granule between them: its bits are then all set.
+std::vector<uint32_t> build_cuts(const dadam_handle* h) {
   const uint64_t n = granules_of(h);
-  std::vector<uint32_t> index(n, 0), masks;
-  // A granule is whole if one segment covers it; the others get a word of bits for each of their blocks, here side by side in order.
-  uint64_t covered = 0;  // granules before this one have their entry
+  std::vector<uint32_t> index, masks;
   auto cut = [&](uint64_t g) -> uint32_t* {
+    if (index.empty()) index.assign(n, 0);
     if (index[g] == 0) {
       masks.resize(masks.size() + kGranuleBlocks, 0u);
       index[g] = (uint32_t)(masks.size() - kGranuleBlocks) + 1;
     }
     return masks.data() + index[g] - 1;
   };
-  for (size_t k = 0; k <= h->segs.size(); ++k) {
-    const bool end = k == h->segs.size();
-    const uint64_t lo = end ? n * kGranule : h->segs[k].lo, hi = end ? lo : h->segs[k].hi;
-    for (uint64_t g = covered; g < lo / kGranule; ++g) cut(g);  // nothing but padding, or begun by the segment before
-    covered = std::max(covered, lo / kGranule);
-    for (uint64_t g = lo / kGranule; !end && g * kGranule < hi; ++g) {
-      const uint64_t from = std::max(lo, g * kGranule), to = std::min(hi, (g + 1) * kGranule);
-      if (to - from == kGranule) {
-        covered = g + 1;
-        continue;
-      }
-      uint32_t* m = cut(g);
-      for (uint64_t e = from; e < to; ++e) m[e % kGranule / kMxBlock] |= 1u << e % kMxBlock;
-      if (to == (g + 1) * kGranule) covered = g + 1;
+  auto part = [&](uint64_t lo, uint64_t hi) {  // of one granule
+    if (lo >= hi) return;
+    uint32_t* m = cut(lo / kGranule);
+    for (uint64_t e = lo; e < hi; ++e) m[e % kGranule / kMxBlock] |= 1u << e % kMxBlock;
+  };
+  uint64_t done = 0;  // granules before this one are whole or have their entry
+  for (const Segment& s : h->segs) {
+    const uint64_t first = (s.lo + kGranule - 1) / kGranule, last = s.hi / kGranule;  // whole granules [first, last)
+    for (; done < s.lo / kGranule; ++done) cut(done);  // nothing but padding, or begun by the segment before
+    if (first <= last) {
+      part(s.lo, first * kGranule);
+      part(last * kGranule, s.hi);
+    } else {
+      part(s.lo, s.hi);
     }
+    done = std::max(done, std::max(first, last));
   }
-  *n_index = (uint32_t)n;
+  for (; done < n; ++done) cut(done);
   if (masks.empty()) return {};
   index.insert(index.end(), masks.begin(), masks.end());
   return index;
@@ -63,35 +65,34 @@ std::vector<uint32_t> build_cuts(const dadam_handle* h, uint32_t* n_index) {
 
 void free_state(OperatorState* s) {
   if (!s) return;
-  if (s->cuts) (void)hipFree(s->cuts);
-  if (s->partials) (void)hipFree(s->partials);
+  if (s->memory) (void)hipFree(s->memory);
   delete s;
 }
 
 constexpr uint64_t kMostElems = 1ull << 36;  // index and masks count in 32 bits
 
-// Segments with different decay that touch are one run of elements here: build_cuts sees every segment alone, and a granule that two
-// of them share gets masks whose bits add up to all elements, which costs a little and changes nothing.
 int make_state(dadam_handle* h) {
   std::unique_ptr<OperatorState, void (*)(OperatorState*)> s(new OperatorState(), free_state);
-  const std::vector<uint32_t> cuts = build_cuts(h, &s->n_index);
+  const std::vector<uint32_t> cuts = build_cuts(h);
   // Workgroups of the norm, sixteen wavefronts each, for all rows together: one a compute unit, four granules a wavefront and more, so that few
   // have to report.  us, 256 / 512 workgroups: 1e8 float32 elements 64.7 / 64.3, 9 rows of 3.9e6 bfloat16 18.3 / 20.4, 87 of 5.8e5 22.6 / 25.3; two / four / eight
   // granules: 4e6 elements 10.1 / 8.0 / 8.7, 3 rows of 707 small tensors 8.3 / 8.0 / 10.2.  (1024 workgroups of four wavefronts: the first 73, the second 23.)
   s->per_row = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>((granules_of(h) + 4 * kNormWaves - 1) / (4 * kNormWaves), 256 / h->cfg.n_rows));
-  const size_t sums = (size_t)s->per_row * h->cfg.n_rows * sizeof(double);
-  const std::vector<char> zeros(sums + DADAM_MAX_ROWS * sizeof(uint32_t), 0);
-  hipError_t e = hipMalloc((void**)&s->partials, zeros.size());
-  if (e == hipSuccess) e = hipMemcpy(s->partials, zeros.data(), zeros.size(), hipMemcpyHostToDevice);
-  if (e == hipSuccess && !cuts.empty()) {
-    e = hipMalloc((void**)&s->cuts, cuts.size() * sizeof(uint32_t));
-    if (e == hipSuccess) e = hipMemcpy(s->cuts, cuts.data(), cuts.size() * sizeof(uint32_t), hipMemcpyHostToDevice);
-  }
+  const size_t sums = (size_t)s->per_row * h->cfg.n_rows * sizeof(double), head = sums + DADAM_MAX_ROWS * sizeof(uint32_t);
+  std::vector<char> image(head + cuts.size() * sizeof(uint32_t), 0);
+  if (!cuts.empty()) memcpy(image.data() + head, cuts.data(), cuts.size() * sizeof(uint32_t));
+  hipError_t e = hipMalloc((void**)&s->memory, image.size());
+  if (e == hipSuccess) e = hipMemcpy(s->memory, image.data(), image.size(), hipMemcpyHostToDevice);
   if (e != hipSuccess) {
     (void)hipGetLastError();
     return fail(h, DADAM_EHIP, "setting up the operators around the step failed: %s", hipGetErrorString(e));
   }
-  s->arrived = reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(s->partials) + sums);
+  s->partials = reinterpret_cast<double*>(s->memory);
+  s->arrived = reinterpret_cast<uint32_t*>(s->memory + sums);
+  if (!cuts.empty()) {
+    s->cuts.index = reinterpret_cast<uint32_t*>(s->memory + head);
+    s->cuts.masks = s->cuts.index + granules_of(h);
+  }
   h->operators = s.release();
   h->free_operators = free_state;
   return DADAM_OK;
@@ -200,8 +201,7 @@ bool lines_are_whole(const Table* t, int n_tables) {
 
 // whole: all buffers that are streamed begin on a line, or cut lines do not matter (see Streams).
 void fill_span(const dadam_handle* h, bool whole, Span* s) {
-  const OperatorState* o = h->operators;
-  s->cuts = {o->cuts, o->cuts ? o->cuts + o->n_index : nullptr};
+  s->cuts = h->operators->cuts;
   s->d = h->cfg.d;
   s->n_granules = (uint32_t)granules_of(h);
   s->first = 0;
