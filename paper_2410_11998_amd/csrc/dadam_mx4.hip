@@ -503,19 +503,29 @@ int enqueue_encode(int xdt, EncodeArgs<N> a, void* stream) {
                    [&](uint32_t grid) { return enqueue_grid(fn, grid, kWave * kMixWaves, &a, 0, stream); });
 }
 
+// Only what the host's rules ask for (fill_span's calls, share_rows, copies_rows) has a kernel; anything else is refused by the launch.
 template <int N, int C, int S>
 KernelFn mix_kernel(int xdt, MixMode mode, uint32_t work) {
-  if (work == kMixCopy) return (KernelFn)k_mx4_copy<S, N, C>;
-  if (work == kMixAllRows) return mode == kMixStore ? (KernelFn)k_mx4_products<kMixStore, S, N, C> : (KernelFn)k_mx4_products<kMixAdd, S, N, C>;
-#define DADAM_MIX(XT, MODE) (work == kMixByGroup ? (KernelFn)k_mx4_shared<XT, MODE, S, N, C> : (KernelFn)k_mx4_mix<XT, MODE, S, N, C>)
-  if (mode == kMixStore) return DADAM_MIX(TF32, kMixStore);
-  if (mode == kMixAdd) return DADAM_MIX(TF32, kMixAdd);
-  return xdt == DADAM_BF16 ? DADAM_MIX(TBF16, kMixGossip) : DADAM_MIX(TF32, kMixGossip);
-#undef DADAM_MIX
+  const bool by_group = work == kMixByGroup;
+  if (mode == kMixGossip) {
+    if (xdt == DADAM_BF16) return by_group ? (KernelFn)k_mx4_shared<TBF16, kMixGossip, S, N, C> : (KernelFn)k_mx4_mix<TBF16, kMixGossip, S, N, C>;
+    return by_group ? (KernelFn)k_mx4_shared<TF32, kMixGossip, S, N, C> : (KernelFn)k_mx4_mix<TF32, kMixGossip, S, N, C>;
+  }
+  if (mode == kMixAdd && by_group) return (KernelFn)k_mx4_shared<TF32, kMixAdd, S, N, C>;
+  if (mode == kMixAdd && work == kMixAllRows) return (KernelFn)k_mx4_products<kMixAdd, S, N, C>;
+  if constexpr (S != kStreamsApart) {  // (rows that do not share their sum, and products that store, keep the hint)
+    if (mode == kMixAdd) return (KernelFn)k_mx4_mix<TF32, kMixAdd, S, N, C>;
+    if (by_group) return (KernelFn)k_mx4_shared<TF32, kMixStore, S, N, C>;
+    if (work == kMixAllRows) return (KernelFn)k_mx4_products<kMixStore, S, N, C>;
+    if (work == kMixByRow) return (KernelFn)k_mx4_mix<TF32, kMixStore, S, N, C>;
+    if constexpr (S == kStreamsHinted) return (KernelFn)k_mx4_copy<S, N, C>;
+  }
+  return nullptr;
 }
 template <int N, int C>
 int enqueue_mix(int xdt, MixMode mode, MixArgs<N, C> a, void* stream) {
   const KernelFn fn = for_streams(a.s.streams, [&](auto s) { return mix_kernel<N, C, decltype(s)::value>(xdt, mode, a.work); });
+  if (fn == nullptr) return (int)hipErrorInvalidDeviceFunction;
   const uint32_t X = a.s.n_xcd;  // kernels that walk rows have as many workgroups on every die
   uint32_t units = kMixWaves, groups = 1;
   if (a.work == kMixByRow) {
@@ -531,22 +541,26 @@ int enqueue_mix(int xdt, MixMode mode, MixArgs<N, C> a, void* stream) {
   return in_pieces(a, units, groups, kWave * kMixWaves, [&](uint32_t grid) { return enqueue_grid(fn, grid, kWave * kMixWaves, &a, 0, stream); });
 }
 
-// Rows a wavefront holds, and its groups a lane: what 128 registers have room for.
+// Rows a wavefront holds, and its groups a lane: what 128 registers have room for.  Up to kFewOperands rows: one where handles do not stream, up to three
+// where they do; more rows: two at least, where handles stream three.
 template <int N, int S>
 KernelFn round_kernel(int xdt, uint32_t each) {
   const bool b = xdt == DADAM_BF16;
 #define DADAM_ROUND(ROWS, V) (b ? (KernelFn)k_mx4_round<TBF16, ROWS, V, S, N> : (KernelFn)k_mx4_round<TF32, ROWS, V, S, N>)
-  if (each <= 1) return DADAM_ROUND(1, 2);
-  if (each <= 2) return DADAM_ROUND(2, 2);
-  if (each <= 3) return DADAM_ROUND(3, 2);
-  if constexpr (N > kFewOperands) {
+  if constexpr (N <= kFewOperands) {
+    if (each <= 1) return DADAM_ROUND(1, 2);
+    if constexpr (S != kStreamsNot) return each <= 2 ? DADAM_ROUND(2, 2) : DADAM_ROUND(3, 2);
+    return nullptr;
+  } else {
+    if constexpr (S == kStreamsNot)
+      if (each <= 2) return DADAM_ROUND(2, 2);
+    if (each <= 3) return DADAM_ROUND(3, 2);
     if (each <= 4) return DADAM_ROUND(4, 2);
     if (each <= 6) return DADAM_ROUND(6, 1);
     if (each <= 8) return DADAM_ROUND(8, 1);
     return DADAM_ROUND(10, 1);
   }
 #undef DADAM_ROUND
-  return nullptr;
 }
 template <int N>
 int enqueue_round(int xdt, RoundArgs<N> a, void* stream) {

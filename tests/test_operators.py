@@ -427,7 +427,7 @@ def test_replicas_agree_and_their_mean_stays():
 
 @pytest.mark.parametrize("shift", [0, 16])
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
-@pytest.mark.parametrize("rows,graph", [(1, "identity"), (3, "ring"), (16, "exp"), (17, "complete"), (40, "ring"), (70, "ring")])
+@pytest.mark.parametrize("rows,graph", [(1, "identity"), (3, "ring"), (16, "exp"), (17, "complete"), (40, "ring"), (60, "complete"), (70, "ring")])
 def test_layouts_that_stream(rows, graph, kind, shift):
     """23 million elements and more in all: accesses carry the streaming hint and the halves of a wavefront lie apart.  Long and short
     tensors, gaps inside and at the ends of the blocks of such halves, an end that is no multiple of 32.  Every call against the oracle
@@ -504,6 +504,41 @@ def test_layouts_that_stream(rows, graph, kind, shift):
     ref = v + float(np.float32(0.4)) * (s - c)
     bound = 0.41 * EPS * (np.abs(s) + np.abs(c)) + 1.01 * EPS * np.abs(ref) + TINY + (2.0 ** -8 * np.abs(ref) if kind == "bf16" else 0)
     assert np.all((np.abs(host(behind[i]) - ref) <= bound)[stored])
+    B.dadam_destroy(h)
+
+
+def test_large_products_whose_rows_share_their_sums():
+    """1e8 elements and more in all rows: one row of every list is formed and the others are copies of it.  Two loops of the alternating
+    exponential ring and two nodes by themselves, 20 rows, gaps and odd ends; every row against the oracle's sum of its list."""
+    rows, d = 20, 5_200_007
+    offsets, sizes = [0, 1_000_003, 3_000_100], [1_000_000, 1_999_777, d - 3_000_103]
+    stored = stored_of((offsets, sizes, d))
+    pad = torch.from_numpy(~stored).to(DEV)
+    csr = WL.aer(rows // 4, 0)
+    h = B.dadam_init(rows, rows, d, offsets, sizes, B.DADAM_F32, B.DADAM_F32)
+    B.dadam_set_topology(h, 0, *csr)
+    info = B.dadam_mx4_get_info(h)
+    msg = []
+    for r in range(rows):
+        m = torch.zeros(info.bytes, dtype=torch.uint8, device=DEV)
+        x = torch.randn(d, device=DEV) * 0.02
+        x[pad] = float("nan")
+        one = B.dadam_init(1, 1, d, offsets, sizes, B.DADAM_F32, B.DADAM_F32)
+        B.dadam_mx4_encode(one, [x], None, None, [m], stream())
+        torch.cuda.synchronize()
+        B.dadam_destroy(one)
+        msg.append(m)
+    out = torch.full((rows, d + 1), float("nan"), device=DEV)       # an even number of elements: every other row misses a line, all are aligned
+    B.dadam_mx4_product(h, 0, msg, out, 0, stream())
+    torch.cuda.synchronize()
+    values = [O.decode(m.cpu().numpy(), d).astype(np.float32).astype(np.float64) for m in msg]
+    for i in range(rows):
+        entries = [int(c) for c in csr[1][csr[0][i]:csr[0][i + 1]]]
+        terms = [float(np.float32(1.0 / len(entries))) * values[c] for c in entries]
+        bound = (len(entries) + 2) * EPS * sum(np.abs(v) for v in terms) + (len(entries) + 2) * TINY
+        got = host(out[i])
+        assert np.all((np.abs(got[:d] - sum(terms)) <= bound)[stored]), i
+        assert np.isnan(got[:d][~stored]).all() and np.isnan(got[d])
     B.dadam_destroy(h)
 
 
