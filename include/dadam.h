@@ -427,8 +427,8 @@ int dadam_place_by_timing(void* arena, uint64_t arena_bytes, int32_t device, con
 
 /* The global norm of every row's gradient over all tensors of the layout,
  *     norms[i] = sqrt(sum_e grads[i][e]^2),
- * to norms[n_rows], DEVICE memory, float32.  Squares and sums are taken in 64 bits, in an order that depends on the layout
- * and n_rows only: the same inputs give the same bits, and no square overflows or vanishes.  A NaN makes the norm NaN,
+ * to norms[n_rows], DEVICE memory, float32.  Squares and sums are taken in 64 bits, in an order that depends on the layout,
+ * n_rows and the entry point only: the same call gives the same bits, and no square overflows or vanishes.  A NaN makes the norm NaN,
  * an infinity (without a NaN) makes it infinite; a norm above float32's range is infinite too.  Calls of dadam_grad_norm and dadam_clip_grads on one handle must not
  * overlap in time: they share the handle's partial sums. */
 int dadam_grad_norm(dadam_handle* h, const void* const* grads, float* norms, void* hip_stream);

@@ -513,5 +513,8 @@ def current_stream() -> int:
     if _raw_stream is None:
         import torch
         torch.cuda.current_stream()     # sets the device up
-        _raw_stream = (torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice)
+        if hasattr(torch._C, "_cuda_getCurrentRawStream") and hasattr(torch._C, "_cuda_getDevice"):
+            _raw_stream = (torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice)
+        else:
+            _raw_stream = (lambda _: int(torch.cuda.current_stream().cuda_stream), lambda: 0)
     return _raw_stream[0](_raw_stream[1]())
