@@ -117,20 +117,24 @@ __global__ __launch_bounds__(kNormThreads) void k_grad_norm(const NormArgs<N> a)
     else add_granules<GT, kAtOnce, false, NT>(a.s, g, i0, stride, lane, sums);
   }
   const double sum = group_sum(sums[0] + sums[1], partial, lane, wave);
-  double* row_partials = a.partials + (uint64_t)row * a.per_row;
-  if (threadIdx.x == 0) {
-    __hip_atomic_store(row_partials + part, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    // Both go to where all dies see them: the sum has to be there before the count.  (A release of the agent's scope would
-    // write the die's whole L2 back for that: norms and clipping of 4 x 1048576 elements 58 us, 13 us without.)
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    last = __hip_atomic_fetch_add(a.arrived + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == a.per_row;
-  }
-  __syncthreads();  // (also: everybody has read the partial sums, which the next sum overwrites)
-  if (last) {
-    const double all = row_sum(row_partials, a.per_row, partial, lane, wave);
+  if (a.per_row == 1) {  // nobody to wait for (the report and its answer take 3 us)
+    if (threadIdx.x == 0) a.norms[row] = (float)__builtin_sqrt(sum);
+  } else {
+    double* row_partials = a.partials + (uint64_t)row * a.per_row;
     if (threadIdx.x == 0) {
-      a.norms[row] = (float)__builtin_sqrt(all);
-      __hip_atomic_store(a.arrived + row, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(row_partials + part, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      // Both go to where all dies see them: the sum has to be there before the count.  (A release of the agent's scope would
+      // write the die's whole L2 back for that: norms and clipping of 4 x 1048576 elements 58 us, 13 us without.)
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      last = __hip_atomic_fetch_add(a.arrived + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == a.per_row;
+    }
+    __syncthreads();  // (also: everybody has read the partial sums, which the next sum overwrites)
+    if (last) {
+      const double all = row_sum(row_partials, a.per_row, partial, lane, wave);
+      if (threadIdx.x == 0) {
+        a.norms[row] = (float)__builtin_sqrt(all);
+        __hip_atomic_store(a.arrived + row, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
     }
   }
 }
