@@ -409,6 +409,34 @@ def test_round_is_encoding_and_gossip(rows, graph, kind):
             c.padding_is_untouched(one[0] + one[1] + one[2])
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_workers_by_themselves_do_what_all_replicas_in_one_handle_do(kind):
+    """Six workers on a ring, each with a handle of one row and three messages (its own and the two it receives), against one handle of six
+    rows: the same bits after four rounds, x, copies and sums."""
+    n = 6
+    with Case("many", n, kind=kind, csr=WL.ring(n), seed=9) as c:
+        x, copy, total = c.values(0.02, kind), c.values(0.02), c.values(0.02)
+        alone = [[t.clone() for t in v] for v in (x, copy, total)]
+        handles, msg = [], c.messages(n)
+        for _ in range(n):
+            h = B.dadam_init(1, 3, c.d, c.offsets, c.sizes, H.ABI_DT[kind], H.ABI_DT[kind])
+            B.dadam_set_topology(h, 0, *WL.node_share_ring())
+            handles.append(h)
+        for _ in range(4):
+            B.dadam_mx4_round(c.h, 0, x, x, copy, total, 0.5, stream())
+            for i, h in enumerate(handles):
+                B.dadam_mx4_encode(h, alone[0][i:i + 1], alone[1][i:i + 1], alone[1][i:i + 1], msg[i:i + 1], stream())
+            for i, h in enumerate(handles):
+                received = [msg[i], msg[(i - 1) % n], msg[(i + 1) % n]]
+                B.dadam_mx4_gossip(h, 0, received, alone[2][i:i + 1], alone[1][i:i + 1], alone[0][i:i + 1], alone[0][i:i + 1], 0.5, stream())
+        torch.cuda.synchronize()
+        for a, b in zip((x, copy, total), alone):
+            for i in range(n):
+                assert same(host(a[i]), host(b[i])), i
+        for h in handles:
+            B.dadam_destroy(h)
+
+
 def test_replicas_agree_and_their_mean_stays():
     """Rounds alone bring replicas together although 4 bits are sent, and their mean moves by rounding only."""
     n, d = 8, 6000
