@@ -32,10 +32,10 @@ __device__ __forceinline__ uint32_t cut_of(const Cuts& c, uint32_t granule) {
   typedef const uint32_t __attribute__((address_space(4))) * Constant;
   return c.index ? ((Constant)c.index)[granule] : 0u;
 }
-// Which of the n elements from e on (multiples of n, 4 or 8) belong to a tensor; none behind the vector.
-__device__ __forceinline__ uint32_t stored_bits(const Cuts& c, uint64_t d, uint64_t e, int n) {
-  const uint32_t all = (1u << n) - 1, cut = c.index && e < d ? c.index[e / kGranule] : 0u;
-  return e >= d ? 0u : cut == 0 ? all : (c.masks[cut - 1 + e % kGranule / kMxBlock] >> (e % kMxBlock)) & all;
+// Which of the n elements from e on (multiples of n, 4 or 8; inside the vector) belong to a tensor; cut: of their granule.
+__device__ __forceinline__ uint32_t stored_bits(const Cuts& c, uint32_t cut, uint32_t e, int n) {
+  const uint32_t all = (1u << n) - 1;
+  return cut == 0 ? all : (c.masks[cut - 1 + e % kGranule / kMxBlock] >> (e % kMxBlock)) & all;
 }
 
 // Where a wavefront's unit of 512 elements (V = 2) or 256 (V = 1) lies: lane l holds V groups of four from a place of its own on, 64 or 256
@@ -49,10 +49,11 @@ struct Units {
   uint32_t left;     // elements from there to the end of the vector (2^31 - 1: so many or more)
   uint32_t first[U];
   uint32_t step;
+  uint32_t cut[U];   // of the granule that the lane's groups of a unit lie in
   bool whole;        // no padding in them
   __device__ __forceinline__ uint32_t at(uint32_t k) const { return first[k / V] + k % V * step; }  // group k of the lane's U V
-  __device__ __forceinline__ Units<V, 1> one(uint32_t u) const { return {base, left, {first[u]}, step, whole}; }
-  __device__ __forceinline__ uint32_t bits(const Cuts& c, uint64_t d, uint32_t k) const { return stored_bits(c, d, base + at(k), 4); }
+  __device__ __forceinline__ Units<V, 1> one(uint32_t u) const { return {base, left, {first[u]}, step, {cut[u]}, whole}; }
+  __device__ __forceinline__ uint32_t bits(const Cuts& c, uint32_t k) const { return at(k) < left ? stored_bits(c, cut[k / V], at(k), 4) : 0u; }
 };
 template <int V>
 constexpr uint32_t kUnitElems = 256 * V;
@@ -73,11 +74,14 @@ __device__ __forceinline__ Units<V, U> units_from(uint32_t i, const Span& s, uin
     if (spread) {
       const uint32_t at = (i % kUnits + u) * (kUnitElems<V> / 2);
       units.first[u] = at + (V == 2 ? 4 * (lane & 15) + 8 * (lane & 16) : 4 * (lane & 31)) + (lane >> 5) * kFar;
-      units.whole &= (cut_of(s.cuts, granule + at / kGranule) | cut_of(s.cuts, granule + (at + kFar) / kGranule)) == 0;
+      const uint32_t near = cut_of(s.cuts, granule + at / kGranule), far = cut_of(s.cuts, granule + (at + kFar) / kGranule);
+      units.whole &= (near | far) == 0;
+      units.cut[u] = lane >> 5 ? far : near;
     } else {
       const uint32_t at = (uint32_t)((uint64_t)i * kUnitElems<V> - units.base) + u * kUnitElems<V>;
       units.first[u] = at + 4 * lane;
-      units.whole &= at < units.left && cut_of(s.cuts, granule + at / kGranule) == 0;
+      units.cut[u] = at < units.left ? cut_of(s.cuts, granule + at / kGranule) : 0u;
+      units.whole &= at < units.left && units.cut[u] == 0;
     }
   }
   return units;

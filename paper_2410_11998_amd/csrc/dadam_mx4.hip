@@ -59,7 +59,7 @@ __device__ __forceinline__ void encode(const float (&u)[4], uint32_t& codes, uin
 }
 
 template <typename XT, bool WHOLE, bool NT>
-__device__ __forceinline__ void encode_unit(const Cuts& cuts, uint64_t d, const Units<2, 1>& t, const RowPointers& p, uint64_t scale_offset) {
+__device__ __forceinline__ void encode_unit(const Cuts& cuts, const Units<2, 1>& t, const RowPointers& p, uint64_t scale_offset) {
   const void* x = based<XT>(buffer<const void, 0>(p), t.base);
   const bool differs = buffer<const void, 1>(p) != nullptr, moves = buffer<void, 2>(p) != nullptr;
   const void* before = based<TF32>(buffer<const void, 1>(p), t.base);
@@ -71,7 +71,7 @@ __device__ __forceinline__ void encode_unit(const Cuts& cuts, uint64_t d, const 
   uint32_t bits[2];
 #pragma unroll
   for (uint32_t k = 0; k < 2; ++k) {
-    bits[k] = WHOLE ? 0xFu : t.bits(cuts, d, k);
+    bits[k] = WHOLE ? 0xFu : t.bits(cuts, k);
     load_group<XT, WHOLE, NT>(x, t.at(k), bits[k], t.left, u[k]);
   }
   if (differs) {
@@ -113,8 +113,8 @@ __global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_encode(const EncodeAr
   const uint32_t i = a.s.first + piece * kMixWaves + wave_of_group();
   if (active && i < a.s.n_granules) {
     const Units<2, 1> t = units_from<2, S != kStreamsNot>(i, a.s, lane);
-    if (t.whole) encode_unit<XT, true, NT>(a.s.cuts, a.s.d, t, a.row[row], a.scale_offset);
-    else encode_unit<XT, false, NT>(a.s.cuts, a.s.d, t, a.row[row], a.scale_offset);
+    if (t.whole) encode_unit<XT, true, NT>(a.s.cuts, t, a.row[row], a.scale_offset);
+    else encode_unit<XT, false, NT>(a.s.cuts, t, a.row[row], a.scale_offset);
   }
 }
 
@@ -218,7 +218,7 @@ __device__ __forceinline__ void mix_position(const A& a, const Units<2, U>& t, u
   constexpr int G = 2 * U;
   uint32_t bits[G];
 #pragma unroll
-  for (uint32_t k = 0; k < G; ++k) bits[k] = WHOLE ? 0xFu : t.bits(a.s.cuts, a.s.d, k);
+  for (uint32_t k = 0; k < G; ++k) bits[k] = WHOLE ? 0xFu : t.bits(a.s.cuts, k);
   float mixed[G][4];
   RowUpdate<XT, MODE, U, WHOLE, NT, A> row;
   row.load(a, p, t, bits);
@@ -252,7 +252,7 @@ template <typename XT, int MODE, bool WHOLE, bool NT, typename A>
 __device__ __forceinline__ void mix_rows(const A& a, const Units<2, 1>& t) {
   uint32_t bits[2];
 #pragma unroll
-  for (uint32_t k = 0; k < 2; ++k) bits[k] = WHOLE ? 0xFu : t.bits(a.s.cuts, a.s.d, k);
+  for (uint32_t k = 0; k < 2; ++k) bits[k] = WHOLE ? 0xFu : t.bits(a.s.cuts, k);
   float mixed[2][4];
   int32_t group = -1;
   for (uint32_t p = 0; p < a.s.n_rows; ++p) {
@@ -284,7 +284,7 @@ __device__ __forceinline__ void copy_unit(const A& a, const Units<2, 1>& t, cons
   float v[2][4];
 #pragma unroll
   for (uint32_t k = 0; k < 2; ++k) {
-    bits[k] = WHOLE ? 0xFu : t.bits(a.s.cuts, a.s.d, k);
+    bits[k] = WHOLE ? 0xFu : t.bits(a.s.cuts, k);
     load_group<TF32, WHOLE, false>(based<TF32>(buffer<const void, 1>(p), t.base), t.at(k), bits[k], t.left, v[k]);
   }
 #pragma unroll
@@ -312,7 +312,7 @@ __device__ __forceinline__ void mix_shared(const A& a, const Units<2, 1>& t, uin
   constexpr int G = 2;
   uint32_t bits[G];
 #pragma unroll
-  for (uint32_t k = 0; k < G; ++k) bits[k] = WHOLE ? 0xFu : t.bits(a.s.cuts, a.s.d, k);
+  for (uint32_t k = 0; k < G; ++k) bits[k] = WHOLE ? 0xFu : t.bits(a.s.cuts, k);
   while (from < to) {
     const MixRow r = mix_row(a.lists, from);
     uint32_t end = from + 1;
@@ -392,7 +392,7 @@ __device__ __forceinline__ void round_unit(const A& a, const Units<V, 1>& t, uin
   const uint32_t lane = threadIdx.x % kWave, from = wave_of_group() * each;
   uint32_t bits[V];
 #pragma unroll
-  for (uint32_t k = 0; k < V; ++k) bits[k] = WHOLE ? 0xFu : t.bits(a.s.cuts, a.s.d, k);
+  for (uint32_t k = 0; k < V; ++k) bits[k] = WHOLE ? 0xFu : t.bits(a.s.cuts, k);
   float x[ROWS][V][4], copy[ROWS][V][4];
 #pragma unroll
   for (uint32_t q = 0; q < ROWS; ++q) {

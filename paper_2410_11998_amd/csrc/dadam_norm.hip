@@ -64,7 +64,8 @@ __device__ __forceinline__ void add_squares(const u4& raw, uint32_t stored, doub
 // kAtOnce granules, `stride` apart; all loads are in flight before the first use.  Not WHOLE: some have padding, end behind the vector or lie
 // there.
 template <typename GT, int AT_ONCE, bool WHOLE, bool NT>
-__device__ __forceinline__ void add_granules(const Span& s, const void* g, uint64_t i0, uint32_t stride, uint32_t lane, double (&sums)[2]) {
+__device__ __forceinline__ void add_granules(const Span& s, const void* g, uint64_t i0, uint32_t stride, const uint32_t (&cut)[AT_ONCE], uint32_t lane,
+                                             double (&sums)[2]) {
   constexpr int V = kVectors<GT>, E = kVectorElems<GT>;
   u4 raw[AT_ONCE][V];
   uint32_t stored[AT_ONCE][V];
@@ -73,7 +74,7 @@ __device__ __forceinline__ void add_granules(const Span& s, const void* g, uint6
 #pragma unroll
     for (uint32_t v = 0; v < V; ++v) {
       const uint64_t i = i0 + (uint64_t)k * stride, e = i * kGranule + v * (kGranule / V) + E * lane;
-      stored[k][v] = WHOLE ? 0u : stored_bits(s.cuts, s.d, e, E);
+      stored[k][v] = WHOLE || e >= s.d ? 0u : stored_bits(s.cuts, cut[k], (uint32_t)(e % kGranule), E);
       raw[k][v] = u4{0, 0, 0, 0};
       if (WHOLE || e + E <= s.d) {
         raw[k][v] = vload<NT>(reinterpret_cast<const u4*>(static_cast<const char*>(g) + e * GT::bytes));
@@ -108,13 +109,15 @@ __global__ __launch_bounds__(kNormThreads) void k_grad_norm(const NormArgs<N> a)
   constexpr int kAtOnce = 8 / kVectors<GT>;
   double sums[2] = {0.0, 0.0};
   for (uint64_t i0 = part * kNormWaves + wave; i0 < n; i0 += (uint64_t)kAtOnce * stride) {
-    uint32_t cuts = i0 + (uint64_t)(kAtOnce - 1) * stride >= n;
-    if (a.s.cuts.index && !cuts) {
+    uint32_t cut[kAtOnce], any = i0 + (uint64_t)(kAtOnce - 1) * stride >= n;
 #pragma unroll
-      for (int k = 0; k < kAtOnce; ++k) cuts |= cut_of(a.s.cuts, (uint32_t)i0 + k * stride);
+    for (int k = 0; k < kAtOnce; ++k) {
+      const uint64_t i = i0 + (uint64_t)k * stride;
+      cut[k] = i < n ? cut_of(a.s.cuts, (uint32_t)i) : 0u;
+      any |= cut[k];
     }
-    if (cuts == 0) add_granules<GT, kAtOnce, true, NT>(a.s, g, i0, stride, lane, sums);
-    else add_granules<GT, kAtOnce, false, NT>(a.s, g, i0, stride, lane, sums);
+    if (any == 0) add_granules<GT, kAtOnce, true, NT>(a.s, g, i0, stride, cut, lane, sums);
+    else add_granules<GT, kAtOnce, false, NT>(a.s, g, i0, stride, cut, lane, sums);
   }
   const double sum = group_sum(sums[0] + sums[1], partial, lane, wave);
   if (a.per_row == 1) {  // nobody to wait for (the report and its answer take 3 us)
@@ -140,12 +143,12 @@ __global__ __launch_bounds__(kNormThreads) void k_grad_norm(const NormArgs<N> a)
 }
 
 template <typename GT, bool WHOLE, bool NT>
-__device__ __forceinline__ void clip_unit(const Cuts& cuts, uint64_t d, const Units<2, 1>& u, const void* g, void* out, float factor) {
+__device__ __forceinline__ void clip_unit(const Cuts& cuts, const Units<2, 1>& u, const void* g, void* out, float factor) {
   float v[2][4];
   uint32_t bits[2];
 #pragma unroll
   for (uint32_t k = 0; k < 2; ++k) {
-    bits[k] = WHOLE ? 0xFu : u.bits(cuts, d, k);
+    bits[k] = WHOLE ? 0xFu : u.bits(cuts, k);
     load_group<GT, WHOLE, NT>(based<GT>(g, u.base), u.at(k), bits[k], u.left, v[k]);
   }
 #pragma unroll
@@ -169,8 +172,8 @@ __global__ __launch_bounds__(kClipThreads) void k_clip(const NormArgs<N> a) {
   if (active && i < a.s.n_granules && (scales || g != out)) {
     const float factor = scales ? a.max_norm / norm : 1.0f;
     const Units<2, 1> u = units_from<2, NT>(i, a.s, lane);
-    if (u.whole) clip_unit<GT, true, NT>(a.s.cuts, a.s.d, u, g, out, factor);
-    else clip_unit<GT, false, NT>(a.s.cuts, a.s.d, u, g, out, factor);
+    if (u.whole) clip_unit<GT, true, NT>(a.s.cuts, u, g, out, factor);
+    else clip_unit<GT, false, NT>(a.s.cuts, u, g, out, factor);
   }
 }
 
@@ -192,7 +195,7 @@ __global__ __launch_bounds__(kWave * kSmallWaves) void k_clip_small(const NormAr
       const Units<2, 1> u = units_from<2, false>(i, a.s, lane);
 #pragma unroll
       for (uint32_t k = 0; k < 2; ++k) {
-        bits[q][k] = u.bits(a.s.cuts, a.s.d, k);
+        bits[q][k] = u.bits(a.s.cuts, k);
         load_group<GT, false, false>(based<GT>(buffer<const void, 0>(p), u.base), u.at(k), bits[q][k], u.left, v[q][k]);
       }
     }
