@@ -51,7 +51,7 @@ struct Span {
   uint32_t first, count;
   uint32_t n_rows;
   uint32_t n_xcd;
-  uint32_t run;
+  uint32_t run;         // pieces of a row that a die takes one after the other (see die_block_piece)
   uint32_t streams;     // Streams
 };
 
@@ -103,6 +103,9 @@ struct RoundArgs {
 // Who does what of a launch: a wavefront a row, a workgroup several rows that share their sum, a wavefront all rows; or rows are copies of
 // others (row 0 the copy, 1 what it is of).
 enum MixWork : uint32_t { kMixByRow = 0, kMixByGroup = 1, kMixAllRows = 2, kMixCopy = 3 };
+static_assert(sizeof(NormArgs<kMaxRows>) <= 4096 && sizeof(EncodeArgs<kMaxRows>) <= 4096 && sizeof(RoundArgs<kMaxRows>) <= 4096 &&
+                  sizeof(MixArgs<kMessageRows, kMaxRows>) <= 4096, "the argument block of a launch holds 4 KB");
+
 enum MixMode : int { kMixStore = 0, kMixAdd = 1, kMixGossip = 2 };
 
 // Launchers: enqueue on `stream`, return the hipError_t of the launch as int.  The large block is given; launches of few rows
