@@ -482,7 +482,9 @@ int dadam_mx4_gossip(dadam_handle* h, uint32_t slot, const void* const* msg, flo
                      const void* const* x_src, void* const* x_dst, float gamma, void* hip_stream);
 
 /* One whole round where the handle holds every replica (n_rows == n_cols): dadam_mx4_encode of x_src against copy (in place) and
- * dadam_mx4_gossip of the messages, in one pass and with the same bits, the messages never leaving the chip.  x_dst[i] may be x_src[i]. */
+ * dadam_mx4_gossip of the messages, in one pass and with the same bits, the messages never leaving the chip.  x_dst[i] may be x_src[i].
+ * The messages of a piece of every row lie in LDS: 272 bytes a row up to 64 rows, 136 beyond (21760 at most).  DADAM_EINVAL if that is above
+ * the handle's lds_limit_bytes: dadam_mx4_encode and dadam_mx4_gossip do the same there. */
 int dadam_mx4_round(dadam_handle* h, uint32_t slot, const void* const* x_src, void* const* x_dst, float* const* copy,
                     float* const* sum, float gamma, void* hip_stream);
 

@@ -344,6 +344,7 @@ template <typename XT, int MODE, int S, int N, int C>
 __global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_shared(const MixArgs<N, C> a) {
   constexpr bool NT = S == kStreamsHinted;
   __shared__ f4 parts[kMixParts][2][kWave];
+  static_assert(sizeof(parts) == kSharedBytes, "what the host allows for");
   uint32_t i, part;
   const bool active = die_block_piece(blockIdx.x, (a.s.n_rows + a.rows_each - 1) / a.rows_each, a.s.n_xcd, a.s.count, kDieBlockTiles, i, part, a.s.run);
   if (active) {
@@ -359,9 +360,7 @@ __global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_shared(const MixArgs<
 // exponential graph 7.7 to 7.9 ms (6.0 to 6.2 TB/s), 8 bfloat16 rows of 3e7 786 to 803 us (6.2 to 6.4).
 // One workgroup takes a unit of all rows: its wavefronts deal the rows among themselves, park their messages in LDS,
 // and after one barrier take the neighbours' from there.  What a row holds in registers until then is its x and its copy.
-template <int V>
-constexpr uint32_t kRoundMessage = kUnitElems<V> / 2 + kUnitElems<V> / kMxBlock;  // bytes of a row's message of a unit, by lane
-constexpr uint32_t kRoundWaves = 16;
+static_assert(kRoundMessage<1> == kUnitElems<1> / 2 + kUnitElems<1> / kMxBlock && kRoundMessage<2> == 2 * kRoundMessage<1>, "codes and scales");
 
 // Entries [first, end) of the lists, from the messages in LDS.
 template <int V, typename A>
@@ -576,14 +575,11 @@ KernelFn round_kernel(int xdt, uint32_t each) {
 }
 template <int N>
 int enqueue_round(int xdt, RoundArgs<N> a, void* stream) {
-  const uint32_t least = (a.s.n_rows + kRoundWaves - 1) / kRoundWaves, most = a.s.n_rows < 3 ? a.s.n_rows : 3;
-  const uint32_t each = a.s.streams && least < most ? most : least, waves = (a.s.n_rows + each - 1) / each;
-  const KernelFn fn = for_streams(a.s.streams, [&](auto s) { return round_kernel<N, decltype(s)::value>(xdt, each); });
+  const RoundShape r = round_shape(a.s.n_rows, a.s.streams != kStreamsNot);
+  const KernelFn fn = for_streams(a.s.streams, [&](auto s) { return round_kernel<N, decltype(s)::value>(xdt, r.each); });
   if (fn == nullptr) return (int)hipErrorInvalidDeviceFunction;
-  const uint32_t units = each <= 4 ? 1 : 2;  // of a granule
-  const uint32_t messages = a.s.n_rows * (units == 1 ? kRoundMessage<2> : kRoundMessage<1>);
-  const uint32_t lds = messages + (messages & 8) + a.n_groups * kMixParts * (2 / units) * kWave * 16;
-  return in_pieces(a, 1, units, kWave * waves, [&](uint32_t grid) { return enqueue_grid(fn, grid, kWave * waves, &a, lds, stream); });
+  return in_pieces(a, 1, r.units, kWave * r.waves,
+                   [&](uint32_t grid) { return enqueue_grid(fn, grid, kWave * r.waves, &a, round_bytes(r, a.n_groups), stream); });
 }
 
 }  // namespace

@@ -220,6 +220,7 @@ size_t message_bytes(const dadam_handle* h) { return (size_t)((blocks_of(h) * 17
 // others: a workgroup does, its wavefronts share the list and the rows, and rows are split until there are 4096 workgroups.
 // us, by workgroup / by wavefront, complete graph, product of 100 rows of 4e6 elements 456 / 370, of 1e6 137 / 119, of 4e5 55 / 78, of 32 rows of 4e6 147 / 111,
 // of 2e6 48 / 53, of 4e5 15.5 / 22, of 8 rows of 2e6 18 / 13.5; gossip of 100 rows of 2e6 777 / 845, of 32 rows of 2e6 237 / 259, of 8 rows of 1e6 33 / 35.5.
+// Handles whose workgroups may not use the 8 KB that a shared sum takes go by wavefronts.
 constexpr uint64_t kProductGranules = 1536, kSharedGroups = 4096;
 bool shares_rows(const dadam_handle* h, const Slot& s) { return h->cfg.n_rows >= 4 * s.mix_firsts.size(); }
 void share_rows(const dadam_handle* h, const Slot& s, MixMode mode, uint32_t n_rows, uint32_t* work, uint32_t* rows_each) {
@@ -227,17 +228,25 @@ void share_rows(const dadam_handle* h, const Slot& s, MixMode mode, uint32_t n_r
   *work = kMixByRow;
   *rows_each = 1;
   if (!shares_rows(h, s)) return;
-  if (mode != kMixGossip && granules >= kProductGranules) {
+  const bool room = h->lds_limit >= kSharedBytes;
+  if (mode != kMixGossip && (granules >= kProductGranules || !room)) {
     *work = kMixAllRows;
     return;
   }
+  if (!room) return;
   const uint64_t parts = (kSharedGroups + granules - 1) / granules;
   *work = kMixByGroup;
   *rows_each = std::min((uint32_t)((n_rows + parts - 1) / parts + kMixParts - 1) / kMixParts * kMixParts, n_rows);
 }
 
 // Rounds whose wavefronts form shared sums together: up to kRoundGroups lists (their parts lie in LDS) of kRoundEntries entries and more on average.
+// Where the parts do not fit beside the messages every wavefront forms its own, the same bits.
 constexpr size_t kRoundGroups = 4, kRoundEntries = 12;
+uint32_t round_groups(const dadam_handle* h, const Slot& s) {
+  const size_t n = s.mix_firsts.size();
+  const bool shares = shares_rows(h, s) && n <= kRoundGroups && s.mix_entries.size() >= kRoundEntries * n;
+  return shares && round_bytes(round_shape(h->cfg.n_rows, h->nontemporal), (uint32_t)n) <= h->lds_limit ? (uint32_t)n : 0;
+}
 
 // Products of 1e8 elements in all rows whose rows share sums: one row of every list is formed, and the others are copied from it, a die taking
 // a run of 256 pieces of one row after the other, with what it copies in its L2.  (A wavefront that writes all rows has as many places of
@@ -447,6 +456,9 @@ int dadam_mx4_round(dadam_handle* h, uint32_t slot, const void* const* x_src, vo
   if (!x_src || !x_dst || !copy || !sum) return fail(h, DADAM_EINVAL, "null table");
   if (h->cfg.n_rows != h->cfg.n_cols) return fail(h, DADAM_ESTATE, "a round needs every replica in the handle (n_rows == n_cols)");
   if (int rc = check_gamma(h, gamma)) return rc;
+  const uint32_t lds = round_bytes(round_shape(h->cfg.n_rows, h->nontemporal), 0);
+  if (lds > h->lds_limit)
+    return fail(h, DADAM_EINVAL, "the messages of a round take %u bytes of LDS, the handle's limit is %u: use dadam_mx4_encode and dadam_mx4_gossip", lds, h->lds_limit);
   return guarded(h, [&] {
     const uint32_t R = h->cfg.n_rows;
     const size_t sb = (size_t)h->cfg.d * 4, xb = (size_t)h->cfg.d * dtype_bytes(h->cfg.param_dtype);
@@ -472,8 +484,7 @@ int dadam_mx4_round(dadam_handle* h, uint32_t slot, const void* const* x_src, vo
       fill_span(h, lines_are_whole(tables, 4), &a.s);
       a.lists = {lists.d_mix_rows, lists.d_mix_entries};
       a.firsts = lists.d_mix_firsts;
-      a.n_groups = shares_rows(h, lists) && lists.mix_firsts.size() <= kRoundGroups && lists.mix_entries.size() >= kRoundEntries * lists.mix_firsts.size()
-                       ? (uint32_t)lists.mix_firsts.size() : 0;
+      a.n_groups = round_groups(h, lists);
       a.gamma = gamma;
       return launch_round((int)h->cfg.param_dtype, a, hip_stream);
     });

@@ -108,6 +108,26 @@ static_assert(sizeof(NormArgs<kMaxRows>) <= 4096 && sizeof(EncodeArgs<kMaxRows>)
 
 enum MixMode : int { kMixStore = 0, kMixAdd = 1, kMixGossip = 2 };
 
+constexpr uint32_t kSharedBytes = kMixParts * 2 * kWave * 16;  // LDS of a workgroup that forms a sum together (k_mx4_shared)
+
+// How a round is dealt to a workgroup: rows a wavefront holds, its wavefronts, units of a granule, and the LDS that the messages of a unit take.
+// Streaming handles: three rows a wavefront, or as many as there are.  Up to four rows a wavefront has two groups of four a lane, beyond that one.
+constexpr uint32_t kRoundWaves = 16;
+template <int V>
+constexpr uint32_t kRoundMessage = 128 * V + 8 * V;  // bytes of a row's message of a unit of 256 V elements, by lane
+struct RoundShape {
+  uint32_t each, waves, units, messages;
+};
+inline RoundShape round_shape(uint32_t n_rows, bool streams) {
+  const uint32_t least = (n_rows + kRoundWaves - 1) / kRoundWaves, most = n_rows < 3 ? n_rows : 3;
+  const uint32_t each = streams && least < most ? most : least, units = each <= 4 ? 1 : 2;
+  return {each, (n_rows + each - 1) / each, units, n_rows * (units == 1 ? kRoundMessage<2> : kRoundMessage<1>)};
+}
+// The LDS of a workgroup: the messages, and the parts of the sums that it forms together.
+inline uint32_t round_bytes(const RoundShape& r, uint32_t n_groups) {
+  return n_groups == 0 ? r.messages : r.messages + (r.messages & 8) + n_groups * kMixParts * (2 / r.units) * kWave * 16;
+}
+
 // Launchers: enqueue on `stream`, return the hipError_t of the launch as int.  The large block is given; launches of few rows
 // and sources send the short one.
 int launch_norm(int gdt, const NormArgs<kMaxRows>& a, void* stream);

@@ -1,0 +1,140 @@
+// What the calls around the step ask of the HIP runtime, without a GPU: the built library on a modelled runtime (this program defines
+// the calls, so the library's references resolve here) that says what it was asked for.  Reads commands, a line each, and prints one
+// line for each: the command, the call's answer, and the allocations, copies and launches (kernel, grid x block, bytes of LDS) that it made.
+// tests/test_operators_calls.py builds and runs it.
+//
+//   handle ROWS COLS D PARAM_TYPE GRAD_TYPE LDS_LIMIT     one tensor of D elements
+//   topology SLOT lists N                                 N complete graphs side by side (rows = cols); N = rows: the identity
+//   topology SLOT ring                                    every row, the one before and the one behind
+//   call NAME SLOT                                        norm, clip, encode, product, add, gossip, round
+//   capture 0|1                                           streams are being captured from now on
+#include "dadam.h"
+#include <hip/hip_runtime_api.h>
+#include <cstdio>
+#include <cstdlib>
+#include <cstring>
+#include <iostream>
+#include <map>
+#include <sstream>
+#include <string>
+#include <vector>
+
+static std::string events;
+static bool capturing = false;
+static std::map<const void*, std::string>& kernels() { static std::map<const void*, std::string> m; return m; }
+static void note(const std::string& what) { events += " | " + what; }
+
+extern "C" {
+void** __hipRegisterFatBinary(const void*) { static void* module; return &module; }
+void __hipUnregisterFatBinary(void**) {}
+void __hipRegisterFunction(void**, const void* host, char*, const char* name, unsigned, void*, void*, void*, void*, int*) { kernels()[host] = name; }
+void __hipRegisterVar(void**, void*, char*, char*, int, size_t, int, int) {}
+hipError_t hipGetDevice(int* d) { *d = 0; return hipSuccess; }
+hipError_t hipSetDevice(int) { return hipSuccess; }
+hipError_t hipDeviceGetAttribute(int* v, hipDeviceAttribute_t a, int) {
+  *v = a == hipDeviceAttributeNumberOfXccs ? 8 : 160 * 1024;
+  return hipSuccess;
+}
+// A real runtime refuses both while a stream is being captured, and ends the capture.
+hipError_t hipMalloc(void** p, size_t n) {
+  note("malloc " + std::to_string(n));
+  if (capturing) return hipErrorStreamCaptureUnsupported;
+  *p = malloc(n);
+  return hipSuccess;
+}
+hipError_t hipMemcpy(void* d, const void* s, size_t n, hipMemcpyKind) {
+  note("memcpy " + std::to_string(n));
+  if (capturing) return hipErrorStreamCaptureImplicit;
+  memcpy(d, s, n);
+  return hipSuccess;
+}
+hipError_t hipFree(void* p) { free(p); return hipSuccess; }
+hipError_t hipGetSymbolAddress(void** p, const void*) { static double array[1024]; *p = array; return hipSuccess; }
+hipError_t hipFuncSetAttribute(const void*, hipFuncAttribute, int) { return hipSuccess; }
+hipError_t hipStreamIsCapturing(hipStream_t, hipStreamCaptureStatus* s) {
+  *s = capturing ? hipStreamCaptureStatusActive : hipStreamCaptureStatusNone;
+  return hipSuccess;
+}
+hipError_t hipGetLastError() { return hipSuccess; }
+hipError_t hipLaunchKernel(const void* fn, dim3 grid, dim3 block, void**, size_t lds, hipStream_t) {
+  note("launch " + kernels()[fn] + " " + std::to_string(grid.x) + "x" + std::to_string(block.x) + " " + std::to_string(lds));
+  return hipSuccess;
+}
+}
+
+static uint32_t R, C;
+static uint64_t d;
+
+static int topology(dadam_handle* h, std::istringstream& in) {
+  uint32_t slot, n = 0;
+  std::string kind;
+  in >> slot >> kind >> n;
+  std::vector<int32_t> ptr(1, 0), col;
+  std::vector<float> w;
+  for (uint32_t i = 0; i < R; ++i) {
+    if (kind == "lists") {
+      const uint32_t each = R / n, first = i / each * each;
+      for (uint32_t k = 0; k < each; ++k) col.push_back((int32_t)(first + k));
+    } else {
+      for (uint32_t k : {i, (i + R - 1) % R, (i + 1) % R}) col.push_back((int32_t)k);
+    }
+    w.resize(col.size(), 1.f / (float)(col.size() - (size_t)ptr.back()));
+    ptr.push_back((int32_t)col.size());
+  }
+  return dadam_set_topology(h, slot, ptr.data(), col.data(), w.data(), nullptr);
+}
+
+static int call(dadam_handle* h, std::istringstream& in) {
+  std::string name;
+  uint32_t slot = 0;
+  in >> name >> slot;
+  // addresses only: nothing is read or written
+  const uint64_t step = (4 * d + 255) / 128 * 128, base = 1ull << 32;
+  std::vector<void*> table[6];
+  for (uint64_t t = 0; t < 6; ++t)
+    for (uint64_t i = 0; i < (R > C ? R : C); ++i) table[t].push_back((void*)(base + (t * DADAM_MAX_ROWS + i) * step));
+  auto in_ = [&](int t) { return (const void* const*)table[t].data(); };
+  auto out = [&](int t) { return (void* const*)table[t].data(); };
+  auto f = [&](int t) { return (float* const*)table[t].data(); };
+  float* norms = (float*)(1ull << 30);
+  if (name == "norm") return dadam_grad_norm(h, in_(0), norms, nullptr);
+  if (name == "clip") return dadam_clip_grads(h, in_(0), out(1), 1.f, norms, nullptr);
+  if (name == "encode") return dadam_mx4_encode(h, in_(0), f(1), f(2), out(3), nullptr);
+  if (name == "product") return dadam_mx4_product(h, slot, in_(5), f(0), 0, nullptr);
+  if (name == "add") return dadam_mx4_product(h, slot, in_(5), f(0), DADAM_MX4_ADD, nullptr);
+  if (name == "gossip") return dadam_mx4_gossip(h, slot, in_(5), f(0), f(1), in_(2), out(3), 0.5f, nullptr);
+  if (name == "round") return dadam_mx4_round(h, slot, in_(0), out(1), f(2), f(3), 0.5f, nullptr);
+  return -100;
+}
+
+int main() {
+  dadam_handle* h = nullptr;
+  std::string line;
+  while (std::getline(std::cin, line)) {
+    std::istringstream in(line);
+    std::string what;
+    in >> what;
+    int rc = -100;
+    events.clear();
+    if (what == "handle") {
+      if (h) dadam_destroy(h);
+      h = nullptr;
+      dadam_config cfg{};
+      in >> R >> C >> d >> cfg.param_dtype >> cfg.grad_dtype >> cfg.lds_limit_bytes;
+      const dadam_tensor_desc t = {0, d, 0.f, 0};
+      cfg.abi_version = DADAM_ABI_VERSION; cfg.n_rows = R; cfg.n_cols = C; cfg.d = d; cfg.n_tensors = 1; cfg.tensors = &t;
+      cfg.lr = 1e-3f; cfg.accum_s = 1; cfg.beta_vhat = -1.f; cfg.eps = 1e-8f;
+      rc = dadam_init(&cfg, &h);
+    } else if (what == "topology") {
+      rc = topology(h, in);
+    } else if (what == "call") {
+      rc = call(h, in);
+    } else if (what == "capture") {
+      in >> capturing;
+      rc = 0;
+    }
+    std::cout << line << ": " << rc << (rc < 0 ? std::string(" ") + dadam_last_error(h) : "") << events << "\n";
+  }
+  if (h) dadam_destroy(h);
+  return 0;
+}

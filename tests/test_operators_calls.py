@@ -1,0 +1,86 @@
+"""What the calls around the step ask of the HIP runtime, without a GPU: which kernels they launch, with how much LDS, and when they
+allocate (tests/host_calls_driver.cpp, the built library on a modelled runtime)."""
+
+import os
+import re
+import subprocess
+
+import pytest
+
+from paper_2410_11998_amd import binding as B
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def driver(tmp_path_factory):
+    clang, rocm = "/opt/rocm/lib/llvm/bin/clang++", "/opt/rocm/lib"
+    if not os.path.exists(clang):
+        pytest.skip("clang++ of the ROCm toolchain not available")
+    exe, libdir = str(tmp_path_factory.mktemp("calls") / "calls_driver"), os.path.dirname(B.LIB_PATH)
+    cmd = [clang, "-std=c++17", "-O1", "-rdynamic", "-D__HIP_PLATFORM_AMD__", "-I", os.path.join(ROOT, "include"), "-I", "/opt/rocm/include",
+           os.path.join(ROOT, "tests", "host_calls_driver.cpp"), "-o", exe, "-L", libdir, "-ldadam", f"-Wl,-rpath,{libdir}",
+           f"-Wl,-rpath,{rocm}", f"-Wl,-rpath-link,{rocm}"]
+    r = subprocess.run(cmd, capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, r.stderr[-2000:]
+    return exe
+
+
+class Answer:
+    """One call: its status, the error's text, bytes allocated, and the launches as (kernel, its template arguments, grid, block, LDS)."""
+
+    def __init__(self, line):
+        head, *events = line.split(": ", 1)[1].split(" | ")
+        self.code, _, self.text = head.partition(" ")
+        self.code = int(self.code)
+        self.mallocs = [int(e.split()[1]) for e in events if e.startswith("malloc")]
+        self.launches = []
+        for e in events:
+            m = re.match(r"launch (?:void )?(?:dadam::\(anonymous namespace\)::)?(\w+)<(.*)>\(.*\) (\d+)x(\d+) (\d+)$", e)
+            if m:
+                args = m.group(2).replace("dadam::(anonymous namespace)::", "").split(", ")
+                self.launches.append((m.group(1), args) + tuple(int(m.group(k)) for k in (3, 4, 5)))
+            else:
+                assert not e.startswith("launch"), e
+
+
+def ask(exe, *commands, **env):
+    r = subprocess.run([exe], input="\n".join(commands) + "\n", capture_output=True, text=True, timeout=600, env={**os.environ, **env})
+    assert r.returncode == 0, (r.stdout[-500:], r.stderr[-2000:])
+    plain = subprocess.run(["c++filt"], input=r.stdout, capture_output=True, text=True, timeout=60).stdout.splitlines()
+    assert len(plain) == len(commands), r.stdout
+    return [Answer(x) for x in plain]
+
+
+SHARED_SUM_LDS = 8192     # four parts of a unit's sum
+
+
+@pytest.mark.parametrize("d", [4096, 1_000_000])
+@pytest.mark.parametrize("rows,lists", [(16, 4), (16, 1), (64, 4), (64, 64), (101, 1), (160, 4), (160, 1), (128, 2)])
+def test_rounds_keep_to_the_handles_lds(driver, rows, lists, d):
+    """A round whose messages fit goes without the shared sums' room where that is too much, and one whose messages do not fit is refused
+    before anything is launched.  The messages of a unit of every row: 272 bytes a row up to four rows a wavefront, 136 beyond."""
+    each = max(-(-rows // 16), min(3, rows) if rows * d * 24 > 512 << 20 else 0)
+    messages = rows * (272 if each <= 4 else 136)
+    for limit in (0, 16384, messages, messages - 1, 65536, 1024):
+        *_, a = ask(driver, f"handle {rows} {rows} {d} 0 0 {limit}", f"topology 0 lists {lists}", "call round 0")
+        if 0 < limit < messages:
+            assert a.code == B.DADAM_EINVAL and not a.launches and "dadam_mx4_gossip" in a.text, (limit, a.text)
+            continue
+        assert a.code == 0 and [x[0] for x in a.launches] == ["k_mx4_round"]
+        lds = a.launches[0][4]
+        assert messages <= lds <= (limit or 160 << 10), limit
+        if limit in (0, 65536) and lists <= 4 and rows // lists >= 12:
+            assert lds > messages
+
+
+@pytest.mark.parametrize("d", [4096, 1_000_000])
+@pytest.mark.parametrize("name", ["product", "add", "gossip"])
+def test_shared_sums_keep_to_the_handles_lds(driver, name, d):
+    """Workgroups that form a sum together hold its parts in 8 KB of LDS; a handle with less has a wavefront form every sum."""
+    for limit in (0, SHARED_SUM_LDS, SHARED_SUM_LDS - 1, 1024):
+        *_, a = ask(driver, f"handle 32 32 {d} 0 0 {limit}", "topology 0 lists 1", f"call {name} 0")
+        assert a.code == 0 and a.launches
+        shared = any(x[0] == "k_mx4_shared" for x in a.launches)
+        assert not shared or not 0 < limit < SHARED_SUM_LDS
+        assert shared or limit or (name != "gossip" and d > 786432)
