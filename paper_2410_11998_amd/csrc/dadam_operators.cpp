@@ -256,12 +256,22 @@ bool copies_rows(const dadam_handle* h, const Slot& s, MixMode mode) {
   return mode == kMixStore && h->cfg.d * h->cfg.n_rows >= kManyElems && shares_rows(h, s) && granules_of(h) >= kProductGranules;
 }
 
-// Runs the launches of a call whose arguments have passed, with the handle's device current and its state made.
+bool captures(void* stream) {
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(reinterpret_cast<hipStream_t>(stream), &status) == hipSuccess) return status != hipStreamCaptureStatusNone;
+  (void)hipGetLastError();
+  return true;
+}
+
+// Runs the launches of a call whose arguments have passed, with the handle's device current and its state made.  (Allocating it would end a
+// capture of the caller's.)
 template <typename Launch>
-int on_device(dadam_handle* h, Launch launch) {
+int on_device(dadam_handle* h, void* stream, Launch launch) {
   DeviceGuard guard(h->cfg.device);
   if (guard.err != hipSuccess) return fail(h, DADAM_EHIP, "hipSetDevice: %s", hipGetErrorString(guard.err));
   if (!h->operators) {
+    if (captures(stream))
+      return fail(h, DADAM_ESTATE, "the first call of an operator around the step on a handle allocates: make one before the stream is captured");
     const int rc = make_state(h);
     if (rc) return rc;
   }
@@ -283,7 +293,7 @@ int norm_impl(dadam_handle* h, const void* const* grads, void* const* out, float
     if ((uintptr_t)norms < (uintptr_t)grads[i] + gb && (uintptr_t)grads[i] < (uintptr_t)(norms + R)) rc = fail(h, DADAM_EALIAS, "norms overlaps grads[%u]", i);
   if (!rc) rc = check_device(h);
   if (rc) return rc;
-  return on_device(h, [&] {
+  return on_device(h, stream, [&] {
     NormArgs<kMaxRows> a;
     memset((void*)&a, 0, sizeof(a));
     for (uint32_t i = 0; i < R; ++i) {
@@ -316,7 +326,7 @@ int mix_impl(dadam_handle* h, uint32_t slot, const void* const* msg, float* cons
   if (!rc) rc = check_tables(h, tables, mode == kMixGossip ? 5 : 2);
   if (!rc) rc = check_device(h);
   if (rc) return rc;
-  return on_device(h, [&] {
+  return on_device(h, stream, [&] {
     const Slot& lists = h->slots[slot];
     const bool copies = copies_rows(h, lists, mode);
     // Positions [0, count) of `rows` in as few launches as the argument block allows, of about the same number each.
@@ -417,7 +427,7 @@ int dadam_mx4_encode(dadam_handle* h, const void* const* x, const float* const* 
     int rc = check_tables(h, tables, 4);
     if (!rc) rc = check_device(h);
     if (rc) return rc;
-    return on_device(h, [&] {
+    return on_device(h, hip_stream, [&] {
       EncodeArgs<kMaxRows> a;
       memset((void*)&a, 0, sizeof(a));
       for (uint32_t i = 0; i < R; ++i) {
@@ -470,7 +480,7 @@ int dadam_mx4_round(dadam_handle* h, uint32_t slot, const void* const* x_src, vo
     if (!rc) rc = check_tables(h, tables, 4);
     if (!rc) rc = check_device(h);
     if (rc) return rc;
-    return on_device(h, [&] {
+    return on_device(h, hip_stream, [&] {
       RoundArgs<kMaxRows> a;
       memset((void*)&a, 0, sizeof(a));
       const Slot& lists = h->slots[slot];

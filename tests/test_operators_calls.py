@@ -84,3 +84,18 @@ def test_shared_sums_keep_to_the_handles_lds(driver, name, d):
         shared = any(x[0] == "k_mx4_shared" for x in a.launches)
         assert not shared or not 0 < limit < SHARED_SUM_LDS
         assert shared or limit or (name != "gossip" and d > 786432)
+
+
+NAMES = ["norm", "clip", "encode", "product", "add", "gossip", "round"]
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_a_first_call_under_capture_is_refused_before_it_allocates(driver, name):
+    """An allocation would end the caller's capture.  Once a call has been made, all of them can be recorded."""
+    answers = ask(driver, "handle 4 4 5000 0 0 0", "topology 0 ring", "capture 1", f"call {name} 0", "capture 0", f"call {name} 0",
+                  "capture 1", *(f"call {n} 0" for n in NAMES))
+    first, second, recorded = answers[3], answers[5], answers[7:]
+    assert first.code == B.DADAM_ESTATE and "captur" in first.text and not first.mallocs and not first.launches
+    assert second.code == 0 and second.mallocs and second.launches
+    for a in recorded:
+        assert a.code == 0 and a.launches and not a.mallocs

@@ -52,3 +52,32 @@ def test_handles_with_little_lds_have_the_same_bits(rows, lists, layout):
         for a, b in ((results[0], results[1]), (results[2], results[3])):
             for p, q in zip(a, b):
                 assert same(host(p), host(q))
+
+
+def test_a_first_call_under_capture_leaves_the_capture_alone():
+    """It is refused, and what was recorded before and behind it runs; after a first call outside, calls are recorded."""
+    with Case("many", 4, csr=WL.ring(4)) as c:
+        g, norms, mark = c.values(0.1), torch.zeros(4, device=DEV), torch.zeros(8, device=DEV)
+        side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(graph, stream=side):
+            mark[:4] += 1
+            with pytest.raises(B.DadamError) as e:
+                B.dadam_grad_norm(c.h, g, norms, stream())
+            mark[4:] += 2
+        assert e.value.code == B.DADAM_ESTATE
+        for k in range(1, 4):
+            graph.replay()
+            torch.cuda.synchronize()
+            assert mark.tolist() == [k] * 4 + [2 * k] * 4 and not norms.any()
+        B.dadam_grad_norm(c.h, g, norms, stream())
+        torch.cuda.synchronize()
+        want = norms.clone()
+        again = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(again, stream=side):
+            B.dadam_grad_norm(c.h, g, norms, stream())
+        for _ in range(3):
+            norms.zero_()
+            again.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(norms, want)
