@@ -421,7 +421,8 @@ int dadam_place_by_timing(void* arena, uint64_t arena_bytes, int32_t device, con
  * gradients cfg.d of grad_dtype, copies and sums cfg.d float32, messages dadam_mx4_info.bytes bytes.  What a call writes must not
  * overlap anything else it reads or writes, but where "in place" is named.  Padding between tensors takes no part: it is
  * neither used nor written.  The first such call on a handle allocates and uploads what tells padding from elements (4 bytes for every 512
- * elements, 64 more where padding lies among them; nothing for one tensor of a multiple of 512) and the scratch of the norms; it may wait for the device and is refused while
+ * elements, 64 more where padding lies among them; nothing for one tensor of a multiple of 512), the scratch of the norms and the lists of the slots
+ * as these calls read them (from then on dadam_set_topology does that); it may wait for the device and is refused while
  * hip_stream is being captured, later calls allocate nothing and may be recorded into a graph.
  * Errors of all: DADAM_EINVAL (null, address too high, value out of range, d above 2^36), DADAM_EALIGN, DADAM_EALIAS, DADAM_ESTATE (slot empty,
  * host-only handle, first call under capture, n_rows != n_cols where named), DADAM_EHIP. */

@@ -38,11 +38,13 @@ struct Slot {
   const int32_t *d_loop_col = nullptr, *d_loop_rows = nullptr;                              // loop kernel
   const float* d_loop_w = nullptr;
   const Loop* d_loops = nullptr;
+  // What the products with 4-bit messages read: made with the handle's OperatorState, and from then on with the slot.
   std::vector<MixRow> mix_rows;       // see MixRow
   std::vector<MixEntry> mix_entries;
   std::vector<MixRow> mix_firsts;     // the first row of every list
   const MixRow *d_mix_rows = nullptr, *d_mix_firsts = nullptr;
   const MixEntry* d_mix_entries = nullptr;
+  char* d_mix = nullptr;              // the allocation of a slot that was set later than the state
 };
 
 struct DeviceGuard {
@@ -130,9 +132,11 @@ struct dadam_handle {
   float lr = 0.f;
   double betav = 0.0;
   mutable std::string err;
-  // What the operators around the step keep for this handle (dadam_operators.cpp makes it on their first call), and what frees it.
+  // What the operators around the step keep for this handle (dadam_operators.cpp makes it on their first call), what frees it, and what gives
+  // a slot that is set later its lists.
   OperatorState* operators = nullptr;
   void (*free_operators)(OperatorState*) = nullptr;
+  int (*add_mix_lists)(dadam_handle*, Slot*) = nullptr;
 };
 
 namespace dadam {

@@ -791,35 +791,7 @@ void find_loops(uint32_t R, uint32_t C, Slot& s, std::vector<int32_t>& col, std:
   s.loop_of_source = of_source;
 }
 
-// Rows and entries as the products with 4-bit messages take them (see MixRow), in order of the first row of each group.
-void find_mix_rows(uint32_t R, Slot& s) {
-  std::map<std::vector<std::pair<int32_t, float>>, std::vector<int32_t>> by_list;
-  std::vector<std::vector<std::pair<int32_t, float>>> sorted(R);
-  for (uint32_t i = 0; i < R; ++i) {
-    for (int32_t k = s.row_ptr[i]; k < s.row_ptr[i + 1]; ++k) sorted[i].push_back({s.col[k], s.w[k]});
-    std::sort(sorted[i].begin(), sorted[i].end());
-    by_list[sorted[i]].push_back((int32_t)i);
-  }
-  for (uint32_t i = 0; i < R; ++i) {
-    const std::vector<int32_t>& rows = by_list[sorted[i]];
-    if (rows.front() != (int32_t)i) continue;
-    const int32_t first = (int32_t)s.mix_entries.size();
-    if (rows.size() > 1) {
-      for (const auto& e : sorted[i]) s.mix_entries.push_back({e.first, e.second});
-    } else {
-      for (int32_t k = s.row_ptr[i]; k < s.row_ptr[i + 1]; ++k) s.mix_entries.push_back({s.col[k], s.w[k]});
-    }
-    const int32_t n = (int32_t)s.mix_entries.size() - first;
-    while (s.mix_entries.size() % kMixAtOnce) s.mix_entries.push_back({s.mix_entries.back().col, 0.f});
-    const int32_t all = (int32_t)s.mix_entries.size() - first, step = kMixAtOnce * (rows.size() > 1 ? kMixParts : 1);
-    const int32_t part = rows.size() > 1 ? (all + step - 1) / step * kMixAtOnce : all;
-    const int16_t group = (int16_t)s.mix_firsts.size();
-    for (int32_t row : rows) s.mix_rows.push_back({(int16_t)row, group, first, n, part});
-    s.mix_firsts.push_back({(int16_t)i, group, first, n, part});
-  }
-}
-
-// Device copies of everything the kernels read of a slot, in one allocation.
+// Device copies of everything the step's kernels read of a slot, in one allocation.
 hipError_t upload_lists(const dadam_handle* h, Slot& s, const std::vector<int32_t>& loop_col, const std::vector<float>& loop_w,
                         const std::vector<int32_t>& loop_rows) {
   const int32_t R = (int32_t)h->cfg.n_rows, stride = s.max_degree;
@@ -844,7 +816,6 @@ hipError_t upload_lists(const dadam_handle* h, Slot& s, const std::vector<int32_
   const bool has_loops = !s.loops.empty();
   const size_t l = has_loops ? add(s.loops) : 0, lc = has_loops ? add(loop_col) : 0, lww = has_loops ? add(loop_w) : 0,
                lr = has_loops ? add(loop_rows) : 0;
-  const size_t mix_rows = add(s.mix_rows), mix_firsts = add(s.mix_firsts), mix_entries = add(s.mix_entries);
   hipError_t e = hipMalloc((void**)&s.d_lists, image.size());
   if (e == hipSuccess) e = hipMemcpy(s.d_lists, image.data(), image.size(), hipMemcpyHostToDevice);
   if (e != hipSuccess) return e;
@@ -856,14 +827,12 @@ hipError_t upload_lists(const dadam_handle* h, Slot& s, const std::vector<int32_
     s.d_loops = reinterpret_cast<const Loop*>(s.d_lists + l);
     s.d_loop_col = ints(lc); s.d_loop_w = floats(lww); s.d_loop_rows = ints(lr);
   }
-  s.d_mix_rows = reinterpret_cast<const MixRow*>(s.d_lists + mix_rows);
-  s.d_mix_firsts = reinterpret_cast<const MixRow*>(s.d_lists + mix_firsts);
-  s.d_mix_entries = reinterpret_cast<const MixEntry*>(s.d_lists + mix_entries);
   return hipSuccess;
 }
 
 void free_slot(Slot& s) {
   if (s.d_lists) (void)hipFree(s.d_lists);
+  if (s.d_mix) (void)hipFree(s.d_mix);
   s = Slot();
 }
 
@@ -1094,7 +1063,6 @@ int dadam_set_topology(dadam_handle* h, uint32_t slot_id, const int32_t* row_ptr
   std::vector<int32_t> loop_col, loop_rows;
   std::vector<float> loop_w;
   find_loops(R, C, fresh, loop_col, loop_w, loop_rows);
-  find_mix_rows(R, fresh);
   if (h->cfg.device != DADAM_DEVICE_NONE) {
     DeviceGuard guard(h->cfg.device);
     hipError_t e = guard.err;
@@ -1102,6 +1070,10 @@ int dadam_set_topology(dadam_handle* h, uint32_t slot_id, const int32_t* row_ptr
     if (e != hipSuccess) {
       free_slot(fresh);
       return fail(h, DADAM_EHIP, "uploading the neighbour list failed: %s", hipGetErrorString(e));
+    }
+    if (const int rc = h->operators ? h->add_mix_lists(h, &fresh) : DADAM_OK) {
+      free_slot(fresh);
+      return rc;
     }
   }
   if (h->cfg.device != DADAM_DEVICE_NONE) {

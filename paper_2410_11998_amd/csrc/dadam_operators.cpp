@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <map>
 #include <memory>
 #include <new>
 #include <vector>
@@ -15,7 +16,7 @@
 namespace dadam {
 
 struct OperatorState {
-  char* memory = nullptr;      // one allocation: partial sums, counters, index and masks
+  char* memory = nullptr;      // one allocation: partial sums, counters, index and masks, lists of the slots
   double* partials = nullptr;  // per_row partial sums a row
   uint32_t* arrived = nullptr;
   uint32_t per_row = 1;
@@ -23,6 +24,16 @@ struct OperatorState {
 };
 
 namespace {
+
+// No exception leaves an entry point.
+template <typename Fn>
+int guarded(dadam_handle* h, Fn fn) {
+  try {
+    return fn();
+  } catch (const std::bad_alloc&) {
+    return fail(h, DADAM_EINVAL, "out of host memory");
+  }
+}
 
 uint64_t granules_of(const dadam_handle* h) { return (h->cfg.d + kGranule - 1) / kGranule; }
 
@@ -63,6 +74,73 @@ std::vector<uint32_t> build_cuts(const dadam_handle* h) {
   return index;
 }
 
+// Rows and entries as the products with 4-bit messages take them (see MixRow), in order of the first row of each group.
+void find_mix_rows(uint32_t R, Slot& s) {
+  s.mix_rows.clear();
+  s.mix_firsts.clear();
+  s.mix_entries.clear();
+  std::map<std::vector<std::pair<int32_t, float>>, std::vector<int32_t>> by_list;
+  std::vector<std::vector<std::pair<int32_t, float>>> sorted(R);
+  for (uint32_t i = 0; i < R; ++i) {
+    for (int32_t k = s.row_ptr[i]; k < s.row_ptr[i + 1]; ++k) sorted[i].push_back({s.col[k], s.w[k]});
+    std::sort(sorted[i].begin(), sorted[i].end());
+    by_list[sorted[i]].push_back((int32_t)i);
+  }
+  for (uint32_t i = 0; i < R; ++i) {
+    const std::vector<int32_t>& rows = by_list[sorted[i]];
+    if (rows.front() != (int32_t)i) continue;
+    const int32_t first = (int32_t)s.mix_entries.size();
+    if (rows.size() > 1) {
+      for (const auto& e : sorted[i]) s.mix_entries.push_back({e.first, e.second});
+    } else {
+      for (int32_t k = s.row_ptr[i]; k < s.row_ptr[i + 1]; ++k) s.mix_entries.push_back({s.col[k], s.w[k]});
+    }
+    const int32_t n = (int32_t)s.mix_entries.size() - first;
+    while (s.mix_entries.size() % kMixAtOnce) s.mix_entries.push_back({s.mix_entries.back().col, 0.f});
+    const int32_t all = (int32_t)s.mix_entries.size() - first, step = kMixAtOnce * (rows.size() > 1 ? kMixParts : 1);
+    const int32_t part = rows.size() > 1 ? (all + step - 1) / step * kMixAtOnce : all;
+    const int16_t group = (int16_t)s.mix_firsts.size();
+    for (int32_t row : rows) s.mix_rows.push_back({(int16_t)row, group, first, n, part});
+    s.mix_firsts.push_back({(int16_t)i, group, first, n, part});
+  }
+}
+
+// A slot's rows and entries in an image of device memory.
+struct ListPlaces {
+  size_t rows, firsts, entries;
+};
+ListPlaces add_lists(const Slot& s, std::vector<char>* image) {
+  auto add = [image](const auto& v) {
+    const size_t at = (image->size() + 15) / 16 * 16;
+    image->resize(at + v.size() * sizeof(v[0]));
+    memcpy(image->data() + at, v.data(), v.size() * sizeof(v[0]));
+    return at;
+  };
+  return {add(s.mix_rows), add(s.mix_firsts), add(s.mix_entries)};
+}
+void point_lists(Slot* s, const char* memory, const ListPlaces& at) {
+  s->d_mix_rows = reinterpret_cast<const MixRow*>(memory + at.rows);
+  s->d_mix_firsts = reinterpret_cast<const MixRow*>(memory + at.firsts);
+  s->d_mix_entries = reinterpret_cast<const MixEntry*>(memory + at.entries);
+}
+
+// Lists of a slot that is set on a handle with state, with the handle's device current.
+int add_mix_lists(dadam_handle* h, Slot* s) {
+  return guarded(h, [&] {
+    find_mix_rows(h->cfg.n_rows, *s);
+    std::vector<char> image;
+    const ListPlaces at = add_lists(*s, &image);
+    hipError_t e = hipMalloc((void**)&s->d_mix, image.size());
+    if (e == hipSuccess) e = hipMemcpy(s->d_mix, image.data(), image.size(), hipMemcpyHostToDevice);
+    if (e != hipSuccess) {
+      (void)hipGetLastError();
+      return fail(h, DADAM_EHIP, "uploading the neighbour list failed: %s", hipGetErrorString(e));
+    }
+    point_lists(s, s->d_mix, at);
+    return DADAM_OK;
+  });
+}
+
 void free_state(OperatorState* s) {
   if (!s) return;
   if (s->memory) (void)hipFree(s->memory);
@@ -81,6 +159,12 @@ int make_state(dadam_handle* h) {
   const size_t sums = (size_t)s->per_row * h->cfg.n_rows * sizeof(double), head = sums + DADAM_MAX_ROWS * sizeof(uint32_t);
   std::vector<char> image(head + cuts.size() * sizeof(uint32_t), 0);
   if (!cuts.empty()) memcpy(image.data() + head, cuts.data(), cuts.size() * sizeof(uint32_t));
+  ListPlaces places[DADAM_MAX_SLOTS];
+  for (uint32_t k = 0; k < DADAM_MAX_SLOTS; ++k) {
+    if (!h->slots[k].set) continue;
+    find_mix_rows(h->cfg.n_rows, h->slots[k]);
+    places[k] = add_lists(h->slots[k], &image);
+  }
   hipError_t e = hipMalloc((void**)&s->memory, image.size());
   if (e == hipSuccess) e = hipMemcpy(s->memory, image.data(), image.size(), hipMemcpyHostToDevice);
   if (e != hipSuccess) {
@@ -93,8 +177,11 @@ int make_state(dadam_handle* h) {
     s->cuts.index = reinterpret_cast<uint32_t*>(s->memory + head);
     s->cuts.masks = s->cuts.index + granules_of(h);
   }
+  for (uint32_t k = 0; k < DADAM_MAX_SLOTS; ++k)
+    if (h->slots[k].set) point_lists(&h->slots[k], s->memory, places[k]);
   h->operators = s.release();
   h->free_operators = free_state;
+  h->add_mix_lists = add_mix_lists;
   return DADAM_OK;
 }
 
@@ -374,16 +461,6 @@ int mix_impl(dadam_handle* h, uint32_t slot, const void* const* msg, float* cons
       put(r, 1, sum[pairs[p].second]);
     });
   });
-}
-
-// No exception leaves an entry point.
-template <typename Fn>
-int guarded(dadam_handle* h, Fn fn) {
-  try {
-    return fn();
-  } catch (const std::bad_alloc&) {
-    return fail(h, DADAM_EINVAL, "out of host memory");
-  }
 }
 
 }  // namespace

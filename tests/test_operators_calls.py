@@ -99,3 +99,24 @@ def test_a_first_call_under_capture_is_refused_before_it_allocates(driver, name)
     assert second.code == 0 and second.mallocs and second.launches
     for a in recorded:
         assert a.code == 0 and a.launches and not a.mallocs
+
+
+def listed_bytes(rows, degree):
+    """What the step's kernels read of a slot without loops: row_ptr, col and w; lengths, columns and weights by row, and the rows' order."""
+    entries = rows * degree
+    return sum(-(-4 * n // 256) * 256 for n in (rows + 1, entries, entries, rows, entries, entries, rows))
+
+
+@pytest.mark.parametrize("rows", [3, 32, 160])
+def test_topologies_of_programs_without_messages_hold_the_steps_lists_only(driver, rows):
+    """What the messages' kernels read of a slot is made on a handle's first call of theirs, for every slot that is set, and from then on by
+    dadam_set_topology: no call but the first allocates."""
+    a = ask(driver, f"handle {rows} {rows} 5000 0 0 0", "topology 0 ring", "topology 3 ring", "topology 0 ring", f"call norm 0", "topology 7 ring",
+            "topology 3 ring", *(f"call {n} {s}" for n in NAMES for s in (0, 3, 7)), "capture 1", *(f"call {n} {s}" for n in NAMES for s in (0, 3, 7)))
+    for k in (1, 2, 3):
+        assert a[k].code == 0 and a[k].mallocs == [listed_bytes(rows, 3)]
+    assert a[4].code == 0 and len(a[4].mallocs) == 1
+    for k in (5, 6):
+        assert a[k].code == 0 and a[k].mallocs[0] == listed_bytes(rows, 3) and len(a[k].mallocs) == 2
+    for x in a[7:7 + 3 * len(NAMES)] + a[8 + 3 * len(NAMES):]:
+        assert x.code == 0 and x.launches and not x.mallocs, x.text
