@@ -389,8 +389,8 @@ def dadam_slot_uses_tile_mode(h, slot: int) -> bool:
 
 def pointer_table(buffers, count: int, length: int, elem_bytes: int, what: str, on_device: bool = False):
     """The host array of `count` device pointers that the calls below take, marshalled and size-checked once: from a sequence of tensors (or
-    integers taken as addresses), or from one tensor whose rows are the buffers.  None stays None, a table made before is
-    passed through.  The tensors must stay alive."""
+    integers taken as addresses), or from one tensor whose rows are the buffers.  None stays None, a table made before (an array of
+    8-byte whole numbers or pointers) is passed through.  The tensors must stay alive."""
     if buffers is None:
         return None
     if hasattr(buffers, "data_ptr"):
@@ -410,6 +410,9 @@ def pointer_table(buffers, count: int, length: int, elem_bytes: int, what: str, 
     if len(buffers) < count:
         raise ValueError(f"{what} holds {len(buffers)} buffers, the handle needs {count}")
     if isinstance(buffers, (array, C.Array)):
+        whole = buffers.typecode in "QqLl" if isinstance(buffers, array) else buffers._type_ in (C.c_void_p, C.c_uint64, C.c_int64)
+        if not whole or (buffers.itemsize if isinstance(buffers, array) else C.sizeof(buffers._type_)) != 8:
+            raise ValueError(f"{what} is an array of something else than addresses of 8 bytes")
         return buffers
     ptrs = []
     for k in range(count):

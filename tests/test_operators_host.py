@@ -229,3 +229,17 @@ def test_host_code_under_address_and_ub_sanitizers(tmp_path):
     assert r.returncode == 0, r.stderr[-2000:]
     r = subprocess.run([exe], capture_output=True, text=True, timeout=600)
     assert r.returncode == 0 and "bad 0" in r.stdout and "ERROR" not in r.stderr, (r.stdout[-500:], r.stderr[-3000:])
+
+
+def test_tables_made_before_are_of_addresses():
+    """What is not an array of 8-byte whole numbers or pointers would be read beyond its end, or as other addresses."""
+    from array import array
+    h, at = handle(), Addresses()(3)
+    for good in (array("Q", at), array("q", at), (C.c_void_p * 3)(*at), (C.c_uint64 * 3)(*at)):
+        with pytest.raises(B.DadamError) as e:
+            B.dadam_grad_norm(h, good, 1 << 16)
+        assert e.value.code == B.DADAM_ESTATE
+    for bad in (array("I", at), array("d", at), array("B", [0] * 24), (C.c_uint32 * 3)(*at), (C.c_double * 3)(*at), (C.c_char * 24)()):
+        with pytest.raises(ValueError):
+            B.dadam_grad_norm(h, bad, 1 << 16)
+    B.dadam_destroy(h)
