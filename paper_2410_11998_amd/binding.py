@@ -437,7 +437,11 @@ def _at(table):
 
 
 def _shape(h):
-    return _SHAPE_OF_HANDLE.get(getattr(h, "value", None), (0, 0, 0, 0, 0, False))
+    """What dadam_init was told of a handle, or of the number that it holds: the library reads as many pointers as that says."""
+    info = _SHAPE_OF_HANDLE.get(h if isinstance(h, int) else getattr(h, "value", None))
+    if info is None:
+        raise ValueError("not a handle of dadam_init, or one that dadam_destroy has freed")
+    return info
 
 
 def _message_bytes(d: int) -> int:
@@ -503,7 +507,7 @@ def dadam_mx4_round(h, slot: int, x_src, x_dst, copy, sum, gamma: float, stream:
 
 
 def dadam_destroy(h) -> None:
-    _SHAPE_OF_HANDLE.pop(getattr(h, "value", None), None)
+    _SHAPE_OF_HANDLE.pop(h if isinstance(h, int) else getattr(h, "value", None), None)
     lib.dadam_destroy(h)
 
 

@@ -243,3 +243,23 @@ def test_tables_made_before_are_of_addresses():
         with pytest.raises(ValueError):
             B.dadam_grad_norm(h, bad, 1 << 16)
     B.dadam_destroy(h)
+
+
+def test_a_handle_by_its_number_and_a_handle_that_is_none():
+    """The number that a handle holds names it as well, sizes are checked by it all the same; what dadam_init has not returned, or
+    dadam_destroy has freed, is refused before the library is asked."""
+    import torch
+    h, at = handle(), Addresses()(3)
+    with pytest.raises(B.DadamError) as e:
+        B.dadam_grad_norm(h.value, at, 1 << 16)
+    assert e.value.code == B.DADAM_ESTATE
+    with pytest.raises(ValueError):
+        B.dadam_grad_norm(h.value, [torch.zeros(D - 1)] * 3, 1 << 16)
+    gone = C.c_void_p(h.value)
+    B.dadam_destroy(h.value)
+    for none in (gone, gone.value, None, C.c_void_p(), 12345):
+        for call in (lambda x: B.dadam_grad_norm(x, at, 1 << 16), lambda x: B.dadam_clip_grads(x, at, at, 1.0, 1 << 16),
+                     lambda x: B.dadam_mx4_encode(x, at, None, None, at), lambda x: B.dadam_mx4_product(x, 0, at, at),
+                     lambda x: B.dadam_mx4_gossip(x, 0, at, at, at, at, at, 0.5), lambda x: B.dadam_mx4_round(x, 0, at, at, at, at, 0.5)):
+            with pytest.raises(ValueError):
+                call(none)
