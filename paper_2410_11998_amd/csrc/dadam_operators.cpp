@@ -416,6 +416,10 @@ int mix_impl(dadam_handle* h, uint32_t slot, const void* const* msg, float* cons
   return on_device(h, stream, [&] {
     const Slot& lists = h->slots[slot];
     const bool copies = copies_rows(h, lists, mode);
+    std::vector<std::pair<int32_t, int32_t>> pairs;  // (copy, of), before anything is launched: host memory may run out
+    if (copies)
+      for (const MixRow& r : lists.mix_rows)
+        if (r.row != lists.mix_firsts[r.group].row) pairs.push_back({r.row, lists.mix_firsts[r.group].row});
     // Positions [0, count) of `rows` in as few launches as the argument block allows, of about the same number each.
     MixArgs<kMessageRows, kMaxRows> a;
     memset((void*)&a, 0, sizeof(a));
@@ -451,9 +455,6 @@ int mix_impl(dadam_handle* h, uint32_t slot, const void* const* msg, float* cons
       put(r, 3, x_dst[i]);
     });
     if (e != (int)hipSuccess || !copies) return e;
-    std::vector<std::pair<int32_t, int32_t>> pairs;  // (copy, of)
-    for (const MixRow& r : lists.mix_rows)
-      if (r.row != lists.mix_firsts[r.group].row) pairs.push_back({r.row, lists.mix_firsts[r.group].row});
     a.work = kMixCopy;
     return in_launches((uint32_t)pairs.size(), [&](RowPointers* r, uint32_t p) {
       if (!r) return;

@@ -8,6 +8,8 @@
 //   topology SLOT ring                                    every row, the one before and the one behind
 //   call NAME SLOT                                        norm, clip, encode, product, add, gossip, round
 //   capture 0|1                                           streams are being captured from now on
+//   memory N                                              of the next call's allocations of host memory the N-th fails, 0 none; answers 0
+//   left                                                  N less those made since, 0 or less: the N-th failed
 #include "dadam.h"
 #include <hip/hip_runtime_api.h>
 #include <cstdio>
@@ -15,6 +17,7 @@
 #include <cstring>
 #include <iostream>
 #include <map>
+#include <new>
 #include <sstream>
 #include <string>
 #include <vector>
@@ -22,7 +25,27 @@
 static std::string events;
 static bool capturing = false;
 static std::map<const void*, std::string>& kernels() { static std::map<const void*, std::string> m; return m; }
+struct Outside {  // the modelled runtime's own strings and tables do not count
+  bool was;
+  Outside();
+  ~Outside();
+};
+static void note(const std::string& what);
+
+// Host memory of the library's calls (inside a call only: the program's own goes through).
+static bool in_call = false;
+static long until = 0;
+void* operator new(size_t n) {
+  if (in_call && until-- == 1) throw std::bad_alloc();
+  void* p = malloc(n ? n : 1);
+  if (!p) throw std::bad_alloc();
+  return p;
+}
+Outside::Outside() : was(in_call) { in_call = false; }
+Outside::~Outside() { in_call = was; }
 static void note(const std::string& what) { events += " | " + what; }
+void operator delete(void* p) noexcept { free(p); }
+void operator delete(void* p, size_t) noexcept { free(p); }
 
 extern "C" {
 void** __hipRegisterFatBinary(const void*) { static void* module; return &module; }
@@ -37,12 +60,14 @@ hipError_t hipDeviceGetAttribute(int* v, hipDeviceAttribute_t a, int) {
 }
 // A real runtime refuses both while a stream is being captured, and ends the capture.
 hipError_t hipMalloc(void** p, size_t n) {
+  Outside o;
   note("malloc " + std::to_string(n));
   if (capturing) return hipErrorStreamCaptureUnsupported;
   *p = malloc(n);
   return hipSuccess;
 }
 hipError_t hipMemcpy(void* d, const void* s, size_t n, hipMemcpyKind) {
+  Outside o;
   note("memcpy " + std::to_string(n));
   if (capturing) return hipErrorStreamCaptureImplicit;
   memcpy(d, s, n);
@@ -57,6 +82,7 @@ hipError_t hipStreamIsCapturing(hipStream_t, hipStreamCaptureStatus* s) {
 }
 hipError_t hipGetLastError() { return hipSuccess; }
 hipError_t hipLaunchKernel(const void* fn, dim3 grid, dim3 block, void**, size_t lds, hipStream_t) {
+  Outside o;
   note("launch " + kernels()[fn] + " " + std::to_string(grid.x) + "x" + std::to_string(block.x) + " " + std::to_string(lds));
   return hipSuccess;
 }
@@ -97,14 +123,17 @@ static int call(dadam_handle* h, std::istringstream& in) {
   auto out = [&](int t) { return (void* const*)table[t].data(); };
   auto f = [&](int t) { return (float* const*)table[t].data(); };
   float* norms = (float*)(1ull << 30);
-  if (name == "norm") return dadam_grad_norm(h, in_(0), norms, nullptr);
-  if (name == "clip") return dadam_clip_grads(h, in_(0), out(1), 1.f, norms, nullptr);
-  if (name == "encode") return dadam_mx4_encode(h, in_(0), f(1), f(2), out(3), nullptr);
-  if (name == "product") return dadam_mx4_product(h, slot, in_(5), f(0), 0, nullptr);
-  if (name == "add") return dadam_mx4_product(h, slot, in_(5), f(0), DADAM_MX4_ADD, nullptr);
-  if (name == "gossip") return dadam_mx4_gossip(h, slot, in_(5), f(0), f(1), in_(2), out(3), 0.5f, nullptr);
-  if (name == "round") return dadam_mx4_round(h, slot, in_(0), out(1), f(2), f(3), 0.5f, nullptr);
-  return -100;
+  int rc = -100;
+  in_call = true;
+  if (name == "norm") rc = dadam_grad_norm(h, in_(0), norms, nullptr);
+  if (name == "clip") rc = dadam_clip_grads(h, in_(0), out(1), 1.f, norms, nullptr);
+  if (name == "encode") rc = dadam_mx4_encode(h, in_(0), f(1), f(2), out(3), nullptr);
+  if (name == "product") rc = dadam_mx4_product(h, slot, in_(5), f(0), 0, nullptr);
+  if (name == "add") rc = dadam_mx4_product(h, slot, in_(5), f(0), DADAM_MX4_ADD, nullptr);
+  if (name == "gossip") rc = dadam_mx4_gossip(h, slot, in_(5), f(0), f(1), in_(2), out(3), 0.5f, nullptr);
+  if (name == "round") rc = dadam_mx4_round(h, slot, in_(0), out(1), f(2), f(3), 0.5f, nullptr);
+  in_call = false;
+  return rc;
 }
 
 int main() {
@@ -132,8 +161,13 @@ int main() {
     } else if (what == "capture") {
       in >> capturing;
       rc = 0;
+    } else if (what == "memory") {
+      in >> until;
+      rc = 0;
+    } else if (what == "left") {
+      rc = (int)until;
     }
-    std::cout << line << ": " << rc << (rc < 0 ? std::string(" ") + dadam_last_error(h) : "") << events << "\n";
+    std::cout << line << ": " << rc << (rc < 0 && what != "left" ? std::string(" ") + dadam_last_error(h) : "") << events << "\n";
   }
   if (h) dadam_destroy(h);
   return 0;

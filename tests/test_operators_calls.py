@@ -120,3 +120,20 @@ def test_topologies_of_programs_without_messages_hold_the_steps_lists_only(drive
         assert a[k].code == 0 and a[k].mallocs[0] == listed_bytes(rows, 3) and len(a[k].mallocs) == 2
     for x in a[7:7 + 3 * len(NAMES)] + a[8 + 3 * len(NAMES):]:
         assert x.code == 0 and x.launches and not x.mallocs, x.text
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_calls_without_host_memory_launch_nothing_and_can_be_made_again(driver, name):
+    """Every allocation of host memory of a handle's first and second call fails once.  The large product copies rows that share their list."""
+    begin = ["handle 8 8 13000000 0 0 0", "topology 0 lists 2"]
+    for first in (True, False):
+        k = failed = 0
+        while True:
+            k += 1
+            *_, got, left, _, again = ask(driver, *begin, *([] if first else ["call encode 0"]), f"memory {k}", f"call {name} 0", "left", "memory 0", f"call {name} 0")
+            assert again.code == 0 and again.launches
+            if left.code > 0:
+                break
+            failed += 1
+            assert got.code == B.DADAM_EINVAL and "host memory" in got.text and not got.launches, (k, got.text)
+        assert got.code == 0 and (failed or not first)
