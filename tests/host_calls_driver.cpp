@@ -1,6 +1,7 @@
 // What the calls around the step ask of the HIP runtime, without a GPU: the built library on a modelled runtime (this program defines
 // the calls, so the library's references resolve here) that says what it was asked for.  Reads commands, a line each, and prints one
-// line for each: the command, the call's answer, and the allocations, copies and launches (kernel, grid x block, bytes of LDS) that it made.
+// line for each: the command, the call's answer, and the allocations, copies and launches (kernel, grid x block, bytes of LDS) that it made; behind
+// launches of products and gossip the rows whose sums they form, or "copy<of" where they copy rows.
 // tests/test_operators_calls.py builds and runs it.
 //
 //   handle ROWS COLS D PARAM_TYPE GRAD_TYPE LDS_LIMIT     one tensor of D elements
@@ -11,6 +12,7 @@
 //   memory N                                              of the next call's allocations of host memory the N-th fails, 0 none; answers 0
 //   left                                                  N less those made since, 0 or less: the N-th failed
 #include "dadam.h"
+#include "dadam_operators.h"
 #include <hip/hip_runtime_api.h>
 #include <cstdio>
 #include <cstdlib>
@@ -22,6 +24,8 @@
 #include <string>
 #include <vector>
 
+static uint32_t R, C;
+static uint64_t d;
 static std::string events;
 static bool capturing = false;
 static std::map<const void*, std::string>& kernels() { static std::map<const void*, std::string> m; return m; }
@@ -40,6 +44,24 @@ void* operator new(size_t n) {
   void* p = malloc(n ? n : 1);
   if (!p) throw std::bad_alloc();
   return p;
+}
+// Buffer i of table t lies at base + (t * DADAM_MAX_ROWS + i) * step.
+static uint64_t step = 1;
+constexpr uint64_t kBase = 1ull << 32;
+static uint64_t row_of(const dadam::RowPointers& r, int k) {
+  const uint64_t at = (((uint64_t)((r.high[k / 2] >> (16 * (k % 2))) & 0xFFFF) << 32) | r.low[k]) << 4;
+  return (at - kBase) / step;  // outputs are table 0
+}
+template <typename A>
+static void note_rows(const std::string& name, const A& a) {
+  std::string text = "rows";
+  for (uint32_t p = 0; p < a.s.n_rows; ++p) {
+    const uint64_t row = row_of(a.row[p], 0);
+    text += " " + std::to_string(row);
+    if (name.find("k_mx4_copy") != std::string::npos) text += "<" + std::to_string(row_of(a.row[p], 1));
+    else if ((uint64_t)a.lists.rows[p].row != row) text += "!";  // the list of another row
+  }
+  note(text);
 }
 Outside::Outside() : was(in_call) { in_call = false; }
 Outside::~Outside() { in_call = was; }
@@ -81,15 +103,17 @@ hipError_t hipStreamIsCapturing(hipStream_t, hipStreamCaptureStatus* s) {
   return hipSuccess;
 }
 hipError_t hipGetLastError() { return hipSuccess; }
-hipError_t hipLaunchKernel(const void* fn, dim3 grid, dim3 block, void**, size_t lds, hipStream_t) {
+hipError_t hipLaunchKernel(const void* fn, dim3 grid, dim3 block, void** args, size_t lds, hipStream_t) {
   Outside o;
   note("launch " + kernels()[fn] + " " + std::to_string(grid.x) + "x" + std::to_string(block.x) + " " + std::to_string(lds));
+  const std::string& name = kernels()[fn];
+  using namespace dadam;
+  if (name.find("MixArgs") == std::string::npos) return hipSuccess;
+  if (name.find("Li16ELi16EEE") != std::string::npos) note_rows(name, *(const MixArgs<kFewOperands, kFewOperands>*)args[0]);
+  else note_rows(name, *(const MixArgs<kMessageRows, kMaxRows>*)args[0]);
   return hipSuccess;
 }
 }
-
-static uint32_t R, C;
-static uint64_t d;
 
 static int topology(dadam_handle* h, std::istringstream& in) {
   uint32_t slot, n = 0;
@@ -115,10 +139,10 @@ static int call(dadam_handle* h, std::istringstream& in) {
   uint32_t slot = 0;
   in >> name >> slot;
   // addresses only: nothing is read or written
-  const uint64_t step = (4 * d + 255) / 128 * 128, base = 1ull << 32;
+  step = (4 * d + 255) / 128 * 128;
   std::vector<void*> table[6];
   for (uint64_t t = 0; t < 6; ++t)
-    for (uint64_t i = 0; i < (R > C ? R : C); ++i) table[t].push_back((void*)(base + (t * DADAM_MAX_ROWS + i) * step));
+    for (uint64_t i = 0; i < (R > C ? R : C); ++i) table[t].push_back((void*)(kBase + (t * DADAM_MAX_ROWS + i) * step));
   auto in_ = [&](int t) { return (const void* const*)table[t].data(); };
   auto out = [&](int t) { return (void* const*)table[t].data(); };
   auto f = [&](int t) { return (float* const*)table[t].data(); };

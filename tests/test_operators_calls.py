@@ -18,8 +18,8 @@ def driver(tmp_path_factory):
     if not os.path.exists(clang):
         pytest.skip("clang++ of the ROCm toolchain not available")
     exe, libdir = str(tmp_path_factory.mktemp("calls") / "calls_driver"), os.path.dirname(B.LIB_PATH)
-    cmd = [clang, "-std=c++17", "-O1", "-rdynamic", "-D__HIP_PLATFORM_AMD__", "-I", os.path.join(ROOT, "include"), "-I", "/opt/rocm/include",
-           os.path.join(ROOT, "tests", "host_calls_driver.cpp"), "-o", exe, "-L", libdir, "-ldadam", f"-Wl,-rpath,{libdir}",
+    cmd = [clang, "-std=c++17", "-O1", "-rdynamic", "-D__HIP_PLATFORM_AMD__", "-I", os.path.join(ROOT, "include"), "-I",
+           os.path.join(ROOT, "paper_2410_11998_amd", "csrc"), "-I", "/opt/rocm/include", os.path.join(ROOT, "tests", "host_calls_driver.cpp"), "-o", exe, "-L", libdir, "-ldadam", f"-Wl,-rpath,{libdir}",
            f"-Wl,-rpath,{rocm}", f"-Wl,-rpath-link,{rocm}"]
     r = subprocess.run(cmd, capture_output=True, text=True, timeout=600)
     assert r.returncode == 0, r.stderr[-2000:]
@@ -27,13 +27,16 @@ def driver(tmp_path_factory):
 
 
 class Answer:
-    """One call: its status, the error's text, bytes allocated, and the launches as (kernel, its template arguments, grid, block, LDS)."""
+    """One call: its status, the error's text, bytes allocated, the launches as (kernel, its template arguments, grid, block, LDS), and of products
+    and gossip the rows that each launch forms, or (copy, of) pairs."""
 
     def __init__(self, line):
         head, *events = line.split(": ", 1)[1].split(" | ")
         self.code, _, self.text = head.partition(" ")
         self.code = int(self.code)
         self.mallocs = [int(e.split()[1]) for e in events if e.startswith("malloc")]
+        self.rows = [e.split()[1:] for e in events if e.startswith("rows")]
+        self.rows = [[tuple(int(v) for v in r.split("<")) if "<" in r else int(r) for r in launch] for launch in self.rows]   # (int refuses a "!")
         self.launches = []
         for e in events:
             m = re.match(r"launch (?:void )?(?:dadam::\(anonymous namespace\)::)?(\w+)<(.*)>\(.*\) (\d+)x(\d+) (\d+)$", e)
@@ -137,3 +140,42 @@ def test_calls_without_host_memory_launch_nothing_and_can_be_made_again(driver, 
             failed += 1
             assert got.code == B.DADAM_EINVAL and "host memory" in got.text and not got.launches, (k, got.text)
         assert got.code == 0 and (failed or not first)
+
+
+@pytest.mark.parametrize("rows,d,per_row", [(1, 8_500_001, 256), (3, 2_100_003, 65), (7, 1_000_000, 31), (5, 100_003, 4), (160, 70_001, 1), (1, 32_768, 1),
+                                            (1, 32_769, 2)])
+def test_workgroups_that_share_a_norm(driver, rows, d, per_row):
+    *_, a = ask(driver, f"handle {rows} {rows} {d} 0 0 0", "call norm 0")
+    assert a.code == 0 and [(x[0], x[2], x[3]) for x in a.launches] == [("k_grad_norm", rows * per_row, 1024)]
+
+
+# d and rows to either side of the rules' limits
+@pytest.mark.parametrize("rows,lists,d", [(8, 1, 1_000_003), (8, 2, 13_000_007), (16, 2, 1_000_000), (24, 2, 800_017), (32, 8, 786_432), (32, 8, 786_433 - 1024),
+                                          (100, 1, 4096), (160, 2, 4096), (160, 1, 786_432), (160, 40, 700_000), (20, 5, 5_200_000), (97, 1, 1_100_000),
+                                          (160, 160, 4096), (97, 97, 4096), (96, 96, 100), (12, 12, 9_000_000)])
+def test_every_row_is_formed_once(driver, rows, lists, d):
+    """Over the launches of a product or of gossip every row comes up once: formed, with the list of that row, or copied from a row of the same
+    list that was formed before."""
+    *_, store, add, gossip, round_ = ask(driver, f"handle {rows} {rows} {d} 0 0 0", f"topology 0 lists {lists}",
+                                         *(f"call {n} 0" for n in ("product", "add", "gossip", "round")))
+    streams, shared, large = rows * d * 24 > 512 << 20, rows >= 4 * lists, d > 1535 * 512
+    each = rows // lists
+    for name, a in (("product", store), ("add", add), ("gossip", gossip)):
+        assert a.code == 0 and len(a.rows) == len(a.launches)
+        formed = [r for launch in a.rows for r in launch if isinstance(r, int)]
+        copied = [r for launch in a.rows for r in launch if not isinstance(r, int)]
+        assert sorted(formed + [r[0] for r in copied]) == list(range(rows))
+        assert all(of in formed and of // each == row // each for row, of in copied)
+        kernels = [x[0] for x in a.launches]
+        copies = name == "product" and shared and large and rows * d >= 10 ** 8
+        if copies:
+            assert kernels == ["k_mx4_mix"] * -(-lists // 96) + ["k_mx4_copy"] * -(-len(copied) // 96) and len(formed) == lists
+        else:
+            want = "k_mx4_mix" if not shared else "k_mx4_products" if name != "gossip" and large else "k_mx4_shared"
+            assert set(kernels) == {want} and not copied
+        long_block = rows > 16
+        for x, launch in zip(a.launches, a.rows):
+            assert len(launch) <= (96 if long_block else 16)
+            hints = int([v for v in x[1] if v not in ("TF32", "TBF16")][0 if x[0] == "k_mx4_copy" else 1])
+            assert hints == (1 if streams else 0)
+    assert [x[0] for x in round_.launches] == ["k_mx4_round"]
