@@ -522,14 +522,18 @@ KernelFn mix_kernel(int xdt, MixMode mode, uint32_t work) {
     if (xdt == DADAM_BF16) return by_group ? (KernelFn)k_mx4_shared<TBF16, kMixGossip, S, N, C> : (KernelFn)k_mx4_mix<TBF16, kMixGossip, S, N, C>;
     return by_group ? (KernelFn)k_mx4_shared<TF32, kMixGossip, S, N, C> : (KernelFn)k_mx4_mix<TF32, kMixGossip, S, N, C>;
   }
-  if (mode == kMixAdd && by_group) return (KernelFn)k_mx4_shared<TF32, kMixAdd, S, N, C>;
+  // Few rows that stream are long: their products go by wavefronts.
+  if constexpr (S == kStreamsNot || N > kFewOperands)
+    if (mode == kMixAdd && by_group) return (KernelFn)k_mx4_shared<TF32, kMixAdd, S, N, C>;
   if (mode == kMixAdd && work == kMixAllRows) return (KernelFn)k_mx4_products<kMixAdd, S, N, C>;
   if constexpr (S != kStreamsApart) {  // (rows that do not share their sum, and products that store, keep the hint)
-    if (mode == kMixAdd) return (KernelFn)k_mx4_mix<TF32, kMixAdd, S, N, C>;
-    if (by_group) return (KernelFn)k_mx4_shared<TF32, kMixStore, S, N, C>;
-    if (work == kMixAllRows) return (KernelFn)k_mx4_products<kMixStore, S, N, C>;
-    if (work == kMixByRow) return (KernelFn)k_mx4_mix<TF32, kMixStore, S, N, C>;
-    if constexpr (S == kStreamsHinted) return (KernelFn)k_mx4_copy<S, N, C>;
+    if (mode == kMixAdd && work == kMixByRow) return (KernelFn)k_mx4_mix<TF32, kMixAdd, S, N, C>;
+    if constexpr (S == kStreamsNot || N > kFewOperands)
+      if (mode == kMixStore && by_group) return (KernelFn)k_mx4_shared<TF32, kMixStore, S, N, C>;
+    if (mode == kMixStore && work == kMixAllRows) return (KernelFn)k_mx4_products<kMixStore, S, N, C>;
+    if (mode == kMixStore && work == kMixByRow) return (KernelFn)k_mx4_mix<TF32, kMixStore, S, N, C>;
+    if constexpr (S == kStreamsHinted)
+      if (work == kMixCopy) return (KernelFn)k_mx4_copy<S, N, C>;
   }
   return nullptr;
 }

@@ -9,6 +9,8 @@
 //   topology SLOT ring                                    every row, the one before and the one behind
 //   call NAME SLOT                                        norm, clip, encode, product, add, gossip, round
 //   capture 0|1                                           streams are being captured from now on
+//   shift BYTES                                           by which every other buffer misses the beginning of a line from now on
+//   kernels                                               the kernels of these calls that the library has
 //   memory N                                              of the next call's allocations of host memory the N-th fails, 0 none; answers 0
 //   left                                                  N less those made since, 0 or less: the N-th failed
 #include "dadam.h"
@@ -45,8 +47,8 @@ void* operator new(size_t n) {
   if (!p) throw std::bad_alloc();
   return p;
 }
-// Buffer i of table t lies at base + (t * DADAM_MAX_ROWS + i) * step.
-static uint64_t step = 1;
+// Buffer i of table t lies at base + (t * DADAM_MAX_ROWS + i) * step, every other one `shift` bytes further.
+static uint64_t step = 1, shift = 0;
 constexpr uint64_t kBase = 1ull << 32;
 static uint64_t row_of(const dadam::RowPointers& r, int k) {
   const uint64_t at = (((uint64_t)((r.high[k / 2] >> (16 * (k % 2))) & 0xFFFF) << 32) | r.low[k]) << 4;
@@ -142,7 +144,7 @@ static int call(dadam_handle* h, std::istringstream& in) {
   step = (4 * d + 255) / 128 * 128;
   std::vector<void*> table[6];
   for (uint64_t t = 0; t < 6; ++t)
-    for (uint64_t i = 0; i < (R > C ? R : C); ++i) table[t].push_back((void*)(kBase + (t * DADAM_MAX_ROWS + i) * step));
+    for (uint64_t i = 0; i < (R > C ? R : C); ++i) table[t].push_back((void*)(kBase + (t * DADAM_MAX_ROWS + i) * step + (t + i) % 2 * shift));
   auto in_ = [&](int t) { return (const void* const*)table[t].data(); };
   auto out = [&](int t) { return (void* const*)table[t].data(); };
   auto f = [&](int t) { return (float* const*)table[t].data(); };
@@ -184,6 +186,14 @@ int main() {
       rc = call(h, in);
     } else if (what == "capture") {
       in >> capturing;
+      rc = 0;
+    } else if (what == "shift") {
+      in >> shift;
+      rc = 0;
+    } else if (what == "kernels") {
+      for (const auto& k : kernels())
+        if (k.second.find("k_mx4_") != std::string::npos || k.second.find("k_clip") != std::string::npos || k.second.find("k_grad_norm") != std::string::npos)
+          note("kernel " + k.second);
       rc = 0;
     } else if (what == "memory") {
       in >> until;

@@ -26,6 +26,10 @@ def driver(tmp_path_factory):
     return exe
 
 
+def plain_kernel(text):
+    return re.sub(r"^void |dadam::|\(anonymous namespace\)::", "", text).split("(")[0]
+
+
 class Answer:
     """One call: its status, the error's text, bytes allocated, the launches as (kernel, its template arguments, grid, block, LDS), and of products
     and gossip the rows that each launch forms, or (copy, of) pairs."""
@@ -37,6 +41,7 @@ class Answer:
         self.mallocs = [int(e.split()[1]) for e in events if e.startswith("malloc")]
         self.rows = [e.split()[1:] for e in events if e.startswith("rows")]
         self.rows = [[tuple(int(v) for v in r.split("<")) if "<" in r else int(r) for r in launch] for launch in self.rows]   # (int refuses a "!")
+        self.kernels = {plain_kernel(e[len("kernel "):]) for e in events if e.startswith("kernel")}
         self.launches = []
         for e in events:
             m = re.match(r"launch (?:void )?(?:dadam::\(anonymous namespace\)::)?(\w+)<(.*)>\(.*\) (\d+)x(\d+) (\d+)$", e)
@@ -179,3 +184,22 @@ def test_every_row_is_formed_once(driver, rows, lists, d):
             hints = int([v for v in x[1] if v not in ("TF32", "TBF16")][0 if x[0] == "k_mx4_copy" else 1])
             assert hints == (1 if streams else 0)
     assert [x[0] for x in round_.launches] == ["k_mx4_round"]
+
+
+def test_every_kernel_of_these_calls_is_reached_and_every_call_has_one(driver):
+    """Handles of both types, from one row to 160, that stream or not, on and off a line, with lists of their own and shared ones."""
+    script, names = ["kernels"], ["norm", "clip", "encode", "product", "add", "gossip", "round"]
+    for rows in (1, 2, 8, 16, 17, 24, 40, 64, 70, 100, 128, 160):
+        for d in (4096, 50_000, 1_000_000, 25_000_000 // rows + 5, 110_000_000 // rows + 5):
+            for kind in (0, 1):
+                script += [f"handle {rows} {rows} {d} {kind} {kind} 0"]
+                for topology in ("lists 1", "ring"):
+                    script += [f"topology 0 {topology}" if topology != "ring" or rows > 2 else f"topology 0 lists {rows}"]
+                    for shift in (0, 16):
+                        script += [f"shift {shift}"] + [f"call {n} 0" for n in names]
+    answers = ask(driver, *script)
+    reached = set()
+    for command, a in zip(script, answers):
+        assert a.code == 0 and (a.launches or not command.startswith("call")), (command, a.text)
+        reached |= {f"{x[0]}<{', '.join(x[1])}>" for x in a.launches}
+    assert reached == answers[0].kernels, (sorted(answers[0].kernels - reached), sorted(reached - answers[0].kernels))
