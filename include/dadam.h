@@ -479,12 +479,19 @@ int dadam_mx4_product(dadam_handle* h, uint32_t slot, const void* const* msg, fl
  *     sum[i] += sum_k w[k] * value(msg[col[k]]);      x_dst[i] = x_src[i] + gamma * (sum[i] - copy[i])
  * with copy[i] the worker's own public copy, already moved by its own message (dadam_mx4_encode), and that message among msg.
  * With a doubly stochastic W the replicas' mean does not move; 0 < gamma <= 1 (smaller for sparser graphs and coarser messages).  x_dst[i] may be x_src[i] (in place).
- * float32, one rounding of x_dst to param_dtype. */
+ * float32, one rounding of x_dst to param_dtype.
+ * A sum belongs to one matrix, which no call can check.  It has to be sum_k w[k] copy[col[k]] before the first round (copies and sums all 0, or all the
+ * x^(0) that the replicas have in common; replicas that start apart start from 0, or from copies that the sums are made of), and it stays that only if it takes
+ * every round's messages with that matrix.  A program whose slots change from round to round therefore keeps a sum for every slot, and adds each
+ * round's messages to all of them: dadam_mx4_gossip with the round's slot on that slot's sum, dadam_mx4_product with DADAM_MX4_ADD and the other slots on
+ * theirs (a worker has to receive the messages of its neighbours in every slot, every round). */
 int dadam_mx4_gossip(dadam_handle* h, uint32_t slot, const void* const* msg, float* const* sum, const float* const* copy,
                      const void* const* x_src, void* const* x_dst, float gamma, void* hip_stream);
 
 /* One whole round where the handle holds every replica (n_rows == n_cols): dadam_mx4_encode of x_src against copy (in place) and
  * dadam_mx4_gossip of the messages, in one pass and with the same bits, the messages never leaving the chip.  x_dst[i] may be x_src[i].
+ * The sums are those of dadam_mx4_gossip, of this slot's matrix from the first round on; the messages are not kept, so a program whose slots
+ * change makes the two calls.
  * The messages of a piece of every row lie in LDS: 272 bytes a row up to 64 rows, 136 beyond (21760 at most).  DADAM_EINVAL if that is above
  * the handle's lds_limit_bytes: dadam_mx4_encode and dadam_mx4_gossip do the same there. */
 int dadam_mx4_round(dadam_handle* h, uint32_t slot, const void* const* x_src, void* const* x_dst, float* const* copy,

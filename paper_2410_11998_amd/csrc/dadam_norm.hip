@@ -95,7 +95,7 @@ __device__ __forceinline__ void add_granules(const Span& s, const void* g, uint6
     for (uint32_t v = 0; v < V; ++v) add_squares<GT, WHOLE>(raw[k][v], stored[k][v], sums);
 }
 
-// per_row workgroups share a row, each wavefront takes every (per_row * 4)-th granule, kAtOnce of them at a time.  The workgroup
+// per_row workgroups share a row, each wavefront takes every (per_row * kNormWaves)-th granule, kAtOnce of them at a time.  The workgroup
 // of a row that is done last adds up the row's partial sums in their fixed order: no second launch, and no sum that depends on
 // who came first.
 template <typename GT, bool NT, int N>
@@ -126,8 +126,10 @@ __global__ __launch_bounds__(kNormThreads) void k_grad_norm(const NormArgs<N> a)
     double* row_partials = a.partials + (uint64_t)row * a.per_row;
     if (threadIdx.x == 0) {
       __hip_atomic_store(row_partials + part, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      // Both go to where all dies see them: the sum has to be there before the count.  (A release of the agent's scope would
-      // write the die's whole L2 back for that: norms and clipping of 4 x 1048576 elements 58 us, 13 us without.)
+      // The sum has to be there before the count.  On gfx950, and only by what its instructions do, not by the language's memory model (nothing there orders relaxed
+      // operations on two places): stores and additions of the agent's scope go past the die's L2 to where all dies see them, vmcnt counts a
+      // store until it is there, and the loads of row_sum, behind a barrier, go past the L2 too.  (A release of the agent's scope, which is
+      // the portable form, writes the die's whole L2 back: norms and clipping of 4 x 1048576 elements 58 us, 13 us without.)
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       last = __hip_atomic_fetch_add(a.arrived + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == a.per_row;
     }

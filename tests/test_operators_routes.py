@@ -343,3 +343,42 @@ def test_streaming_rounds_of_many_rows(rows, graph, kind, shift):
         assert torch.equal(a.nan_to_num(nan=7.0), b.nan_to_num(nan=7.0))
         assert torch.isnan(a[:, pad]).all() and not torch.isnan(a[:, ~pad]).any()
     B.dadam_destroy(h)
+
+
+# ---------------------------------------------------------------------------------------------
+# matrices that change
+# ---------------------------------------------------------------------------------------------
+
+def test_a_sum_for_every_matrix_where_matrices_change():
+    """One-peer exponential graph on 8 replicas, a slot a phase, 150 rounds: gossip with the round's slot on that slot's sum, its messages added
+    to the other sums too.  Every sum stays W copy, replicas agree and their mean stays, also where they start apart from copies at 0.
+    Two of the slots are set after the handle's first call.
+    Bounds: a round's rounding of a sum is 4 eps of what it is made of (two products), of a copy 1 eps, twice in W copy; magnitudes below 8."""
+    n, phases, rounds = 8, 3, 150
+    with Case("many", n, csr=WL.one_peer_exponential(n, 0), seed=2) as c:
+        stored = torch.from_numpy(c.stored).to(DEV)
+        x = [t.nan_to_num(nan=0.0) for t in c.values(1.0)]
+        start = torch.stack(x).double()
+        copy = [torch.zeros(c.d, device=DEV) for _ in range(n)]
+        sums = [[torch.zeros(c.d, device=DEV) for _ in range(n)] for _ in range(phases)]
+        msg, norms = c.messages(n), torch.zeros(n, device=DEV)
+        B.dadam_grad_norm(c.h, x, norms, stream())
+        for p in range(1, phases):
+            B.dadam_set_topology(c.h, p, *WL.one_peer_exponential(n, p))
+        for k in range(rounds):
+            B.dadam_mx4_encode(c.h, x, copy, copy, msg, stream())
+            for p in range(phases):
+                if p != k % phases:
+                    B.dadam_mx4_product(c.h, p, msg, sums[p], B.DADAM_MX4_ADD, stream())
+            B.dadam_mx4_gossip(c.h, k % phases, msg, sums[k % phases], copy, x, x, 0.5, stream())
+        torch.cuda.synchronize()
+        h = torch.stack(copy).double()
+        assert float(h.abs().max()) < 8
+        for p in range(phases):
+            ptr, col, w = WL.one_peer_exponential(n, p)
+            for i in range(n):
+                want = sum(float(w[e]) * h[int(col[e])] for e in range(ptr[i], ptr[i + 1]))
+                assert float((sums[p][i].double() - want).abs()[stored].max()) <= rounds * 6 * EPS * 8, (p, i)
+        spread = lambda t: float((t - t.mean(0))[:, stored].norm())  # noqa: E731
+        assert spread(torch.stack(x).double()) < 1e-2 * spread(start)
+        assert float((torch.stack(x).double().mean(0) - start.mean(0)).abs()[stored].max()) < 1e-4
