@@ -54,7 +54,11 @@ std::vector<uint32_t> build_cuts(const dadam_handle* h) {
   auto part = [&](uint64_t lo, uint64_t hi) {  // of one granule
     if (lo >= hi) return;
     uint32_t* m = cut(lo / kGranule);
-    for (uint64_t e = lo; e < hi; ++e) m[e % kGranule / kMxBlock] |= 1u << e % kMxBlock;
+    const uint32_t first = (uint32_t)(lo % kGranule), last = first + (uint32_t)(hi - lo) - 1;
+    for (uint32_t w = first / kMxBlock; w <= last / kMxBlock; ++w) {
+      const uint32_t from = w == first / kMxBlock ? first % kMxBlock : 0, to = w == last / kMxBlock ? last % kMxBlock : kMxBlock - 1;
+      m[w] |= (~0u << from) & (~0u >> (kMxBlock - 1 - to));
+    }
   };
   uint64_t done = 0;  // granules before this one are whole or have their entry
   for (const Segment& s : h->segs) {

@@ -5,6 +5,8 @@
 // tests/test_operators_calls.py builds and runs it.
 //
 //   handle ROWS COLS D PARAM_TYPE GRAD_TYPE LDS_LIMIT     one tensor of D elements
+//   tensors COUNT LEN                                     a row of COUNT tensors of LEN elements, up to two apart: dadam_init and a first norm; behind
+//                                                         the answer the microseconds that the host spent in each, the shortest of five
 //   topology SLOT lists N                                 N complete graphs side by side (rows = cols); N = rows: the identity
 //   topology SLOT ring                                    every row, the one before and the one behind
 //   call NAME SLOT                                        norm, clip, encode, product, add, gossip, round
@@ -16,6 +18,8 @@
 #include "dadam.h"
 #include "dadam_operators.h"
 #include <hip/hip_runtime_api.h>
+#include <algorithm>
+#include <chrono>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -162,6 +166,33 @@ static int call(dadam_handle* h, std::istringstream& in) {
   return rc;
 }
 
+static int tensors(std::istringstream& in) {
+  uint64_t count, len, end = 0;
+  in >> count >> len;
+  std::vector<dadam_tensor_desc> ts;
+  for (uint64_t k = 0; k < count; ++k, end += len + end % 3) ts.push_back({end, len, 0.f, 0});
+  dadam_config cfg{};
+  cfg.abi_version = DADAM_ABI_VERSION; cfg.n_rows = cfg.n_cols = 1; cfg.d = end; cfg.n_tensors = (uint32_t)count; cfg.tensors = ts.data();
+  cfg.lr = 1e-3f; cfg.accum_s = 1; cfg.beta_vhat = -1.f; cfg.eps = 1e-8f;
+  long best[2] = {1L << 40, 1L << 40};
+  auto now = [] { return std::chrono::steady_clock::now(); };
+  for (int k = 0; k < 5; ++k) {
+    dadam_handle* one = nullptr;
+    const void* grads = (const void*)kBase;
+    const auto t0 = now();
+    int rc = dadam_init(&cfg, &one);
+    const auto t1 = now();
+    if (rc == DADAM_OK) rc = dadam_grad_norm(one, &grads, (float*)(1ull << 30), nullptr);
+    const auto t2 = now();
+    dadam_destroy(one);
+    if (rc != DADAM_OK) return rc;
+    best[0] = std::min(best[0], (long)std::chrono::duration_cast<std::chrono::microseconds>(t1 - t0).count());
+    best[1] = std::min(best[1], (long)std::chrono::duration_cast<std::chrono::microseconds>(t2 - t1).count());
+  }
+  note("us " + std::to_string(best[0]) + " " + std::to_string(best[1]));
+  return 0;
+}
+
 int main() {
   dadam_handle* h = nullptr;
   std::string line;
@@ -180,6 +211,8 @@ int main() {
       cfg.abi_version = DADAM_ABI_VERSION; cfg.n_rows = R; cfg.n_cols = C; cfg.d = d; cfg.n_tensors = 1; cfg.tensors = &t;
       cfg.lr = 1e-3f; cfg.accum_s = 1; cfg.beta_vhat = -1.f; cfg.eps = 1e-8f;
       rc = dadam_init(&cfg, &h);
+    } else if (what == "tensors") {
+      rc = tensors(in);
     } else if (what == "topology") {
       rc = topology(h, in);
     } else if (what == "call") {
