@@ -103,7 +103,7 @@ __device__ __forceinline__ void encode_unit(const Cuts& cuts, const Units<2, 1>&
 }
 
 // A wavefront takes a unit of one row, all of its loads in flight before the first use.  355 million bfloat16 elements without a copy before 373 us
-// (6.2 TB/s; vector instructions fill 44 % of the issue slots), 8 float32 rows of 3e7 329 us (6.2).
+// (6.2 TB/s, 366 to 377 over machines; vector instructions fill 46 % of the issue slots), 8 float32 rows of 3e7 329 us (6.2).
 template <typename XT, int S, int N>
 __global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_encode(const EncodeArgs<N> a) {
   constexpr bool NT = S == kStreamsHinted;
@@ -357,7 +357,7 @@ __global__ __launch_bounds__(kWave * kMixWaves) void k_mx4_shared(const MixArgs<
 
 // Both sides of a round are elementwise in the vector and couple rows only through messages: with all rows of a unit in one workgroup the messages
 // need not leave the chip, and x and the copy are read once (24 bytes an element in float32 instead of 33 in two calls).  16 rows of 124 million on the
-// exponential graph 7.7 to 7.9 ms (6.0 to 6.2 TB/s), 8 bfloat16 rows of 3e7 786 to 803 us (6.2 to 6.4).
+// exponential graph 7.7 to 8.1 ms (5.9 to 6.2 TB/s), 8 bfloat16 rows of 3e7 786 to 803 us (6.2 to 6.4).
 // One workgroup takes a unit of all rows: its wavefronts deal the rows among themselves, park their messages in LDS,
 // and after one barrier take the neighbours' from there.  What a row holds in registers until then is its x and its copy.
 static_assert(kRoundMessage<1> == kUnitElems<1> / 2 + kUnitElems<1> / kMxBlock && kRoundMessage<2> == 2 * kRoundMessage<1>, "codes and scales");

@@ -2,7 +2,7 @@
 //
 //   n_i = sqrt(sum_e g_i[e]^2),   out_i = g_i  or  g_i (max_norm / n_i)
 //
-// One pass over g for the norm, bound by reading it (8 rows of 355 million bfloat16 elements 831 to 839 us, 6.8 TB/s; 1e8 float32 elements 65 to 66 us,
+// One pass over g for the norm, bound by reading it (8 rows of 355 million bfloat16 elements 831 to 886 us, 6.4 to 6.8 TB/s; 1e8 float32 elements 65 to 66 us,
 // 6.1), one more to scale it (355 million float32 elements with both passes 654 to 665 us, 6.4 to 6.5 TB/s of the three streams).  A float32 square is exact
 // in 64 bits (24 + 24 of 53), so sums in double lose next to nothing whatever their order, and nothing overflows or vanishes on the way; vector
 // instructions fill 29 % of the issue slots in bfloat16.  Tried and dropped: clipping in reverse order, for what the norm's pass left in the 256 MB cache
