@@ -211,3 +211,19 @@ def test_a_first_call_on_many_short_tensors_takes_no_longer_than_the_handle(driv
     against dadam_init's on the same layout (twice that by elements)."""
     (a,) = ask(driver, "tensors 40000 500")
     assert a.code == 0 and a.us[1] < a.us[0], a.us
+
+
+def test_lists_under_address_and_ub_sanitizers(tmp_path):
+    """What launches are given of matrices whose rows share lists or do not, against the matrix (tests/host_lists_driver.cpp)."""
+    clang = "/opt/rocm/lib/llvm/bin/clang++"
+    if not os.path.exists(clang):
+        pytest.skip("clang++ of the ROCm toolchain not available")
+    exe, csrc = str(tmp_path / "lists_driver"), os.path.join(ROOT, "paper_2410_11998_amd", "csrc")
+    cmd = [clang, "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=undefined", "-D__HIP_PLATFORM_AMD__",
+           "-I", os.path.join(ROOT, "include"), "-I", csrc, "-I", "/opt/rocm/include", os.path.join(ROOT, "tests", "host_lists_driver.cpp"),
+           os.path.join(csrc, "dadam_host.cpp"), os.path.join(csrc, "dadam_operators.cpp"), "-o", exe]
+    r = subprocess.run(cmd, capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, r.stderr[-2000:]
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0 and " bad 0" in r.stdout and "ERROR" not in r.stderr, (r.stdout[-500:], r.stderr[-3000:])
+    assert int(r.stdout.split()[1]) > 4000
