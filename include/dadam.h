@@ -497,6 +497,63 @@ int dadam_mx4_gossip(dadam_handle* h, uint32_t slot, const void* const* msg, flo
 int dadam_mx4_round(dadam_handle* h, uint32_t slot, const void* const* x_src, void* const* x_dst, float* const* copy,
                     float* const* sum, float gamma, void* hip_stream);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * The ends of an iteration: the loss of a language model's head, and the step of its matrices along an orthogonalised direction
+ *
+ * These calls take a workspace: DEVICE memory, caller-owned, 256-byte aligned, that a call may overwrite throughout and that holds nothing between
+ * calls.  Calls that may overlap in time need one each, and so do graphs that are replayed side by side.  The calls themselves allocate nothing, and may be
+ * recorded into a graph.  With less workspace than `bytes` of the information calls (but `least_bytes`) they go in more, smaller launches, with the same
+ * results up to the order of sums.  What a call writes must not overlap anything else that it reads or writes, but where "in place" is named.
+ * Errors of all: DADAM_EINVAL (null, value out of range, workspace too small), DADAM_EALIGN, DADAM_EALIAS, DADAM_ESTATE, DADAM_EHIP. */
+
+/* A matrix of the packed layout: element (r, c) is element first + r * ld + c of the tensor.  Several may share a tensor (projections that are
+ * fused side by side) but no element, and columns do not run on into the next row: first % ld + cols <= ld.  scale multiplies the orthogonalised direction
+ * (for instance sqrt(max(1, rows / cols)), or 0.2 sqrt(max(rows, cols)) for updates of Adam's size).  flags must be 0. */
+typedef struct {
+  uint32_t tensor;
+  uint32_t rows, cols; /* 1 to 65536 */
+  uint32_t ld;         /* >= cols */
+  uint64_t first;
+  float scale;
+  uint32_t flags;
+} dadam_matrix_desc;
+
+/* Register the matrices that the two calls below are about, in place of those registered before; n may be 0.  matrices[n] is a HOST array and is
+ * copied.  Allocates and uploads 64 bytes a matrix and about 8 bytes for every 128 x 128 elements, and may wait for the device: not for use under stream capture, and
+ * only while no launched work still uses the old ones. */
+int dadam_set_matrices(dadam_handle* h, const dadam_matrix_desc* matrices, uint32_t n);
+
+/* The iterations that orthogonalise: coefficients[3 k ...] (HOST) are a, b, c of iteration k.  The default is five times 3.4445, -4.7750, 2.0315, which takes
+ * singular values from about 0.01 on to between 0.7 and 1.2.  DADAM_EINVAL where a singular value of up to 1 would go beyond 1024 on the way. */
+#define DADAM_ORTHO_MAX_STEPS 16u
+int dadam_set_ortho_schedule(dadam_handle* h, uint32_t n_steps, const float* coefficients);
+
+typedef struct {
+  uint32_t n_matrices, reserved;
+  uint64_t least_bytes; /* the workspace without which a call is refused: that of one replica's largest matrix */
+  uint64_t bytes;       /* what a call makes good use of */
+} dadam_ortho_info;
+int dadam_ortho_get_info(const dadam_handle* h, dadam_ortho_info* out);
+
+/* Every registered matrix M of every row i brought near its orthogonal polar factor by Newton-Schulz iterations:
+ *     X = M / (|M| + 1e-7)   (Frobenius norm, summed in 64 bits);   every iteration:  A = X X^T,  X = a X + (b A + c A A) X
+ * (of a matrix with more rows than columns, its transpose's).  in and out: n_rows buffers of cfg.d elements of grad_dtype; out[i] may be in[i] (in place).
+ * Elements outside the matrices are neither used nor written.  A matrix of zeros stays one; a NaN or an infinity makes its own matrix NaN and no other.
+ * float32 results come from operands of 22 bits, bfloat16 results from operands of 11 bits (X itself of 22), sums are float32: the error is about 3e-6 and 2e-3 of
+ * the result (2-norms). */
+int dadam_orthogonalize(dadam_handle* h, const void* const* in, void* const* out, void* workspace, uint64_t workspace_bytes, void* hip_stream);
+
+/* The step of the registered matrices along the orthogonalised first moment, in iteration t of Algorithm 3 and on the bound buffers: with
+ *     m = beta1 * m_hat_i + (1 - beta1) * g_i                               line 6
+ *     u = m,  or  beta1 * m + (1 - beta1) * g_i  with DADAM_ORTHO_NESTEROV
+ *     x_dst_i = sum_k w[k] * x_src[col[k]] - lr * (scale * O(u) + weight_decay * x_src[i])       O: dadam_orthogonalize of the matrix
+ * and with DADAM_FUSE_ACCUM lines 9 to 13 for m_hat and b (v_hat takes no part).  O does not depend on the length of u, so there is no bias correction.  Elements outside
+ * the matrices are left to dadam_gossip_step_range over the other tensors.  Arguments as there, and the same rules for updates in place: x_dst[i] may be a source that no
+ * other row reads.  Precision of O by param_dtype; sums over neighbours and the step in float32, one rounding to param_dtype. */
+#define DADAM_ORTHO_NESTEROV 8u
+int dadam_ortho_step(dadam_handle* h, uint32_t slot, const void* const* grads, uint64_t t, uint32_t flags, void* workspace,
+                     uint64_t workspace_bytes, void* hip_stream);
+
 /* Text of the last error recorded on this handle ("" if none).  With h == NULL: the text of the
  * last dadam_init failure of the calling thread.  The pointer stays valid until the next call on
  * the same handle (thread). */

@@ -31,6 +31,7 @@ DADAM_OK, DADAM_EINVAL, DADAM_EALIGN, DADAM_ETOPO, DADAM_EALIAS, DADAM_ESTATE, D
 DADAM_FUSE_ACCUM, DADAM_FORCE_DIRECT, DADAM_FORCE_TILE = 1, 2, 4
 DADAM_WARN_NOT_COLUMN_STOCHASTIC = 1
 DADAM_MX4_BLOCK, DADAM_MX4_ADD = 32, 1
+DADAM_ORTHO_MAX_STEPS, DADAM_ORTHO_NESTEROV = 16, 8
 DADAM_PLACE_TWO_REGIONS, DADAM_PLACE_ARENA_ELSEWHERE, DADAM_PLACE_TOO_LARGE = 1, 2, 4
 
 EXPORTS = [
@@ -39,6 +40,7 @@ EXPORTS = [
     "dadam_slot_uses_tile_mode", "dadam_get_row_order", "dadam_pack_offsets", "dadam_spread_offsets", "dadam_place_offsets", "dadam_deal_offsets", "dadam_find_stretches", "dadam_regions_from_stretches",
     "dadam_place_by_timing",
     "dadam_grad_norm", "dadam_clip_grads", "dadam_mx4_get_info", "dadam_mx4_encode", "dadam_mx4_product", "dadam_mx4_gossip", "dadam_mx4_round",
+    "dadam_set_matrices", "dadam_set_ortho_schedule", "dadam_ortho_get_info", "dadam_orthogonalize", "dadam_ortho_step",
     "dadam_last_error",
     "dadam_destroy",
 ]
@@ -75,6 +77,15 @@ class dadam_plan_info(C.Structure):
 
 class dadam_mx4_info(C.Structure):
     _fields_ = [("n_blocks", C.c_uint64), ("scale_offset", C.c_uint64), ("bytes", C.c_uint64)]
+
+
+class dadam_matrix_desc(C.Structure):
+    _fields_ = [("tensor", C.c_uint32), ("rows", C.c_uint32), ("cols", C.c_uint32), ("ld", C.c_uint32), ("first", C.c_uint64), ("scale", C.c_float),
+                ("flags", C.c_uint32)]
+
+
+class dadam_ortho_info(C.Structure):
+    _fields_ = [("n_matrices", C.c_uint32), ("reserved", C.c_uint32), ("least_bytes", C.c_uint64), ("bytes", C.c_uint64)]
 
 
 PROBE_CHUNK_BYTES, PROBE_STEP_BYTES, MAX_STRETCHES = 1 << 30, 4 << 30, 6
@@ -132,6 +143,11 @@ def _load() -> C.CDLL:
     lib.dadam_mx4_product.argtypes = [H, C.c_uint32, P, P, C.c_uint32, C.c_void_p]
     lib.dadam_mx4_gossip.argtypes = [H, C.c_uint32, P, P, P, P, P, C.c_float, C.c_void_p]
     lib.dadam_mx4_round.argtypes = [H, C.c_uint32, P, P, P, P, C.c_float, C.c_void_p]
+    lib.dadam_set_matrices.argtypes = [H, C.POINTER(dadam_matrix_desc), C.c_uint32]
+    lib.dadam_set_ortho_schedule.argtypes = [H, C.c_uint32, C.POINTER(C.c_float)]
+    lib.dadam_ortho_get_info.argtypes = [H, C.POINTER(dadam_ortho_info)]
+    lib.dadam_orthogonalize.argtypes = [H, P, P, C.c_void_p, C.c_uint64, C.c_void_p]
+    lib.dadam_ortho_step.argtypes = [H, C.c_uint32, P, C.c_uint64, C.c_uint32, C.c_void_p, C.c_uint64, C.c_void_p]
     lib.dadam_last_error.argtypes = [H]
     lib.dadam_last_error.restype = C.c_char_p
     lib.dadam_destroy.argtypes = [H]
@@ -504,6 +520,62 @@ def dadam_mx4_round(h, slot: int, x_src, x_dst, copy, sum, gamma: float, stream:
     x_src, x_dst = pointer_table(x_src, rows, d, pb, "x_src", gpu), pointer_table(x_dst, rows, d, pb, "x_dst", gpu)
     copy, sum = pointer_table(copy, rows, d, 4, "copy", gpu), pointer_table(sum, rows, d, 4, "sum", gpu)
     _check(h, lib.dadam_mx4_round(h, slot, _at(x_src), _at(x_dst), _at(copy), _at(sum), gamma, stream))
+
+
+def dadam_set_matrices(h, matrices) -> None:
+    """matrices: (tensor, rows, cols, ld, first, scale), from ld on by default cols, 0 and 1 (a sequence may stop early), or dadam_matrix_desc."""
+    descs = (dadam_matrix_desc * max(1, len(matrices)))()
+    for k, m in enumerate(matrices):
+        if isinstance(m, dadam_matrix_desc):
+            descs[k] = m
+            continue
+        m = tuple(m)
+        if not 3 <= len(m) <= 6:
+            raise ValueError("a matrix is (tensor, rows, cols, ld, first, scale)")
+        tensor, rows, cols, ld, first, scale = m + (m[2], 0, 1.0)[len(m) - 3:]
+        descs[k] = dadam_matrix_desc(int(tensor), int(rows), int(cols), int(ld), int(first), float(scale), 0)
+    _check(h, lib.dadam_set_matrices(h, descs, len(matrices)))
+
+
+def dadam_set_ortho_schedule(h, coefficients) -> None:
+    """coefficients: (a, b, c) of every iteration."""
+    flat = [float(v) for abc in coefficients for v in abc]
+    if len(flat) != 3 * len(coefficients):
+        raise ValueError("an iteration has three coefficients")
+    _check(h, lib.dadam_set_ortho_schedule(h, len(coefficients), (C.c_float * max(1, len(flat)))(*flat)))
+
+
+def dadam_ortho_get_info(h) -> dadam_ortho_info:
+    info = dadam_ortho_info()
+    _check(h, lib.dadam_ortho_get_info(h, C.byref(info)))
+    return info
+
+
+def _workspace(workspace, on_device: bool):
+    """(address, bytes) of a workspace: a contiguous tensor of any type, (address, bytes), or None."""
+    if workspace is None:
+        return 0, 0
+    if isinstance(workspace, tuple):
+        return workspace
+    if not workspace.is_contiguous():
+        raise ValueError("workspace is not contiguous")
+    if on_device and not workspace.is_cuda:
+        raise ValueError("workspace is not on a GPU")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def dadam_orthogonalize(h, in_, out, workspace, stream: int = 0) -> None:
+    """workspace: a device tensor of dadam_ortho_get_info(h).bytes bytes (or (address, bytes))."""
+    d, _, gb, rows, _, gpu = _shape(h)
+    i, o = pointer_table(in_, rows, d, gb, "in", gpu), pointer_table(out, rows, d, gb, "out", gpu)
+    _check(h, lib.dadam_orthogonalize(h, _at(i), _at(o), *_workspace(workspace, gpu), stream))
+
+
+def dadam_ortho_step(h, slot: int, grads, t: int, flags: int, workspace, stream: int = 0) -> None:
+    """grads as dadam_gossip_step takes them, or one tensor whose rows they are; workspace as dadam_orthogonalize."""
+    d, _, gb, rows, _, gpu = _shape(h)
+    g = pointer_table(grads, rows, d, gb, "grads", gpu)
+    _check(h, lib.dadam_ortho_step(h, slot, _at(g), t, flags, *_workspace(workspace, gpu), stream))
 
 
 def dadam_destroy(h) -> None:

@@ -64,6 +64,7 @@ struct DeviceGuard {
 };
 
 struct OperatorState;
+struct MatrixState;
 
 }  // namespace dadam
 
@@ -137,6 +138,9 @@ struct dadam_handle {
   OperatorState* operators = nullptr;
   void (*free_operators)(OperatorState*) = nullptr;
   int (*add_mix_lists)(dadam_handle*, Slot*) = nullptr;
+  // The matrices of the layout as dadam_set_matrices was told of them (dadam_ortho.cpp), and what frees that.
+  MatrixState* matrices = nullptr;
+  void (*free_matrices)(MatrixState*) = nullptr;
 };
 
 namespace dadam {
@@ -162,6 +166,10 @@ inline int check_device(const dadam_handle* h) {
     return fail(h, DADAM_ESTATE, "host-only handle (device = DADAM_DEVICE_NONE) cannot launch");
   return DADAM_OK;
 }
+
+// What a step that goes row by row (every row reads its own list of sources) checks before it launches, and its phase and scalars
+// (dadam_host.cpp).
+int prepare_step(dadam_handle* h, uint32_t slot, const void* const* grads, uint64_t t, bool fuse, Phase* phase, Scalars* scalars);
 
 }  // namespace dadam
 

@@ -841,6 +841,27 @@ void free_slot(Slot& s) {
 // -------------------------------------------------------------------------------------------------
 // C ABI
 // -------------------------------------------------------------------------------------------------
+namespace dadam {
+
+int prepare_step(dadam_handle* h, uint32_t slot_id, const void* const* grads, uint64_t t, bool fuse, Phase* phase, Scalars* scalars) {
+  int rc = check_bound(h);
+  if (rc) return rc;
+  if (slot_id >= DADAM_MAX_SLOTS || !h->slots[slot_id].set) return fail(h, DADAM_ESTATE, "topology slot %u is not set", slot_id);
+  if (t == 0) return fail(h, DADAM_EINVAL, "iterations are numbered from 1");
+  rc = check_grads(h, grads);
+  if (rc) return rc;
+  *phase = fuse ? fused_phase(h, t) : kUpdateOnly;
+  if (h->cfg.accum_s > 1 && fuse)
+    for (uint32_t i = 0; i < h->cfg.n_rows; ++i)
+      if (!h->acc[i]) return fail(h, DADAM_ESTATE, "accumulator of row %u is not bound", i);
+  if (!direct_is_legal(h, h->slots[slot_id], h->decays))
+    return fail(h, DADAM_EALIAS, "a row updated in place overwrites a source that another row reads");
+  fill_scalars(h, t, scalars);
+  return DADAM_OK;
+}
+
+}  // namespace dadam
+
 extern "C" {
 
 int dadam_init(const dadam_config* cfg, dadam_handle** out) {
@@ -1431,11 +1452,14 @@ void dadam_destroy(dadam_handle* h) {
   if (h->cfg.device != DADAM_DEVICE_NONE) {
     DeviceGuard guard(h->cfg.device);
     if (h->free_operators) h->free_operators(h->operators);
+    if (h->free_matrices) h->free_matrices(h->matrices);
     for (Slot& s : h->slots) free_slot(s);
     if (h->d_segs) (void)hipFree(h->d_segs);
     if (h->d_map) (void)hipFree(h->d_map);
     if (h->d_partials) (void)hipFree(h->d_partials);
     if (h->d_tables) (void)hipFree(h->d_tables);
+  } else if (h->free_matrices) {
+    h->free_matrices(h->matrices);
   }
   delete h;
 }

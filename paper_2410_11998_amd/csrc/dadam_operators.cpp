@@ -10,6 +10,7 @@
 #include <new>
 #include <vector>
 
+#include "dadam_checks.h"
 #include "dadam_handle.h"
 #include "dadam_operators.h"
 
@@ -24,16 +25,6 @@ struct OperatorState {
 };
 
 namespace {
-
-// No exception leaves an entry point.
-template <typename Fn>
-int guarded(dadam_handle* h, Fn fn) {
-  try {
-    return fn();
-  } catch (const std::bad_alloc&) {
-    return fail(h, DADAM_EINVAL, "out of host memory");
-  }
-}
 
 uint64_t granules_of(const dadam_handle* h) { return (h->cfg.d + kGranule - 1) / kGranule; }
 
@@ -151,8 +142,6 @@ void free_state(OperatorState* s) {
   delete s;
 }
 
-constexpr uint64_t kMostElems = 1ull << 36;  // index and masks count in 32 bits
-
 int make_state(dadam_handle* h) {
   std::unique_ptr<OperatorState, void (*)(OperatorState*)> s(new OperatorState(), free_state);
   const std::vector<uint32_t> cuts = build_cuts(h);
@@ -189,80 +178,9 @@ int make_state(dadam_handle* h) {
   return DADAM_OK;
 }
 
-// One argument of a call: n buffers of `bytes` bytes.
-struct Table {
-  const void* const* p;
-  uint32_t n;
-  size_t bytes;
-  const char* name;
-  bool written;
-  int in_place_of;  // the table whose entry of the same number this one's may be, -1 none
-};
-
-struct Range {
-  uintptr_t lo, hi;
-  int table;
-  uint32_t index;
-};
-
-constexpr uintptr_t kHighest = (uintptr_t)1 << 52;
-
-// Nothing that is written overlaps anything else, but the same entry of the table it may be in place of.
-int check_overlaps(const dadam_handle* h, const Table* t, int n_tables) {
-  Range all[5 * DADAM_MAX_ROWS], open[5 * DADAM_MAX_ROWS];  // open: earlier ranges that reach beyond where the walk is
-  uint32_t n = 0, n_open = 0;
-  for (int k = 0; k < n_tables; ++k)
-    for (uint32_t i = 0; t[k].p && i < t[k].n; ++i) all[n++] = {(uintptr_t)t[k].p[i], (uintptr_t)t[k].p[i] + t[k].bytes, k, i};
-  std::sort(all, all + n, [](const Range& a, const Range& b) { return a.lo < b.lo; });
-  for (uint32_t q = 0; q < n; ++q) {
-    const Range& r = all[q];
-    n_open = (uint32_t)(std::remove_if(open, open + n_open, [&](const Range& o) { return o.hi <= r.lo; }) - open);
-    for (uint32_t k = 0; k < n_open; ++k) {
-      const Range& o = open[k];
-      if (!t[r.table].written && !t[o.table].written) continue;
-      const bool pair = t[r.table].in_place_of == o.table || t[o.table].in_place_of == r.table;
-      if (pair && r.lo == o.lo && r.index == o.index) continue;
-      return fail(h, DADAM_EALIAS, "%s[%u] overlaps %s[%u]", t[r.table].name, r.index, t[o.table].name, o.index);
-    }
-    open[n_open++] = r;
-  }
-  return DADAM_OK;
-}
-
-// Every buffer is there, aligned and within reach, and does not overlap what it must not.
-int check_tables(const dadam_handle* h, const Table* t, int n_tables) {
-  if (h->cfg.d > kMostElems) return fail(h, DADAM_EINVAL, "the operators around the step take up to 2^36 elements");
-  bool apart = true;  // tables of increasing buffers, one table's behind the other's: nothing overlaps
-  uintptr_t lows[5], highs[5];
-  int n_used = 0;
-  for (int k = 0; k < n_tables; ++k) {
-    if (!t[k].p || t[k].n == 0) continue;
-    uintptr_t end = 0;
-    for (uint32_t i = 0; i < t[k].n; ++i) {
-      const uintptr_t at = (uintptr_t)t[k].p[i];
-      if (!at) return fail(h, DADAM_EINVAL, "%s[%u] is null", t[k].name, i);
-      if (at & 15u) return fail(h, DADAM_EALIGN, "%s[%u] is not 16-byte aligned", t[k].name, i);
-      if (at >= kHighest || t[k].bytes > kHighest - at) return fail(h, DADAM_EINVAL, "%s[%u] reaches above address 2^52", t[k].name, i);
-      apart &= at >= end;
-      end = at + t[k].bytes;
-    }
-    lows[n_used] = (uintptr_t)t[k].p[0];
-    highs[n_used++] = end;
-  }
-  for (int k = 0; k < n_used; ++k)
-    for (int m = 0; m < k; ++m) apart &= highs[k] <= lows[m] || highs[m] <= lows[k];
-  return apart ? DADAM_OK : check_overlaps(h, t, n_tables);
-}
-
 int check_norms(const dadam_handle* h, const float* norms) {
   if (!norms) return fail(h, DADAM_EINVAL, "norms is null");
   if ((uintptr_t)norms & 3u) return fail(h, DADAM_EALIGN, "norms is not 4-byte aligned");
-  return DADAM_OK;
-}
-
-int check_slot(const dadam_handle* h, uint32_t slot) {
-  if (slot >= DADAM_MAX_SLOTS) return fail(h, DADAM_EINVAL, "slot %u out of range", slot);
-  if (!h->slots[slot].set) return fail(h, DADAM_ESTATE, "slot %u has no topology", slot);
   return DADAM_OK;
 }
 
@@ -345,13 +263,6 @@ uint32_t round_groups(const dadam_handle* h, const Slot& s) {
 // 309, 100 of 4e6 373 / 330, of 1e6 129 / 110; 8 rows of 8e6 45 / 59.  Runs of 32 / 128 / 1024 pieces: the first 802 / 759 / 1050.
 bool copies_rows(const dadam_handle* h, const Slot& s, MixMode mode) {
   return mode == kMixStore && h->cfg.d * h->cfg.n_rows >= kManyElems && shares_rows(h, s) && granules_of(h) >= kProductGranules;
-}
-
-bool captures(void* stream) {
-  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(reinterpret_cast<hipStream_t>(stream), &status) == hipSuccess) return status != hipStreamCaptureStatusNone;
-  (void)hipGetLastError();
-  return true;
 }
 
 // Runs the launches of a call whose arguments have passed, with the handle's device current and its state made.  (Allocating it would end a

@@ -1,0 +1,422 @@
+// Host side of orthogonalised updates (include/dadam.h, "The ends of an iteration"): the matrices of a layout, the schedule of the iteration, what
+// the operands are held times, and the launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <memory>
+#include <vector>
+
+#include "dadam_checks.h"
+#include "dadam_handle.h"
+#include "dadam_ortho.h"
+
+namespace dadam {
+
+struct MatrixState {
+  // dadam_set_matrices: by size, the largest first
+  std::vector<OrthoTask> tasks;
+  std::vector<uint64_t> need[2];  // bytes of workspace of a matrix and a replica, with one plane and with two
+  char* memory = nullptr;         // tasks, and the matrix of every tile of either kind
+  const OrthoTask* d_tasks[2] = {};
+  const uint32_t *d_gram = nullptr, *d_whole = nullptr;
+  uint32_t gram_units = 0, whole_units = 0;
+  // dadam_set_ortho_schedule
+  std::vector<float> coefficients{3.4445f, -4.7750f, 2.0315f, 3.4445f, -4.7750f, 2.0315f, 3.4445f, -4.7750f, 2.0315f, 3.4445f, -4.7750f, 2.0315f, 3.4445f, -4.7750f, 2.0315f};
+};
+
+namespace {
+
+void free_matrices(MatrixState* m) {
+  if (!m) return;
+  if (m->memory) (void)hipFree(m->memory);
+  delete m;
+}
+
+MatrixState* state_of(dadam_handle* h) {
+  if (!h->matrices) {
+    h->matrices = new MatrixState();
+    h->free_matrices = free_matrices;
+  }
+  return h->matrices;
+}
+
+uint32_t filled(uint32_t n) { return (n + kOrthoPad - 1) / kOrthoPad * kOrthoPad; }
+
+constexpr uint32_t kMostMatrices = 65536, kMostSide = 65536;
+
+// Rectangles of one tensor that is read as rows of ld elements.
+struct Rectangle {
+  uint64_t r0, r1, c0, c1;
+};
+
+int check_matrices(const dadam_handle* h, const dadam_matrix_desc* m, uint32_t n) {
+  std::vector<std::vector<uint32_t>> of_tensor(h->tensors.size());
+  for (uint32_t k = 0; k < n; ++k) {
+    if (m[k].tensor >= h->tensors.size()) return fail(h, DADAM_EINVAL, "matrix %u: tensor %u out of range", k, m[k].tensor);
+    if (m[k].flags) return fail(h, DADAM_EINVAL, "matrix %u: flags must be 0", k);
+    if (!std::isfinite(m[k].scale)) return fail(h, DADAM_EINVAL, "matrix %u: scale must be finite", k);
+    const uint64_t rows = m[k].rows, cols = m[k].cols, ld = m[k].ld, numel = h->tensors[m[k].tensor].numel;
+    if (!rows || !cols || rows > kMostSide || cols > kMostSide) return fail(h, DADAM_EINVAL, "matrix %u: rows and columns must be 1 to %u", k, kMostSide);
+    if (ld < cols || m[k].first % ld + cols > ld) return fail(h, DADAM_EINVAL, "matrix %u: its columns do not lie in one row of ld elements", k);
+    if (m[k].first >= numel || numel - m[k].first < cols || (rows - 1) > (numel - m[k].first - cols) / ld)
+      return fail(h, DADAM_EINVAL, "matrix %u reaches beyond its tensor", k);
+    of_tensor[m[k].tensor].push_back(k);
+  }
+  for (std::vector<uint32_t>& list : of_tensor) {
+    auto end = [&](uint32_t k) { return m[k].first + (uint64_t)(m[k].rows - 1) * m[k].ld + m[k].cols; };
+    std::sort(list.begin(), list.end(), [&](uint32_t a, uint32_t b) { return m[a].first < m[b].first; });
+    for (size_t i = 0; i < list.size(); ++i)
+      for (size_t j = i + 1; j < list.size() && m[list[j]].first < end(list[i]); ++j) {
+        const dadam_matrix_desc &a = m[list[i]], &b = m[list[j]];
+        auto box = [](const dadam_matrix_desc& x) { return Rectangle{x.first / x.ld, x.first / x.ld + x.rows, x.first % x.ld, x.first % x.ld + x.cols}; };
+        const Rectangle p = box(a), q = box(b);
+        if (a.ld != b.ld || (p.r0 < q.r1 && q.r0 < p.r1 && p.c0 < q.c1 && q.c0 < p.c1))
+          return fail(h, DADAM_EINVAL, "matrices %u and %u share elements", list[i], list[j]);
+      }
+  }
+  return DADAM_OK;
+}
+
+int set_matrices(dadam_handle* h, const dadam_matrix_desc* m, uint32_t n) {
+  if (const int rc = check_matrices(h, m, n)) return rc;
+  std::unique_ptr<MatrixState, void (*)(MatrixState*)> s(new MatrixState(), free_matrices);
+  if (h->matrices) s->coefficients = h->matrices->coefficients;
+  std::vector<OrthoTask> tasks(n);
+  for (uint32_t k = 0; k < n; ++k) {
+    OrthoTask& t = tasks[k];
+    const dadam_tensor_desc& tensor = h->tensors[m[k].tensor];
+    t.first = tensor.offset_elems + m[k].first;
+    t.ld = m[k].ld;
+    t.tall = m[k].rows > m[k].cols;
+    t.p = std::min(m[k].rows, m[k].cols);
+    t.q = std::max(m[k].rows, m[k].cols);
+    t.P = filled(t.p);
+    t.Q = filled(t.q);
+    t.scale = m[k].scale;
+    t.decay = tensor.weight_decay;
+  }
+  std::stable_sort(tasks.begin(), tasks.end(), [](const OrthoTask& a, const OrthoTask& b) { return (uint64_t)a.P * a.P * a.Q > (uint64_t)b.P * b.P * b.Q; });
+  std::vector<uint32_t> gram, whole;
+  uint64_t gram_units = 0, whole_units = 0;
+  for (const OrthoTask& t : tasks) {
+    const uint64_t across = t.P / kOrthoPad;
+    gram_units += across * (across + 1) / 2;
+    whole_units += across * (t.Q / kOrthoPad);
+  }
+  if (whole_units >> 31) return fail(h, DADAM_EINVAL, "the matrices have more than 2^31 tiles");
+  gram.reserve(gram_units);
+  whole.reserve(whole_units);
+  std::vector<OrthoTask> planes[2] = {tasks, tasks};
+  for (uint32_t p = 0; p < 2; ++p) {
+    uint64_t at = 0;
+    for (uint32_t k = 0; k < n; ++k) {
+      OrthoTask& t = planes[p][k];
+      if (p == 0) {
+        tasks[k].gram_units = (uint32_t)gram.size();
+        tasks[k].whole_units = (uint32_t)whole.size();
+        const uint64_t across = t.P / kOrthoPad;
+        gram.insert(gram.end(), across * (across + 1) / 2, k);
+        whole.insert(whole.end(), across * (t.Q / kOrthoPad), k);
+      }
+      t.gram_units = tasks[k].gram_units;
+      t.whole_units = tasks[k].whole_units;
+      t.at = at;
+      s->need[p].push_back(ortho_places(t.P, t.Q, p + 1).bytes);
+      at += s->need[p].back();
+    }
+    s->need[p].push_back(at);
+  }
+  s->tasks = planes[0];
+  s->gram_units = (uint32_t)gram.size();
+  s->whole_units = (uint32_t)whole.size();
+  if (h->cfg.device != DADAM_DEVICE_NONE && n) {
+    DeviceGuard guard(h->cfg.device);
+    if (guard.err != hipSuccess) return fail(h, DADAM_EHIP, "hipSetDevice: %s", hipGetErrorString(guard.err));
+    const size_t list = n * sizeof(OrthoTask), g = gram.size() * 4, w = whole.size() * 4;
+    std::vector<char> image(2 * list + g + w);
+    memcpy(image.data(), planes[0].data(), list);
+    memcpy(image.data() + list, planes[1].data(), list);
+    memcpy(image.data() + 2 * list, gram.data(), g);
+    memcpy(image.data() + 2 * list + g, whole.data(), w);
+    hipError_t e = hipMalloc((void**)&s->memory, image.size());
+    if (e == hipSuccess) e = hipMemcpy(s->memory, image.data(), image.size(), hipMemcpyHostToDevice);
+    if (e != hipSuccess) {
+      (void)hipGetLastError();
+      return fail(h, DADAM_EHIP, "uploading the matrices failed: %s", hipGetErrorString(e));
+    }
+    s->d_tasks[0] = reinterpret_cast<const OrthoTask*>(s->memory);
+    s->d_tasks[1] = s->d_tasks[0] + n;
+    s->d_gram = reinterpret_cast<const uint32_t*>(s->memory + 2 * list);
+    s->d_whole = s->d_gram + gram.size();
+    MatrixState* old = h->matrices;
+    h->matrices = s.release();
+    h->free_matrices = free_matrices;
+    free_matrices(old);
+    return DADAM_OK;
+  }
+  if (h->cfg.device != DADAM_DEVICE_NONE && h->matrices) {
+    DeviceGuard guard(h->cfg.device);
+    free_matrices(h->matrices);
+  } else {
+    free_matrices(h->matrices);
+  }
+  h->matrices = s.release();
+  h->free_matrices = free_matrices;
+  return DADAM_OK;
+}
+
+// The largest |f| on [0, limit], by samples close enough for a bound with a margin.
+template <typename Fn>
+double largest(double limit, Fn f) {
+  double most = 0.0;
+  constexpr int n = 2048;
+  for (int k = 0; k <= n; ++k) most = std::max(most, std::fabs(f(limit * k / n)));
+  return 1.01 * most;
+}
+
+// What X, A and B of every iteration are held times: the power of two that brings a bound of the spectral norm, and with it of every element, to
+// [2^12, 2^13], an eighth of what a half can hold.  X of iteration 0 has Frobenius norm 1.
+struct Powers {
+  std::vector<int> x, a, b;
+};
+constexpr double kLargestNorm = 1024.0;
+int power_for(double bound) { return 13 - (int)std::ceil(std::log2(std::max(bound, 1e-3))); }
+bool find_powers(const std::vector<float>& c, Powers* out) {
+  double bound = 1.0;
+  for (size_t k = 0; k + 2 < c.size(); k += 3) {
+    const double a = c[k], b = c[k + 1], cc = c[k + 2];
+    out->x.push_back(power_for(bound));
+    out->a.push_back(power_for(bound * bound));
+    out->b.push_back(power_for(largest(bound * bound, [&](double s) { return b * s + cc * s * s; })));
+    bound = largest(bound, [&](double s) { return a * s + b * s * s * s + cc * s * s * s * s * s; });
+    if (!(bound <= kLargestNorm)) return false;
+  }
+  return true;
+}
+
+// Workspace that a call makes good use of.  Beyond it a larger one gains nothing: the matrices go in groups that fill the chip.
+constexpr uint64_t kOrthoWorkspace = 1ull << 30;
+
+uint32_t planes_of(uint32_t dtype) { return dtype == DADAM_BF16 ? 1 : 2; }
+
+struct Call {
+  const void* const* grads;
+  void* const* out;
+  OrthoSource source;
+  Phase phase;
+  Scalars c;
+  bool mix;
+  uint32_t slot, dtype;  // of the result
+  char* workspace;
+  uint64_t bytes;
+};
+
+// A matrices-by-replicas rectangle, whole.
+int run_group(dadam_handle* h, const Call& call, const Powers& pw, uint32_t k0, uint32_t k1, uint32_t i0, uint32_t replicas, void* stream) {
+  const MatrixState& m = *h->matrices;
+  const uint32_t planes = planes_of(call.dtype), n = (uint32_t)m.tasks.size();
+  auto units = [&](bool gram, uint32_t* first) {
+    auto before = [&](uint32_t k) { return gram ? (k < n ? m.tasks[k].gram_units : m.gram_units) : (k < n ? m.tasks[k].whole_units : m.whole_units); };
+    *first = before(k0);
+    return before(k1) - before(k0);
+  };
+  OrthoSpan gram{}, whole{};
+  gram.tasks = m.d_tasks[planes - 1];
+  gram.workspace = (uint64_t)(uintptr_t)call.workspace;
+  for (uint32_t k = 0; k < k0; ++k) gram.before += m.need[planes - 1][k];
+  for (uint32_t k = k0; k < k1; ++k) gram.stride += m.need[planes - 1][k];
+  gram.n_xcd = h->n_xcds;
+  whole = gram;
+  gram.units = m.d_gram;
+  whole.units = m.d_whole;
+  const uint32_t gram_units = units(true, &gram.first_unit), whole_units = units(false, &whole.first_unit);
+  OrthoBeginArgs<kMaxRows> begin;
+  memset((void*)&begin, 0, sizeof(begin));
+  begin.s = whole;
+  for (uint32_t r = 0; r < replicas; ++r) {
+    begin.grad[r] = call.grads[i0 + r];
+    if (call.source == kOrthoGiven) continue;
+    begin.m_hat[r] = h->m_hat[i0 + r];
+    begin.acc[r] = h->acc[i0 + r];
+  }
+  begin.c = call.c;
+  begin.scale = std::ldexp(1.f, pw.x[0]);
+  begin.source = call.source;
+  begin.phase = call.phase;
+  int e = launch_ortho_norm((int)h->cfg.grad_dtype, begin, planes, whole_units, replicas, stream);
+  if (!e) e = launch_ortho_begin((int)h->cfg.grad_dtype, begin, planes, whole_units, replicas, stream);
+  const size_t steps = pw.x.size();
+  for (size_t k = 0; k < steps && !e; ++k) {
+    const float a = m.coefficients[3 * k], b = m.coefficients[3 * k + 1], c = m.coefficients[3 * k + 2];
+    const int x = pw.x[k], pa = pw.a[k], pb = pw.b[k];
+    OrthoStepArgs s{};
+    s.s = gram;
+    s.fresh = std::ldexp(1.f, pa - 2 * x);
+    e = launch_ortho_gram(false, s, planes, gram_units, replicas, stream);
+    s.gain = std::ldexp(b, pb - pa);
+    s.fresh = std::ldexp(c, pb - 2 * pa);
+    if (!e) e = launch_ortho_gram(true, s, planes, gram_units, replicas, stream);
+    if (e) break;
+    s.s = whole;
+    s.from = (uint32_t)(k & 1);
+    s.to = s.from ^ 1;
+    if (k + 1 < steps) {
+      s.gain = std::ldexp(a, pw.x[k + 1] - x);
+      s.fresh = std::ldexp(1.f, pw.x[k + 1] - x - pb);
+      e = launch_ortho_next(s, planes, whole_units, replicas, stream);
+      continue;
+    }
+    OrthoEndArgs<kMaxRows> end;
+    memset((void*)&end, 0, sizeof(end));
+    end.s = whole;
+    end.gain = std::ldexp(a, -x);
+    end.fresh = std::ldexp(1.f, -x - pb);
+    end.from = s.from;
+    end.mix = call.mix;
+    for (uint32_t r = 0; r < replicas; ++r) end.out[r] = call.out[i0 + r];
+    if (call.mix) {
+      for (uint32_t q = 0; q < h->cfg.n_cols; ++q) end.x_src[q] = h->x_src[q];
+      const Slot& slot = h->slots[call.slot];
+      end.row_ptr = slot.d_row_ptr;
+      end.col = slot.d_col;
+      end.w = slot.d_w;
+      end.first_row = i0;
+      end.lr = call.c.lr;
+    }
+    e = launch_ortho_end((int)call.dtype, end, h->cfg.n_cols, planes, whole_units, replicas, stream);
+  }
+  return e;
+}
+
+int check_workspace(const dadam_handle* h, const void* workspace, uint64_t bytes, uint64_t least) {
+  if (!workspace && least) return fail(h, DADAM_EINVAL, "workspace is null");
+  if ((uintptr_t)workspace & 255u) return fail(h, DADAM_EALIGN, "workspace is not 256-byte aligned");
+  if (bytes < least) return fail(h, DADAM_EINVAL, "workspace has %llu bytes, %llu are needed", (unsigned long long)bytes, (unsigned long long)least);
+  return DADAM_OK;
+}
+
+uint64_t least_bytes(const dadam_handle* h, uint32_t planes) {
+  const std::vector<uint64_t>& need = h->matrices->need[planes - 1];
+  return need.size() < 2 ? 0 : *std::max_element(need.begin(), need.end() - 1);
+}
+
+int run(dadam_handle* h, const Call& call, void* stream) {
+  Powers pw;
+  (void)find_powers(h->matrices->coefficients, &pw);
+  const std::vector<uint64_t>& need = h->matrices->need[planes_of(call.dtype) - 1];
+  const uint32_t n = (uint32_t)h->matrices->tasks.size(), R = h->cfg.n_rows;
+  DeviceGuard guard(h->cfg.device);
+  if (guard.err != hipSuccess) return fail(h, DADAM_EHIP, "hipSetDevice: %s", hipGetErrorString(guard.err));
+  int e = (int)hipSuccess;
+  for (uint32_t k = 0; k < n && !e;) {
+    uint32_t end = k;
+    uint64_t bytes = 0;
+    while (end < n && (bytes + need[end]) * R <= call.bytes) bytes += need[end++];
+    if (end > k) {
+      e = run_group(h, call, pw, k, end, 0, R, stream);
+    } else {  // one matrix, as many replicas as there is room for
+      end = k + 1;
+      const uint32_t each = (uint32_t)std::min<uint64_t>(R, call.bytes / need[k]);
+      for (uint32_t i = 0; i < R && !e; i += each) e = run_group(h, call, pw, k, end, i, std::min(each, R - i), stream);
+    }
+    k = end;
+  }
+  if (e != (int)hipSuccess) return fail(h, DADAM_EHIP, "kernel launch failed: %s", hipGetErrorString((hipError_t)e));
+  return DADAM_OK;
+}
+
+int check_set(const dadam_handle* h) {
+  if (!h->matrices || h->matrices->need[0].empty()) return fail(h, DADAM_ESTATE, "no matrices: call dadam_set_matrices first");
+  return DADAM_OK;
+}
+
+}  // namespace
+}  // namespace dadam
+
+extern "C" {
+
+int dadam_set_matrices(dadam_handle* h, const dadam_matrix_desc* matrices, uint32_t n) {
+  if (!h) return DADAM_EINVAL;
+  if (!matrices && n) return fail(h, DADAM_EINVAL, "matrices is null");
+  if (n > kMostMatrices) return fail(h, DADAM_EINVAL, "more than %u matrices", kMostMatrices);
+  return guarded(h, [&] { return set_matrices(h, matrices, n); });
+}
+
+int dadam_set_ortho_schedule(dadam_handle* h, uint32_t n_steps, const float* coefficients) {
+  if (!h) return DADAM_EINVAL;
+  if (!coefficients) return fail(h, DADAM_EINVAL, "coefficients is null");
+  if (n_steps < 1 || n_steps > DADAM_ORTHO_MAX_STEPS) return fail(h, DADAM_EINVAL, "1 to %u iterations", DADAM_ORTHO_MAX_STEPS);
+  return guarded(h, [&] {
+    const std::vector<float> c(coefficients, coefficients + 3 * n_steps);
+    for (float v : c)
+      if (!std::isfinite(v)) return fail(h, DADAM_EINVAL, "coefficients must be finite");
+    Powers pw;
+    if (!find_powers(c, &pw)) return fail(h, DADAM_EINVAL, "singular values of up to 1 leave the iteration above %g", kLargestNorm);
+    state_of(h)->coefficients = c;
+    return DADAM_OK;
+  });
+}
+
+int dadam_ortho_get_info(const dadam_handle* h, dadam_ortho_info* out) {
+  if (!h) return DADAM_EINVAL;
+  if (!out) return fail(h, DADAM_EINVAL, "out is null");
+  if (const int rc = check_set(h)) return rc;
+  // the same for both entry points: a step goes by the parameters' type, the operator by the gradients'
+  const uint32_t planes = std::max(planes_of(h->cfg.param_dtype), planes_of(h->cfg.grad_dtype));
+  out->n_matrices = (uint32_t)h->matrices->tasks.size();
+  out->reserved = 0;
+  out->least_bytes = least_bytes(h, planes);
+  out->bytes = std::max(out->least_bytes, std::min(h->matrices->need[planes - 1].back() * h->cfg.n_rows, kOrthoWorkspace));
+  return DADAM_OK;
+}
+
+int dadam_orthogonalize(dadam_handle* h, const void* const* in, void* const* out, void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+  if (!h) return DADAM_EINVAL;
+  if (!in || !out) return fail(h, DADAM_EINVAL, "in or out is null");
+  return guarded(h, [&] {
+    int rc = check_set(h);
+    if (rc) return rc;
+    const uint32_t R = h->cfg.n_rows, dt = h->cfg.grad_dtype;
+    const size_t gb = (size_t)h->cfg.d * dtype_bytes(dt);
+    rc = check_workspace(h, workspace, workspace_bytes, least_bytes(h, planes_of(dt)));
+    const void* const one[1] = {workspace};
+    const Table tables[3] = {{in, R, gb, "in", false, -1}, {out, R, gb, "out", true, 0}, {one, workspace ? 1u : 0u, (size_t)workspace_bytes, "workspace", true, -1}};
+    if (!rc) rc = check_tables(h, tables, 3);
+    if (!rc) rc = check_device(h);
+    if (rc) return rc;
+    Call call{};
+    call.grads = in, call.out = out, call.source = kOrthoGiven, call.phase = kUpdateOnly;
+    call.dtype = dt, call.workspace = (char*)workspace, call.bytes = workspace_bytes;
+    return run(h, call, hip_stream);
+  });
+}
+
+int dadam_ortho_step(dadam_handle* h, uint32_t slot, const void* const* grads, uint64_t t, uint32_t flags, void* workspace, uint64_t workspace_bytes,
+                     void* hip_stream) {
+  if (!h) return DADAM_EINVAL;
+  if (flags & ~(DADAM_FUSE_ACCUM | DADAM_ORTHO_NESTEROV)) return fail(h, DADAM_EINVAL, "unknown flag bits 0x%x", flags);
+  return guarded(h, [&] {
+    Call call{};
+    int rc = prepare_step(h, slot, grads, t, (flags & DADAM_FUSE_ACCUM) != 0, &call.phase, &call.c);
+    if (!rc) rc = check_set(h);
+    if (!rc) rc = check_workspace(h, workspace, workspace_bytes, least_bytes(h, planes_of(h->cfg.param_dtype)));
+    if (rc) return rc;
+    const uint32_t R = h->cfg.n_rows, C = h->cfg.n_cols;
+    const size_t gb = (size_t)h->cfg.d * dtype_bytes(h->cfg.grad_dtype), xb = (size_t)h->cfg.d * dtype_bytes(h->cfg.param_dtype), sb = (size_t)h->cfg.d * 4;
+    const uintptr_t lo = (uintptr_t)workspace, hi = lo + workspace_bytes;
+    auto meets = [&](const void* p, size_t bytes) { return p && (uintptr_t)p < hi && lo < (uintptr_t)p + bytes; };
+    for (uint32_t i = 0; i < R && !rc; ++i)
+      if (meets(grads[i], gb) || meets(h->x_dst[i], xb) || meets(h->m_hat[i], sb) || meets(h->acc[i], sb)) rc = fail(h, DADAM_EALIAS, "workspace overlaps a buffer of row %u", i);
+    for (uint32_t c = 0; c < C && !rc; ++c)
+      if (meets(h->x_src[c], xb)) rc = fail(h, DADAM_EALIAS, "workspace overlaps x_src[%u]", c);
+    if (!rc) rc = check_device(h);
+    if (rc) return rc;
+    call.grads = grads, call.out = h->x_dst, call.source = flags & DADAM_ORTHO_NESTEROV ? kOrthoNesterov : kOrthoMoment;
+    call.mix = true, call.slot = slot, call.dtype = h->cfg.param_dtype, call.workspace = (char*)workspace, call.bytes = workspace_bytes;
+    return run(h, call, hip_stream);
+  });
+}
+
+}  // extern "C"

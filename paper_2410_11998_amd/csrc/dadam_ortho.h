@@ -1,0 +1,99 @@
+// Internal interface between the host side of orthogonalised updates (dadam_ortho.cpp) and their kernels (dadam_ortho.hip).
+#ifndef DADAM_ORTHO_H_
+#define DADAM_ORTHO_H_
+
+#include <stdint.h>
+
+#include "dadam_internal.h"
+
+namespace dadam {
+
+constexpr uint32_t kOrthoPad = 128;  // rows and columns of operands are filled up to a multiple of this
+
+// One matrix, the same for every replica.  X has p rows and q >= p columns: the matrix itself, or its transpose where it is tall.
+struct OrthoTask {
+  uint64_t first;        // its first element in the packed vector
+  uint64_t at;           // bytes of workspace of the matrices before it, for one replica
+  uint32_t ld;           // elements from row to row
+  uint32_t p, q, P, Q;   // P, Q: filled up
+  uint32_t tall;
+  uint32_t gram_units, whole_units;  // tiles of the matrices before it: of the lower half of P x P, and of P x Q
+  float scale, decay;
+};
+
+// Workspace of a matrix, one replica: X, twice its transpose (with what one half leaves of it behind, see k_ortho_next), A = X X^T,
+// B = b A + c A A, partial sums of the norm.
+struct OrthoPlaces {
+  uint64_t x, turned[2], a, b, sums, bytes;
+};
+inline constexpr OrthoPlaces ortho_places(uint64_t P, uint64_t Q, uint64_t planes) {
+  OrthoPlaces w{};
+  uint64_t at = 0;
+  w.x = at, at += P * Q * 2 * planes;
+  w.turned[0] = at, at += P * Q * 4;
+  w.turned[1] = at, at += P * Q * 4;
+  w.a = at, at += P * P * 2 * planes;
+  w.b = at, at += P * P * 2 * planes;
+  w.sums = at, at += ((P / kOrthoPad) * (Q / kOrthoPad) * 8 + 255) / 256 * 256;
+  w.bytes = at;
+  return w;
+}
+
+// What all launches of a group of matrices have in common.
+struct OrthoSpan {
+  const OrthoTask* tasks;   // device, of all matrices
+  const uint32_t* units;    // device: the matrix of every tile, of this launch's kind
+  uint64_t workspace, stride;  // of the group's first matrix and replica, and from replica to replica
+  uint64_t before;          // OrthoTask::at of the group's first matrix
+  uint32_t first_unit;      // tiles before the group
+  uint32_t n_xcd;
+};
+
+enum OrthoSource : int { kOrthoGiven = 0, kOrthoMoment = 1, kOrthoNesterov = 2 };
+
+template <int N>
+struct OrthoBeginArgs {
+  OrthoSpan s;
+  const void* grad[N];   // by replica of the group
+  float* m_hat[N];
+  float* acc[N];
+  Scalars c;
+  float scale;           // power of two that X is held times
+  uint32_t source;       // OrthoSource
+  uint32_t phase;        // Phase
+};
+
+struct OrthoStepArgs {
+  OrthoSpan s;
+  float gain, fresh;     // what is stored of the term held already, and of the new product
+  uint32_t from, to;     // which of the turned copies is read and written
+};
+
+template <int N>
+struct OrthoEndArgs {
+  OrthoSpan s;
+  float gain, fresh;
+  uint32_t from;
+  uint32_t mix;          // 0: out = the matrix, 1: the step
+  void* out[N];          // by replica of the group
+  const void* x_src[N];
+  const int32_t* row_ptr;  // of the slot (device)
+  const int32_t* col;
+  const float* w;
+  uint32_t first_row;
+  float lr;
+};
+
+constexpr int kOrthoFew = 16;
+static_assert(sizeof(OrthoBeginArgs<kMaxRows>) <= 4096 && sizeof(OrthoEndArgs<kMaxRows>) <= 4096, "the argument block of a launch holds 4 KB");
+
+// Launchers.  units: tiles of the group, replicas: of the group.  planes: 1 or 2 (see dadam_mfma.h).
+int launch_ortho_norm(int gdt, const OrthoBeginArgs<kMaxRows>& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream);
+int launch_ortho_begin(int gdt, const OrthoBeginArgs<kMaxRows>& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream);
+int launch_ortho_gram(bool square, const OrthoStepArgs& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream);
+int launch_ortho_next(const OrthoStepArgs& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream);
+int launch_ortho_end(int dtype, const OrthoEndArgs<kMaxRows>& a, uint32_t n_cols, uint32_t planes, uint32_t units, uint32_t replicas, void* stream);
+
+}  // namespace dadam
+
+#endif  // DADAM_ORTHO_H_

@@ -1,0 +1,310 @@
+"""Orthogonalised updates on the GPU, through the C ABI, against their statement in 64 bits (oracle/ends_oracle.py, which also derives how far the
+products' roundings may take the result: orthogonalised_error).  EPS is half a step of float32, HALF of a result's type."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import ends_oracle as O
+from paper_2410_11998_amd import binding as B
+from paper_2410_11998_amd import workloads as WL
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+EPS = 2.0 ** -24
+TYPES = {"f32": (B.DADAM_F32, torch.float32, 2.0 ** -24, 2), "bf16": (B.DADAM_BF16, torch.bfloat16, 2.0 ** -8, 1)}
+SENTINEL = 7.0
+
+
+def pack(shapes, gap=0):
+    """(offsets, sizes, d, matrices) of tensors of the given shapes; a fourth entry of a shape is the number of matrices side by side."""
+    offsets, sizes, matrices, at = [], [], [], 3 if gap else 0
+    for k, s in enumerate(shapes):
+        r, c = s[:2]
+        parts = s[2] if len(s) > 2 else 1
+        offsets.append(at)
+        sizes.append(r * c)
+        matrices += [(k, r, c // parts, c, p * (c // parts), 0.5 + 0.25 * (k % 3)) for p in range(parts)]
+        at += r * c + gap
+    return offsets, sizes, -(-(at + gap) // 8) * 8, matrices
+
+
+def view(vector, offsets, m):
+    k, r, c, ld, first = m[:5]
+    at = offsets[k] + first
+    return np.lib.stride_tricks.as_strided(vector[at:], (r, c), (vector.strides[0] * ld, vector.strides[0]))
+
+
+class Layout:
+    def __init__(self, shapes, kind="f32", rows=1, cols=None, csr=None, gap=0, grad=None, device=0, **kw):
+        self.offsets, self.sizes, self.d, self.matrices = pack(shapes, gap)
+        self.kind, self.rows = kind, rows
+        self.h = B.dadam_init(rows, cols or rows, self.d, self.offsets, self.sizes, TYPES[kind][0], TYPES[grad or kind][0], device=device, **kw)
+        B.dadam_set_topology(self.h, 0, *(csr or WL.identity(rows)))
+        B.dadam_set_matrices(self.h, self.matrices)
+        self.info = B.dadam_ortho_get_info(self.h)
+
+    def workspace(self, n_bytes=None, device=DEV):
+        w = torch.empty(self.info.bytes if n_bytes is None else n_bytes, dtype=torch.uint8, device=device)
+        w.fill_(0xFF)                                    # NaN, whatever it is read as
+        return w
+
+    def mask(self):
+        m = np.zeros(self.d, dtype=bool)
+        for x in self.matrices:
+            view(m, self.offsets, x)[:] = True
+        return m
+
+    def random(self, seed, rows=None, std=1e-2):
+        """Decaying singular values under noise; NaN outside the matrices."""
+        rng = np.random.default_rng(seed)
+        out = np.full((rows or self.rows, self.d), np.nan, dtype=np.float32)
+        for v in out:
+            for x in self.matrices:
+                r, c = x[1:3]
+                k = max(1, min(r, c) // 4)
+                strong = rng.standard_normal((r, k)) * 2.0 ** -(np.arange(k) * 6.0 / k) @ rng.standard_normal((k, c))
+                view(v, self.offsets, x)[:] = std * (strong / np.sqrt(k) + 0.2 * rng.standard_normal((r, c)))
+        return out
+
+    def close(self):
+        B.dadam_destroy(self.h)
+
+
+def on_device(a, kind, device=DEV):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(device).to(TYPES[kind][1])
+
+
+def host(t):
+    return t.float().cpu().numpy()
+
+
+def check_orthogonal(L, given, got, kind):
+    """given: what the device had, got: what it made of it."""
+    _, _, half, planes = TYPES[kind]
+    mask = L.mask()
+    for i in range(L.rows):
+        assert (got[i][~mask] == SENTINEL).all(), f"row {i}: elements outside the matrices were written"
+        for m in L.matrices:
+            a = view(given[i], L.offsets, m)
+            want = O.orthogonalised(a)
+            off = np.linalg.norm(view(got[i], L.offsets, m) - want)
+            may = O.orthogonalised_error(a, planes) + half * np.linalg.norm(want)
+            assert off <= may, f"row {i} matrix {m}: off by {off}, may be {may} (norm {np.linalg.norm(want)})"
+
+
+SHAPES = {
+    "one": [(1, 1)],
+    "vectors": [(1, 7), (9, 1), (1, 300)],
+    "small": [(5, 3), (3, 5), (64, 48), (48, 192)],
+    "tile": [(128, 128)],
+    "edges": [(127, 129), (129, 127), (128, 256), (257, 128)],
+    "odd": [(33, 301), (300, 129), (131, 517), (260, 259)],
+    "side by side": [(96, 288, 3), (130, 390, 3)],
+}
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("name", SHAPES)
+def test_matrices_of_every_shape(name, kind):
+    for rows, gap in ((1, 0), (3, 5)):
+        L = Layout(SHAPES[name], kind, rows=rows, gap=gap)
+        g = on_device(L.random(1 + rows), kind)
+        out = torch.full_like(g, SENTINEL)
+        B.dadam_orthogonalize(L.h, g, out, L.workspace(), B.current_stream())
+        check_orthogonal(L, host(g), host(out), kind)
+        L.close()
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_small_workspaces_and_in_place_give_the_same_bits(kind):
+    L = Layout([(140, 300), (64, 64), (300, 130), (7, 5)], kind, rows=5)
+    g = on_device(L.random(5), kind)
+    outs = []
+    least, n = L.info.least_bytes, L.info.bytes
+    for n_bytes in (n, least, 2 * least, 3 * least + 256):
+        out = torch.full_like(g, SENTINEL)
+        B.dadam_orthogonalize(L.h, g, out, L.workspace(n_bytes), B.current_stream())
+        outs.append(out)
+    same = g.clone()
+    B.dadam_orthogonalize(L.h, same, same, L.workspace(), B.current_stream())
+    mask = torch.from_numpy(L.mask()).to(DEV)
+    for o in outs[1:] + [same]:
+        assert torch.equal(o[:, mask], outs[0][:, mask])
+    check_orthogonal(L, host(g), host(outs[0]), kind)
+    L.close()
+
+
+def test_zeros_nan_and_infinity_keep_to_their_matrix():
+    L = Layout([(40, 50), (50, 40), (30, 30), (20, 140)], rows=2)
+    g = L.random(3)
+    view(g[0], L.offsets, L.matrices[0])[:] = 0
+    view(g[0], L.offsets, L.matrices[1])[3, 4] = np.nan
+    view(g[1], L.offsets, L.matrices[2])[0, 29] = np.inf
+    view(g[1], L.offsets, L.matrices[0])[:] *= 1e30          # squares beyond float32
+    view(g[1], L.offsets, L.matrices[3])[:] *= 1e-30         # and below: the norm is as nothing beside 1e-7
+    dev = on_device(g, "f32")
+    out = torch.full_like(dev, SENTINEL)
+    B.dadam_orthogonalize(L.h, dev, out, L.workspace(), B.current_stream())
+    got = host(out)
+    assert (view(got[0], L.offsets, L.matrices[0]) == 0).all()
+    assert np.isnan(view(got[0], L.offsets, L.matrices[1])).all() and np.isnan(view(got[1], L.offsets, L.matrices[2])).all()
+    for i, k in ((0, 2), (0, 3), (1, 0), (1, 1)):
+        m = L.matrices[k]
+        a = view(g[i], L.offsets, m)
+        want = O.orthogonalised(a)
+        assert np.linalg.norm(view(got[i], L.offsets, m) - want) <= O.orthogonalised_error(a, 2) + EPS * np.linalg.norm(want)
+    tiny = view(got[1], L.offsets, L.matrices[3])
+    assert np.abs(tiny).max() <= 1e-20                       # (operands hold elements down to 2^-37 of the bound)
+    L.close()
+
+
+def test_other_schedules():
+    schedules = [[(1.5, -0.5, 0.0)] * 3, [(4.0, -6.0, 2.5), (3.0, -3.2, 1.2), (1.875, -1.25, 0.375)], [(1.0, 0.0, 0.0)]]
+    L = Layout([(70, 150), (129, 60)], rows=2)
+    g = on_device(L.random(9), "f32")
+    for s in schedules:
+        s = [tuple(float(np.float32(v)) for v in abc) for abc in s]
+        B.dadam_set_ortho_schedule(L.h, s)
+        out = torch.full_like(g, SENTINEL)
+        B.dadam_orthogonalize(L.h, g, out, L.workspace(), B.current_stream())
+        for i in range(2):
+            for m in L.matrices:
+                a = view(host(g)[i], L.offsets, m)
+                want = O.orthogonalised(a, s)
+                assert np.linalg.norm(view(host(out)[i], L.offsets, m) - want) <= O.orthogonalised_error(a, 2, s) + EPS * np.linalg.norm(want)
+    L.close()
+
+
+class Step:
+    """A handle with buffers, and Algorithm 3 with the orthogonalised direction beside it in 64 bits."""
+
+    def __init__(self, L, seed, lr, beta, s, csr, cols, decay):
+        self.L, self.lr, self.beta, self.s, self.csr, self.decay = L, float(np.float32(lr)), float(np.float32(beta)), s, csr, decay
+        kind = TYPES[L.kind][1]
+        rng = np.random.default_rng(seed)
+        self.x = torch.from_numpy(rng.standard_normal((cols, L.d)).astype(np.float32) * 0.05).to(DEV).to(kind)
+        self.out = torch.full((L.rows, L.d), SENTINEL, device=DEV, dtype=kind)
+        self.m = torch.from_numpy(rng.standard_normal((L.rows, L.d)).astype(np.float32) * 1e-3).to(DEV)
+        self.v = torch.full((L.rows, L.d), SENTINEL, device=DEV)
+        self.acc = torch.full((L.rows, L.d), np.nan, device=DEV) if s > 1 else None
+
+    def bind(self, out=None):
+        B.dadam_bind(self.L.h, list(self.x), list(self.out if out is None else out), list(self.m), list(self.v), None if self.acc is None else list(self.acc))
+
+    def expected(self, g, m0, b0, x0, t, nesterov, fuse, planes):
+        """Per row and matrix: x, how far it may be off (2-norm), m_hat, b."""
+        L, be = self.L, self.beta
+        rp, col, w = self.csr
+        for i in range(L.rows):
+            for mat in L.matrices:
+                gi, mi = view(g[i], L.offsets, mat).astype(np.float64), view(m0[i], L.offsets, mat).astype(np.float64)
+                m = be * mi + (1 - be) * gi
+                u = be * m + (1 - be) * gi if nesterov else m
+                o = O.orthogonalised(u)
+                mixed = sum(float(w[k]) * view(x0[col[k]], L.offsets, mat).astype(np.float64) for k in range(rp[i], rp[i + 1]))
+                size = sum(float(w[k]) * np.abs(view(x0[col[k]], L.offsets, mat)).astype(np.float64) for k in range(rp[i], rp[i + 1]))
+                own = view(x0[i], L.offsets, mat).astype(np.float64)
+                x = mixed - self.lr * (mat[5] * o + self.decay * own)
+                # u is rounded some four times before it is orthogonalised: the largest slope of five iterations is below 3.9^5 = 900
+                n = np.linalg.norm
+                u_off = 4 * EPS * (n(np.abs(be * mi) + np.abs((1 - be) * gi))) / max(n(u), 1e-30)
+                may = self.lr * abs(mat[5]) * (O.orthogonalised_error(u, planes) + 900 * u_off) + (rp[i + 1] - rp[i] + 3) * EPS * n(size) + 4 * EPS * n(x - mixed) + TYPES[L.kind][2] * n(x)
+                b = None
+                if fuse:
+                    first, last = (t - 1) % self.s == 0, t % self.s == 0
+                    b = gi / self.s + (0 if first else view(b0[i], L.offsets, mat).astype(np.float64))
+                    if last:
+                        mi, b = be * mi + (1 - be) * b, np.zeros_like(b)
+                yield i, mat, x, may, mi, b
+
+
+@pytest.mark.parametrize("nesterov", [False, True])
+@pytest.mark.parametrize("kind,grad", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("topology,s", [("ring", 1), ("share", 2), ("complete", 3)])
+def test_steps(topology, s, kind, grad, nesterov):
+    rows = {"ring": 4, "share": 1, "complete": 3}[topology]
+    csr = {"ring": lambda: WL.ring(4), "share": lambda: (np.array([0, 3], np.int32), np.array([0, 2, 1], np.int32), np.array([0.5, 0.25, 0.25], np.float32)),
+           "complete": lambda: WL.complete(3)}[topology]()
+    cols = 3 if topology == "share" else rows
+    decay = 0.0 if topology == "ring" else 0.125
+    shapes = [(40, 72), (130, 65), (96, 288, 3), (1, 17)]
+    L = Layout(shapes, kind, rows=rows, cols=cols, csr=csr, gap=5, grad=grad, lr=0.02, beta1=0.9, accum_s=s, weight_decay=[decay] * len(shapes))
+    S = Step(L, 3, 0.02, 0.9, s, csr, cols, decay)
+    S.bind()
+    mask = L.mask()
+    for t in range(1, 2 * s + 1):
+        fuse = t != 2
+        g = on_device(L.random(10 + t), grad)
+        m0, x0, b0 = S.m.cpu().numpy(), host(S.x), None if S.acc is None else S.acc.cpu().numpy()
+        flags = (B.DADAM_FUSE_ACCUM if fuse else 0) | (B.DADAM_ORTHO_NESTEROV if nesterov else 0)
+        B.dadam_ortho_step(L.h, 0, g, t, flags, L.workspace(), B.current_stream())
+        x, m = host(S.out), S.m.cpu().numpy()
+        assert (x[:, ~mask] == SENTINEL).all() and np.array_equal(m[:, ~mask], m0[:, ~mask]) and bool((S.v == SENTINEL).all())
+        for i, mat, want, may, mi, b in S.expected(host(g), m0, b0, x0, t, nesterov, fuse, TYPES[kind][3]):
+            off = np.linalg.norm(view(x[i], L.offsets, mat) - want)
+            assert off <= may, f"t {t} row {i} matrix {mat}: off by {off}, may be {may}"
+            near = 6 * EPS * (np.abs(mi) + 1e-2)             # products and sums of at most 1e-1
+            assert (np.abs(view(m[i], L.offsets, mat) - mi) <= near).all()
+            if fuse and s > 1:
+                assert (np.abs(view(S.acc.cpu().numpy()[i], L.offsets, mat) - b) <= near).all()
+        if not fuse:
+            if S.acc is not None and t == 1:
+                S.acc.nan_to_num_()
+            B.dadam_accumulate(L.h, list(torch.nan_to_num(g)), t, B.current_stream())
+            S.v.fill_(SENTINEL)
+    L.close()
+
+
+def test_updates_in_place_and_their_refusal():
+    shapes = [(40, 72), (72, 40)]
+    L = Layout(shapes, rows=2, lr=0.02)
+    S = Step(L, 4, 0.02, 0.9, 1, WL.identity(2), 2, 0.0)
+    g = on_device(L.random(8), "f32")
+    S.bind()
+    m0 = S.m.clone()
+    B.dadam_ortho_step(L.h, 0, g, 1, B.DADAM_FUSE_ACCUM, L.workspace(), B.current_stream())
+    S.m.copy_(m0)
+    S.bind(out=S.x)
+    B.dadam_ortho_step(L.h, 0, g, 1, B.DADAM_FUSE_ACCUM, L.workspace(), B.current_stream())
+    mask = torch.from_numpy(L.mask()).to(DEV)
+    assert torch.equal(S.x[:, mask], S.out[:, mask])
+    B.dadam_set_topology(L.h, 1, *WL.ring(2))
+    before = S.x.clone()
+    with pytest.raises(B.DadamError) as e:
+        B.dadam_ortho_step(L.h, 1, g, 2, B.DADAM_FUSE_ACCUM, L.workspace(), B.current_stream())
+    assert e.value.code == B.DADAM_EALIAS and torch.equal(S.x, before)
+    L.close()
+
+
+def test_recorded_into_a_graph_and_on_another_stream():
+    L = Layout([(140, 64), (64, 200)], "bf16", rows=2)
+    g = on_device(L.random(2), "bf16")
+    work, out, eager = L.workspace(), torch.zeros_like(g), torch.zeros_like(g)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        B.dadam_orthogonalize(L.h, g, out, work, B.current_stream())
+    mask = torch.from_numpy(L.mask()).to(DEV)
+    for k in range(3):
+        g.copy_(on_device(L.random(20 + k), "bf16"))
+        graph.replay()
+        B.dadam_orthogonalize(L.h, g, eager, L.workspace(), B.current_stream())
+        torch.cuda.synchronize()
+        assert torch.equal(out[:, mask], eager[:, mask]) and bool((out[:, mask] != 0).any())
+    L.close()
+
+
+def test_more_replicas_than_a_short_argument_block_names():
+    L = Layout([(20, 30), (150, 40)], rows=70, csr=WL.ring(70), lr=0.02)
+    S = Step(L, 6, 0.02, 0.9, 1, WL.ring(70), 70, 0.0)
+    S.bind()
+    g = on_device(L.random(5), "f32")
+    m0, x0 = S.m.cpu().numpy(), host(S.x)
+    B.dadam_ortho_step(L.h, 0, g, 1, B.DADAM_FUSE_ACCUM, L.workspace(), B.current_stream())
+    x = host(S.out)
+    for i, mat, want, may, _, _ in S.expected(host(g), m0, None, x0, 1, False, True, 2):
+        assert np.linalg.norm(view(x[i], L.offsets, mat) - want) <= may
+    L.close()
