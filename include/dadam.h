@@ -506,6 +506,40 @@ int dadam_mx4_round(dadam_handle* h, uint32_t slot, const void* const* x_src, vo
  * results up to the order of sums.  What a call writes must not overlap anything else that it reads or writes, but where "in place" is named.
  * Errors of all: DADAM_EINVAL (null, value out of range, workspace too small), DADAM_EALIGN, DADAM_EALIAS, DADAM_ESTATE, DADAM_EHIP. */
 
+/* The output matrix of a language model: tensor `tensor` of the layout, vocab rows (one a word) of width elements, and the words' bias, a tensor of vocab
+ * elements, or DADAM_HEAD_NO_BIAS.  vocab is 1 to 2^24, width 1 to 65536. */
+#define DADAM_HEAD_NO_BIAS 0xffffffffu
+typedef struct {
+  uint32_t tensor, bias_tensor;
+  uint32_t vocab, width;
+} dadam_head;
+
+typedef struct {
+  uint64_t least_bytes; /* the workspace without which a call is refused: one replica at a time, 128 words at a time */
+  uint64_t bytes;       /* what a call makes good use of */
+} dadam_head_info;
+/* The workspace of dadam_head_loss for n_tokens tokens a row, with (gradient != 0) or without gradients. */
+int dadam_head_get_info(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, uint32_t gradient, dadam_head_info* out);
+
+/* Softmax cross entropy of every row's hidden vectors against its own head, in pieces of the vocabulary, without keeping the logits: with W and bias in
+ * params[i], h_t the t-th of hidden[i]'s n_tokens vectors of width elements, y_t = targets[i][t]
+ *     z = W h_t + bias;    nll[i][t] = log sum_v exp z[v] - z[y_t];    losses[i] = s * sum_t nll[i][t]
+ *     dz_t = s (softmax z - e[y_t]);    dhidden[i][t] = W^T dz_t;    in grads[i]: dW = sum_t dz_t h_t^T, dbias = sum_t dz_t
+ * s is scale, with DADAM_HEAD_MEAN divided by the number of row i's tokens that have a target.  A token whose target is negative or vocab and above has none: it takes no
+ * part (nll 0, dhidden 0), whatever its hidden vector holds.  With DADAM_HEAD_ADD dW and dbias are added to what grads holds (a head that
+ * is the embedding too, or gradients of several calls), otherwise written; other elements of grads are not touched.
+ * params: n_rows packed vectors of param_dtype; hidden and dhidden: n_rows times n_tokens x width of param_dtype; targets: int32; losses (n_rows, DEVICE) and nll: float32;
+ * grads: n_rows packed vectors of grad_dtype.  nll, dhidden and grads may be null; without the last two only the loss is formed.  Of all these only params and grads
+ * have to be 16-byte aligned, the others by their elements.  n_tokens is 0 to 2^20.
+ * Sums are float32 (the loss 64 bits).  With bfloat16 parameters and gradients softmax - e[y] is rounded to bfloat16 before the gradients' products; otherwise
+ * operands have 22 bits, or 2^-39 of the largest magnitude of the head, of the hidden vectors or (softmax) of 1.  An infinity or NaN in W, or in a hidden vector that
+ * takes part, makes its replica's loss and gradients NaN; a bias of minus infinity takes its word out. */
+#define DADAM_HEAD_MEAN 1u
+#define DADAM_HEAD_ADD 2u
+int dadam_head_loss(dadam_handle* h, const dadam_head* head, const void* const* params, const void* const* hidden,
+                    const int32_t* const* targets, uint32_t n_tokens, float scale, uint32_t flags, float* losses, float* const* nll,
+                    void* const* dhidden, void* const* grads, void* workspace, uint64_t workspace_bytes, void* hip_stream);
+
 /* A matrix of the packed layout: element (r, c) is element first + r * ld + c of the tensor.  Several may share a tensor (projections that are
  * fused side by side) but no element, and columns do not run on into the next row: first % ld + cols <= ld.  scale multiplies the orthogonalised direction
  * (for instance sqrt(max(1, rows / cols)), or 0.2 sqrt(max(rows, cols)) for updates of Adam's size).  flags must be 0. */

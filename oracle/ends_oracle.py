@@ -43,3 +43,52 @@ def orthogonalised_error(m, planes, schedule=SCHEDULE):
         e = slope * (e + u2 * f(x)) + top * db + f(B, 2) * u1 * f(x) + sums(len(g)) * f(np.abs(B) @ np.abs(x)) + 2.0 ** -23 * f(a * x)
         x = a * x + B @ x
     return e + 2.0 ** -22 * f(x)
+
+
+def head_loss(hidden, head, bias, targets, scale=1.0, mean=True):
+    """{"loss", "nll", "dz", "dhidden", "dhead", "dbias"} of one replica; tokens without a target take no part."""
+    with np.errstate(invalid="ignore", over="ignore"):
+        w, y = np.asarray(head, dtype=np.float64), np.asarray(targets)
+        taken = (y >= 0) & (y < len(w))
+        h = np.where(taken[:, None], np.asarray(hidden, dtype=np.float64), 0.0)
+        z = h @ w.T + (0 if bias is None else np.asarray(bias, dtype=np.float64))
+        top = z.max(axis=1, keepdims=True) if len(z) else z
+        lse = (top + np.log(np.exp(z - top).sum(axis=1, keepdims=True)))[:, 0] if len(z) else np.zeros(0)
+        s = scale / (max(1, int(taken.sum())) if mean else 1)
+        word = np.where(taken, y, 0)
+        nll = np.where(taken, lse - z[np.arange(len(y)), word], 0.0)
+        dz = np.exp(z - lse[:, None])
+        dz[np.arange(len(y)), word] -= 1
+        dz = np.where(taken[:, None], dz, 0.0)
+        return {"loss": s * nll.sum(), "nll": nll, "dz": dz, "s": s, "z": z, "h": h, "dhidden": s * dz @ w, "dhead": s * dz.T @ h, "dbias": s * dz.sum(axis=0)}
+
+
+def head_loss_error(r, head, bias, planes, half):
+    """Bounds, element by element, of what the library's roundings make of head_loss's results r.  half: half a step of the results' type.
+
+    Logits: operands of 2^-22 a plane pair (of one bfloat16 plane: as given), a sum of K products in float32 off by four times sqrt(K) roundings of 2^-24.
+    softmax: twice a logit's error, an exponential good to 2^-21 and to 2^-23 of its argument; held to 2^-22 and 2^-38 of 1, or to 2^-8.
+    What is below 2^-126, float32's (and bfloat16's) smallest normal number, may come out as 0: an exponential of -100 is 2^-144, off by all of itself."""
+    w = np.abs(np.asarray(head, dtype=np.float64))
+    h, z, s = np.abs(r["h"]), r["z"], abs(r["s"])
+    sums = lambda k: 4 * np.sqrt(max(1, k)) * 2.0 ** -24  # noqa: E731
+    operand = 2.0 ** -21 if planes == 2 else 0.0
+    dlogit = (operand + sums(w.shape[1])) * (h @ w.T) + 2.0 ** -38 * planes * (h.sum(1)[:, None] * w.max(initial=0) + w.sum(1)[None] * h.max(initial=0))
+    if bias is not None:
+        dlogit = dlogit + 2.0 ** -23 * np.abs(np.where(np.isfinite(z), z, 0))
+    worst = dlogit.max(axis=1) if len(z) else np.zeros(0)
+    taken = (r["dz"] != 0).any(axis=1)
+    finite = np.where(np.isfinite(z), np.abs(z), 0)
+    nll = np.where(taken | (r["nll"] != 0), 2 * worst + 2.0 ** -20 + 2.0 ** -22 * (finite.max(axis=1) if len(z) else 0) + 2.0 ** -22 * np.abs(r["nll"]), 0.0)
+    dz = np.abs(r["dz"])
+    p = np.where(r["dz"] < 0, 1 + r["dz"], r["dz"])
+    relative = 2 * worst[:, None] + 2.0 ** -20 + 2.0 ** -22 * finite
+    held = (2.0 ** -22 * dz + 2.0 ** -38) if planes == 2 else 2.0 ** -8 * dz
+    ddz = np.where(taken[:, None], relative * (p + dz) + held + 2.0 ** -126, 0.0)
+    k, t = w.shape[0], len(z)
+    lost = 2.0 ** -126
+    tiny = 2.0 ** -38 * planes
+    return {"nll": nll, "loss": s * nll.sum() + 2.0 ** -23 * abs(r["loss"]),
+            "dhidden": s * (ddz @ w + (operand + sums(k) + 2.0 ** -22) * (dz @ w) + tiny * dz.sum(1)[:, None] * w.max(initial=0)) + half * np.abs(r["dhidden"]) + lost,
+            "dhead": s * (ddz.T @ h + (operand + sums(t) + 2.0 ** -22) * (dz.T @ h) + tiny * dz.sum(0)[:, None] * h.max(initial=0)) + half * np.abs(r["dhead"]) + lost,
+            "dbias": s * (ddz.sum(axis=0) + (sums(t) + 2.0 ** -22) * dz.sum(axis=0)) + half * np.abs(r["dbias"]) + lost}

@@ -32,6 +32,7 @@ DADAM_FUSE_ACCUM, DADAM_FORCE_DIRECT, DADAM_FORCE_TILE = 1, 2, 4
 DADAM_WARN_NOT_COLUMN_STOCHASTIC = 1
 DADAM_MX4_BLOCK, DADAM_MX4_ADD = 32, 1
 DADAM_ORTHO_MAX_STEPS, DADAM_ORTHO_NESTEROV = 16, 8
+DADAM_HEAD_NO_BIAS, DADAM_HEAD_MEAN, DADAM_HEAD_ADD = 0xffffffff, 1, 2
 DADAM_PLACE_TWO_REGIONS, DADAM_PLACE_ARENA_ELSEWHERE, DADAM_PLACE_TOO_LARGE = 1, 2, 4
 
 EXPORTS = [
@@ -41,6 +42,7 @@ EXPORTS = [
     "dadam_place_by_timing",
     "dadam_grad_norm", "dadam_clip_grads", "dadam_mx4_get_info", "dadam_mx4_encode", "dadam_mx4_product", "dadam_mx4_gossip", "dadam_mx4_round",
     "dadam_set_matrices", "dadam_set_ortho_schedule", "dadam_ortho_get_info", "dadam_orthogonalize", "dadam_ortho_step",
+    "dadam_head_get_info", "dadam_head_loss",
     "dadam_last_error",
     "dadam_destroy",
 ]
@@ -86,6 +88,14 @@ class dadam_matrix_desc(C.Structure):
 
 class dadam_ortho_info(C.Structure):
     _fields_ = [("n_matrices", C.c_uint32), ("reserved", C.c_uint32), ("least_bytes", C.c_uint64), ("bytes", C.c_uint64)]
+
+
+class dadam_head(C.Structure):
+    _fields_ = [("tensor", C.c_uint32), ("bias_tensor", C.c_uint32), ("vocab", C.c_uint32), ("width", C.c_uint32)]
+
+
+class dadam_head_info(C.Structure):
+    _fields_ = [("least_bytes", C.c_uint64), ("bytes", C.c_uint64)]
 
 
 PROBE_CHUNK_BYTES, PROBE_STEP_BYTES, MAX_STRETCHES = 1 << 30, 4 << 30, 6
@@ -148,6 +158,8 @@ def _load() -> C.CDLL:
     lib.dadam_ortho_get_info.argtypes = [H, C.POINTER(dadam_ortho_info)]
     lib.dadam_orthogonalize.argtypes = [H, P, P, C.c_void_p, C.c_uint64, C.c_void_p]
     lib.dadam_ortho_step.argtypes = [H, C.c_uint32, P, C.c_uint64, C.c_uint32, C.c_void_p, C.c_uint64, C.c_void_p]
+    lib.dadam_head_get_info.argtypes = [H, C.POINTER(dadam_head), C.c_uint32, C.c_uint32, C.POINTER(dadam_head_info)]
+    lib.dadam_head_loss.argtypes = [H, C.POINTER(dadam_head), P, P, P, C.c_uint32, C.c_float, C.c_uint32, C.c_void_p, P, P, P, C.c_void_p, C.c_uint64, C.c_void_p]
     lib.dadam_last_error.argtypes = [H]
     lib.dadam_last_error.restype = C.c_char_p
     lib.dadam_destroy.argtypes = [H]
@@ -468,9 +480,9 @@ def _row_values(norms, rows: int, on_device: bool) -> int:
     if isinstance(norms, int):
         return norms
     if norms.numel() < rows or norms.element_size() != 4 or not norms.is_contiguous():
-        raise ValueError("norms must hold one float32 a row")
+        raise ValueError("the values of the rows: one float32 each is needed")
     if on_device and not norms.is_cuda:
-        raise ValueError("norms is not on a GPU")
+        raise ValueError("the values of the rows are not on a GPU")
     return norms.data_ptr()
 
 
@@ -576,6 +588,24 @@ def dadam_ortho_step(h, slot: int, grads, t: int, flags: int, workspace, stream:
     d, _, gb, rows, _, gpu = _shape(h)
     g = pointer_table(grads, rows, d, gb, "grads", gpu)
     _check(h, lib.dadam_ortho_step(h, slot, _at(g), t, flags, *_workspace(workspace, gpu), stream))
+
+
+def dadam_head_get_info(h, head, n_tokens: int, gradient) -> dadam_head_info:
+    info = dadam_head_info()
+    _check(h, lib.dadam_head_get_info(h, C.byref(head), int(n_tokens), 1 if gradient else 0, C.byref(info)))
+    return info
+
+
+def dadam_head_loss(h, head, params, hidden, targets, n_tokens: int, scale: float, flags: int, losses, nll, dhidden, grads, workspace, stream: int = 0) -> None:
+    """hidden and dhidden: a buffer of n_tokens * width elements a row; targets (int32) and nll: n_tokens; losses: a device tensor of n_rows float32 (or an integer
+    device address); nll, dhidden and grads may be None; workspace: a device tensor of dadam_head_get_info(...).bytes bytes (or (address, bytes))."""
+    d, pb, gb, rows, _, gpu = _shape(h)
+    n = int(n_tokens) * head.width
+    x, v = pointer_table(params, rows, d, pb, "params", gpu), pointer_table(hidden, rows, n, pb, "hidden", gpu)
+    y, l = pointer_table(targets, rows, int(n_tokens), 4, "targets", gpu), pointer_table(nll, rows, int(n_tokens), 4, "nll", gpu)
+    dv, g = pointer_table(dhidden, rows, n, pb, "dhidden", gpu), pointer_table(grads, rows, d, gb, "grads", gpu)
+    _check(h, lib.dadam_head_loss(h, C.byref(head), _at(x), _at(v), _at(y), int(n_tokens), scale, flags, _row_values(losses, rows, gpu), _at(l), _at(dv), _at(g),
+                                  *_workspace(workspace, gpu), stream))
 
 
 def dadam_destroy(h) -> None:

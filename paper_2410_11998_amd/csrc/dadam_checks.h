@@ -31,6 +31,7 @@ struct Table {
   const char* name;
   bool written;
   int in_place_of;  // the table whose entry of the same number this one's may be, -1 none
+  uint32_t align = 16;
 };
 
 struct Range {
@@ -76,7 +77,7 @@ inline int check_tables(const dadam_handle* h, const Table* t, int n_tables) {
     for (uint32_t i = 0; i < t[k].n; ++i) {
       const uintptr_t at = (uintptr_t)t[k].p[i];
       if (!at) return fail(h, DADAM_EINVAL, "%s[%u] is null", t[k].name, i);
-      if (at & 15u) return fail(h, DADAM_EALIGN, "%s[%u] is not 16-byte aligned", t[k].name, i);
+      if (at & (t[k].align - 1)) return fail(h, DADAM_EALIGN, "%s[%u] is not %u-byte aligned", t[k].name, i, t[k].align);
       if (at >= kHighest || t[k].bytes > kHighest - at) return fail(h, DADAM_EINVAL, "%s[%u] reaches above address 2^52", t[k].name, i);
       apart &= at >= end;
       end = at + t[k].bytes;

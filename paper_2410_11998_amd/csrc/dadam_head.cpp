@@ -1,0 +1,213 @@
+// Host side of a head's loss (include/dadam.h, "The ends of an iteration"): validation, how the vocabulary and the replicas go in pieces, and the launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "dadam_checks.h"
+#include "dadam_handle.h"
+#include "dadam_head.h"
+
+namespace dadam {
+namespace {
+
+constexpr uint32_t kMostWords = 1u << 24, kMostWidth = 65536, kMostTokens = 1u << 20;
+
+uint32_t filled(uint32_t n, uint32_t each) { return std::max((n + each - 1) / each, 1u) * each; }
+
+uint32_t planes_of(const dadam_handle* h) { return h->cfg.param_dtype == DADAM_BF16 && h->cfg.grad_dtype == DADAM_BF16 ? 1 : 2; }
+
+int check_head(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens) {
+  if (!head) return fail(h, DADAM_EINVAL, "head is null");
+  if (!head->vocab || head->vocab > kMostWords) return fail(h, DADAM_EINVAL, "vocab must be 1 to %u", kMostWords);
+  if (!head->width || head->width > kMostWidth) return fail(h, DADAM_EINVAL, "width must be 1 to %u", kMostWidth);
+  if (n_tokens > kMostTokens) return fail(h, DADAM_EINVAL, "n_tokens must be at most %u", kMostTokens);
+  if (head->tensor >= h->tensors.size()) return fail(h, DADAM_EINVAL, "the head's tensor %u is out of range", head->tensor);
+  if (h->tensors[head->tensor].numel != (uint64_t)head->vocab * head->width) return fail(h, DADAM_EINVAL, "the head's tensor does not have vocab x width elements");
+  if (head->bias_tensor == DADAM_HEAD_NO_BIAS) return DADAM_OK;
+  if (head->bias_tensor >= h->tensors.size()) return fail(h, DADAM_EINVAL, "the bias's tensor %u is out of range", head->bias_tensor);
+  if (h->tensors[head->bias_tensor].numel != head->vocab) return fail(h, DADAM_EINVAL, "the bias's tensor does not have vocab elements");
+  return DADAM_OK;
+}
+
+// How a call goes: words of a piece, replicas of a launch, parts of the sums over words.
+constexpr uint32_t kGoodTiles = 2048;     // eight a compute unit
+constexpr uint32_t kGoodWords = 8192;     // of a piece at least, so that the product over tokens fills the chip
+constexpr uint32_t kGoodSums = 512;
+struct Way {
+  HeadShape s;
+  uint32_t rows;
+  uint64_t each;  // workspace of a replica
+};
+
+void fill_shape(const dadam_head* head, uint32_t n_tokens, uint32_t planes, uint32_t rows, uint32_t piece, HeadShape* s) {
+  s->tokens = n_tokens;
+  s->vocab = head->vocab;
+  s->width = head->width;
+  s->T = filled(n_tokens, kHeadTile);
+  s->D = filled(head->width, kHeadTile);
+  s->K = filled(head->width, 64);
+  const uint32_t pieces = (head->vocab + piece - 1) / piece;
+  s->piece = filled((head->vocab + pieces - 1) / pieces, kHeadTile);
+  s->slices = filled(head->vocab, kHeadTile) / kHeadSlice;
+  const uint64_t tiles = (uint64_t)(s->T / kHeadTile) * (s->D / kHeadTile) * rows, stages = (uint64_t)s->piece * planes / 64;
+  s->splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(std::min<uint64_t>((kGoodSums + tiles - 1) / tiles, stages / 8), kHeadSplits));
+}
+
+Way good_way(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, bool gradient) {
+  Way w{};
+  const uint32_t planes = planes_of(h), T = filled(n_tokens, kHeadTile) / kHeadTile, V = filled(head->vocab, kHeadTile) / kHeadTile;
+  const uint32_t piece = std::min(V, std::max(kGoodTiles / T, kGoodWords / kHeadTile));
+  w.rows = std::min<uint32_t>(std::min<uint32_t>(h->cfg.n_rows, kHeadRows), std::max(1u, kGoodTiles / (piece * T)));
+  fill_shape(head, n_tokens, planes, w.rows, piece * kHeadTile, &w.s);
+  w.each = head_places(w.s, planes, gradient).bytes;
+  return w;
+}
+
+Way least_way(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, bool gradient) {
+  Way w{};
+  w.rows = 1;
+  fill_shape(head, n_tokens, planes_of(h), 1, kHeadTile, &w.s);
+  w.each = head_places(w.s, planes_of(h), gradient).bytes;
+  return w;
+}
+
+// The good way, with fewer replicas at a time or smaller pieces where the workspace asks for it.
+Way way_for(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, bool gradient, uint64_t bytes) {
+  Way w = good_way(h, head, n_tokens, gradient);
+  if (w.each <= bytes) {
+    w.rows = (uint32_t)std::min<uint64_t>(w.rows, bytes / w.each);
+    return w;
+  }
+  w.rows = 1;
+  uint32_t low = 1, high = w.s.piece / kHeadTile;  // tiles of a piece: what fits, and what does not
+  while (low + 1 < high) {
+    const uint32_t middle = (low + high) / 2;
+    fill_shape(head, n_tokens, planes_of(h), 1, middle * kHeadTile, &w.s);
+    (head_places(w.s, planes_of(h), gradient).bytes <= bytes ? low : high) = middle;
+  }
+  fill_shape(head, n_tokens, planes_of(h), 1, low * kHeadTile, &w.s);
+  w.each = head_places(w.s, planes_of(h), gradient).bytes;
+  return w;
+}
+
+int run_rows(const dadam_handle* h, HeadArgs a, bool dhidden, bool dhead, bool dbias, uint32_t rows, void* stream) {
+  const int x = (int)h->cfg.param_dtype, g = (int)h->cfg.grad_dtype;
+  const bool gradient = dhidden || dhead;
+  const uint32_t pieces = (a.s.vocab + a.s.piece - 1) / a.s.piece;
+  auto piece = [&](uint32_t k) {
+    a.first_word = k * a.s.piece;
+    a.words = std::min(a.s.piece, a.s.vocab - a.first_word);
+    a.later = k > 0;
+  };
+  int e = launch_head_begin(x, g, a, rows, stream);
+  if (!e) e = launch_head_hidden(x, g, gradient, a, rows, stream);
+  for (uint32_t k = 0; k < pieces && !e; ++k) {
+    piece(k);
+    e = launch_head_words(x, g, gradient && pieces == 1, a, rows, stream);
+    if (!e) e = launch_head_logits(x, g, false, a, rows, stream);
+  }
+  if (!e) e = launch_head_losses(a, rows, stream);
+  if (!gradient) return e;
+  for (uint32_t k = 0; k < pieces && !e; ++k) {
+    piece(k);
+    if (pieces > 1) e = launch_head_words(x, g, true, a, rows, stream);
+    if (!e) e = launch_head_logits(x, g, true, a, rows, stream);
+    if (!e && dhead) e = launch_head_dhead(x, g, a, rows, stream);
+    if (!e && dbias) e = launch_head_dbias(x, g, a, rows, stream);
+    if (!e && dhidden) e = launch_head_dhidden(x, g, a, rows, stream);
+  }
+  if (!e && dhidden && a.s.tokens) e = launch_head_end(x, g, a, rows, stream);
+  return e;
+}
+
+}  // namespace
+}  // namespace dadam
+
+extern "C" {
+
+int dadam_head_get_info(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, uint32_t gradient, dadam_head_info* out) {
+  if (!h) return DADAM_EINVAL;
+  if (!out) return fail(h, DADAM_EINVAL, "out is null");
+  if (const int rc = check_head(h, head, n_tokens)) return rc;
+  const Way w = good_way(h, head, n_tokens, gradient != 0);
+  out->least_bytes = least_way(h, head, n_tokens, gradient != 0).each;
+  out->bytes = std::max(out->least_bytes, w.each * w.rows);
+  return DADAM_OK;
+}
+
+int dadam_head_loss(dadam_handle* h, const dadam_head* head, const void* const* params, const void* const* hidden, const int32_t* const* targets,
+                    uint32_t n_tokens, float scale, uint32_t flags, float* losses, float* const* nll, void* const* dhidden, void* const* grads,
+                    void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+  if (!h) return DADAM_EINVAL;
+  if (!params || !hidden || !targets) return fail(h, DADAM_EINVAL, "params, hidden or targets is null");
+  if (!losses) return fail(h, DADAM_EINVAL, "losses is null");
+  if ((uintptr_t)losses & 3u) return fail(h, DADAM_EALIGN, "losses is not 4-byte aligned");
+  if (!std::isfinite(scale)) return fail(h, DADAM_EINVAL, "scale must be finite");
+  if (flags & ~(DADAM_HEAD_MEAN | DADAM_HEAD_ADD)) return fail(h, DADAM_EINVAL, "unknown flag bits 0x%x", flags);
+  return guarded(h, [&] {
+    int rc = check_head(h, head, n_tokens);
+    if (rc) return rc;
+    const uint32_t R = h->cfg.n_rows, xs = (uint32_t)dtype_bytes(h->cfg.param_dtype), gs = (uint32_t)dtype_bytes(h->cfg.grad_dtype);
+    const size_t vectors = (size_t)n_tokens * head->width * xs, values = (size_t)n_tokens * 4;
+    const bool gradient = dhidden || grads;
+    const uint64_t least = least_way(h, head, n_tokens, gradient).each;
+    if (!workspace) return fail(h, DADAM_EINVAL, "workspace is null");
+    if ((uintptr_t)workspace & 255u) return fail(h, DADAM_EALIGN, "workspace is not 256-byte aligned");
+    if (workspace_bytes < least)
+      return fail(h, DADAM_EINVAL, "workspace has %llu bytes, %llu are needed", (unsigned long long)workspace_bytes, (unsigned long long)least);
+    const void* const one[1] = {workspace};
+    const Table tables[7] = {{params, R, (size_t)h->cfg.d * xs, "params", false, -1},
+                             {hidden, R, vectors, "hidden", false, -1, xs},
+                             {(const void* const*)targets, R, values, "targets", false, -1, 4},
+                             {(const void* const*)nll, nll ? R : 0, values, "nll", true, -1, 4},
+                             {dhidden, dhidden ? R : 0, vectors, "dhidden", true, -1, xs},
+                             {grads, grads ? R : 0, (size_t)h->cfg.d * gs, "grads", true, -1},
+                             {one, 1, (size_t)workspace_bytes, "workspace", true, -1}};
+    rc = check_tables(h, tables, 7);
+    const uintptr_t lo = (uintptr_t)losses, hi = lo + 4 * R;
+    for (const Table& t : tables)
+      for (uint32_t i = 0; i < t.n && !rc; ++i)
+        if (lo < (uintptr_t)t.p[i] + t.bytes && (uintptr_t)t.p[i] < hi) rc = fail(h, DADAM_EALIAS, "losses overlaps %s[%u]", t.name, i);
+    if (!rc) rc = check_device(h);
+    if (rc) return rc;
+    const Way way = way_for(h, head, n_tokens, gradient, workspace_bytes);
+    const uint64_t at = h->tensors[head->tensor].offset_elems;
+    const bool biased = head->bias_tensor != DADAM_HEAD_NO_BIAS;
+    const uint64_t bias_at = biased ? h->tensors[head->bias_tensor].offset_elems : 0;
+    DeviceGuard guard(h->cfg.device);
+    if (guard.err != hipSuccess) return fail(h, DADAM_EHIP, "hipSetDevice: %s", hipGetErrorString(guard.err));
+    int e = (int)hipSuccess;
+    for (uint32_t i = 0; i < R && !e; i += way.rows) {
+      const uint32_t rows = std::min(way.rows, R - i);
+      HeadArgs a;
+      memset((void*)&a, 0, sizeof(a));
+      a.s = way.s;
+      a.w = head_places(way.s, planes_of(h), gradient);
+      a.workspace = (uint64_t)(uintptr_t)workspace;
+      a.stride = way.each;
+      a.losses = losses + i;
+      a.scale = scale;
+      a.mean = (flags & DADAM_HEAD_MEAN) != 0;
+      a.add = (flags & DADAM_HEAD_ADD) != 0;
+      a.n_xcd = h->n_xcds;
+      for (uint32_t r = 0; r < rows; ++r) {
+        HeadRow& row = a.row[r];
+        row.head = (uint64_t)(uintptr_t)params[i + r] + at * xs;
+        row.bias = biased ? (uint64_t)(uintptr_t)params[i + r] + bias_at * xs : 0;
+        row.hidden = (uint64_t)(uintptr_t)hidden[i + r];
+        row.target = (uint64_t)(uintptr_t)targets[i + r];
+        row.nll = nll ? (uint64_t)(uintptr_t)nll[i + r] : 0;
+        row.dhidden = dhidden ? (uint64_t)(uintptr_t)dhidden[i + r] : 0;
+        row.dhead = grads ? (uint64_t)(uintptr_t)grads[i + r] + at * gs : 0;
+        row.dbias = grads && biased ? (uint64_t)(uintptr_t)grads[i + r] + bias_at * gs : 0;
+      }
+      e = run_rows(h, a, dhidden != nullptr, grads != nullptr, grads && biased, rows, hip_stream);
+    }
+    if (e != (int)hipSuccess) return fail(h, DADAM_EHIP, "kernel launch failed: %s", hipGetErrorString((hipError_t)e));
+    return DADAM_OK;
+  });
+}
+
+}  // extern "C"

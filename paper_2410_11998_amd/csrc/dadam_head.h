@@ -1,0 +1,84 @@
+// Internal interface between the host side of a head's loss (dadam_head.cpp) and its kernels (dadam_head.hip).
+#ifndef DADAM_HEAD_H_
+#define DADAM_HEAD_H_
+
+#include <stdint.h>
+
+#include "dadam_internal.h"
+
+namespace dadam {
+
+constexpr uint32_t kHeadTile = 128;   // rows of operands are filled up to a multiple of this
+constexpr uint32_t kHeadSlice = 64;   // words whose exponentials a wavefront adds up
+constexpr int kHeadRows = 32;         // replicas of a launch
+constexpr uint32_t kHeadSplits = 16;  // most parts that the sum over words of a hidden vector's gradient goes in
+
+struct HeadRow {  // device addresses, 0 where there is none
+  uint64_t head, bias, hidden, target, nll, dhidden, dhead, dbias;
+};
+
+// Workspace of a replica.  Operands have `planes` halves or bfloat16s an element; n: rows as they lie, t: the other way round.
+struct HeadPlaces {
+  uint64_t words, lse, hit, stats, hidden_n, hidden_t, head_n, head_t, p_n, p_t, sums, bytes;
+};
+struct HeadShape {
+  uint32_t tokens, vocab, width;
+  uint32_t T, D, K;        // tokens and width filled up to kHeadTile, width filled up to a stage
+  uint32_t piece, slices;  // words of a piece (a multiple of kHeadTile), slices of all words
+  uint32_t splits;
+};
+inline constexpr HeadPlaces head_places(const HeadShape& s, uint64_t planes, bool gradient) {
+  HeadPlaces w{};
+  uint64_t at = 0, b = 2 * planes;
+  auto take = [&at](uint64_t bytes) {
+    const uint64_t here = at;
+    at += (bytes + 255) / 256 * 256;
+    return here;
+  };
+  w.words = take(64);
+  w.lse = take((uint64_t)s.T * 4);
+  w.hit = take((uint64_t)s.T * 4);
+  w.stats = take((uint64_t)s.slices * s.T * 8);
+  w.hidden_n = take((uint64_t)s.T * s.K * b);
+  w.head_n = take((uint64_t)s.piece * s.K * b);
+  if (gradient) {
+    w.hidden_t = take((uint64_t)s.D * s.T * b);
+    w.head_t = take((uint64_t)s.D * s.piece * b);
+    w.p_n = take((uint64_t)s.T * s.piece * b);
+    w.p_t = take((uint64_t)s.piece * s.T * b);
+    w.sums = take((uint64_t)s.splits * s.T * s.D * 4);
+  }
+  w.bytes = at;
+  return w;
+}
+// HeadPlaces::words
+enum HeadWord : uint32_t { kHeadCount = 0, kHeadMostHidden = 1, kHeadMostHead = 2 };
+
+struct HeadArgs {
+  HeadShape s;
+  HeadPlaces w;
+  uint64_t workspace, stride;
+  float* losses;        // [row]
+  float scale;
+  uint32_t mean, add;
+  uint32_t first_word, words;  // of the piece
+  uint32_t later;       // a piece before this one has begun the sums
+  uint32_t n_xcd;
+  HeadRow row[kHeadRows];
+};
+static_assert(sizeof(HeadArgs) <= 4096, "the argument block of a launch holds 4 KB");
+
+// Launchers, of `rows` replicas.  xdt: type of parameters and hidden vectors, gdt of gradients; two planes unless both are bfloat16.
+int launch_head_begin(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                   // tokens with a target, powers of two
+int launch_head_hidden(int xdt, int gdt, bool gradient, const HeadArgs& a, uint32_t rows, void* stream);   // operands of the hidden vectors
+int launch_head_words(int xdt, int gdt, bool turned, const HeadArgs& a, uint32_t rows, void* stream);      // operands of a piece of the head
+int launch_head_logits(int xdt, int gdt, bool gradient, const HeadArgs& a, uint32_t rows, void* stream);   // statistics, or the logits' gradient
+int launch_head_losses(const HeadArgs& a, uint32_t rows, void* stream);
+int launch_head_dhead(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);
+int launch_head_dbias(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);
+int launch_head_dhidden(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                 // a piece's part of the sums
+int launch_head_end(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                     // the hidden vectors' gradients from the sums
+
+}  // namespace dadam
+
+#endif  // DADAM_HEAD_H_

@@ -46,10 +46,69 @@ struct Brain {
   static __device__ __forceinline__ float value(uint32_t b) { return __uint_as_float(b << 16); }
 };
 
+// Elements of parameters, gradients and state.
+struct F32 {
+  using type = float;
+  static __device__ __forceinline__ float load(uint64_t p, uint64_t e) { return global<const float>(p)[e]; }
+  static __device__ __forceinline__ void store(uint64_t p, uint64_t e, float v) { global<float>(p)[e] = v; }
+};
+struct B16 {
+  using type = uint16_t;
+  static __device__ __forceinline__ float load(uint64_t p, uint64_t e) { return Brain::value(global<const uint16_t>(p)[e]); }
+  static __device__ __forceinline__ void store(uint64_t p, uint64_t e, float v) { global<uint16_t>(p)[e] = (uint16_t)Brain::bits(v); }
+};
+
 constexpr int kStageBytes = 128;  // of a row's elements that a stage takes: 64 elements of one plane, 32 of two
 
 // Where element k of a row of a two-plane operand has its high (the low is 32 behind it).
 __device__ __forceinline__ uint32_t high_at(uint32_t k) { return (k & ~31u) * 2 + (k & 31u); }
+
+__device__ __forceinline__ uint32_t pair(uint32_t low, uint32_t high) { return low | high << 16; }
+__device__ __forceinline__ uint2v four(const uint32_t (&b)[4]) { return uint2v{pair(b[0], b[1]), pair(b[2], b[3])}; }
+
+// A value as the halves of an operand.
+template <typename OP>
+__device__ __forceinline__ void halves(float v, uint32_t& high, uint32_t& low) {
+  high = OP::bits(v);
+  low = OP::bits(v - OP::value(high));
+}
+
+// Elements k .. k+3 (k % 4 == 0) of row r of an operand of `cols` columns.
+template <typename OP, int PLANES>
+__device__ __forceinline__ void store4(uint64_t base, uint64_t r, uint32_t cols, uint32_t k, const float4v& v) {
+  uint32_t h[4], l[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) halves<OP>(v[e], h[e], l[e]);
+  if constexpr (PLANES == 1) {
+    global<uint2v>(base + (r * cols + k) * 2)[0] = four(h);
+  } else {
+    global<uint2v>(base + (r * cols * 2 + high_at(k)) * 2)[0] = four(h);
+    global<uint2v>(base + (r * cols * 2 + high_at(k) + 32) * 2)[0] = four(l);
+  }
+}
+template <typename OP, int PLANES>
+__device__ __forceinline__ void store1(uint64_t base, uint64_t r, uint32_t cols, uint32_t k, float v) {
+  uint32_t h, l;
+  halves<OP>(v, h, l);
+  if constexpr (PLANES == 1) {
+    global<uint16_t>(base)[r * cols + k] = (uint16_t)h;
+  } else {
+    global<uint16_t>(base)[r * cols * 2 + high_at(k)] = (uint16_t)h;
+    global<uint16_t>(base)[r * cols * 2 + high_at(k) + 32] = (uint16_t)l;
+  }
+}
+template <typename OP, int PLANES>
+__device__ __forceinline__ float4v load4(uint64_t base, uint64_t r, uint32_t cols, uint32_t k) {
+  auto unpack = [](uint2v b) { return float4v{OP::value(b[0] & 0xffff), OP::value(b[0] >> 16), OP::value(b[1] & 0xffff), OP::value(b[1] >> 16)}; };
+  if constexpr (PLANES == 1) return unpack(global<const uint2v>(base + (r * cols + k) * 2)[0]);
+  return unpack(global<const uint2v>(base + (r * cols * 2 + high_at(k)) * 2)[0]) + unpack(global<const uint2v>(base + (r * cols * 2 + high_at(k) + 32) * 2)[0]);
+}
+
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int step = 32; step; step >>= 1) v += __shfl_xor(v, step);
+  return v;
+}
 
 // Shape of a workgroup's tile: WM x WN wavefronts, each MT x NT blocks of 32 x 32.
 template <typename OP, int PLANES, int MT, int NT, int WM, int WN>

@@ -18,73 +18,24 @@ namespace {
 
 extern __shared__ char ortho_lds[];
 
-struct F32 {
-  static __device__ __forceinline__ float load(uint64_t p, uint64_t e) { return global<const float>(p)[e]; }
-  static __device__ __forceinline__ void store(uint64_t p, uint64_t e, float v) { global<float>(p)[e] = v; }
-};
-struct B16 {
-  static __device__ __forceinline__ float load(uint64_t p, uint64_t e) { return Brain::value(global<const uint16_t>(p)[e]); }
-  static __device__ __forceinline__ void store(uint64_t p, uint64_t e, float v) { global<uint16_t>(p)[e] = (uint16_t)Brain::bits(v); }
-};
-
 template <int PLANES>
 using OrthoTile = Tile<Half, PLANES, 2, 2, 2, 2>;
-
-__device__ __forceinline__ uint32_t pair(uint32_t low, uint32_t high) { return low | high << 16; }
-__device__ __forceinline__ uint2v four(const uint32_t (&b)[4]) { return uint2v{pair(b[0], b[1]), pair(b[2], b[3])}; }
-
-// A value as the halves of an operand.
-__device__ __forceinline__ void halves(float v, uint32_t& high, uint32_t& low) {
-  high = Half::bits(v);
-  low = Half::bits(v - Half::value(high));
-}
-
-// Elements k .. k+3 (k % 4 == 0) of row r of an operand of `cols` columns.
-template <int PLANES>
-__device__ __forceinline__ void store4(uint64_t base, uint64_t r, uint32_t cols, uint32_t k, const float4v& v) {
-  uint32_t h[4], l[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) halves(v[e], h[e], l[e]);
-  if constexpr (PLANES == 1) {
-    global<uint2v>(base + (r * cols + k) * 2)[0] = four(h);
-  } else {
-    global<uint2v>(base + (r * cols * 2 + high_at(k)) * 2)[0] = four(h);
-    global<uint2v>(base + (r * cols * 2 + high_at(k) + 32) * 2)[0] = four(l);
-  }
-}
-template <int PLANES>
-__device__ __forceinline__ void store1(uint64_t base, uint64_t r, uint32_t cols, uint32_t k, float v) {
-  uint32_t h, l;
-  halves(v, h, l);
-  if constexpr (PLANES == 1) {
-    global<uint16_t>(base)[r * cols + k] = (uint16_t)h;
-  } else {
-    global<uint16_t>(base)[r * cols * 2 + high_at(k)] = (uint16_t)h;
-    global<uint16_t>(base)[r * cols * 2 + high_at(k) + 32] = (uint16_t)l;
-  }
-}
-template <int PLANES>
-__device__ __forceinline__ float4v load4(uint64_t base, uint64_t r, uint32_t cols, uint32_t k) {
-  auto unpack = [](uint2v b) { return float4v{Half::value(b[0] & 0xffff), Half::value(b[0] >> 16), Half::value(b[1] & 0xffff), Half::value(b[1] >> 16)}; };
-  if constexpr (PLANES == 1) return unpack(global<const uint2v>(base + (r * cols + k) * 2)[0]);
-  return unpack(global<const uint2v>(base + (r * cols * 2 + high_at(k)) * 2)[0]) + unpack(global<const uint2v>(base + (r * cols * 2 + high_at(k) + 32) * 2)[0]);
-}
 
 // The turned copy of X: Q rows of P, the operand, and with one plane what the half leaves as a second array behind it.
 template <int PLANES>
 __device__ __forceinline__ void store_turned4(uint64_t base, const OrthoTask& t, uint32_t q, uint32_t p, const float4v& v) {
-  store4<PLANES>(base, q, t.P, p, v);
+  store4<Half, PLANES>(base, q, t.P, p, v);
   if constexpr (PLANES == 1) {
     uint32_t h, l[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) halves(v[e], h, l[e]);
+    for (int e = 0; e < 4; ++e) halves<Half>(v[e], h, l[e]);
     global<uint2v>(base + ((uint64_t)t.Q * t.P + (uint64_t)q * t.P + p) * 2)[0] = four(l);
   }
 }
 template <int PLANES>
 __device__ __forceinline__ float4v load_turned4(uint64_t base, const OrthoTask& t, uint32_t q, uint32_t p) {
-  float4v v = load4<PLANES>(base, q, t.P, p);
-  if constexpr (PLANES == 1) v += load4<1>(base + (uint64_t)t.Q * t.P * 2, q, t.P, p);
+  float4v v = load4<Half, PLANES>(base, q, t.P, p);
+  if constexpr (PLANES == 1) v += load4<Half, 1>(base + (uint64_t)t.Q * t.P * 2, q, t.P, p);
   return v;
 }
 template <int PLANES>
@@ -136,12 +87,6 @@ __device__ __forceinline__ float source_value(const Scalars& c, uint32_t source,
   if (source == kOrthoGiven) return g;
   const float m = fmaf(c.beta1, mh, c.omb1 * g);
   return source == kOrthoMoment ? m : fmaf(c.beta1, m, c.omb1 * g);
-}
-
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int step = 32; step; step >>= 1) v += __shfl_xor(v, step);
-  return v;
 }
 
 // Squares of a tile, in 64 bits, to the tile's place among the matrix's partial sums.
@@ -209,9 +154,9 @@ __global__ __launch_bounds__(256) void k_ortho_begin(OrthoBeginArgs<N> a) {
     for (int e = 0; e < 4; ++e) v[e] = tile[r * kTurnPitch + k4 + e], t[e] = tile[(k4 + e) * kTurnPitch + r];
     if (u.t.tall) {
       store_turned4<PLANES>(u.base + w.turned[0], u.t, c.r0 + r, c.c0 + k4, v);
-      store4<PLANES>(u.base + w.x, c.c0 + r, u.t.Q, c.r0 + k4, t);
+      store4<Half, PLANES>(u.base + w.x, c.c0 + r, u.t.Q, c.r0 + k4, t);
     } else {
-      store4<PLANES>(u.base + w.x, c.r0 + r, u.t.Q, c.c0 + k4, v);
+      store4<Half, PLANES>(u.base + w.x, c.r0 + r, u.t.Q, c.c0 + k4, v);
       store_turned4<PLANES>(u.base + w.turned[0], u.t, c.c0 + r, c.r0 + k4, t);
     }
   }
@@ -236,11 +181,11 @@ __global__ __launch_bounds__(256) void k_ortho_gram(OrthoStepArgs a) {
     m += i * T::kM;
     n += j * T::kN;
     v *= a.fresh;
-    if constexpr (SQUARE) v += load4<PLANES>(u.base + w.a, n, u.t.P, m) * a.gain;
-    store4<PLANES>(out, n, u.t.P, m, v);
+    if constexpr (SQUARE) v += load4<Half, PLANES>(u.base + w.a, n, u.t.P, m) * a.gain;
+    store4<Half, PLANES>(out, n, u.t.P, m, v);
     if (i != j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) store1<PLANES>(out, m + e, u.t.P, n, v[e]);
+      for (int e = 0; e < 4; ++e) store1<Half, PLANES>(out, m + e, u.t.P, n, v[e]);
   });
 }
 
@@ -261,7 +206,7 @@ __global__ __launch_bounds__(256) void k_ortho_next(OrthoStepArgs a) {
     v = load_turned4<PLANES>(from, u.t, n, m) * a.gain + v * a.fresh;
     store_turned4<PLANES>(to, u.t, n, m, v);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) store1<PLANES>(u.base + w.x, m + e, u.t.Q, n, v[e]);
+    for (int e = 0; e < 4; ++e) store1<Half, PLANES>(u.base + w.x, m + e, u.t.Q, n, v[e]);
   });
 }
 
