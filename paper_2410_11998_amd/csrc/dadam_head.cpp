@@ -32,35 +32,45 @@ int check_head(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens)
 }
 
 // How a call goes: words of a piece, replicas of a launch, parts of the sums over words.
-constexpr uint32_t kGoodTiles = 2048;     // eight a compute unit
-constexpr uint32_t kGoodWords = 8192;     // of a piece at least, so that the product over tokens fills the chip
-constexpr uint32_t kGoodSums = 512;
 struct Way {
   HeadShape s;
   uint32_t rows;
   uint64_t each;  // workspace of a replica
 };
 
-void fill_shape(const dadam_head* head, uint32_t n_tokens, uint32_t planes, uint32_t rows, uint32_t piece, HeadShape* s) {
+constexpr uint32_t kSplits = 16;              // at most
+constexpr uint64_t kMostOfPiece = 1ull << 27;  // tokens times words of a piece
+// Workgroups that the chip holds at a time: one large tile a compute unit, two small ones.
+uint32_t at_once(uint32_t edge) { return edge == 256 ? 256 : 512; }
+
+bool suits_large(uint32_t n) { return 8 * (uint64_t)filled(n, 256) <= 9 * (uint64_t)filled(n, 128); }
+
+void fill_shape(const dadam_head* head, uint32_t n_tokens, uint32_t planes, uint32_t edge, uint32_t rows, uint32_t piece, HeadShape* s) {
   s->tokens = n_tokens;
   s->vocab = head->vocab;
   s->width = head->width;
-  s->T = filled(n_tokens, kHeadTile);
-  s->D = filled(head->width, kHeadTile);
+  s->edge = edge;
+  s->T = filled(n_tokens, edge);
+  s->D = filled(head->width, edge);
   s->K = filled(head->width, 64);
-  const uint32_t pieces = (head->vocab + piece - 1) / piece;
-  s->piece = filled((head->vocab + pieces - 1) / pieces, kHeadTile);
-  s->slices = filled(head->vocab, kHeadTile) / kHeadSlice;
-  const uint64_t tiles = (uint64_t)(s->T / kHeadTile) * (s->D / kHeadTile) * rows, stages = (uint64_t)s->piece * planes / 64;
-  s->splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(std::min<uint64_t>((kGoodSums + tiles - 1) / tiles, stages / 8), kHeadSplits));
+  s->piece = std::min(piece, filled(head->vocab, edge));
+  s->slices = filled(head->vocab, edge) / (edge / 2);
+  const uint64_t tiles = (uint64_t)(s->T / edge) * (s->D / edge) * rows, stages = (uint64_t)s->piece * planes / 64;
+  s->splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(std::min<uint64_t>((at_once(edge) + tiles - 1) / tiles, stages / 8), kSplits));
 }
 
 Way good_way(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, bool gradient) {
   Way w{};
-  const uint32_t planes = planes_of(h), T = filled(n_tokens, kHeadTile) / kHeadTile, V = filled(head->vocab, kHeadTile) / kHeadTile;
-  const uint32_t piece = std::min(V, std::max(kGoodTiles / T, kGoodWords / kHeadTile));
-  w.rows = std::min<uint32_t>(std::min<uint32_t>(h->cfg.n_rows, kHeadRows), std::max(1u, kGoodTiles / (piece * T)));
-  fill_shape(head, n_tokens, planes, w.rows, piece * kHeadTile, &w.s);
+  const uint32_t planes = planes_of(h), V = head->vocab, R = std::min<uint32_t>(h->cfg.n_rows, kHeadRows);
+  const uint64_t large = (uint64_t)(filled(V, 256) / 256) * (filled(n_tokens, 256) / 256) * R;
+  const uint32_t edge = suits_large(n_tokens) && suits_large(head->width) && suits_large(V) && large >= 256 ? 256 : 128;
+  // pieces whose tiles of the head's gradient are what the chip holds at a time
+  const uint32_t across = filled(head->width, edge) / edge;
+  uint64_t piece = (uint64_t)std::max(1u, at_once(edge) / across) * edge;
+  piece = std::max<uint64_t>(edge, std::min(piece, kMostOfPiece / filled(n_tokens, edge) / edge * edge));
+  piece = std::min<uint64_t>(piece, filled(V, edge));
+  w.rows = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(R, 2 * at_once(edge) / (piece / edge * across)));
+  fill_shape(head, n_tokens, planes, edge, w.rows, (uint32_t)piece, &w.s);
   w.each = head_places(w.s, planes, gradient).bytes;
   return w;
 }
@@ -68,7 +78,7 @@ Way good_way(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, b
 Way least_way(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, bool gradient) {
   Way w{};
   w.rows = 1;
-  fill_shape(head, n_tokens, planes_of(h), 1, kHeadTile, &w.s);
+  fill_shape(head, n_tokens, planes_of(h), 128, 1, 128, &w.s);
   w.each = head_places(w.s, planes_of(h), gradient).bytes;
   return w;
 }
@@ -80,15 +90,16 @@ Way way_for(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, bo
     w.rows = (uint32_t)std::min<uint64_t>(w.rows, bytes / w.each);
     return w;
   }
-  w.rows = 1;
-  uint32_t low = 1, high = w.s.piece / kHeadTile;  // tiles of a piece: what fits, and what does not
+  const uint32_t planes = planes_of(h);
+  uint32_t low = 1, high = std::max(2u, w.s.piece / 128);  // small tiles of a piece: what fits, and what does not or need not
   while (low + 1 < high) {
     const uint32_t middle = (low + high) / 2;
-    fill_shape(head, n_tokens, planes_of(h), 1, middle * kHeadTile, &w.s);
-    (head_places(w.s, planes_of(h), gradient).bytes <= bytes ? low : high) = middle;
+    fill_shape(head, n_tokens, planes, 128, 1, middle * 128, &w.s);
+    (head_places(w.s, planes, gradient).bytes <= bytes ? low : high) = middle;
   }
-  fill_shape(head, n_tokens, planes_of(h), 1, low * kHeadTile, &w.s);
-  w.each = head_places(w.s, planes_of(h), gradient).bytes;
+  w.rows = 1;
+  fill_shape(head, n_tokens, planes, 128, 1, low * 128, &w.s);
+  w.each = head_places(w.s, planes, gradient).bytes;
   return w;
 }
 
@@ -102,17 +113,17 @@ int run_rows(const dadam_handle* h, HeadArgs a, bool dhidden, bool dhead, bool d
     a.later = k > 0;
   };
   int e = launch_head_begin(x, g, a, rows, stream);
-  if (!e) e = launch_head_hidden(x, g, gradient, a, rows, stream);
+  if (!e && (gradient || !a.straight)) e = launch_head_hidden(x, g, gradient, a, rows, stream);
   for (uint32_t k = 0; k < pieces && !e; ++k) {
     piece(k);
-    e = launch_head_words(x, g, gradient && pieces == 1, a, rows, stream);
+    if (!a.straight) e = launch_head_words(x, g, gradient && pieces == 1, a, rows, stream);
     if (!e) e = launch_head_logits(x, g, false, a, rows, stream);
   }
   if (!e) e = launch_head_losses(a, rows, stream);
   if (!gradient) return e;
   for (uint32_t k = 0; k < pieces && !e; ++k) {
     piece(k);
-    if (pieces > 1) e = launch_head_words(x, g, true, a, rows, stream);
+    if (pieces > 1 || a.straight) e = launch_head_words(x, g, true, a, rows, stream);
     if (!e) e = launch_head_logits(x, g, true, a, rows, stream);
     if (!e && dhead) e = launch_head_dhead(x, g, a, rows, stream);
     if (!e && dbias) e = launch_head_dbias(x, g, a, rows, stream);
@@ -192,11 +203,13 @@ int dadam_head_loss(dadam_handle* h, const dadam_head* head, const void* const* 
       a.mean = (flags & DADAM_HEAD_MEAN) != 0;
       a.add = (flags & DADAM_HEAD_ADD) != 0;
       a.n_xcd = h->n_xcds;
+      a.straight = n_tokens && planes_of(h) == 1 && head->width % 64 == 0 && at * xs % 16 == 0;
       for (uint32_t r = 0; r < rows; ++r) {
         HeadRow& row = a.row[r];
         row.head = (uint64_t)(uintptr_t)params[i + r] + at * xs;
         row.bias = biased ? (uint64_t)(uintptr_t)params[i + r] + bias_at * xs : 0;
         row.hidden = (uint64_t)(uintptr_t)hidden[i + r];
+        a.straight &= row.hidden % 16 == 0;
         row.target = (uint64_t)(uintptr_t)targets[i + r];
         row.nll = nll ? (uint64_t)(uintptr_t)nll[i + r] : 0;
         row.dhidden = dhidden ? (uint64_t)(uintptr_t)dhidden[i + r] : 0;

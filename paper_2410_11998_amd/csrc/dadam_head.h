@@ -8,8 +8,6 @@
 
 namespace dadam {
 
-constexpr uint32_t kHeadTile = 128;   // rows of operands are filled up to a multiple of this
-constexpr uint32_t kHeadSlice = 64;   // words whose exponentials a wavefront adds up
 constexpr int kHeadRows = 32;         // replicas of a launch
 constexpr uint32_t kHeadSplits = 16;  // most parts that the sum over words of a hidden vector's gradient goes in
 
@@ -23,9 +21,10 @@ struct HeadPlaces {
 };
 struct HeadShape {
   uint32_t tokens, vocab, width;
-  uint32_t T, D, K;        // tokens and width filled up to kHeadTile, width filled up to a stage
-  uint32_t piece, slices;  // words of a piece (a multiple of kHeadTile), slices of all words
-  uint32_t splits;
+  uint32_t edge;           // of the products' tiles: 128 or 256
+  uint32_t T, D, K;        // tokens and width filled up to the edge, width filled up to a stage
+  uint32_t piece, slices;  // words of a piece (a multiple of the edge), slices of edge / 2 of all words
+  uint32_t splits;         // parts that the sum over words of a hidden vector's gradient goes in
 };
 inline constexpr HeadPlaces head_places(const HeadShape& s, uint64_t planes, bool gradient) {
   HeadPlaces w{};
@@ -64,6 +63,7 @@ struct HeadArgs {
   uint32_t first_word, words;  // of the piece
   uint32_t later;       // a piece before this one has begun the sums
   uint32_t n_xcd;
+  uint32_t straight;    // the hidden vectors and the head are operands as they lie, for the products over the width
   HeadRow row[kHeadRows];
 };
 static_assert(sizeof(HeadArgs) <= 4096, "the argument block of a launch holds 4 KB");

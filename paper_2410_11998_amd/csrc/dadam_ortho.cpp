@@ -18,10 +18,10 @@ struct MatrixState {
   // dadam_set_matrices: by size, the largest first
   std::vector<OrthoTask> tasks;
   std::vector<uint64_t> need[2];  // bytes of workspace of a matrix and a replica, with one plane and with two
-  char* memory = nullptr;         // tasks, and the matrix of every tile of either kind
+  char* memory = nullptr;         // tasks, and the matrix of every tile of each kind
   const OrthoTask* d_tasks[2] = {};
-  const uint32_t *d_gram = nullptr, *d_whole = nullptr;
-  uint32_t gram_units = 0, whole_units = 0;
+  const uint32_t* d_units[3] = {};  // OrthoTask::gram_units, whole_units, cell_units
+  uint32_t n_units[3] = {};
   // dadam_set_ortho_schedule
   std::vector<float> coefficients{3.4445f, -4.7750f, 2.0315f, 3.4445f, -4.7750f, 2.0315f, 3.4445f, -4.7750f, 2.0315f, 3.4445f, -4.7750f, 2.0315f, 3.4445f, -4.7750f, 2.0315f};
 };
@@ -42,7 +42,14 @@ MatrixState* state_of(dadam_handle* h) {
   return h->matrices;
 }
 
-uint32_t filled(uint32_t n) { return (n + kOrthoPad - 1) / kOrthoPad * kOrthoPad; }
+uint32_t filled(uint32_t n, uint32_t each) { return (n + each - 1) / each * each; }
+
+uint64_t lower_half(uint64_t n) { return n * (n + 1) / 2; }
+
+// Large tiles: for matrices whose sides they fill up by an eighth more than the small ones at most, if there are enough of them for the chip (256 compute
+// units, that hold one each).
+bool suits_large(uint32_t n) { return 8 * (uint64_t)filled(n, kLargeEdge) <= 9 * (uint64_t)filled(n, kSmallEdge); }
+constexpr uint64_t kEnoughLarge = 256;
 
 constexpr uint32_t kMostMatrices = 65536, kMostSide = 65536;
 
@@ -92,36 +99,41 @@ int set_matrices(dadam_handle* h, const dadam_matrix_desc* m, uint32_t n) {
     t.tall = m[k].rows > m[k].cols;
     t.p = std::min(m[k].rows, m[k].cols);
     t.q = std::max(m[k].rows, m[k].cols);
-    t.P = filled(t.p);
-    t.Q = filled(t.q);
+    t.edge = suits_large(t.p) && suits_large(t.q) ? kLargeEdge : kSmallEdge;
     t.scale = m[k].scale;
     t.decay = tensor.weight_decay;
   }
-  std::stable_sort(tasks.begin(), tasks.end(), [](const OrthoTask& a, const OrthoTask& b) { return (uint64_t)a.P * a.P * a.Q > (uint64_t)b.P * b.P * b.Q; });
-  std::vector<uint32_t> gram, whole;
-  uint64_t gram_units = 0, whole_units = 0;
-  for (const OrthoTask& t : tasks) {
-    const uint64_t across = t.P / kOrthoPad;
-    gram_units += across * (across + 1) / 2;
-    whole_units += across * (t.Q / kOrthoPad);
+  uint64_t large = 0, units[3] = {};
+  for (const OrthoTask& t : tasks)
+    if (t.edge == kLargeEdge) large += lower_half(filled(t.p, kLargeEdge) / kLargeEdge);
+  for (OrthoTask& t : tasks) {
+    if (large * h->cfg.n_rows < kEnoughLarge) t.edge = kSmallEdge;
+    t.P = filled(t.p, t.edge);
+    t.Q = filled(t.q, t.edge);
+    units[0] += lower_half(t.P / t.edge);
+    units[1] += (uint64_t)(t.P / t.edge) * (t.Q / t.edge);
+    units[2] += (uint64_t)(t.P / kOrthoCell) * (t.Q / kOrthoCell);
   }
-  if (whole_units >> 31) return fail(h, DADAM_EINVAL, "the matrices have more than 2^31 tiles");
-  gram.reserve(gram_units);
-  whole.reserve(whole_units);
+  if (units[2] >> 31) return fail(h, DADAM_EINVAL, "the matrices have more than 2^31 tiles");
+  // by tile and size, the largest first
+  std::stable_sort(tasks.begin(), tasks.end(), [](const OrthoTask& a, const OrthoTask& b) {
+    return a.edge != b.edge ? a.edge > b.edge : (uint64_t)a.P * a.P * a.Q > (uint64_t)b.P * b.P * b.Q;
+  });
+  std::vector<uint32_t> of_unit[3];
+  for (int kind = 0; kind < 3; ++kind) of_unit[kind].reserve(units[kind]);
+  for (uint32_t k = 0; k < n; ++k) {
+    OrthoTask& t = tasks[k];
+    t.gram_units = (uint32_t)of_unit[0].size();
+    t.whole_units = (uint32_t)of_unit[1].size();
+    t.cell_units = (uint32_t)of_unit[2].size();
+    of_unit[0].insert(of_unit[0].end(), lower_half(t.P / t.edge), k);
+    of_unit[1].insert(of_unit[1].end(), (uint64_t)(t.P / t.edge) * (t.Q / t.edge), k);
+    of_unit[2].insert(of_unit[2].end(), (uint64_t)(t.P / kOrthoCell) * (t.Q / kOrthoCell), k);
+  }
   std::vector<OrthoTask> planes[2] = {tasks, tasks};
   for (uint32_t p = 0; p < 2; ++p) {
     uint64_t at = 0;
-    for (uint32_t k = 0; k < n; ++k) {
-      OrthoTask& t = planes[p][k];
-      if (p == 0) {
-        tasks[k].gram_units = (uint32_t)gram.size();
-        tasks[k].whole_units = (uint32_t)whole.size();
-        const uint64_t across = t.P / kOrthoPad;
-        gram.insert(gram.end(), across * (across + 1) / 2, k);
-        whole.insert(whole.end(), across * (t.Q / kOrthoPad), k);
-      }
-      t.gram_units = tasks[k].gram_units;
-      t.whole_units = tasks[k].whole_units;
+    for (OrthoTask& t : planes[p]) {
       t.at = at;
       s->need[p].push_back(ortho_places(t.P, t.Q, p + 1).bytes);
       at += s->need[p].back();
@@ -129,27 +141,26 @@ int set_matrices(dadam_handle* h, const dadam_matrix_desc* m, uint32_t n) {
     s->need[p].push_back(at);
   }
   s->tasks = planes[0];
-  s->gram_units = (uint32_t)gram.size();
-  s->whole_units = (uint32_t)whole.size();
+  for (int kind = 0; kind < 3; ++kind) s->n_units[kind] = (uint32_t)of_unit[kind].size();
   if (h->cfg.device != DADAM_DEVICE_NONE && n) {
     DeviceGuard guard(h->cfg.device);
     if (guard.err != hipSuccess) return fail(h, DADAM_EHIP, "hipSetDevice: %s", hipGetErrorString(guard.err));
-    const size_t list = n * sizeof(OrthoTask), g = gram.size() * 4, w = whole.size() * 4;
-    std::vector<char> image(2 * list + g + w);
-    memcpy(image.data(), planes[0].data(), list);
-    memcpy(image.data() + list, planes[1].data(), list);
-    memcpy(image.data() + 2 * list, gram.data(), g);
-    memcpy(image.data() + 2 * list + g, whole.data(), w);
+    std::vector<char> image;
+    auto add = [&image](const auto& v) {
+      const size_t at = image.size();
+      image.resize(at + (v.size() * sizeof(v[0]) + 63) / 64 * 64);
+      memcpy(image.data() + at, v.data(), v.size() * sizeof(v[0]));
+      return at;
+    };
+    size_t at[5] = {add(planes[0]), add(planes[1]), add(of_unit[0]), add(of_unit[1]), add(of_unit[2])};
     hipError_t e = hipMalloc((void**)&s->memory, image.size());
     if (e == hipSuccess) e = hipMemcpy(s->memory, image.data(), image.size(), hipMemcpyHostToDevice);
     if (e != hipSuccess) {
       (void)hipGetLastError();
       return fail(h, DADAM_EHIP, "uploading the matrices failed: %s", hipGetErrorString(e));
     }
-    s->d_tasks[0] = reinterpret_cast<const OrthoTask*>(s->memory);
-    s->d_tasks[1] = s->d_tasks[0] + n;
-    s->d_gram = reinterpret_cast<const uint32_t*>(s->memory + 2 * list);
-    s->d_whole = s->d_gram + gram.size();
+    for (int p = 0; p < 2; ++p) s->d_tasks[p] = reinterpret_cast<const OrthoTask*>(s->memory + at[p]);
+    for (int kind = 0; kind < 3; ++kind) s->d_units[kind] = reinterpret_cast<const uint32_t*>(s->memory + at[2 + kind]);
     MatrixState* old = h->matrices;
     h->matrices = s.release();
     h->free_matrices = free_matrices;
@@ -217,24 +228,29 @@ struct Call {
 int run_group(dadam_handle* h, const Call& call, const Powers& pw, uint32_t k0, uint32_t k1, uint32_t i0, uint32_t replicas, void* stream) {
   const MatrixState& m = *h->matrices;
   const uint32_t planes = planes_of(call.dtype), n = (uint32_t)m.tasks.size();
-  auto units = [&](bool gram, uint32_t* first) {
-    auto before = [&](uint32_t k) { return gram ? (k < n ? m.tasks[k].gram_units : m.gram_units) : (k < n ? m.tasks[k].whole_units : m.whole_units); };
-    *first = before(k0);
-    return before(k1) - before(k0);
-  };
-  OrthoSpan gram{}, whole{};
-  gram.tasks = m.d_tasks[planes - 1];
-  gram.workspace = (uint64_t)(uintptr_t)call.workspace;
-  for (uint32_t k = 0; k < k0; ++k) gram.before += m.need[planes - 1][k];
-  for (uint32_t k = k0; k < k1; ++k) gram.stride += m.need[planes - 1][k];
-  gram.n_xcd = h->n_xcds;
-  whole = gram;
-  gram.units = m.d_gram;
-  whole.units = m.d_whole;
-  const uint32_t gram_units = units(true, &gram.first_unit), whole_units = units(false, &whole.first_unit);
+  OrthoSpan spans[3] = {};
+  uint32_t units[3];
+  for (int kind = 0; kind < 3; ++kind) {
+    auto before = [&](uint32_t k) {
+      if (k == n) return m.n_units[kind];
+      const OrthoTask& t = m.tasks[k];
+      return kind == 0 ? t.gram_units : kind == 1 ? t.whole_units : t.cell_units;
+    };
+    OrthoSpan& s = spans[kind];
+    s.tasks = m.d_tasks[planes - 1];
+    s.units = m.d_units[kind];
+    s.workspace = (uint64_t)(uintptr_t)call.workspace;
+    for (uint32_t k = 0; k < k0; ++k) s.before += m.need[planes - 1][k];
+    for (uint32_t k = k0; k < k1; ++k) s.stride += m.need[planes - 1][k];
+    s.first_unit = before(k0);
+    s.n_xcd = h->n_xcds;
+    units[kind] = before(k1) - s.first_unit;
+  }
+  const OrthoSpan &gram = spans[0], &whole = spans[1];
+  const uint32_t gram_units = units[0], whole_units = units[1], edge = m.tasks[k0].edge;
   OrthoBeginArgs<kMaxRows> begin;
   memset((void*)&begin, 0, sizeof(begin));
-  begin.s = whole;
+  begin.s = spans[2];
   for (uint32_t r = 0; r < replicas; ++r) {
     begin.grad[r] = call.grads[i0 + r];
     if (call.source == kOrthoGiven) continue;
@@ -245,8 +261,8 @@ int run_group(dadam_handle* h, const Call& call, const Powers& pw, uint32_t k0, 
   begin.scale = std::ldexp(1.f, pw.x[0]);
   begin.source = call.source;
   begin.phase = call.phase;
-  int e = launch_ortho_norm((int)h->cfg.grad_dtype, begin, planes, whole_units, replicas, stream);
-  if (!e) e = launch_ortho_begin((int)h->cfg.grad_dtype, begin, planes, whole_units, replicas, stream);
+  int e = launch_ortho_norm((int)h->cfg.grad_dtype, begin, planes, units[2], replicas, stream);
+  if (!e) e = launch_ortho_begin((int)h->cfg.grad_dtype, begin, planes, units[2], replicas, stream);
   const size_t steps = pw.x.size();
   for (size_t k = 0; k < steps && !e; ++k) {
     const float a = m.coefficients[3 * k], b = m.coefficients[3 * k + 1], c = m.coefficients[3 * k + 2];
@@ -254,10 +270,10 @@ int run_group(dadam_handle* h, const Call& call, const Powers& pw, uint32_t k0, 
     OrthoStepArgs s{};
     s.s = gram;
     s.fresh = std::ldexp(1.f, pa - 2 * x);
-    e = launch_ortho_gram(false, s, planes, gram_units, replicas, stream);
+    e = launch_ortho_gram(false, edge, s, planes, gram_units, replicas, stream);
     s.gain = std::ldexp(b, pb - pa);
     s.fresh = std::ldexp(c, pb - 2 * pa);
-    if (!e) e = launch_ortho_gram(true, s, planes, gram_units, replicas, stream);
+    if (!e) e = launch_ortho_gram(true, edge, s, planes, gram_units, replicas, stream);
     if (e) break;
     s.s = whole;
     s.from = (uint32_t)(k & 1);
@@ -265,7 +281,7 @@ int run_group(dadam_handle* h, const Call& call, const Powers& pw, uint32_t k0, 
     if (k + 1 < steps) {
       s.gain = std::ldexp(a, pw.x[k + 1] - x);
       s.fresh = std::ldexp(1.f, pw.x[k + 1] - x - pb);
-      e = launch_ortho_next(s, planes, whole_units, replicas, stream);
+      e = launch_ortho_next(edge, s, planes, whole_units, replicas, stream);
       continue;
     }
     OrthoEndArgs<kMaxRows> end;
@@ -285,7 +301,7 @@ int run_group(dadam_handle* h, const Call& call, const Powers& pw, uint32_t k0, 
       end.first_row = i0;
       end.lr = call.c.lr;
     }
-    e = launch_ortho_end((int)call.dtype, end, h->cfg.n_cols, planes, whole_units, replicas, stream);
+    e = launch_ortho_end((int)call.dtype, edge, end, h->cfg.n_cols, whole_units, replicas, stream);
   }
   return e;
 }
@@ -306,14 +322,15 @@ int run(dadam_handle* h, const Call& call, void* stream) {
   Powers pw;
   (void)find_powers(h->matrices->coefficients, &pw);
   const std::vector<uint64_t>& need = h->matrices->need[planes_of(call.dtype) - 1];
-  const uint32_t n = (uint32_t)h->matrices->tasks.size(), R = h->cfg.n_rows;
+  const std::vector<OrthoTask>& tasks = h->matrices->tasks;
+  const uint32_t n = (uint32_t)tasks.size(), R = h->cfg.n_rows;
   DeviceGuard guard(h->cfg.device);
   if (guard.err != hipSuccess) return fail(h, DADAM_EHIP, "hipSetDevice: %s", hipGetErrorString(guard.err));
   int e = (int)hipSuccess;
   for (uint32_t k = 0; k < n && !e;) {
     uint32_t end = k;
     uint64_t bytes = 0;
-    while (end < n && (bytes + need[end]) * R <= call.bytes) bytes += need[end++];
+    while (end < n && tasks[end].edge == tasks[k].edge && (bytes + need[end]) * R <= call.bytes) bytes += need[end++];
     if (end > k) {
       e = run_group(h, call, pw, k, end, 0, R, stream);
     } else {  // one matrix, as many replicas as there is room for

@@ -8,33 +8,36 @@
 
 namespace dadam {
 
-constexpr uint32_t kOrthoPad = 128;  // rows and columns of operands are filled up to a multiple of this
+constexpr uint32_t kOrthoCell = 128;               // side of the tiles that the iteration's beginning goes by
+constexpr uint32_t kSmallEdge = 128, kLargeEdge = 256;  // sides of the products' tiles
 
 // One matrix, the same for every replica.  X has p rows and q >= p columns: the matrix itself, or its transpose where it is tall.
 struct OrthoTask {
   uint64_t first;        // its first element in the packed vector
   uint64_t at;           // bytes of workspace of the matrices before it, for one replica
   uint32_t ld;           // elements from row to row
-  uint32_t p, q, P, Q;   // P, Q: filled up
+  uint32_t p, q, P, Q;   // P, Q: filled up to a multiple of the products' tiles
   uint32_t tall;
-  uint32_t gram_units, whole_units;  // tiles of the matrices before it: of the lower half of P x P, and of P x Q
+  uint32_t gram_units, whole_units, cell_units;  // tiles of the matrices before it: of the lower half of P x P, of P x Q, and cells of P x Q
   float scale, decay;
+  uint32_t edge;         // of the products' tiles
 };
 
-// Workspace of a matrix, one replica: X, twice its transpose (with what one half leaves of it behind, see k_ortho_next), A = X X^T,
+// Workspace of a matrix, one replica: X, with one plane what the half leaves of it (see dadam_ortho.hip), twice its transpose, A = X X^T,
 // B = b A + c A A, partial sums of the norm.
 struct OrthoPlaces {
-  uint64_t x, turned[2], a, b, sums, bytes;
+  uint64_t x, low, turned[2], a, b, sums, bytes;
 };
 inline constexpr OrthoPlaces ortho_places(uint64_t P, uint64_t Q, uint64_t planes) {
   OrthoPlaces w{};
   uint64_t at = 0;
   w.x = at, at += P * Q * 2 * planes;
-  w.turned[0] = at, at += P * Q * 4;
-  w.turned[1] = at, at += P * Q * 4;
+  w.low = at, at += planes == 1 ? P * Q * 2 : 0;
+  w.turned[0] = at, at += P * Q * 2 * planes;
+  w.turned[1] = at, at += P * Q * 2 * planes;
   w.a = at, at += P * P * 2 * planes;
   w.b = at, at += P * P * 2 * planes;
-  w.sums = at, at += ((P / kOrthoPad) * (Q / kOrthoPad) * 8 + 255) / 256 * 256;
+  w.sums = at, at += ((P / kOrthoCell) * (Q / kOrthoCell) * 8 + 255) / 256 * 256;
   w.bytes = at;
   return w;
 }
@@ -87,12 +90,12 @@ struct OrthoEndArgs {
 constexpr int kOrthoFew = 16;
 static_assert(sizeof(OrthoBeginArgs<kMaxRows>) <= 4096 && sizeof(OrthoEndArgs<kMaxRows>) <= 4096, "the argument block of a launch holds 4 KB");
 
-// Launchers.  units: tiles of the group, replicas: of the group.  planes: 1 or 2 (see dadam_mfma.h).
+// Launchers.  units: tiles of the group, replicas: of the group.  planes: 1 or 2 (see dadam_mfma.h); of launch_ortho_end 1 for bfloat16, 2 for float32.
 int launch_ortho_norm(int gdt, const OrthoBeginArgs<kMaxRows>& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream);
 int launch_ortho_begin(int gdt, const OrthoBeginArgs<kMaxRows>& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream);
-int launch_ortho_gram(bool square, const OrthoStepArgs& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream);
-int launch_ortho_next(const OrthoStepArgs& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream);
-int launch_ortho_end(int dtype, const OrthoEndArgs<kMaxRows>& a, uint32_t n_cols, uint32_t planes, uint32_t units, uint32_t replicas, void* stream);
+int launch_ortho_gram(bool square, uint32_t edge, const OrthoStepArgs& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream);
+int launch_ortho_next(uint32_t edge, const OrthoStepArgs& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream);
+int launch_ortho_end(int dtype, uint32_t edge, const OrthoEndArgs<kMaxRows>& a, uint32_t n_cols, uint32_t units, uint32_t replicas, void* stream);
 
 }  // namespace dadam
 

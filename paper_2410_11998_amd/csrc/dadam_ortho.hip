@@ -10,6 +10,8 @@
 // fall.  For bfloat16 results one half is enough in the products, but not for X itself: what X loses to 11 bits in the directions of small singular
 // values grows by a = 3.4 an iteration, 1e-3 of the result for equal singular values, 1.4e-2 for ones that fall by 1000 in 50.  a X is therefore taken
 // from two halves as well (1.4e-3 and 5e-4), the second of which no product reads.
+#include <type_traits>
+
 #include "dadam_mfma.h"
 #include "dadam_ortho.h"
 
@@ -18,33 +20,8 @@ namespace {
 
 extern __shared__ char ortho_lds[];
 
-template <int PLANES>
-using OrthoTile = Tile<Half, PLANES, 2, 2, 2, 2>;
-
-// The turned copy of X: Q rows of P, the operand, and with one plane what the half leaves as a second array behind it.
-template <int PLANES>
-__device__ __forceinline__ void store_turned4(uint64_t base, const OrthoTask& t, uint32_t q, uint32_t p, const float4v& v) {
-  store4<Half, PLANES>(base, q, t.P, p, v);
-  if constexpr (PLANES == 1) {
-    uint32_t h, l[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) halves<Half>(v[e], h, l[e]);
-    global<uint2v>(base + ((uint64_t)t.Q * t.P + (uint64_t)q * t.P + p) * 2)[0] = four(l);
-  }
-}
-template <int PLANES>
-__device__ __forceinline__ float4v load_turned4(uint64_t base, const OrthoTask& t, uint32_t q, uint32_t p) {
-  float4v v = load4<Half, PLANES>(base, q, t.P, p);
-  if constexpr (PLANES == 1) v += load4<Half, 1>(base + (uint64_t)t.Q * t.P * 2, q, t.P, p);
-  return v;
-}
-template <int PLANES>
-__device__ __forceinline__ float load_turned1(uint64_t base, const OrthoTask& t, uint32_t q, uint32_t p) {
-  const uint64_t e = (uint64_t)q * t.P + p;
-  if constexpr (PLANES == 1) return Half::value(global<const uint16_t>(base)[e]) + Half::value(global<const uint16_t>(base)[(uint64_t)t.Q * t.P + e]);
-  const uint64_t at = (uint64_t)q * t.P * 2 + high_at(p);
-  return Half::value(global<const uint16_t>(base)[at]) + Half::value(global<const uint16_t>(base)[at + 32]);
-}
+template <int PLANES, int EDGE>
+using OrthoTile = typename std::conditional<EDGE == (int)kLargeEdge, LargeTile<Half, PLANES>, SmallTile<Half, PLANES>>::type;
 
 // A workgroup's matrix, the tile of it and where its workspace begins.
 struct Unit {
@@ -52,7 +29,8 @@ struct Unit {
   uint32_t tile;
   uint64_t base;
 };
-template <bool GRAM>
+enum Kind : int { kGram = 0, kWhole = 1, kCells = 2 };
+template <Kind KIND>
 __device__ __forceinline__ Unit find_unit(const OrthoSpan& s) {
   const uint32_t u = s.first_unit + die_run(blockIdx.x, gridDim.x, s.n_xcd);
   const uint32_t k = global<const uint32_t>(s.units)[u];
@@ -63,20 +41,20 @@ __device__ __forceinline__ Unit find_unit(const OrthoSpan& s) {
 #pragma unroll
   for (uint32_t i = 0; i < sizeof(OrthoTask) / 4; ++i) words.w[i] = global<const uint32_t>(s.tasks + k)[i];
   r.t = __builtin_bit_cast(OrthoTask, words);
-  r.tile = u - (GRAM ? r.t.gram_units : r.t.whole_units);
+  r.tile = u - (KIND == kGram ? r.t.gram_units : KIND == kWhole ? r.t.whole_units : r.t.cell_units);
   r.base = s.workspace + (uint64_t)blockIdx.y * s.stride + (r.t.at - s.before);
   return r;
 }
 
-// Where a tile of X begins in the matrix as it lies in memory, and the matrix's own rows and columns.
+// Where a cell of X begins in the matrix as it lies in memory, and the matrix's own rows and columns.
 struct Cell {
   uint32_t r0, c0, rows, cols;
 };
 __device__ __forceinline__ Cell cell_of(const Unit& u) {
-  const uint32_t across = u.t.Q / kOrthoPad, i = u.tile / across, j = u.tile % across;
+  const uint32_t across = u.t.Q / kOrthoCell, i = u.tile / across, j = u.tile % across;
   Cell c;
-  c.r0 = (u.t.tall ? j : i) * kOrthoPad;
-  c.c0 = (u.t.tall ? i : j) * kOrthoPad;
+  c.r0 = (u.t.tall ? j : i) * kOrthoCell;
+  c.c0 = (u.t.tall ? i : j) * kOrthoCell;
   c.rows = u.t.tall ? u.t.q : u.t.p;
   c.cols = u.t.tall ? u.t.p : u.t.q;
   return c;
@@ -89,20 +67,28 @@ __device__ __forceinline__ float source_value(const Scalars& c, uint32_t source,
   return source == kOrthoMoment ? m : fmaf(c.beta1, m, c.omb1 * g);
 }
 
-// Squares of a tile, in 64 bits, to the tile's place among the matrix's partial sums.
+// Elements of a row of the matrix from column `col` on.
+__device__ __forceinline__ uint32_t left(uint32_t cols, uint32_t col) { return col < cols ? cols - col : 0; }
+
+// Squares of a cell, in 64 bits, to its place among the matrix's partial sums.
 template <typename GT, int PLANES, int N>
 __global__ __launch_bounds__(256) void k_ortho_norm(OrthoBeginArgs<N> a) {
-  const Unit u = find_unit<false>(a.s);
+  const Unit u = find_unit<kCells>(a.s);
   const Cell c = cell_of(u);
-  const uint32_t row = blockIdx.y;
+  const uint32_t row = blockIdx.y, col = c.c0 + threadIdx.x % 16 * 8, n = left(c.cols, col);
   const uint64_t g = (uint64_t)a.grad[row], mh = (uint64_t)a.m_hat[row];
-  const uint32_t lane_col = c.c0 + threadIdx.x % kOrthoPad;
   double sum = 0.0;
-  if (lane_col < c.cols)
-    for (uint32_t r = c.r0 + threadIdx.x / kOrthoPad; r < c.r0 + kOrthoPad && r < c.rows; r += 256 / kOrthoPad) {
-      const uint64_t e = u.t.first + (uint64_t)r * u.t.ld + lane_col;
-      const float v = source_value(a.c, a.source, GT::load(g, e), a.source == kOrthoGiven ? 0.f : F32::load(mh, e));
-      sum += (double)v * (double)v;
+  if (n)
+    for (uint32_t r = c.r0 + threadIdx.x / 16; r < c.r0 + kOrthoCell && r < c.rows; r += 16) {
+      const uint64_t e = u.t.first + (uint64_t)r * u.t.ld + col;
+      float gv[8], m[8] = {};
+      GT::load8(g, e, n, gv);
+      if (a.source != kOrthoGiven) F32::load8(mh, e, n, m);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const double v = (double)source_value(a.c, a.source, gv[k], m[k]);
+        sum = fma(v, v, sum);
+      }
     }
   __shared__ double parts[4];
   sum = wave_sum(sum);
@@ -112,12 +98,12 @@ __global__ __launch_bounds__(256) void k_ortho_norm(OrthoBeginArgs<N> a) {
 }
 
 // X and its transpose from the matrix, and of a step lines 9 to 13 of Algorithm 3 for the first moment and the accumulator.
-constexpr uint32_t kTurnPitch = kOrthoPad + 1;
+constexpr uint32_t kTurnPitch = kOrthoCell + 1;
 template <typename GT, int PLANES, int N>
 __global__ __launch_bounds__(256) void k_ortho_begin(OrthoBeginArgs<N> a) {
-  const Unit u = find_unit<false>(a.s);
+  const Unit u = find_unit<kCells>(a.s);
   const Cell c = cell_of(u);
-  const uint32_t row = blockIdx.y, tiles = (u.t.P / kOrthoPad) * (u.t.Q / kOrthoPad);
+  const uint32_t row = blockIdx.y, tiles = (u.t.P / kOrthoCell) * (u.t.Q / kOrthoCell);
   const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES);
   float DADAM_LDS* tile = (float DADAM_LDS*)ortho_lds;
   __shared__ double parts[4];
@@ -128,45 +114,62 @@ __global__ __launch_bounds__(256) void k_ortho_begin(OrthoBeginArgs<N> a) {
   __syncthreads();
   const float factor = (float)((double)a.scale / (sqrt(parts[0] + parts[1] + parts[2] + parts[3]) + 1e-7));
   const uint64_t g = (uint64_t)a.grad[row], mh = (uint64_t)a.m_hat[row], acc = (uint64_t)a.acc[row];
-  const uint32_t lane_col = threadIdx.x % kOrthoPad, col = c.c0 + lane_col;
-  for (uint32_t r = threadIdx.x / kOrthoPad; r < kOrthoPad; r += 256 / kOrthoPad) {
-    float v = 0.f;
-    if (c.r0 + r < c.rows && col < c.cols) {
-      const uint64_t e = u.t.first + (uint64_t)(c.r0 + r) * u.t.ld + col;
-      const float gv = GT::load(g, e);
-      float m = a.source == kOrthoGiven ? 0.f : F32::load(mh, e);
-      v = source_value(a.c, a.source, gv, m) * factor;
+  const uint32_t k8 = threadIdx.x % 16 * 8, n = left(c.cols, c.c0 + k8);
+  for (uint32_t r = threadIdx.x / 16; r < kOrthoCell; r += 16) {
+    float v[8] = {};
+    if (c.r0 + r < c.rows && n) {
+      const uint64_t e = u.t.first + (uint64_t)(c.r0 + r) * u.t.ld + c.c0 + k8;
+      float gv[8], m[8] = {};
+      GT::load8(g, e, n, gv);
+      if (a.source != kOrthoGiven) F32::load8(mh, e, n, m);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = source_value(a.c, a.source, gv[k], m[k]) * factor;
       if (a.source != kOrthoGiven && a.phase != kUpdateOnly) {
-        float b = gv * a.c.inv_s;
-        if (a.phase == kPlain || a.phase == kFold) b = fmaf(gv, a.c.inv_s, F32::load(acc, e));
-        if (a.phase == kFold || a.phase == kAlg1) F32::store(mh, e, fmaf(a.c.beta1, m, a.c.omb1 * b));
-        if (a.phase != kAlg1) F32::store(acc, e, a.phase == kFold ? 0.f : b);
+        float b[8] = {};
+        if (a.phase == kPlain || a.phase == kFold) F32::load8(acc, e, n, b);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          b[k] = a.phase == kPlain || a.phase == kFold ? fmaf(gv[k], a.c.inv_s, b[k]) : gv[k] * a.c.inv_s;
+          m[k] = fmaf(a.c.beta1, m[k], a.c.omb1 * b[k]);
+          if (a.phase == kFold) b[k] = 0.f;
+        }
+        if (a.phase == kFold || a.phase == kAlg1) F32::store8(mh, e, n, m);
+        if (a.phase != kAlg1) F32::store8(acc, e, n, b);
       }
     }
-    tile[r * kTurnPitch + lane_col] = v;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) tile[r * kTurnPitch + k8 + k] = v[k];
   }
   __syncthreads();
-  // as it lies: rows of four columns; turned: columns of four rows
-  const uint32_t k4 = threadIdx.x % 32 * 4;
-  for (uint32_t r = threadIdx.x / 32; r < kOrthoPad; r += 8) {
-    float4v v, t;
+  // as it lies, and turned
+  for (uint32_t r = threadIdx.x / 16; r < kOrthoCell; r += 16) {
+    uint32_t v[8], t[8];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = tile[r * kTurnPitch + k4 + e], t[e] = tile[(k4 + e) * kTurnPitch + r];
+    for (int k = 0; k < 8; ++k) v[k] = halves<Half>(tile[r * kTurnPitch + k8 + k]), t[k] = halves<Half>(tile[(k8 + k) * kTurnPitch + r]);
+    auto straight = [&](uint32_t p, uint32_t q, const uint32_t (&x)[8]) {
+      store8<PLANES>(u.base + w.x, p, u.t.Q, q, x);
+      if constexpr (PLANES == 1) global<uint4v>(u.base + w.low + ((uint64_t)p * u.t.Q + q) * 2)[0] = highs(x);
+    };
     if (u.t.tall) {
-      store_turned4<PLANES>(u.base + w.turned[0], u.t, c.r0 + r, c.c0 + k4, v);
-      store4<Half, PLANES>(u.base + w.x, c.c0 + r, u.t.Q, c.r0 + k4, t);
+      store8<PLANES>(u.base + w.turned[0], c.r0 + r, u.t.P, c.c0 + k8, v);
+      straight(c.c0 + r, c.r0 + k8, t);
     } else {
-      store4<Half, PLANES>(u.base + w.x, c.r0 + r, u.t.Q, c.c0 + k4, v);
-      store_turned4<PLANES>(u.base + w.turned[0], u.t, c.c0 + r, c.r0 + k4, t);
+      straight(c.r0 + r, c.c0 + k8, v);
+      store8<PLANES>(u.base + w.turned[0], c.c0 + r, u.t.P, c.r0 + k8, t);
     }
   }
 }
 
+__device__ __forceinline__ void to_words(const float (&v)[8], uint32_t (&w)[8]) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(v[k]);
+}
+
 // A tile (i, j), j <= i, of A = X X^T or of B = b A + c A A, and its mirror image.
-template <int PLANES, bool SQUARE>
-__global__ __launch_bounds__(256) void k_ortho_gram(OrthoStepArgs a) {
-  using T = OrthoTile<PLANES>;
-  const Unit u = find_unit<true>(a.s);
+template <int PLANES, int EDGE, bool SQUARE>
+__global__ __launch_bounds__(2 * EDGE) void k_ortho_gram(OrthoStepArgs a) {
+  using T = OrthoTile<PLANES, EDGE>;
+  const Unit u = find_unit<kGram>(a.s);
   const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES);
   uint32_t i = (uint32_t)((sqrtf(8.f * (float)u.tile + 1.f) - 1.f) * 0.5f);  // (the root may round across the border of a row of tiles)
   while (i * (i + 1) / 2 > u.tile) --i;
@@ -174,56 +177,89 @@ __global__ __launch_bounds__(256) void k_ortho_gram(OrthoStepArgs a) {
   const uint32_t j = u.tile - i * (i + 1) / 2, inner = SQUARE ? u.t.P : u.t.Q;
   const uint64_t pitch = (uint64_t)inner * 2 * PLANES;
   const char DADAM_GLOBAL* in = global<const char>(u.base + (SQUARE ? w.a : w.x));
+  char DADAM_LDS* lds = (char DADAM_LDS*)ortho_lds;
   T t;
-  t.product(in + (uint64_t)i * T::kM * pitch, pitch, in + (uint64_t)j * T::kN * pitch, pitch, (uint32_t)(pitch / kStageBytes), (char DADAM_LDS*)ortho_lds);
+  t.product(in + (uint64_t)i * T::kM * pitch, pitch, in + (uint64_t)j * T::kN * pitch, pitch, (uint32_t)(pitch / kStageBytes), lds);
   const uint64_t out = u.base + (SQUARE ? w.b : w.a);
-  t.each([&](uint32_t m, uint32_t n, float4v v) {
-    m += i * T::kM;
-    n += j * T::kN;
-    v *= a.fresh;
-    if constexpr (SQUARE) v += load4<Half, PLANES>(u.base + w.a, n, u.t.P, m) * a.gain;
-    store4<Half, PLANES>(out, n, u.t.P, m, v);
-    if (i != j)
+  t.hand_out(lds, i != j,
+             [&](uint32_t m, uint32_t n, float (&v)[8]) {
+               float held[8] = {};
+               if constexpr (SQUARE) load8<Half, PLANES>(held, u.base + w.a, j * T::kN + n, u.t.P, i * T::kM + m);
+               uint32_t words[8];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) store1<Half, PLANES>(out, m + e, u.t.P, n, v[e]);
-  });
+               for (int k = 0; k < 8; ++k) {
+                 words[k] = halves<Half>(SQUARE ? fmaf(held[k], a.gain, v[k] * a.fresh) : v[k] * a.fresh);
+                 v[k] = __uint_as_float(words[k]);
+               }
+               store8<PLANES>(out, j * T::kN + n, u.t.P, i * T::kM + m, words);
+             },
+             [&](uint32_t m, uint32_t n, const float (&v)[8]) {
+               uint32_t words[8];
+               to_words(v, words);
+               store8<PLANES>(out, i * T::kM + m, u.t.P, j * T::kN + n, words);
+             });
 }
 
-// A tile of a X + B X: rows p of B against columns q of X.
+// X of eight elements, whole.
 template <int PLANES>
-__global__ __launch_bounds__(256) void k_ortho_next(OrthoStepArgs a) {
-  using T = OrthoTile<PLANES>;
-  const Unit u = find_unit<false>(a.s);
-  const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES);
-  const uint32_t across = u.t.Q / T::kN, i = u.tile / across, j = u.tile % across;
-  const uint64_t pitch = (uint64_t)u.t.P * 2 * PLANES, from = u.base + w.turned[a.from], to = u.base + w.turned[a.to];
-  T t;
-  t.product(global<const char>(u.base + w.b) + (uint64_t)i * T::kM * pitch, pitch, global<const char>(from) + (uint64_t)j * T::kN * pitch, pitch,
-            (uint32_t)(pitch / kStageBytes), (char DADAM_LDS*)ortho_lds);
-  t.each([&](uint32_t m, uint32_t n, float4v v) {
-    m += i * T::kM;
-    n += j * T::kN;
-    v = load_turned4<PLANES>(from, u.t, n, m) * a.gain + v * a.fresh;
-    store_turned4<PLANES>(to, u.t, n, m, v);
+__device__ __forceinline__ void load_x(float (&x)[8], uint64_t base, const OrthoPlaces& w, const OrthoTask& t, uint32_t p, uint32_t q) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) store1<Half, PLANES>(u.base + w.x, m + e, u.t.Q, n, v[e]);
-  });
+  for (int k = 0; k < 8; ++k) x[k] = 0.f;
+  load8<Half, PLANES>(x, base + w.x, p, t.Q, q);
+  if constexpr (PLANES == 1) add8<Half>(x, base + w.low + ((uint64_t)p * t.Q + q) * 2);
 }
 
-// The last iteration's tile, straight into the result: rows of the matrix as it lies in memory are the tile's rows, so of a tall one rows q of X
-// against columns p of B (its own transpose).
-template <typename DT, int PLANES, int N>
-__global__ __launch_bounds__(256) void k_ortho_end(OrthoEndArgs<N> a) {
-  using T = OrthoTile<PLANES>;
-  const Unit u = find_unit<false>(a.s);
+// The product of a tile of a X + B X, transposed: rows q of X's transpose against rows p of B (its own).
+template <typename T, int PLANES>
+__device__ __forceinline__ void next_product(T& t, const Unit& u, const OrthoPlaces& w, uint32_t from, uint32_t& q0, uint32_t& p0, char DADAM_LDS* lds) {
+  const uint32_t across = u.t.P / T::kN;
+  q0 = u.tile / across * T::kM;
+  p0 = u.tile % across * T::kN;
+  const uint64_t pitch = (uint64_t)u.t.P * 2 * PLANES;
+  t.product(global<const char>(u.base + (from ? w.turned[1] : w.turned[0])) + q0 * pitch, pitch, global<const char>(u.base + w.b) + p0 * pitch, pitch, (uint32_t)(pitch / kStageBytes), lds);
+}
+
+// X of the next iteration in place of this one's, and its transpose to the other copy.
+template <int PLANES, int EDGE>
+__global__ __launch_bounds__(2 * EDGE) void k_ortho_next(OrthoStepArgs a) {
+  using T = OrthoTile<PLANES, EDGE>;
+  const Unit u = find_unit<kWhole>(a.s);
   const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES);
-  const Cell c = cell_of(u);
-  const uint64_t pitch = (uint64_t)u.t.P * 2 * PLANES, from = u.base + w.turned[a.from], b = u.base + w.b;
-  const char DADAM_GLOBAL* rows = global<const char>(u.t.tall ? from : b);
-  const char DADAM_GLOBAL* cols = global<const char>(u.t.tall ? b : from);
+  char DADAM_LDS* lds = (char DADAM_LDS*)ortho_lds;
+  uint32_t q0, p0;
   T t;
-  t.product(rows + c.r0 * pitch, pitch, cols + c.c0 * pitch, pitch, (uint32_t)(pitch / kStageBytes), (char DADAM_LDS*)ortho_lds);
-  const uint32_t replica = blockIdx.y;
+  next_product<T, PLANES>(t, u, w, a.from, q0, p0, lds);
+  t.hand_out(lds, true,
+             [&](uint32_t m, uint32_t n, float (&v)[8]) {
+               float x[8];
+               load_x<PLANES>(x, u.base, w, u.t, p0 + n, q0 + m);
+               uint32_t words[8];
+#pragma unroll
+               for (int k = 0; k < 8; ++k) {
+                 words[k] = halves<Half>(fmaf(x[k], a.gain, v[k] * a.fresh));
+                 v[k] = __uint_as_float(words[k]);
+               }
+               store8<PLANES>(u.base + w.x, p0 + n, u.t.Q, q0 + m, words);
+               if constexpr (PLANES == 1) global<uint4v>(u.base + w.low + ((uint64_t)(p0 + n) * u.t.Q + q0 + m) * 2)[0] = highs(words);
+             },
+             [&](uint32_t m, uint32_t n, const float (&v)[8]) {
+               uint32_t words[8];
+               to_words(v, words);
+               store8<PLANES>(u.base + (a.to ? w.turned[1] : w.turned[0]), q0 + m, u.t.P, p0 + n, words);
+             });
+}
+
+// The last iteration, straight into the result: the matrix, or the parameters mixed and moved along it.
+template <typename DT, int PLANES, int EDGE, int N>
+__global__ __launch_bounds__(2 * EDGE) void k_ortho_end(OrthoEndArgs<N> a) {
+  using T = OrthoTile<PLANES, EDGE>;
+  const Unit u = find_unit<kWhole>(a.s);
+  const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES);
+  char DADAM_LDS* lds = (char DADAM_LDS*)ortho_lds;
+  uint32_t q0, p0;
+  T t;
+  next_product<T, PLANES>(t, u, w, a.from, q0, p0, lds);
+  const uint32_t replica = blockIdx.y, rows = u.t.tall ? u.t.q : u.t.p, cols = u.t.tall ? u.t.p : u.t.q;
   const uint64_t out = (uint64_t)a.out[replica];
   int32_t first = 0, last = 0;
   uint64_t own = 0;
@@ -232,42 +268,41 @@ __global__ __launch_bounds__(256) void k_ortho_end(OrthoEndArgs<N> a) {
     last = global<const int32_t>(a.row_ptr)[a.first_row + replica + 1];
     own = (uint64_t)a.x_src[a.first_row + replica];
   }
-  t.each([&](uint32_t m, uint32_t n, float4v v) {
-    m += c.r0;
-    n += c.c0;
-    if (u.t.tall) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = load_turned1<PLANES>(from, u.t, m + e, n) * a.gain + v[e] * a.fresh;
-    } else {
-      v = load_turned4<PLANES>(from, u.t, n, m) * a.gain + v * a.fresh;
+  // elements (r, c) ... of the matrix as it lies
+  auto finish = [&](uint32_t r, uint32_t c, const float (&v)[8]) {
+    const uint32_t n = r < rows ? left(cols, c) : 0;
+    if (n == 0) return;
+    const uint64_t e = u.t.first + (uint64_t)r * u.t.ld + c;
+    if (!a.mix) {
+      DT::store8(out, e, n, v);
+      return;
     }
-    if (n >= c.cols) return;
-    const uint64_t at = u.t.first + (uint64_t)m * u.t.ld + n;
+    float mixed[8], x[8];
+    for (int32_t k = first; k < last; ++k) {
+      const float weight = global<const float>(a.w)[k];
+      DT::load8((uint64_t)a.x_src[global<const int32_t>(a.col)[k]], e, n, x);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (m + e >= c.rows) continue;
-      const uint64_t x = at + (uint64_t)e * u.t.ld;
-      float r = v[e];
-      if (a.mix) {
-        float mixed = 0.f;
-        for (int32_t k = first; k < last; ++k) {
-          const float weight = global<const float>(a.w)[k], value = DT::load((uint64_t)a.x_src[global<const int32_t>(a.col)[k]], x);
-          mixed = k == first ? weight * value : fmaf(weight, value, mixed);
-        }
-        float direction = u.t.scale * r;
-        if (u.t.decay != 0.f) direction = fmaf(u.t.decay, DT::load(own, x), direction);
-        r = fmaf(-a.lr, direction, mixed);
-      }
-      DT::store(out, x, r);
+      for (int i = 0; i < 8; ++i) mixed[i] = k == first ? weight * x[i] : fmaf(weight, x[i], mixed[i]);
     }
-  });
+    if (u.t.decay != 0.f) DT::load8(own, e, n, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float direction = u.t.scale * v[i];
+      if (u.t.decay != 0.f) direction = fmaf(u.t.decay, x[i], direction);
+      mixed[i] = fmaf(-a.lr, direction, mixed[i]);
+    }
+    DT::store8(out, e, n, mixed);
+  };
+  t.hand_out(lds, u.t.tall,
+             [&](uint32_t m, uint32_t n, float (&v)[8]) {
+               float x[8];
+               load_x<PLANES>(x, u.base, w, u.t, p0 + n, q0 + m);
+#pragma unroll
+               for (int k = 0; k < 8; ++k) v[k] = fmaf(x[k], a.gain, v[k] * a.fresh);
+               if (!u.t.tall) finish(p0 + n, q0 + m, v);
+             },
+             [&](uint32_t m, uint32_t n, const float (&v)[8]) { finish(q0 + m, p0 + n, v); });
 }
-
-template <typename K>
-int reserve(K kernel, int bytes) {
-  return bytes <= 65536 ? (int)hipSuccess : (int)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-}
-
 
 template <int N>
 OrthoBeginArgs<N> shorter(const OrthoBeginArgs<kMaxRows>& a) {
@@ -284,32 +319,45 @@ OrthoEndArgs<N> shorter(const OrthoEndArgs<kMaxRows>& a) {
   return s;
 }
 
-template <typename K, typename A>
-int launch(K kernel, const A& a, uint32_t units, uint32_t replicas, uint32_t lds, void* stream) {
-  if (const int e = reserve(kernel, (int)lds)) return e;
-  kernel<<<dim3(units, replicas), 256, lds, (hipStream_t)stream>>>(a);
+// Launches KERNEL, whose workgroups take `lds` bytes of LDS: more than 64 KB have to be asked for once on every device.
+template <auto KERNEL, typename A>
+int launch(const A& a, uint32_t threads, uint32_t units, uint32_t replicas, uint32_t lds, void* stream) {
+  if (lds > 65536)
+    if (const int e = ask_for_lds<KERNEL>(lds)) return e;
+  KERNEL<<<dim3(units, replicas), threads, lds, (hipStream_t)stream>>>(a);
   return (int)hipGetLastError();
 }
 
 template <typename GT, int PLANES>
 int begin(bool norm, const OrthoBeginArgs<kMaxRows>& a, uint32_t units, uint32_t replicas, void* stream) {
-  const uint32_t lds = kOrthoPad * kTurnPitch * 4;
+  const uint32_t lds = kOrthoCell * kTurnPitch * 4;
   if (replicas <= (uint32_t)kOrthoFew) {
     const OrthoBeginArgs<kOrthoFew> s = shorter<kOrthoFew>(a);
-    return norm ? launch(k_ortho_norm<GT, PLANES, kOrthoFew>, s, units, replicas, 0, stream) : launch(k_ortho_begin<GT, PLANES, kOrthoFew>, s, units, replicas, lds, stream);
+    return norm ? launch<k_ortho_norm<GT, PLANES, kOrthoFew>>(s, 256, units, replicas, 0, stream) : launch<k_ortho_begin<GT, PLANES, kOrthoFew>>(s, 256, units, replicas, lds, stream);
   }
-  return norm ? launch(k_ortho_norm<GT, PLANES, kMaxRows>, a, units, replicas, 0, stream) : launch(k_ortho_begin<GT, PLANES, kMaxRows>, a, units, replicas, lds, stream);
+  return norm ? launch<k_ortho_norm<GT, PLANES, kMaxRows>>(a, 256, units, replicas, 0, stream) : launch<k_ortho_begin<GT, PLANES, kMaxRows>>(a, 256, units, replicas, lds, stream);
 }
 int begin_any(bool norm, int gdt, const OrthoBeginArgs<kMaxRows>& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream) {
   if (gdt == (int)DADAM_F32) return planes == 1 ? begin<F32, 1>(norm, a, units, replicas, stream) : begin<F32, 2>(norm, a, units, replicas, stream);
   return planes == 1 ? begin<B16, 1>(norm, a, units, replicas, stream) : begin<B16, 2>(norm, a, units, replicas, stream);
 }
 
-template <typename DT, int PLANES>
+template <int PLANES, int EDGE>
+int gram(bool square, const OrthoStepArgs& a, uint32_t units, uint32_t replicas, void* stream) {
+  using T = OrthoTile<PLANES, EDGE>;
+  return square ? launch<k_ortho_gram<PLANES, EDGE, true>>(a, T::kThreads, units, replicas, T::kLds, stream) : launch<k_ortho_gram<PLANES, EDGE, false>>(a, T::kThreads, units, replicas, T::kLds, stream);
+}
+template <int PLANES, int EDGE>
+int next(const OrthoStepArgs& a, uint32_t units, uint32_t replicas, void* stream) {
+  using T = OrthoTile<PLANES, EDGE>;
+  return launch<k_ortho_next<PLANES, EDGE>>(a, T::kThreads, units, replicas, T::kLds, stream);
+}
+template <typename DT, int PLANES, int EDGE>
 int end(const OrthoEndArgs<kMaxRows>& a, uint32_t n_cols, uint32_t units, uint32_t replicas, void* stream) {
-  const uint32_t lds = OrthoTile<PLANES>::kLds;
-  if (replicas <= (uint32_t)kOrthoFew && n_cols <= (uint32_t)kOrthoFew) return launch(k_ortho_end<DT, PLANES, kOrthoFew>, shorter<kOrthoFew>(a), units, replicas, lds, stream);
-  return launch(k_ortho_end<DT, PLANES, kMaxRows>, a, units, replicas, lds, stream);
+  using T = OrthoTile<PLANES, EDGE>;
+  if (replicas <= (uint32_t)kOrthoFew && n_cols <= (uint32_t)kOrthoFew)
+    return launch<k_ortho_end<DT, PLANES, EDGE, kOrthoFew>>(shorter<kOrthoFew>(a), T::kThreads, units, replicas, T::kLds, stream);
+  return launch<k_ortho_end<DT, PLANES, EDGE, kMaxRows>>(a, T::kThreads, units, replicas, T::kLds, stream);
 }
 
 }  // namespace
@@ -320,18 +368,18 @@ int launch_ortho_norm(int gdt, const OrthoBeginArgs<kMaxRows>& a, uint32_t plane
 int launch_ortho_begin(int gdt, const OrthoBeginArgs<kMaxRows>& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream) {
   return begin_any(false, gdt, a, planes, units, replicas, stream);
 }
-int launch_ortho_gram(bool square, const OrthoStepArgs& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream) {
-  if (planes == 1) return launch(square ? k_ortho_gram<1, true> : k_ortho_gram<1, false>, a, units, replicas, OrthoTile<1>::kLds, stream);
-  return launch(square ? k_ortho_gram<2, true> : k_ortho_gram<2, false>, a, units, replicas, OrthoTile<2>::kLds, stream);
+int launch_ortho_gram(bool square, uint32_t edge, const OrthoStepArgs& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream) {
+  if (edge == kLargeEdge) return planes == 1 ? gram<1, 256>(square, a, units, replicas, stream) : gram<2, 256>(square, a, units, replicas, stream);
+  return planes == 1 ? gram<1, 128>(square, a, units, replicas, stream) : gram<2, 128>(square, a, units, replicas, stream);
 }
-int launch_ortho_next(const OrthoStepArgs& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream) {
-  return planes == 1 ? launch(k_ortho_next<1>, a, units, replicas, OrthoTile<1>::kLds, stream) : launch(k_ortho_next<2>, a, units, replicas, OrthoTile<2>::kLds, stream);
+int launch_ortho_next(uint32_t edge, const OrthoStepArgs& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream) {
+  if (edge == kLargeEdge) return planes == 1 ? next<1, 256>(a, units, replicas, stream) : next<2, 256>(a, units, replicas, stream);
+  return planes == 1 ? next<1, 128>(a, units, replicas, stream) : next<2, 128>(a, units, replicas, stream);
 }
-int launch_ortho_end(int dtype, const OrthoEndArgs<kMaxRows>& a, uint32_t n_cols, uint32_t planes, uint32_t units, uint32_t replicas, void* stream) {
-  // one plane where the result is bfloat16 (see the top)
-  if (dtype == (int)DADAM_F32) return end<F32, 2>(a, n_cols, units, replicas, stream);
-  (void)planes;
-  return end<B16, 1>(a, n_cols, units, replicas, stream);
+int launch_ortho_end(int dtype, uint32_t edge, const OrthoEndArgs<kMaxRows>& a, uint32_t n_cols, uint32_t units, uint32_t replicas, void* stream) {
+  if (edge == kLargeEdge)
+    return dtype == (int)DADAM_F32 ? end<F32, 2, 256>(a, n_cols, units, replicas, stream) : end<B16, 1, 256>(a, n_cols, units, replicas, stream);
+  return dtype == (int)DADAM_F32 ? end<F32, 2, 128>(a, n_cols, units, replicas, stream) : end<B16, 1, 128>(a, n_cols, units, replicas, stream);
 }
 
 }  // namespace dadam
