@@ -113,17 +113,17 @@ int run_rows(const dadam_handle* h, HeadArgs a, bool dhidden, bool dhead, bool d
     a.later = k > 0;
   };
   int e = launch_head_begin(x, g, a, rows, stream);
-  if (!e && (gradient || !a.straight)) e = launch_head_hidden(x, g, gradient, a, rows, stream);
+  if (!e) e = launch_head_hidden(x, g, a, rows, stream);
   for (uint32_t k = 0; k < pieces && !e; ++k) {
     piece(k);
-    if (!a.straight) e = launch_head_words(x, g, gradient && pieces == 1, a, rows, stream);
+    if (!a.straight) e = launch_head_words(x, g, a, rows, stream);
     if (!e) e = launch_head_logits(x, g, false, a, rows, stream);
   }
   if (!e) e = launch_head_losses(a, rows, stream);
   if (!gradient) return e;
   for (uint32_t k = 0; k < pieces && !e; ++k) {
     piece(k);
-    if (pieces > 1 || a.straight) e = launch_head_words(x, g, true, a, rows, stream);
+    if (pieces > 1 && !a.straight) e = launch_head_words(x, g, a, rows, stream);
     if (!e) e = launch_head_logits(x, g, true, a, rows, stream);
     if (!e && dhead) e = launch_head_dhead(x, g, a, rows, stream);
     if (!e && dbias) e = launch_head_dbias(x, g, a, rows, stream);
@@ -203,13 +203,12 @@ int dadam_head_loss(dadam_handle* h, const dadam_head* head, const void* const* 
       a.mean = (flags & DADAM_HEAD_MEAN) != 0;
       a.add = (flags & DADAM_HEAD_ADD) != 0;
       a.n_xcd = h->n_xcds;
-      a.straight = n_tokens && planes_of(h) == 1 && head->width % 64 == 0 && at * xs % 16 == 0;
+      a.straight = planes_of(h) == 1 && head->width == way.s.D && at * xs % 16 == 0;
       for (uint32_t r = 0; r < rows; ++r) {
         HeadRow& row = a.row[r];
         row.head = (uint64_t)(uintptr_t)params[i + r] + at * xs;
         row.bias = biased ? (uint64_t)(uintptr_t)params[i + r] + bias_at * xs : 0;
         row.hidden = (uint64_t)(uintptr_t)hidden[i + r];
-        a.straight &= row.hidden % 16 == 0;
         row.target = (uint64_t)(uintptr_t)targets[i + r];
         row.nll = nll ? (uint64_t)(uintptr_t)nll[i + r] : 0;
         row.dhidden = dhidden ? (uint64_t)(uintptr_t)dhidden[i + r] : 0;

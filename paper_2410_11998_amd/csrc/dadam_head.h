@@ -15,9 +15,10 @@ struct HeadRow {  // device addresses, 0 where there is none
   uint64_t head, bias, hidden, target, nll, dhidden, dhead, dbias;
 };
 
-// Workspace of a replica.  Operands have `planes` halves or bfloat16s an element; n: rows as they lie, t: the other way round.
+// Workspace of a replica.  Operands have `planes` halves or bfloat16s an element: hidden vectors and a piece of the head by rows of D, softmax - e[target] of a
+// piece by rows of its words, a token each.
 struct HeadPlaces {
-  uint64_t words, lse, hit, stats, hidden_n, hidden_t, head_n, head_t, p_n, p_t, sums, bytes;
+  uint64_t words, lse, hit, stats, hidden, head, p, sums, bytes;
 };
 struct HeadShape {
   uint32_t tokens, vocab, width;
@@ -38,13 +39,10 @@ inline constexpr HeadPlaces head_places(const HeadShape& s, uint64_t planes, boo
   w.lse = take((uint64_t)s.T * 4);
   w.hit = take((uint64_t)s.T * 4);
   w.stats = take((uint64_t)s.slices * s.T * 8);
-  w.hidden_n = take((uint64_t)s.T * s.K * b);
-  w.head_n = take((uint64_t)s.piece * s.K * b);
+  w.hidden = take((uint64_t)s.T * s.D * b);
+  w.head = take((uint64_t)s.piece * s.D * b);
   if (gradient) {
-    w.hidden_t = take((uint64_t)s.D * s.T * b);
-    w.head_t = take((uint64_t)s.D * s.piece * b);
-    w.p_n = take((uint64_t)s.T * s.piece * b);
-    w.p_t = take((uint64_t)s.piece * s.T * b);
+    w.p = take((uint64_t)s.T * s.piece * b);
     w.sums = take((uint64_t)s.splits * s.T * s.D * 4);
   }
   w.bytes = at;
@@ -63,15 +61,15 @@ struct HeadArgs {
   uint32_t first_word, words;  // of the piece
   uint32_t later;       // a piece before this one has begun the sums
   uint32_t n_xcd;
-  uint32_t straight;    // the hidden vectors and the head are operands as they lie, for the products over the width
+  uint32_t straight;    // the head is an operand as it lies
   HeadRow row[kHeadRows];
 };
 static_assert(sizeof(HeadArgs) <= 4096, "the argument block of a launch holds 4 KB");
 
 // Launchers, of `rows` replicas.  xdt: type of parameters and hidden vectors, gdt of gradients; two planes unless both are bfloat16.
 int launch_head_begin(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                   // tokens with a target, powers of two
-int launch_head_hidden(int xdt, int gdt, bool gradient, const HeadArgs& a, uint32_t rows, void* stream);   // operands of the hidden vectors
-int launch_head_words(int xdt, int gdt, bool turned, const HeadArgs& a, uint32_t rows, void* stream);      // operands of a piece of the head
+int launch_head_hidden(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                  // operands of the hidden vectors
+int launch_head_words(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                   // operands of a piece of the head
 int launch_head_logits(int xdt, int gdt, bool gradient, const HeadArgs& a, uint32_t rows, void* stream);   // statistics, or the logits' gradient
 int launch_head_losses(const HeadArgs& a, uint32_t rows, void* stream);
 int launch_head_dhead(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);

@@ -3,16 +3,14 @@
 //
 // The logits never leave the chip.  A first product gives every token the largest logit and the sum of exponentials of some words
 // (k_head_logits), from which k_head_losses makes the logarithm of the sum; a second one recomputes the logits a piece of the vocabulary at a time
-// and stores softmax - e[target] of it, both ways round, as the operand of the two gradient products.  dW of a piece is complete; dh adds up
-// over pieces.  Four products of tokens x vocabulary x width, of which a program that keeps the logits (4 bytes for each, read and written
-// several times) needs three.
+// and stores softmax - e[target] of it, the operand of the two gradient products.  dW of a piece is complete; dh adds up over pieces.  Four products of
+// tokens x vocabulary x width, of which a program that keeps the logits (4 bytes for each, read and written several times) needs three.  All operands
+// lie as they are made: the gradients sum over tokens and over words, so their tiles are turned on the way from LDS to the registers.
 //
 // bfloat16 parameters and gradients: the operands are what is given, softmax - e[target] is rounded to bfloat16, 8 bits relative whatever its size;
 // sums are float32.  Otherwise: two halves an element (dadam_mfma.h), times a power of two by the largest magnitude of the head and of the
 // hidden vectors, so that an element is held to 22 bits or to 2^-39 of the largest.  Tokens without a target: their hidden vectors are taken as zeros,
 // whatever they hold.
-#include <type_traits>
-
 #include "dadam_head.h"
 #include "dadam_mfma.h"
 
@@ -37,9 +35,6 @@ template <>
 struct Types<B16, F32> : Types<F32, F32> {};
 template <>
 struct Types<F32, B16> : Types<F32, F32> {};
-
-template <typename TY, int EDGE>
-using HeadTile = typename std::conditional<EDGE == 256, LargeTile<typename TY::op, TY::planes>, SmallTile<typename TY::op, TY::planes>>::type;
 
 __device__ __forceinline__ uint32_t left(uint32_t n, uint32_t at) { return at < n ? n - at : 0; }
 
@@ -136,89 +131,80 @@ __global__ __launch_bounds__(256) void k_head_most(HeadArgs a) {
   }
 }
 
-// A 64 x 64 tile of a matrix of `rows` rows and `width` columns as operands: as it lies (`plain`, of K columns), and the other way round (`turned`, D rows
-// of `across`); either may be 0.  Beyond the matrix stand zeros.
-constexpr uint32_t kCut = 64, kCutPitch = kCut + 1;
+// `rows` rows of `width` elements as an operand of a.s.D columns, `filled` rows in all; the rest zeros.  A thread takes eight elements.
 template <typename XT, typename TY>
-__device__ __forceinline__ void operands(uint64_t data, uint32_t rows, uint32_t width, float factor, uint64_t plain, uint32_t K, uint64_t turned, uint32_t D,
-                                         uint32_t across, uint64_t target, const HeadArgs& a) {
+__device__ __forceinline__ void make_operand(uint64_t data, uint32_t rows, uint32_t filled, float factor, uint64_t to, uint64_t target, const HeadArgs& a) {
   using OP = typename TY::op;
-  const uint32_t r0 = blockIdx.x * kCut, c0 = blockIdx.y * kCut, k8 = threadIdx.x % 8 * 8;
-  float DADAM_LDS* tile = (float DADAM_LDS*)head_lds;
+  const uint32_t each = a.s.D / 8;
+  const uint64_t e = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  const uint32_t r = (uint32_t)(e / each), c = (uint32_t)(e % each) * 8;
+  if (r >= filled) return;
+  float v[8] = {};
+  int32_t word;
+  const uint32_t n = r < rows ? left(a.s.width, c) : 0;
+  if (n && (!target || has_target(a, target, r, word))) XT::load8(data, (uint64_t)r * a.s.width + c, n, v);
+  uint32_t w[8];
 #pragma unroll
-  for (uint32_t r = threadIdx.x / 8; r < kCut; r += 32) {
-    float v[8] = {};
-    int32_t word;
-    const uint32_t n = left(width, c0 + k8);
-    if (r0 + r < rows && n && (!target || has_target(a, target, r0 + r, word))) XT::load8(data, (uint64_t)(r0 + r) * width + c0 + k8, n, v);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) tile[r * kCutPitch + k8 + k] = v[k] * factor;
-  }
-  __syncthreads();
-#pragma unroll
-  for (uint32_t r = threadIdx.x / 8; r < kCut; r += 32) {
-    uint32_t v[8], t[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      v[k] = operand_word<OP, TY::planes>(tile[r * kCutPitch + k8 + k]);
-      t[k] = operand_word<OP, TY::planes>(tile[(k8 + k) * kCutPitch + r]);
-    }
-    if (plain && c0 < K) store8<TY::planes>(plain, r0 + r, K, c0 + k8, v);
-    if (turned && c0 < D) store8<TY::planes>(turned, c0 + r, across, r0 + k8, t);
-  }
+  for (int k = 0; k < 8; ++k) w[k] = operand_word<OP, TY::planes>(v[k] * factor);
+  store8<TY::planes>(to, r, a.s.D, c, w);
+}
+template <typename XT, typename TY>
+__global__ __launch_bounds__(256) void k_head_hidden(HeadArgs a) {
+  const HeadRow& row = a.row[blockIdx.z];
+  const uint64_t base = base_of(a);
+  make_operand<XT, TY>(row.hidden, a.s.tokens, a.s.T, ldexpf(1.f, power_of<TY>(base, a, kHeadMostHidden)), base + a.w.hidden, row.target, a);
+}
+template <typename XT, typename TY>
+__global__ __launch_bounds__(256) void k_head_words(HeadArgs a) {
+  const HeadRow& row = a.row[blockIdx.z];
+  const uint64_t base = base_of(a), from = row.head + (uint64_t)a.first_word * a.s.width * sizeof(typename XT::type);
+  make_operand<XT, TY>(from, a.words, (a.words + a.s.edge - 1) / a.s.edge * a.s.edge, ldexpf(1.f, power_of<TY>(base, a, kHeadMostHead)), base + a.w.head, 0, a);
 }
 
-template <typename XT, typename TY>
-__global__ __launch_bounds__(256) void k_head_hidden(HeadArgs a, uint32_t gradient) {
-  const HeadRow& row = a.row[blockIdx.z];
-  const uint64_t base = base_of(a);
-  const float factor = ldexpf(1.f, power_of<TY>(base, a, kHeadMostHidden));
-  operands<XT, TY>(row.hidden, a.s.tokens, a.s.width, factor, a.straight ? 0 : base + a.w.hidden_n, a.s.K, gradient ? base + a.w.hidden_t : 0, a.s.D, a.s.T, row.target, a);
-}
-template <typename XT, typename TY>
-__global__ __launch_bounds__(256) void k_head_words(HeadArgs a, uint32_t turned) {
-  const HeadRow& row = a.row[blockIdx.z];
-  const uint64_t base = base_of(a);
-  const float factor = ldexpf(1.f, power_of<TY>(base, a, kHeadMostHead));
-  const uint64_t bytes = sizeof(typename XT::type);
-  operands<XT, TY>(row.head + (uint64_t)a.first_word * a.s.width * bytes, a.words, a.s.width, factor, a.straight ? 0 : base + a.w.head_n, a.s.K, turned ? base + a.w.head_t : 0, a.s.D,
-                   a.s.piece, 0, a);
+// The piece's words as an operand, rows from `row` on: as they lie in the parameters, or their copy.
+template <typename TY>
+__device__ __forceinline__ Operand head_operand(uint64_t base, const HeadRow& row, const HeadArgs& a, uint32_t first, uint64_t offset) {
+  const uint64_t pitch = (uint64_t)a.s.D * 2 * TY::planes;
+  if (a.straight) return operand(row.head + (uint64_t)(a.first_word + first) * pitch + offset, pitch, a.words - first);
+  return operand(base + a.w.head + first * pitch + offset, pitch);
 }
 
 // The logits of a tile of words (m) and tokens (n).  Without gradients: the largest and the sum of exponentials of each wavefront's words, and the
-// target's logit.  With: softmax - e[target], both ways round.
+// target's logit.  With: softmax - e[target].
 template <typename XT, typename TY, int EDGE, bool GRADIENT>
 __global__ __launch_bounds__(2 * EDGE) void k_head_logits(HeadArgs a) {
-  using T = HeadTile<TY, EDGE>;
+  using T = TileOf<typename TY::op, TY::planes, EDGE, false, false>;
   using OP = typename TY::op;
   const HeadRow& row = a.row[blockIdx.z];
   const uint64_t base = base_of(a);
   const uint32_t across = a.s.T / T::kN, u = die_run(blockIdx.x, gridDim.x, a.n_xcd), i = u / across, j = u % across;
   char DADAM_LDS* lds = (char DADAM_LDS*)head_lds;
+  const uint64_t pitch = (uint64_t)a.s.D * 2 * TY::planes;
   T t;
-  if constexpr (TY::planes == 1) {
-    // rows beyond the piece's words and the tokens come to nothing below, whatever stands in them
-    const uint64_t pitch = (uint64_t)a.s.K * 2, head = a.straight ? row.head + (uint64_t)a.first_word * pitch : base + a.w.head_n, hidden = a.straight ? row.hidden : base + a.w.hidden_n;
-    t.template product<true>(global<const char>(head) + (uint64_t)i * T::kM * pitch, pitch, global<const char>(hidden) + (uint64_t)j * T::kN * pitch, pitch,
-                             (uint32_t)(pitch / kStageBytes), lds, a.words - i * T::kM, left(a.s.tokens, j * T::kN) ? a.s.tokens - j * T::kN : 1);
-  } else {
-    const uint64_t pitch = (uint64_t)a.s.K * 4;
-    t.product(global<const char>(base + a.w.head_n) + (uint64_t)i * T::kM * pitch, pitch, global<const char>(base + a.w.hidden_n) + (uint64_t)j * T::kN * pitch, pitch,
-              (uint32_t)(pitch / kStageBytes), lds);
-  }
+  // (words beyond the piece come to nothing below, whatever stands for them)
+  t.product(head_operand<TY>(base, row, a, i * T::kM, 0), operand(base + a.w.hidden + (uint64_t)j * T::kN * pitch, pitch), a.s.K * TY::planes / 64, lds);
   const float held = ldexpf(1.f, -power_of<TY>(base, a, kHeadMostHidden) - power_of<TY>(base, a, kHeadMostHead));
   if constexpr (GRADIENT) {
-    t.hand_out(lds, true,
-               [&](uint32_t m, uint32_t n, float (&v)[8]) {
+    struct Token {
+      int32_t target;  // -1: none
+      float lse;
+    };
+    t.hand_out(lds, false,
+               [&](uint32_t, uint32_t n) {
+                 Token x;
+                 if (!has_target(a, row.target, j * T::kN + n, x.target)) x.target = -1;
+                 x.lse = global<const float>(base + a.w.lse)[j * T::kN + n];
+                 return x;
+               },
+               [&](uint32_t m, uint32_t n, float (&v)[8], const Token& x) {
                  m += i * T::kM;
                  n += j * T::kN;
-                 int32_t target;
-                 const bool taken = has_target(a, row.target, n, target);
-                 const float lse = taken ? global<const float>(base + a.w.lse)[n] : 0.f;
+                 const bool taken = x.target >= 0;
+                 const float lse = x.lse;
                  const uint32_t words = left(a.words, m);
                  float bias[8] = {};
                  if (row.bias && words) XT::load8(row.bias, a.first_word + m, words, bias);
-                 const uint32_t hit = (uint32_t)target - a.first_word - m;
+                 const uint32_t hit = (uint32_t)x.target - a.first_word - m;
                  uint32_t w[8];
 #pragma unroll
                  for (uint32_t k = 0; k < 8; ++k) {
@@ -226,16 +212,10 @@ __global__ __launch_bounds__(2 * EDGE) void k_head_logits(HeadArgs a) {
                    float p = taken && k < words ? __expf(z) : 0.f;
                    if (taken && k == hit) p = expm1f(z);
                    w[k] = operand_word<OP, TY::planes>(TY::planes == 1 ? p : p * (float)(1 << kHeldAt));
-                   v[k] = __uint_as_float(w[k]);
                  }
-                 store8<TY::planes>(base + a.w.p_n, n, a.s.piece, m, w);
+                 store8<TY::planes>(base + a.w.p, n, a.s.piece, m, w);
                },
-               [&](uint32_t m, uint32_t n, const float (&v)[8]) {
-                 uint32_t w[8];
-#pragma unroll
-                 for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(v[k]);
-                 store8<TY::planes>(base + a.w.p_t, i * T::kM + m, a.s.T, j * T::kN + n, w);
-               });
+               [](uint32_t, uint32_t, const float (&)[8]) {});
   } else {
     constexpr int MT = EDGE == 256 ? 4 : 2, WM = 2, WN = EDGE == 256 ? 4 : 2;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % WM, wn = wave / WM;
@@ -327,21 +307,20 @@ __global__ __launch_bounds__(256) void k_head_sum(HeadArgs a) {
   }
 }
 
-// dW of a tile of columns (m) and words (n).
+// dW of a tile of columns (m) and words (n): both operands lie by tokens.
 template <typename GT, typename TY, int EDGE>
 __global__ __launch_bounds__(2 * EDGE) void k_head_dhead(HeadArgs a) {
-  using T = HeadTile<TY, EDGE>;
+  using T = TileOf<typename TY::op, TY::planes, EDGE, true, true>;
   const HeadRow& row = a.row[blockIdx.z];
   const uint64_t base = base_of(a);
   const uint32_t across = a.s.D / T::kM, u = die_run(blockIdx.x, gridDim.x, a.n_xcd), i = u % across, j = u / across;
-  const uint64_t pitch = (uint64_t)a.s.T * 2 * TY::planes;
+  const uint64_t b = 2 * TY::planes;
   char DADAM_LDS* lds = (char DADAM_LDS*)head_lds;
   T t;
-  t.product(global<const char>(base + a.w.hidden_t) + (uint64_t)i * T::kM * pitch, pitch, global<const char>(base + a.w.p_t) + (uint64_t)j * T::kN * pitch, pitch,
-            (uint32_t)(pitch / kStageBytes), lds);
+  t.product(operand(base + a.w.hidden + i * T::kM * b, a.s.D * b), operand(base + a.w.p + j * T::kN * b, a.s.piece * b), a.s.T * TY::planes / 64, lds);
   const float factor = factor_of(base, a) * (TY::planes == 1 ? 1.f : ldexpf(1.f, -power_of<TY>(base, a, kHeadMostHidden) - kHeldAt));
-  t.hand_out(lds, false,
-             [&](uint32_t m, uint32_t n, float (&v)[8]) {
+  t.hand_out(lds, false, nothing_ahead,
+             [&](uint32_t m, uint32_t n, float (&v)[8], Nothing) {
                m += i * T::kM;
                n += j * T::kN;
                const uint32_t columns = n < a.words ? left(a.s.width, m) : 0;
@@ -356,53 +335,60 @@ __global__ __launch_bounds__(2 * EDGE) void k_head_dhead(HeadArgs a) {
              [](uint32_t, uint32_t, const float (&)[8]) {});
 }
 
-// dbias: a wavefront a word.
+// dbias: 64 words a workgroup, 8 of them a thread; 32 threads share the tokens.
 template <typename GT, typename TY>
 __global__ __launch_bounds__(256) void k_head_dbias(HeadArgs a) {
   using OP = typename TY::op;
   const HeadRow& row = a.row[blockIdx.z];
   const uint64_t base = base_of(a);
-  const uint32_t n = blockIdx.x * 4 + threadIdx.x / 64, lane = threadIdx.x % 64;
-  if (n < a.words) {
-    float sum[8] = {};
-    for (uint32_t t = lane * 8; t < a.s.T; t += 512) load8<OP, TY::planes>(sum, base + a.w.p_t, n, a.s.T, t);
-    float all = ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));
+  const uint32_t k8 = threadIdx.x % 8 * 8, m = blockIdx.x * 64 + k8, part = threadIdx.x / 8;
+  __shared__ float parts[32][65];
+  float sum[8] = {};
+#pragma unroll 4
+  for (uint32_t t = part; t < a.s.T; t += 32) {
+    const Eight p = load8<TY::planes>(base + a.w.p, t, a.s.piece, m);
 #pragma unroll
-    for (int step = 32; step; step >>= 1) all += __shfl_xor(all, step);
-    if (lane == 0) {
-      const float g = all * factor_of(base, a) * (TY::planes == 1 ? 1.f : ldexpf(1.f, -kHeldAt));
-      const uint64_t e = a.first_word + n;
-      GT::store(row.dbias, e, a.add ? GT::load(row.dbias, e) + g : g);
-    }
+    for (int k = 0; k < 8; ++k) sum[k] += value_of<OP, TY::planes == 2>(p, k);
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) parts[part][k8 + k] = sum[k];
+  __syncthreads();
+  const uint32_t n = blockIdx.x * 64 + threadIdx.x;
+  if (threadIdx.x < 64 && n < a.words) {
+    float all = 0.f;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) all += parts[k][threadIdx.x];
+    const float g = all * factor_of(base, a) * (TY::planes == 1 ? 1.f : ldexpf(1.f, -kHeldAt));
+    const uint64_t e = a.first_word + n;
+    GT::store(row.dbias, e, a.add ? GT::load(row.dbias, e) + g : g);
   }
 }
 
-// dh of a tile of columns (m) and tokens (n), over a part of the piece's words.
+// dh of a tile of columns (m) and tokens (n), over a part of the piece's words: the head lies by words.
 template <typename TY, int EDGE>
 __global__ __launch_bounds__(2 * EDGE) void k_head_dhidden(HeadArgs a) {
-  using T = HeadTile<TY, EDGE>;
+  using T = TileOf<typename TY::op, TY::planes, EDGE, true, false>;
+  const HeadRow& row = a.row[blockIdx.z];
   const uint64_t base = base_of(a);
   const uint32_t across = a.s.D / T::kM, u = die_run(blockIdx.x, gridDim.x, a.n_xcd), i = u % across, j = u / across, split = blockIdx.y;
-  const uint64_t pitch = (uint64_t)a.s.piece * 2 * TY::planes;
-  const uint32_t stages = (uint32_t)(((uint64_t)(a.words + EDGE - 1) / EDGE * EDGE * 2 * TY::planes) / kStageBytes);
+  const uint64_t b = 2 * TY::planes, pitch = a.s.piece * b;
+  constexpr uint32_t kEach = 64 / TY::planes;  // words of a stage
+  const uint32_t stages = (a.words + kEach - 1) / kEach;
   const uint32_t from = (uint32_t)((uint64_t)stages * split / a.s.splits), to = (uint32_t)((uint64_t)stages * (split + 1) / a.s.splits);
   char DADAM_LDS* lds = (char DADAM_LDS*)head_lds;
   T t;
   t.clear();
-  if (from < to)
-    t.product(global<const char>(base + a.w.head_t) + (uint64_t)i * T::kM * pitch + (uint64_t)from * kStageBytes, pitch,
-              global<const char>(base + a.w.p_n) + (uint64_t)j * T::kN * pitch + (uint64_t)from * kStageBytes, pitch, to - from, lds);
+  if (from < to)  // (of words beyond the piece softmax is 0, and the last word stands for them)
+    t.product(head_operand<TY>(base, row, a, from * kEach, i * T::kM * b), operand(base + a.w.p + (uint64_t)j * T::kN * pitch + (uint64_t)from * kStageBytes, pitch), to - from, lds);
   const uint64_t sums = base + a.w.sums + (uint64_t)split * a.s.T * a.s.D * 4;
-  t.hand_out(lds, false,
-             [&](uint32_t m, uint32_t n, float (&v)[8]) {
-               const uint64_t e = (uint64_t)(j * T::kN + n) * a.s.D + i * T::kM + m;
-               if (a.later) {
-                 float held[8];
-                 F32::load8(sums, e, 8, held);
-#pragma unroll
-                 for (int k = 0; k < 8; ++k) v[k] += held[k];
-               }
-               F32::store8(sums, e, 8, v);
+  struct Held {
+    float4v a, b;
+  };
+  auto at = [&](uint32_t m, uint32_t n) { return global<float4v>(sums + ((uint64_t)(j * T::kN + n) * a.s.D + i * T::kM + m) * 4); };
+  t.hand_out(lds, false, [&](uint32_t m, uint32_t n) { return a.later ? Held{at(m, n)[0], at(m, n)[1]} : Held{}; },
+             [&](uint32_t m, uint32_t n, float (&v)[8], const Held& held) {
+               at(m, n)[0] = float4v{v[0], v[1], v[2], v[3]} + held.a;
+               at(m, n)[1] = float4v{v[4], v[5], v[6], v[7]} + held.b;
              },
              [](uint32_t, uint32_t, const float (&)[8]) {});
 }
@@ -438,7 +424,6 @@ int with_types(int xdt, int gdt, Fn fn) {
   return gdt == (int)DADAM_BF16 ? fn(F32{}, B16{}, Types<F32, B16>{}) : fn(F32{}, F32{}, Types<F32, F32>{});
 }
 
-constexpr uint32_t kCutLds = kCut * kCutPitch * 4;
 uint32_t upto(uint64_t n, uint32_t each) { return (uint32_t)((n + each - 1) / each); }
 
 // fn(types of parameters, gradients and operands, edge of the tiles as a type).
@@ -458,19 +443,20 @@ int launch_head_begin(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* 
   const dim3 grid(most < kMostGroups ? most : kMostGroups, 2, rows);
   return xdt == (int)DADAM_BF16 ? launch<k_head_most<B16>>(grid, 256, 0, stream, a) : launch<k_head_most<F32>>(grid, 256, 0, stream, a);
 }
-int launch_head_hidden(int xdt, int gdt, bool gradient, const HeadArgs& a, uint32_t rows, void* stream) {
+int launch_head_hidden(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
   return with_types(xdt, gdt, [&](auto x, auto, auto ty) {
-    return launch<k_head_hidden<decltype(x), decltype(ty)>>(dim3(a.s.T / kCut, upto(gradient ? a.s.D : a.s.K, kCut), rows), 256, kCutLds, stream, a, (uint32_t)gradient);
+    return launch<k_head_hidden<decltype(x), decltype(ty)>>(dim3(upto((uint64_t)a.s.T * a.s.D, 2048), 1, rows), 256, 0, stream, a);
   });
 }
-int launch_head_words(int xdt, int gdt, bool turned, const HeadArgs& a, uint32_t rows, void* stream) {
+int launch_head_words(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
   return with_types(xdt, gdt, [&](auto x, auto, auto ty) {
-    return launch<k_head_words<decltype(x), decltype(ty)>>(dim3(upto(a.words, a.s.edge) * (a.s.edge / kCut), upto(turned ? a.s.D : a.s.K, kCut), rows), 256, kCutLds, stream, a, (uint32_t)turned);
+    const uint64_t words = (uint64_t)upto(a.words, a.s.edge) * a.s.edge;
+    return launch<k_head_words<decltype(x), decltype(ty)>>(dim3(upto(words * a.s.D, 2048), 1, rows), 256, 0, stream, a);
   });
 }
 int launch_head_logits(int xdt, int gdt, bool gradient, const HeadArgs& a, uint32_t rows, void* stream) {
   return with_tiles(xdt, gdt, a.s.edge, [&](auto x, auto, auto ty, auto edge) {
-    using T = HeadTile<decltype(ty), decltype(edge)::value>;
+    using T = TileOf<typename decltype(ty)::op, decltype(ty)::planes, decltype(edge)::value, false, false>;
     const dim3 grid(upto(a.words, a.s.edge) * (a.s.T / a.s.edge), 1, rows);
     return gradient ? launch<k_head_logits<decltype(x), decltype(ty), decltype(edge)::value, true>>(grid, T::kThreads, T::kLds, stream, a)
                     : launch<k_head_logits<decltype(x), decltype(ty), decltype(edge)::value, false>>(grid, T::kThreads, T::kLds, stream, a);
@@ -482,16 +468,16 @@ int launch_head_losses(const HeadArgs& a, uint32_t rows, void* stream) {
 }
 int launch_head_dhead(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
   return with_tiles(xdt, gdt, a.s.edge, [&](auto, auto g, auto ty, auto edge) {
-    using T = HeadTile<decltype(ty), decltype(edge)::value>;
+    using T = TileOf<typename decltype(ty)::op, decltype(ty)::planes, decltype(edge)::value, true, true>;
     return launch<k_head_dhead<decltype(g), decltype(ty), decltype(edge)::value>>(dim3(upto(a.words, a.s.edge) * (a.s.D / a.s.edge), 1, rows), T::kThreads, T::kLds, stream, a);
   });
 }
 int launch_head_dbias(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
-  return with_types(xdt, gdt, [&](auto, auto g, auto ty) { return launch<k_head_dbias<decltype(g), decltype(ty)>>(dim3(upto(a.words, 4), 1, rows), 256, 0, stream, a); });
+  return with_types(xdt, gdt, [&](auto, auto g, auto ty) { return launch<k_head_dbias<decltype(g), decltype(ty)>>(dim3(upto(a.words, 64), 1, rows), 256, 0, stream, a); });
 }
 int launch_head_dhidden(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
   return with_tiles(xdt, gdt, a.s.edge, [&](auto, auto, auto ty, auto edge) {
-    using T = HeadTile<decltype(ty), decltype(edge)::value>;
+    using T = TileOf<typename decltype(ty)::op, decltype(ty)::planes, decltype(edge)::value, true, false>;
     return launch<k_head_dhidden<decltype(ty), decltype(edge)::value>>(dim3((a.s.T / a.s.edge) * (a.s.D / a.s.edge), a.s.splits, rows), T::kThreads, T::kLds, stream, a);
   });
 }

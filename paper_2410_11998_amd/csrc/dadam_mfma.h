@@ -1,10 +1,10 @@
 // Matrix products on the matrix cores, shared by the kernels of orthogonalised updates and of a head's loss (included by their .hip files only).
 //
-// Every product here is C[m][n] = sum_k A[m][k] B[n][k]: both operands have the summed index innermost, rows a multiple of the tile and the summed
-// index a multiple of kStageBytes, the padding zero.  An operand element is 16 bits (bfloat16, or half precision times a power of two that keeps it
-// in range) or, where 32 bits are called for, two halves that together hold 22 bits of it: element = high + low.  Then a row holds 32 highs, their
-// 32 lows, the next 32 highs and so on, and a product takes three instructions instead of one (high high, high low, low high; low low is below the
-// last place that is kept).  Sums are float32 throughout.
+// Every product here is C[m][n] = sum_k A[m][k] B[n][k].  An operand lies by rows (m or n, the summed index innermost) or by columns (rows of the summed
+// index); either way its rows, columns and the summed index are filled up to the tiles with zeros, or with what comes to nothing.  An element is 16 bits
+// (bfloat16, or half precision times a power of two that keeps it in range) or, where 32 bits are called for, two halves that together hold 22 bits of it:
+// element = high + low.  Then 32 highs are followed by their 32 lows, the next 32 highs and so on, and a product takes three instructions instead of one
+// (high high, high low, low high; low low is below the last place that is kept).  Sums are float32 throughout.
 #ifndef DADAM_MFMA_H_
 #define DADAM_MFMA_H_
 
@@ -12,6 +12,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <type_traits>
 
 namespace dadam {
 namespace {
@@ -21,6 +22,7 @@ typedef __bf16 brain8 __attribute__((ext_vector_type(8)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef float float2v __attribute__((ext_vector_type(2)));
 typedef float float4v __attribute__((ext_vector_type(4)));
+typedef short short4v __attribute__((ext_vector_type(4)));
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 
 #define DADAM_GLOBAL __attribute__((address_space(1)))
@@ -104,6 +106,16 @@ struct B16 {
   }
 };
 
+// Where a tile's side of an operand begins (at the first stage), its rows' distance in bytes (below 2^32), and how many of them there are: beyond, the last one
+// is taken again.
+struct Operand {
+  const char DADAM_GLOBAL* at;
+  uint64_t pitch;
+  uint32_t limit;
+};
+constexpr uint32_t kNoLimit = 0xffffffffu;
+__device__ __forceinline__ Operand operand(uint64_t at, uint64_t pitch, uint32_t limit = kNoLimit) { return {global<const char>(at), pitch, limit}; }
+
 constexpr int kStageBytes = 128;  // of a row's elements that a stage takes: 64 elements of one plane, 32 of two
 
 // Where element k of a row of a two-plane operand has its high (the low is 32 behind it).
@@ -148,22 +160,20 @@ __device__ __forceinline__ void store8(uint64_t base, uint64_t r, uint32_t cols,
     global<uint4v>(at + 64)[0] = highs(w);
   }
 }
-template <typename OP>
-__device__ __forceinline__ void add8(float (&v)[8], uint64_t at) {
-  const uint4v b = global<const uint4v>(at)[0];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) v[2 * e] += OP::value(b[e] & 0xffffu), v[2 * e + 1] += OP::value(b[e] >> 16);
+// Elements k .. k+7 of row r of an operand, as loaded: their highs and lows.
+struct Eight {
+  uint4v high, low;
+};
+template <int PLANES>
+__device__ __forceinline__ Eight load8(uint64_t base, uint64_t r, uint32_t cols, uint32_t k) {
+  if constexpr (PLANES == 1) return {global<const uint4v>(base + (r * cols + k) * 2)[0], uint4v{0, 0, 0, 0}};
+  const uint64_t at = base + (r * cols * 2 + high_at(k)) * 2;
+  return {global<const uint4v>(at)[0], global<const uint4v>(at + 64)[0]};
 }
-// Their sum onto v.
-template <typename OP, int PLANES>
-__device__ __forceinline__ void load8(float (&v)[8], uint64_t base, uint64_t r, uint32_t cols, uint32_t k) {
-  if constexpr (PLANES == 1) {
-    add8<OP>(v, base + (r * cols + k) * 2);
-  } else {
-    const uint64_t at = base + (r * cols * 2 + high_at(k)) * 2;
-    add8<OP>(v, at);
-    add8<OP>(v, at + 64);
-  }
+template <typename OP, bool LOW>
+__device__ __forceinline__ float value_of(const Eight& x, int e) {
+  const float high = OP::value(x.high[e / 2] >> 16 * (e & 1) & 0xffffu);
+  return LOW ? high + OP::value(x.low[e / 2] >> 16 * (e & 1) & 0xffffu) : high;
 }
 
 __device__ __forceinline__ double wave_sum(double v) {
@@ -172,11 +182,66 @@ __device__ __forceinline__ double wave_sum(double v) {
   return v;
 }
 
+// What this wavefront has asked for is in LDS, and so is what the others have.
+__device__ __forceinline__ void everybody_has_loaded() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+}
+
+// Fragments of blocks that lie by columns: elements of two times four rows, AT and NEXT bytes behind at[...].  The reads are one block with their wait in it:
+// written with the compiler's builtin, each of them waits for all loads into LDS that are under way, the next stage's among them.
+template <int AT, int NEXT, typename V>
+__device__ __forceinline__ void read_turned(V (&out)[2], const uint32_t (&at)[2]) {
+  short4v o[4];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
+      "ds_read_b64_tr_b16 %2, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(o[0]), "=&v"(o[1]), "=&v"(o[2]), "=&v"(o[3])
+      : "v"(at[0]), "v"(at[1]), "n"(AT), "n"(NEXT)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 2; ++i) out[i] = __builtin_bit_cast(V, __builtin_shufflevector(o[2 * i], o[2 * i + 1], 0, 1, 2, 3, 4, 5, 6, 7));
+}
+template <int AT, int NEXT, typename V>
+__device__ __forceinline__ void read_turned(V (&out)[4], const uint32_t (&at)[4]) {
+  short4v o[8];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
+      "ds_read_b64_tr_b16 %2, %9 offset:%12\n\tds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
+      "ds_read_b64_tr_b16 %4, %10 offset:%12\n\tds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
+      "ds_read_b64_tr_b16 %6, %11 offset:%12\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(o[0]), "=&v"(o[1]), "=&v"(o[2]), "=&v"(o[3]), "=&v"(o[4]), "=&v"(o[5]), "=&v"(o[6]), "=&v"(o[7])
+      : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(AT), "n"(NEXT)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 4; ++i) out[i] = __builtin_bit_cast(V, __builtin_shufflevector(o[2 * i], o[2 * i + 1], 0, 1, 2, 3, 4, 5, 6, 7));
+}
+template <int AT, int NEXT, typename V>
+__device__ __forceinline__ void read_turned(V (&out)[6], const uint32_t (&at)[6]) {
+  short4v o[12];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %12 offset:%18\n\tds_read_b64_tr_b16 %1, %12 offset:%19\n\t"
+      "ds_read_b64_tr_b16 %2, %13 offset:%18\n\tds_read_b64_tr_b16 %3, %13 offset:%19\n\t"
+      "ds_read_b64_tr_b16 %4, %14 offset:%18\n\tds_read_b64_tr_b16 %5, %14 offset:%19\n\t"
+      "ds_read_b64_tr_b16 %6, %15 offset:%18\n\tds_read_b64_tr_b16 %7, %15 offset:%19\n\t"
+      "ds_read_b64_tr_b16 %8, %16 offset:%18\n\tds_read_b64_tr_b16 %9, %16 offset:%19\n\t"
+      "ds_read_b64_tr_b16 %10, %17 offset:%18\n\tds_read_b64_tr_b16 %11, %17 offset:%19\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(o[0]), "=&v"(o[1]), "=&v"(o[2]), "=&v"(o[3]), "=&v"(o[4]), "=&v"(o[5]), "=&v"(o[6]), "=&v"(o[7]), "=&v"(o[8]), "=&v"(o[9]), "=&v"(o[10]), "=&v"(o[11])
+      : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "n"(AT), "n"(NEXT)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 6; ++i) out[i] = __builtin_bit_cast(V, __builtin_shufflevector(o[2 * i], o[2 * i + 1], 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
 // Shape of a workgroup's tile: WM x WN wavefronts, each MT x NT blocks of 32 x 32; block (i, j) of wavefront (wm, wn) has rows (wm MT + i) 32 ... and columns
 // (j WN + wn) 32 ...  The large tile (256 x 256, eight wavefronts) is bound by LDS as much as by the matrix cores: a stage reads 192 KB and is written 64 KB, 2048
 // cycles, for 2048 cycles of products.  The small one (128 x 128, four) takes 768 cycles of LDS for 512 of products, and is for what has too few large tiles.
 // TFLOP/s, large / small / library, 8192 x 8192 x 8192 1119 / 914 / 1319, x 1024 1061 / 805 / 1078, 1024 x 49152 x 4096 1087 / 915 / 1295.
-template <typename OP, int PLANES, int MT, int NT, int WM, int WN>
+// A_DOWN, B_DOWN: that operand lies by columns.
+template <typename OP, int PLANES, int MT, int NT, int WM, int WN, bool A_DOWN, bool B_DOWN>
 struct Tile {
   static constexpr int kWaves = WM * WN, kThreads = kWaves * 64;
   static constexpr int kM = WM * MT * 32, kN = WN * NT * 32;
@@ -197,21 +262,33 @@ struct Tile {
         for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
   }
 
-  // One stage of ROWS rows into LDS, straight from memory: a wavefront's instruction brings 8 rows of 128 bytes, lane l the 16 bytes that
-  // belong at l * 16 of them.  The 16-byte pieces of row r lie in the order piece ^ (r & 7), so that the lanes of a fragment, which read one piece
-  // of 32 rows, touch all banks.  LIMITED: beyond `limit` rows (at least 1) the last one is brought again.
-  template <int ROWS, bool LIMITED>
-  static __device__ __forceinline__ void fetch(const char DADAM_GLOBAL* rows, uint64_t pitch, uint32_t limit, char DADAM_LDS* lds, int wave, int lane) {
-    const uint32_t piece = (uint32_t)((lane & 7) ^ (lane >> 3)) * 16u, own = (uint32_t)(lane >> 3) * (uint32_t)pitch + piece;
+  // By columns, the 32-byte pieces of row k of a stage lie in the order piece ^ mixed(k): a fragment's instruction reads two pieces side by side of
+  // rows k .. k+3 and k+8 .. k+11, which are then all different.
+  template <int SIDE>
+  static __device__ __forceinline__ uint32_t mixed(uint32_t k) {
+    constexpr uint32_t kPieces = SIDE * 2 * PLANES / 32;
+    return ((k & 3) << 1 | (k >> 3 & 1) << 3) & (kPieces - 1);
+  }
+
+  // Stage s of SIDE rows (DOWN: columns) of an operand into LDS, straight from memory; a wavefront's instruction brings 1 KB, lane l the 16 bytes that belong at
+  // l * 16 of it.  By rows that is 8 rows of 128 bytes, whose 16-byte pieces lie in the order piece ^ (row & 7), so that the lanes of a fragment, which read
+  // one piece of 32 rows, touch all banks.
+  template <int SIDE, bool DOWN>
+  static __device__ __forceinline__ void fetch(const Operand& o, uint32_t s, char DADAM_LDS* lds, int wave, int lane) {
 #pragma unroll
-    for (int j = 0; j < ROWS / 8 / kWaves; ++j) {
-      const int eight = j * kWaves + wave;
-      const char DADAM_GLOBAL* from = rows + (uint64_t)eight * 8 * pitch + own;
-      if constexpr (LIMITED) {
-        const uint32_t row = (uint32_t)(eight * 8 + (lane >> 3));
-        from = rows + (uint64_t)(row < limit ? row : limit - 1) * (uint32_t)pitch + piece;
+    for (int j = 0; j < SIDE / 8 / kWaves; ++j) {
+      const int part = j * kWaves + wave;
+      const char DADAM_GLOBAL* from;
+      if constexpr (DOWN) {
+        constexpr int kRowBytes = SIDE * 2 * PLANES, kPieces = kRowBytes / 16;
+        const uint32_t k = (uint32_t)((part * 64 + lane) / kPieces), piece = (uint32_t)(lane % kPieces) ^ (mixed<SIDE>(k) << 1);
+        const uint32_t row = s * (16 * kSteps) + k;
+        from = o.at + (uint64_t)(row < o.limit ? row : o.limit - 1) * (uint32_t)o.pitch + piece * 16;
+      } else {
+        const uint32_t row = (uint32_t)(part * 8 + (lane >> 3)), piece = (uint32_t)((lane & 7) ^ (lane >> 3));
+        from = o.at + (uint64_t)s * kStageBytes + (uint64_t)(row < o.limit ? row : o.limit - 1) * (uint32_t)o.pitch + piece * 16;
       }
-      __builtin_amdgcn_global_load_lds((const uint32_t DADAM_GLOBAL*)from, (uint32_t DADAM_LDS*)(lds + eight * 1024), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((const uint32_t DADAM_GLOBAL*)from, (uint32_t DADAM_LDS*)(lds + part * 1024), 16, 0, 0);
     }
   }
 
@@ -219,16 +296,54 @@ struct Tile {
   struct Fragments {
     vec a[PLANES][MT], b[PLANES][NT];
   };
-  static __device__ __forceinline__ void read(Fragments& f, const char DADAM_LDS* stage, int step, int wm, int wn, int lane) {
-    const uint32_t order = (uint32_t)((lane >> 5) ^ (lane & 7)), row = (uint32_t)(lane & 31) * kStageBytes;
+  // By rows: block `block` of 32.
+  static __device__ __forceinline__ vec fragment(const char DADAM_LDS* side, int block, int plane, int step, int lane) {
+    const uint32_t piece = (uint32_t)((lane >> 5) ^ (lane & 7)) ^ (uint32_t)((step + 2 * plane) << 1);
+    return *(const vec DADAM_LDS*)(side + (block * 32 + (lane & 31)) * kStageBytes + piece * 16);
+  }
+  // By columns: where the lane's part of block `block` of SIDE begins.  Sixteen lanes get four rows of sixteen columns, every lane the four of its column.
+  template <int SIDE>
+  static __device__ __forceinline__ uint32_t column_part(const char DADAM_LDS* side, int block, int plane, int lane) {
+    const uint32_t k = (uint32_t)(lane >> 5) * 8 + ((uint32_t)(lane & 15) >> 2);
+    const uint32_t piece = (uint32_t)(block * 2 * PLANES + plane * 2 + (lane >> 4 & 1)) ^ mixed<SIDE>(k);
+    return (uint32_t)(uintptr_t)(side + k * (SIDE * 2 * PLANES) + piece * 32 + (lane & 3) * 8);
+  }
+  template <int STEP>
+  static __device__ __forceinline__ void read(Fragments& f, const char DADAM_LDS* stage, int wm, int wn, int lane) {
+    const char DADAM_LDS* b_side = stage + kM * kStageBytes;
+    static_assert(kM == kN, "rows of either side have the same length");
+    constexpr int kAt = STEP * 16 * kM * 2 * PLANES, kNext = kAt + 4 * kM * 2 * PLANES;
 #pragma unroll
     for (int p = 0; p < PLANES; ++p) {
-      const char DADAM_LDS* at = stage + row + ((order ^ (uint32_t)((step + 2 * p) << 1)) << 4);
+      if constexpr (!A_DOWN)
 #pragma unroll
-      for (int i = 0; i < MT; ++i) f.a[p][i] = *(const vec DADAM_LDS*)(at + (wm * MT + i) * 32 * kStageBytes);
+        for (int i = 0; i < MT; ++i) f.a[p][i] = fragment(stage, wm * MT + i, p, STEP, lane);
+      if constexpr (!B_DOWN)
 #pragma unroll
-      for (int j = 0; j < NT; ++j) f.b[p][j] = *(const vec DADAM_LDS*)(at + (kM + (j * WN + wn) * 32) * kStageBytes);
+        for (int j = 0; j < NT; ++j) f.b[p][j] = fragment(b_side, j * WN + wn, p, STEP, lane);
     }
+#pragma unroll
+    for (int p = 0; p < PLANES; ++p) {
+      if constexpr (A_DOWN && B_DOWN) {
+        uint32_t at[MT + NT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) at[i] = column_part<kM>(stage, wm * MT + i, p, lane);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) at[MT + j] = column_part<kN>(b_side, j * WN + wn, p, lane);
+        vec out[MT + NT];
+        read_turned<kAt, kNext>(out, at);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) f.a[p][i] = out[i];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) f.b[p][j] = out[MT + j];
+      } else if constexpr (A_DOWN) {
+        uint32_t at[MT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) at[i] = column_part<kM>(stage, wm * MT + i, p, lane);
+        read_turned<kAt, kNext>(f.a[p], at);
+      }
+    }
+    static_assert(A_DOWN || !B_DOWN, "an operand that lies by columns is the first one");
   }
   __device__ __forceinline__ void multiply(const Fragments& f) {
 #pragma unroll
@@ -243,65 +358,81 @@ struct Tile {
       }
   }
 
-  // The sums over `stages` stages, from zero on.  a and b: the tile's first rows, at their first stage; pitches in bytes.  While a stage is multiplied
-  // the next one is on its way, and with one plane (two have no registers for it) while a step is multiplied the next one's fragments are: 128 x 128 x 1024
-  // tiles 805 TFLOP/s instead of 695.
-  template <bool LIMITED = false>
-  __device__ __forceinline__ void product(const char DADAM_GLOBAL* a, uint64_t a_pitch, const char DADAM_GLOBAL* b, uint64_t b_pitch, uint32_t stages, char DADAM_LDS* lds,
-                                          uint32_t a_limit = 0, uint32_t b_limit = 0) {
+  // The sums over `stages` stages (of 64 summed elements, or 32 of two planes), from zero on.  While a stage is multiplied the next one is on its way, and with one
+  // plane by rows (two have no registers for it, and what is turned is waited for where it is read) while a step is multiplied the next one's fragments are:
+  // 128 x 128 x 1024 tiles 805 TFLOP/s instead of 695.
+  __device__ __forceinline__ void product(const Operand& a, const Operand& b, uint32_t stages, char DADAM_LDS* lds) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WM, wn = wave / WM;
     auto bring = [&](uint32_t s) {
       char DADAM_LDS* to = lds + (s & 1) * kStage;
-      fetch<kM, LIMITED>(a + (uint64_t)s * kStageBytes, a_pitch, a_limit, to, wave, lane);
-      fetch<kN, LIMITED>(b + (uint64_t)s * kStageBytes, b_pitch, b_limit, to + kM * kStageBytes, wave, lane);
+      fetch<kM, A_DOWN>(a, s, to, wave, lane);
+      fetch<kN, B_DOWN>(b, s, to + kM * kStageBytes, wave, lane);
     };
     clear();
     bring(0);
-    if constexpr (PLANES == 1) {
+    if constexpr (PLANES == 1 && !A_DOWN && !B_DOWN) {
       Fragments f[2];
-      __syncthreads();
-      read(f[0], lds, 0, wm, wn, lane);
+      everybody_has_loaded();
+      read<0>(f[0], lds, wm, wn, lane);
       for (uint32_t s = 0; s < stages; ++s) {
+        const char DADAM_LDS* stage = lds + (s & 1) * kStage;
         if (s + 1 < stages) bring(s + 1);
-#pragma unroll
-        for (int k = 0; k < kSteps; ++k) {
-          if (k + 1 < kSteps) {
-            read(f[(k + 1) & 1], lds + (s & 1) * kStage, k + 1, wm, wn, lane);
-          } else {
-            __syncthreads();  // everybody has read this stage, and the next one is there
-            if (s + 1 < stages) read(f[(k + 1) & 1], lds + ((s + 1) & 1) * kStage, 0, wm, wn, lane);
-          }
+        auto step = [&](int k) {
           __builtin_amdgcn_sched_barrier(0);
           multiply(f[k & 1]);
           __builtin_amdgcn_sched_barrier(0);
-        }
+        };
+        read<1>(f[1], stage, wm, wn, lane);
+        step(0);
+        read<2>(f[0], stage, wm, wn, lane);
+        step(1);
+        read<3>(f[1], stage, wm, wn, lane);
+        step(2);
+        everybody_has_loaded();  // and read this stage
+        if (s + 1 < stages) read<0>(f[0], lds + ((s + 1) & 1) * kStage, wm, wn, lane);
+        step(3);
       }
     } else {
       for (uint32_t s = 0; s < stages; ++s) {
-        __syncthreads();
+        const char DADAM_LDS* stage = lds + (s & 1) * kStage;
+        everybody_has_loaded();
         if (s + 1 < stages) bring(s + 1);
-#pragma unroll
-        for (int k = 0; k < kSteps; ++k) {
+        auto step = [&](auto k) {
           Fragments f;
-          read(f, lds + (s & 1) * kStage, k, wm, wn, lane);
+          read<decltype(k)::value>(f, stage, wm, wn, lane);
           multiply(f);
+        };
+        step(std::integral_constant<int, 0>{});
+        step(std::integral_constant<int, 1>{});
+        if constexpr (kSteps == 4) {
+          step(std::integral_constant<int, 2>{});
+          step(std::integral_constant<int, 3>{});
         }
       }
     }
   }
 
   // Hands the sums out by whole pieces of rows and of columns, through LDS (a lane holds four rows of one column of every block; stored from there, an
-  // instruction writes 16 bytes each to 32 lines).  kRows columns at a time: column(m, n, v) gets C[m .. m+7][n] in v and may replace them by 32-bit values of its
-  // own; with `turned`, row(m, n, v) then gets those of C[m][n .. n+7].  The 16-byte pieces of a column lie in the order piece ^ n ^ n / 8, so that neither
-  // the lanes that write, 32 columns of one piece, nor those that read, 128 columns of one row, meet in a bank.
-  template <typename Column, typename Row>
-  __device__ __forceinline__ void hand_out(char DADAM_LDS* lds, bool turned, Column column, Row row) {
+  // instruction writes 16 bytes each to 32 lines).  kRows columns at a time: column(m, n, v, held) gets C[m .. m+7][n] in v, and what ahead(m, n) has loaded;
+  // with `turned` it leaves 32-bit values in v, of which row(m, n, v) then gets those of C[m][n .. n+7].  Loads go out four pieces at a time, before anything is
+  // stored: one by one, each waits for memory behind the last one's store (half of the time of a tile of 1024 summed elements).
+  // The 16-byte pieces of a column lie in the order piece ^ n ^ n / 8, so that neither the lanes that write, 32 columns of one piece, nor those that read,
+  // 128 columns of one row, meet in a bank.
+  template <typename Ahead, typename Column, typename Row>
+  __device__ __forceinline__ void hand_out(char DADAM_LDS* lds, bool turned, Ahead ahead, Column column, Row row) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WM, wn = wave / WM;
+    constexpr int kEach = kRows * kM / 8 / kThreads, kAhead = 4;  // pieces of a thread
+    static_assert(kEach % kAhead == 0, "whole batches");
     auto place = [&](uint32_t n, uint32_t piece) { return lds + n * (kM * 4) + ((piece ^ ((n ^ (n >> 3)) & 31u)) << 4); };
+    auto m_of = [&](int k) { return (threadIdx.x + (uint32_t)k * kThreads) % (kM / 8) * 8; };
+    auto n_of = [&](int k) { return (threadIdx.x + (uint32_t)k * kThreads) / (kM / 8); };
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
+      decltype(ahead(0u, 0u)) held[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) held[k] = ahead(m_of(k), (uint32_t)(j * kRows) + n_of(k));
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < MT; ++i)
@@ -311,16 +442,20 @@ struct Tile {
           *(float4v DADAM_LDS*)place((uint32_t)(wn * 32 + (lane & 31)), (uint32_t)((wm * MT + i) * 8 + g * 2 + (lane >> 5))) = v;
         }
       __syncthreads();
-#pragma unroll 2
-      for (uint32_t k = threadIdx.x; k < (uint32_t)(kRows * kM / 8); k += kThreads) {
-        const uint32_t n = k / (kM / 8), m = k % (kM / 8) * 8;
+#pragma unroll
+      for (int k = 0; k < kEach; ++k) {
+        const uint32_t n = n_of(k), m = m_of(k);
         float v[8];
         float4v DADAM_LDS* low = (float4v DADAM_LDS*)place(n, m / 4);
         float4v DADAM_LDS* high = (float4v DADAM_LDS*)place(n, m / 4 + 1);
         const float4v a = *low, b = *high;
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
-        column(m, (uint32_t)(j * kRows) + n, v);
+        if (k && k % kAhead == 0) {
+#pragma unroll
+          for (int x = 0; x < kAhead; ++x) held[x] = ahead(m_of(k + x), (uint32_t)(j * kRows) + n_of(k + x));
+        }
+        column(m, (uint32_t)(j * kRows) + n, v, held[k % kAhead]);
         if (turned) {
           *low = float4v{v[0], v[1], v[2], v[3]};
           *high = float4v{v[4], v[5], v[6], v[7]};
@@ -340,10 +475,12 @@ struct Tile {
   }
 };
 
-template <typename OP, int PLANES>
-using LargeTile = Tile<OP, PLANES, 4, 2, 2, 4>;
-template <typename OP, int PLANES>
-using SmallTile = Tile<OP, PLANES, 2, 2, 2, 2>;
+// ahead of hand_out where there is nothing to load.
+struct Nothing {};
+__device__ __forceinline__ Nothing nothing_ahead(uint32_t, uint32_t) { return {}; }
+
+template <typename OP, int PLANES, int EDGE, bool A_DOWN, bool B_DOWN>
+using TileOf = typename std::conditional<EDGE == 256, Tile<OP, PLANES, 4, 2, 2, 4, A_DOWN, B_DOWN>, Tile<OP, PLANES, 2, 2, 2, 2, A_DOWN, B_DOWN>>::type;
 
 // Workgroup b of n as its die takes it: consecutive workgroup ids go to the dies in turn, each die takes a contiguous run of tiles, whose operands
 // its L2 then holds.

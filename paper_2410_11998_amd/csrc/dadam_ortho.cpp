@@ -269,6 +269,8 @@ int run_group(dadam_handle* h, const Call& call, const Powers& pw, uint32_t k0, 
     const int x = pw.x[k], pa = pw.a[k], pb = pw.b[k];
     OrthoStepArgs s{};
     s.s = gram;
+    s.from = (uint32_t)(k & 1);
+    s.to = s.from ^ 1;
     s.fresh = std::ldexp(1.f, pa - 2 * x);
     e = launch_ortho_gram(false, edge, s, planes, gram_units, replicas, stream);
     s.gain = std::ldexp(b, pb - pa);
@@ -276,8 +278,6 @@ int run_group(dadam_handle* h, const Call& call, const Powers& pw, uint32_t k0, 
     if (!e) e = launch_ortho_gram(true, edge, s, planes, gram_units, replicas, stream);
     if (e) break;
     s.s = whole;
-    s.from = (uint32_t)(k & 1);
-    s.to = s.from ^ 1;
     if (k + 1 < steps) {
       s.gain = std::ldexp(a, pw.x[k + 1] - x);
       s.fresh = std::ldexp(1.f, pw.x[k + 1] - x - pb);

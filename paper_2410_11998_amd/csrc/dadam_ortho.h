@@ -23,18 +23,17 @@ struct OrthoTask {
   uint32_t edge;         // of the products' tiles
 };
 
-// Workspace of a matrix, one replica: X, with one plane what the half leaves of it (see dadam_ortho.hip), twice its transpose, A = X X^T,
-// B = b A + c A A, partial sums of the norm.
+// Workspace of a matrix, one replica: X twice (an iteration reads one and writes the other), with one plane what the half leaves of it (see dadam_ortho.hip),
+// A = X X^T, B = b A + c A A, partial sums of the norm.
 struct OrthoPlaces {
-  uint64_t x, low, turned[2], a, b, sums, bytes;
+  uint64_t x[2], low, a, b, sums, bytes;
 };
 inline constexpr OrthoPlaces ortho_places(uint64_t P, uint64_t Q, uint64_t planes) {
   OrthoPlaces w{};
   uint64_t at = 0;
-  w.x = at, at += P * Q * 2 * planes;
+  w.x[0] = at, at += P * Q * 2 * planes;
+  w.x[1] = at, at += P * Q * 2 * planes;
   w.low = at, at += planes == 1 ? P * Q * 2 : 0;
-  w.turned[0] = at, at += P * Q * 2 * planes;
-  w.turned[1] = at, at += P * Q * 2 * planes;
   w.a = at, at += P * P * 2 * planes;
   w.b = at, at += P * P * 2 * planes;
   w.sums = at, at += ((P / kOrthoCell) * (Q / kOrthoCell) * 8 + 255) / 256 * 256;
@@ -69,7 +68,7 @@ struct OrthoBeginArgs {
 struct OrthoStepArgs {
   OrthoSpan s;
   float gain, fresh;     // what is stored of the term held already, and of the new product
-  uint32_t from, to;     // which of the turned copies is read and written
+  uint32_t from, to;     // which X is read and written
 };
 
 template <int N>

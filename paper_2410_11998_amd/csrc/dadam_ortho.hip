@@ -1,17 +1,15 @@
 // Orthogonalised updates: X <- a X + (b A + c A A) X, A = X X^T, from X = U / |U| (Frobenius), for all matrices of a layout in all replicas.
 //
 // An iteration is three launches over the tiles of a group of matrices: A (k_ortho_gram), B = b A + c A A (k_ortho_gram again, as A is its own
-// transpose), and a X + B X (k_ortho_next; the last one, k_ortho_end, stores the matrix or takes the step).  All three have the summed index innermost
-// on both sides if X is there in both orientations, so every iteration writes X and its transpose.  A and B are symmetric: only the tiles of their
-// lower half are computed, each stored twice, which leaves 3 p^2 q + p^3 of 4 p^2 q + 2 p^3 operations.
+// transpose), and a X + B X (k_ortho_next; the last one, k_ortho_end, stores the matrix or takes the step).  A and B are symmetric: only the tiles of their
+// lower half are computed, each stored twice, which leaves 3 p^2 q + p^3 of 4 p^2 q + 2 p^3 operations.  B X sums over X's rows: its tiles come into LDS as they
+// lie and are turned on the way to the registers.
 //
 // Operands are half precision times a power of two (their spectral norms are bounded, so their elements are, see dadam_ortho.cpp).  Results of
 // 32 bits have two halves an element (dadam_mfma.h): the error of five iterations is 2e-7 to 3e-6 of the result, by how fast the singular values
 // fall.  For bfloat16 results one half is enough in the products, but not for X itself: what X loses to 11 bits in the directions of small singular
 // values grows by a = 3.4 an iteration, 1e-3 of the result for equal singular values, 1.4e-2 for ones that fall by 1000 in 50.  a X is therefore taken
 // from two halves as well (1.4e-3 and 5e-4), the second of which no product reads.
-#include <type_traits>
-
 #include "dadam_mfma.h"
 #include "dadam_ortho.h"
 
@@ -20,8 +18,13 @@ namespace {
 
 extern __shared__ char ortho_lds[];
 
+// Of A and B, whose operands both lie by rows, and of a X + B X (transposed: q by p), whose X lies by columns.
 template <int PLANES, int EDGE>
-using OrthoTile = typename std::conditional<EDGE == (int)kLargeEdge, LargeTile<Half, PLANES>, SmallTile<Half, PLANES>>::type;
+using GramTile = TileOf<Half, PLANES, EDGE, false, false>;
+template <int PLANES, int EDGE>
+using NextTile = TileOf<Half, PLANES, EDGE, true, false>;
+
+__device__ __forceinline__ uint64_t x_at(const OrthoPlaces& w, uint32_t which) { return which ? w.x[1] : w.x[0]; }
 
 // A workgroup's matrix, the tile of it and where its workspace begins.
 struct Unit {
@@ -97,7 +100,7 @@ __global__ __launch_bounds__(256) void k_ortho_norm(OrthoBeginArgs<N> a) {
   if (threadIdx.x == 0) global<double>(u.base + ortho_places(u.t.P, u.t.Q, PLANES).sums)[u.tile] = parts[0] + parts[1] + parts[2] + parts[3];
 }
 
-// X and its transpose from the matrix, and of a step lines 9 to 13 of Algorithm 3 for the first moment and the accumulator.
+// X from the matrix, and of a step lines 9 to 13 of Algorithm 3 for the first moment and the accumulator.
 constexpr uint32_t kTurnPitch = kOrthoCell + 1;
 template <typename GT, int PLANES, int N>
 __global__ __launch_bounds__(256) void k_ortho_begin(OrthoBeginArgs<N> a) {
@@ -141,22 +144,13 @@ __global__ __launch_bounds__(256) void k_ortho_begin(OrthoBeginArgs<N> a) {
     for (int k = 0; k < 8; ++k) tile[r * kTurnPitch + k8 + k] = v[k];
   }
   __syncthreads();
-  // as it lies, and turned
   for (uint32_t r = threadIdx.x / 16; r < kOrthoCell; r += 16) {
-    uint32_t v[8], t[8];
+    uint32_t x[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = halves<Half>(tile[r * kTurnPitch + k8 + k]), t[k] = halves<Half>(tile[(k8 + k) * kTurnPitch + r]);
-    auto straight = [&](uint32_t p, uint32_t q, const uint32_t (&x)[8]) {
-      store8<PLANES>(u.base + w.x, p, u.t.Q, q, x);
-      if constexpr (PLANES == 1) global<uint4v>(u.base + w.low + ((uint64_t)p * u.t.Q + q) * 2)[0] = highs(x);
-    };
-    if (u.t.tall) {
-      store8<PLANES>(u.base + w.turned[0], c.r0 + r, u.t.P, c.c0 + k8, v);
-      straight(c.c0 + r, c.r0 + k8, t);
-    } else {
-      straight(c.r0 + r, c.c0 + k8, v);
-      store8<PLANES>(u.base + w.turned[0], c.c0 + r, u.t.P, c.r0 + k8, t);
-    }
+    for (int k = 0; k < 8; ++k) x[k] = halves<Half>(u.t.tall ? tile[(k8 + k) * kTurnPitch + r] : tile[r * kTurnPitch + k8 + k]);
+    const uint32_t p = (u.t.tall ? c.c0 : c.r0) + r, q = (u.t.tall ? c.r0 : c.c0) + k8;
+    store8<PLANES>(u.base + w.x[0], p, u.t.Q, q, x);
+    if constexpr (PLANES == 1) global<uint4v>(u.base + w.low + ((uint64_t)p * u.t.Q + q) * 2)[0] = highs(x);
   }
 }
 
@@ -168,7 +162,7 @@ __device__ __forceinline__ void to_words(const float (&v)[8], uint32_t (&w)[8]) 
 // A tile (i, j), j <= i, of A = X X^T or of B = b A + c A A, and its mirror image.
 template <int PLANES, int EDGE, bool SQUARE>
 __global__ __launch_bounds__(2 * EDGE) void k_ortho_gram(OrthoStepArgs a) {
-  using T = OrthoTile<PLANES, EDGE>;
+  using T = GramTile<PLANES, EDGE>;
   const Unit u = find_unit<kGram>(a.s);
   const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES);
   uint32_t i = (uint32_t)((sqrtf(8.f * (float)u.tile + 1.f) - 1.f) * 0.5f);  // (the root may round across the border of a row of tiles)
@@ -176,19 +170,23 @@ __global__ __launch_bounds__(2 * EDGE) void k_ortho_gram(OrthoStepArgs a) {
   while ((i + 1) * (i + 2) / 2 <= u.tile) ++i;
   const uint32_t j = u.tile - i * (i + 1) / 2, inner = SQUARE ? u.t.P : u.t.Q;
   const uint64_t pitch = (uint64_t)inner * 2 * PLANES;
-  const char DADAM_GLOBAL* in = global<const char>(u.base + (SQUARE ? w.a : w.x));
+  const uint64_t in = u.base + (SQUARE ? w.a : x_at(w, a.from));
   char DADAM_LDS* lds = (char DADAM_LDS*)ortho_lds;
   T t;
-  t.product(in + (uint64_t)i * T::kM * pitch, pitch, in + (uint64_t)j * T::kN * pitch, pitch, (uint32_t)(pitch / kStageBytes), lds);
+  t.product(operand(in + (uint64_t)i * T::kM * pitch, pitch), operand(in + (uint64_t)j * T::kN * pitch, pitch), (uint32_t)(pitch / kStageBytes), lds);
   const uint64_t out = u.base + (SQUARE ? w.b : w.a);
   t.hand_out(lds, i != j,
-             [&](uint32_t m, uint32_t n, float (&v)[8]) {
-               float held[8] = {};
-               if constexpr (SQUARE) load8<Half, PLANES>(held, u.base + w.a, j * T::kN + n, u.t.P, i * T::kM + m);
+             [&](uint32_t m, uint32_t n) {
+               if constexpr (SQUARE) return load8<PLANES>(u.base + w.a, j * T::kN + n, u.t.P, i * T::kM + m);
+               else return Nothing{};
+             },
+             [&](uint32_t m, uint32_t n, float (&v)[8], const auto& held) {
                uint32_t words[8];
 #pragma unroll
                for (int k = 0; k < 8; ++k) {
-                 words[k] = halves<Half>(SQUARE ? fmaf(held[k], a.gain, v[k] * a.fresh) : v[k] * a.fresh);
+                 if constexpr (SQUARE) v[k] = fmaf(value_of<Half, PLANES == 2>(held, k), a.gain, v[k] * a.fresh);
+                 else v[k] *= a.fresh;
+                 words[k] = operand_word<Half, PLANES>(v[k]);
                  v[k] = __uint_as_float(words[k]);
                }
                store8<PLANES>(out, j * T::kN + n, u.t.P, i * T::kM + m, words);
@@ -200,59 +198,50 @@ __global__ __launch_bounds__(2 * EDGE) void k_ortho_gram(OrthoStepArgs a) {
              });
 }
 
-// X of eight elements, whole.
+// X of eight elements, highs and lows.
 template <int PLANES>
-__device__ __forceinline__ void load_x(float (&x)[8], uint64_t base, const OrthoPlaces& w, const OrthoTask& t, uint32_t p, uint32_t q) {
-#pragma unroll
-  for (int k = 0; k < 8; ++k) x[k] = 0.f;
-  load8<Half, PLANES>(x, base + w.x, p, t.Q, q);
-  if constexpr (PLANES == 1) add8<Half>(x, base + w.low + ((uint64_t)p * t.Q + q) * 2);
+__device__ __forceinline__ Eight load_x(uint64_t base, const OrthoPlaces& w, uint32_t which, const OrthoTask& t, uint32_t p, uint32_t q) {
+  Eight x = load8<PLANES>(base + x_at(w, which), p, t.Q, q);
+  if constexpr (PLANES == 1) x.low = global<const uint4v>(base + w.low + ((uint64_t)p * t.Q + q) * 2)[0];
+  return x;
 }
 
-// The product of a tile of a X + B X, transposed: rows q of X's transpose against rows p of B (its own).
+// The product of a tile of a X + B X, transposed: columns q of X against rows p of B (its own).
 template <typename T, int PLANES>
 __device__ __forceinline__ void next_product(T& t, const Unit& u, const OrthoPlaces& w, uint32_t from, uint32_t& q0, uint32_t& p0, char DADAM_LDS* lds) {
   const uint32_t across = u.t.P / T::kN;
   q0 = u.tile / across * T::kM;
   p0 = u.tile % across * T::kN;
   const uint64_t pitch = (uint64_t)u.t.P * 2 * PLANES;
-  t.product(global<const char>(u.base + (from ? w.turned[1] : w.turned[0])) + q0 * pitch, pitch, global<const char>(u.base + w.b) + p0 * pitch, pitch, (uint32_t)(pitch / kStageBytes), lds);
+  t.product(operand(u.base + x_at(w, from) + (uint64_t)q0 * 2 * PLANES, (uint64_t)u.t.Q * 2 * PLANES), operand(u.base + w.b + p0 * pitch, pitch),
+            (uint32_t)(pitch / kStageBytes), lds);
 }
 
-// X of the next iteration in place of this one's, and its transpose to the other copy.
+// X of the next iteration.
 template <int PLANES, int EDGE>
 __global__ __launch_bounds__(2 * EDGE) void k_ortho_next(OrthoStepArgs a) {
-  using T = OrthoTile<PLANES, EDGE>;
+  using T = NextTile<PLANES, EDGE>;
   const Unit u = find_unit<kWhole>(a.s);
   const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES);
   char DADAM_LDS* lds = (char DADAM_LDS*)ortho_lds;
   uint32_t q0, p0;
   T t;
   next_product<T, PLANES>(t, u, w, a.from, q0, p0, lds);
-  t.hand_out(lds, true,
-             [&](uint32_t m, uint32_t n, float (&v)[8]) {
-               float x[8];
-               load_x<PLANES>(x, u.base, w, u.t, p0 + n, q0 + m);
+  t.hand_out(lds, false, [&](uint32_t m, uint32_t n) { return load_x<PLANES>(u.base, w, a.from, u.t, p0 + n, q0 + m); },
+             [&](uint32_t m, uint32_t n, float (&v)[8], const Eight& x) {
                uint32_t words[8];
 #pragma unroll
-               for (int k = 0; k < 8; ++k) {
-                 words[k] = halves<Half>(fmaf(x[k], a.gain, v[k] * a.fresh));
-                 v[k] = __uint_as_float(words[k]);
-               }
-               store8<PLANES>(u.base + w.x, p0 + n, u.t.Q, q0 + m, words);
+               for (int k = 0; k < 8; ++k) words[k] = halves<Half>(fmaf(value_of<Half, true>(x, k), a.gain, v[k] * a.fresh));
+               store8<PLANES>(u.base + x_at(w, a.to), p0 + n, u.t.Q, q0 + m, words);
                if constexpr (PLANES == 1) global<uint4v>(u.base + w.low + ((uint64_t)(p0 + n) * u.t.Q + q0 + m) * 2)[0] = highs(words);
              },
-             [&](uint32_t m, uint32_t n, const float (&v)[8]) {
-               uint32_t words[8];
-               to_words(v, words);
-               store8<PLANES>(u.base + (a.to ? w.turned[1] : w.turned[0]), q0 + m, u.t.P, p0 + n, words);
-             });
+             [](uint32_t, uint32_t, const float (&)[8]) {});
 }
 
 // The last iteration, straight into the result: the matrix, or the parameters mixed and moved along it.
 template <typename DT, int PLANES, int EDGE, int N>
 __global__ __launch_bounds__(2 * EDGE) void k_ortho_end(OrthoEndArgs<N> a) {
-  using T = OrthoTile<PLANES, EDGE>;
+  using T = NextTile<PLANES, EDGE>;
   const Unit u = find_unit<kWhole>(a.s);
   const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES);
   char DADAM_LDS* lds = (char DADAM_LDS*)ortho_lds;
@@ -293,12 +282,10 @@ __global__ __launch_bounds__(2 * EDGE) void k_ortho_end(OrthoEndArgs<N> a) {
     }
     DT::store8(out, e, n, mixed);
   };
-  t.hand_out(lds, u.t.tall,
-             [&](uint32_t m, uint32_t n, float (&v)[8]) {
-               float x[8];
-               load_x<PLANES>(x, u.base, w, u.t, p0 + n, q0 + m);
+  t.hand_out(lds, u.t.tall, [&](uint32_t m, uint32_t n) { return load_x<PLANES>(u.base, w, a.from, u.t, p0 + n, q0 + m); },
+             [&](uint32_t m, uint32_t n, float (&v)[8], const Eight& x) {
 #pragma unroll
-               for (int k = 0; k < 8; ++k) v[k] = fmaf(x[k], a.gain, v[k] * a.fresh);
+               for (int k = 0; k < 8; ++k) v[k] = fmaf(value_of<Half, true>(x, k), a.gain, v[k] * a.fresh);
                if (!u.t.tall) finish(p0 + n, q0 + m, v);
              },
              [&](uint32_t m, uint32_t n, const float (&v)[8]) { finish(q0 + m, p0 + n, v); });
@@ -344,17 +331,17 @@ int begin_any(bool norm, int gdt, const OrthoBeginArgs<kMaxRows>& a, uint32_t pl
 
 template <int PLANES, int EDGE>
 int gram(bool square, const OrthoStepArgs& a, uint32_t units, uint32_t replicas, void* stream) {
-  using T = OrthoTile<PLANES, EDGE>;
+  using T = GramTile<PLANES, EDGE>;
   return square ? launch<k_ortho_gram<PLANES, EDGE, true>>(a, T::kThreads, units, replicas, T::kLds, stream) : launch<k_ortho_gram<PLANES, EDGE, false>>(a, T::kThreads, units, replicas, T::kLds, stream);
 }
 template <int PLANES, int EDGE>
 int next(const OrthoStepArgs& a, uint32_t units, uint32_t replicas, void* stream) {
-  using T = OrthoTile<PLANES, EDGE>;
+  using T = NextTile<PLANES, EDGE>;
   return launch<k_ortho_next<PLANES, EDGE>>(a, T::kThreads, units, replicas, T::kLds, stream);
 }
 template <typename DT, int PLANES, int EDGE>
 int end(const OrthoEndArgs<kMaxRows>& a, uint32_t n_cols, uint32_t units, uint32_t replicas, void* stream) {
-  using T = OrthoTile<PLANES, EDGE>;
+  using T = NextTile<PLANES, EDGE>;
   if (replicas <= (uint32_t)kOrthoFew && n_cols <= (uint32_t)kOrthoFew)
     return launch<k_ortho_end<DT, PLANES, EDGE, kOrthoFew>>(shorter<kOrthoFew>(a), T::kThreads, units, replicas, T::kLds, stream);
   return launch<k_ortho_end<DT, PLANES, EDGE, kMaxRows>>(a, T::kThreads, units, replicas, T::kLds, stream);
