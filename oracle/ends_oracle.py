@@ -67,7 +67,8 @@ def head_loss_error(r, head, bias, planes, half):
     """Bounds, element by element, of what the library's roundings make of head_loss's results r.  half: half a step of the results' type.
 
     Logits: operands of 2^-22 a plane pair (of one bfloat16 plane: as given), a sum of K products in float32 off by four times sqrt(K) roundings of 2^-24.
-    softmax: twice a logit's error, an exponential good to 2^-21 and to 2^-23 of its argument; held to 2^-22 and 2^-38 of 1, or to 2^-8.
+    softmax: twice a logit's error, an exponential good to 2^-21 and to 2^-23 of its argument; held to 2^-22 twice and 2^-38 of 1, or to
+    2^-11 and 2^-40 of the largest and then to 2^-8 (half precision, then bfloat16: (1 + 2^-11) (1 + 2^-8) - 1 < 2^-8 + 2^-10).
     What is below 2^-126, float32's (and bfloat16's) smallest normal number, may come out as 0: an exponential of -100 is 2^-144, off by all of itself."""
     w = np.abs(np.asarray(head, dtype=np.float64))
     h, z, s = np.abs(r["h"]), r["z"], abs(r["s"])
@@ -83,7 +84,7 @@ def head_loss_error(r, head, bias, planes, half):
     dz = np.abs(r["dz"])
     p = np.where(r["dz"] < 0, 1 + r["dz"], r["dz"])
     relative = 2 * worst[:, None] + 2.0 ** -20 + 2.0 ** -22 * finite
-    held = (2.0 ** -22 * dz + 2.0 ** -38) if planes == 2 else 2.0 ** -8 * dz
+    held = (2.0 ** -21 * dz + 2.0 ** -38) if planes == 2 else (2.0 ** -8 + 2.0 ** -10) * dz + 2.0 ** -40
     ddz = np.where(taken[:, None], relative * (p + dz) + held + 2.0 ** -126, 0.0)
     k, t = w.shape[0], len(z)
     lost = 2.0 ** -126

@@ -40,6 +40,7 @@ struct Way {
 
 constexpr uint32_t kSplits = 16;              // at most
 constexpr uint64_t kMostOfPiece = 1ull << 27;  // tokens times words of a piece
+constexpr uint64_t kMostKept = 1ull << 31;     // bytes of softmax that a replica may keep
 // Workgroups that the chip holds at a time: one large tile a compute unit, two small ones.
 uint32_t at_once(uint32_t edge) { return edge == 256 ? 256 : 512; }
 
@@ -55,24 +56,34 @@ void fill_shape(const dadam_head* head, uint32_t n_tokens, uint32_t planes, uint
   s->K = filled(head->width, 64);
   s->piece = std::min(piece, filled(head->vocab, edge));
   s->slices = filled(head->vocab, edge) / (edge / 2);
+  s->keeps = 0;
   const uint64_t tiles = (uint64_t)(s->T / edge) * (s->D / edge) * rows, stages = (uint64_t)s->piece * planes / 64;
   s->splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(std::min<uint64_t>((at_once(edge) + tiles - 1) / tiles, stages / 8), kSplits));
 }
 
-Way good_way(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, bool gradient) {
+Way good_way(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, bool gradient, bool keeps) {
   Way w{};
   const uint32_t planes = planes_of(h), V = head->vocab, R = std::min<uint32_t>(h->cfg.n_rows, kHeadRows);
   const uint64_t large = (uint64_t)(filled(V, 256) / 256) * (filled(n_tokens, 256) / 256) * R;
   const uint32_t edge = suits_large(n_tokens) && suits_large(head->width) && suits_large(V) && large >= 256 ? 256 : 128;
-  // pieces whose tiles of the head's gradient are what the chip holds at a time
-  const uint32_t across = filled(head->width, edge) / edge;
-  uint64_t piece = (uint64_t)std::max(1u, at_once(edge) / across) * edge;
-  piece = std::max<uint64_t>(edge, std::min(piece, kMostOfPiece / filled(n_tokens, edge) / edge * edge));
-  piece = std::min<uint64_t>(piece, filled(V, edge));
-  w.rows = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(R, 2 * at_once(edge) / (piece / edge * across)));
+  const uint64_t across = filled(head->width, edge) / edge, down = filled(n_tokens, edge) / edge, all = filled(V, edge);
+  uint64_t piece = all;
+  if (!keeps && gradient) {
+    // pieces whose tiles, of the logits and of the head's gradient, are what the chip holds at a time or more
+    piece = std::max<uint64_t>(1, at_once(edge) / std::min(across, down)) * edge;
+    piece = std::max<uint64_t>(edge, std::min(piece, kMostOfPiece / (down * edge) / edge * edge));
+    piece = std::min(piece, all);
+  }
+  w.rows = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(R, 2 * at_once(edge) / (piece / edge * std::min(across, down))));
   fill_shape(head, n_tokens, planes, edge, w.rows, (uint32_t)piece, &w.s);
+  w.s.keeps = keeps;
   w.each = head_places(w.s, planes, gradient).bytes;
   return w;
+}
+
+// Whether a replica's softmax is small enough to be kept.
+bool may_keep(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, bool gradient) {
+  return gradient && (uint64_t)filled(n_tokens, 256) * filled(head->vocab, 256) * 2 * planes_of(h) <= kMostKept;
 }
 
 Way least_way(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, bool gradient) {
@@ -83,9 +94,11 @@ Way least_way(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, 
   return w;
 }
 
-// The good way, with fewer replicas at a time or smaller pieces where the workspace asks for it.
+// Keeping softmax, or in pieces, or with fewer replicas at a time or smaller pieces where the workspace asks for it.
 Way way_for(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, bool gradient, uint64_t bytes) {
-  Way w = good_way(h, head, n_tokens, gradient);
+  Way w{};
+  if (may_keep(h, head, n_tokens, gradient)) w = good_way(h, head, n_tokens, gradient, true);
+  if (w.rows == 0 || w.each > bytes) w = good_way(h, head, n_tokens, gradient, false);
   if (w.each <= bytes) {
     w.rows = (uint32_t)std::min<uint64_t>(w.rows, bytes / w.each);
     return w;
@@ -117,14 +130,15 @@ int run_rows(const dadam_handle* h, HeadArgs a, bool dhidden, bool dhead, bool d
   for (uint32_t k = 0; k < pieces && !e; ++k) {
     piece(k);
     if (!a.straight) e = launch_head_words(x, g, a, rows, stream);
-    if (!e) e = launch_head_logits(x, g, false, a, rows, stream);
+    if (!e) e = launch_head_logits(x, g, a.s.keeps ? kHeadKeep : kHeadStatistics, a, rows, stream);
   }
   if (!e) e = launch_head_losses(a, rows, stream);
   if (!gradient) return e;
+  if (!e && a.s.keeps) e = launch_head_scale(x, g, a, rows, stream);
   for (uint32_t k = 0; k < pieces && !e; ++k) {
     piece(k);
     if (pieces > 1 && !a.straight) e = launch_head_words(x, g, a, rows, stream);
-    if (!e) e = launch_head_logits(x, g, true, a, rows, stream);
+    if (!e && !a.s.keeps) e = launch_head_logits(x, g, kHeadGradient, a, rows, stream);
     if (!e && dhead) e = launch_head_dhead(x, g, a, rows, stream);
     if (!e && dbias) e = launch_head_dbias(x, g, a, rows, stream);
     if (!e && dhidden) e = launch_head_dhidden(x, g, a, rows, stream);
@@ -142,7 +156,7 @@ int dadam_head_get_info(const dadam_handle* h, const dadam_head* head, uint32_t 
   if (!h) return DADAM_EINVAL;
   if (!out) return fail(h, DADAM_EINVAL, "out is null");
   if (const int rc = check_head(h, head, n_tokens)) return rc;
-  const Way w = good_way(h, head, n_tokens, gradient != 0);
+  const Way w = good_way(h, head, n_tokens, gradient != 0, may_keep(h, head, n_tokens, gradient != 0));
   out->least_bytes = least_way(h, head, n_tokens, gradient != 0).each;
   out->bytes = std::max(out->least_bytes, w.each * w.rows);
   return DADAM_OK;

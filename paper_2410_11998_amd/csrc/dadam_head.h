@@ -26,6 +26,7 @@ struct HeadShape {
   uint32_t T, D, K;        // tokens and width filled up to the edge, width filled up to a stage
   uint32_t piece, slices;  // words of a piece (a multiple of the edge), slices of edge / 2 of all words
   uint32_t splits;         // parts that the sum over words of a hidden vector's gradient goes in
+  uint32_t keeps;          // softmax of all words is kept from the statistics on: one piece
 };
 inline constexpr HeadPlaces head_places(const HeadShape& s, uint64_t planes, bool gradient) {
   HeadPlaces w{};
@@ -70,8 +71,11 @@ static_assert(sizeof(HeadArgs) <= 4096, "the argument block of a launch holds 4 
 int launch_head_begin(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                   // tokens with a target, powers of two
 int launch_head_hidden(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                  // operands of the hidden vectors
 int launch_head_words(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                   // operands of a piece of the head
-int launch_head_logits(int xdt, int gdt, bool gradient, const HeadArgs& a, uint32_t rows, void* stream);   // statistics, or the logits' gradient
+// Statistics; statistics, and the slices' exponentials kept; or the logits' gradient.
+enum HeadMode : int { kHeadStatistics = 0, kHeadKeep = 1, kHeadGradient = 2 };
+int launch_head_logits(int xdt, int gdt, HeadMode mode, const HeadArgs& a, uint32_t rows, void* stream);
 int launch_head_losses(const HeadArgs& a, uint32_t rows, void* stream);
+int launch_head_scale(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                   // the logits' gradient from what was kept
 int launch_head_dhead(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);
 int launch_head_dbias(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);
 int launch_head_dhidden(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                 // a piece's part of the sums

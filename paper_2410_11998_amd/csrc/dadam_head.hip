@@ -1,10 +1,12 @@
 // The loss of a language model's head: z = W h + bias, nll = log sum exp z - z[target], and with s the gradient's scale
 //     dz = s (softmax z - e[target]),   dh = sum over words dz W,   dW = sum over tokens dz h,   dbias = sum over tokens dz.
 //
-// The logits never leave the chip.  A first product gives every token the largest logit and the sum of exponentials of some words
+// Two ways.  Where the workspace has room for 2 (or two planes: 4) bytes for every logit, the product of the logits stores the exponentials of each slice of
+// words against the slice's largest logit, and k_head_scale makes softmax - e[target] of them in place once the sums are known: three products of tokens x
+// vocabulary x width.  Elsewhere nothing of the logits leaves the chip but a piece of the vocabulary at a time.  A first product gives every token the largest logit and the sum of exponentials of some words
 // (k_head_logits), from which k_head_losses makes the logarithm of the sum; a second one recomputes the logits a piece of the vocabulary at a time
-// and stores softmax - e[target] of it, the operand of the two gradient products.  dW of a piece is complete; dh adds up over pieces.  Four products of
-// tokens x vocabulary x width, of which a program that keeps the logits (4 bytes for each, read and written several times) needs three.  All operands
+// and stores softmax - e[target] of it, the operand of the two gradient products.  dW of a piece is complete; dh adds up over pieces.  Four products.
+// All operands
 // lie as they are made: the gradients sum over tokens and over words, so their tiles are turned on the way from LDS to the registers.
 //
 // bfloat16 parameters and gradients: the operands are what is given, softmax - e[target] is rounded to bfloat16, 8 bits relative whatever its size;
@@ -99,8 +101,30 @@ __global__ __launch_bounds__(256) void k_head_most(HeadArgs a) {
   float v[8];
   if (blockIdx.y == 0) {
     const uint64_t n = (uint64_t)a.s.vocab * a.s.width;
-#pragma unroll 4
-    for (uint64_t e = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * 8; e < n; e += (uint64_t)gridDim.x * 2048) {
+    const uint64_t step = (uint64_t)gridDim.x * 2048;
+    uint64_t e = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (row.head % 16 == 0)
+      for (; e + 3 * step + 8 <= n; e += 4 * step) {  // four loads on their way at a time
+        uint4v b[4][sizeof(typename XT::type) / 2];
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k)
+#pragma unroll
+          for (uint32_t h = 0; h < sizeof(typename XT::type) / 2; ++h) b[k][h] = global<const uint4v>(row.head + (e + k * step) * sizeof(typename XT::type))[h];
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k)
+#pragma unroll
+          for (uint32_t h = 0; h < sizeof(typename XT::type) / 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if (sizeof(typename XT::type) == 4) {
+                larger(most, __uint_as_float(b[k][h][i]));
+              } else {
+                larger(most, __uint_as_float(b[k][h][i] << 16));
+                larger(most, __uint_as_float(b[k][h][i] & 0xffff0000u));
+              }
+            }
+      }
+    for (; e < n; e += step) {
       XT::load8(row.head, e, n - e < 8 ? (uint32_t)(n - e) : 8, v);
 #pragma unroll
       for (int k = 0; k < 8; ++k) larger(most, v[k]);
@@ -169,9 +193,16 @@ __device__ __forceinline__ Operand head_operand(uint64_t base, const HeadRow& ro
   return operand(base + a.w.head + first * pitch + offset, pitch);
 }
 
+// What a slice's exponentials, at most 1, are kept times.  For bfloat16 they are kept in half precision, which has three bits more than what is made of them: times
+// 2^15 those down to 2^-29 have 11 bits, the others 2^-40 of the slice's largest.
+template <typename TY>
+__device__ __forceinline__ constexpr float kept_times() {
+  return TY::planes == 1 ? 32768.f : (float)(1 << kHeldAt);
+}
+
 // The logits of a tile of words (m) and tokens (n).  Without gradients: the largest and the sum of exponentials of each wavefront's words, and the
 // target's logit.  With: softmax - e[target].
-template <typename XT, typename TY, int EDGE, bool GRADIENT>
+template <typename XT, typename TY, int EDGE, int MODE>
 __global__ __launch_bounds__(2 * EDGE) void k_head_logits(HeadArgs a) {
   using T = TileOf<typename TY::op, TY::planes, EDGE, false, false>;
   using OP = typename TY::op;
@@ -184,7 +215,7 @@ __global__ __launch_bounds__(2 * EDGE) void k_head_logits(HeadArgs a) {
   // (words beyond the piece come to nothing below, whatever stands for them)
   t.product(head_operand<TY>(base, row, a, i * T::kM, 0), operand(base + a.w.hidden + (uint64_t)j * T::kN * pitch, pitch), a.s.K * TY::planes / 64, lds);
   const float held = ldexpf(1.f, -power_of<TY>(base, a, kHeadMostHidden) - power_of<TY>(base, a, kHeadMostHead));
-  if constexpr (GRADIENT) {
+  if constexpr (MODE == kHeadGradient) {
     struct Token {
       int32_t target;  // -1: none
       float lse;
@@ -219,22 +250,31 @@ __global__ __launch_bounds__(2 * EDGE) void k_head_logits(HeadArgs a) {
   } else {
     constexpr int MT = EDGE == 256 ? 4 : 2, WM = 2, WN = EDGE == 256 ? 4 : 2;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % WM, wn = wave / WM;
+    // the words' bias; of words beyond the piece an infinity, so that they cannot come
+    float DADAM_LDS* bias = (float DADAM_LDS*)lds;
+    __syncthreads();
+    if (threadIdx.x < EDGE) {
+      const uint32_t m = i * T::kM + threadIdx.x;
+      bias[threadIdx.x] = m >= a.words ? -INFINITY : row.bias ? XT::load(row.bias, a.first_word + m) : 0.f;
+    }
+    __syncthreads();
 #pragma unroll
     for (int jn = 0; jn < 2; ++jn) {
       const uint32_t n = j * T::kN + (jn * WN + wn) * 32 + (lane & 31);
       int32_t target;
-      const bool taken = has_target(a, row.target, n, target);
+      const uint32_t hit = has_target(a, row.target, n, target) ? (uint32_t)target - a.first_word - i * T::kM : 0xffffffffu;  // in the tile
       float most = -INFINITY;
+      asm volatile("" ::: "memory");  // (the biases are read again rather than kept in registers)
 #pragma unroll
       for (int im = 0; im < MT; ++im)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const uint32_t m = i * T::kM + (wm * MT + im) * 32 + g * 8 + (lane >> 5) * 4;  // in the piece
+          const uint32_t m = (wm * MT + im) * 32 + g * 8 + (lane >> 5) * 4;
+          const float4v b = *(const float4v DADAM_LDS*)(bias + m);
 #pragma unroll
           for (uint32_t e = 0; e < 4; ++e) {
-            float z = -INFINITY;
-            if (m + e < a.words) z = fmaf(t.acc[im][jn][4 * g + e], held, row.bias ? XT::load(row.bias, a.first_word + m + e) : 0.f);
-            if (taken && a.first_word + m + e == (uint32_t)target) global<float>(base + a.w.hit)[n] = z;
+            const float z = fmaf(t.acc[im][jn][4 * g + e], held, b[e]);
+            if (m + e == hit) global<float>(base + a.w.hit)[n] = z;
             most = fmaxf(most, z);
             t.acc[im][jn][4 * g + e] = z;
           }
@@ -245,14 +285,52 @@ __global__ __launch_bounds__(2 * EDGE) void k_head_logits(HeadArgs a) {
 #pragma unroll
       for (int im = 0; im < MT; ++im)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sum += __expf(t.acc[im][jn][r] - from);
+        for (int r = 0; r < 16; ++r) {
+          const float e = __expf(t.acc[im][jn][r] - from);
+          sum += e;
+          t.acc[im][jn][r] = e;
+        }
       sum += __shfl_xor(sum, 32);
       if (lane < 32) {
         const uint32_t slice = (a.first_word + i * T::kM) / (EDGE / 2) + wm;
         global<float2v>(base + a.w.stats)[(uint64_t)slice * a.s.T + n] = float2v{most, sum};
       }
     }
+    if constexpr (MODE == kHeadKeep)
+      t.hand_out(lds, false, nothing_ahead,
+                 [&](uint32_t m, uint32_t n, float (&v)[8], Nothing) {
+                   uint32_t w[8];
+#pragma unroll
+                   for (int k = 0; k < 8; ++k) w[k] = operand_word<Half, TY::planes>(v[k] * kept_times<TY>());
+                   store8<TY::planes>(base + a.w.p, j * T::kN + n, a.s.piece, i * T::kM + m, w);
+                 },
+                 [](uint32_t, uint32_t, const float (&)[8]) {});
   }
+}
+
+// softmax - e[target] in place of the slices' exponentials: a thread takes eight words of a token.
+template <typename TY>
+__global__ __launch_bounds__(256) void k_head_scale(HeadArgs a) {
+  using OP = typename TY::op;
+  const HeadRow& row = a.row[blockIdx.z];
+  const uint64_t base = base_of(a);
+  const uint32_t n = blockIdx.y, m = (blockIdx.x * 256 + threadIdx.x) * 8;
+  if (m >= a.s.piece) return;
+  int32_t target;
+  uint32_t w[8] = {};
+  if (has_target(a, row.target, n, target)) {
+    const float lse = global<const float>(base + a.w.lse)[n], most = global<const float2v>(base + a.w.stats)[(uint64_t)(m / (a.s.edge / 2)) * a.s.T + n][0];
+    const float factor = __expf(most - lse) * (TY::planes == 1 ? 1.f / kept_times<TY>() : 1.f);
+    const Eight e = load8<TY::planes>(base + a.w.p, n, a.s.piece, m);
+    const uint32_t hit = (uint32_t)target - m;
+#pragma unroll
+    for (uint32_t k = 0; k < 8; ++k) {
+      float p = value_of<Half, TY::planes == 2>(e, k) * factor;
+      if (k == hit) p = expm1f(-global<const float>(base + a.w.hit)[n]) * (TY::planes == 1 ? 1.f : (float)(1 << kHeldAt));
+      w[k] = operand_word<OP, TY::planes>(p);
+    }
+  }
+  store8<TY::planes>(base + a.w.p, n, a.s.piece, m, w);
 }
 
 // Every token's logarithm of the sum of exponentials and its loss: 16 tokens a workgroup, 16 threads a token.
@@ -454,13 +532,20 @@ int launch_head_words(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* 
     return launch<k_head_words<decltype(x), decltype(ty)>>(dim3(upto(words * a.s.D, 2048), 1, rows), 256, 0, stream, a);
   });
 }
-int launch_head_logits(int xdt, int gdt, bool gradient, const HeadArgs& a, uint32_t rows, void* stream) {
+int launch_head_logits(int xdt, int gdt, HeadMode mode, const HeadArgs& a, uint32_t rows, void* stream) {
   return with_tiles(xdt, gdt, a.s.edge, [&](auto x, auto, auto ty, auto edge) {
-    using T = TileOf<typename decltype(ty)::op, decltype(ty)::planes, decltype(edge)::value, false, false>;
+    using X = decltype(x);
+    using TY = decltype(ty);
+    constexpr int kEdge = decltype(edge)::value;
+    using T = TileOf<typename TY::op, TY::planes, kEdge, false, false>;
     const dim3 grid(upto(a.words, a.s.edge) * (a.s.T / a.s.edge), 1, rows);
-    return gradient ? launch<k_head_logits<decltype(x), decltype(ty), decltype(edge)::value, true>>(grid, T::kThreads, T::kLds, stream, a)
-                    : launch<k_head_logits<decltype(x), decltype(ty), decltype(edge)::value, false>>(grid, T::kThreads, T::kLds, stream, a);
+    if (mode == kHeadStatistics) return launch<k_head_logits<X, TY, kEdge, kHeadStatistics>>(grid, T::kThreads, T::kLds, stream, a);
+    if (mode == kHeadKeep) return launch<k_head_logits<X, TY, kEdge, kHeadKeep>>(grid, T::kThreads, T::kLds, stream, a);
+    return launch<k_head_logits<X, TY, kEdge, kHeadGradient>>(grid, T::kThreads, T::kLds, stream, a);
   });
+}
+int launch_head_scale(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
+  return with_types(xdt, gdt, [&](auto, auto, auto ty) { return launch<k_head_scale<decltype(ty)>>(dim3(upto(a.s.piece, 2048), a.s.T, rows), 256, 0, stream, a); });
 }
 int launch_head_losses(const HeadArgs& a, uint32_t rows, void* stream) {
   if (const int e = launch<k_head_losses>(dim3(a.s.T / 16, 1, rows), 256, 0, stream, a)) return e;
