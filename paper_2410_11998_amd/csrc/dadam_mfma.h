@@ -106,15 +106,19 @@ struct B16 {
   }
 };
 
-// Where a tile's side of an operand begins (at the first stage), its rows' distance in bytes (below 2^32), and how many of them there are: beyond, the last one
-// is taken again.
+// Where a tile's side of an operand begins (at the first stage), its rows' distance in bytes (a stage's rows within 2^32 of each other), and how many of
+// them there are: beyond, the last one is taken again.
 struct Operand {
-  const char DADAM_GLOBAL* at;
-  uint64_t pitch;
-  uint32_t limit;
+  uint64_t at;
+  uint32_t pitch, rows;
 };
 constexpr uint32_t kNoLimit = 0xffffffffu;
-__device__ __forceinline__ Operand operand(uint64_t at, uint64_t pitch, uint32_t limit = kNoLimit) { return {global<const char>(at), pitch, limit}; }
+__device__ __forceinline__ Operand operand(uint64_t at, uint64_t pitch, uint32_t rows = kNoLimit) { return {at, (uint32_t)pitch, rows}; }
+// The same for the whole wavefront, in scalar registers.
+__device__ __forceinline__ Operand uniform(const Operand& o) {
+  const uint32_t low = __builtin_amdgcn_readfirstlane((uint32_t)o.at), high = __builtin_amdgcn_readfirstlane((uint32_t)(o.at >> 32));
+  return {(uint64_t)high << 32 | low, (uint32_t)__builtin_amdgcn_readfirstlane(o.pitch), (uint32_t)__builtin_amdgcn_readfirstlane(o.rows)};
+}
 
 constexpr int kStageBytes = 128;  // of a row's elements that a stage takes: 64 elements of one plane, 32 of two
 
@@ -182,9 +186,10 @@ __device__ __forceinline__ double wave_sum(double v) {
   return v;
 }
 
-// What this wavefront has asked for is in LDS, and so is what the others have.
+// What this wavefront has asked for is in LDS, and so is what the others have; and nobody reads what was there before.  Nothing else is under way either: scalar
+// loads that are, and are not needed before the products' end, make the compiler wait for all fragments where it needs the older ones only.
 __device__ __forceinline__ void everybody_has_loaded() {
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
   __syncthreads();
 }
 
@@ -270,25 +275,27 @@ struct Tile {
     return ((k & 3) << 1 | (k >> 3 & 1) << 3) & (kPieces - 1);
   }
 
-  // Stage s of SIDE rows (DOWN: columns) of an operand into LDS, straight from memory; a wavefront's instruction brings 1 KB, lane l the 16 bytes that belong at
+  // A stage of SIDE rows (DOWN: columns) of an operand into LDS, straight from memory; a wavefront's instruction brings 1 KB, lane l the 16 bytes that belong at
   // l * 16 of it.  By rows that is 8 rows of 128 bytes, whose 16-byte pieces lie in the order piece ^ (row & 7), so that the lanes of a fragment, which read
-  // one piece of 32 rows, touch all banks.
+  // one piece of 32 rows, touch all banks.  `rows`: of the operand from the stage on.  (Buffer loads: of the global ones that go to LDS the compiler takes it that LDS
+  // reads may overtake them, and waits for all fragments where it needs the older ones only.)
+  static constexpr uint32_t kSummed = 16 * kSteps;  // of a stage
   template <int SIDE, bool DOWN>
-  static __device__ __forceinline__ void fetch(const Operand& o, uint32_t s, char DADAM_LDS* lds, int wave, int lane) {
+  static __device__ __forceinline__ void fetch(uint64_t at, uint32_t pitch, uint32_t rows, char DADAM_LDS* lds, int wave, int lane) {
+    const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, -1, 0x00020000);
 #pragma unroll
     for (int j = 0; j < SIDE / 8 / kWaves; ++j) {
       const int part = j * kWaves + wave;
-      const char DADAM_GLOBAL* from;
+      uint32_t from;
       if constexpr (DOWN) {
         constexpr int kRowBytes = SIDE * 2 * PLANES, kPieces = kRowBytes / 16;
-        const uint32_t k = (uint32_t)((part * 64 + lane) / kPieces), piece = (uint32_t)(lane % kPieces) ^ (mixed<SIDE>(k) << 1);
-        const uint32_t row = s * (16 * kSteps) + k;
-        from = o.at + (uint64_t)(row < o.limit ? row : o.limit - 1) * (uint32_t)o.pitch + piece * 16;
+        const uint32_t k = (uint32_t)(part * 64 + lane) / kPieces, piece = (uint32_t)(lane % kPieces) ^ (mixed<SIDE>(k) << 1);
+        from = (k < rows ? k : rows - 1) * pitch + piece * 16;
       } else {
         const uint32_t row = (uint32_t)(part * 8 + (lane >> 3)), piece = (uint32_t)((lane & 7) ^ (lane >> 3));
-        from = o.at + (uint64_t)s * kStageBytes + (uint64_t)(row < o.limit ? row : o.limit - 1) * (uint32_t)o.pitch + piece * 16;
+        from = (row < rows ? row : rows - 1) * pitch + piece * 16;
       }
-      __builtin_amdgcn_global_load_lds((const uint32_t DADAM_GLOBAL*)from, (uint32_t DADAM_LDS*)(lds + part * 1024), 16, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (void DADAM_LDS*)(lds + part * 1024), 16, from, 0, 0, 0);
     }
   }
 
@@ -364,10 +371,12 @@ struct Tile {
   __device__ __forceinline__ void product(const Operand& a, const Operand& b, uint32_t stages, char DADAM_LDS* lds) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WM, wn = wave / WM;
+    const Operand ua = uniform(a), ub = uniform(b);
     auto bring = [&](uint32_t s) {
       char DADAM_LDS* to = lds + (s & 1) * kStage;
-      fetch<kM, A_DOWN>(a, s, to, wave, lane);
-      fetch<kN, B_DOWN>(b, s, to + kM * kStageBytes, wave, lane);
+      fetch<kM, A_DOWN>(ua.at + (A_DOWN ? (uint64_t)s * kSummed * ua.pitch : (uint64_t)s * kStageBytes), ua.pitch, A_DOWN ? ua.rows - s * kSummed : ua.rows, to, wave, lane);
+      fetch<kN, B_DOWN>(ub.at + (B_DOWN ? (uint64_t)s * kSummed * ub.pitch : (uint64_t)s * kStageBytes), ub.pitch, B_DOWN ? ub.rows - s * kSummed : ub.rows,
+                        to + kM * kStageBytes, wave, lane);
     };
     clear();
     bring(0);
