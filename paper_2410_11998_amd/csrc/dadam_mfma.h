@@ -186,6 +186,13 @@ __device__ __forceinline__ double wave_sum(double v) {
   return v;
 }
 
+// 16 bytes a lane from `offset` of a buffer to LDS, 1 KB side by side from `to` on.  Nothing waits for it but everybody_has_loaded().  (In assembly, as the compiler
+// takes the builtin's load for one that any LDS read may depend on: of the global loads it then waits for all fragments where it needs the older ones only,
+// and before a read that turns for all loads.  No register is written but m0, which nothing else here uses.)
+__device__ __forceinline__ void load_to_lds(uint4v buffer, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(buffer) : "memory");
+}
+
 // What this wavefront has asked for is in LDS, and so is what the others have; and nobody reads what was there before.  Nothing else is under way either: scalar
 // loads that are, and are not needed before the products' end, make the compiler wait for all fragments where it needs the older ones only.
 __device__ __forceinline__ void everybody_has_loaded() {
@@ -193,52 +200,15 @@ __device__ __forceinline__ void everybody_has_loaded() {
   __syncthreads();
 }
 
-// Fragments of blocks that lie by columns: elements of two times four rows, AT and NEXT bytes behind at[...].  The reads are one block with their wait in it:
-// written with the compiler's builtin, each of them waits for all loads into LDS that are under way, the next stage's among them.
-template <int AT, int NEXT, typename V>
-__device__ __forceinline__ void read_turned(V (&out)[2], const uint32_t (&at)[2]) {
-  short4v o[4];
-  asm volatile(
-      "ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
-      "ds_read_b64_tr_b16 %2, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(o[0]), "=&v"(o[1]), "=&v"(o[2]), "=&v"(o[3])
-      : "v"(at[0]), "v"(at[1]), "n"(AT), "n"(NEXT)
-      : "memory");
+// Fragments of blocks that lie by columns: elements of two times four rows, AT and NEXT bytes behind at[...].
+template <int AT, int NEXT, typename V, int N>
+__device__ __forceinline__ void read_turned(V (&out)[N], const uint32_t (&at)[N]) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i) out[i] = __builtin_bit_cast(V, __builtin_shufflevector(o[2 * i], o[2 * i + 1], 0, 1, 2, 3, 4, 5, 6, 7));
-}
-template <int AT, int NEXT, typename V>
-__device__ __forceinline__ void read_turned(V (&out)[4], const uint32_t (&at)[4]) {
-  short4v o[8];
-  asm volatile(
-      "ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
-      "ds_read_b64_tr_b16 %2, %9 offset:%12\n\tds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
-      "ds_read_b64_tr_b16 %4, %10 offset:%12\n\tds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
-      "ds_read_b64_tr_b16 %6, %11 offset:%12\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(o[0]), "=&v"(o[1]), "=&v"(o[2]), "=&v"(o[3]), "=&v"(o[4]), "=&v"(o[5]), "=&v"(o[6]), "=&v"(o[7])
-      : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(AT), "n"(NEXT)
-      : "memory");
-#pragma unroll
-  for (int i = 0; i < 4; ++i) out[i] = __builtin_bit_cast(V, __builtin_shufflevector(o[2 * i], o[2 * i + 1], 0, 1, 2, 3, 4, 5, 6, 7));
-}
-template <int AT, int NEXT, typename V>
-__device__ __forceinline__ void read_turned(V (&out)[6], const uint32_t (&at)[6]) {
-  short4v o[12];
-  asm volatile(
-      "ds_read_b64_tr_b16 %0, %12 offset:%18\n\tds_read_b64_tr_b16 %1, %12 offset:%19\n\t"
-      "ds_read_b64_tr_b16 %2, %13 offset:%18\n\tds_read_b64_tr_b16 %3, %13 offset:%19\n\t"
-      "ds_read_b64_tr_b16 %4, %14 offset:%18\n\tds_read_b64_tr_b16 %5, %14 offset:%19\n\t"
-      "ds_read_b64_tr_b16 %6, %15 offset:%18\n\tds_read_b64_tr_b16 %7, %15 offset:%19\n\t"
-      "ds_read_b64_tr_b16 %8, %16 offset:%18\n\tds_read_b64_tr_b16 %9, %16 offset:%19\n\t"
-      "ds_read_b64_tr_b16 %10, %17 offset:%18\n\tds_read_b64_tr_b16 %11, %17 offset:%19\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(o[0]), "=&v"(o[1]), "=&v"(o[2]), "=&v"(o[3]), "=&v"(o[4]), "=&v"(o[5]), "=&v"(o[6]), "=&v"(o[7]), "=&v"(o[8]), "=&v"(o[9]), "=&v"(o[10]), "=&v"(o[11])
-      : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "n"(AT), "n"(NEXT)
-      : "memory");
-#pragma unroll
-  for (int i = 0; i < 6; ++i) out[i] = __builtin_bit_cast(V, __builtin_shufflevector(o[2 * i], o[2 * i + 1], 0, 1, 2, 3, 4, 5, 6, 7));
+  for (int i = 0; i < N; ++i) {
+    const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v DADAM_LDS*)(uintptr_t)(at[i] + AT));
+    const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v DADAM_LDS*)(uintptr_t)(at[i] + NEXT));
+    out[i] = __builtin_bit_cast(V, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
 }
 
 // Shape of a workgroup's tile: WM x WN wavefronts, each MT x NT blocks of 32 x 32; block (i, j) of wavefront (wm, wn) has rows (wm MT + i) 32 ... and columns
@@ -276,13 +246,12 @@ struct Tile {
   }
 
   // A stage of SIDE rows (DOWN: columns) of an operand into LDS, straight from memory; a wavefront's instruction brings 1 KB, lane l the 16 bytes that belong at
-  // l * 16 of it.  By rows that is 8 rows of 128 bytes, whose 16-byte pieces lie in the order piece ^ (row & 7), so that the lanes of a fragment, which read
-  // one piece of 32 rows, touch all banks.  `rows`: of the operand from the stage on.  (Buffer loads: of the global ones that go to LDS the compiler takes it that LDS
-  // reads may overtake them, and waits for all fragments where it needs the older ones only.)
+  // l * 16 of it.  By rows that is 8 rows of 128 bytes, whose 16-byte pieces lie in the order piece ^ (row / 2 & 7): the lanes of a fragment read one piece of 32
+  // rows, sixteen of them at a time, which are then in sixteen different places of 256 bytes.  (With row & 7 in eight: half of the LDS cycles were conflicts.)  `rows`: of the operand from the stage on.
   static constexpr uint32_t kSummed = 16 * kSteps;  // of a stage
   template <int SIDE, bool DOWN>
   static __device__ __forceinline__ void fetch(uint64_t at, uint32_t pitch, uint32_t rows, char DADAM_LDS* lds, int wave, int lane) {
-    const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, -1, 0x00020000);
+    const uint4v buffer = {(uint32_t)at, (uint32_t)(at >> 32), 0xffffffffu, 0x00020000u};
 #pragma unroll
     for (int j = 0; j < SIDE / 8 / kWaves; ++j) {
       const int part = j * kWaves + wave;
@@ -292,10 +261,10 @@ struct Tile {
         const uint32_t k = (uint32_t)(part * 64 + lane) / kPieces, piece = (uint32_t)(lane % kPieces) ^ (mixed<SIDE>(k) << 1);
         from = (k < rows ? k : rows - 1) * pitch + piece * 16;
       } else {
-        const uint32_t row = (uint32_t)(part * 8 + (lane >> 3)), piece = (uint32_t)((lane & 7) ^ (lane >> 3));
+        const uint32_t row = (uint32_t)(part * 8 + (lane >> 3)), piece = (uint32_t)(lane & 7) ^ (row >> 1 & 7);
         from = (row < rows ? row : rows - 1) * pitch + piece * 16;
       }
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (void DADAM_LDS*)(lds + part * 1024), 16, from, 0, 0, 0);
+      load_to_lds(buffer, from, (uint32_t)(uintptr_t)(lds + part * 1024));
     }
   }
 
@@ -305,7 +274,7 @@ struct Tile {
   };
   // By rows: block `block` of 32.
   static __device__ __forceinline__ vec fragment(const char DADAM_LDS* side, int block, int plane, int step, int lane) {
-    const uint32_t piece = (uint32_t)((lane >> 5) ^ (lane & 7)) ^ (uint32_t)((step + 2 * plane) << 1);
+    const uint32_t piece = (uint32_t)((lane >> 5) ^ (lane >> 1 & 7)) ^ (uint32_t)((step + 2 * plane) << 1);
     return *(const vec DADAM_LDS*)(side + (block * 32 + (lane & 31)) * kStageBytes + piece * 16);
   }
   // By columns: where the lane's part of block `block` of SIDE begins.  Sixteen lanes get four rows of sixteen columns, every lane the four of its column.
@@ -353,21 +322,17 @@ struct Tile {
     static_assert(A_DOWN || !B_DOWN, "an operand that lies by columns is the first one");
   }
   __device__ __forceinline__ void multiply(const Fragments& f) {
+    // (one product of all blocks after the other: three in a row onto the same sums would wait for each other)
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+    for (int p = PLANES == 1 ? 2 : 0; p < 3; ++p)
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        if constexpr (PLANES == 2) {
-          acc[i][j] = OP::mfma(f.a[1][i], f.b[0][j], acc[i][j]);
-          acc[i][j] = OP::mfma(f.a[0][i], f.b[1][j], acc[i][j]);
-        }
-        acc[i][j] = OP::mfma(f.a[0][i], f.b[0][j], acc[i][j]);
-      }
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = OP::mfma(f.a[p == 0 ? PLANES - 1 : 0][i], f.b[p == 1 ? PLANES - 1 : 0][j], acc[i][j]);
   }
 
-  // The sums over `stages` stages (of 64 summed elements, or 32 of two planes), from zero on.  While a stage is multiplied the next one is on its way, and with one
-  // plane by rows (two have no registers for it, and what is turned is waited for where it is read) while a step is multiplied the next one's fragments are:
-  // 128 x 128 x 1024 tiles 805 TFLOP/s instead of 695.
+  // The sums over `stages` stages (of 64 summed elements, or 32 of two planes), from zero on.  While a stage is multiplied the next one is on its way, and while a
+  // step is multiplied the next one's fragments are.
   __device__ __forceinline__ void product(const Operand& a, const Operand& b, uint32_t stages, char DADAM_LDS* lds) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WM, wn = wave / WM;
@@ -380,45 +345,28 @@ struct Tile {
     };
     clear();
     bring(0);
-    if constexpr (PLANES == 1 && !A_DOWN && !B_DOWN) {
-      Fragments f[2];
-      everybody_has_loaded();
-      read<0>(f[0], lds, wm, wn, lane);
-      for (uint32_t s = 0; s < stages; ++s) {
-        const char DADAM_LDS* stage = lds + (s & 1) * kStage;
-        if (s + 1 < stages) bring(s + 1);
-        auto step = [&](int k) {
-          __builtin_amdgcn_sched_barrier(0);
-          multiply(f[k & 1]);
-          __builtin_amdgcn_sched_barrier(0);
-        };
-        read<1>(f[1], stage, wm, wn, lane);
-        step(0);
+    Fragments f[2];
+    everybody_has_loaded();
+    read<0>(f[0], lds, wm, wn, lane);
+    for (uint32_t s = 0; s < stages; ++s) {
+      const char DADAM_LDS* stage = lds + (s & 1) * kStage;
+      if (s + 1 < stages) bring(s + 1);
+      auto step = [&](int k) {
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(f[k & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      read<1>(f[1], stage, wm, wn, lane);
+      step(0);
+      if constexpr (kSteps == 4) {
         read<2>(f[0], stage, wm, wn, lane);
         step(1);
         read<3>(f[1], stage, wm, wn, lane);
         step(2);
-        everybody_has_loaded();  // and read this stage
-        if (s + 1 < stages) read<0>(f[0], lds + ((s + 1) & 1) * kStage, wm, wn, lane);
-        step(3);
       }
-    } else {
-      for (uint32_t s = 0; s < stages; ++s) {
-        const char DADAM_LDS* stage = lds + (s & 1) * kStage;
-        everybody_has_loaded();
-        if (s + 1 < stages) bring(s + 1);
-        auto step = [&](auto k) {
-          Fragments f;
-          read<decltype(k)::value>(f, stage, wm, wn, lane);
-          multiply(f);
-        };
-        step(std::integral_constant<int, 0>{});
-        step(std::integral_constant<int, 1>{});
-        if constexpr (kSteps == 4) {
-          step(std::integral_constant<int, 2>{});
-          step(std::integral_constant<int, 3>{});
-        }
-      }
+      everybody_has_loaded();  // and read this stage
+      if (s + 1 < stages) read<0>(f[0], lds + ((s + 1) & 1) * kStage, wm, wn, lane);
+      step(1);
     }
   }
 
