@@ -38,15 +38,16 @@ struct Way {
   uint64_t each;  // workspace of a replica
 };
 
-constexpr uint32_t kSplits = 16;              // at most
+constexpr uint32_t kSplits = 64;               // at most
 constexpr uint64_t kMostOfPiece = 1ull << 27;  // tokens times words of a piece
 constexpr uint64_t kMostKept = 1ull << 31;     // bytes of softmax that a replica may keep
+constexpr uint64_t kMostAtOnce = 1ull << 31;   // bytes of workspace for which replicas are taken together
 // Workgroups that the chip holds at a time: one large tile a compute unit, two small ones.
 uint32_t at_once(uint32_t edge) { return edge == 256 ? 256 : 512; }
 
 bool suits_large(uint32_t n) { return 8 * (uint64_t)filled(n, 256) <= 9 * (uint64_t)filled(n, 128); }
 
-void fill_shape(const dadam_head* head, uint32_t n_tokens, uint32_t planes, uint32_t edge, uint32_t rows, uint32_t piece, HeadShape* s) {
+void fill_shape(const dadam_head* head, uint32_t n_tokens, uint32_t planes, uint32_t edge, uint32_t piece, HeadShape* s) {
   s->tokens = n_tokens;
   s->vocab = head->vocab;
   s->width = head->width;
@@ -57,7 +58,7 @@ void fill_shape(const dadam_head* head, uint32_t n_tokens, uint32_t planes, uint
   s->piece = std::min(piece, filled(head->vocab, edge));
   s->slices = filled(head->vocab, edge) / (edge / 2);
   s->keeps = 0;
-  const uint64_t tiles = (uint64_t)(s->T / edge) * (s->D / edge) * rows, stages = (uint64_t)s->piece * planes / 64;
+  const uint64_t tiles = (uint64_t)(s->T / edge) * (s->D / edge), stages = (uint64_t)s->piece * planes / 64;
   s->splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(std::min<uint64_t>((at_once(edge) + tiles - 1) / tiles, stages / 8), kSplits));
 }
 
@@ -74,8 +75,10 @@ Way good_way(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, b
     piece = std::max<uint64_t>(edge, std::min(piece, kMostOfPiece / (down * edge) / edge * edge));
     piece = std::min(piece, all);
   }
-  w.rows = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(R, 2 * at_once(edge) / (piece / edge * std::min(across, down))));
-  fill_shape(head, n_tokens, planes, edge, w.rows, (uint32_t)piece, &w.s);
+  // Replicas together, so that the last workgroups of a launch have company: tiles of one replica's head are 3.1 times what the chip holds (4 x 4096 tokens, 50257
+  // words, width 1024), of four 12.3 times.
+  fill_shape(head, n_tokens, planes, edge, (uint32_t)piece, &w.s);
+  w.rows = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(R, kMostAtOnce / head_places(w.s, planes, gradient).bytes));
   w.s.keeps = keeps;
   w.each = head_places(w.s, planes, gradient).bytes;
   return w;
@@ -89,7 +92,7 @@ bool may_keep(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, 
 Way least_way(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, bool gradient) {
   Way w{};
   w.rows = 1;
-  fill_shape(head, n_tokens, planes_of(h), 128, 1, 128, &w.s);
+  fill_shape(head, n_tokens, planes_of(h), 128, 128, &w.s);
   w.each = head_places(w.s, planes_of(h), gradient).bytes;
   return w;
 }
@@ -107,11 +110,11 @@ Way way_for(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, bo
   uint32_t low = 1, high = std::max(2u, w.s.piece / 128);  // small tiles of a piece: what fits, and what does not or need not
   while (low + 1 < high) {
     const uint32_t middle = (low + high) / 2;
-    fill_shape(head, n_tokens, planes, 128, 1, middle * 128, &w.s);
+    fill_shape(head, n_tokens, planes, 128, middle * 128, &w.s);
     (head_places(w.s, planes, gradient).bytes <= bytes ? low : high) = middle;
   }
   w.rows = 1;
-  fill_shape(head, n_tokens, planes, 128, 1, low * 128, &w.s);
+  fill_shape(head, n_tokens, planes, 128, low * 128, &w.s);
   w.each = head_places(w.s, planes, gradient).bytes;
   return w;
 }

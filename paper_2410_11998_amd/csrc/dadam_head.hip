@@ -89,7 +89,7 @@ __global__ __launch_bounds__(256) void k_head_count(HeadArgs a) {
 }
 
 // Largest finite magnitudes: of the head (blockIdx.y 0) and of the hidden vectors of tokens with a target (1).  The largest is the same in any order.
-constexpr uint32_t kMostGroups = 2048;  // workgroups
+constexpr uint32_t kMostGroups = 512;  // workgroups: each ends in an atomic on one word
 __device__ __forceinline__ void larger(uint32_t& most, float v) {
   const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
   if (b < 0x7f800000u && b > most) most = b;
@@ -208,7 +208,9 @@ __global__ __launch_bounds__(2 * EDGE) void k_head_logits(HeadArgs a) {
   using OP = typename TY::op;
   const HeadRow& row = a.row[blockIdx.z];
   const uint64_t base = base_of(a);
-  const uint32_t across = a.s.T / T::kN, u = die_run(blockIdx.x, gridDim.x, a.n_xcd), i = u / across, j = u % across;
+  const uint32_t across = a.s.T / T::kN;
+  uint32_t i, j;
+  banded(die_run(blockIdx.x, gridDim.x, a.n_xcd), across, gridDim.x / across, j, i);
   char DADAM_LDS* lds = (char DADAM_LDS*)head_lds;
   const uint64_t pitch = (uint64_t)a.s.D * 2 * TY::planes;
   T t;
@@ -391,7 +393,9 @@ __global__ __launch_bounds__(2 * EDGE) void k_head_dhead(HeadArgs a) {
   using T = TileOf<typename TY::op, TY::planes, EDGE, true, true>;
   const HeadRow& row = a.row[blockIdx.z];
   const uint64_t base = base_of(a);
-  const uint32_t across = a.s.D / T::kM, u = die_run(blockIdx.x, gridDim.x, a.n_xcd), i = u % across, j = u / across;
+  const uint32_t across = a.s.D / T::kM;
+  uint32_t i, j;
+  banded(die_run(blockIdx.x, gridDim.x, a.n_xcd), across, gridDim.x / across, i, j);
   const uint64_t b = 2 * TY::planes;
   char DADAM_LDS* lds = (char DADAM_LDS*)head_lds;
   T t;
@@ -448,7 +452,9 @@ __global__ __launch_bounds__(2 * EDGE) void k_head_dhidden(HeadArgs a) {
   using T = TileOf<typename TY::op, TY::planes, EDGE, true, false>;
   const HeadRow& row = a.row[blockIdx.z];
   const uint64_t base = base_of(a);
-  const uint32_t across = a.s.D / T::kM, u = die_run(blockIdx.x, gridDim.x, a.n_xcd), i = u % across, j = u / across, split = blockIdx.y;
+  const uint32_t across = a.s.D / T::kM, down = a.s.T / T::kN, u = die_run(blockIdx.x, gridDim.x, a.n_xcd), split = u / (across * down);
+  uint32_t i, j;
+  banded(u % (across * down), across, down, i, j);
   const uint64_t b = 2 * TY::planes, pitch = a.s.piece * b;
   constexpr uint32_t kEach = 64 / TY::planes;  // words of a stage
   const uint32_t stages = (a.words + kEach - 1) / kEach;
@@ -463,28 +469,33 @@ __global__ __launch_bounds__(2 * EDGE) void k_head_dhidden(HeadArgs a) {
     float4v a, b;
   };
   auto at = [&](uint32_t m, uint32_t n) { return global<float4v>(sums + ((uint64_t)(j * T::kN + n) * a.s.D + i * T::kM + m) * 4); };
-  t.hand_out(lds, false, [&](uint32_t m, uint32_t n) { return a.later ? Held{at(m, n)[0], at(m, n)[1]} : Held{}; },
+  t.hand_out(lds, false, [&](uint32_t m, uint32_t n) { return a.later && j * T::kN + n < a.s.tokens ? Held{at(m, n)[0], at(m, n)[1]} : Held{}; },
              [&](uint32_t m, uint32_t n, float (&v)[8], const Held& held) {
+               if (j * T::kN + n >= a.s.tokens) return;
                at(m, n)[0] = float4v{v[0], v[1], v[2], v[3]} + held.a;
                at(m, n)[1] = float4v{v[4], v[5], v[6], v[7]} + held.b;
              },
              [](uint32_t, uint32_t, const float (&)[8]) {});
 }
 
+// dh of 256 columns of a token, four a thread, from the parts of its sum.
 template <typename XT, typename TY>
-__global__ __launch_bounds__(256) void k_head_end(HeadArgs a) {
+__global__ __launch_bounds__(64) void k_head_end(HeadArgs a) {
   const HeadRow& row = a.row[blockIdx.z];
-  const uint64_t base = base_of(a), each = (uint64_t)a.s.T * a.s.D;
+  const uint64_t base = base_of(a), each = (uint64_t)a.s.T * a.s.D * 4;
   const float factor = factor_of(base, a) * (TY::planes == 1 ? 1.f : ldexpf(1.f, -power_of<TY>(base, a, kHeadMostHead) - kHeldAt));
-  const uint32_t n = blockIdx.x;
+  const uint32_t n = blockIdx.x, c = blockIdx.y * 256 + threadIdx.x * 4;
+  if (c >= a.s.width) return;
   int32_t target;
-  const bool taken = has_target(a, row.target, n, target);
-  for (uint32_t c = threadIdx.x; c < a.s.width; c += 256) {
-    float v = 0.f;
-    if (taken)
-      for (uint32_t s = 0; s < a.s.splits; ++s) v += global<const float>(base + a.w.sums)[s * each + (uint64_t)n * a.s.D + c];
-    XT::store(row.dhidden, (uint64_t)n * a.s.width + c, v * factor);
+  float4v v = {0.f, 0.f, 0.f, 0.f};
+  if (has_target(a, row.target, n, target)) {
+    const uint64_t at = base + a.w.sums + ((uint64_t)n * a.s.D + c) * 4;
+#pragma unroll 8
+    for (uint32_t s = 0; s < a.s.splits; ++s) v += global<const float4v>(at + s * each)[0];
   }
+#pragma unroll
+  for (uint32_t k = 0; k < 4; ++k)
+    if (c + k < a.s.width) XT::store(row.dhidden, (uint64_t)n * a.s.width + c + k, v[k] * factor);
 }
 
 template <auto KERNEL, typename... A>
@@ -563,11 +574,11 @@ int launch_head_dbias(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* 
 int launch_head_dhidden(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
   return with_tiles(xdt, gdt, a.s.edge, [&](auto, auto, auto ty, auto edge) {
     using T = TileOf<typename decltype(ty)::op, decltype(ty)::planes, decltype(edge)::value, true, false>;
-    return launch<k_head_dhidden<decltype(ty), decltype(edge)::value>>(dim3((a.s.T / a.s.edge) * (a.s.D / a.s.edge), a.s.splits, rows), T::kThreads, T::kLds, stream, a);
+    return launch<k_head_dhidden<decltype(ty), decltype(edge)::value>>(dim3((a.s.T / a.s.edge) * (a.s.D / a.s.edge) * a.s.splits, 1, rows), T::kThreads, T::kLds, stream, a);
   });
 }
 int launch_head_end(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
-  return with_types(xdt, gdt, [&](auto x, auto, auto ty) { return launch<k_head_end<decltype(x), decltype(ty)>>(dim3(a.s.tokens, 1, rows), 256, 0, stream, a); });
+  return with_types(xdt, gdt, [&](auto x, auto, auto ty) { return launch<k_head_end<decltype(x), decltype(ty)>>(dim3(a.s.tokens, upto(a.s.width, 256), rows), 64, 0, stream, a); });
 }
 
 }  // namespace dadam

@@ -55,6 +55,12 @@ struct Brain {
 // stored).
 struct F32 {
   using type = float;
+  struct Piece {  // eight elements as they lie, of a whole piece
+    float4v a, b;
+    __device__ __forceinline__ float operator[](int k) const { return k < 4 ? a[k] : b[k - 4]; }
+  };
+  static __device__ __forceinline__ bool is_whole(uint64_t p, uint64_t e, uint32_t n) { return n >= 8 && (p + e * 4) % 16 == 0; }
+  static __device__ __forceinline__ Piece piece(uint64_t p, uint64_t e) { return {global<const float4v>(p + e * 4)[0], global<const float4v>(p + e * 4)[1]}; }
   static __device__ __forceinline__ float load(uint64_t p, uint64_t e) { return global<const float>(p)[e]; }
   static __device__ __forceinline__ void store(uint64_t p, uint64_t e, float v) { global<float>(p)[e] = v; }
   static __device__ __forceinline__ void load8(uint64_t p, uint64_t e, uint32_t n, float (&v)[8]) {
@@ -80,6 +86,12 @@ struct F32 {
 };
 struct B16 {
   using type = uint16_t;
+  struct Piece {
+    uint4v a;
+    __device__ __forceinline__ float operator[](int k) const { return Brain::value(a[k / 2] >> 16 * (k & 1) & 0xffffu); }
+  };
+  static __device__ __forceinline__ bool is_whole(uint64_t p, uint64_t e, uint32_t n) { return n >= 8 && (p + e * 2) % 16 == 0; }
+  static __device__ __forceinline__ Piece piece(uint64_t p, uint64_t e) { return {global<const uint4v>(p + e * 2)[0]}; }
   static __device__ __forceinline__ float load(uint64_t p, uint64_t e) { return Brain::value(global<const uint16_t>(p)[e]); }
   static __device__ __forceinline__ void store(uint64_t p, uint64_t e, float v) { global<uint16_t>(p)[e] = (uint16_t)Brain::bits(v); }
   static __device__ __forceinline__ void load8(uint64_t p, uint64_t e, uint32_t n, float (&v)[8]) {
@@ -457,6 +469,15 @@ int ask_for_lds(uint32_t bytes) {
   const hipError_t e = hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
   if (e == hipSuccess) asked.fetch_or(bit, std::memory_order_relaxed);
   return (int)e;
+}
+
+// Tile u of `across` x `down`, in bands of kBand across: the workgroups that a die runs at a time, neighbours in this order, then share few rows and columns of
+// the operands.  8192 x 8192 x 1024 by large tiles: 1196 TFLOP/s in bands of 8, 999 row by row.
+constexpr uint32_t kBand = 8;
+__device__ __forceinline__ void banded(uint32_t u, uint32_t across, uint32_t down, uint32_t& i, uint32_t& j) {
+  const uint32_t band = u / (kBand * down), in = u % (kBand * down), wide = across - band * kBand < kBand ? across - band * kBand : kBand;
+  i = band * kBand + in % wide;
+  j = in / wide;
 }
 
 }  // namespace

@@ -20,8 +20,8 @@ struct MatrixState {
   std::vector<uint64_t> need[2];  // bytes of workspace of a matrix and a replica, with one plane and with two
   char* memory = nullptr;         // tasks, and the matrix of every tile of each kind
   const OrthoTask* d_tasks[2] = {};
-  const uint32_t* d_units[3] = {};  // OrthoTask::gram_units, whole_units, cell_units
-  uint32_t n_units[3] = {};
+  const uint32_t* d_units[4] = {};  // OrthoTask::gram_units, whole_units, cell_units, small_units
+  uint32_t n_units[4] = {};
   // dadam_set_ortho_schedule
   std::vector<float> coefficients{3.4445f, -4.7750f, 2.0315f, 3.4445f, -4.7750f, 2.0315f, 3.4445f, -4.7750f, 2.0315f, 3.4445f, -4.7750f, 2.0315f, 3.4445f, -4.7750f, 2.0315f};
 };
@@ -103,7 +103,7 @@ int set_matrices(dadam_handle* h, const dadam_matrix_desc* m, uint32_t n) {
     t.scale = m[k].scale;
     t.decay = tensor.weight_decay;
   }
-  uint64_t large = 0, units[3] = {};
+  uint64_t large = 0, units[4] = {};
   for (const OrthoTask& t : tasks)
     if (t.edge == kLargeEdge) large += lower_half(filled(t.p, kLargeEdge) / kLargeEdge);
   for (OrthoTask& t : tasks) {
@@ -113,22 +113,25 @@ int set_matrices(dadam_handle* h, const dadam_matrix_desc* m, uint32_t n) {
     units[0] += lower_half(t.P / t.edge);
     units[1] += (uint64_t)(t.P / t.edge) * (t.Q / t.edge);
     units[2] += (uint64_t)(t.P / kOrthoCell) * (t.Q / kOrthoCell);
+    units[3] += lower_half(t.P / kSmallEdge);
   }
   if (units[2] >> 31) return fail(h, DADAM_EINVAL, "the matrices have more than 2^31 tiles");
   // by tile and size, the largest first
   std::stable_sort(tasks.begin(), tasks.end(), [](const OrthoTask& a, const OrthoTask& b) {
     return a.edge != b.edge ? a.edge > b.edge : (uint64_t)a.P * a.P * a.Q > (uint64_t)b.P * b.P * b.Q;
   });
-  std::vector<uint32_t> of_unit[3];
-  for (int kind = 0; kind < 3; ++kind) of_unit[kind].reserve(units[kind]);
+  std::vector<uint32_t> of_unit[4];
+  for (int kind = 0; kind < 4; ++kind) of_unit[kind].reserve(units[kind]);
   for (uint32_t k = 0; k < n; ++k) {
     OrthoTask& t = tasks[k];
     t.gram_units = (uint32_t)of_unit[0].size();
     t.whole_units = (uint32_t)of_unit[1].size();
     t.cell_units = (uint32_t)of_unit[2].size();
+    t.small_units = (uint32_t)of_unit[3].size();
     of_unit[0].insert(of_unit[0].end(), lower_half(t.P / t.edge), k);
     of_unit[1].insert(of_unit[1].end(), (uint64_t)(t.P / t.edge) * (t.Q / t.edge), k);
     of_unit[2].insert(of_unit[2].end(), (uint64_t)(t.P / kOrthoCell) * (t.Q / kOrthoCell), k);
+    of_unit[3].insert(of_unit[3].end(), lower_half(t.P / kSmallEdge), k);
   }
   std::vector<OrthoTask> planes[2] = {tasks, tasks};
   for (uint32_t p = 0; p < 2; ++p) {
@@ -141,7 +144,7 @@ int set_matrices(dadam_handle* h, const dadam_matrix_desc* m, uint32_t n) {
     s->need[p].push_back(at);
   }
   s->tasks = planes[0];
-  for (int kind = 0; kind < 3; ++kind) s->n_units[kind] = (uint32_t)of_unit[kind].size();
+  for (int kind = 0; kind < 4; ++kind) s->n_units[kind] = (uint32_t)of_unit[kind].size();
   if (h->cfg.device != DADAM_DEVICE_NONE && n) {
     DeviceGuard guard(h->cfg.device);
     if (guard.err != hipSuccess) return fail(h, DADAM_EHIP, "hipSetDevice: %s", hipGetErrorString(guard.err));
@@ -152,7 +155,7 @@ int set_matrices(dadam_handle* h, const dadam_matrix_desc* m, uint32_t n) {
       memcpy(image.data() + at, v.data(), v.size() * sizeof(v[0]));
       return at;
     };
-    size_t at[5] = {add(planes[0]), add(planes[1]), add(of_unit[0]), add(of_unit[1]), add(of_unit[2])};
+    size_t at[6] = {add(planes[0]), add(planes[1]), add(of_unit[0]), add(of_unit[1]), add(of_unit[2]), add(of_unit[3])};
     hipError_t e = hipMalloc((void**)&s->memory, image.size());
     if (e == hipSuccess) e = hipMemcpy(s->memory, image.data(), image.size(), hipMemcpyHostToDevice);
     if (e != hipSuccess) {
@@ -160,7 +163,7 @@ int set_matrices(dadam_handle* h, const dadam_matrix_desc* m, uint32_t n) {
       return fail(h, DADAM_EHIP, "uploading the matrices failed: %s", hipGetErrorString(e));
     }
     for (int p = 0; p < 2; ++p) s->d_tasks[p] = reinterpret_cast<const OrthoTask*>(s->memory + at[p]);
-    for (int kind = 0; kind < 3; ++kind) s->d_units[kind] = reinterpret_cast<const uint32_t*>(s->memory + at[2 + kind]);
+    for (int kind = 0; kind < 4; ++kind) s->d_units[kind] = reinterpret_cast<const uint32_t*>(s->memory + at[2 + kind]);
     MatrixState* old = h->matrices;
     h->matrices = s.release();
     h->free_matrices = free_matrices;
@@ -228,13 +231,13 @@ struct Call {
 int run_group(dadam_handle* h, const Call& call, const Powers& pw, uint32_t k0, uint32_t k1, uint32_t i0, uint32_t replicas, void* stream) {
   const MatrixState& m = *h->matrices;
   const uint32_t planes = planes_of(call.dtype), n = (uint32_t)m.tasks.size();
-  OrthoSpan spans[3] = {};
-  uint32_t units[3];
-  for (int kind = 0; kind < 3; ++kind) {
+  OrthoSpan spans[4] = {};
+  uint32_t units[4];
+  for (int kind = 0; kind < 4; ++kind) {
     auto before = [&](uint32_t k) {
       if (k == n) return m.n_units[kind];
       const OrthoTask& t = m.tasks[k];
-      return kind == 0 ? t.gram_units : kind == 1 ? t.whole_units : t.cell_units;
+      return kind == 0 ? t.gram_units : kind == 1 ? t.whole_units : kind == 2 ? t.cell_units : t.small_units;
     };
     OrthoSpan& s = spans[kind];
     s.tasks = m.d_tasks[planes - 1];
@@ -246,8 +249,14 @@ int run_group(dadam_handle* h, const Call& call, const Powers& pw, uint32_t k0, 
     s.n_xcd = h->n_xcds;
     units[kind] = before(k1) - s.first_unit;
   }
-  const OrthoSpan &gram = spans[0], &whole = spans[1];
-  const uint32_t gram_units = units[0], whole_units = units[1], edge = m.tasks[k0].edge;
+  const uint32_t edge = m.tasks[k0].edge, whole_units = units[1];
+  const OrthoSpan& whole = spans[1];
+  // A and B by small tiles where the chip is through with them sooner: it holds 256 large or 512 small ones at a time, and two small ones beside each other take 0.58
+  // of a large one's time (0.55 with two planes).
+  const double large = std::ceil(units[0] * (double)replicas / 256), small = std::ceil(units[3] * (double)replicas / 512) * (planes == 1 ? 0.58 : 0.55);
+  const bool by_large = edge == kLargeEdge && large <= small;
+  const uint32_t gram_edge = by_large ? kLargeEdge : kSmallEdge, gram_units = units[by_large ? 0 : 3];
+  const OrthoSpan& gram = spans[by_large ? 0 : 3];
   OrthoBeginArgs<kMaxRows> begin;
   memset((void*)&begin, 0, sizeof(begin));
   begin.s = spans[2];
@@ -272,10 +281,10 @@ int run_group(dadam_handle* h, const Call& call, const Powers& pw, uint32_t k0, 
     s.from = (uint32_t)(k & 1);
     s.to = s.from ^ 1;
     s.fresh = std::ldexp(1.f, pa - 2 * x);
-    e = launch_ortho_gram(false, edge, s, planes, gram_units, replicas, stream);
+    e = launch_ortho_gram(false, gram_edge, s, planes, gram_units, replicas, stream);
     s.gain = std::ldexp(b, pb - pa);
     s.fresh = std::ldexp(c, pb - 2 * pa);
-    if (!e) e = launch_ortho_gram(true, edge, s, planes, gram_units, replicas, stream);
+    if (!e) e = launch_ortho_gram(true, gram_edge, s, planes, gram_units, replicas, stream);
     if (e) break;
     s.s = whole;
     if (k + 1 < steps) {

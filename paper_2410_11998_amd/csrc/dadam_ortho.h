@@ -18,7 +18,8 @@ struct OrthoTask {
   uint32_t ld;           // elements from row to row
   uint32_t p, q, P, Q;   // P, Q: filled up to a multiple of the products' tiles
   uint32_t tall;
-  uint32_t gram_units, whole_units, cell_units;  // tiles of the matrices before it: of the lower half of P x P, of P x Q, and cells of P x Q
+  uint32_t gram_units, whole_units, cell_units, small_units;  // tiles of the matrices before it: of the lower half of P x P, of P x Q, cells of P x Q, and
+                                                              // small tiles of the lower half
   float scale, decay;
   uint32_t edge;         // of the products' tiles
 };

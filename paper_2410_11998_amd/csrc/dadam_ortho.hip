@@ -32,7 +32,7 @@ struct Unit {
   uint32_t tile;
   uint64_t base;
 };
-enum Kind : int { kGram = 0, kWhole = 1, kCells = 2 };
+enum Kind : int { kGram = 0, kWhole = 1, kCells = 2, kSmallGram = 3 };
 template <Kind KIND>
 __device__ __forceinline__ Unit find_unit(const OrthoSpan& s) {
   const uint32_t u = s.first_unit + die_run(blockIdx.x, gridDim.x, s.n_xcd);
@@ -44,7 +44,7 @@ __device__ __forceinline__ Unit find_unit(const OrthoSpan& s) {
 #pragma unroll
   for (uint32_t i = 0; i < sizeof(OrthoTask) / 4; ++i) words.w[i] = global<const uint32_t>(s.tasks + k)[i];
   r.t = __builtin_bit_cast(OrthoTask, words);
-  r.tile = u - (KIND == kGram ? r.t.gram_units : KIND == kWhole ? r.t.whole_units : r.t.cell_units);
+  r.tile = u - (KIND == kGram ? r.t.gram_units : KIND == kWhole ? r.t.whole_units : KIND == kCells ? r.t.cell_units : r.t.small_units);
   r.base = s.workspace + (uint64_t)blockIdx.y * s.stride + (r.t.at - s.before);
   return r;
 }
@@ -163,7 +163,7 @@ __device__ __forceinline__ void to_words(const float (&v)[8], uint32_t (&w)[8]) 
 template <int PLANES, int EDGE, bool SQUARE>
 __global__ __launch_bounds__(2 * EDGE) void k_ortho_gram(OrthoStepArgs a) {
   using T = GramTile<PLANES, EDGE>;
-  const Unit u = find_unit<kGram>(a.s);
+  const Unit u = find_unit < EDGE == (int)kLargeEdge ? kGram : kSmallGram > (a.s);
   const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES);
   uint32_t i = (uint32_t)((sqrtf(8.f * (float)u.tile + 1.f) - 1.f) * 0.5f);  // (the root may round across the border of a row of tiles)
   while (i * (i + 1) / 2 > u.tile) --i;
@@ -238,6 +238,8 @@ __global__ __launch_bounds__(2 * EDGE) void k_ortho_next(OrthoStepArgs a) {
              [](uint32_t, uint32_t, const float (&)[8]) {});
 }
 
+constexpr int kEarly = 3;  // sources whose elements are on their way together
+
 // The last iteration, straight into the result: the matrix, or the parameters mixed and moved along it.
 template <typename DT, int PLANES, int EDGE, int N>
 __global__ __launch_bounds__(2 * EDGE) void k_ortho_end(OrthoEndArgs<N> a) {
@@ -251,11 +253,18 @@ __global__ __launch_bounds__(2 * EDGE) void k_ortho_end(OrthoEndArgs<N> a) {
   const uint32_t replica = blockIdx.y, rows = u.t.tall ? u.t.q : u.t.p, cols = u.t.tall ? u.t.p : u.t.q;
   const uint64_t out = (uint64_t)a.out[replica];
   int32_t first = 0, last = 0;
-  uint64_t own = 0;
+  uint64_t own = 0, early[kEarly] = {};  // the first sources, and their weights
+  float weights[kEarly] = {};
   if (a.mix) {
     first = global<const int32_t>(a.row_ptr)[a.first_row + replica];
     last = global<const int32_t>(a.row_ptr)[a.first_row + replica + 1];
     own = (uint64_t)a.x_src[a.first_row + replica];
+#pragma unroll
+    for (int32_t k = 0; k < kEarly; ++k) {
+      if (first + k >= last) continue;
+      early[k] = (uint64_t)a.x_src[global<const int32_t>(a.col)[first + k]];
+      weights[k] = global<const float>(a.w)[first + k];
+    }
   }
   // elements (r, c) ... of the matrix as it lies
   auto finish = [&](uint32_t r, uint32_t c, const float (&v)[8]) {
@@ -267,7 +276,21 @@ __global__ __launch_bounds__(2 * EDGE) void k_ortho_end(OrthoEndArgs<N> a) {
       return;
     }
     float mixed[8], x[8];
-    for (int32_t k = first; k < last; ++k) {
+    int32_t k = first;
+    if (DT::is_whole(out, e, n)) {  // (all buffers begin at a multiple of 16 bytes)
+      typename DT::Piece early_pieces[kEarly];
+#pragma unroll
+      for (int32_t q = 0; q < kEarly; ++q)
+        if (first + q < last) early_pieces[q] = DT::piece(early[q], e);
+#pragma unroll
+      for (int32_t q = 0; q < kEarly; ++q)
+        if (first + q < last) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) mixed[i] = q == 0 ? weights[q] * early_pieces[q][i] : fmaf(weights[q], early_pieces[q][i], mixed[i]);
+        }
+      k = first + kEarly;
+    }
+    for (; k < last; ++k) {
       const float weight = global<const float>(a.w)[k];
       DT::load8((uint64_t)a.x_src[global<const int32_t>(a.col)[k]], e, n, x);
 #pragma unroll
