@@ -202,9 +202,9 @@ __device__ __forceinline__ constexpr float kept_times() {
 
 // The logits of a tile of words (m) and tokens (n).  Without gradients: the largest and the sum of exponentials of each wavefront's words, and the
 // target's logit.  With: softmax - e[target].
-template <typename XT, typename TY, int EDGE, int MODE>
+template <typename XT, typename TY, int EDGE, int BUFFERS, int MODE>
 __global__ __launch_bounds__(2 * EDGE) void k_head_logits(HeadArgs a) {
-  using T = TileOf<typename TY::op, TY::planes, EDGE, false, false>;
+  using T = TileOf<typename TY::op, TY::planes, EDGE, BUFFERS, false, false>;
   using OP = typename TY::op;
   const HeadRow& row = a.row[blockIdx.z];
   const uint64_t base = base_of(a);
@@ -388,9 +388,9 @@ __global__ __launch_bounds__(256) void k_head_sum(HeadArgs a) {
 }
 
 // dW of a tile of columns (m) and words (n): both operands lie by tokens.
-template <typename GT, typename TY, int EDGE>
+template <typename GT, typename TY, int EDGE, int BUFFERS>
 __global__ __launch_bounds__(2 * EDGE) void k_head_dhead(HeadArgs a) {
-  using T = TileOf<typename TY::op, TY::planes, EDGE, true, true>;
+  using T = TileOf<typename TY::op, TY::planes, EDGE, BUFFERS, true, true>;
   const HeadRow& row = a.row[blockIdx.z];
   const uint64_t base = base_of(a);
   const uint32_t across = a.s.D / T::kM;
@@ -447,9 +447,9 @@ __global__ __launch_bounds__(256) void k_head_dbias(HeadArgs a) {
 }
 
 // dh of a tile of columns (m) and tokens (n), over a part of the piece's words: the head lies by words.
-template <typename TY, int EDGE>
+template <typename TY, int EDGE, int BUFFERS>
 __global__ __launch_bounds__(2 * EDGE) void k_head_dhidden(HeadArgs a) {
-  using T = TileOf<typename TY::op, TY::planes, EDGE, true, false>;
+  using T = TileOf<typename TY::op, TY::planes, EDGE, BUFFERS, true, false>;
   const HeadRow& row = a.row[blockIdx.z];
   const uint64_t base = base_of(a);
   const uint32_t across = a.s.D / T::kM, down = a.s.T / T::kN, u = die_run(blockIdx.x, gridDim.x, a.n_xcd), split = u / (across * down);
@@ -515,11 +515,14 @@ int with_types(int xdt, int gdt, Fn fn) {
 
 uint32_t upto(uint64_t n, uint32_t each) { return (uint32_t)((n + each - 1) / each); }
 
-// fn(types of parameters, gradients and operands, edge of the tiles as a type).
+// fn(types of parameters, gradients and operands, edge and buffers of the tiles as types), for a launch of so many tiles.
 template <typename Fn>
-int with_tiles(int xdt, int gdt, uint32_t edge, Fn fn) {
+int with_tiles(int xdt, int gdt, uint32_t edge, uint32_t tiles, Fn fn) {
+  using Large = std::integral_constant<int, 256>;
+  using Small = std::integral_constant<int, 128>;
   return with_types(xdt, gdt, [&](auto x, auto g, auto ty) {
-    return edge == 256 ? fn(x, g, ty, std::integral_constant<int, 256>{}) : fn(x, g, ty, std::integral_constant<int, 128>{});
+    if (edge == 256) return fn(x, g, ty, Large{}, std::integral_constant<int, 2>{});
+    return tiles <= kOneEach ? fn(x, g, ty, Small{}, std::integral_constant<int, 4>{}) : fn(x, g, ty, Small{}, std::integral_constant<int, 2>{});
   });
 }
 
@@ -544,15 +547,15 @@ int launch_head_words(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* 
   });
 }
 int launch_head_logits(int xdt, int gdt, HeadMode mode, const HeadArgs& a, uint32_t rows, void* stream) {
-  return with_tiles(xdt, gdt, a.s.edge, [&](auto x, auto, auto ty, auto edge) {
+  const dim3 grid(upto(a.words, a.s.edge) * (a.s.T / a.s.edge), 1, rows);
+  return with_tiles(xdt, gdt, a.s.edge, grid.x * rows, [&](auto x, auto, auto ty, auto edge, auto buffers) {
     using X = decltype(x);
     using TY = decltype(ty);
-    constexpr int kEdge = decltype(edge)::value;
-    using T = TileOf<typename TY::op, TY::planes, kEdge, false, false>;
-    const dim3 grid(upto(a.words, a.s.edge) * (a.s.T / a.s.edge), 1, rows);
-    if (mode == kHeadStatistics) return launch<k_head_logits<X, TY, kEdge, kHeadStatistics>>(grid, T::kThreads, T::kLds, stream, a);
-    if (mode == kHeadKeep) return launch<k_head_logits<X, TY, kEdge, kHeadKeep>>(grid, T::kThreads, T::kLds, stream, a);
-    return launch<k_head_logits<X, TY, kEdge, kHeadGradient>>(grid, T::kThreads, T::kLds, stream, a);
+    constexpr int kEdge = decltype(edge)::value, kBuffers = decltype(buffers)::value;
+    using T = TileOf<typename TY::op, TY::planes, kEdge, kBuffers, false, false>;
+    if (mode == kHeadStatistics) return launch<k_head_logits<X, TY, kEdge, kBuffers, kHeadStatistics>>(grid, T::kThreads, T::kLds, stream, a);
+    if (mode == kHeadKeep) return launch<k_head_logits<X, TY, kEdge, kBuffers, kHeadKeep>>(grid, T::kThreads, T::kLds, stream, a);
+    return launch<k_head_logits<X, TY, kEdge, kBuffers, kHeadGradient>>(grid, T::kThreads, T::kLds, stream, a);
   });
 }
 int launch_head_scale(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
@@ -563,18 +566,22 @@ int launch_head_losses(const HeadArgs& a, uint32_t rows, void* stream) {
   return launch<k_head_sum>(dim3(1, 1, rows), 256, 0, stream, a);
 }
 int launch_head_dhead(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
-  return with_tiles(xdt, gdt, a.s.edge, [&](auto, auto g, auto ty, auto edge) {
-    using T = TileOf<typename decltype(ty)::op, decltype(ty)::planes, decltype(edge)::value, true, true>;
-    return launch<k_head_dhead<decltype(g), decltype(ty), decltype(edge)::value>>(dim3(upto(a.words, a.s.edge) * (a.s.D / a.s.edge), 1, rows), T::kThreads, T::kLds, stream, a);
+  const dim3 grid(upto(a.words, a.s.edge) * (a.s.D / a.s.edge), 1, rows);
+  return with_tiles(xdt, gdt, a.s.edge, grid.x * rows, [&](auto, auto g, auto ty, auto edge, auto buffers) {
+    using TY = decltype(ty);
+    using T = TileOf<typename TY::op, TY::planes, decltype(edge)::value, decltype(buffers)::value, true, true>;
+    return launch<k_head_dhead<decltype(g), TY, decltype(edge)::value, decltype(buffers)::value>>(grid, T::kThreads, T::kLds, stream, a);
   });
 }
 int launch_head_dbias(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
   return with_types(xdt, gdt, [&](auto, auto g, auto ty) { return launch<k_head_dbias<decltype(g), decltype(ty)>>(dim3(upto(a.words, 64), 1, rows), 256, 0, stream, a); });
 }
 int launch_head_dhidden(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
-  return with_tiles(xdt, gdt, a.s.edge, [&](auto, auto, auto ty, auto edge) {
-    using T = TileOf<typename decltype(ty)::op, decltype(ty)::planes, decltype(edge)::value, true, false>;
-    return launch<k_head_dhidden<decltype(ty), decltype(edge)::value>>(dim3((a.s.T / a.s.edge) * (a.s.D / a.s.edge) * a.s.splits, 1, rows), T::kThreads, T::kLds, stream, a);
+  const dim3 grid((a.s.T / a.s.edge) * (a.s.D / a.s.edge) * a.s.splits, 1, rows);
+  return with_tiles(xdt, gdt, a.s.edge, grid.x * rows, [&](auto, auto, auto ty, auto edge, auto buffers) {
+    using TY = decltype(ty);
+    using T = TileOf<typename TY::op, TY::planes, decltype(edge)::value, decltype(buffers)::value, true, false>;
+    return launch<k_head_dhidden<TY, decltype(edge)::value, decltype(buffers)::value>>(grid, T::kThreads, T::kLds, stream, a);
   });
 }
 int launch_head_end(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {

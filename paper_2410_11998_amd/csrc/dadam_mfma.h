@@ -205,11 +205,16 @@ __device__ __forceinline__ void load_to_lds(uint4v buffer, uint32_t offset, uint
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(buffer) : "memory");
 }
 
-// What this wavefront has asked for is in LDS, and so is what the others have; and nobody reads what was there before.  Nothing else is under way either: scalar
-// loads that are, and are not needed before the products' end, make the compiler wait for all fragments where it needs the older ones only.
+// What this wavefront has asked for is in LDS, but for its LEFT last loads, and so is what the others have; and nobody reads what was there before.  (Not
+// __syncthreads(), which waits for all loads that the compiler knows of.)  Nothing else is under way either: scalar loads that are, and are not needed before the
+// products' end, make the compiler wait for all fragments where it needs the older ones only.
+template <int LEFT>
 __device__ __forceinline__ void everybody_has_loaded() {
-  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
-  __syncthreads();
+  static_assert(LEFT < 64, "six bits");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070 | (LEFT & 15) | (LEFT >> 4) << 14);  // vmcnt(LEFT) lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
 
 // Fragments of blocks that lie by columns: elements of two times four rows, AT and NEXT bytes behind at[...].
@@ -227,14 +232,15 @@ __device__ __forceinline__ void read_turned(V (&out)[N], const uint32_t (&at)[N]
 // (j WN + wn) 32 ...  The large tile (256 x 256, eight wavefronts) is bound by LDS as much as by the matrix cores: a stage reads 192 KB and is written 64 KB, 2048
 // cycles, for 2048 cycles of products.  The small one (128 x 128, four) takes 768 cycles of LDS for 512 of products, and is for what has too few large tiles.
 // TFLOP/s, large / small / library, 8192 x 8192 x 8192 1119 / 914 / 1319, x 1024 1061 / 805 / 1078, 1024 x 49152 x 4096 1087 / 915 / 1295.
-// A_DOWN, B_DOWN: that operand lies by columns.
-template <typename OP, int PLANES, int MT, int NT, int WM, int WN, bool A_DOWN, bool B_DOWN>
+// A_DOWN, B_DOWN: that operand lies by columns.  BUFFERS: stages in LDS, of which all but one are on their way.
+template <typename OP, int PLANES, int MT, int NT, int WM, int WN, bool A_DOWN, bool B_DOWN, int BUFFERS>
 struct Tile {
   static constexpr int kWaves = WM * WN, kThreads = kWaves * 64;
   static constexpr int kM = WM * MT * 32, kN = WN * NT * 32;
   static constexpr int kStage = (kM + kN) * kStageBytes;  // LDS of a stage
   static constexpr int kRows = WN * 32;                   // columns of C that are finished at a time
-  static constexpr int kLds = 2 * kStage > kRows * kM * 4 ? 2 * kStage : kRows * kM * 4;
+  static constexpr int kLds = BUFFERS * kStage;
+  static_assert(kLds >= kRows * kM * 4, "columns that are finished find room");
   static constexpr int kSteps = PLANES == 1 ? 4 : 2;      // of 16 summed elements, in a stage
   using vec = typename OP::vec;
 
@@ -349,20 +355,32 @@ struct Tile {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WM, wn = wave / WM;
     const Operand ua = uniform(a), ub = uniform(b);
+    auto stage_at = [&](uint32_t s) { return lds + s % BUFFERS * kStage; };
     auto bring = [&](uint32_t s) {
-      char DADAM_LDS* to = lds + (s & 1) * kStage;
+      char DADAM_LDS* to = stage_at(s);
       fetch<kM, A_DOWN>(ua.at + (A_DOWN ? (uint64_t)s * kSummed * ua.pitch : (uint64_t)s * kStageBytes), ua.pitch, A_DOWN ? ua.rows - s * kSummed : ua.rows, to, wave, lane);
       fetch<kN, B_DOWN>(ub.at + (B_DOWN ? (uint64_t)s * kSummed * ub.pitch : (uint64_t)s * kStageBytes), ub.pitch, B_DOWN ? ub.rows - s * kSummed : ub.rows,
                         to + kM * kStageBytes, wave, lane);
     };
+    // Stage s is there: only the loads of the stages behind it, as many as have been asked for, may be left.
+    constexpr int kLoads = (kM + kN) / 8 / kWaves;
+    auto loaded = [&](uint32_t s) {
+      const uint32_t behind = stages - 1 - s < (uint32_t)(BUFFERS - 2) ? stages - 1 - s : (uint32_t)(BUFFERS - 2);
+      if (BUFFERS > 3 && behind == 2) return everybody_has_loaded<2 * kLoads>();
+      if (BUFFERS > 2 && behind == 1) return everybody_has_loaded<kLoads>();
+      return everybody_has_loaded<0>();
+    };
+    static_assert(BUFFERS == 2 || BUFFERS == 4, "loaded() counts for these");
     clear();
-    bring(0);
+#pragma unroll
+    for (uint32_t s = 0; s + 1 < (uint32_t)BUFFERS; ++s)
+      if (s < stages) bring(s);
     Fragments f[2];
-    everybody_has_loaded();
+    loaded(0);
     read<0>(f[0], lds, wm, wn, lane);
     for (uint32_t s = 0; s < stages; ++s) {
-      const char DADAM_LDS* stage = lds + (s & 1) * kStage;
-      if (s + 1 < stages) bring(s + 1);
+      const char DADAM_LDS* stage = stage_at(s);
+      if (s + BUFFERS - 1 < stages) bring(s + BUFFERS - 1);
       auto step = [&](int k) {
         __builtin_amdgcn_sched_barrier(0);
         multiply(f[k & 1]);
@@ -376,8 +394,10 @@ struct Tile {
         read<3>(f[1], stage, wm, wn, lane);
         step(2);
       }
-      everybody_has_loaded();  // and read this stage
-      if (s + 1 < stages) read<0>(f[0], lds + ((s + 1) & 1) * kStage, wm, wn, lane);
+      if (s + 1 < stages) {
+        loaded(s + 1);  // and everybody has read this stage
+        read<0>(f[0], stage_at(s + 1), wm, wn, lane);
+      }
       step(1);
     }
   }
@@ -448,8 +468,11 @@ struct Tile {
 struct Nothing {};
 __device__ __forceinline__ Nothing nothing_ahead(uint32_t, uint32_t) { return {}; }
 
-template <typename OP, int PLANES, int EDGE, bool A_DOWN, bool B_DOWN>
-using TileOf = typename std::conditional<EDGE == 256, Tile<OP, PLANES, 4, 2, 2, 4, A_DOWN, B_DOWN>, Tile<OP, PLANES, 2, 2, 2, 2, A_DOWN, B_DOWN>>::type;
+// Small tiles of a launch that gives every compute unit one at most keep four stages: a stage then has three times as long to come, and it is the length of a tile that
+// counts.  (Two tiles of two stages each fit a compute unit otherwise.)
+template <typename OP, int PLANES, int EDGE, int BUFFERS, bool A_DOWN, bool B_DOWN>
+using TileOf = typename std::conditional<EDGE == 256, Tile<OP, PLANES, 4, 2, 2, 4, A_DOWN, B_DOWN, BUFFERS>, Tile<OP, PLANES, 2, 2, 2, 2, A_DOWN, B_DOWN, BUFFERS>>::type;
+constexpr uint32_t kOneEach = 256;  // compute units
 
 // Workgroup b of n as its die takes it: consecutive workgroup ids go to the dies in turn, each die takes a contiguous run of tiles, whose operands
 // its L2 then holds.

@@ -251,9 +251,9 @@ int run_group(dadam_handle* h, const Call& call, const Powers& pw, uint32_t k0, 
   }
   const uint32_t edge = m.tasks[k0].edge, whole_units = units[1];
   const OrthoSpan& whole = spans[1];
-  // A and B by small tiles where the chip is through with them sooner: it holds 256 large or 512 small ones at a time, and two small ones beside each other take 0.58
+  // A and B by small tiles where the chip is through with them sooner: it holds 256 large or 512 small ones at a time, and two small ones beside each other take 0.66
   // of a large one's time (0.55 with two planes).
-  const double large = std::ceil(units[0] * (double)replicas / 256), small = std::ceil(units[3] * (double)replicas / 512) * (planes == 1 ? 0.58 : 0.55);
+  const double large = std::ceil(units[0] * (double)replicas / 256), small = std::ceil(units[3] * (double)replicas / 512) * (planes == 1 ? 0.66 : 0.55);
   const bool by_large = edge == kLargeEdge && large <= small;
   const uint32_t gram_edge = by_large ? kLargeEdge : kSmallEdge, gram_units = units[by_large ? 0 : 3];
   const OrthoSpan& gram = spans[by_large ? 0 : 3];

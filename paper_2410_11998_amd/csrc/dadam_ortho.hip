@@ -19,10 +19,10 @@ namespace {
 extern __shared__ char ortho_lds[];
 
 // Of A and B, whose operands both lie by rows, and of a X + B X (transposed: q by p), whose X lies by columns.
-template <int PLANES, int EDGE>
-using GramTile = TileOf<Half, PLANES, EDGE, false, false>;
-template <int PLANES, int EDGE>
-using NextTile = TileOf<Half, PLANES, EDGE, true, false>;
+template <int PLANES, int EDGE, int BUFFERS>
+using GramTile = TileOf<Half, PLANES, EDGE, BUFFERS, false, false>;
+template <int PLANES, int EDGE, int BUFFERS>
+using NextTile = TileOf<Half, PLANES, EDGE, BUFFERS, true, false>;
 
 __device__ __forceinline__ uint64_t x_at(const OrthoPlaces& w, uint32_t which) { return which ? w.x[1] : w.x[0]; }
 
@@ -160,9 +160,9 @@ __device__ __forceinline__ void to_words(const float (&v)[8], uint32_t (&w)[8]) 
 }
 
 // A tile (i, j), j <= i, of A = X X^T or of B = b A + c A A, and its mirror image.
-template <int PLANES, int EDGE, bool SQUARE>
+template <int PLANES, int EDGE, int BUFFERS, bool SQUARE>
 __global__ __launch_bounds__(2 * EDGE) void k_ortho_gram(OrthoStepArgs a) {
-  using T = GramTile<PLANES, EDGE>;
+  using T = GramTile<PLANES, EDGE, BUFFERS>;
   const Unit u = find_unit < EDGE == (int)kLargeEdge ? kGram : kSmallGram > (a.s);
   const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES);
   uint32_t i = (uint32_t)((sqrtf(8.f * (float)u.tile + 1.f) - 1.f) * 0.5f);  // (the root may round across the border of a row of tiles)
@@ -218,9 +218,9 @@ __device__ __forceinline__ void next_product(T& t, const Unit& u, const OrthoPla
 }
 
 // X of the next iteration.
-template <int PLANES, int EDGE>
+template <int PLANES, int EDGE, int BUFFERS>
 __global__ __launch_bounds__(2 * EDGE) void k_ortho_next(OrthoStepArgs a) {
-  using T = NextTile<PLANES, EDGE>;
+  using T = NextTile<PLANES, EDGE, BUFFERS>;
   const Unit u = find_unit<kWhole>(a.s);
   const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES);
   char DADAM_LDS* lds = (char DADAM_LDS*)ortho_lds;
@@ -241,9 +241,9 @@ __global__ __launch_bounds__(2 * EDGE) void k_ortho_next(OrthoStepArgs a) {
 constexpr int kEarly = 3;  // sources whose elements are on their way together
 
 // The last iteration, straight into the result: the matrix, or the parameters mixed and moved along it.
-template <typename DT, int PLANES, int EDGE, int N>
+template <typename DT, int PLANES, int EDGE, int BUFFERS, int N>
 __global__ __launch_bounds__(2 * EDGE) void k_ortho_end(OrthoEndArgs<N> a) {
-  using T = NextTile<PLANES, EDGE>;
+  using T = NextTile<PLANES, EDGE, BUFFERS>;
   const Unit u = find_unit<kWhole>(a.s);
   const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES);
   char DADAM_LDS* lds = (char DADAM_LDS*)ortho_lds;
@@ -352,22 +352,41 @@ int begin_any(bool norm, int gdt, const OrthoBeginArgs<kMaxRows>& a, uint32_t pl
   return planes == 1 ? begin<B16, 1>(norm, a, units, replicas, stream) : begin<B16, 2>(norm, a, units, replicas, stream);
 }
 
-template <int PLANES, int EDGE>
-int gram(bool square, const OrthoStepArgs& a, uint32_t units, uint32_t replicas, void* stream) {
-  using T = GramTile<PLANES, EDGE>;
-  return square ? launch<k_ortho_gram<PLANES, EDGE, true>>(a, T::kThreads, units, replicas, T::kLds, stream) : launch<k_ortho_gram<PLANES, EDGE, false>>(a, T::kThreads, units, replicas, T::kLds, stream);
+// fn(edge, buffers) as types, for a launch of small or large tiles.
+template <typename Fn>
+int with_tiles(uint32_t edge, uint32_t tiles, Fn fn) {
+  using Large = std::integral_constant<int, 256>;
+  using Small = std::integral_constant<int, 128>;
+  if (edge == kLargeEdge) return fn(Large{}, std::integral_constant<int, 2>{});
+  return tiles <= kOneEach ? fn(Small{}, std::integral_constant<int, 4>{}) : fn(Small{}, std::integral_constant<int, 2>{});
 }
-template <int PLANES, int EDGE>
-int next(const OrthoStepArgs& a, uint32_t units, uint32_t replicas, void* stream) {
-  using T = NextTile<PLANES, EDGE>;
-  return launch<k_ortho_next<PLANES, EDGE>>(a, T::kThreads, units, replicas, T::kLds, stream);
+
+template <int PLANES>
+int gram(bool square, uint32_t edge, const OrthoStepArgs& a, uint32_t units, uint32_t replicas, void* stream) {
+  return with_tiles(edge, units * replicas, [&](auto e, auto b) {
+    constexpr int kEdge = decltype(e)::value, kBuffers = decltype(b)::value;
+    using T = GramTile<PLANES, kEdge, kBuffers>;
+    return square ? launch<k_ortho_gram<PLANES, kEdge, kBuffers, true>>(a, T::kThreads, units, replicas, T::kLds, stream)
+                  : launch<k_ortho_gram<PLANES, kEdge, kBuffers, false>>(a, T::kThreads, units, replicas, T::kLds, stream);
+  });
 }
-template <typename DT, int PLANES, int EDGE>
-int end(const OrthoEndArgs<kMaxRows>& a, uint32_t n_cols, uint32_t units, uint32_t replicas, void* stream) {
-  using T = NextTile<PLANES, EDGE>;
-  if (replicas <= (uint32_t)kOrthoFew && n_cols <= (uint32_t)kOrthoFew)
-    return launch<k_ortho_end<DT, PLANES, EDGE, kOrthoFew>>(shorter<kOrthoFew>(a), T::kThreads, units, replicas, T::kLds, stream);
-  return launch<k_ortho_end<DT, PLANES, EDGE, kMaxRows>>(a, T::kThreads, units, replicas, T::kLds, stream);
+template <int PLANES>
+int next(uint32_t edge, const OrthoStepArgs& a, uint32_t units, uint32_t replicas, void* stream) {
+  return with_tiles(edge, units * replicas, [&](auto e, auto b) {
+    constexpr int kEdge = decltype(e)::value, kBuffers = decltype(b)::value;
+    using T = NextTile<PLANES, kEdge, kBuffers>;
+    return launch<k_ortho_next<PLANES, kEdge, kBuffers>>(a, T::kThreads, units, replicas, T::kLds, stream);
+  });
+}
+template <typename DT, int PLANES>
+int end(uint32_t edge, const OrthoEndArgs<kMaxRows>& a, uint32_t n_cols, uint32_t units, uint32_t replicas, void* stream) {
+  return with_tiles(edge, units * replicas, [&](auto e, auto b) {
+    constexpr int kEdge = decltype(e)::value, kBuffers = decltype(b)::value;
+    using T = NextTile<PLANES, kEdge, kBuffers>;
+    if (replicas <= (uint32_t)kOrthoFew && n_cols <= (uint32_t)kOrthoFew)
+      return launch<k_ortho_end<DT, PLANES, kEdge, kBuffers, kOrthoFew>>(shorter<kOrthoFew>(a), T::kThreads, units, replicas, T::kLds, stream);
+    return launch<k_ortho_end<DT, PLANES, kEdge, kBuffers, kMaxRows>>(a, T::kThreads, units, replicas, T::kLds, stream);
+  });
 }
 
 }  // namespace
@@ -379,17 +398,13 @@ int launch_ortho_begin(int gdt, const OrthoBeginArgs<kMaxRows>& a, uint32_t plan
   return begin_any(false, gdt, a, planes, units, replicas, stream);
 }
 int launch_ortho_gram(bool square, uint32_t edge, const OrthoStepArgs& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream) {
-  if (edge == kLargeEdge) return planes == 1 ? gram<1, 256>(square, a, units, replicas, stream) : gram<2, 256>(square, a, units, replicas, stream);
-  return planes == 1 ? gram<1, 128>(square, a, units, replicas, stream) : gram<2, 128>(square, a, units, replicas, stream);
+  return planes == 1 ? gram<1>(square, edge, a, units, replicas, stream) : gram<2>(square, edge, a, units, replicas, stream);
 }
 int launch_ortho_next(uint32_t edge, const OrthoStepArgs& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream) {
-  if (edge == kLargeEdge) return planes == 1 ? next<1, 256>(a, units, replicas, stream) : next<2, 256>(a, units, replicas, stream);
-  return planes == 1 ? next<1, 128>(a, units, replicas, stream) : next<2, 128>(a, units, replicas, stream);
+  return planes == 1 ? next<1>(edge, a, units, replicas, stream) : next<2>(edge, a, units, replicas, stream);
 }
 int launch_ortho_end(int dtype, uint32_t edge, const OrthoEndArgs<kMaxRows>& a, uint32_t n_cols, uint32_t units, uint32_t replicas, void* stream) {
-  if (edge == kLargeEdge)
-    return dtype == (int)DADAM_F32 ? end<F32, 2, 256>(a, n_cols, units, replicas, stream) : end<B16, 1, 256>(a, n_cols, units, replicas, stream);
-  return dtype == (int)DADAM_F32 ? end<F32, 2, 128>(a, n_cols, units, replicas, stream) : end<B16, 1, 128>(a, n_cols, units, replicas, stream);
+  return dtype == (int)DADAM_F32 ? end<F32, 2>(edge, a, n_cols, units, replicas, stream) : end<B16, 1>(edge, a, n_cols, units, replicas, stream);
 }
 
 }  // namespace dadam
