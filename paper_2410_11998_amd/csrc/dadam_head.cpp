@@ -119,6 +119,22 @@ Way way_for(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, bo
   return w;
 }
 
+// dW of a piece.  What large tiles there are beyond a multiple of what the chip holds go by small ones, if that takes less than one more round of large ones: three rounds
+// and 72 small tiles instead of four (50257 words, width 1024).
+int run_dhead(int x, int g, HeadArgs a, uint32_t rows, void* stream) {
+  const uint32_t down = (a.words + a.s.edge - 1) / a.s.edge, tiles_of_word = a.s.D / a.s.edge * rows, tiles = down * tiles_of_word, over = tiles % at_once(a.s.edge);
+  const uint32_t all = a.words;
+  if (a.s.edge == 256 && tiles > at_once(256) && over && over <= at_once(256) / 4) {
+    const uint32_t first = (tiles - over) / tiles_of_word * 256;
+    a.words = first;
+    if (const int e = launch_head_dhead(x, g, 256, a, rows, stream)) return e;
+    a.skip = first;
+    a.words = all;
+    return launch_head_dhead(x, g, 128, a, rows, stream);
+  }
+  return launch_head_dhead(x, g, a.s.edge, a, rows, stream);
+}
+
 int run_rows(const dadam_handle* h, HeadArgs a, bool dhidden, bool dhead, bool dbias, uint32_t rows, void* stream) {
   const int x = (int)h->cfg.param_dtype, g = (int)h->cfg.grad_dtype;
   const bool gradient = dhidden || dhead;
@@ -142,7 +158,7 @@ int run_rows(const dadam_handle* h, HeadArgs a, bool dhidden, bool dhead, bool d
     piece(k);
     if (pieces > 1 && !a.straight) e = launch_head_words(x, g, a, rows, stream);
     if (!e && !a.s.keeps) e = launch_head_logits(x, g, kHeadGradient, a, rows, stream);
-    if (!e && dhead) e = launch_head_dhead(x, g, a, rows, stream);
+    if (!e && dhead) e = run_dhead(x, g, a, rows, stream);
     if (!e && dbias) e = launch_head_dbias(x, g, a, rows, stream);
     if (!e && dhidden) e = launch_head_dhidden(x, g, a, rows, stream);
   }

@@ -60,6 +60,7 @@ struct HeadArgs {
   float scale;
   uint32_t mean, add;
   uint32_t first_word, words;  // of the piece
+  uint32_t skip;        // words of the piece that another launch of launch_head_dhead takes: those before
   uint32_t later;       // a piece before this one has begun the sums
   uint32_t n_xcd;
   uint32_t straight;    // the head is an operand as it lies
@@ -76,7 +77,7 @@ enum HeadMode : int { kHeadStatistics = 0, kHeadKeep = 1, kHeadGradient = 2 };
 int launch_head_logits(int xdt, int gdt, HeadMode mode, const HeadArgs& a, uint32_t rows, void* stream);
 int launch_head_losses(const HeadArgs& a, uint32_t rows, void* stream);
 int launch_head_scale(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                   // the logits' gradient from what was kept
-int launch_head_dhead(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);
+int launch_head_dhead(int xdt, int gdt, uint32_t edge, const HeadArgs& a, uint32_t rows, void* stream);
 int launch_head_dbias(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);
 int launch_head_dhidden(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                 // a piece's part of the sums
 int launch_head_end(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                     // the hidden vectors' gradients from the sums

@@ -399,12 +399,12 @@ __global__ __launch_bounds__(2 * EDGE) void k_head_dhead(HeadArgs a) {
   const uint64_t b = 2 * TY::planes;
   char DADAM_LDS* lds = (char DADAM_LDS*)head_lds;
   T t;
-  t.product(operand(base + a.w.hidden + i * T::kM * b, a.s.D * b), operand(base + a.w.p + j * T::kN * b, a.s.piece * b), a.s.T * TY::planes / 64, lds);
+  t.product(operand(base + a.w.hidden + i * T::kM * b, a.s.D * b), operand(base + a.w.p + (a.skip + j * T::kN) * b, a.s.piece * b), a.s.T * TY::planes / 64, lds);
   const float factor = factor_of(base, a) * (TY::planes == 1 ? 1.f : ldexpf(1.f, -power_of<TY>(base, a, kHeadMostHidden) - kHeldAt));
   t.hand_out(lds, false, nothing_ahead,
              [&](uint32_t m, uint32_t n, float (&v)[8], Nothing) {
                m += i * T::kM;
-               n += j * T::kN;
+               n += a.skip + j * T::kN;
                const uint32_t columns = n < a.words ? left(a.s.width, m) : 0;
                if (columns == 0) return;
                const uint64_t e = (uint64_t)(a.first_word + n) * a.s.width + m;
@@ -565,12 +565,12 @@ int launch_head_losses(const HeadArgs& a, uint32_t rows, void* stream) {
   if (const int e = launch<k_head_losses>(dim3(a.s.T / 16, 1, rows), 256, 0, stream, a)) return e;
   return launch<k_head_sum>(dim3(1, 1, rows), 256, 0, stream, a);
 }
-int launch_head_dhead(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
-  const dim3 grid(upto(a.words, a.s.edge) * (a.s.D / a.s.edge), 1, rows);
-  return with_tiles(xdt, gdt, a.s.edge, grid.x * rows, [&](auto, auto g, auto ty, auto edge, auto buffers) {
+int launch_head_dhead(int xdt, int gdt, uint32_t edge, const HeadArgs& a, uint32_t rows, void* stream) {
+  const dim3 grid(upto(a.words - a.skip, edge) * (a.s.D / edge), 1, rows);
+  return with_tiles(xdt, gdt, edge, grid.x * rows, [&](auto, auto g, auto ty, auto edge_, auto buffers) {
     using TY = decltype(ty);
-    using T = TileOf<typename TY::op, TY::planes, decltype(edge)::value, decltype(buffers)::value, true, true>;
-    return launch<k_head_dhead<decltype(g), TY, decltype(edge)::value, decltype(buffers)::value>>(grid, T::kThreads, T::kLds, stream, a);
+    using T = TileOf<typename TY::op, TY::planes, decltype(edge_)::value, decltype(buffers)::value, true, true>;
+    return launch<k_head_dhead<decltype(g), TY, decltype(edge_)::value, decltype(buffers)::value>>(grid, T::kThreads, T::kLds, stream, a);
   });
 }
 int launch_head_dbias(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {

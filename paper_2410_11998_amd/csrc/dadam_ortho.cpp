@@ -227,6 +227,40 @@ struct Call {
   uint64_t bytes;
 };
 
+// What a launch of so many tiles takes, in the time of a large one: the chip holds 256 large or 512 small ones at a time, and two small ones beside each other take 0.66
+// of a large one's time (0.55 with two planes).
+double time_of(uint32_t edge, double tiles, uint32_t planes) {
+  return edge == kLargeEdge ? std::ceil(tiles / 256) : std::ceil(tiles / 512) * (planes == 1 ? 0.66 : 0.55);
+}
+// A and B by large tiles, or by small ones where the chip is through with those sooner.
+bool gram_by_large(uint32_t edge, double large, double small, uint32_t planes) {
+  return edge == kLargeEdge && time_of(kLargeEdge, large, planes) <= time_of(kSmallEdge, small, planes);
+}
+
+// Matrices k0 .. that go together, of all replicas in `most` bytes: those whose launches leave the least of the chip idle.
+uint32_t end_of_group(const dadam_handle* h, uint32_t planes, uint32_t k0, uint64_t most) {
+  const std::vector<OrthoTask>& tasks = h->matrices->tasks;
+  const std::vector<uint64_t>& need = h->matrices->need[planes - 1];
+  const double R = h->cfg.n_rows, unit = tasks[k0].edge == kLargeEdge ? 256 : 512;
+  double gram = 0, small = 0, whole = 0, long_gram = 0, best = 0;
+  uint32_t chosen = k0;
+  uint64_t bytes = 0;
+  for (uint32_t k = k0; k < tasks.size() && tasks[k].edge == tasks[k0].edge && bytes + need[k] <= most / h->cfg.n_rows; ++k) {
+    const OrthoTask& t = tasks[k];
+    bytes += need[k];
+    gram += R * lower_half(t.P / t.edge);
+    small += R * lower_half(t.P / kSmallEdge);
+    whole += R * (double)(t.P / t.edge) * (t.Q / t.edge);
+    long_gram = std::max(long_gram, (double)t.Q / t.P);  // X X^T sums that much longer than the other products
+    // the share of the time in which the chip is full, A A and X X^T by the tiles that they go by; a launch begins and ends like half a round of tiles
+    const bool by_large = gram_by_large(t.edge, gram, small, planes);
+    const double tiles = by_large ? gram : small, slots = by_large ? 256 : 512, idle = (std::ceil(tiles / slots) + 0.5) * slots / tiles;
+    const double share = (2 * whole + (1 + long_gram) * gram) / (2 * (std::ceil(whole / unit) + 0.5) * unit + (1 + long_gram) * gram * idle);
+    if (share >= best || k + 1 == tasks.size() || tasks[k + 1].edge != t.edge) best = share, chosen = k + 1;  // (all that are left, if there is room for them)
+  }
+  return chosen;
+}
+
 // A matrices-by-replicas rectangle, whole.
 int run_group(dadam_handle* h, const Call& call, const Powers& pw, uint32_t k0, uint32_t k1, uint32_t i0, uint32_t replicas, void* stream) {
   const MatrixState& m = *h->matrices;
@@ -251,10 +285,7 @@ int run_group(dadam_handle* h, const Call& call, const Powers& pw, uint32_t k0, 
   }
   const uint32_t edge = m.tasks[k0].edge, whole_units = units[1];
   const OrthoSpan& whole = spans[1];
-  // A and B by small tiles where the chip is through with them sooner: it holds 256 large or 512 small ones at a time, and two small ones beside each other take 0.66
-  // of a large one's time (0.55 with two planes).
-  const double large = std::ceil(units[0] * (double)replicas / 256), small = std::ceil(units[3] * (double)replicas / 512) * (planes == 1 ? 0.66 : 0.55);
-  const bool by_large = edge == kLargeEdge && large <= small;
+  const bool by_large = gram_by_large(edge, units[0] * (double)replicas, units[3] * (double)replicas, planes);
   const uint32_t gram_edge = by_large ? kLargeEdge : kSmallEdge, gram_units = units[by_large ? 0 : 3];
   const OrthoSpan& gram = spans[by_large ? 0 : 3];
   OrthoBeginArgs<kMaxRows> begin;
@@ -331,15 +362,12 @@ int run(dadam_handle* h, const Call& call, void* stream) {
   Powers pw;
   (void)find_powers(h->matrices->coefficients, &pw);
   const std::vector<uint64_t>& need = h->matrices->need[planes_of(call.dtype) - 1];
-  const std::vector<OrthoTask>& tasks = h->matrices->tasks;
-  const uint32_t n = (uint32_t)tasks.size(), R = h->cfg.n_rows;
+  const uint32_t n = (uint32_t)h->matrices->tasks.size(), R = h->cfg.n_rows;
   DeviceGuard guard(h->cfg.device);
   if (guard.err != hipSuccess) return fail(h, DADAM_EHIP, "hipSetDevice: %s", hipGetErrorString(guard.err));
   int e = (int)hipSuccess;
   for (uint32_t k = 0; k < n && !e;) {
-    uint32_t end = k;
-    uint64_t bytes = 0;
-    while (end < n && tasks[end].edge == tasks[k].edge && (bytes + need[end]) * R <= call.bytes) bytes += need[end++];
+    uint32_t end = end_of_group(h, planes_of(call.dtype), k, call.bytes);
     if (end > k) {
       e = run_group(h, call, pw, k, end, 0, R, stream);
     } else {  // one matrix, as many replicas as there is room for
