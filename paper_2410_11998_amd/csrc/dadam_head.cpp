@@ -119,6 +119,39 @@ Way way_for(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, bo
   return w;
 }
 
+// Few tokens: a wavefront sums a hidden vector's gradient over four blocks of words, or more where there are more than kFewItems of those.
+constexpr uint64_t kFewItems = 4096;
+struct Few {
+  FewShape s;
+  uint32_t rows;
+  uint64_t each;
+};
+Few few_way(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, bool gradient) {
+  Few f{};
+  f.s.tokens = n_tokens;
+  f.s.vocab = head->vocab;
+  f.s.width = head->width;
+  f.s.T = filled(n_tokens, 32);
+  f.s.D = filled(head->width, kFewColumns);
+  f.s.blocks = (head->vocab + kFewWords - 1) / kFewWords;
+  f.s.each = (uint32_t)std::max<uint64_t>(4, ((uint64_t)f.s.blocks * (f.s.D / kFewColumns) + kFewItems - 1) / kFewItems);
+  f.s.ranges = (f.s.blocks + f.s.each - 1) / f.s.each;
+  f.each = few_places(f.s, planes_of(h), gradient).bytes;
+  f.rows = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(std::min<uint32_t>(h->cfg.n_rows, kHeadRows), kMostAtOnce / f.each));
+  return f;
+}
+bool are_few(uint32_t n_tokens) { return n_tokens >= 1 && n_tokens <= kFewTokens; }
+
+int run_few(const dadam_handle* h, const FewArgs& a, bool dhidden, bool gradient, uint32_t rows, void* stream) {
+  const int x = (int)h->cfg.param_dtype, g = (int)h->cfg.grad_dtype;
+  int e = launch_few_logits(x, g, a, rows, stream);
+  if (!e) e = launch_few_losses(a, rows, stream);
+  if (!e && gradient) e = launch_few_softmax(x, g, a, rows, stream);
+  if (!e && gradient) e = launch_few_gradients(x, g, a, rows, stream);
+  if (!e && dhidden) e = launch_few_end(x, g, a, rows, stream);
+  return e;
+}
+
 // dW of a piece.  What large tiles there are beyond a multiple of what the chip holds go by small ones, if that takes less than one more round of large ones: three rounds
 // and 72 small tiles instead of four (50257 words, width 1024).
 int run_dhead(int x, int g, HeadArgs a, uint32_t rows, void* stream) {
@@ -175,8 +208,13 @@ int dadam_head_get_info(const dadam_handle* h, const dadam_head* head, uint32_t 
   if (!h) return DADAM_EINVAL;
   if (!out) return fail(h, DADAM_EINVAL, "out is null");
   if (const int rc = check_head(h, head, n_tokens)) return rc;
-  const Way w = good_way(h, head, n_tokens, gradient != 0, may_keep(h, head, n_tokens, gradient != 0));
   out->least_bytes = least_way(h, head, n_tokens, gradient != 0).each;
+  if (are_few(n_tokens)) {
+    const Few f = few_way(h, head, n_tokens, gradient != 0);
+    out->bytes = std::max(out->least_bytes, f.each * f.rows);
+    return DADAM_OK;
+  }
+  const Way w = good_way(h, head, n_tokens, gradient != 0, may_keep(h, head, n_tokens, gradient != 0));
   out->bytes = std::max(out->least_bytes, w.each * w.rows);
   return DADAM_OK;
 }
@@ -216,29 +254,18 @@ int dadam_head_loss(dadam_handle* h, const dadam_head* head, const void* const* 
         if (lo < (uintptr_t)t.p[i] + t.bytes && (uintptr_t)t.p[i] < hi) rc = fail(h, DADAM_EALIAS, "losses overlaps %s[%u]", t.name, i);
     if (!rc) rc = check_device(h);
     if (rc) return rc;
-    const Way way = way_for(h, head, n_tokens, gradient, workspace_bytes);
     const uint64_t at = h->tensors[head->tensor].offset_elems;
     const bool biased = head->bias_tensor != DADAM_HEAD_NO_BIAS;
     const uint64_t bias_at = biased ? h->tensors[head->bias_tensor].offset_elems : 0;
-    DeviceGuard guard(h->cfg.device);
-    if (guard.err != hipSuccess) return fail(h, DADAM_EHIP, "hipSetDevice: %s", hipGetErrorString(guard.err));
-    int e = (int)hipSuccess;
-    for (uint32_t i = 0; i < R && !e; i += way.rows) {
-      const uint32_t rows = std::min(way.rows, R - i);
-      HeadArgs a;
-      memset((void*)&a, 0, sizeof(a));
-      a.s = way.s;
-      a.w = head_places(way.s, planes_of(h), gradient);
-      a.workspace = (uint64_t)(uintptr_t)workspace;
-      a.stride = way.each;
-      a.losses = losses + i;
-      a.scale = scale;
-      a.mean = (flags & DADAM_HEAD_MEAN) != 0;
-      a.add = (flags & DADAM_HEAD_ADD) != 0;
-      a.n_xcd = h->n_xcds;
-      a.straight = planes_of(h) == 1 && head->width == way.s.D && at * xs % 16 == 0;
+    auto fill = [&](auto* a, uint32_t i, uint32_t rows) {
+      memset((void*)a, 0, sizeof(*a));
+      a->workspace = (uint64_t)(uintptr_t)workspace;
+      a->losses = losses + i;
+      a->scale = scale;
+      a->mean = (flags & DADAM_HEAD_MEAN) != 0;
+      a->add = (flags & DADAM_HEAD_ADD) != 0;
       for (uint32_t r = 0; r < rows; ++r) {
-        HeadRow& row = a.row[r];
+        HeadRow& row = a->row[r];
         row.head = (uint64_t)(uintptr_t)params[i + r] + at * xs;
         row.bias = biased ? (uint64_t)(uintptr_t)params[i + r] + bias_at * xs : 0;
         row.hidden = (uint64_t)(uintptr_t)hidden[i + r];
@@ -248,7 +275,38 @@ int dadam_head_loss(dadam_handle* h, const dadam_head* head, const void* const* 
         row.dhead = grads ? (uint64_t)(uintptr_t)grads[i + r] + at * gs : 0;
         row.dbias = grads && biased ? (uint64_t)(uintptr_t)grads[i + r] + bias_at * gs : 0;
       }
-      e = run_rows(h, a, dhidden != nullptr, grads != nullptr, grads && biased, rows, hip_stream);
+    };
+    DeviceGuard guard(h->cfg.device);
+    if (guard.err != hipSuccess) return fail(h, DADAM_EHIP, "hipSetDevice: %s", hipGetErrorString(guard.err));
+    int e = (int)hipSuccess;
+    const Few few = are_few(n_tokens) ? few_way(h, head, n_tokens, gradient) : Few{};
+    if (are_few(n_tokens) && few.each <= workspace_bytes) {
+      const uint32_t together = (uint32_t)std::min<uint64_t>(few.rows, workspace_bytes / few.each);
+      for (uint32_t i = 0; i < R && !e; i += together) {
+        const uint32_t rows = std::min(together, R - i);
+        FewArgs a;
+        fill(&a, i, rows);
+        a.s = few.s;
+        a.w = few_places(few.s, planes_of(h), gradient);
+        a.stride = few.each;
+        uint64_t low = (uint64_t)head->width * xs;  // what the head, its rows and the hidden vectors begin at
+        for (uint32_t r = 0; r < rows; ++r) low |= a.row[r].head | a.row[r].hidden | a.row[r].dhidden;
+        a.wide = (low % 16 == 0 ? 1 : 0) | (head->width % 4 == 0 && at * gs % 16 == 0 ? 2 : 0);
+        e = run_few(h, a, dhidden != nullptr, gradient, rows, hip_stream);
+      }
+    } else {
+      const Way way = way_for(h, head, n_tokens, gradient, workspace_bytes);
+      for (uint32_t i = 0; i < R && !e; i += way.rows) {
+        const uint32_t rows = std::min(way.rows, R - i);
+        HeadArgs a;
+        fill(&a, i, rows);
+        a.s = way.s;
+        a.w = head_places(way.s, planes_of(h), gradient);
+        a.stride = way.each;
+        a.n_xcd = h->n_xcds;
+        a.straight = planes_of(h) == 1 && head->width == way.s.D && at * xs % 16 == 0;
+        e = run_rows(h, a, dhidden != nullptr, grads != nullptr, grads && biased, rows, hip_stream);
+      }
     }
     if (e != (int)hipSuccess) return fail(h, DADAM_EHIP, "kernel launch failed: %s", hipGetErrorString((hipError_t)e));
     return DADAM_OK;

@@ -68,6 +68,58 @@ struct HeadArgs {
 };
 static_assert(sizeof(HeadArgs) <= 4096, "the argument block of a launch holds 4 KB");
 
+// The way of few tokens (dadam_head_few.hip): the head is read as it lies, 32 words at a time.
+constexpr uint32_t kFewTokens = 64, kFewWords = 32, kFewColumns = 128;
+struct FewPlaces {
+  uint64_t words, lse, hit, stats, z, p, p_turned, hidden, sums, bytes;
+};
+struct FewShape {
+  uint32_t tokens, vocab, width;
+  uint32_t T, D;             // tokens filled up to 32, width to kFewColumns
+  uint32_t blocks;           // of kFewWords words
+  uint32_t each, ranges;     // blocks of a range that a wavefront sums a hidden vector's gradient over, and ranges
+};
+inline constexpr FewPlaces few_places(const FewShape& s, uint64_t planes, bool gradient) {
+  FewPlaces w{};
+  uint64_t at = 0;
+  auto take = [&at](uint64_t bytes) {
+    const uint64_t here = at;
+    at += (bytes + 255) / 256 * 256;
+    return here;
+  };
+  w.words = take(64);
+  w.lse = take((uint64_t)s.T * 4);
+  w.hit = take((uint64_t)s.T * 4);
+  w.stats = take((uint64_t)s.blocks * s.T * 8);
+  w.z = take((uint64_t)s.blocks * s.T * kFewWords * 4);  // of a block: T rows of kFewWords logits, with two planes softmax - e[target] in their place
+  if (gradient) {
+    if (planes == 1) {
+      w.p = take((uint64_t)s.blocks * s.T * kFewWords * 2);         // as bfloat16
+      w.p_turned = take((uint64_t)s.blocks * s.T * kFewWords * 2);  // and turned: kFewWords rows of T
+    }
+    w.hidden = take((uint64_t)s.T * s.D * 4);  // rows of D, with one plane D rows of T bfloat16s
+    w.sums = take((uint64_t)s.ranges * s.tokens * s.D * 4);
+  }
+  w.bytes = at;
+  return w;
+}
+struct FewArgs {
+  FewShape s;
+  FewPlaces w;
+  uint64_t workspace, stride;
+  float* losses;
+  float scale;
+  uint32_t mean, add;
+  uint32_t wide;  // four elements side by side lie together: bit 0 of the head and the hidden vectors, bit 1 of the head's gradient
+  HeadRow row[kHeadRows];
+};
+static_assert(sizeof(FewArgs) <= 4096, "the argument block of a launch holds 4 KB");
+int launch_few_logits(int xdt, int gdt, const FewArgs& a, uint32_t rows, void* stream);
+int launch_few_losses(const FewArgs& a, uint32_t rows, void* stream);
+int launch_few_softmax(int xdt, int gdt, const FewArgs& a, uint32_t rows, void* stream);    // and the bias's gradient
+int launch_few_gradients(int xdt, int gdt, const FewArgs& a, uint32_t rows, void* stream);
+int launch_few_end(int xdt, int gdt, const FewArgs& a, uint32_t rows, void* stream);
+
 // Launchers, of `rows` replicas.  xdt: type of parameters and hidden vectors, gdt of gradients; two planes unless both are bfloat16.
 int launch_head_begin(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                   // tokens with a target, powers of two
 int launch_head_hidden(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                  // operands of the hidden vectors

@@ -23,6 +23,7 @@ typedef float float16v __attribute__((ext_vector_type(16)));
 typedef float float2v __attribute__((ext_vector_type(2)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 typedef short short4v __attribute__((ext_vector_type(4)));
+typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 
 #define DADAM_GLOBAL __attribute__((address_space(1)))
@@ -55,6 +56,25 @@ struct Brain {
 // stored).
 struct F32 {
   using type = float;
+  static __device__ __forceinline__ void load4(uint64_t p, uint64_t e, uint32_t n, bool wide, float (&v)[4]) {
+    if (wide && n >= 4) {
+      const float4v a = global<const float4v>(p + e * 4)[0];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = a[k];
+      return;
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < 4; ++k) v[k] = k < n ? load(p, e + k) : 0.f;
+  }
+  static __device__ __forceinline__ void store4(uint64_t p, uint64_t e, uint32_t n, bool wide, const float (&v)[4]) {
+    if (wide && n >= 4) {
+      global<float4v>(p + e * 4)[0] = float4v{v[0], v[1], v[2], v[3]};
+      return;
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < 4; ++k)
+      if (k < n) store(p, e + k, v[k]);
+  }
   struct Piece {  // eight elements as they lie, of a whole piece
     float4v a, b;
     __device__ __forceinline__ float operator[](int k) const { return k < 4 ? a[k] : b[k - 4]; }
@@ -86,6 +106,25 @@ struct F32 {
 };
 struct B16 {
   using type = uint16_t;
+  // four side by side, `wide` if the buffer's 8 bytes allow it
+  static __device__ __forceinline__ void load4(uint64_t p, uint64_t e, uint32_t n, bool wide, float (&v)[4]) {
+    if (wide && n >= 4) {
+      const uint2v a = global<const uint2v>(p + e * 2)[0];
+      v[0] = Brain::value(a[0] & 0xffffu), v[1] = Brain::value(a[0] >> 16), v[2] = Brain::value(a[1] & 0xffffu), v[3] = Brain::value(a[1] >> 16);
+      return;
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < 4; ++k) v[k] = k < n ? load(p, e + k) : 0.f;
+  }
+  static __device__ __forceinline__ void store4(uint64_t p, uint64_t e, uint32_t n, bool wide, const float (&v)[4]) {
+    if (wide && n >= 4) {
+      global<uint2v>(p + e * 2)[0] = uint2v{Brain::bits(v[0]) | Brain::bits(v[1]) << 16, Brain::bits(v[2]) | Brain::bits(v[3]) << 16};
+      return;
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < 4; ++k)
+      if (k < n) store(p, e + k, v[k]);
+  }
   struct Piece {
     uint4v a;
     __device__ __forceinline__ float operator[](int k) const { return Brain::value(a[k / 2] >> 16 * (k & 1) & 0xffffu); }
