@@ -17,6 +17,7 @@ namespace dadam {
 struct MatrixState {
   // dadam_set_matrices: by size, the largest first
   std::vector<OrthoTask> tasks;
+  std::vector<uint32_t> parts[2]; // OrthoTask::parts, with one plane and with two
   std::vector<uint64_t> need[2];  // bytes of workspace of a matrix and a replica, with one plane and with two
   char* memory = nullptr;         // tasks, and the matrix of every tile of each kind
   const OrthoTask* d_tasks[2] = {};
@@ -49,7 +50,27 @@ uint64_t lower_half(uint64_t n) { return n * (n + 1) / 2; }
 // Large tiles: for matrices whose sides they fill up by an eighth more than the small ones at most, if there are enough of them for the chip (256 compute
 // units, that hold one each).
 bool suits_large(uint32_t n) { return 8 * (uint64_t)filled(n, kLargeEdge) <= 9 * (uint64_t)filled(n, kSmallEdge); }
-constexpr uint64_t kEnoughLarge = 256;
+constexpr uint64_t kEnoughLarge = 256, kComputeUnits = 256;
+
+// X X^T of a matrix whose tiles sum for longer than the chip takes for all small tiles together: in ranges of columns, of as many stages as leave every compute unit the
+// same, but eight at least.  (A product of fewer than 32 stages takes no longer than the second launch.)  It depends on the layout alone, so that the workspace's size
+// changes no result.
+constexpr uint64_t kLongSum = 32, kLeastStages = 8;
+uint64_t stages_of(const OrthoTask& t, uint32_t planes) { return (uint64_t)t.Q * planes / 64; }
+void split_sums(std::vector<OrthoTask>* tasks, uint32_t planes, uint64_t replicas) {
+  uint64_t all = 0, most = 0;
+  for (const OrthoTask& t : *tasks)
+    if (t.edge == kSmallEdge) all += lower_half(t.P / kSmallEdge) * stages_of(t, planes) * replicas;
+  const uint64_t each = std::max(kLeastStages, all / kComputeUnits);
+  for (OrthoTask& t : *tasks) {
+    if (t.edge != kSmallEdge) continue;
+    const uint64_t stages = stages_of(t, planes);
+    t.parts = stages < kLongSum ? 1 : (uint32_t)std::max<uint64_t>(1, stages / each);
+    most = std::max<uint64_t>(most, t.parts);
+  }
+  if (most > 1) return;
+  for (OrthoTask& t : *tasks) t.parts = 0;
+}
 
 constexpr uint32_t kMostMatrices = 65536, kMostSide = 65536;
 
@@ -135,10 +156,12 @@ int set_matrices(dadam_handle* h, const dadam_matrix_desc* m, uint32_t n) {
   }
   std::vector<OrthoTask> planes[2] = {tasks, tasks};
   for (uint32_t p = 0; p < 2; ++p) {
+    split_sums(&planes[p], p + 1, h->cfg.n_rows);
     uint64_t at = 0;
     for (OrthoTask& t : planes[p]) {
       t.at = at;
-      s->need[p].push_back(ortho_places(t.P, t.Q, p + 1).bytes);
+      s->parts[p].push_back(t.parts);
+      s->need[p].push_back(ortho_places(t.P, t.Q, p + 1, t.parts).bytes);
       at += s->need[p].back();
     }
     s->need[p].push_back(at);
@@ -288,6 +311,7 @@ int run_group(dadam_handle* h, const Call& call, const Powers& pw, uint32_t k0, 
   const bool by_large = gram_by_large(edge, units[0] * (double)replicas, units[3] * (double)replicas, planes);
   const uint32_t gram_edge = by_large ? kLargeEdge : kSmallEdge, gram_units = units[by_large ? 0 : 3];
   const OrthoSpan& gram = spans[by_large ? 0 : 3];
+  const uint32_t parts = *std::max_element(m.parts[planes - 1].begin() + k0, m.parts[planes - 1].begin() + k1);
   OrthoBeginArgs<kMaxRows> begin;
   memset((void*)&begin, 0, sizeof(begin));
   begin.s = spans[2];
@@ -312,7 +336,7 @@ int run_group(dadam_handle* h, const Call& call, const Powers& pw, uint32_t k0, 
     s.from = (uint32_t)(k & 1);
     s.to = s.from ^ 1;
     s.fresh = std::ldexp(1.f, pa - 2 * x);
-    e = launch_ortho_gram(false, gram_edge, s, planes, gram_units, replicas, stream);
+    e = parts > 1 ? launch_ortho_parts(s, planes, parts, gram_units, replicas, stream) : launch_ortho_gram(false, gram_edge, s, planes, gram_units, replicas, stream);
     s.gain = std::ldexp(b, pb - pa);
     s.fresh = std::ldexp(c, pb - 2 * pa);
     if (!e) e = launch_ortho_gram(true, gram_edge, s, planes, gram_units, replicas, stream);

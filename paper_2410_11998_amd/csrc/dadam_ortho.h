@@ -22,14 +22,15 @@ struct OrthoTask {
                                                               // small tiles of the lower half
   float scale, decay;
   uint32_t edge;         // of the products' tiles
+  uint32_t parts;        // X X^T of so many ranges of columns, or 0: in one
 };
 
 // Workspace of a matrix, one replica: X twice (an iteration reads one and writes the other), with one plane what the half leaves of it (see dadam_ortho.hip),
-// A = X X^T, B = b A + c A A, partial sums of the norm.
+// A = X X^T, B = b A + c A A, partial sums of the norm, the ranges' parts of X X^T.
 struct OrthoPlaces {
-  uint64_t x[2], low, a, b, sums, bytes;
+  uint64_t x[2], low, a, b, sums, parts, bytes;
 };
-inline constexpr OrthoPlaces ortho_places(uint64_t P, uint64_t Q, uint64_t planes) {
+inline constexpr OrthoPlaces ortho_places(uint64_t P, uint64_t Q, uint64_t planes, uint64_t parts) {
   OrthoPlaces w{};
   uint64_t at = 0;
   w.x[0] = at, at += P * Q * 2 * planes;
@@ -38,6 +39,7 @@ inline constexpr OrthoPlaces ortho_places(uint64_t P, uint64_t Q, uint64_t plane
   w.a = at, at += P * P * 2 * planes;
   w.b = at, at += P * P * 2 * planes;
   w.sums = at, at += ((P / kOrthoCell) * (Q / kOrthoCell) * 8 + 255) / 256 * 256;
+  w.parts = at, at += parts * P * P * 4;
   w.bytes = at;
   return w;
 }
@@ -94,6 +96,8 @@ static_assert(sizeof(OrthoBeginArgs<kMaxRows>) <= 4096 && sizeof(OrthoEndArgs<kM
 int launch_ortho_norm(int gdt, const OrthoBeginArgs<kMaxRows>& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream);
 int launch_ortho_begin(int gdt, const OrthoBeginArgs<kMaxRows>& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream);
 int launch_ortho_gram(bool square, uint32_t edge, const OrthoStepArgs& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream);
+// The same of ranges of columns, by small tiles, and their sum: most is the largest OrthoTask::parts.
+int launch_ortho_parts(const OrthoStepArgs& a, uint32_t planes, uint32_t most, uint32_t units, uint32_t replicas, void* stream);
 int launch_ortho_next(uint32_t edge, const OrthoStepArgs& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream);
 int launch_ortho_end(int dtype, uint32_t edge, const OrthoEndArgs<kMaxRows>& a, uint32_t n_cols, uint32_t units, uint32_t replicas, void* stream);
 

@@ -97,7 +97,7 @@ __global__ __launch_bounds__(256) void k_ortho_norm(OrthoBeginArgs<N> a) {
   sum = wave_sum(sum);
   if (threadIdx.x % 64 == 0) parts[threadIdx.x / 64] = sum;
   __syncthreads();
-  if (threadIdx.x == 0) global<double>(u.base + ortho_places(u.t.P, u.t.Q, PLANES).sums)[u.tile] = parts[0] + parts[1] + parts[2] + parts[3];
+  if (threadIdx.x == 0) global<double>(u.base + ortho_places(u.t.P, u.t.Q, PLANES, u.t.parts).sums)[u.tile] = parts[0] + parts[1] + parts[2] + parts[3];
 }
 
 // X from the matrix, and of a step lines 9 to 13 of Algorithm 3 for the first moment and the accumulator.
@@ -107,7 +107,7 @@ __global__ __launch_bounds__(256) void k_ortho_begin(OrthoBeginArgs<N> a) {
   const Unit u = find_unit<kCells>(a.s);
   const Cell c = cell_of(u);
   const uint32_t row = blockIdx.y, tiles = (u.t.P / kOrthoCell) * (u.t.Q / kOrthoCell);
-  const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES);
+  const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES, u.t.parts);
   float DADAM_LDS* tile = (float DADAM_LDS*)ortho_lds;
   __shared__ double parts[4];
   double sum = 0.0;
@@ -159,16 +159,21 @@ __device__ __forceinline__ void to_words(const float (&v)[8], uint32_t (&w)[8]) 
   for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(v[k]);
 }
 
+// The row of a tile among those of the lower half.
+__device__ __forceinline__ uint32_t lower_row(uint32_t tile) {
+  uint32_t i = (uint32_t)((sqrtf(8.f * (float)tile + 1.f) - 1.f) * 0.5f);  // (the root may round across the border of a row of tiles)
+  while (i * (i + 1) / 2 > tile) --i;
+  while ((i + 1) * (i + 2) / 2 <= tile) ++i;
+  return i;
+}
+
 // A tile (i, j), j <= i, of A = X X^T or of B = b A + c A A, and its mirror image.
 template <int PLANES, int EDGE, int BUFFERS, bool SQUARE>
 __global__ __launch_bounds__(2 * EDGE) void k_ortho_gram(OrthoStepArgs a) {
   using T = GramTile<PLANES, EDGE, BUFFERS>;
   const Unit u = find_unit < EDGE == (int)kLargeEdge ? kGram : kSmallGram > (a.s);
-  const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES);
-  uint32_t i = (uint32_t)((sqrtf(8.f * (float)u.tile + 1.f) - 1.f) * 0.5f);  // (the root may round across the border of a row of tiles)
-  while (i * (i + 1) / 2 > u.tile) --i;
-  while ((i + 1) * (i + 2) / 2 <= u.tile) ++i;
-  const uint32_t j = u.tile - i * (i + 1) / 2, inner = SQUARE ? u.t.P : u.t.Q;
+  const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES, u.t.parts);
+  const uint32_t i = lower_row(u.tile), j = u.tile - i * (i + 1) / 2, inner = SQUARE ? u.t.P : u.t.Q;
   const uint64_t pitch = (uint64_t)inner * 2 * PLANES;
   const uint64_t in = u.base + (SQUARE ? w.a : x_at(w, a.from));
   char DADAM_LDS* lds = (char DADAM_LDS*)ortho_lds;
@@ -198,6 +203,49 @@ __global__ __launch_bounds__(2 * EDGE) void k_ortho_gram(OrthoStepArgs a) {
              });
 }
 
+// X X^T of a matrix whose tiles would leave most of the chip idle for the length of Q: a range of columns (blockIdx.z), 32 bits, with its mirror image.
+template <int PLANES, int BUFFERS>
+__global__ __launch_bounds__(2 * kSmallEdge) void k_ortho_part(OrthoStepArgs a) {
+  using T = GramTile<PLANES, (int)kSmallEdge, BUFFERS>;
+  const Unit u = find_unit<kSmallGram>(a.s);
+  if (blockIdx.z >= u.t.parts) return;
+  const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES, u.t.parts);
+  const uint32_t i = lower_row(u.tile), j = u.tile - i * (i + 1) / 2;
+  const uint64_t pitch = (uint64_t)u.t.Q * 2 * PLANES;
+  const uint32_t stages = (uint32_t)(pitch / kStageBytes), from = (uint32_t)((uint64_t)stages * blockIdx.z / u.t.parts), to = (uint32_t)((uint64_t)stages * (blockIdx.z + 1) / u.t.parts);
+  const uint64_t in = u.base + x_at(w, a.from) + (uint64_t)from * kStageBytes, out = u.base + w.parts + (uint64_t)blockIdx.z * u.t.P * u.t.P * 4;
+  char DADAM_LDS* lds = (char DADAM_LDS*)ortho_lds;
+  T t;
+  t.product(operand(in + (uint64_t)i * T::kM * pitch, pitch), operand(in + (uint64_t)j * T::kN * pitch, pitch), to - from, lds);
+  t.hand_out(lds, i != j, nothing_ahead,
+             [&](uint32_t m, uint32_t n, float (&v)[8], const Nothing&) { F32::store8(out, (uint64_t)(j * T::kN + n) * u.t.P + i * T::kM + m, 8, v); },
+             [&](uint32_t m, uint32_t n, const float (&v)[8]) { F32::store8(out, (uint64_t)(i * T::kM + m) * u.t.P + j * T::kN + n, 8, v); });
+}
+
+// A from its parts, in their order: 16 rows of a tile and of its mirror image (blockIdx.z), eight columns a thread.
+template <int PLANES>
+__global__ __launch_bounds__(256) void k_ortho_join(OrthoStepArgs a) {
+  const Unit u = find_unit<kSmallGram>(a.s);
+  const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES, u.t.parts);
+  const uint32_t i = lower_row(u.tile), j = u.tile - i * (i + 1) / 2, m = blockIdx.z * 16 + threadIdx.x / 16, n = threadIdx.x % 16 * 8;
+  for (int mirror = 0; mirror < (i == j ? 1 : 2); ++mirror) {
+    const uint32_t r = (mirror ? j : i) * kSmallEdge + m, c = (mirror ? i : j) * kSmallEdge + n;
+    const uint64_t e = (uint64_t)r * u.t.P + c, step = (uint64_t)u.t.P * u.t.P;
+    float v[8] = {};
+#pragma unroll 4
+    for (uint32_t k = 0; k < u.t.parts; ++k) {
+      float x[8];
+      F32::load8(u.base + w.parts, k * step + e, 8, x);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] += x[q];
+    }
+    uint32_t words[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) words[q] = operand_word<Half, PLANES>(v[q] * a.fresh);
+    store8<PLANES>(u.base + w.a, r, u.t.P, c, words);
+  }
+}
+
 // X of eight elements, highs and lows.
 template <int PLANES>
 __device__ __forceinline__ Eight load_x(uint64_t base, const OrthoPlaces& w, uint32_t which, const OrthoTask& t, uint32_t p, uint32_t q) {
@@ -222,7 +270,7 @@ template <int PLANES, int EDGE, int BUFFERS>
 __global__ __launch_bounds__(2 * EDGE) void k_ortho_next(OrthoStepArgs a) {
   using T = NextTile<PLANES, EDGE, BUFFERS>;
   const Unit u = find_unit<kWhole>(a.s);
-  const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES);
+  const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES, u.t.parts);
   char DADAM_LDS* lds = (char DADAM_LDS*)ortho_lds;
   uint32_t q0, p0;
   T t;
@@ -245,7 +293,7 @@ template <typename DT, int PLANES, int EDGE, int BUFFERS, int N>
 __global__ __launch_bounds__(2 * EDGE) void k_ortho_end(OrthoEndArgs<N> a) {
   using T = NextTile<PLANES, EDGE, BUFFERS>;
   const Unit u = find_unit<kWhole>(a.s);
-  const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES);
+  const OrthoPlaces w = ortho_places(u.t.P, u.t.Q, PLANES, u.t.parts);
   char DADAM_LDS* lds = (char DADAM_LDS*)ortho_lds;
   uint32_t q0, p0;
   T t;
@@ -331,10 +379,10 @@ OrthoEndArgs<N> shorter(const OrthoEndArgs<kMaxRows>& a) {
 
 // Launches KERNEL, whose workgroups take `lds` bytes of LDS: more than 64 KB have to be asked for once on every device.
 template <auto KERNEL, typename A>
-int launch(const A& a, uint32_t threads, uint32_t units, uint32_t replicas, uint32_t lds, void* stream) {
+int launch(const A& a, uint32_t threads, uint32_t units, uint32_t replicas, uint32_t lds, void* stream, uint32_t parts = 1) {
   if (lds > 65536)
     if (const int e = ask_for_lds<KERNEL>(lds)) return e;
-  KERNEL<<<dim3(units, replicas), threads, lds, (hipStream_t)stream>>>(a);
+  KERNEL<<<dim3(units, replicas, parts), threads, lds, (hipStream_t)stream>>>(a);
   return (int)hipGetLastError();
 }
 
@@ -371,6 +419,15 @@ int gram(bool square, uint32_t edge, const OrthoStepArgs& a, uint32_t units, uin
   });
 }
 template <int PLANES>
+int parts(const OrthoStepArgs& a, uint32_t most, uint32_t units, uint32_t replicas, void* stream) {
+  const int e = with_tiles(kSmallEdge, units * replicas * most, [&](auto, auto b) {
+    constexpr int kBuffers = decltype(b)::value;
+    using T = GramTile<PLANES, (int)kSmallEdge, kBuffers>;
+    return launch<k_ortho_part<PLANES, kBuffers>>(a, T::kThreads, units, replicas, T::kLds, stream, most);
+  });
+  return e ? e : launch<k_ortho_join<PLANES>>(a, 256, units, replicas, 0, stream, kSmallEdge / 16);
+}
+template <int PLANES>
 int next(uint32_t edge, const OrthoStepArgs& a, uint32_t units, uint32_t replicas, void* stream) {
   return with_tiles(edge, units * replicas, [&](auto e, auto b) {
     constexpr int kEdge = decltype(e)::value, kBuffers = decltype(b)::value;
@@ -399,6 +456,9 @@ int launch_ortho_begin(int gdt, const OrthoBeginArgs<kMaxRows>& a, uint32_t plan
 }
 int launch_ortho_gram(bool square, uint32_t edge, const OrthoStepArgs& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream) {
   return planes == 1 ? gram<1>(square, edge, a, units, replicas, stream) : gram<2>(square, edge, a, units, replicas, stream);
+}
+int launch_ortho_parts(const OrthoStepArgs& a, uint32_t planes, uint32_t most, uint32_t units, uint32_t replicas, void* stream) {
+  return planes == 1 ? parts<1>(a, most, units, replicas, stream) : parts<2>(a, most, units, replicas, stream);
 }
 int launch_ortho_next(uint32_t edge, const OrthoStepArgs& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream) {
   return planes == 1 ? next<1>(edge, a, units, replicas, stream) : next<2>(edge, a, units, replicas, stream);

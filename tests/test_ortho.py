@@ -308,3 +308,39 @@ def test_more_replicas_than_a_short_argument_block_names():
     for i, mat, want, may, _, _ in S.expected(host(g), m0, None, x0, 1, False, True, 2):
         assert np.linalg.norm(view(x[i], L.offsets, mat) - want) <= may
     L.close()
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("shapes", [[(5, 6759)], [(6759, 5), (1, 1)], [(130, 8200), (64, 64)], [(2500, 300), (3, 4)], [(1, 65536)]])
+def test_long_sums_in_ranges_of_columns(shapes, kind):
+    L = Layout(shapes, kind, rows=2)
+    g = on_device(L.random(13), kind)
+    outs = []
+    for n_bytes in (L.info.bytes, L.info.least_bytes):
+        outs.append(torch.full_like(g, SENTINEL))
+        B.dadam_orthogonalize(L.h, g, outs[-1], L.workspace(n_bytes), B.current_stream())
+    mask = torch.from_numpy(L.mask()).to(DEV)
+    assert torch.equal(outs[0][:, mask], outs[1][:, mask])
+    check_orthogonal(L, host(g), host(outs[0]), kind)
+    L.close()
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_large_tiles(kind):
+    """As many matrices as make 256 large tiles of X X^T, and smaller ones beside them."""
+    L = Layout([(512, 768), (768, 512), (500, 1010)] * 8 + [(256, 256)] * 2 + [(130, 200), (9, 7)], kind, rows=4)
+    g = on_device(L.random(14), kind)
+    given = host(g)
+    out = torch.full_like(g, SENTINEL)
+    B.dadam_orthogonalize(L.h, g, out, L.workspace(), B.current_stream())
+    got = host(out)
+    mask = L.mask()
+    assert all((got[i][~mask] == SENTINEL).all() for i in range(4))
+    _, _, half, planes = TYPES[kind]
+    for i in range(4):
+        for k in range(i, len(L.matrices), 7):           # the statement in 64 bits of every seventh
+            m = L.matrices[k]
+            a = view(given[i], L.offsets, m)
+            want = O.orthogonalised(a)
+            assert np.linalg.norm(view(got[i], L.offsets, m) - want) <= O.orthogonalised_error(a, planes) + half * np.linalg.norm(want)
+    L.close()
