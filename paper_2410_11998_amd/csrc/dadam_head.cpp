@@ -289,9 +289,6 @@ int dadam_head_loss(dadam_handle* h, const dadam_head* head, const void* const* 
         a.s = few.s;
         a.w = few_places(few.s, planes_of(h), gradient);
         a.stride = few.each;
-        uint64_t low = (uint64_t)head->width * xs;  // what the head, its rows and the hidden vectors begin at
-        for (uint32_t r = 0; r < rows; ++r) low |= a.row[r].head | a.row[r].hidden | a.row[r].dhidden;
-        a.wide = (low % 16 == 0 ? 1 : 0) | (head->width % 4 == 0 && at * gs % 16 == 0 ? 2 : 0);
         e = run_few(h, a, dhidden != nullptr, gradient, rows, hip_stream);
       }
     } else {

@@ -110,7 +110,6 @@ struct FewArgs {
   float* losses;
   float scale;
   uint32_t mean, add;
-  uint32_t wide;  // four elements side by side lie together: bit 0 of the head and the hidden vectors, bit 1 of the head's gradient
   HeadRow row[kHeadRows];
 };
 static_assert(sizeof(FewArgs) <= 4096, "the argument block of a launch holds 4 KB");

@@ -41,10 +41,10 @@ __device__ __forceinline__ bool few_target(const FewArgs& a, uint64_t target, ui
 }
 
 // Eight bfloat16s of a row from column k on; beyond the row zeros.
-__device__ __forceinline__ brain8 eight(uint64_t row, uint32_t width, uint32_t k, bool wide) {
+__device__ __forceinline__ brain8 eight(uint64_t row, uint32_t width, uint32_t k) {
   uint4v v = {0, 0, 0, 0};
-  if (wide && k + 8 <= width) {
-    v = global<const uint4v>(row + (uint64_t)k * 2)[0];
+  if (k + 8 <= width) {
+    v = global<const uint4u>(row + (uint64_t)k * 2)[0];
   } else {
 #pragma unroll
     for (uint32_t e = 0; e < 8; ++e)
@@ -62,7 +62,6 @@ __global__ __launch_bounds__(256) void k_few_logits(FewArgs a) {
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), block = SHARED ? blockIdx.x : blockIdx.x * 4 + wave;
   if (block >= a.s.blocks) return;
-  const bool wide = a.wide & 1;
   const uint32_t mine = block * kFewWords + (lane & 31), word = mine < a.s.vocab ? mine : a.s.vocab - 1;
   const uint64_t size = sizeof(typename XT::type), w = row.head + (uint64_t)word * a.s.width * size;
   uint64_t h[NB];
@@ -76,7 +75,7 @@ __global__ __launch_bounds__(256) void k_few_logits(FewArgs a) {
   for (int b = 0; b < NB; ++b) acc[b] = nothing();
   constexpr uint32_t kStep = BRAIN ? 16 : 8;
   const uint32_t steps = (a.s.width + kStep - 1) / kStep, from = SHARED ? steps * wave / 4 * kStep : 0, to = SHARED ? steps * (wave + 1) / 4 * kStep : steps * kStep;
-  const uint32_t whole = wide ? (to < a.s.width ? to : a.s.width / kStep * kStep) : from;  // up to here whole pieces
+  const uint32_t whole = to < a.s.width ? to : a.s.width / kStep * kStep;  // up to here whole pieces
   uint32_t k0 = from;
   constexpr uint32_t kAhead = NB == 1 ? 8 : 4;  // pieces of a row on their way at once
   for (; k0 + kAhead * kStep <= whole; k0 += kAhead * kStep) {
@@ -85,9 +84,9 @@ __global__ __launch_bounds__(256) void k_few_logits(FewArgs a) {
       brain8 x[kAhead], y[kAhead][NB];
 #pragma unroll
       for (uint32_t s = 0; s < kAhead; ++s) {
-        x[s] = global<const brain8>(w + (uint64_t)(k + s * kStep) * 2)[0];
+        x[s] = __builtin_bit_cast(brain8, (uint4v)global<const uint4u>(w + (uint64_t)(k + s * kStep) * 2)[0]);
 #pragma unroll
-        for (int b = 0; b < NB; ++b) y[s][b] = global<const brain8>(h[b] + (uint64_t)(k + s * kStep) * 2)[0];
+        for (int b = 0; b < NB; ++b) y[s][b] = __builtin_bit_cast(brain8, (uint4v)global<const uint4u>(h[b] + (uint64_t)(k + s * kStep) * 2)[0]);
       }
 #pragma unroll
       for (uint32_t s = 0; s < kAhead; ++s)
@@ -97,9 +96,9 @@ __global__ __launch_bounds__(256) void k_few_logits(FewArgs a) {
       float x[kAhead][4], y[kAhead][NB][4];
 #pragma unroll
       for (uint32_t s = 0; s < kAhead; ++s) {
-        XT::load4(w, k + s * kStep, 4, true, x[s]);
+        XT::load4(w, k + s * kStep, 4, x[s]);
 #pragma unroll
-        for (int b = 0; b < NB; ++b) XT::load4(h[b], k + s * kStep, 4, true, y[s][b]);
+        for (int b = 0; b < NB; ++b) XT::load4(h[b], k + s * kStep, 4, y[s][b]);
       }
 #pragma unroll
       for (uint32_t s = 0; s < kAhead; ++s)
@@ -112,14 +111,14 @@ __global__ __launch_bounds__(256) void k_few_logits(FewArgs a) {
   for (; k0 < to; k0 += kStep) {
     const uint32_t k = k0 + half * (kStep / 2);
     if constexpr (BRAIN) {
-      const brain8 x = eight(w, a.s.width, k, wide);
+      const brain8 x = eight(w, a.s.width, k);
 #pragma unroll
-      for (int b = 0; b < NB; ++b) acc[b] = Brain::mfma(x, eight(h[b], a.s.width, k, wide), acc[b]);
+      for (int b = 0; b < NB; ++b) acc[b] = Brain::mfma(x, eight(h[b], a.s.width, k), acc[b]);
     } else {
       float x[4], y[NB][4];
-      XT::load4(w, k, rest(a.s.width, k), wide, x);
+      XT::load4(w, k, rest(a.s.width, k), x);
 #pragma unroll
-      for (int b = 0; b < NB; ++b) XT::load4(h[b], k, rest(a.s.width, k), wide, y[b]);
+      for (int b = 0; b < NB; ++b) XT::load4(h[b], k, rest(a.s.width, k), y[b]);
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -304,7 +303,6 @@ __device__ __forceinline__ void few_dhead(const FewArgs& a, const HeadRow& row, 
     }
   }
   const float factor = few_factor(base, a);
-  const bool wide = a.wide & 2;
   const uint32_t columns = rest(a.s.width, d);
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
@@ -312,10 +310,10 @@ __device__ __forceinline__ void few_dhead(const FewArgs& a, const HeadRow& row, 
     if (word >= a.s.vocab || columns == 0) continue;
     const uint64_t e = (uint64_t)word * a.s.width + d;
     float g[4] = {};
-    if (a.add) GT::load4(row.dhead, e, columns, wide, g);
+    if (a.add) GT::load4(row.dhead, e, columns, g);
 #pragma unroll
     for (int j = 0; j < 4; ++j) g[j] = fmaf(acc[j][r], factor, g[j]);
-    GT::store4(row.dhead, e, columns, wide, g);
+    GT::store4(row.dhead, e, columns, g);
   }
 }
 
@@ -343,7 +341,7 @@ __device__ __forceinline__ void few_dhidden(const FewArgs& a, const HeadRow& row
           const uint32_t mine = block * kFewWords + s + half * 8 + e, word = mine < a.s.vocab ? mine : a.s.vocab - 1;
           const uint64_t at = row.head + ((uint64_t)word * a.s.width + from) * 2;
           if (WIDE) {
-            w[e] = global<const uint2v>(at)[0];
+            w[e] = global<const uint2u>(at)[0];
           } else {
             w[e] = uint2v{0, 0};
 #pragma unroll
@@ -373,7 +371,7 @@ __device__ __forceinline__ void few_dhidden(const FewArgs& a, const HeadRow& row
         for (uint32_t e = 0; e < 4; ++e) {
           const uint32_t mine = block * kFewWords + s + half * 4 + e, word = mine < a.s.vocab ? mine : a.s.vocab - 1;
           float w[4];
-          XT::load4(row.head, (uint64_t)word * a.s.width + from, WIDE ? 4 : columns, WIDE, w);
+          XT::load4(row.head, (uint64_t)word * a.s.width + from, WIDE ? 4 : columns, w);
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -401,7 +399,7 @@ __global__ __launch_bounds__(256) void k_few_gradients(FewArgs a) {
   const uint32_t chunks = a.s.D / kFewColumns, first = row.dhidden ? a.s.ranges * chunks : 0;
   uint32_t item = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / 64);
   if (item < first) {
-    if (a.wide & 1) few_dhidden<XT, BRAIN, NB, true>(a, row, base, item / chunks, item % chunks * kFewColumns, lane);
+    if (item % chunks * kFewColumns + kFewColumns <= a.s.width || a.s.width % 4 == 0) few_dhidden<XT, BRAIN, NB, true>(a, row, base, item / chunks, item % chunks * kFewColumns, lane);
     else few_dhidden<XT, BRAIN, NB, false>(a, row, base, item / chunks, item % chunks * kFewColumns, lane);
   } else if (row.dhead && item - first < a.s.blocks * chunks) {
     item -= first;
@@ -426,7 +424,7 @@ __global__ __launch_bounds__(256) void k_few_end(FewArgs a) {
     int32_t target;
     const float factor = few_target(a, row.target, t, target) ? few_factor(base, a) : 0.f;
     const float g[4] = {factor == 0.f ? 0.f : v[0] * factor, factor == 0.f ? 0.f : v[1] * factor, factor == 0.f ? 0.f : v[2] * factor, factor == 0.f ? 0.f : v[3] * factor};
-    XT::store4(row.dhidden, (uint64_t)t * a.s.width + c, rest(a.s.width, c), a.wide & 1, g);
+    XT::store4(row.dhidden, (uint64_t)t * a.s.width + c, rest(a.s.width, c), g);
   }
 }
 

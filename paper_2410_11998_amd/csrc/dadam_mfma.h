@@ -26,6 +26,12 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 
+// The same where elements lie as a caller's buffer has them, at a multiple of an element's size only (memory takes such pieces at any address; element by element, a vector of
+// odd width takes three times as long).
+typedef float4v float4u __attribute__((aligned(4)));
+typedef uint2v uint2u __attribute__((aligned(2)));
+typedef uint4v uint4u __attribute__((aligned(2)));
+
 #define DADAM_GLOBAL __attribute__((address_space(1)))
 #define DADAM_LDS __attribute__((address_space(3)))
 
@@ -52,13 +58,12 @@ struct Brain {
   static __device__ __forceinline__ float value(uint32_t b) { return __uint_as_float(b << 16); }
 };
 
-// Elements of parameters, gradients and state: one, or up to eight side by side (a whole piece where the buffer's 16 bytes allow it; beyond n: zeros, not
-// stored).
+// Elements of parameters, gradients and state: one, or up to four or eight side by side (beyond n: zeros, not stored).
 struct F32 {
   using type = float;
-  static __device__ __forceinline__ void load4(uint64_t p, uint64_t e, uint32_t n, bool wide, float (&v)[4]) {
-    if (wide && n >= 4) {
-      const float4v a = global<const float4v>(p + e * 4)[0];
+  static __device__ __forceinline__ void load4(uint64_t p, uint64_t e, uint32_t n, float (&v)[4]) {
+    if (n >= 4) {
+      const float4v a = global<const float4u>(p + e * 4)[0];
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[k] = a[k];
       return;
@@ -66,9 +71,9 @@ struct F32 {
 #pragma unroll
     for (uint32_t k = 0; k < 4; ++k) v[k] = k < n ? load(p, e + k) : 0.f;
   }
-  static __device__ __forceinline__ void store4(uint64_t p, uint64_t e, uint32_t n, bool wide, const float (&v)[4]) {
-    if (wide && n >= 4) {
-      global<float4v>(p + e * 4)[0] = float4v{v[0], v[1], v[2], v[3]};
+  static __device__ __forceinline__ void store4(uint64_t p, uint64_t e, uint32_t n, const float (&v)[4]) {
+    if (n >= 4) {
+      global<float4u>(p + e * 4)[0] = float4v{v[0], v[1], v[2], v[3]};
       return;
     }
 #pragma unroll
@@ -79,13 +84,13 @@ struct F32 {
     float4v a, b;
     __device__ __forceinline__ float operator[](int k) const { return k < 4 ? a[k] : b[k - 4]; }
   };
-  static __device__ __forceinline__ bool is_whole(uint64_t p, uint64_t e, uint32_t n) { return n >= 8 && (p + e * 4) % 16 == 0; }
-  static __device__ __forceinline__ Piece piece(uint64_t p, uint64_t e) { return {global<const float4v>(p + e * 4)[0], global<const float4v>(p + e * 4)[1]}; }
+  static __device__ __forceinline__ bool is_whole(uint32_t n) { return n >= 8; }
+  static __device__ __forceinline__ Piece piece(uint64_t p, uint64_t e) { return {global<const float4u>(p + e * 4)[0], global<const float4u>(p + e * 4)[1]}; }
   static __device__ __forceinline__ float load(uint64_t p, uint64_t e) { return global<const float>(p)[e]; }
   static __device__ __forceinline__ void store(uint64_t p, uint64_t e, float v) { global<float>(p)[e] = v; }
   static __device__ __forceinline__ void load8(uint64_t p, uint64_t e, uint32_t n, float (&v)[8]) {
-    if (n >= 8 && (p + e * 4) % 16 == 0) {
-      const float4v a = global<const float4v>(p + e * 4)[0], b = global<const float4v>(p + e * 4)[1];
+    if (n >= 8) {
+      const float4v a = global<const float4u>(p + e * 4)[0], b = global<const float4u>(p + e * 4)[1];
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[k] = a[k], v[4 + k] = b[k];
       return;
@@ -94,9 +99,9 @@ struct F32 {
     for (uint32_t k = 0; k < 8; ++k) v[k] = k < n ? load(p, e + k) : 0.f;
   }
   static __device__ __forceinline__ void store8(uint64_t p, uint64_t e, uint32_t n, const float (&v)[8]) {
-    if (n >= 8 && (p + e * 4) % 16 == 0) {
-      global<float4v>(p + e * 4)[0] = float4v{v[0], v[1], v[2], v[3]};
-      global<float4v>(p + e * 4)[1] = float4v{v[4], v[5], v[6], v[7]};
+    if (n >= 8) {
+      global<float4u>(p + e * 4)[0] = float4v{v[0], v[1], v[2], v[3]};
+      global<float4u>(p + e * 4)[1] = float4v{v[4], v[5], v[6], v[7]};
       return;
     }
 #pragma unroll
@@ -106,19 +111,18 @@ struct F32 {
 };
 struct B16 {
   using type = uint16_t;
-  // four side by side, `wide` if the buffer's 8 bytes allow it
-  static __device__ __forceinline__ void load4(uint64_t p, uint64_t e, uint32_t n, bool wide, float (&v)[4]) {
-    if (wide && n >= 4) {
-      const uint2v a = global<const uint2v>(p + e * 2)[0];
+  static __device__ __forceinline__ void load4(uint64_t p, uint64_t e, uint32_t n, float (&v)[4]) {
+    if (n >= 4) {
+      const uint2v a = global<const uint2u>(p + e * 2)[0];
       v[0] = Brain::value(a[0] & 0xffffu), v[1] = Brain::value(a[0] >> 16), v[2] = Brain::value(a[1] & 0xffffu), v[3] = Brain::value(a[1] >> 16);
       return;
     }
 #pragma unroll
     for (uint32_t k = 0; k < 4; ++k) v[k] = k < n ? load(p, e + k) : 0.f;
   }
-  static __device__ __forceinline__ void store4(uint64_t p, uint64_t e, uint32_t n, bool wide, const float (&v)[4]) {
-    if (wide && n >= 4) {
-      global<uint2v>(p + e * 2)[0] = uint2v{Brain::bits(v[0]) | Brain::bits(v[1]) << 16, Brain::bits(v[2]) | Brain::bits(v[3]) << 16};
+  static __device__ __forceinline__ void store4(uint64_t p, uint64_t e, uint32_t n, const float (&v)[4]) {
+    if (n >= 4) {
+      global<uint2u>(p + e * 2)[0] = uint2v{Brain::bits(v[0]) | Brain::bits(v[1]) << 16, Brain::bits(v[2]) | Brain::bits(v[3]) << 16};
       return;
     }
 #pragma unroll
@@ -129,13 +133,13 @@ struct B16 {
     uint4v a;
     __device__ __forceinline__ float operator[](int k) const { return Brain::value(a[k / 2] >> 16 * (k & 1) & 0xffffu); }
   };
-  static __device__ __forceinline__ bool is_whole(uint64_t p, uint64_t e, uint32_t n) { return n >= 8 && (p + e * 2) % 16 == 0; }
-  static __device__ __forceinline__ Piece piece(uint64_t p, uint64_t e) { return {global<const uint4v>(p + e * 2)[0]}; }
+  static __device__ __forceinline__ bool is_whole(uint32_t n) { return n >= 8; }
+  static __device__ __forceinline__ Piece piece(uint64_t p, uint64_t e) { return {global<const uint4u>(p + e * 2)[0]}; }
   static __device__ __forceinline__ float load(uint64_t p, uint64_t e) { return Brain::value(global<const uint16_t>(p)[e]); }
   static __device__ __forceinline__ void store(uint64_t p, uint64_t e, float v) { global<uint16_t>(p)[e] = (uint16_t)Brain::bits(v); }
   static __device__ __forceinline__ void load8(uint64_t p, uint64_t e, uint32_t n, float (&v)[8]) {
-    if (n >= 8 && (p + e * 2) % 16 == 0) {
-      const uint4v a = global<const uint4v>(p + e * 2)[0];
+    if (n >= 8) {
+      const uint4v a = global<const uint4u>(p + e * 2)[0];
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[2 * k] = Brain::value(a[k] & 0xffffu), v[2 * k + 1] = Brain::value(a[k] >> 16);
       return;
@@ -144,11 +148,11 @@ struct B16 {
     for (uint32_t k = 0; k < 8; ++k) v[k] = k < n ? load(p, e + k) : 0.f;
   }
   static __device__ __forceinline__ void store8(uint64_t p, uint64_t e, uint32_t n, const float (&v)[8]) {
-    if (n >= 8 && (p + e * 2) % 16 == 0) {
+    if (n >= 8) {
       uint4v r;
 #pragma unroll
       for (int k = 0; k < 4; ++k) r[k] = Brain::bits(v[2 * k]) | Brain::bits(v[2 * k + 1]) << 16;
-      global<uint4v>(p + e * 2)[0] = r;
+      global<uint4u>(p + e * 2)[0] = r;
       return;
     }
 #pragma unroll

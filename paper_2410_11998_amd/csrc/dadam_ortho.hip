@@ -325,7 +325,7 @@ __global__ __launch_bounds__(2 * EDGE) void k_ortho_end(OrthoEndArgs<N> a) {
     }
     float mixed[8], x[8];
     int32_t k = first;
-    if (DT::is_whole(out, e, n)) {  // (all buffers begin at a multiple of 16 bytes)
+    if (DT::is_whole(n)) {
       typename DT::Piece early_pieces[kEarly];
 #pragma unroll
       for (int32_t q = 0; q < kEarly; ++q)
