@@ -238,3 +238,62 @@ def test_recorded_into_a_graph():
         for a, b in zip(eager, (c.losses, c.nll, c.dhidden, c.g)):
             assert torch.equal(a, b)
     c.close()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("tokens", [1, 30, 64])
+def test_few_tokens_with_a_workspace_for_pieces_only(tokens, kind):
+    """Up to 64 tokens have a way of their own, which a workspace of least_bytes does not allow where the vocabulary is long."""
+    c = Head(tokens, 20011, 90, kind, rows=2, bias=True, seed=13)
+    info = c.info()
+    assert info.least_bytes < info.bytes
+    for n_bytes in (info.bytes, info.bytes // 2, info.least_bytes):
+        if n_bytes < info.least_bytes:
+            continue
+        c.g.fill_(SENTINEL)
+        c.dhidden.fill_(SENTINEL)
+        c.run(work=c.workspace(n_bytes))
+        c.check()
+    c.close()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("share", [1.0, 0.4])
+def test_large_tiles(kind, share):
+    """As many words and tokens as make 256 large tiles, with what large tiles leave over; share: of the workspace that a call makes good use of."""
+    c = Head(1024, 16400, 256, kind, bias=True, seed=14)
+    work = c.workspace(int(c.info().bytes * share))
+    c.run(work=work)
+    c.check()
+    c.close()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_operands_as_they_lie_and_vectors_of_any_beginning(kind):
+    """A head whose rows begin at multiples of 16 bytes and fill whole tiles, and hidden vectors that begin at an odd element."""
+    c = Head(200, 384, 128, kind, rows=2, seed=15, before=7)       # (behind 7 elements and a gap of one)
+    assert c.at % 8 == 0
+    flat = torch.full((2, 200 * 128 + 1), SENTINEL, device=DEV, dtype=c.hidden.dtype)
+    flat[:, 1:] = c.hidden.flatten(1)
+    out = torch.full((2, 200 * 128 + 1), SENTINEL, device=DEV, dtype=c.hidden.dtype)
+    B.dadam_head_loss(c.h, c.head, c.x, [v[1:] for v in flat], c.y, 200, 1.0, B.DADAM_HEAD_MEAN, c.losses, c.nll, [v[1:] for v in out], c.g, c.workspace(), B.current_stream())
+    assert bool((out[:, 0] == SENTINEL).all())
+    c.dhidden.copy_(out[:, 1:].view(2, 200, 128))
+    c.check()
+    c.close()
+
+
+@pytest.mark.parametrize("tokens", [40, 300])
+def test_two_calls_at_once_on_streams_of_their_own(tokens):
+    """Two replicas' losses by two handles, each with a stream and a workspace."""
+    cs = [Head(tokens, 900, 80, "bf16", bias=True, seed=16 + k) for k in range(2)]
+    works = [c.workspace() for c in cs]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for c, w in zip(cs, works):
+            with torch.cuda.stream(torch.cuda.Stream()):
+                c.run(work=w)
+    torch.cuda.synchronize()
+    for c in cs:
+        c.check()
+        c.close()
