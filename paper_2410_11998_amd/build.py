@@ -28,7 +28,7 @@ TYPES = {"f32": "TF32", "bf16": "TBF16"}
 # (object name, source, extra definitions)
 UNITS = [("dadam_host", "dadam_host.cpp", []), ("dadam_place", "dadam_place.cpp", []), ("dadam_kernels", "dadam_kernels.hip", []),
          ("dadam_operators", "dadam_operators.cpp", []), ("dadam_norm", "dadam_norm.hip", []), ("dadam_mx4", "dadam_mx4.hip", []),
-         ("dadam_ortho_host", "dadam_ortho.cpp", []), ("dadam_ortho", "dadam_ortho.hip", []),
+         ("dadam_ortho_host", "dadam_ortho.cpp", []), ("dadam_ortho", "dadam_ortho.hip", []), ("dadam_ortho_lone", "dadam_ortho_lone.hip", []),
          ("dadam_head_host", "dadam_head.cpp", []), ("dadam_head", "dadam_head.hip", []), ("dadam_head_few", "dadam_head_few.hip", [])]
 for _x in ("f32", "bf16"):
     for _g in ("f32", "bf16"):

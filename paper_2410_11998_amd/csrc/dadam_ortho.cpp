@@ -23,6 +23,7 @@ struct MatrixState {
   const OrthoTask* d_tasks[2] = {};
   const uint32_t* d_units[4] = {};  // OrthoTask::gram_units, whole_units, cell_units, small_units
   uint32_t n_units[4] = {};
+  uint32_t lone_lds = 0;          // where a workgroup holds each of them: the most that one takes
   // dadam_set_ortho_schedule
   std::vector<float> coefficients{3.4445f, -4.7750f, 2.0315f, 3.4445f, -4.7750f, 2.0315f, 3.4445f, -4.7750f, 2.0315f, 3.4445f, -4.7750f, 2.0315f, 3.4445f, -4.7750f, 2.0315f};
 };
@@ -111,6 +112,9 @@ int set_matrices(dadam_handle* h, const dadam_matrix_desc* m, uint32_t n) {
   if (const int rc = check_matrices(h, m, n)) return rc;
   std::unique_ptr<MatrixState, void (*)(MatrixState*)> s(new MatrixState(), free_matrices);
   if (h->matrices) s->coefficients = h->matrices->coefficients;
+  // A layout of matrices that each fit a compute unit goes by those (64 x 48 and 48 x 192: 47 us instead of 138).  Beside larger ones they go with those, whose launches
+  // they lengthen by little (40 matrices of odd sizes 466 us, the small ones apart 623).
+  bool lone = n > 0;
   std::vector<OrthoTask> tasks(n);
   for (uint32_t k = 0; k < n; ++k) {
     OrthoTask& t = tasks[k];
@@ -121,6 +125,7 @@ int set_matrices(dadam_handle* h, const dadam_matrix_desc* m, uint32_t n) {
     t.p = std::min(m[k].rows, m[k].cols);
     t.q = std::max(m[k].rows, m[k].cols);
     t.edge = suits_large(t.p) && suits_large(t.q) ? kLargeEdge : kSmallEdge;
+    lone = lone && lone_lds_bytes(filled(t.p, kLoneEdge), filled(t.q, kLoneEdge)) <= kMostLoneLds;
     t.scale = m[k].scale;
     t.decay = tensor.weight_decay;
   }
@@ -129,8 +134,13 @@ int set_matrices(dadam_handle* h, const dadam_matrix_desc* m, uint32_t n) {
     if (t.edge == kLargeEdge) large += lower_half(filled(t.p, kLargeEdge) / kLargeEdge);
   for (OrthoTask& t : tasks) {
     if (large * h->cfg.n_rows < kEnoughLarge) t.edge = kSmallEdge;
+    if (lone) t.edge = kLoneEdge;
     t.P = filled(t.p, t.edge);
     t.Q = filled(t.q, t.edge);
+    if (lone) {
+      s->lone_lds = std::max(s->lone_lds, (uint32_t)lone_lds_bytes(t.P, t.Q));
+      continue;
+    }
     units[0] += lower_half(t.P / t.edge);
     units[1] += (uint64_t)(t.P / t.edge) * (t.Q / t.edge);
     units[2] += (uint64_t)(t.P / kOrthoCell) * (t.Q / kOrthoCell);
@@ -143,7 +153,7 @@ int set_matrices(dadam_handle* h, const dadam_matrix_desc* m, uint32_t n) {
   });
   std::vector<uint32_t> of_unit[4];
   for (int kind = 0; kind < 4; ++kind) of_unit[kind].reserve(units[kind]);
-  for (uint32_t k = 0; k < n; ++k) {
+  for (uint32_t k = 0; k < n && !lone; ++k) {
     OrthoTask& t = tasks[k];
     t.gram_units = (uint32_t)of_unit[0].size();
     t.whole_units = (uint32_t)of_unit[1].size();
@@ -161,7 +171,7 @@ int set_matrices(dadam_handle* h, const dadam_matrix_desc* m, uint32_t n) {
     for (OrthoTask& t : planes[p]) {
       t.at = at;
       s->parts[p].push_back(t.parts);
-      s->need[p].push_back(ortho_places(t.P, t.Q, p + 1, t.parts).bytes);
+      s->need[p].push_back(lone ? 0 : ortho_places(t.P, t.Q, p + 1, t.parts).bytes);
       at += s->need[p].back();
     }
     s->need[p].push_back(at);
@@ -370,6 +380,50 @@ int run_group(dadam_handle* h, const Call& call, const Powers& pw, uint32_t k0, 
   return e;
 }
 
+// The matrices that a workgroup holds, of all replicas.
+int run_lone(dadam_handle* h, const Call& call, const Powers& pw, void* stream) {
+  const MatrixState& m = *h->matrices;
+  const uint32_t R = h->cfg.n_rows;
+  OrthoLoneArgs<kLoneRows, kMaxRows> a;
+  memset((void*)&a, 0, sizeof(a));
+  a.tasks = m.d_tasks[planes_of(call.dtype) - 1];
+  a.n_steps = (uint32_t)pw.x.size();
+  a.source = call.source;
+  a.phase = call.phase;
+  a.c = call.c;
+  a.scale = std::ldexp(1.f, pw.x[0]);
+  for (uint32_t k = 0; k < a.n_steps; ++k) {
+    const int x = pw.x[k], pa = pw.a[k], pb = pw.b[k], next = k + 1 < a.n_steps ? pw.x[k + 1] : 0;
+    a.step[k].a_fresh = std::ldexp(1.f, pa - 2 * x);
+    a.step[k].b_gain = std::ldexp(m.coefficients[3 * k + 1], pb - pa);
+    a.step[k].b_fresh = std::ldexp(m.coefficients[3 * k + 2], pb - 2 * pa);
+    a.step[k].x_gain = std::ldexp(m.coefficients[3 * k], next - x);
+    a.step[k].x_fresh = std::ldexp(1.f, next - x - pb);
+  }
+  if (call.mix) {
+    for (uint32_t q = 0; q < h->cfg.n_cols; ++q) a.x_src[q] = h->x_src[q];
+    const Slot& slot = h->slots[call.slot];
+    a.mix = 1;
+    a.row_ptr = slot.d_row_ptr;
+    a.col = slot.d_col;
+    a.w = slot.d_w;
+    a.lr = call.c.lr;
+  }
+  int e = (int)hipSuccess;
+  for (uint32_t i = 0; i < R && !e; i += kLoneRows) {
+    const uint32_t replicas = std::min<uint32_t>(kLoneRows, R - i);
+    a.first_row = i;
+    for (uint32_t r = 0; r < replicas; ++r) {
+      a.grad[r] = call.grads[i + r];
+      a.out[r] = call.out[i + r];
+      a.m_hat[r] = call.source == kOrthoGiven ? nullptr : h->m_hat[i + r];
+      a.acc[r] = call.source == kOrthoGiven ? nullptr : h->acc[i + r];
+    }
+    e = launch_ortho_lone((int)h->cfg.grad_dtype, (int)call.dtype, a, call.mix ? h->cfg.n_cols : 1, (uint32_t)m.tasks.size(), replicas, m.lone_lds, stream);
+  }
+  return e;
+}
+
 int check_workspace(const dadam_handle* h, const void* workspace, uint64_t bytes, uint64_t least) {
   if (!workspace && least) return fail(h, DADAM_EINVAL, "workspace is null");
   if ((uintptr_t)workspace & 255u) return fail(h, DADAM_EALIGN, "workspace is not 256-byte aligned");
@@ -389,8 +443,9 @@ int run(dadam_handle* h, const Call& call, void* stream) {
   const uint32_t n = (uint32_t)h->matrices->tasks.size(), R = h->cfg.n_rows;
   DeviceGuard guard(h->cfg.device);
   if (guard.err != hipSuccess) return fail(h, DADAM_EHIP, "hipSetDevice: %s", hipGetErrorString(guard.err));
-  int e = (int)hipSuccess;
-  for (uint32_t k = 0; k < n && !e;) {
+  const bool lone = h->matrices->lone_lds != 0;
+  int e = lone ? run_lone(h, call, pw, stream) : (int)hipSuccess;
+  for (uint32_t k = 0; k < n && !lone && !e;) {
     uint32_t end = end_of_group(h, planes_of(call.dtype), k, call.bytes);
     if (end > k) {
       e = run_group(h, call, pw, k, end, 0, R, stream);

@@ -89,6 +89,34 @@ struct OrthoEndArgs {
   float lr;
 };
 
+// Matrices that a workgroup holds in LDS (dadam_ortho_lone.hip): their rows and columns are filled up to multiples of kLoneEdge, and no workspace is theirs.
+constexpr uint32_t kLoneEdge = 32, kLoneThreads = 512, kMostLoneLds = 160 * 1024 - 256;
+constexpr int kLoneRows = 64;
+inline constexpr uint64_t lone_lds_bytes(uint64_t P, uint64_t Q) {
+  return P > 4 * kLoneEdge ? ~0ull : (P * (Q + 4) + P * (P + 4) + (P <= 2 * kLoneEdge ? 8192 : 0)) * 4;
+}
+// What is stored of a product, and of the term held already.
+struct LoneStep {
+  float a_fresh, b_gain, b_fresh, x_gain, x_fresh;
+};
+template <int N, int C>
+struct OrthoLoneArgs {
+  const OrthoTask* tasks;  // device, the first of them
+  uint32_t n_steps, source, phase, mix, first_row;
+  float scale, lr;
+  Scalars c;
+  const int32_t* row_ptr;
+  const int32_t* col;
+  const float* w;
+  LoneStep step[DADAM_ORTHO_MAX_STEPS];
+  const void* grad[N];
+  float* m_hat[N];
+  float* acc[N];
+  void* out[N];
+  const void* x_src[C];
+};
+static_assert(sizeof(OrthoLoneArgs<kLoneRows, kMaxRows>) <= 4096, "the argument block of a launch holds 4 KB");
+
 constexpr int kOrthoFew = 16;
 static_assert(sizeof(OrthoBeginArgs<kMaxRows>) <= 4096 && sizeof(OrthoEndArgs<kMaxRows>) <= 4096, "the argument block of a launch holds 4 KB");
 
@@ -100,6 +128,7 @@ int launch_ortho_gram(bool square, uint32_t edge, const OrthoStepArgs& a, uint32
 int launch_ortho_parts(const OrthoStepArgs& a, uint32_t planes, uint32_t most, uint32_t units, uint32_t replicas, void* stream);
 int launch_ortho_next(uint32_t edge, const OrthoStepArgs& a, uint32_t planes, uint32_t units, uint32_t replicas, void* stream);
 int launch_ortho_end(int dtype, uint32_t edge, const OrthoEndArgs<kMaxRows>& a, uint32_t n_cols, uint32_t units, uint32_t replicas, void* stream);
+int launch_ortho_lone(int gdt, int dtype, const OrthoLoneArgs<kLoneRows, kMaxRows>& a, uint32_t n_cols, uint32_t matrices, uint32_t replicas, uint32_t lds, void* stream);
 
 }  // namespace dadam
 

@@ -12,6 +12,7 @@
 // from two halves as well (1.4e-3 and 5e-4), the second of which no product reads.
 #include "dadam_mfma.h"
 #include "dadam_ortho.h"
+#include "dadam_ortho_source.h"
 
 namespace dadam {
 namespace {
@@ -63,16 +64,6 @@ __device__ __forceinline__ Cell cell_of(const Unit& u) {
   return c;
 }
 
-// What is orthogonalised, of one element: the gradient, the moment of line 6 of Algorithm 3, or that looked ahead.
-__device__ __forceinline__ float source_value(const Scalars& c, uint32_t source, float g, float mh) {
-  if (source == kOrthoGiven) return g;
-  const float m = fmaf(c.beta1, mh, c.omb1 * g);
-  return source == kOrthoMoment ? m : fmaf(c.beta1, m, c.omb1 * g);
-}
-
-// Elements of a row of the matrix from column `col` on.
-__device__ __forceinline__ uint32_t left(uint32_t cols, uint32_t col) { return col < cols ? cols - col : 0; }
-
 // Squares of a cell, in 64 bits, to its place among the matrix's partial sums.
 template <typename GT, int PLANES, int N>
 __global__ __launch_bounds__(256) void k_ortho_norm(OrthoBeginArgs<N> a) {
@@ -84,14 +75,9 @@ __global__ __launch_bounds__(256) void k_ortho_norm(OrthoBeginArgs<N> a) {
   if (n)
     for (uint32_t r = c.r0 + threadIdx.x / 16; r < c.r0 + kOrthoCell && r < c.rows; r += 16) {
       const uint64_t e = u.t.first + (uint64_t)r * u.t.ld + col;
-      float gv[8], m[8] = {};
-      GT::load8(g, e, n, gv);
-      if (a.source != kOrthoGiven) F32::load8(mh, e, n, m);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const double v = (double)source_value(a.c, a.source, gv[k], m[k]);
-        sum = fma(v, v, sum);
-      }
+      float gv[8], m[8], v[8];
+      load_source<GT>(a.c, a.source, g, mh, e, n, gv, m, v);
+      sum = add_squares(v, sum);
     }
   __shared__ double parts[4];
   sum = wave_sum(sum);
@@ -122,23 +108,11 @@ __global__ __launch_bounds__(256) void k_ortho_begin(OrthoBeginArgs<N> a) {
     float v[8] = {};
     if (c.r0 + r < c.rows && n) {
       const uint64_t e = u.t.first + (uint64_t)(c.r0 + r) * u.t.ld + c.c0 + k8;
-      float gv[8], m[8] = {};
-      GT::load8(g, e, n, gv);
-      if (a.source != kOrthoGiven) F32::load8(mh, e, n, m);
+      float gv[8], m[8];
+      load_source<GT>(a.c, a.source, g, mh, e, n, gv, m, v);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = source_value(a.c, a.source, gv[k], m[k]) * factor;
-      if (a.source != kOrthoGiven && a.phase != kUpdateOnly) {
-        float b[8] = {};
-        if (a.phase == kPlain || a.phase == kFold) F32::load8(acc, e, n, b);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          b[k] = a.phase == kPlain || a.phase == kFold ? fmaf(gv[k], a.c.inv_s, b[k]) : gv[k] * a.c.inv_s;
-          m[k] = fmaf(a.c.beta1, m[k], a.c.omb1 * b[k]);
-          if (a.phase == kFold) b[k] = 0.f;
-        }
-        if (a.phase == kFold || a.phase == kAlg1) F32::store8(mh, e, n, m);
-        if (a.phase != kAlg1) F32::store8(acc, e, n, b);
-      }
+      for (int k = 0; k < 8; ++k) v[k] *= factor;
+      if (a.source != kOrthoGiven) move_moment(a.c, a.phase, mh, acc, e, n, gv, m);
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) tile[r * kTurnPitch + k8 + k] = v[k];
