@@ -36,7 +36,8 @@
  *     frees or copies them and never synchronises a stream.  The library owns only metadata on host and
  *     device: the segment table, the CSR slots and, for layouts of many short tensors with at most seven
  *     elements between two of them, a byte of device memory for every four elements of one buffer, up
- *     to 64 MB (d of 2^28); for handles that call what is described under "Around the step", what that needs.  (One set-up call is the exception and says so: dadam_place_by_timing
+ *     to 64 MB (d of 2^28); for handles that call what is described under "Around the step", what that needs, and the tables of
+ *     dadam_set_matrices.  (One set-up call is the exception and says so: dadam_place_by_timing
  *     overwrites the empty arena it is given and returns when its measurements are done.)
  *   - Launching entry points enqueue work on the given HIP stream (a hipStream_t passed as
  *     void*; NULL = the default stream) and return at once.  The caller keeps every buffer alive
@@ -502,8 +503,9 @@ int dadam_mx4_round(dadam_handle* h, uint32_t slot, const void* const* x_src, vo
  *
  * These calls take a workspace: DEVICE memory, caller-owned, 256-byte aligned, that a call may overwrite throughout and that holds nothing between
  * calls.  Calls that may overlap in time need one each, and so do graphs that are replayed side by side.  The calls themselves allocate nothing, and may be
- * recorded into a graph.  With less workspace than `bytes` of the information calls (but `least_bytes`) they go in more, smaller launches, with the same
- * results up to the order of sums.  What a call writes must not overlap anything else that it reads or writes, but where "in place" is named.
+ * recorded into a graph.  With less workspace than `bytes` of the information calls (but `least_bytes`) they go in more, smaller launches: orthogonalised matrices
+ * are the same bits then, losses and their gradients differ within what is said below.  Every call on the same inputs and as much workspace gives the same bits.
+ * What a call writes must not overlap anything else that it reads or writes, but where "in place" is named.
  * Errors of all: DADAM_EINVAL (null, value out of range, workspace too small), DADAM_EALIGN, DADAM_EALIAS, DADAM_ESTATE, DADAM_EHIP. */
 
 /* The output matrix of a language model: tensor `tensor` of the layout, vocab rows (one a word) of width elements, and the words' bias, a tensor of vocab
@@ -515,13 +517,13 @@ typedef struct {
 } dadam_head;
 
 typedef struct {
-  uint64_t least_bytes; /* the workspace without which a call is refused: one replica at a time, 128 words at a time */
+  uint64_t least_bytes; /* the workspace without which a call is refused: one replica and 128 words at a time */
   uint64_t bytes;       /* what a call makes good use of */
 } dadam_head_info;
 /* The workspace of dadam_head_loss for n_tokens tokens a row, with (gradient != 0) or without gradients. */
 int dadam_head_get_info(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, uint32_t gradient, dadam_head_info* out);
 
-/* Softmax cross entropy of every row's hidden vectors against its own head, in pieces of the vocabulary, without keeping the logits: with W and bias in
+/* Softmax cross entropy of every row's hidden vectors against its own head: with W and bias in
  * params[i], h_t the t-th of hidden[i]'s n_tokens vectors of width elements, y_t = targets[i][t]
  *     z = W h_t + bias;    nll[i][t] = log sum_v exp z[v] - z[y_t];    losses[i] = s * sum_t nll[i][t]
  *     dz_t = s (softmax z - e[y_t]);    dhidden[i][t] = W^T dz_t;    in grads[i]: dW = sum_t dz_t h_t^T, dbias = sum_t dz_t
@@ -531,9 +533,12 @@ int dadam_head_get_info(const dadam_handle* h, const dadam_head* head, uint32_t 
  * params: n_rows packed vectors of param_dtype; hidden and dhidden: n_rows times n_tokens x width of param_dtype; targets: int32; losses (n_rows, DEVICE) and nll: float32;
  * grads: n_rows packed vectors of grad_dtype.  nll, dhidden and grads may be null; without the last two only the loss is formed.  Of all these only params and grads
  * have to be 16-byte aligned, the others by their elements.  n_tokens is 0 to 2^20.
- * Sums are float32 (the loss 64 bits).  With bfloat16 parameters and gradients softmax - e[y] is rounded to bfloat16 before the gradients' products; otherwise
- * operands have 22 bits, or 2^-39 of the largest magnitude of the head, of the hidden vectors or (softmax) of 1.  An infinity or NaN in W, or in a hidden vector that
- * takes part, makes its replica's loss and gradients NaN; a bias of minus infinity takes its word out. */
+ * The logits are kept for up to 64 tokens (4 bytes each).  Of more tokens only softmax is, 2 bytes a logit with bfloat16 parameters and gradients and 4 otherwise, and
+ * only where a replica's is at most 2 GiB and the workspace has room for it; elsewhere they are formed twice, a piece of the vocabulary at a time.
+ * Sums are float32 (the loss 64 bits).  With bfloat16 parameters and gradients softmax - e[y] is rounded to bfloat16 before the gradients' products (where it is kept, to half
+ * precision before that: 2^-11 of itself or 2^-40 of the largest of its 64 or 128 words); otherwise operands have 22 bits, or 2^-39 of the largest magnitude of the head,
+ * of the hidden vectors or (softmax) of 1.  An infinity or NaN in W, or in a hidden vector that takes part, leaves its own replica's loss and gradients without
+ * meaning, and no other's; a bias of minus infinity takes its word out. */
 #define DADAM_HEAD_MEAN 1u
 #define DADAM_HEAD_ADD 2u
 int dadam_head_loss(dadam_handle* h, const dadam_head* head, const void* const* params, const void* const* hidden,
@@ -553,7 +558,7 @@ typedef struct {
 } dadam_matrix_desc;
 
 /* Register the matrices that the two calls below are about, in place of those registered before; n may be 0.  matrices[n] is a HOST array and is
- * copied.  Allocates and uploads 64 bytes a matrix and about 8 bytes for every 128 x 128 elements, and may wait for the device: not for use under stream capture, and
+ * copied.  Allocates and uploads 160 bytes a matrix and up to 16 bytes for every 128 x 128 elements, and may wait for the device: not for use under stream capture, and
  * only while no launched work still uses the old ones. */
 int dadam_set_matrices(dadam_handle* h, const dadam_matrix_desc* matrices, uint32_t n);
 
@@ -564,7 +569,8 @@ int dadam_set_ortho_schedule(dadam_handle* h, uint32_t n_steps, const float* coe
 
 typedef struct {
   uint32_t n_matrices, reserved;
-  uint64_t least_bytes; /* the workspace without which a call is refused: that of one replica's largest matrix */
+  uint64_t least_bytes; /* the workspace without which a call is refused: that of one replica's largest matrix; 0 where every
+                           matrix fits a compute unit (for instance 128 x 160 or 64 x 544 at most), and workspace may be null */
   uint64_t bytes;       /* what a call makes good use of */
 } dadam_ortho_info;
 int dadam_ortho_get_info(const dadam_handle* h, dadam_ortho_info* out);

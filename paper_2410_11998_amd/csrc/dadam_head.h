@@ -9,7 +9,6 @@
 namespace dadam {
 
 constexpr int kHeadRows = 32;         // replicas of a launch
-constexpr uint32_t kHeadSplits = 16;  // most parts that the sum over words of a hidden vector's gradient goes in
 
 struct HeadRow {  // device addresses, 0 where there is none
   uint64_t head, bias, hidden, target, nll, dhidden, dhead, dbias;

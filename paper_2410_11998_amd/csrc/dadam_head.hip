@@ -3,11 +3,11 @@
 //
 // Two ways.  Where the workspace has room for 2 (or two planes: 4) bytes for every logit, the product of the logits stores the exponentials of each slice of
 // words against the slice's largest logit, and k_head_scale makes softmax - e[target] of them in place once the sums are known: three products of tokens x
-// vocabulary x width.  Elsewhere nothing of the logits leaves the chip but a piece of the vocabulary at a time.  A first product gives every token the largest logit and the sum of exponentials of some words
-// (k_head_logits), from which k_head_losses makes the logarithm of the sum; a second one recomputes the logits a piece of the vocabulary at a time
-// and stores softmax - e[target] of it, the operand of the two gradient products.  dW of a piece is complete; dh adds up over pieces.  Four products.
-// All operands
-// lie as they are made: the gradients sum over tokens and over words, so their tiles are turned on the way from LDS to the registers.
+// vocabulary x width.  Elsewhere nothing of the logits leaves the chip but a piece of the vocabulary at a time.  A first product gives every token the largest
+// logit and the sum of exponentials of some words (k_head_logits), from which k_head_losses makes the logarithm of the sum; a second one recomputes the logits
+// a piece of the vocabulary at a time and stores softmax - e[target] of it, the operand of the two gradient products.  dW of a piece is complete; dh adds up over
+// pieces.  Four products.  (Up to 64 tokens: dadam_head_few.hip.)
+// All operands lie as they are made: the gradients sum over tokens and over words, so their tiles are turned on the way from LDS to the registers.
 //
 // bfloat16 parameters and gradients: the operands are what is given, softmax - e[target] is rounded to bfloat16, 8 bits relative whatever its size;
 // sums are float32.  Otherwise: two halves an element (dadam_mfma.h), times a power of two by the largest magnitude of the head and of the
