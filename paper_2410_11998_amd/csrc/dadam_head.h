@@ -17,7 +17,7 @@ struct HeadRow {  // device addresses, 0 where there is none
 // Workspace of a replica.  Operands have `planes` halves or bfloat16s an element: hidden vectors and a piece of the head by rows of D, softmax - e[target] of a
 // piece by rows of its words, a token each.
 struct HeadPlaces {
-  uint64_t words, lse, hit, stats, hidden, head, p, sums, bytes;
+  uint64_t words, top, hit, stats, hidden, head, p, sums, bytes;
 };
 struct HeadShape {
   uint32_t tokens, vocab, width;
@@ -36,7 +36,7 @@ inline constexpr HeadPlaces head_places(const HeadShape& s, uint64_t planes, boo
     return here;
   };
   w.words = take(64);
-  w.lse = take((uint64_t)s.T * 4);
+  w.top = take((uint64_t)s.T * 8);  // a token's largest logit and 1 / its sum of exponentials
   w.hit = take((uint64_t)s.T * 4);
   w.stats = take((uint64_t)s.slices * s.T * 8);
   w.hidden = take((uint64_t)s.T * s.D * b);
@@ -70,7 +70,7 @@ static_assert(sizeof(HeadArgs) <= 4096, "the argument block of a launch holds 4 
 // The way of few tokens (dadam_head_few.hip): the head is read as it lies, 32 words at a time.
 constexpr uint32_t kFewTokens = 64, kFewWords = 32, kFewColumns = 128;
 struct FewPlaces {
-  uint64_t words, lse, hit, stats, z, p, p_turned, hidden, sums, bytes;
+  uint64_t words, top, hit, stats, z, p, p_turned, hidden, sums, bytes;
 };
 struct FewShape {
   uint32_t tokens, vocab, width;
@@ -87,7 +87,7 @@ inline constexpr FewPlaces few_places(const FewShape& s, uint64_t planes, bool g
     return here;
   };
   w.words = take(64);
-  w.lse = take((uint64_t)s.T * 4);
+  w.top = take((uint64_t)s.T * 8);
   w.hit = take((uint64_t)s.T * 4);
   w.stats = take((uint64_t)s.blocks * s.T * 8);
   w.z = take((uint64_t)s.blocks * s.T * kFewWords * 4);  // of a block: T rows of kFewWords logits, with two planes softmax - e[target] in their place

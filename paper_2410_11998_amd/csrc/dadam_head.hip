@@ -220,20 +220,19 @@ __global__ __launch_bounds__(2 * EDGE) void k_head_logits(HeadArgs a) {
   if constexpr (MODE == kHeadGradient) {
     struct Token {
       int32_t target;  // -1: none
-      float lse;
+      float2v top;
     };
     t.hand_out(lds, false,
                [&](uint32_t, uint32_t n) {
                  Token x;
                  if (!has_target(a, row.target, j * T::kN + n, x.target)) x.target = -1;
-                 x.lse = global<const float>(base + a.w.lse)[j * T::kN + n];
+                 x.top = global<const float2v>(base + a.w.top)[j * T::kN + n];
                  return x;
                },
                [&](uint32_t m, uint32_t n, float (&v)[8], const Token& x) {
                  m += i * T::kM;
                  n += j * T::kN;
                  const bool taken = x.target >= 0;
-                 const float lse = x.lse;
                  const uint32_t words = left(a.words, m);
                  float bias[8] = {};
                  if (row.bias && words) XT::load8(row.bias, a.first_word + m, words, bias);
@@ -241,9 +240,9 @@ __global__ __launch_bounds__(2 * EDGE) void k_head_logits(HeadArgs a) {
                  uint32_t w[8];
 #pragma unroll
                  for (uint32_t k = 0; k < 8; ++k) {
-                   const float z = fmaf(v[k], held, bias[k]) - lse;
-                   float p = taken && k < words ? __expf(z) : 0.f;
-                   if (taken && k == hit) p = expm1f(z);
+                   const float z = fmaf(v[k], held, bias[k]) - x.top[0];
+                   float p = taken && k < words ? exponential<TY::planes == 2>(z) * x.top[1] : 0.f;
+                   if (taken && k == hit) p = expm1f(-global<const float>(base + a.w.hit)[n]);
                    w[k] = operand_word<OP, TY::planes>(TY::planes == 1 ? p : p * (float)(1 << kHeldAt));
                  }
                  store8<TY::planes>(base + a.w.p, n, a.s.piece, m, w);
@@ -288,7 +287,7 @@ __global__ __launch_bounds__(2 * EDGE) void k_head_logits(HeadArgs a) {
       for (int im = 0; im < MT; ++im)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float e = __expf(t.acc[im][jn][r] - from);
+          const float e = exponential<TY::planes == 2>(t.acc[im][jn][r] - from);
           sum += e;
           t.acc[im][jn][r] = e;
         }
@@ -321,8 +320,9 @@ __global__ __launch_bounds__(256) void k_head_scale(HeadArgs a) {
   int32_t target;
   uint32_t w[8] = {};
   if (has_target(a, row.target, n, target)) {
-    const float lse = global<const float>(base + a.w.lse)[n], most = global<const float2v>(base + a.w.stats)[(uint64_t)(m / (a.s.edge / 2)) * a.s.T + n][0];
-    const float factor = __expf(most - lse) * (TY::planes == 1 ? 1.f / kept_times<TY>() : 1.f);
+    const float2v top = global<const float2v>(base + a.w.top)[n];
+    const float most = global<const float2v>(base + a.w.stats)[(uint64_t)(m / (a.s.edge / 2)) * a.s.T + n][0];
+    const float factor = exponential<TY::planes == 2>(most - top[0]) * top[1] * (TY::planes == 1 ? 1.f / kept_times<TY>() : 1.f);
     const Eight e = load8<TY::planes>(base + a.w.p, n, a.s.piece, m);
     const uint32_t hit = (uint32_t)target - m;
 #pragma unroll
@@ -354,7 +354,7 @@ __global__ __launch_bounds__(256) void k_head_losses(HeadArgs a) {
 #pragma unroll 4
   for (uint32_t s = part; s < a.s.slices; s += 16) {
     const float2v v = stats[(uint64_t)s * a.s.T];
-    sum += v[0] == -INFINITY ? v[1] : v[1] * __expf(v[0] - most);
+    sum += v[0] == -INFINITY ? v[1] : v[1] * exponential<true>(v[0] - most);
   }
   parts[part][at] = sum;
   __syncthreads();
@@ -364,9 +364,8 @@ __global__ __launch_bounds__(256) void k_head_losses(HeadArgs a) {
     for (int k = 0; k < 16; ++k) sum += parts[k][at];
     int32_t target;
     const bool taken = has_target(a, row.target, n, target);
-    const float lse = most + logf(sum);
-    global<float>(base + a.w.lse)[n] = lse;
-    const float nll = taken ? lse - global<const float>(base + a.w.hit)[n] : 0.f;
+    global<float2v>(base + a.w.top)[n] = float2v{most, 1.f / sum};
+    const float nll = taken ? logf(sum) + (most - global<const float>(base + a.w.hit)[n]) : 0.f;
     if (n < a.s.tokens && row.nll) global<float>(row.nll)[n] = nll;
     global<float>(base + a.w.hit)[n] = nll;
   }

@@ -161,6 +161,16 @@ struct B16 {
   }
 };
 
+// e^x for x <= 0 (or NaN), with CLOSE to about two places of float32: the instruction's 2^y of y = x log2(e) in two parts, y = high + low, 2^low = 1 + low ln 2.  Without, the
+// rounding of y makes it |x| 2^-24 of the value.
+template <bool CLOSE>
+__device__ __forceinline__ float exponential(float x) {
+  if constexpr (!CLOSE) return __expf(x);
+  x = x < -200.f ? -200.f : x;  // (0 as well, and no infinity less an infinity)
+  const float high = x * 1.44269502f, low = fmaf(x, 1.44269502f, -high) + x * 1.92596299e-8f, e = __builtin_amdgcn_exp2f(high);
+  return fmaf(e, low * 0.693147181f, e);
+}
+
 // Where a tile's side of an operand begins (at the first stage), its rows' distance in bytes (a stage's rows within 2^32 of each other), and how many of
 // them there are: beyond, the last one is taken again.
 struct Operand {

@@ -26,9 +26,9 @@ struct OrthoTask {
 };
 
 // Workspace of a matrix, one replica: X twice (an iteration reads one and writes the other), with one plane what the half leaves of it (see dadam_ortho.hip),
-// A = X X^T, B = b A + c A A, partial sums of the norm, the ranges' parts of X X^T.
+// A = X X^T, B = b A + c A A without its diagonal, which lies apart in 32 bits, partial sums of the norm, the ranges' parts of X X^T.
 struct OrthoPlaces {
-  uint64_t x[2], low, a, b, sums, parts, bytes;
+  uint64_t x[2], low, a, b, diagonal, sums, parts, bytes;
 };
 inline constexpr OrthoPlaces ortho_places(uint64_t P, uint64_t Q, uint64_t planes, uint64_t parts) {
   OrthoPlaces w{};
@@ -38,6 +38,7 @@ inline constexpr OrthoPlaces ortho_places(uint64_t P, uint64_t Q, uint64_t plane
   w.low = at, at += planes == 1 ? P * Q * 2 : 0;
   w.a = at, at += P * P * 2 * planes;
   w.b = at, at += P * P * 2 * planes;
+  w.diagonal = at, at += P * 4;  // (P is a multiple of 128)
   w.sums = at, at += ((P / kOrthoCell) * (Q / kOrthoCell) * 8 + 255) / 256 * 256;
   w.parts = at, at += parts * P * P * 4;
   w.bytes = at;
@@ -93,7 +94,7 @@ struct OrthoEndArgs {
 constexpr uint32_t kLoneEdge = 32, kLoneThreads = 512, kMostLoneLds = 160 * 1024 - 256;
 constexpr int kLoneRows = 64;
 inline constexpr uint64_t lone_lds_bytes(uint64_t P, uint64_t Q) {
-  return P > 4 * kLoneEdge ? ~0ull : (P * (Q + 4) + P * (P + 4) + (P <= 2 * kLoneEdge ? 8192 : 0)) * 4;
+  return P > 4 * kLoneEdge ? ~0ull : (P * (Q + 4) + P * (P + 4) + P + (P <= 2 * kLoneEdge ? 8192 : 0)) * 4;
 }
 // What is stored of a product, and of the term held already.
 struct LoneStep {

@@ -9,7 +9,9 @@
 // 32 bits have two halves an element (dadam_mfma.h): the error of five iterations is 2e-7 to 3e-6 of the result, by how fast the singular values
 // fall.  For bfloat16 results one half is enough in the products, but not for X itself: what X loses to 11 bits in the directions of small singular
 // values grows by a = 3.4 an iteration, 1e-3 of the result for equal singular values, 1.4e-2 for ones that fall by 1000 in 50.  a X is therefore taken
-// from two halves as well (1.4e-3 and 5e-4), the second of which no product reads.
+// from two halves as well (1.4e-3 and 5e-4), the second of which no product reads.  B's diagonal is most of it where q is much larger than p (A is near I / p), so it does not go
+// through the product either, but into a X's factor, a row's own: the error of a random 150 x 1189 is 5.8e-4 instead of 1.6e-3, of 12 x 5948 7.1e-4 instead of 3.2e-3,
+// of 1024 x 1024 7.4e-4 instead of 1.3e-3 (modelled; what bfloat16 itself costs is 1.7e-3).
 #include "dadam_mfma.h"
 #include "dadam_ortho.h"
 #include "dadam_ortho_source.h"
@@ -161,10 +163,18 @@ __global__ __launch_bounds__(2 * EDGE) void k_ortho_gram(OrthoStepArgs a) {
              },
              [&](uint32_t m, uint32_t n, float (&v)[8], const auto& held) {
                uint32_t words[8];
+               const uint32_t on_diagonal = j * T::kN + n - (i * T::kM + m);
 #pragma unroll
                for (int k = 0; k < 8; ++k) {
-                 if constexpr (SQUARE) v[k] = fmaf(value_of<Half, PLANES == 2>(held, k), a.gain, v[k] * a.fresh);
-                 else v[k] *= a.fresh;
+                 if constexpr (SQUARE) {
+                   v[k] = fmaf(value_of<Half, PLANES == 2>(held, k), a.gain, v[k] * a.fresh);
+                   if (on_diagonal == (uint32_t)k) {
+                     global<float>(u.base + w.diagonal)[j * T::kN + n] = v[k];
+                     v[k] = 0.f;
+                   }
+                 } else {
+                   v[k] *= a.fresh;
+                 }
                  words[k] = operand_word<Half, PLANES>(v[k]);
                  v[k] = __uint_as_float(words[k]);
                }
@@ -220,12 +230,16 @@ __global__ __launch_bounds__(256) void k_ortho_join(OrthoStepArgs a) {
   }
 }
 
-// X of eight elements, highs and lows.
+// X of eight elements of a row, highs and lows, and what B's diagonal has there.
+struct RowOfX {
+  Eight x;
+  float diagonal;
+};
 template <int PLANES>
-__device__ __forceinline__ Eight load_x(uint64_t base, const OrthoPlaces& w, uint32_t which, const OrthoTask& t, uint32_t p, uint32_t q) {
-  Eight x = load8<PLANES>(base + x_at(w, which), p, t.Q, q);
-  if constexpr (PLANES == 1) x.low = global<const uint4v>(base + w.low + ((uint64_t)p * t.Q + q) * 2)[0];
-  return x;
+__device__ __forceinline__ RowOfX load_x(uint64_t base, const OrthoPlaces& w, uint32_t which, const OrthoTask& t, uint32_t p, uint32_t q) {
+  RowOfX r = {load8<PLANES>(base + x_at(w, which), p, t.Q, q), global<const float>(base + w.diagonal)[p]};
+  if constexpr (PLANES == 1) r.x.low = global<const uint4v>(base + w.low + ((uint64_t)p * t.Q + q) * 2)[0];
+  return r;
 }
 
 // The product of a tile of a X + B X, transposed: columns q of X against rows p of B (its own).
@@ -250,10 +264,11 @@ __global__ __launch_bounds__(2 * EDGE) void k_ortho_next(OrthoStepArgs a) {
   T t;
   next_product<T, PLANES>(t, u, w, a.from, q0, p0, lds);
   t.hand_out(lds, false, [&](uint32_t m, uint32_t n) { return load_x<PLANES>(u.base, w, a.from, u.t, p0 + n, q0 + m); },
-             [&](uint32_t m, uint32_t n, float (&v)[8], const Eight& x) {
+             [&](uint32_t m, uint32_t n, float (&v)[8], const RowOfX& row) {
                uint32_t words[8];
+               const float gain = fmaf(row.diagonal, a.fresh, a.gain);
 #pragma unroll
-               for (int k = 0; k < 8; ++k) words[k] = halves<Half>(fmaf(value_of<Half, true>(x, k), a.gain, v[k] * a.fresh));
+               for (int k = 0; k < 8; ++k) words[k] = halves<Half>(fmaf(value_of<Half, true>(row.x, k), gain, v[k] * a.fresh));
                store8<PLANES>(u.base + x_at(w, a.to), p0 + n, u.t.Q, q0 + m, words);
                if constexpr (PLANES == 1) global<uint4v>(u.base + w.low + ((uint64_t)(p0 + n) * u.t.Q + q0 + m) * 2)[0] = highs(words);
              },
@@ -328,9 +343,10 @@ __global__ __launch_bounds__(2 * EDGE) void k_ortho_end(OrthoEndArgs<N> a) {
     DT::store8(out, e, n, mixed);
   };
   t.hand_out(lds, u.t.tall, [&](uint32_t m, uint32_t n) { return load_x<PLANES>(u.base, w, a.from, u.t, p0 + n, q0 + m); },
-             [&](uint32_t m, uint32_t n, float (&v)[8], const Eight& x) {
+             [&](uint32_t m, uint32_t n, float (&v)[8], const RowOfX& row) {
+               const float gain = fmaf(row.diagonal, a.fresh, a.gain);
 #pragma unroll
-               for (int k = 0; k < 8; ++k) v[k] = fmaf(value_of<Half, true>(x, k), a.gain, v[k] * a.fresh);
+               for (int k = 0; k < 8; ++k) v[k] = fmaf(value_of<Half, true>(row.x, k), gain, v[k] * a.fresh);
                if (!u.t.tall) finish(p0 + n, q0 + m, v);
              },
              [&](uint32_t m, uint32_t n, const float (&v)[8]) { finish(q0 + m, p0 + n, v); });

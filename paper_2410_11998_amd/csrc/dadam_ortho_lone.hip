@@ -1,7 +1,7 @@
 // Orthogonalised updates of matrices that fit a compute unit: a workgroup holds one in LDS from the gradient to the parameters, in one launch where the tiles of
 // dadam_ortho.hip take three an iteration, whose beginnings and ends are all that such matrices' time goes into.
 //
-// X (its short side's rows) and A = X X^T lie in LDS as words of two halves, 22 bits, whatever the result's type.  Rows are filled up to multiples of 32 and have four
+// X (its short side's rows), A = X X^T and B without its diagonal (see dadam_ortho.hip) lie in LDS as words of two halves, 22 bits, whatever the result's type.  Rows are filled up to multiples of 32 and have four
 // more words, so that eight rows' pieces of 16 bytes meet no bank twice.  A and B = b A + c A A by blocks of the lower half, a wavefront each; X X^T of one or three
 // blocks by ranges of columns, joined in their order.  Columns of a X + B X depend on the same columns of X only: a wavefront has all rows of 32, and writes them where
 // they were.
@@ -68,7 +68,7 @@ __device__ __forceinline__ void block_of(uint32_t n, uint32_t& i, uint32_t& j) {
 
 // An iteration of a matrix of NB blocks of rows; the last leaves float32 values.
 template <int NB>
-__device__ __forceinline__ void iterate(Words x, Words a, Words parts, uint32_t P, uint32_t Q, const LoneStep& s, bool last) {
+__device__ __forceinline__ void iterate(Words x, Words a, Words diagonal, Words parts, uint32_t P, uint32_t Q, const LoneStep& s, bool last) {
   constexpr uint32_t kBlocks = NB * (NB + 1) / 2, kParts = NB == 1 ? 8 : NB == 2 ? 2 : 1, kEach = (kBlocks + kWaves - 1) / kWaves;
   const int lane = threadIdx.x & 63;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), xp = Q + 4, ap = P + 4, column = lane & 31;
@@ -114,7 +114,12 @@ __device__ __forceinline__ void iterate(Words x, Words a, Words parts, uint32_t 
     block_of(item, i, j);
     const float16v acc = block_product(a, ap, i, j, 0, P / 16, lane);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) words[n][r] = halves<Half>(fmaf(value(a[(i * 32 + row_of(r, lane)) * ap + j * 32 + column]), s.b_gain, acc[r] * s.b_fresh));
+    for (int r = 0; r < 16; ++r) {
+      const uint32_t m = i * 32 + row_of(r, lane), c = j * 32 + column;
+      const float v = fmaf(value(a[m * ap + c]), s.b_gain, acc[r] * s.b_fresh);
+      if (m == c) diagonal[m] = __float_as_uint(v);
+      words[n][r] = m == c ? 0 : halves<Half>(v);
+    }
   }
   __syncthreads();
 #pragma unroll
@@ -146,8 +151,9 @@ __device__ __forceinline__ void iterate(Words x, Words a, Words parts, uint32_t 
     for (int i = 0; i < NB; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const Words w = x + (i * 32 + row_of(r, lane)) * xp + q * 32 + column;
-        const float v = fmaf(value(*w), s.x_gain, acc[i][r] * s.x_fresh);
+        const uint32_t m = i * 32 + row_of(r, lane);
+        const Words w = x + m * xp + q * 32 + column;
+        const float v = fmaf(value(*w), fmaf(__uint_as_float(diagonal[m]), s.x_fresh, s.x_gain), acc[i][r] * s.x_fresh);
         *w = last ? __float_as_uint(v) : halves<Half>(v);
       }
   }
@@ -164,7 +170,7 @@ __global__ __launch_bounds__(kLoneThreads) void k_ortho_lone(OrthoLoneArgs<N, C>
   for (uint32_t i = 0; i < sizeof(OrthoTask) / 4; ++i) task_words.w[i] = global<const uint32_t>(task)[i];
   const OrthoTask t = __builtin_bit_cast(OrthoTask, task_words);
   const uint32_t replica = blockIdx.y, rows = t.tall ? t.q : t.p, cols = t.tall ? t.p : t.q, pieces = (cols + 7) / 8, xp = t.Q + 4;
-  const Words x = (Words)lone_lds, A = x + t.P * xp, parts = A + t.P * (t.P + 4);
+  const Words x = (Words)lone_lds, A = x + t.P * xp, diagonal = A + t.P * (t.P + 4), parts = diagonal + t.P;
   const uint64_t g = (uint64_t)a.grad[replica], mh = (uint64_t)a.m_hat[replica], b = (uint64_t)a.acc[replica];
   for (uint32_t k = threadIdx.x; k < t.P * xp; k += kLoneThreads) x[k] = 0;
   __syncthreads();
@@ -195,10 +201,10 @@ __global__ __launch_bounds__(kLoneThreads) void k_ortho_lone(OrthoLoneArgs<N, C>
   for (uint32_t k = 0; k < a.n_steps; ++k) {
     const bool last = k + 1 == a.n_steps;
     switch (t.P / 32) {
-      case 1: iterate<1>(x, A, parts, t.P, t.Q, a.step[k], last); break;
-      case 2: iterate<2>(x, A, parts, t.P, t.Q, a.step[k], last); break;
-      case 3: iterate<3>(x, A, parts, t.P, t.Q, a.step[k], last); break;
-      default: iterate<4>(x, A, parts, t.P, t.Q, a.step[k], last); break;
+      case 1: iterate<1>(x, A, diagonal, parts, t.P, t.Q, a.step[k], last); break;
+      case 2: iterate<2>(x, A, diagonal, parts, t.P, t.Q, a.step[k], last); break;
+      case 3: iterate<3>(x, A, diagonal, parts, t.P, t.Q, a.step[k], last); break;
+      default: iterate<4>(x, A, diagonal, parts, t.P, t.Q, a.step[k], last); break;
     }
   }
   const uint64_t out = (uint64_t)a.out[replica];
