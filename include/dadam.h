@@ -570,7 +570,7 @@ int dadam_set_ortho_schedule(dadam_handle* h, uint32_t n_steps, const float* coe
 typedef struct {
   uint32_t n_matrices, reserved;
   uint64_t least_bytes; /* the workspace without which a call is refused: that of one replica's largest matrix; 0 where every
-                           matrix fits a compute unit (for instance 128 x 160 or 64 x 544 at most), and workspace may be null */
+                           matrix fits a compute unit (for instance 128 x 160 or 64 x 416 at most), and workspace may be null */
   uint64_t bytes;       /* what a call makes good use of */
 } dadam_ortho_info;
 int dadam_ortho_get_info(const dadam_handle* h, dadam_ortho_info* out);

@@ -58,6 +58,7 @@ void fill_shape(const dadam_head* head, uint32_t n_tokens, uint32_t planes, uint
   s->piece = std::min(piece, filled(head->vocab, edge));
   s->slices = filled(head->vocab, edge) / (edge / 2);
   s->keeps = 0;
+  s->parts = 1;
   const uint64_t tiles = (uint64_t)(s->T / edge) * (s->D / edge), stages = (uint64_t)s->piece * planes / 64;
   s->splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(std::min<uint64_t>((at_once(edge) + tiles - 1) / tiles, stages / 8), kSplits));
 }
@@ -78,6 +79,12 @@ Way good_way(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, b
   // Replicas together, so that the last workgroups of a launch have company: tiles of one replica's head are 3.1 times what the chip holds (4 x 4096 tokens, 50257
   // words, width 1024), of four 12.3 times.
   fill_shape(head, n_tokens, planes, edge, (uint32_t)piece, &w.s);
+  if (gradient && edge == 128) {
+    // The head's gradient where its tiles are less than half of what there are compute units, and sum over 32 stages of tokens and more: in parts of eight and more (8824
+    // tokens, 3387 words, width 108: 85 us in one, 25 in parts with their sum; 3053 tokens, 4 words, two replicas 69 / 14).
+    const uint64_t tiles = R * all / 128 * across, stages = (uint64_t)w.s.T * planes / 64;
+    if (2 * tiles <= 256 && stages >= 32) w.s.parts = (uint32_t)std::min<uint64_t>({256 / tiles, stages / 8, kSplits});
+  }
   w.rows = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(R, kMostAtOnce / head_places(w.s, planes, gradient).bytes));
   w.s.keeps = keeps;
   w.each = head_places(w.s, planes, gradient).bytes;
@@ -119,8 +126,9 @@ Way way_for(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, bo
   return w;
 }
 
-// Few tokens: a wavefront sums a hidden vector's gradient over four blocks of words, or more where there are more than kFewItems of those.
-constexpr uint64_t kFewItems = 4096;
+// Few tokens: a wavefront sums a hidden vector's gradient over four blocks of words, or more where there are more than kFewItems of those, or as many as make the sums half
+// of what is read of the head (57 tokens, 94661 words, width 512, five replicas: 799 / 654 us) if that leaves the chip kFewLeast.
+constexpr uint64_t kFewItems = 4096, kFewLeast = 2048;
 struct Few {
   FewShape s;
   uint32_t rows;
@@ -134,10 +142,12 @@ Few few_way(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, bo
   f.s.T = filled(n_tokens, 32);
   f.s.D = filled(head->width, kFewColumns);
   f.s.blocks = (head->vocab + kFewWords - 1) / kFewWords;
-  f.s.each = (uint32_t)std::max<uint64_t>(4, ((uint64_t)f.s.blocks * (f.s.D / kFewColumns) + kFewItems - 1) / kFewItems);
+  const uint64_t rows = std::min<uint32_t>(h->cfg.n_rows, kHeadRows);
+  const uint64_t items = (uint64_t)f.s.blocks * (f.s.D / kFewColumns), by_tokens = n_tokens / (2 * dtype_bytes(h->cfg.param_dtype));
+  f.s.each = (uint32_t)std::max<uint64_t>({4, (items + kFewItems - 1) / kFewItems, std::min(by_tokens, rows * items / kFewLeast)});
   f.s.ranges = (f.s.blocks + f.s.each - 1) / f.s.each;
   f.each = few_places(f.s, planes_of(h), gradient).bytes;
-  f.rows = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(std::min<uint32_t>(h->cfg.n_rows, kHeadRows), kMostAtOnce / f.each));
+  f.rows = (uint32_t)std::max<uint64_t>(1, std::min(rows, kMostAtOnce / f.each));
   return f;
 }
 bool are_few(uint32_t n_tokens) { return n_tokens >= 1 && n_tokens <= kFewTokens; }
@@ -157,6 +167,7 @@ int run_few(const dadam_handle* h, const FewArgs& a, bool dhidden, bool gradient
 int run_dhead(int x, int g, HeadArgs a, uint32_t rows, void* stream) {
   const uint32_t down = (a.words + a.s.edge - 1) / a.s.edge, tiles_of_word = a.s.D / a.s.edge * rows, tiles = down * tiles_of_word, over = tiles % at_once(a.s.edge);
   const uint32_t all = a.words;
+  if (a.s.parts > 1) return launch_head_dhead_parts(x, g, a, rows, stream);
   if (a.s.edge == 256 && tiles > at_once(256) && over && over <= at_once(256) / 4) {
     const uint32_t first = (tiles - over) / tiles_of_word * 256;
     a.words = first;

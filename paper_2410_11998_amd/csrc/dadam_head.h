@@ -17,7 +17,7 @@ struct HeadRow {  // device addresses, 0 where there is none
 // Workspace of a replica.  Operands have `planes` halves or bfloat16s an element: hidden vectors and a piece of the head by rows of D, softmax - e[target] of a
 // piece by rows of its words, a token each.
 struct HeadPlaces {
-  uint64_t words, top, hit, stats, hidden, head, p, sums, bytes;
+  uint64_t words, top, hit, stats, hidden, head, p, sums, parts, bytes;
 };
 struct HeadShape {
   uint32_t tokens, vocab, width;
@@ -25,6 +25,7 @@ struct HeadShape {
   uint32_t T, D, K;        // tokens and width filled up to the edge, width filled up to a stage
   uint32_t piece, slices;  // words of a piece (a multiple of the edge), slices of edge / 2 of all words
   uint32_t splits;         // parts that the sum over words of a hidden vector's gradient goes in
+  uint32_t parts;          // that the sum over tokens of the head's gradient goes in
   uint32_t keeps;          // softmax of all words is kept from the statistics on: one piece
 };
 inline constexpr HeadPlaces head_places(const HeadShape& s, uint64_t planes, bool gradient) {
@@ -44,6 +45,7 @@ inline constexpr HeadPlaces head_places(const HeadShape& s, uint64_t planes, boo
   if (gradient) {
     w.p = take((uint64_t)s.T * s.piece * b);
     w.sums = take((uint64_t)s.splits * s.T * s.D * 4);
+    if (s.parts > 1) w.parts = take((uint64_t)s.parts * s.piece * s.D * 4);
   }
   w.bytes = at;
   return w;
@@ -128,6 +130,8 @@ int launch_head_logits(int xdt, int gdt, HeadMode mode, const HeadArgs& a, uint3
 int launch_head_losses(const HeadArgs& a, uint32_t rows, void* stream);
 int launch_head_scale(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                   // the logits' gradient from what was kept
 int launch_head_dhead(int xdt, int gdt, uint32_t edge, const HeadArgs& a, uint32_t rows, void* stream);
+// The same by small tiles, in HeadShape::parts of the tokens, and their sum.
+int launch_head_dhead_parts(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);
 int launch_head_dbias(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);
 int launch_head_dhidden(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                 // a piece's part of the sums
 int launch_head_end(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                     // the hidden vectors' gradients from the sums

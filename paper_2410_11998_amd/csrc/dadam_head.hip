@@ -416,6 +416,45 @@ __global__ __launch_bounds__(2 * EDGE) void k_head_dhead(HeadArgs a) {
              [](uint32_t, uint32_t, const float (&)[8]) {});
 }
 
+// The same where there are so few tiles that the chip would wait for the tokens' sums: a part of the tokens (blockIdx.y), 32 bits, by rows of words.
+template <typename TY, int BUFFERS>
+__global__ __launch_bounds__(256) void k_head_dhead_part(HeadArgs a) {
+  using T = TileOf<typename TY::op, TY::planes, 128, BUFFERS, true, true>;
+  const uint64_t base = base_of(a), b = 2 * TY::planes;
+  const uint32_t across = a.s.D / T::kM, i = blockIdx.x % across, j = blockIdx.x / across, stages = a.s.T * TY::planes / 64;
+  const uint32_t from = (uint32_t)((uint64_t)stages * blockIdx.y / a.s.parts), to = (uint32_t)((uint64_t)stages * (blockIdx.y + 1) / a.s.parts);
+  const uint64_t token = (uint64_t)from * (64 / TY::planes), out = base + a.w.parts + (uint64_t)blockIdx.y * a.s.piece * a.s.D * 4;
+  char DADAM_LDS* lds = (char DADAM_LDS*)head_lds;
+  T t;
+  t.product(operand(base + a.w.hidden + (token * a.s.D + i * T::kM) * b, a.s.D * b), operand(base + a.w.p + (token * a.s.piece + j * T::kN) * b, a.s.piece * b), to - from, lds);
+  t.hand_out(lds, false, nothing_ahead,
+             [&](uint32_t m, uint32_t n, float (&v)[8], Nothing) { F32::store8(out, (uint64_t)(j * T::kN + n) * a.s.D + i * T::kM + m, 8, v); },
+             [](uint32_t, uint32_t, const float (&)[8]) {});
+}
+
+// dW from its parts, in their order: eight columns of a word a thread.
+template <typename GT, typename TY>
+__global__ __launch_bounds__(256) void k_head_join(HeadArgs a) {
+  const HeadRow& row = a.row[blockIdx.z];
+  const uint64_t base = base_of(a);
+  const uint32_t k = blockIdx.x * 256 + threadIdx.x, pieces = a.s.D / 8, n = k / pieces, m = k % pieces * 8, columns = n < a.words ? left(a.s.width, m) : 0;
+  if (columns == 0) return;
+  const uint64_t e = (uint64_t)(a.first_word + n) * a.s.width + m;
+  float v[8] = {}, held[8] = {};
+#pragma unroll 4
+  for (uint32_t q = 0; q < a.s.parts; ++q) {
+    float x[8];
+    F32::load8(base + a.w.parts, ((uint64_t)q * a.s.piece + n) * a.s.D + m, 8, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += x[i];
+  }
+  const float factor = factor_of(base, a) * (TY::planes == 1 ? 1.f : ldexpf(1.f, -power_of<TY>(base, a, kHeadMostHidden) - kHeldAt));
+  if (a.add) GT::load8(row.dhead, e, columns, held);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) held[i] = fmaf(v[i], factor, held[i]);
+  GT::store8(row.dhead, e, columns, held);
+}
+
 // dbias: 64 words a workgroup, 8 of them a thread; 32 threads share the tokens.
 template <typename GT, typename TY>
 __global__ __launch_bounds__(256) void k_head_dbias(HeadArgs a) {
@@ -571,6 +610,15 @@ int launch_head_dhead(int xdt, int gdt, uint32_t edge, const HeadArgs& a, uint32
     using T = TileOf<typename TY::op, TY::planes, decltype(edge_)::value, decltype(buffers)::value, true, true>;
     return launch<k_head_dhead<decltype(g), TY, decltype(edge_)::value, decltype(buffers)::value>>(grid, T::kThreads, T::kLds, stream, a);
   });
+}
+int launch_head_dhead_parts(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
+  const dim3 grid(upto(a.words, 128) * (a.s.D / 128), a.s.parts, rows);
+  const int e = with_tiles(xdt, gdt, 128, grid.x * grid.y * rows, [&](auto, auto, auto ty, auto, auto buffers) {
+    using TY = decltype(ty);
+    using T = TileOf<typename TY::op, TY::planes, 128, decltype(buffers)::value, true, true>;
+    return launch<k_head_dhead_part<TY, decltype(buffers)::value>>(grid, T::kThreads, T::kLds, stream, a);
+  });
+  return e ? e : with_types(xdt, gdt, [&](auto, auto g, auto ty) { return launch<k_head_join<decltype(g), decltype(ty)>>(dim3(upto((uint64_t)a.words * (a.s.D / 8), 256), 1, rows), 256, 0, stream, a); });
 }
 int launch_head_dbias(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
   return with_types(xdt, gdt, [&](auto, auto g, auto ty) { return launch<k_head_dbias<decltype(g), decltype(ty)>>(dim3(upto(a.words, 64), 1, rows), 256, 0, stream, a); });

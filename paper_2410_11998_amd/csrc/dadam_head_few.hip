@@ -70,8 +70,8 @@ __global__ __launch_bounds__(256) void k_few_logits(FewArgs a) {
     const uint32_t t = b * 32 + (lane & 31);
     h[b] = row.hidden + (uint64_t)(t < a.s.tokens ? t : a.s.tokens - 1) * a.s.width * size;
   }
-  // float32 products go to four (two) sums in turn: one sum of 1327 elements, rounded at every second one, leaves gradients off by 1.1e-6 of their norm, four 2.9e-7
-  constexpr int kSums = BRAIN ? 1 : 4 / NB;
+  // float32 products go to four sums in turn (two where four wavefronts share the width; half as many of 64 tokens): one sum of 1327 elements, rounded at every second one, leaves gradients off by 1.1e-6 of their norm, four 2.9e-7
+  constexpr int kSums = BRAIN ? 1 : (SHARED ? 2 : 4) / NB;
   float16v sums[kSums][NB];
 #pragma unroll
   for (int k = 0; k < kSums; ++k)
@@ -257,28 +257,42 @@ __global__ __launch_bounds__(256) void k_few_softmax(FewArgs a) {
     else F32::store(base + a.w.hidden, e, v);
     return;
   }
+  __shared__ float2v tops[T];
+  __shared__ float hits[T];
+  __shared__ int32_t targets[T];
+  if (threadIdx.x < T) {
+    tops[threadIdx.x] = global<const float2v>(base + a.w.top)[threadIdx.x];
+    hits[threadIdx.x] = global<const float>(base + a.w.hit)[threadIdx.x];
+    targets[threadIdx.x] = few_target(a, row.target, threadIdx.x, target) ? target : -1;
+  }
+  __syncthreads();
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const uint32_t block = blockIdx.x * 4 + threadIdx.x / 64, word = block * kFewWords + (lane & 31);
   if (block >= a.s.blocks) return;
   float sum = 0.f;
-#pragma unroll 4
-  for (uint32_t t0 = 0; t0 < T; t0 += 2) {
-    const uint32_t t = t0 + half;
-    const uint64_t e = ((uint64_t)block * T + t) * kFewWords + (lane & 31);
-    float p = 0.f;
-    if (few_target(a, row.target, t, target) && word < a.s.vocab) {
-      const float2v top = global<const float2v>(base + a.w.top)[t];
-      p = exponential<!BRAIN>(global<const float>(base + a.w.z)[e] - top[0]) * top[1];
-      if (word == (uint32_t)target) p = expm1f(-global<const float>(base + a.w.hit)[t]);
+#pragma unroll
+  for (uint32_t t0 = 0; t0 < T; t0 += 16) {  // eight tokens a lane: 16 bytes of the turned operand
+    float p[8];
+#pragma unroll
+    for (uint32_t k = 0; k < 8; ++k) p[k] = global<const float>(base + a.w.z)[((uint64_t)block * T + t0 + half * 8 + k) * kFewWords + (lane & 31)];
+    uint4v turned = {0, 0, 0, 0};
+#pragma unroll
+    for (uint32_t k = 0; k < 8; ++k) {
+      const uint32_t t = t0 + half * 8 + k;
+      p[k] = targets[t] >= 0 && word < a.s.vocab ? exponential<!BRAIN>(p[k] - tops[t][0]) * tops[t][1] : 0.f;
+      if (targets[t] >= 0 && word == (uint32_t)targets[t]) p[k] = expm1f(-hits[t]);
+      const uint64_t e = ((uint64_t)block * T + t) * kFewWords + (lane & 31);
+      if constexpr (BRAIN) {
+        const uint32_t bits = Brain::bits(p[k]);
+        p[k] = Brain::value(bits);
+        turned[k / 2] |= bits << 16 * (k & 1);
+        global<uint16_t>(base + a.w.p)[e] = (uint16_t)bits;
+      } else {
+        F32::store(base + a.w.z, e, p[k]);
+      }
+      sum += p[k];
     }
-    if constexpr (BRAIN) {
-      p = Brain::value(Brain::bits(p));
-      B16::store(base + a.w.p, e, p);
-      B16::store(base + a.w.p_turned, ((uint64_t)block * kFewWords + (lane & 31)) * T + t, p);
-    } else {
-      F32::store(base + a.w.z, e, p);
-    }
-    sum += p;
+    if constexpr (BRAIN) global<uint4v>(base + a.w.p_turned)[(((uint64_t)block * kFewWords + (lane & 31)) * T + t0) / 8 + half] = turned;
   }
   sum += __shfl_xor(sum, 32);
   if (row.dbias && half == 0 && word < a.s.vocab) {

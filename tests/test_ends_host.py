@@ -10,11 +10,11 @@ from paper_2410_11998_amd import binding as B
 from paper_2410_11998_amd import workloads as WL
 
 ROWS, VOCAB, WIDTH, TOKENS = 3, 100, 24, 7
-SIZES = [VOCAB * WIDTH, VOCAB, 40 * 30, 30 * 96]
+SIZES = [VOCAB * WIDTH, VOCAB, 40 * 30, 200 * 300]
 OFFSETS = [0, 2400, 2504, 3704]
-D = 6584
+D = 63704
 HEAD = B.dadam_head(0, 1, VOCAB, WIDTH)
-STEP = 1 << 16
+STEP = 1 << 18
 NAN = float("nan")
 
 
@@ -117,15 +117,15 @@ def test_workspaces_of_a_loss(tokens):
     B.dadam_destroy(h)
 
 
-GOOD = [(2, 40, 30), (3, 30, 32, 96, 0, 2.0), (3, 30, 32, 96, 32), (3, 30, 32, 96, 64, -1.0)]
+GOOD = [(2, 40, 30), (3, 200, 100, 300, 0, 2.0), (3, 200, 100, 300, 100), (3, 200, 100, 300, 200, -1.0)]
 
 
 def test_matrices():
     h = handle()
     assert code(lambda: B.dadam_ortho_get_info(h)) == B.DADAM_ESTATE
     for bad in ([(4, 2, 2)], [(2, 41, 30)], [(2, 40, 31)], [(2, 0, 30)], [(2, 40, 0)], [(2, 65537, 1, 1)], [(2, 1, 65537)], [(2, 40, 30, 29)], [(2, 40, 30, 30, 1)], [(2, 39, 30, 30, 31)],
-                [(2, 1, 1, 1, 1200)], [(2, 1, 1, 1, 2 ** 63)], [(3, 30, 32, 96, 65)], [(2, 40, 30, 30, 0, NAN)], [(2, 40, 30, 30, 0, float("inf"))],
-                [(2, 40, 30), (2, 1, 1)], [(3, 30, 32, 96, 0), (3, 30, 32, 96, 31)], [(2, 20, 30), (2, 20, 30, 30, 570)], [(3, 30, 32, 96, 0), (3, 2, 48, 48, 96)],
+                [(2, 1, 1, 1, 1200)], [(2, 1, 1, 1, 2 ** 63)], [(3, 200, 100, 300, 201)], [(2, 40, 30, 30, 0, NAN)], [(2, 40, 30, 30, 0, float("inf"))],
+                [(2, 40, 30), (2, 1, 1)], [(3, 200, 100, 300, 0), (3, 200, 100, 300, 99)], [(2, 20, 30), (2, 20, 30, 30, 570)], [(3, 200, 100, 300, 0), (3, 2, 48, 48, 96)],
                 [B.dadam_matrix_desc(2, 40, 30, 30, 0, 1.0, 1)]):
         assert code(lambda: B.dadam_set_matrices(h, bad)) == B.DADAM_EINVAL, bad
     B.dadam_set_matrices(h, GOOD)
@@ -133,7 +133,7 @@ def test_matrices():
     assert info.n_matrices == 4 and 0 < info.least_bytes <= info.bytes
     assert code(lambda: B.dadam_set_matrices(h, [(4, 2, 2)])) == B.DADAM_EINVAL
     assert B.dadam_ortho_get_info(h).n_matrices == 4                       # a refused set leaves the last one
-    B.dadam_set_matrices(h, [(3, 30, 96), (2, 20, 30), (2, 20, 30, 30, 600)])
+    B.dadam_set_matrices(h, [(3, 200, 300), (2, 20, 30), (2, 20, 30, 30, 600)])
     B.dadam_set_matrices(h, [])
     assert B.dadam_ortho_get_info(h).n_matrices == 0 and B.dadam_ortho_get_info(h).bytes == 0
     assert B.lib.dadam_set_matrices(h, None, 1) == B.DADAM_EINVAL and B.lib.dadam_set_matrices(h, None, 65537) == B.DADAM_EINVAL
@@ -224,7 +224,7 @@ def test_a_workspace_grows_with_what_it_holds():
         h = B.dadam_init(1, 1, 5 * q + (-5 * q) % 8, [0], [5 * q], device=B.DADAM_DEVICE_NONE)
         B.dadam_set_matrices(h, [(0, 5, q)])
         info = B.dadam_ortho_get_info(h)
-        assert info.least_bytes == info.bytes >= max(last, 2 * 128 * q * 4)
+        assert info.least_bytes == info.bytes >= max(last, 2 * 128 * q * 4 if q > 960 else 0)  # (up to there a compute unit holds it)
         last = info.bytes
         B.dadam_destroy(h)
     h = handle()

@@ -297,3 +297,17 @@ def test_two_calls_at_once_on_streams_of_their_own(tokens):
     for c in cs:
         c.check()
         c.close()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("tokens,vocab,width", [(3053, 4, 8), (2113, 300, 72), (4096, 129, 130)])
+def test_many_tokens_of_few_words(tokens, vocab, width, kind):
+    """The head's gradient in parts of the tokens, written and added to."""
+    c = Head(tokens, vocab, width, kind, rows=2, bias=True, seed=17)
+    c.run()
+    c.check()
+    before = torch.randn(c.g.shape, device=DEV).to(c.g.dtype)
+    c.g.copy_(before)
+    c.run(flags=B.DADAM_HEAD_MEAN | B.DADAM_HEAD_ADD)
+    c.check(before=before)
+    c.close()

@@ -336,6 +336,11 @@ def test_large_tiles(kind):
     got = host(out)
     mask = L.mask()
     assert all((got[i][~mask] == SENTINEL).all() for i in range(4))
+    inside = torch.from_numpy(mask).to(DEV)
+    for n_bytes in (L.info.least_bytes, L.info.bytes // 5):      # other groups, smaller tiles: the same sums in the same order
+        again = torch.full_like(g, SENTINEL)
+        B.dadam_orthogonalize(L.h, g, again, L.workspace(n_bytes), B.current_stream())
+        assert torch.equal(again[:, inside], out[:, inside])
     _, _, half, planes = TYPES[kind]
     for i in range(4):
         for k in range(i, len(L.matrices), 7):           # the statement in 64 bits of every seventh
@@ -344,3 +349,20 @@ def test_large_tiles(kind):
             want = O.orthogonalised(a)
             assert np.linalg.norm(view(got[i], L.offsets, m) - want) <= O.orthogonalised_error(a, planes) + half * np.linalg.norm(want)
     L.close()
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("shapes", [[(32, 960)], [(960, 31), (7, 5)], [(64, 416)], [(60, 400), (33, 1)], [(96, 320), (65, 97)], [(128, 160), (160, 128), (1, 1)], [(100, 100)] * 40])
+def test_matrices_that_a_compute_unit_holds(shapes, kind):
+    """The largest of each number of 32 rows, and layouts of such matrices only: no workspace."""
+    for rows in (1, 70):
+        L = Layout(shapes, kind, rows=rows, gap=3)
+        assert L.info.bytes == 0
+        g = on_device(L.random(18), kind)
+        out = torch.full_like(g, SENTINEL)
+        B.dadam_orthogonalize(L.h, g, out, (0, 0), B.current_stream())
+        got, given = host(out), host(g)
+        L.rows = min(rows, 2)
+        check_orthogonal(L, given, got, kind)
+        L.rows = rows
+        L.close()
