@@ -201,7 +201,8 @@ __device__ __forceinline__ constexpr float kept_times() {
 }
 
 // The logits of a tile of words (m) and tokens (n).  Without gradients: the largest and the sum of exponentials of each wavefront's words, and the
-// target's logit.  With: softmax - e[target].
+// target's logit.  With: softmax - e[target].  (2048 tokens, 50257 words, width 1024, bfloat16, without gradients 219 us, 963 TFLOP/s; two replicas of 4096 tokens with the
+// exponentials kept 1058 us, 796: behind its product a tile computes and stores 65536 exponentials while nobody multiplies.)
 template <typename XT, typename TY, int EDGE, int BUFFERS, int MODE>
 __global__ __launch_bounds__(2 * EDGE) void k_head_logits(HeadArgs a) {
   using T = TileOf<typename TY::op, TY::planes, EDGE, BUFFERS, false, false>;
@@ -309,7 +310,7 @@ __global__ __launch_bounds__(2 * EDGE) void k_head_logits(HeadArgs a) {
   }
 }
 
-// softmax - e[target] in place of the slices' exponentials: a thread takes eight words of a token.
+// softmax - e[target] in place of the slices' exponentials: a thread takes eight words of a token.  (Bound by memory: 282 us for 1.6 GB.)
 template <typename TY>
 __global__ __launch_bounds__(256) void k_head_scale(HeadArgs a) {
   using OP = typename TY::op;
@@ -386,7 +387,7 @@ __global__ __launch_bounds__(256) void k_head_sum(HeadArgs a) {
   }
 }
 
-// dW of a tile of columns (m) and words (n): both operands lie by tokens.
+// dW of a tile of columns (m) and words (n): both operands lie by tokens.  (Two replicas of 4096 tokens, 50257 words, width 1024, bfloat16: 783 and 53 us, 1007 TFLOP/s.)
 template <typename GT, typename TY, int EDGE, int BUFFERS>
 __global__ __launch_bounds__(2 * EDGE) void k_head_dhead(HeadArgs a) {
   using T = TileOf<typename TY::op, TY::planes, EDGE, BUFFERS, true, true>;
@@ -484,7 +485,8 @@ __global__ __launch_bounds__(256) void k_head_dbias(HeadArgs a) {
   }
 }
 
-// dh of a tile of columns (m) and tokens (n), over a part of the piece's words: the head lies by words.
+// dh of a tile of columns (m) and tokens (n), over a part of the piece's words: the head lies by words.  (Two replicas as above: 788 us, 1069
+// TFLOP/s.)
 template <typename TY, int EDGE, int BUFFERS>
 __global__ __launch_bounds__(2 * EDGE) void k_head_dhidden(HeadArgs a) {
   using T = TileOf<typename TY::op, TY::planes, EDGE, BUFFERS, true, false>;
@@ -618,7 +620,8 @@ int launch_head_dhead_parts(int xdt, int gdt, const HeadArgs& a, uint32_t rows, 
     using T = TileOf<typename TY::op, TY::planes, 128, decltype(buffers)::value, true, true>;
     return launch<k_head_dhead_part<TY, decltype(buffers)::value>>(grid, T::kThreads, T::kLds, stream, a);
   });
-  return e ? e : with_types(xdt, gdt, [&](auto, auto g, auto ty) { return launch<k_head_join<decltype(g), decltype(ty)>>(dim3(upto((uint64_t)a.words * (a.s.D / 8), 256), 1, rows), 256, 0, stream, a); });
+  const dim3 pieces(upto((uint64_t)a.words * (a.s.D / 8), 256), 1, rows);
+  return e ? e : with_types(xdt, gdt, [&](auto, auto g, auto ty) { return launch<k_head_join<decltype(g), decltype(ty)>>(pieces, 256, 0, stream, a); });
 }
 int launch_head_dbias(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
   return with_types(xdt, gdt, [&](auto, auto g, auto ty) { return launch<k_head_dbias<decltype(g), decltype(ty)>>(dim3(upto(a.words, 64), 1, rows), 256, 0, stream, a); });

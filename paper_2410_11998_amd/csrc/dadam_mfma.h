@@ -284,7 +284,8 @@ __device__ __forceinline__ void read_turned(V (&out)[N], const uint32_t (&at)[N]
 // Shape of a workgroup's tile: WM x WN wavefronts, each MT x NT blocks of 32 x 32; block (i, j) of wavefront (wm, wn) has rows (wm MT + i) 32 ... and columns
 // (j WN + wn) 32 ...  The large tile (256 x 256, eight wavefronts) is bound by LDS as much as by the matrix cores: a stage reads 192 KB and is written 64 KB, 2048
 // cycles, for 2048 cycles of products.  The small one (128 x 128, four) takes 768 cycles of LDS for 512 of products, and is for what has too few large tiles.
-// TFLOP/s, large / small / library, 8192 x 8192 x 8192 1119 / 914 / 1319, x 1024 1061 / 805 / 1078, 1024 x 49152 x 4096 1087 / 915 / 1295.
+// TFLOP/s of products alone, large / small / library's whole product: 8192 x 8192 x 8192 1293 / 1081 / 1347, x 1024 1162 / 1020 / 1092, 4096 x 50176 x 1024 1190 / 1040 / 1096;
+// with two planes, of instructions, 1383, 1324 and 1287.  (Zeros reach 1600 to 1900: what random numbers cost beyond that is the power that the chip may take.)
 // A_DOWN, B_DOWN: that operand lies by columns.  BUFFERS: stages in LDS, of which all but one are on their way.
 template <typename OP, int PLANES, int MT, int NT, int WM, int WN, bool A_DOWN, bool B_DOWN, int BUFFERS>
 struct Tile {

@@ -1,10 +1,11 @@
 // Orthogonalised updates of matrices that fit a compute unit: a workgroup holds one in LDS from the gradient to the parameters, in one launch where the tiles of
 // dadam_ortho.hip take three an iteration, whose beginnings and ends are all that such matrices' time goes into.
 //
-// X (its short side's rows), A = X X^T and B without its diagonal (see dadam_ortho.hip) lie in LDS as words of two halves, 22 bits, whatever the result's type.  Rows are filled up to multiples of 32 and have four
-// more words, so that eight rows' pieces of 16 bytes meet no bank twice.  A and B = b A + c A A by blocks of the lower half, a wavefront each; X X^T of one or three
-// blocks by ranges of columns, joined in their order.  Columns of a X + B X depend on the same columns of X only: a wavefront has all rows of 32, and writes them where
-// they were.
+// X (its short side's rows), A = X X^T and B without its diagonal (see dadam_ortho.hip) lie in LDS as words of two halves, 22 bits, whatever the result's
+// type.  Rows are filled up to multiples of 32 and have four more words, so that eight rows' pieces of 16 bytes meet no bank twice.  A and B = b A + c A A by
+// blocks of the lower half, a wavefront each; X X^T of one or three blocks by ranges of columns, joined in their order.  Columns of a X + B X depend on the same
+// columns of X only: a wavefront has all rows of 32, and writes them where they were.
+// Bound by latency: 64 x 48 and 48 x 192 take 47 us, of which an iteration is 8 (three barriers, and a chain of products that depend on each other).
 #include "dadam_mfma.h"
 #include "dadam_ortho.h"
 #include "dadam_ortho_source.h"
