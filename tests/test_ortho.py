@@ -94,6 +94,10 @@ def check_orthogonal(L, given, got, kind):
             assert off <= may, f"row {i} matrix {m}: off by {off}, may be {may} (norm {np.linalg.norm(want)})"
 
 
+# Layouts of matrices that each fit a compute unit take a kernel of their own: beside this one they go by tiles.
+BIG = (170, 230)
+HOW = pytest.mark.parametrize("more", [[], [BIG]], ids=["held", "tiles"])
+
 SHAPES = {
     "one": [(1, 1)],
     "vectors": [(1, 7), (9, 1), (1, 300)],
@@ -136,8 +140,9 @@ def test_small_workspaces_and_in_place_give_the_same_bits(kind):
     L.close()
 
 
-def test_zeros_nan_and_infinity_keep_to_their_matrix():
-    L = Layout([(40, 50), (50, 40), (30, 30), (20, 140)], rows=2)
+@HOW
+def test_zeros_nan_and_infinity_keep_to_their_matrix(more):
+    L = Layout([(40, 50), (50, 40), (30, 30), (20, 140)] + more, rows=2)
     g = L.random(3)
     view(g[0], L.offsets, L.matrices[0])[:] = 0
     view(g[0], L.offsets, L.matrices[1])[3, 4] = np.nan
@@ -160,9 +165,10 @@ def test_zeros_nan_and_infinity_keep_to_their_matrix():
     L.close()
 
 
-def test_other_schedules():
+@HOW
+def test_other_schedules(more):
     schedules = [[(1.5, -0.5, 0.0)] * 3, [(4.0, -6.0, 2.5), (3.0, -3.2, 1.2), (1.875, -1.25, 0.375)], [(1.0, 0.0, 0.0)]]
-    L = Layout([(70, 150), (129, 60)], rows=2)
+    L = Layout([(70, 150), (129, 60)] + more, rows=2)
     g = on_device(L.random(9), "f32")
     for s in schedules:
         s = [tuple(float(np.float32(v)) for v in abc) for abc in s]
@@ -193,12 +199,12 @@ class Step:
     def bind(self, out=None):
         B.dadam_bind(self.L.h, list(self.x), list(self.out if out is None else out), list(self.m), list(self.v), None if self.acc is None else list(self.acc))
 
-    def expected(self, g, m0, b0, x0, t, nesterov, fuse, planes):
-        """Per row and matrix: x, how far it may be off (2-norm), m_hat, b."""
+    def expected(self, g, m0, b0, x0, t, nesterov, fuse, planes, every=1):
+        """Per row and matrix (every so many): x, how far it may be off (2-norm), m_hat, b."""
         L, be = self.L, self.beta
         rp, col, w = self.csr
         for i in range(L.rows):
-            for mat in L.matrices:
+            for mat in L.matrices[i % every::every]:
                 gi, mi = view(g[i], L.offsets, mat).astype(np.float64), view(m0[i], L.offsets, mat).astype(np.float64)
                 m = be * mi + (1 - be) * gi
                 u = be * m + (1 - be) * gi if nesterov else m
@@ -220,16 +226,17 @@ class Step:
                 yield i, mat, x, may, mi, b
 
 
+@HOW
 @pytest.mark.parametrize("nesterov", [False, True])
 @pytest.mark.parametrize("kind,grad", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
 @pytest.mark.parametrize("topology,s", [("ring", 1), ("share", 2), ("complete", 3)])
-def test_steps(topology, s, kind, grad, nesterov):
+def test_steps(topology, s, kind, grad, nesterov, more):
     rows = {"ring": 4, "share": 1, "complete": 3}[topology]
     csr = {"ring": lambda: WL.ring(4), "share": lambda: (np.array([0, 3], np.int32), np.array([0, 2, 1], np.int32), np.array([0.5, 0.25, 0.25], np.float32)),
            "complete": lambda: WL.complete(3)}[topology]()
     cols = 3 if topology == "share" else rows
     decay = 0.0 if topology == "ring" else 0.125
-    shapes = [(40, 72), (130, 65), (96, 288, 3), (1, 17)]
+    shapes = [(40, 72), (130, 65), (96, 288, 3), (1, 17)] + more
     L = Layout(shapes, kind, rows=rows, cols=cols, csr=csr, gap=5, grad=grad, lr=0.02, beta1=0.9, accum_s=s, weight_decay=[decay] * len(shapes))
     S = Step(L, 3, 0.02, 0.9, s, csr, cols, decay)
     S.bind()
@@ -257,8 +264,9 @@ def test_steps(topology, s, kind, grad, nesterov):
     L.close()
 
 
-def test_updates_in_place_and_their_refusal():
-    shapes = [(40, 72), (72, 40)]
+@HOW
+def test_updates_in_place_and_their_refusal(more):
+    shapes = [(40, 72), (72, 40)] + more
     L = Layout(shapes, rows=2, lr=0.02)
     S = Step(L, 4, 0.02, 0.9, 1, WL.identity(2), 2, 0.0)
     g = on_device(L.random(8), "f32")
@@ -278,8 +286,9 @@ def test_updates_in_place_and_their_refusal():
     L.close()
 
 
-def test_recorded_into_a_graph_and_on_another_stream():
-    L = Layout([(140, 64), (64, 200)], "bf16", rows=2)
+@HOW
+def test_recorded_into_a_graph_and_on_another_stream(more):
+    L = Layout([(140, 64), (64, 200)] + more, "bf16", rows=2)
     g = on_device(L.random(2), "bf16")
     work, out, eager = L.workspace(), torch.zeros_like(g), torch.zeros_like(g)
     side = torch.cuda.Stream()
@@ -297,8 +306,9 @@ def test_recorded_into_a_graph_and_on_another_stream():
     L.close()
 
 
-def test_more_replicas_than_a_short_argument_block_names():
-    L = Layout([(20, 30), (150, 40)], rows=70, csr=WL.ring(70), lr=0.02)
+@HOW
+def test_more_replicas_than_a_short_argument_block_names(more):
+    L = Layout([(20, 30), (150, 40)] + more, rows=70, csr=WL.ring(70), lr=0.02)
     S = Step(L, 6, 0.02, 0.9, 1, WL.ring(70), 70, 0.0)
     S.bind()
     g = on_device(L.random(5), "f32")
@@ -366,3 +376,21 @@ def test_matrices_that_a_compute_unit_holds(shapes, kind):
         check_orthogonal(L, given, got, kind)
         L.rows = rows
         L.close()
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_steps_by_large_tiles(kind):
+    shapes = [(512, 768), (768, 520)] * 11 + [(256, 256)] * 2 + [(130, 200)]
+    L = Layout(shapes, kind, rows=4, csr=WL.ring(4), lr=0.02, beta1=0.9, accum_s=2, weight_decay=[0.125] * len(shapes))
+    S = Step(L, 19, 0.02, 0.9, 2, WL.ring(4), 4, 0.125)
+    S.bind()
+    S.acc.nan_to_num_()
+    g = on_device(L.random(20), kind)
+    m0, x0, b0 = S.m.cpu().numpy(), host(S.x), S.acc.cpu().numpy()
+    B.dadam_ortho_step(L.h, 0, g, 2, B.DADAM_FUSE_ACCUM | B.DADAM_ORTHO_NESTEROV, L.workspace(), B.current_stream())
+    x, m, acc = host(S.out), S.m.cpu().numpy(), S.acc.cpu().numpy()
+    for i, mat, want, may, mi, b in S.expected(host(g), m0, b0, x0, 2, True, True, TYPES[kind][3], every=7):
+        assert np.linalg.norm(view(x[i], L.offsets, mat) - want) <= may
+        near = 6 * EPS * (np.abs(mi) + 1e-2)
+        assert (np.abs(view(m[i], L.offsets, mat) - mi) <= near).all() and (view(acc[i], L.offsets, mat) == 0).all()
+    L.close()
