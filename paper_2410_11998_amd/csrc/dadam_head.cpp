@@ -40,6 +40,7 @@ struct Way {
 
 constexpr uint32_t kSplits = 64;               // at most
 constexpr uint64_t kMostOfPiece = 1ull << 27;  // tokens times words of a piece
+constexpr uint64_t kMostOfLaunch = 1ull << 37;  // and of a launch, whose threads are counted in 32 bits
 constexpr uint64_t kMostKept = 1ull << 31;     // bytes of softmax that a replica may keep
 constexpr uint64_t kMostAtOnce = 1ull << 31;   // bytes of workspace for which replicas are taken together
 // Workgroups that the chip holds at a time: one large tile a compute unit, two small ones.
@@ -69,7 +70,7 @@ Way good_way(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens, b
   const uint64_t large = (uint64_t)(filled(V, 256) / 256) * (filled(n_tokens, 256) / 256) * R;
   const uint32_t edge = suits_large(n_tokens) && suits_large(head->width) && suits_large(V) && large >= 256 ? 256 : 128;
   const uint64_t across = filled(head->width, edge) / edge, down = filled(n_tokens, edge) / edge, all = filled(V, edge);
-  uint64_t piece = all;
+  uint64_t piece = std::min(all, std::max<uint64_t>(1, kMostOfLaunch / (down * edge) / edge) * edge);
   if (!keeps && gradient) {
     // pieces whose tiles, of the logits and of the head's gradient, are what the chip holds at a time or more
     piece = std::max<uint64_t>(1, at_once(edge) / std::min(across, down)) * edge;

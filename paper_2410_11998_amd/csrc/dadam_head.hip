@@ -316,7 +316,7 @@ __global__ __launch_bounds__(256) void k_head_scale(HeadArgs a) {
   using OP = typename TY::op;
   const HeadRow& row = a.row[blockIdx.z];
   const uint64_t base = base_of(a);
-  const uint32_t n = blockIdx.y, m = (blockIdx.x * 256 + threadIdx.x) * 8;
+  const uint32_t each = (a.s.piece + 2047) / 2048, n = blockIdx.x / each, m = (blockIdx.x % each * 256 + threadIdx.x) * 8;  // (there may be more tokens than a grid's y)
   if (m >= a.s.piece) return;
   int32_t target;
   uint32_t w[8] = {};
@@ -599,7 +599,7 @@ int launch_head_logits(int xdt, int gdt, HeadMode mode, const HeadArgs& a, uint3
   });
 }
 int launch_head_scale(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
-  return with_types(xdt, gdt, [&](auto, auto, auto ty) { return launch<k_head_scale<decltype(ty)>>(dim3(upto(a.s.piece, 2048), a.s.T, rows), 256, 0, stream, a); });
+  return with_types(xdt, gdt, [&](auto, auto, auto ty) { return launch<k_head_scale<decltype(ty)>>(dim3(a.s.T * upto(a.s.piece, 2048), 1, rows), 256, 0, stream, a); });
 }
 int launch_head_losses(const HeadArgs& a, uint32_t rows, void* stream) {
   if (const int e = launch<k_head_losses>(dim3(a.s.T / 16, 1, rows), 256, 0, stream, a)) return e;

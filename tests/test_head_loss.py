@@ -147,6 +147,12 @@ def test_small_workspaces(kind):
         c.g.fill_(SENTINEL)
         c.run(work=c.workspace(n_bytes))
         c.check()
+    c.g.fill_(SENTINEL)
+    c.dhidden.fill_(SENTINEL)
+    least = c.info(False).least_bytes
+    assert least < c.info(False).bytes
+    c.run(work=c.workspace(least), gradient=False)
+    c.check(gradient=False)
     c.close()
 
 
@@ -300,7 +306,7 @@ def test_two_calls_at_once_on_streams_of_their_own(tokens):
 
 
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("tokens,vocab,width", [(3053, 4, 8), (2113, 300, 72), (4096, 129, 130)])
+@pytest.mark.parametrize("tokens,vocab,width", [(3053, 4, 8), (2113, 300, 72), (4096, 129, 130), (70001, 40, 8)])
 def test_many_tokens_of_few_words(tokens, vocab, width, kind):
     """The head's gradient in parts of the tokens, written and added to."""
     c = Head(tokens, vocab, width, kind, rows=2, bias=True, seed=17)
