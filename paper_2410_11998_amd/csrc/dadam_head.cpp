@@ -189,11 +189,12 @@ int run_rows(const dadam_handle* h, HeadArgs a, bool dhidden, bool dhead, bool d
     a.words = std::min(a.s.piece, a.s.vocab - a.first_word);
     a.later = k > 0;
   };
-  int e = launch_head_begin(x, g, a, rows, stream);
-  if (!e) e = launch_head_hidden(x, g, a, rows, stream);
+  a.groups = planes_of(h) == 2 ? head_most_groups(a) : 0;
+  int e = a.groups ? launch_head_most(x, a, rows, stream) : (int)hipSuccess;
   for (uint32_t k = 0; k < pieces && !e; ++k) {
     piece(k);
-    if (!a.straight) e = launch_head_words(x, g, a, rows, stream);
+    e = launch_head_operands(x, g, a, k == 0, rows, stream);
+    a.groups = 0;
     if (!e) e = launch_head_logits(x, g, a.s.keeps ? kHeadKeep : kHeadStatistics, a, rows, stream);
   }
   if (!e) e = launch_head_losses(a, rows, stream);
@@ -201,7 +202,7 @@ int run_rows(const dadam_handle* h, HeadArgs a, bool dhidden, bool dhead, bool d
   if (!e && a.s.keeps) e = launch_head_scale(x, g, a, rows, stream);
   for (uint32_t k = 0; k < pieces && !e; ++k) {
     piece(k);
-    if (pieces > 1 && !a.straight) e = launch_head_words(x, g, a, rows, stream);
+    if (pieces > 1) e = launch_head_operands(x, g, a, false, rows, stream);
     if (!e && !a.s.keeps) e = launch_head_logits(x, g, kHeadGradient, a, rows, stream);
     if (!e && dhead) e = run_dhead(x, g, a, rows, stream);
     if (!e && dbias) e = launch_head_dbias(x, g, a, rows, stream);

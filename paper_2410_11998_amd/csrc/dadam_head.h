@@ -14,6 +14,10 @@ struct HeadRow {  // device addresses, 0 where there is none
   uint64_t head, bias, hidden, target, nll, dhidden, dhead, dbias;
 };
 
+// HeadPlaces::words: how many tokens have a target, largest magnitudes, and from kHeadShares on those of kMostGroups workgroups, of the head and of the hidden vectors.
+enum HeadWord : uint32_t { kHeadCount = 0, kHeadMostHidden = 1, kHeadMostHead = 2, kHeadShares = 16 };
+constexpr uint32_t kMostGroups = 512;
+
 // Workspace of a replica.  Operands have `planes` halves or bfloat16s an element: hidden vectors and a piece of the head by rows of D, softmax - e[target] of a
 // piece by rows of its words, a token each.
 struct HeadPlaces {
@@ -36,7 +40,7 @@ inline constexpr HeadPlaces head_places(const HeadShape& s, uint64_t planes, boo
     at += (bytes + 255) / 256 * 256;
     return here;
   };
-  w.words = take(64);
+  w.words = take((kHeadShares + 2 * kMostGroups) * 4);
   w.top = take((uint64_t)s.T * 8);  // a token's largest logit and 1 / its sum of exponentials
   w.hit = take((uint64_t)s.T * 4);
   w.stats = take((uint64_t)s.slices * s.T * 8);
@@ -50,8 +54,6 @@ inline constexpr HeadPlaces head_places(const HeadShape& s, uint64_t planes, boo
   w.bytes = at;
   return w;
 }
-// HeadPlaces::words
-enum HeadWord : uint32_t { kHeadCount = 0, kHeadMostHidden = 1, kHeadMostHead = 2 };
 
 struct HeadArgs {
   HeadShape s;
@@ -62,6 +64,7 @@ struct HeadArgs {
   uint32_t mean, add;
   uint32_t first_word, words;  // of the piece
   uint32_t skip;        // words of the piece that another launch of launch_head_dhead takes: those before
+  uint32_t groups;      // whose largest magnitudes the operands go by, 0: they are known
   uint32_t later;       // a piece before this one has begun the sums
   uint32_t n_xcd;
   uint32_t straight;    // the head is an operand as it lies
@@ -121,9 +124,9 @@ int launch_few_gradients(int xdt, int gdt, const FewArgs& a, uint32_t rows, void
 int launch_few_end(int xdt, int gdt, const FewArgs& a, uint32_t rows, void* stream);
 
 // Launchers, of `rows` replicas.  xdt: type of parameters and hidden vectors, gdt of gradients; two planes unless both are bfloat16.
-int launch_head_begin(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                   // tokens with a target, powers of two
-int launch_head_hidden(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                  // operands of the hidden vectors
-int launch_head_words(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream);                   // operands of a piece of the head
+uint32_t head_most_groups(const HeadArgs& a);
+int launch_head_most(int xdt, const HeadArgs& a, uint32_t rows, void* stream);  // with two planes only
+int launch_head_operands(int xdt, int gdt, const HeadArgs& a, bool hidden, uint32_t rows, void* stream);  // of a piece, and of the hidden vectors
 // Statistics; statistics, and the slices' exponentials kept; or the logits' gradient.
 enum HeadMode : int { kHeadStatistics = 0, kHeadKeep = 1, kHeadGradient = 2 };
 int launch_head_logits(int xdt, int gdt, HeadMode mode, const HeadArgs& a, uint32_t rows, void* stream);

@@ -70,26 +70,7 @@ __device__ __forceinline__ float factor_of(uint64_t base, const HeadArgs& a) {
   return a.mean ? a.scale / fmaxf(count, 1.f) : a.scale;
 }
 
-// Tokens with a target, and the words of the largest magnitudes cleared.
-__global__ __launch_bounds__(256) void k_head_count(HeadArgs a) {
-  const uint64_t base = base_of(a), target = a.row[blockIdx.z].target;
-  __shared__ uint32_t parts[4];
-  uint32_t n = 0;
-  int32_t word;
-  for (uint32_t t = threadIdx.x; t < a.s.tokens; t += 256) n += has_target(a, target, t, word) ? 1 : 0;
-#pragma unroll
-  for (int step = 32; step; step >>= 1) n += __shfl_xor(n, step);
-  if (threadIdx.x % 64 == 0) parts[threadIdx.x / 64] = n;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    global<float>(base + a.w.words)[kHeadCount] = (float)(parts[0] + parts[1] + parts[2] + parts[3]);
-    global<uint32_t>(base + a.w.words)[kHeadMostHidden] = 0;
-    global<uint32_t>(base + a.w.words)[kHeadMostHead] = 0;
-  }
-}
-
-// Largest finite magnitudes: of the head (blockIdx.y 0) and of the hidden vectors of tokens with a target (1).  The largest is the same in any order.
-constexpr uint32_t kMostGroups = 512;  // workgroups: each ends in an atomic on one word
+// Largest finite magnitudes: of the head (blockIdx.y 0) and of the hidden vectors of tokens with a target (1), of every workgroup's share.
 __device__ __forceinline__ void larger(uint32_t& most, float v) {
   const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
   if (b < 0x7f800000u && b > most) most = b;
@@ -150,39 +131,71 @@ __global__ __launch_bounds__(256) void k_head_most(HeadArgs a) {
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int k = 1; k < 4; ++k) most = parts[k] > most ? parts[k] : most;
-    if (most)
-      __hip_atomic_fetch_max(global<uint32_t>(base_of(a) + a.w.words) + (blockIdx.y == 0 ? kHeadMostHead : kHeadMostHidden), most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    global<uint32_t>(base_of(a) + a.w.words)[kHeadShares + blockIdx.y * kMostGroups + blockIdx.x] = most;
   }
 }
 
-// `rows` rows of `width` elements as an operand of a.s.D columns, `filled` rows in all; the rest zeros.  A thread takes eight elements.
+// The power of two of an operand, by all threads of a workgroup: from the workgroups' largest, of which the first one here leaves the largest for the others, or (a later
+// piece of the head) as it was left.
+template <typename TY>
+__device__ __forceinline__ int found_power(uint64_t base, const HeadArgs& a, HeadWord word) {
+  if constexpr (TY::planes == 1) return 0;
+  if (a.groups == 0) return power_of<TY>(base, a, word);
+  const uint32_t DADAM_GLOBAL* shares = global<const uint32_t>(base + a.w.words) + kHeadShares + (word == kHeadMostHead ? 0 : kMostGroups);
+  uint32_t most = 0;
+  for (uint32_t k = threadIdx.x; k < a.groups; k += 256) most = shares[k] > most ? shares[k] : most;
+#pragma unroll
+  for (int step = 32; step; step >>= 1) {
+    const uint32_t other = __shfl_xor(most, step);
+    most = other > most ? other : most;
+  }
+  __shared__ uint32_t parts[4];
+  if (threadIdx.x % 64 == 0) parts[threadIdx.x / 64] = most;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 4; ++k) most = parts[k] > most ? parts[k] : most;
+  if (blockIdx.x == 0 && threadIdx.x == 0) global<uint32_t>(base + a.w.words)[word] = most;
+  return held_power(most);
+}
+
+// `rows` rows of `width` elements as an operand of a.s.D columns, `filled` rows in all; the rest zeros.  A thread takes eight elements, four times.
+constexpr uint32_t kOperandPieces = 4;
 template <typename XT, typename TY>
-__device__ __forceinline__ void make_operand(uint64_t data, uint32_t rows, uint32_t filled, float factor, uint64_t to, uint64_t target, const HeadArgs& a) {
+__device__ __forceinline__ void make_operand(uint64_t data, uint32_t rows, uint32_t filled, HeadWord most, uint64_t base, uint64_t to, uint64_t target, const HeadArgs& a) {
   using OP = typename TY::op;
   const uint32_t each = a.s.D / 8;
-  const uint64_t e = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-  const uint32_t r = (uint32_t)(e / each), c = (uint32_t)(e % each) * 8;
-  if (r >= filled) return;
-  float v[8] = {};
-  int32_t word;
-  const uint32_t n = r < rows ? left(a.s.width, c) : 0;
-  if (n && (!target || has_target(a, target, r, word))) XT::load8(data, (uint64_t)r * a.s.width + c, n, v);
-  uint32_t w[8];
+  float v[kOperandPieces][8];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) w[k] = operand_word<OP, TY::planes>(v[k] * factor);
-  store8<TY::planes>(to, r, a.s.D, c, w);
+  for (uint32_t i = 0; i < kOperandPieces; ++i) {
+    const uint64_t e = ((uint64_t)blockIdx.x * kOperandPieces + i) * 256 + threadIdx.x;
+    const uint32_t r = (uint32_t)(e / each), c = (uint32_t)(e % each) * 8, n = r < rows && r < filled ? left(a.s.width, c) : 0;
+    int32_t word;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[i][k] = 0.f;
+    if (n && (!target || has_target(a, target, r, word))) XT::load8(data, (uint64_t)r * a.s.width + c, n, v[i]);
+  }
+  const float factor = ldexpf(1.f, found_power<TY>(base, a, most));  // (while the elements are on their way)
+#pragma unroll
+  for (uint32_t i = 0; i < kOperandPieces; ++i) {
+    const uint64_t e = ((uint64_t)blockIdx.x * kOperandPieces + i) * 256 + threadIdx.x;
+    const uint32_t r = (uint32_t)(e / each), c = (uint32_t)(e % each) * 8;
+    if (r >= filled) return;
+    uint32_t w[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = operand_word<OP, TY::planes>(v[i][k] * factor);
+    store8<TY::planes>(to, r, a.s.D, c, w);
+  }
 }
+
+// The operands that are not read as they lie: a piece of the head (blockIdx.y 0), the hidden vectors (1, or 0 where the head lies as it should).
 template <typename XT, typename TY>
-__global__ __launch_bounds__(256) void k_head_hidden(HeadArgs a) {
-  const HeadRow& row = a.row[blockIdx.z];
-  const uint64_t base = base_of(a);
-  make_operand<XT, TY>(row.hidden, a.s.tokens, a.s.T, ldexpf(1.f, power_of<TY>(base, a, kHeadMostHidden)), base + a.w.hidden, row.target, a);
-}
-template <typename XT, typename TY>
-__global__ __launch_bounds__(256) void k_head_words(HeadArgs a) {
+__global__ __launch_bounds__(256) void k_head_operands(HeadArgs a) {
   const HeadRow& row = a.row[blockIdx.z];
   const uint64_t base = base_of(a), from = row.head + (uint64_t)a.first_word * a.s.width * sizeof(typename XT::type);
-  make_operand<XT, TY>(from, a.words, (a.words + a.s.edge - 1) / a.s.edge * a.s.edge, ldexpf(1.f, power_of<TY>(base, a, kHeadMostHead)), base + a.w.head, 0, a);
+  if (blockIdx.y == 0 && !a.straight)
+    make_operand<XT, TY>(from, a.words, (a.words + a.s.edge - 1) / a.s.edge * a.s.edge, kHeadMostHead, base, base + a.w.head, 0, a);
+  else
+    make_operand<XT, TY>(row.hidden, a.s.tokens, a.s.T, kHeadMostHidden, base, base + a.w.hidden, row.target, a);
 }
 
 // The piece's words as an operand, rows from `row` on: as they lie in the parameters, or their copy.
@@ -372,18 +385,26 @@ __global__ __launch_bounds__(256) void k_head_losses(HeadArgs a) {
   }
 }
 
-// The loss of a replica, summed in 64 bits in the order of the tokens' numbers by 256.
-__global__ __launch_bounds__(256) void k_head_sum(HeadArgs a) {
-  const uint64_t base = base_of(a);
-  __shared__ double parts[4];
-  double sum = 0.0;
-  for (uint32_t t = threadIdx.x; t < a.s.tokens; t += 256) sum += (double)global<const float>(base + a.w.hit)[t];
+// The loss of a replica, summed in 64 bits in the order of the tokens' numbers by 1024, and how many tokens have a target.
+__global__ __launch_bounds__(1024) void k_head_sum(HeadArgs a) {
+  const uint64_t base = base_of(a), target = a.row[blockIdx.z].target;
+  __shared__ double parts[2][16];
+  double sum = 0.0, count = 0.0;
+  for (uint32_t t = threadIdx.x; t < a.s.tokens; t += 1024) {
+    int32_t word;
+    if (!has_target(a, target, t, word)) continue;
+    sum += (double)global<const float>(base + a.w.hit)[t];
+    count += 1.0;
+  }
   sum = wave_sum(sum);
-  if (threadIdx.x % 64 == 0) parts[threadIdx.x / 64] = sum;
+  count = wave_sum(count);
+  if (threadIdx.x % 64 == 0) parts[0][threadIdx.x / 64] = sum, parts[1][threadIdx.x / 64] = count;
   __syncthreads();
   if (threadIdx.x == 0) {
-    const double count = (double)global<const float>(base + a.w.words)[kHeadCount], all = parts[0] + parts[1] + parts[2] + parts[3];
-    global<float>(a.losses)[blockIdx.z] = (float)((double)a.scale * all / (a.mean && count > 1.0 ? count : 1.0));
+    sum = count = 0.0;
+    for (int k = 0; k < 16; ++k) sum += parts[0][k], count += parts[1][k];
+    global<float>(base + a.w.words)[kHeadCount] = (float)count;
+    global<float>(a.losses)[blockIdx.z] = (float)((double)a.scale * sum / (a.mean && count > 1.0 ? count : 1.0));
   }
 }
 
@@ -568,23 +589,20 @@ int with_tiles(int xdt, int gdt, uint32_t edge, uint32_t tiles, Fn fn) {
 
 }  // namespace
 
-int launch_head_begin(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
-  int e = launch<k_head_count>(dim3(1, 1, rows), 256, 0, stream, a);
-  if (e || (xdt == (int)DADAM_BF16 && gdt == (int)DADAM_BF16)) return e;
+uint32_t head_most_groups(const HeadArgs& a) {
   const uint32_t head = upto((uint64_t)a.s.vocab * a.s.width, 2048), most = head > a.s.tokens ? head : a.s.tokens;
-  const dim3 grid(most < kMostGroups ? most : kMostGroups, 2, rows);
+  return most < kMostGroups ? most : kMostGroups;
+}
+int launch_head_most(int xdt, const HeadArgs& a, uint32_t rows, void* stream) {
+  const dim3 grid(a.groups, 2, rows);
   return xdt == (int)DADAM_BF16 ? launch<k_head_most<B16>>(grid, 256, 0, stream, a) : launch<k_head_most<F32>>(grid, 256, 0, stream, a);
 }
-int launch_head_hidden(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
-  return with_types(xdt, gdt, [&](auto x, auto, auto ty) {
-    return launch<k_head_hidden<decltype(x), decltype(ty)>>(dim3(upto((uint64_t)a.s.T * a.s.D, 2048), 1, rows), 256, 0, stream, a);
-  });
-}
-int launch_head_words(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
-  return with_types(xdt, gdt, [&](auto x, auto, auto ty) {
-    const uint64_t words = (uint64_t)upto(a.words, a.s.edge) * a.s.edge;
-    return launch<k_head_words<decltype(x), decltype(ty)>>(dim3(upto(words * a.s.D, 2048), 1, rows), 256, 0, stream, a);
-  });
+int launch_head_operands(int xdt, int gdt, const HeadArgs& a, bool hidden, uint32_t rows, void* stream) {
+  const uint32_t words = a.straight ? 0 : upto((uint64_t)upto(a.words, a.s.edge) * a.s.edge * a.s.D, kOperandPieces * 2048),
+                 vectors = hidden ? upto((uint64_t)a.s.T * a.s.D, kOperandPieces * 2048) : 0;
+  const dim3 grid(words > vectors ? words : vectors, (words ? 1 : 0) + (vectors ? 1 : 0), rows);
+  if (grid.x == 0) return 0;
+  return with_types(xdt, gdt, [&](auto x, auto, auto ty) { return launch<k_head_operands<decltype(x), decltype(ty)>>(grid, 256, 0, stream, a); });
 }
 int launch_head_logits(int xdt, int gdt, HeadMode mode, const HeadArgs& a, uint32_t rows, void* stream) {
   const dim3 grid(upto(a.words, a.s.edge) * (a.s.T / a.s.edge), 1, rows);
@@ -603,7 +621,7 @@ int launch_head_scale(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* 
 }
 int launch_head_losses(const HeadArgs& a, uint32_t rows, void* stream) {
   if (const int e = launch<k_head_losses>(dim3(a.s.T / 16, 1, rows), 256, 0, stream, a)) return e;
-  return launch<k_head_sum>(dim3(1, 1, rows), 256, 0, stream, a);
+  return launch<k_head_sum>(dim3(1, 1, rows), 1024, 0, stream, a);
 }
 int launch_head_dhead(int xdt, int gdt, uint32_t edge, const HeadArgs& a, uint32_t rows, void* stream) {
   const dim3 grid(upto(a.words - a.skip, edge) * (a.s.D / edge), 1, rows);
