@@ -55,14 +55,15 @@ __device__ __forceinline__ brain8 eight(uint64_t row, uint32_t width, uint32_t k
   return __builtin_bit_cast(brain8, v);
 }
 
-// Logits of a block of words, their largest and their sum of exponentials, and the target's.  A wavefront takes a block or, SHARED, the four of a workgroup take a quarter
-// of its width each: where there are so few blocks that the chip would wait for them (2009 words, 11 tokens, width of 12 KB, four replicas 154 / 40 us).
-template <typename XT, bool BRAIN, int NB, bool SHARED>
-__global__ __launch_bounds__(256) void k_few_logits(FewArgs a) {
+// Logits of a block of words, their largest and their sum of exponentials, and the target's.  A wavefront takes a block or, where there are so few blocks that the chip
+// would wait for them, SHARE of a workgroup take a part of its width each (2009 words, 11 tokens, 12 KB a row, four replicas: 154 us by one, 40 by four, 36 by eight;
+// 145 words, one token, six replicas 45 and 28).
+template <typename XT, bool BRAIN, int NB, uint32_t SHARE>
+__global__ __launch_bounds__(SHARE == 8 ? 512 : 256) void k_few_logits(FewArgs a) {
   const HeadRow& row = a.row[blockIdx.z];
   const uint64_t base = few_base(a);
   const int lane = threadIdx.x & 63, half = lane >> 5;
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), block = SHARED ? blockIdx.x : blockIdx.x * 4 + wave;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), block = SHARE > 1 ? blockIdx.x : blockIdx.x * 4 + wave;
   if (block >= a.s.blocks) return;
   const uint32_t mine = block * kFewWords + (lane & 31), word = mine < a.s.vocab ? mine : a.s.vocab - 1;
   const uint64_t size = sizeof(typename XT::type), w = row.head + (uint64_t)word * a.s.width * size;
@@ -72,16 +73,16 @@ __global__ __launch_bounds__(256) void k_few_logits(FewArgs a) {
     const uint32_t t = b * 32 + (lane & 31);
     h[b] = row.hidden + (uint64_t)(t < a.s.tokens ? t : a.s.tokens - 1) * a.s.width * size;
   }
-  // float32 products go to four sums in turn (two where four wavefronts share the width; half as many of 64 tokens): one sum of 1327 elements, rounded at every
+  // float32 products go to four sums in turn (two where four wavefronts share the width, one of eight; half as many of 64 tokens): one sum of 1327 elements, rounded at every
   // second one, leaves gradients off by 1.1e-6 of their norm, four 2.9e-7.
-  constexpr int kSums = BRAIN ? 1 : (SHARED ? 2 : 4) / NB;
+  constexpr int kSums = BRAIN || SHARE == 8 ? 1 : (SHARE == 4 ? 2 : 4) / NB;
   float16v sums[kSums][NB];
 #pragma unroll
   for (int k = 0; k < kSums; ++k)
 #pragma unroll
     for (int b = 0; b < NB; ++b) sums[k][b] = nothing();
   constexpr uint32_t kStep = BRAIN ? 16 : 8;
-  const uint32_t steps = (a.s.width + kStep - 1) / kStep, from = SHARED ? steps * wave / 4 * kStep : 0, to = SHARED ? steps * (wave + 1) / 4 * kStep : steps * kStep;
+  const uint32_t steps = (a.s.width + kStep - 1) / kStep, from = SHARE > 1 ? steps * wave / SHARE * kStep : 0, to = SHARE > 1 ? steps * (wave + 1) / SHARE * kStep : steps * kStep;
   const uint32_t whole = to < a.s.width ? to : a.s.width / kStep * kStep;  // up to here whole pieces
   uint32_t k0 = from;
   constexpr uint32_t kAhead = NB == 1 ? 8 : 4;  // pieces of a row on their way at once
@@ -139,8 +140,8 @@ __global__ __launch_bounds__(256) void k_few_logits(FewArgs a) {
     if constexpr (kSums == 2) acc[b] += sums[1][b];
     if constexpr (kSums == 4) acc[b] = (acc[b] + sums[1][b]) + (sums[2][b] + sums[3][b]);
   }
-  if constexpr (SHARED) {
-    __shared__ float parts[3][NB][16][64];
+  if constexpr (SHARE > 1) {
+    __shared__ float parts[SHARE - 1][NB][16][64];
     if (wave > 0)
 #pragma unroll
       for (int b = 0; b < NB; ++b)
@@ -151,7 +152,14 @@ __global__ __launch_bounds__(256) void k_few_logits(FewArgs a) {
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[b][r] = (acc[b][r] + parts[0][b][r][lane]) + (parts[1][b][r][lane] + parts[2][b][r][lane]);
+      for (int r = 0; r < 16; ++r) {
+        float pairs[SHARE / 2];
+        pairs[0] = acc[b][r] + parts[0][b][r][lane];
+#pragma unroll
+        for (uint32_t k = 1; k < SHARE / 2; ++k) pairs[k] = parts[2 * k - 1][b][r][lane] + parts[2 * k][b][r][lane];
+        acc[b][r] = pairs[0] + pairs[1];
+        if constexpr (SHARE == 8) acc[b][r] += pairs[2] + pairs[3];
+      }
   }
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
@@ -481,8 +489,14 @@ int with_few(int xdt, int gdt, const FewArgs& a, Fn fn) {
 
 int launch_few_logits(int xdt, int gdt, const FewArgs& a, uint32_t rows, void* stream) {
   return with_few(xdt, gdt, a, [&](auto x, auto, auto brain, auto nb) {
-    if (a.s.blocks * rows < kFewBlocks) return launch(k_few_logits<decltype(x), decltype(brain)::value, decltype(nb)::value, true>, dim3(a.s.blocks, 1, rows), 256, stream, a);
-    return launch(k_few_logits<decltype(x), decltype(brain)::value, decltype(nb)::value, false>, dim3(upto(a.s.blocks, 4), 1, rows), 256, stream, a);
+    using X = decltype(x);
+    constexpr bool kBrain = decltype(brain)::value;
+    constexpr int kNB = decltype(nb)::value;
+    const uint32_t blocks = a.s.blocks * rows;
+    if constexpr (kNB == 1)  // (the parts of 64 tokens do not fit the registers)
+      if (blocks < kFewBlocks / 4) return launch(k_few_logits<X, kBrain, kNB, 8>, dim3(a.s.blocks, 1, rows), 512, stream, a);
+    if (blocks < kFewBlocks) return launch(k_few_logits<X, kBrain, kNB, 4>, dim3(a.s.blocks, 1, rows), 256, stream, a);
+    return launch(k_few_logits<X, kBrain, kNB, 1>, dim3(upto(a.s.blocks, 4), 1, rows), 256, stream, a);
   });
 }
 int launch_few_losses(const FewArgs& a, uint32_t rows, void* stream) {
