@@ -112,7 +112,7 @@ int set_matrices(dadam_handle* h, const dadam_matrix_desc* m, uint32_t n) {
   if (const int rc = check_matrices(h, m, n)) return rc;
   std::unique_ptr<MatrixState, void (*)(MatrixState*)> s(new MatrixState(), free_matrices);
   if (h->matrices) s->coefficients = h->matrices->coefficients;
-  // A layout of matrices that each fit a compute unit goes by those (64 x 48 and 48 x 192: 47 us instead of 138).  Beside larger ones they go with those, whose launches
+  // A layout of matrices that each fit a compute unit goes by those (64 x 48 and 48 x 192: 42 us instead of 138).  Beside larger ones they go with those, whose launches
   // they lengthen by little (40 matrices of odd sizes 466 us, the small ones apart 623).
   bool lone = n > 0;
   std::vector<OrthoTask> tasks(n);

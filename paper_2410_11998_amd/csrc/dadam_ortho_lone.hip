@@ -5,7 +5,8 @@
 // type.  Rows are filled up to multiples of 32 and have four more words, so that eight rows' pieces of 16 bytes meet no bank twice.  A and B = b A + c A A by
 // blocks of the lower half, a wavefront each; X X^T of one or three blocks by ranges of columns, joined in their order.  Columns of a X + B X depend on the same
 // columns of X only: a wavefront has all rows of 32, and writes them where they were.
-// Bound by latency: 64 x 48 and 48 x 192 take 47 us, of which an iteration is 8 (three barriers, and a chain of products that depend on each other).
+// Bound by latency: 64 x 48 and 48 x 192 take 42 us, of which an iteration is 7 (four barriers, and a chain of products that depend on each other; three sums, none of
+// which waits for another, are slower: 44), 128 x 128 takes 70.
 #include "dadam_mfma.h"
 #include "dadam_ortho.h"
 #include "dadam_ortho_source.h"
@@ -67,6 +68,16 @@ __device__ __forceinline__ void block_of(uint32_t n, uint32_t& i, uint32_t& j) {
   j = n - i * (i + 1) / 2;
 }
 
+// A block's words and their mirror image.
+__device__ __forceinline__ void put_block(Words a, uint32_t ap, uint32_t i, uint32_t j, const uint32_t (&w)[16], int lane) {
+  const Words at = a + (i * 32 + row_of(0, lane)) * ap + j * 32 + (lane & 31), mirror = a + (j * 32 + (lane & 31)) * ap + i * 32 + row_of(0, lane);
+#pragma unroll
+  for (int r = 0; r < 16; ++r) at[row_of(r, 0) * ap] = w[r];
+  if (i == j) return;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) *(uint4v DADAM_LDS*)(mirror + g * 8) = uint4v{w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]};
+}
+
 // An iteration of a matrix of NB blocks of rows; the last leaves float32 values.
 template <int NB>
 __device__ __forceinline__ void iterate(Words x, Words a, Words diagonal, Words parts, uint32_t P, uint32_t Q, const LoneStep& s, bool last) {
@@ -80,15 +91,14 @@ __device__ __forceinline__ void iterate(Words x, Words a, Words diagonal, Words 
     uint32_t i, j;
     block_of(item % kBlocks, i, j);
     const float16v acc = block_product(x, xp, i, j, Q / 16 * (item / kBlocks) / kParts, Q / 16 * (item / kBlocks + 1) / kParts, lane);
+    if constexpr (kParts > 1) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      if constexpr (kParts > 1) {
-        parts[item * 1024 + r * 64 + lane] = __float_as_uint(acc[r]);
-      } else {
-        const uint32_t m = i * 32 + row_of(r, lane), c = j * 32 + column, w = halves<Half>(acc[r] * s.a_fresh);
-        a[m * ap + c] = w;
-        if (i != j) a[c * ap + m] = w;
-      }
+      for (int r = 0; r < 16; ++r) parts[item * 1024 + r * 64 + lane] = __float_as_uint(acc[r]);
+    } else {
+      uint32_t w[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) w[r] = halves<Half>(acc[r] * s.a_fresh);
+      put_block(a, ap, i, j, w, lane);
     }
   }
   __syncthreads();
@@ -114,13 +124,21 @@ __device__ __forceinline__ void iterate(Words x, Words a, Words diagonal, Words 
     uint32_t i, j;
     block_of(item, i, j);
     const float16v acc = block_product(a, ap, i, j, 0, P / 16, lane);
+    const Words at = a + (i * 32 + row_of(0, lane)) * ap + j * 32 + column;
+    float v[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) v[r] = fmaf(value(at[row_of(r, 0) * ap]), s.b_gain, acc[r] * s.b_fresh);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) words[n][r] = halves<Half>(v[r]);
+    if (i != j) continue;
+    float mine = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const uint32_t m = i * 32 + row_of(r, lane), c = j * 32 + column;
-      const float v = fmaf(value(a[m * ap + c]), s.b_gain, acc[r] * s.b_fresh);
-      if (m == c) diagonal[m] = __float_as_uint(v);
-      words[n][r] = m == c ? 0 : halves<Half>(v);
+      const bool on = row_of(r, lane) == (int)column;
+      mine = on ? v[r] : mine;
+      words[n][r] = on ? 0 : words[n][r];
     }
+    if ((column >> 2 & 1) == (uint32_t)(lane >> 5)) diagonal[i * 32 + column] = __float_as_uint(mine);
   }
   __syncthreads();
 #pragma unroll
@@ -129,12 +147,7 @@ __device__ __forceinline__ void iterate(Words x, Words a, Words diagonal, Words 
     if (item >= kBlocks) continue;
     uint32_t i, j;
     block_of(item, i, j);
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const uint32_t m = i * 32 + row_of(r, lane), c = j * 32 + column;
-      a[m * ap + c] = words[n][r];
-      if (i != j) a[c * ap + m] = words[n][r];
-    }
+    put_block(a, ap, i, j, words[n], lane);
   }
   __syncthreads();
   for (uint32_t q = wave; q < Q / 32; q += kWaves) {
@@ -149,14 +162,19 @@ __device__ __forceinline__ void iterate(Words x, Words a, Words diagonal, Words 
       for (int i = 0; i < NB; ++i) acc[i] = multiply(along(b + i * 32 * ap + k * 16), f, acc[i]);
     }
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
+    for (int i = 0; i < NB; ++i) {
+      const Words w = x + (i * 32 + row_of(0, lane)) * xp + q * 32 + column, d = diagonal + i * 32 + row_of(0, lane);
+      float v[16];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const uint32_t m = i * 32 + row_of(r, lane);
-        const Words w = x + m * xp + q * 32 + column;
-        const float v = fmaf(value(*w), fmaf(__uint_as_float(diagonal[m]), s.x_fresh, s.x_gain), acc[i][r] * s.x_fresh);
-        *w = last ? __float_as_uint(v) : halves<Half>(v);
+      for (int r = 0; r < 16; ++r) v[r] = fmaf(value(w[row_of(r, 0) * xp]), fmaf(__uint_as_float(d[row_of(r, 0)]), s.x_fresh, s.x_gain), acc[i][r] * s.x_fresh);
+      if (last) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) w[row_of(r, 0) * xp] = __float_as_uint(v[r]);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) w[row_of(r, 0) * xp] = halves<Half>(v[r]);
       }
+    }
   }
   __syncthreads();
 }
