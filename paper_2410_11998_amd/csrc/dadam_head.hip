@@ -218,7 +218,7 @@ __device__ __forceinline__ constexpr float kept_times() {
 // exponentials kept 1058 us, 796: behind its product a tile computes and stores 65536 exponentials while nobody multiplies.)
 template <typename XT, typename TY, int EDGE, int BUFFERS, int MODE>
 __global__ __launch_bounds__(2 * EDGE) void k_head_logits(HeadArgs a) {
-  using T = TileOf<typename TY::op, TY::planes, EDGE, BUFFERS, false, false>;
+  using T = TileOf<typename TY::op, TY::planes, EDGE, BUFFERS, false, false, TY::planes == 2 && BUFFERS == 4>;
   using OP = typename TY::op;
   const HeadRow& row = a.row[blockIdx.z];
   const uint64_t base = base_of(a);
@@ -610,7 +610,7 @@ int launch_head_logits(int xdt, int gdt, HeadMode mode, const HeadArgs& a, uint3
     using X = decltype(x);
     using TY = decltype(ty);
     constexpr int kEdge = decltype(edge)::value, kBuffers = decltype(buffers)::value;
-    using T = TileOf<typename TY::op, TY::planes, kEdge, kBuffers, false, false>;
+    using T = TileOf<typename TY::op, TY::planes, kEdge, kBuffers, false, false, TY::planes == 2 && kBuffers == 4>;
     if (mode == kHeadStatistics) return launch<k_head_logits<X, TY, kEdge, kBuffers, kHeadStatistics>>(grid, T::kThreads, T::kLds, stream, a);
     if (mode == kHeadKeep) return launch<k_head_logits<X, TY, kEdge, kBuffers, kHeadKeep>>(grid, T::kThreads, T::kLds, stream, a);
     return launch<k_head_logits<X, TY, kEdge, kBuffers, kHeadGradient>>(grid, T::kThreads, T::kLds, stream, a);

@@ -287,7 +287,9 @@ __device__ __forceinline__ void read_turned(V (&out)[N], const uint32_t (&at)[N]
 // TFLOP/s of products alone, large / small / library's whole product: 8192 x 8192 x 8192 1293 / 1081 / 1347, x 1024 1162 / 1020 / 1092, 4096 x 50176 x 1024 1190 / 1040 / 1096;
 // with two planes, of instructions, 1383, 1324 and 1287.  (Zeros reach 1600 to 1900: what random numbers cost beyond that is the power that the chip may take.)
 // A_DOWN, B_DOWN: that operand lies by columns.  BUFFERS: stages in LDS, of which all but one are on their way.
-template <typename OP, int PLANES, int MT, int NT, int WM, int WN, bool A_DOWN, bool B_DOWN, int BUFFERS>
+// APART: products with a low half have sums of their own, so that a sum of large values is rounded a third as often (32-bit logits of a width of 2304 to 3072:
+// gradients off by 7e-7 instead of 1.3e-6 of their norm).  It has to be the only tile of its compute unit: two of them would not fit the registers, nor a large one.
+template <typename OP, int PLANES, int MT, int NT, int WM, int WN, bool A_DOWN, bool B_DOWN, int BUFFERS, bool APART = false>
 struct Tile {
   static constexpr int kWaves = WM * WN, kThreads = kWaves * 64;
   static constexpr int kM = WM * MT * 32, kN = WN * NT * 32;
@@ -299,6 +301,7 @@ struct Tile {
   using vec = typename OP::vec;
 
   float16v acc[MT][NT];
+  float16v lows_apart[APART ? MT : 1][APART ? NT : 1];
 
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -306,7 +309,10 @@ struct Tile {
 #pragma unroll
       for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+        for (int r = 0; r < 16; ++r) {
+          acc[i][j][r] = 0.f;
+          if constexpr (APART) lows_apart[i][j][r] = 0.f;
+        }
   }
 
   // By columns, the 32-byte pieces of row k of a stage lie in the order piece ^ mixed(k): a fragment's instruction reads two pieces side by side of
@@ -400,7 +406,10 @@ struct Tile {
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = OP::mfma(f.a[p == 0 ? PLANES - 1 : 0][i], f.b[p == 1 ? PLANES - 1 : 0][j], acc[i][j]);
+        for (int j = 0; j < NT; ++j) {
+          float16v& sum = APART && p < 2 ? lows_apart[APART ? i : 0][APART ? j : 0] : acc[i][j];
+          sum = OP::mfma(f.a[p == 0 ? PLANES - 1 : 0][i], f.b[p == 1 ? PLANES - 1 : 0][j], sum);
+        }
   }
 
   // The sums over `stages` stages (of 64 summed elements, or 32 of two planes), from zero on.  While a stage is multiplied the next one is on its way, and while a
@@ -453,6 +462,12 @@ struct Tile {
         read<0>(f[0], stage_at(s + 1), wm, wn, lane);
       }
       step(1);
+    }
+    if constexpr (APART) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] += lows_apart[i][j];
     }
   }
 
@@ -524,8 +539,9 @@ __device__ __forceinline__ Nothing nothing_ahead(uint32_t, uint32_t) { return {}
 
 // Small tiles of a launch that gives every compute unit one at most keep four stages: a stage then has three times as long to come, and it is the length of a tile that
 // counts.  (Two tiles of two stages each fit a compute unit otherwise.)
-template <typename OP, int PLANES, int EDGE, int BUFFERS, bool A_DOWN, bool B_DOWN>
-using TileOf = typename std::conditional<EDGE == 256, Tile<OP, PLANES, 4, 2, 2, 4, A_DOWN, B_DOWN, BUFFERS>, Tile<OP, PLANES, 2, 2, 2, 2, A_DOWN, B_DOWN, BUFFERS>>::type;
+template <typename OP, int PLANES, int EDGE, int BUFFERS, bool A_DOWN, bool B_DOWN, bool APART = false>
+using TileOf =
+    typename std::conditional<EDGE == 256, Tile<OP, PLANES, 4, 2, 2, 4, A_DOWN, B_DOWN, BUFFERS>, Tile<OP, PLANES, 2, 2, 2, 2, A_DOWN, B_DOWN, BUFFERS, APART>>::type;
 constexpr uint32_t kOneEach = 256;  // compute units
 
 // Workgroup b of n as its die takes it: consecutive workgroup ids go to the dies in turn, each die takes a contiguous run of tiles, whose operands
