@@ -287,7 +287,7 @@ __device__ __forceinline__ void read_turned(V (&out)[N], const uint32_t (&at)[N]
 // TFLOP/s of products alone, large / small / library's whole product: 8192 x 8192 x 8192 1293 / 1081 / 1347, x 1024 1162 / 1020 / 1092, 4096 x 50176 x 1024 1190 / 1040 / 1096;
 // with two planes, of instructions, 1383, 1324 and 1287.  (Zeros reach 1600 to 1900: what random numbers cost beyond that is the power that the chip may take.)
 // A_DOWN, B_DOWN: that operand lies by columns.  BUFFERS: stages in LDS, of which all but one are on their way.
-// APART: products with a low half have sums of their own, so that a sum of large values is rounded a third as often (32-bit logits of a width of 2304 to 3072:
+// APART: products with a low half have sums of their own, so that a sum of large values is rounded a third as often (32-bit logits of a width of 2304 and more:
 // gradients off by 7e-7 instead of 1.3e-6 of their norm).  It has to be the only tile of its compute unit: two of them would not fit the registers, nor a large one.
 template <typename OP, int PLANES, int MT, int NT, int WM, int WN, bool A_DOWN, bool B_DOWN, int BUFFERS, bool APART = false>
 struct Tile {
