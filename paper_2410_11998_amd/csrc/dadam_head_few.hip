@@ -73,9 +73,9 @@ __global__ __launch_bounds__(SHARE == 8 ? 512 : 256) void k_few_logits(FewArgs a
     const uint32_t t = b * 32 + (lane & 31);
     h[b] = row.hidden + (uint64_t)(t < a.s.tokens ? t : a.s.tokens - 1) * a.s.width * size;
   }
-  // float32 products go to four sums in turn (two where four wavefronts share the width, one of eight; half as many of 64 tokens): one sum of 1327 elements, rounded at every
+  // float32 products go to four sums in turn (two of 64 tokens): one sum of 1327 elements, rounded at every
   // second one, leaves gradients off by 1.1e-6 of their norm, four 2.9e-7.
-  constexpr int kSums = BRAIN || SHARE == 8 ? 1 : (SHARE == 4 ? 2 : 4) / NB;
+  constexpr int kSums = BRAIN ? 1 : 4 / NB;
   float16v sums[kSums][NB];
 #pragma unroll
   for (int k = 0; k < kSums; ++k)
