@@ -164,13 +164,13 @@ int run_few(const dadam_handle* h, const FewArgs& a, bool dhidden, bool gradient
 }
 
 // dW of a piece.  What large tiles there are beyond a multiple of what the chip holds go by small ones, if that takes less than one more round of large ones: three rounds
-// and 72 small tiles instead of four (50257 words, width 1024).
+// and 72 small tiles instead of four (50257 words, width 1024).  Whole rows of tiles only, as a launch's words are: where one row of all replicas is more than the chip
+// holds (32 replicas, width 2304: 288 tiles), a piece of one row stays whole.
 int run_dhead(int x, int g, HeadArgs a, uint32_t rows, void* stream) {
   const uint32_t down = (a.words + a.s.edge - 1) / a.s.edge, tiles_of_word = a.s.D / a.s.edge * rows, tiles = down * tiles_of_word, over = tiles % at_once(a.s.edge);
-  const uint32_t all = a.words;
+  const uint32_t all = a.words, first = (tiles - over) / tiles_of_word * a.s.edge;
   if (a.s.parts > 1) return launch_head_dhead_parts(x, g, a, rows, stream);
-  if (a.s.edge == 256 && tiles > at_once(256) && over && over <= at_once(256) / 4) {
-    const uint32_t first = (tiles - over) / tiles_of_word * 256;
+  if (a.s.edge == 256 && first && over && over <= at_once(256) / 4) {
     a.words = first;
     if (const int e = launch_head_dhead(x, g, 256, a, rows, stream)) return e;
     a.skip = first;

@@ -1,0 +1,98 @@
+"""Which kernels the calls at the ends of an iteration launch, over how much, without a GPU (tests/host_ends_driver.cpp, the built library on a modelled
+runtime that refuses what the real one refuses)."""
+
+import os
+import re
+import subprocess
+
+import pytest
+
+from paper_2410_11998_amd import binding as B
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+TYPES = {"f32": B.DADAM_F32, "bf16": B.DADAM_BF16}
+
+
+@pytest.fixture(scope="module")
+def driver(tmp_path_factory):
+    clang, rocm = "/opt/rocm/lib/llvm/bin/clang++", "/opt/rocm/lib"
+    if not os.path.exists(clang):
+        pytest.skip("clang++ of the ROCm toolchain not available")
+    exe, libdir = str(tmp_path_factory.mktemp("ends") / "ends_driver"), os.path.dirname(B.LIB_PATH)
+    cmd = [clang, "-std=c++17", "-O1", "-rdynamic", "-D__HIP_PLATFORM_AMD__", "-I", os.path.join(ROOT, "include"), "-I",
+           os.path.join(ROOT, "paper_2410_11998_amd", "csrc"), "-I", "/opt/rocm/include", os.path.join(ROOT, "tests", "host_ends_driver.cpp"), "-o", exe, "-L", libdir, "-ldadam", f"-Wl,-rpath,{libdir}",
+           f"-Wl,-rpath,{rocm}", f"-Wl,-rpath-link,{rocm}"]
+    r = subprocess.run(cmd, capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, r.stderr[-2000:]
+    return exe
+
+
+class Launch:
+    """A kernel, its template arguments, grid, and of the head's gradient (the piece's first word, its words, how many of them are left out)."""
+
+    def __init__(self, text):
+        m = re.match(r"launch (?:void |int )?(?:dadam::\(anonymous namespace\)::)?(\w+)(?:<(.*)>)?\(.*\) (\d+),(\d+),(\d+)x(\d+) (\d+)(?: words (\d+) (\d+) (\d+))?$", text)
+        assert m, text
+        self.kernel, self.args = m.group(1), (m.group(2) or "").replace("dadam::(anonymous namespace)::", "").replace("Types<F32, F32>", "two").replace(
+            "Types<B16, B16>", "one").replace("Types<B16, F32>", "two").replace("Types<F32, B16>", "two").replace(" ", "").split(",")
+        self.grid, self.threads, self.lds = tuple(int(m.group(k)) for k in (3, 4, 5)), int(m.group(6)), int(m.group(7))
+        self.words = tuple(int(m.group(k)) for k in (8, 9, 10)) if m.group(8) else None
+
+
+class Answer:
+    def __init__(self, line):
+        head, *events = line.split(": ", 1)[1].split(" | ")
+        self.code, _, self.text = head.partition(" ")
+        self.code, self.launches = int(self.code), [Launch(e) for e in events]
+
+    def of(self, kernel):
+        return [x for x in self.launches if x.kernel == kernel]
+
+
+def ask(exe, commands):
+    r = subprocess.run([exe], input="\n".join(commands) + "\n", capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, (r.stdout[-500:], r.stderr[-2000:])
+    plain = subprocess.run(["c++filt"], input=r.stdout, capture_output=True, text=True, timeout=60).stdout.splitlines()
+    assert len(plain) == len(commands), r.stdout[-500:]
+    return [Answer(x) for x in plain]
+
+
+def loss(rows, kind, tokens, vocab, width, grad=None, before=0, gradient=True, share=100):
+    return f"loss {rows} {TYPES[kind]} {TYPES[grad or kind]} {tokens} {vocab} {width} {before} {int(gradient)} {share}"
+
+
+def check_head_gradient(a, rows, vocab, width, what):
+    """No launch without a workgroup, and every word's row of the head's gradient is in exactly one launch of each group of replicas."""
+    assert a.code == 0, (what, a.code, a.text)
+    reached, groups = 0, 0
+    for x in a.of("k_head_dhead"):
+        edge = int(x.args[2])
+        first, words, skip = x.words
+        across, (tiles, _, z) = -(-width // edge), x.grid
+        assert tiles == -(-(words - skip) // edge) * across and skip < words, what
+        if first + skip == 0:
+            assert reached in (0, vocab), what               # the last group's are whole
+            reached, groups = 0, groups + z
+        assert first + skip == reached, what
+        reached = first + words
+    if a.of("k_head_dhead"):
+        assert reached == vocab and groups == rows, what
+
+
+SIZES = [(32, "bf16", 2048, 256, 2304), (32, "f32", 2048, 256, 2304), (32, "bf16", 2048, 256, 2560), (32, "f32", 2048, 200, 2400), (17, "bf16", 4096, 256, 4096), (20, "bf16", 4096, 256, 4096),
+         (2, "bf16", 1024, 8448, 1024), (4, "bf16", 4096, 50257, 1024), (1, "f32", 2048, 50257, 1024), (40, "bf16", 2048, 300, 2304)]
+
+
+@pytest.mark.parametrize("rows,kind,tokens,vocab,width", SIZES)
+def test_the_heads_gradient_of_large_tiles(driver, rows, kind, tokens, vocab, width):
+    """What large tiles there are beyond whole rounds of the chip go by small ones: all words once, whole and in pieces of the vocabulary."""
+    shares = (100, 60, 30, 10, 1)
+    for share, a in zip(shares, ask(driver, [loss(rows, kind, tokens, vocab, width, share=s) for s in shares])):
+        check_head_gradient(a, rows, vocab, width, (share,))
+
+
+def test_every_launch_of_a_loss_has_workgroups(driver):
+    rows, widths, vocabs, tokens = (1, 3, 8, 17, 20, 31, 32, 33), (8, 256, 1024, 2304, 2560, 4096, 4352), (2, 200, 256, 300, 512, 5000), (0, 1, 64, 65, 777, 2048, 4096, 16384)
+    calls = [(r, kind, t, v, w) for r in rows for kind in TYPES for t in tokens for v in vocabs for w in widths]
+    for c, a in zip(calls, ask(driver, [loss(*c) for c in calls])):
+        check_head_gradient(a, c[0], c[3], c[4], c)
