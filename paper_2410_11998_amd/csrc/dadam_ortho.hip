@@ -146,6 +146,8 @@ __device__ __forceinline__ uint32_t lower_row(uint32_t tile) {
 
 // A tile (i, j), j <= i, of A = X X^T or of B = b A + c A A without its diagonal, and its mirror image.  (100 million elements of matrices 1024 wide: 690 TFLOP/s of the lower
 // half by small tiles, bfloat16; 75 million in 32 bits 1070 of instructions by large ones.  What it loses to the products alone is the ends of its rounds of tiles.)
+// A large tile on the diagonal mirrors its own lower quarter, as small tiles there do: with two planes the sums of an element and of its mirror image come in another order (low
+// high and high low change places), and the tiles' size, which goes by the workspace, is to change no bit.
 template <int PLANES, int EDGE, int BUFFERS, bool SQUARE>
 __global__ __launch_bounds__(2 * EDGE) void k_ortho_gram(OrthoStepArgs a) {
   using T = GramTile<PLANES, EDGE, BUFFERS>;
@@ -158,12 +160,15 @@ __global__ __launch_bounds__(2 * EDGE) void k_ortho_gram(OrthoStepArgs a) {
   T t;
   t.product(operand(in + (uint64_t)i * T::kM * pitch, pitch), operand(in + (uint64_t)j * T::kN * pitch, pitch), (uint32_t)(pitch / kStageBytes), lds);
   const uint64_t out = u.base + (SQUARE ? w.b : w.a);
-  t.hand_out(lds, i != j,
+  constexpr bool kQuarters = EDGE == (int)kLargeEdge && PLANES == 2;
+  auto above = [&](uint32_t m, uint32_t n) { return kQuarters && i == j && m / kSmallEdge < n / kSmallEdge; };  // of the quarter that is a mirror image
+  t.hand_out(lds, i != j || kQuarters,
              [&](uint32_t m, uint32_t n) {
                if constexpr (SQUARE) return load8<PLANES>(u.base + w.a, j * T::kN + n, u.t.P, i * T::kM + m);
                else return Nothing{};
              },
              [&](uint32_t m, uint32_t n, float (&v)[8], const auto& held) {
+               if (above(m, n)) return;
                uint32_t words[8];
                const uint32_t on_diagonal = j * T::kN + n - (i * T::kM + m);
 #pragma unroll
@@ -183,6 +188,7 @@ __global__ __launch_bounds__(2 * EDGE) void k_ortho_gram(OrthoStepArgs a) {
                store8<PLANES>(out, j * T::kN + n, u.t.P, i * T::kM + m, words);
              },
              [&](uint32_t m, uint32_t n, const float (&v)[8]) {
+               if (kQuarters && i == j && m / kSmallEdge <= n / kSmallEdge) return;
                uint32_t words[8];
                to_words(v, words);
                store8<PLANES>(out, i * T::kM + m, u.t.P, j * T::kN + n, words);

@@ -96,3 +96,22 @@ def test_every_launch_of_a_loss_has_workgroups(driver):
     calls = [(r, kind, t, v, w) for r in rows for kind in TYPES for t in tokens for v in vocabs for w in widths]
     for c, a in zip(calls, ask(driver, [loss(*c) for c in calls])):
         check_head_gradient(a, c[0], c[3], c[4], c)
+
+
+def ortho(rows, kind, shapes, step=False, grad=None, share=100):
+    return f"ortho {rows} {TYPES[kind]} {TYPES[grad or kind]} {int(step)} {share} " + " ".join(f"{r}x{c}" for r, c in shapes)
+
+
+# 256 large tiles of X X^T in four replicas, of matrices that fill them or nearly
+LARGE = {"256": [(256, 256)] * 64, "512": [(512, 512)] * 8 + [(500, 512)] * 7 + [(512, 498)] * 6 + [(250, 256)]}
+
+
+@pytest.mark.parametrize("step", [False, True])
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("name", LARGE)
+def test_tiles_of_matrices_go_by_the_workspace(driver, name, kind, step):
+    """A and B by large tiles with the workspace that is asked for and by small ones with less, X by large ones with either: what tests/test_ortho_tiles.py compares."""
+    for share, edge in ((100, "256"), (20, "128"), (0, "128")):
+        a, = ask(driver, [ortho(4, kind, LARGE[name], step, share=share)])
+        assert a.code == 0 and {x.args[1] for x in a.of("k_ortho_gram")} == {edge}
+        assert {x.args[1] for x in a.of("k_ortho_next")} == {x.args[2] for x in a.of("k_ortho_end")} == {"256"}
