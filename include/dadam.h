@@ -508,8 +508,8 @@ int dadam_mx4_round(dadam_handle* h, uint32_t slot, const void* const* x_src, vo
  * What a call writes must not overlap anything else that it reads or writes, but where "in place" is named.
  * Errors of all: DADAM_EINVAL (null, value out of range, workspace too small), DADAM_EALIGN, DADAM_EALIAS, DADAM_ESTATE, DADAM_EHIP. */
 
-/* The output matrix of a language model: tensor `tensor` of the layout, vocab rows (one a word) of width elements, and the words' bias, a tensor of vocab
- * elements, or DADAM_HEAD_NO_BIAS.  vocab is 1 to 2^24, width 1 to 65536. */
+/* The output matrix of a language model: tensor `tensor` of the layout, vocab rows (one a word) of width elements, and the words' bias, another tensor, of
+ * vocab elements, or DADAM_HEAD_NO_BIAS.  vocab is 1 to 2^24, width 1 to 65536. */
 #define DADAM_HEAD_NO_BIAS 0xffffffffu
 typedef struct {
   uint32_t tensor, bias_tensor;

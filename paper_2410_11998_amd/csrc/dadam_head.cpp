@@ -26,6 +26,7 @@ int check_head(const dadam_handle* h, const dadam_head* head, uint32_t n_tokens)
   if (head->tensor >= h->tensors.size()) return fail(h, DADAM_EINVAL, "the head's tensor %u is out of range", head->tensor);
   if (h->tensors[head->tensor].numel != (uint64_t)head->vocab * head->width) return fail(h, DADAM_EINVAL, "the head's tensor does not have vocab x width elements");
   if (head->bias_tensor == DADAM_HEAD_NO_BIAS) return DADAM_OK;
+  if (head->bias_tensor == head->tensor) return fail(h, DADAM_EINVAL, "the head and its bias are the same tensor");  // (of width 1: their gradients would share elements)
   if (head->bias_tensor >= h->tensors.size()) return fail(h, DADAM_EINVAL, "the bias's tensor %u is out of range", head->bias_tensor);
   if (h->tensors[head->bias_tensor].numel != head->vocab) return fail(h, DADAM_EINVAL, "the bias's tensor does not have vocab elements");
   return DADAM_OK;

@@ -232,3 +232,15 @@ def test_a_workspace_grows_with_what_it_holds():
     assert least == sorted(least)
     assert np.all([B.dadam_head_get_info(h, HEAD, n, False).least_bytes <= B.dadam_head_get_info(h, HEAD, n, True).least_bytes for n in (1, 100, 5000)])
     B.dadam_destroy(h)
+
+
+def test_a_head_of_one_column_is_not_its_own_bias():
+    """Both gradients would be written to the same elements."""
+    h = B.dadam_init(2, 2, 2 * VOCAB, [0, VOCAB], [VOCAB, VOCAB], device=B.DADAM_DEVICE_NONE)
+    c = Loss(h)
+    for tensor in (0, 1):
+        own = B.dadam_head(tensor, tensor, VOCAB, 1)
+        assert c.code(head=own) == B.DADAM_EINVAL and b"same tensor" in B.lib.dadam_last_error(h)
+        assert code(lambda: B.dadam_head_get_info(h, own, TOKENS, True)) == B.DADAM_EINVAL
+        assert c.code(head=B.dadam_head(tensor, 1 - tensor, VOCAB, 1)) == B.DADAM_ESTATE
+    B.dadam_destroy(h)
