@@ -532,7 +532,8 @@ int dadam_head_get_info(const dadam_handle* h, const dadam_head* head, uint32_t 
  * is the embedding too, or gradients of several calls), otherwise written; other elements of grads are not touched.
  * params: n_rows packed vectors of param_dtype; hidden and dhidden: n_rows times n_tokens x width of param_dtype; targets: int32; losses (n_rows, DEVICE) and nll: float32;
  * grads: n_rows packed vectors of grad_dtype.  nll, dhidden and grads may be null; without the last two only the loss is formed.  Of all these only params and grads
- * have to be 16-byte aligned, the others by their elements.  n_tokens is 0 to 2^20.
+ * have to be 16-byte aligned, the others by their elements.  n_tokens is 0 to 2^20;
+ * buffers of no tokens are not looked at (a table of nulls will do).
  * The logits are kept for up to 64 tokens (4 bytes each).  Of more tokens only softmax is, 2 bytes a logit with bfloat16 parameters and gradients and 4 otherwise, and
  * only where a replica's is at most 2 GiB and the workspace has room for it; elsewhere they are formed twice, a piece of the vocabulary at a time.
  * Sums are float32 (the loss 64 bits).  With bfloat16 parameters and gradients softmax - e[y] is rounded to bfloat16 before the gradients' products (where it is kept, to half

@@ -23,7 +23,7 @@ int guarded(dadam_handle* h, Fn fn) {
 
 constexpr uint64_t kMostElems = 1ull << 36;  // index and masks count in 32 bits
 
-// One argument of a call: n buffers of `bytes` bytes.
+// One argument of a call: n buffers of `bytes` bytes (of none: they may be null, and lie anywhere).
 struct Table {
   const void* const* p;
   uint32_t n;
@@ -48,7 +48,7 @@ inline int check_overlaps(const dadam_handle* h, const Table* t, int n_tables) {
   Range all[kMostTables * DADAM_MAX_ROWS], open[kMostTables * DADAM_MAX_ROWS];  // open: earlier ranges that reach beyond where the walk is
   uint32_t n = 0, n_open = 0;
   for (int k = 0; k < n_tables; ++k)
-    for (uint32_t i = 0; t[k].p && i < t[k].n; ++i) all[n++] = {(uintptr_t)t[k].p[i], (uintptr_t)t[k].p[i] + t[k].bytes, k, i};
+    for (uint32_t i = 0; t[k].p && t[k].bytes && i < t[k].n; ++i) all[n++] = {(uintptr_t)t[k].p[i], (uintptr_t)t[k].p[i] + t[k].bytes, k, i};
   std::sort(all, all + n, [](const Range& a, const Range& b) { return a.lo < b.lo; });
   for (uint32_t q = 0; q < n; ++q) {
     const Range& r = all[q];
@@ -72,7 +72,7 @@ inline int check_tables(const dadam_handle* h, const Table* t, int n_tables) {
   uintptr_t lows[kMostTables], highs[kMostTables];
   int n_used = 0;
   for (int k = 0; k < n_tables; ++k) {
-    if (!t[k].p || t[k].n == 0) continue;
+    if (!t[k].p || t[k].n == 0 || t[k].bytes == 0) continue;
     uintptr_t end = 0;
     for (uint32_t i = 0; i < t[k].n; ++i) {
       const uintptr_t at = (uintptr_t)t[k].p[i];

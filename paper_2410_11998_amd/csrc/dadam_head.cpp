@@ -264,7 +264,7 @@ int dadam_head_loss(dadam_handle* h, const dadam_head* head, const void* const* 
     rc = check_tables(h, tables, 7);
     const uintptr_t lo = (uintptr_t)losses, hi = lo + 4 * R;
     for (const Table& t : tables)
-      for (uint32_t i = 0; i < t.n && !rc; ++i)
+      for (uint32_t i = 0; t.bytes && i < t.n && !rc; ++i)
         if (lo < (uintptr_t)t.p[i] + t.bytes && (uintptr_t)t.p[i] < hi) rc = fail(h, DADAM_EALIAS, "losses overlaps %s[%u]", t.name, i);
     if (!rc) rc = check_device(h);
     if (rc) return rc;

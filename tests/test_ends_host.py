@@ -244,3 +244,17 @@ def test_a_head_of_one_column_is_not_its_own_bias():
         assert code(lambda: B.dadam_head_get_info(h, own, TOKENS, True)) == B.DADAM_EINVAL
         assert c.code(head=B.dadam_head(tensor, 1 - tensor, VOCAB, 1)) == B.DADAM_ESTATE
     B.dadam_destroy(h)
+
+
+def test_no_tokens_need_no_memory():
+    """Buffers of no elements may be null, as empty tensors are, and lie anywhere."""
+    h = handle()
+    c = Loss(h)
+    none = {k: [0] * ROWS for k in ("hidden", "targets", "nll", "dhidden")}
+    assert c.code(n=0, **none) == B.DADAM_ESTATE and b"device" in B.lib.dadam_last_error(h)
+    for inside in (c.params[1] + 64, c.grads[0] + 64, c.workspace[0] + 64, c.losses + 4):
+        assert c.code(n=0, **{k: [inside] * ROWS for k in none}) == B.DADAM_ESTATE, inside
+    for k in none:
+        assert c.code(**{k: none[k]}) == B.DADAM_EINVAL
+    assert c.code(n=0, params=[0] * ROWS, **none) == B.DADAM_EINVAL and c.code(n=0, **dict(none, hidden=None)) == B.DADAM_EINVAL
+    B.dadam_destroy(h)

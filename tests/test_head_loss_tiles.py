@@ -4,7 +4,10 @@ statement in 64 bits (oracle/ends_oracle.py) for some of the replicas."""
 import copy
 
 import pytest
-from test_head_loss import KINDS, Head
+import torch
+from test_head_loss import KINDS, SENTINEL, Head
+
+from paper_2410_11998_amd import binding as B
 
 pytestmark = pytest.mark.gpu
 
@@ -23,4 +26,21 @@ def test_a_vocabulary_of_one_row_of_tiles(kind):
     c = Head(2048, 256, 2304, kind, rows=32, seed=21)
     c.run()
     check_some(c, (0, 17, 31))
+    c.close()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_no_tokens_in_empty_tensors(kind):
+    c = Head(0, 40, 24, kind, rows=2, bias=True, seed=7)
+    assert c.hidden.data_ptr() == 0
+    c.run()
+    assert bool((c.losses == 0).all())
+    for at, n in ((c.at, 40 * 24), (c.bias_at, 40)):
+        assert bool((c.g[:, at:at + n] == 0).all())
+        c.g[:, at:at + n] = SENTINEL
+    assert bool((c.g == SENTINEL).all())
+    c.hidden, c.dhidden = list(c.hidden), list(c.dhidden)
+    B.dadam_head_loss(c.h, c.head, c.x, c.hidden, list(c.y), 0, 1.0, 0, c.losses, list(c.nll), c.dhidden, c.g, c.workspace(), B.current_stream())
+    assert bool((c.losses == 0).all()) and bool((c.g[:, c.at:c.at + 40 * 24] == 0).all())
+    torch.cuda.synchronize()
     c.close()
