@@ -476,14 +476,14 @@ def _message_bytes(d: int) -> int:
     return -(-(-(-d // DADAM_MX4_BLOCK) * 17) // 16) * 16
 
 
-def _row_values(norms, rows: int, on_device: bool) -> int:
-    if isinstance(norms, int):
-        return norms
-    if norms.numel() < rows or norms.element_size() != 4 or not norms.is_contiguous():
-        raise ValueError("the values of the rows: one float32 each is needed")
-    if on_device and not norms.is_cuda:
-        raise ValueError("the values of the rows are not on a GPU")
-    return norms.data_ptr()
+def _row_values(values, rows: int, on_device: bool, what: str = "norms") -> int:
+    if isinstance(values, int):
+        return values
+    if values.numel() < rows or values.element_size() != 4 or not values.is_contiguous():
+        raise ValueError(f"{what} must hold one float32 a row")
+    if on_device and not values.is_cuda:
+        raise ValueError(f"{what} is not on a GPU")
+    return values.data_ptr()
 
 
 def dadam_grad_norm(h, grads, norms, stream: int = 0) -> None:
@@ -604,7 +604,7 @@ def dadam_head_loss(h, head, params, hidden, targets, n_tokens: int, scale: floa
     x, v = pointer_table(params, rows, d, pb, "params", gpu), pointer_table(hidden, rows, n, pb, "hidden", gpu)
     y, l = pointer_table(targets, rows, int(n_tokens), 4, "targets", gpu), pointer_table(nll, rows, int(n_tokens), 4, "nll", gpu)
     dv, g = pointer_table(dhidden, rows, n, pb, "dhidden", gpu), pointer_table(grads, rows, d, gb, "grads", gpu)
-    _check(h, lib.dadam_head_loss(h, C.byref(head), _at(x), _at(v), _at(y), int(n_tokens), scale, flags, _row_values(losses, rows, gpu), _at(l), _at(dv), _at(g),
+    _check(h, lib.dadam_head_loss(h, C.byref(head), _at(x), _at(v), _at(y), int(n_tokens), scale, flags, _row_values(losses, rows, gpu, "losses"), _at(l), _at(dv), _at(g),
                                   *_workspace(workspace, gpu), stream))
 
 

@@ -263,3 +263,21 @@ def test_a_handle_by_its_number_and_a_handle_that_is_none():
                      lambda x: B.dadam_mx4_gossip(x, 0, at, at, at, at, at, 0.5), lambda x: B.dadam_mx4_round(x, 0, at, at, at, at, 0.5)):
             with pytest.raises(ValueError):
                 call(none)
+
+
+def test_the_binding_names_what_it_refuses():
+    """Values of the rows by the name of the argument, on the CPU and on none."""
+    import torch
+    h = handle()
+    t = tables("norm")["grads"]
+    head, rows = B.dadam_head(0, B.DADAM_HEAD_NO_BIAS, 10, 100), [t] * 3
+    for bad in (torch.zeros(2), torch.zeros(3, dtype=torch.float64), torch.zeros(6)[::2]):
+        for call in (lambda: B.dadam_grad_norm(h, t, bad), lambda: B.dadam_clip_grads(h, t, t, 1.0, bad)):
+            with pytest.raises(ValueError, match="norms must hold one float32 a row"):
+                call()
+        with pytest.raises(ValueError, match="losses must hold one float32 a row"):
+            B.dadam_head_loss(h, head, rows[0], rows[1], rows[2], 1, 1.0, 0, bad, None, None, None, None)
+    for name in ("norms", "losses"):
+        with pytest.raises(ValueError, match=f"{name} is not on a GPU"):
+            B._row_values(torch.zeros(3), 3, True, name)
+    B.dadam_destroy(h)
