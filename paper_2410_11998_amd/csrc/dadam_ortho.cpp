@@ -75,10 +75,19 @@ void split_sums(std::vector<OrthoTask>* tasks, uint32_t planes, uint64_t replica
 
 constexpr uint32_t kMostMatrices = 65536, kMostSide = 65536;
 
-// Rectangles of one tensor that is read as rows of ld elements.
-struct Rectangle {
-  uint64_t r0, r1, c0, c1;
-};
+// Whether two matrices of a tensor share elements.
+bool share_elements(const dadam_matrix_desc& one, const dadam_matrix_desc& other) {
+  if (one.ld == other.ld) {  // rectangles of rows of ld elements
+    auto apart = [](uint64_t p, uint64_t n, uint64_t q, uint64_t m) { return p + n <= q || q + m <= p; };
+    return !apart(one.first / one.ld, one.rows, other.first / one.ld, other.rows) && !apart(one.first % one.ld, one.cols, other.first % one.ld, other.cols);
+  }
+  const dadam_matrix_desc &a = one.rows <= other.rows ? one : other, &b = one.rows <= other.rows ? other : one;
+  for (uint64_t r = 0; r < a.rows; ++r) {
+    const uint64_t at = a.first + r * a.ld, end = b.first + b.cols, k = at < end ? 0 : (at - end) / b.ld + 1;  // the first row of b that ends behind at
+    if (k < b.rows && b.first + k * b.ld < at + a.cols) return true;
+  }
+  return false;
+}
 
 int check_matrices(const dadam_handle* h, const dadam_matrix_desc* m, uint32_t n) {
   std::vector<std::vector<uint32_t>> of_tensor(h->tensors.size());
@@ -97,13 +106,8 @@ int check_matrices(const dadam_handle* h, const dadam_matrix_desc* m, uint32_t n
     auto end = [&](uint32_t k) { return m[k].first + (uint64_t)(m[k].rows - 1) * m[k].ld + m[k].cols; };
     std::sort(list.begin(), list.end(), [&](uint32_t a, uint32_t b) { return m[a].first < m[b].first; });
     for (size_t i = 0; i < list.size(); ++i)
-      for (size_t j = i + 1; j < list.size() && m[list[j]].first < end(list[i]); ++j) {
-        const dadam_matrix_desc &a = m[list[i]], &b = m[list[j]];
-        auto box = [](const dadam_matrix_desc& x) { return Rectangle{x.first / x.ld, x.first / x.ld + x.rows, x.first % x.ld, x.first % x.ld + x.cols}; };
-        const Rectangle p = box(a), q = box(b);
-        if (a.ld != b.ld || (p.r0 < q.r1 && q.r0 < p.r1 && p.c0 < q.c1 && q.c0 < p.c1))
-          return fail(h, DADAM_EINVAL, "matrices %u and %u share elements", list[i], list[j]);
-      }
+      for (size_t j = i + 1; j < list.size() && m[list[j]].first < end(list[i]); ++j)
+        if (share_elements(m[list[i]], m[list[j]])) return fail(h, DADAM_EINVAL, "matrices %u and %u share elements", list[i], list[j]);
   }
   return DADAM_OK;
 }

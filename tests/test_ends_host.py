@@ -258,3 +258,32 @@ def test_no_tokens_need_no_memory():
         assert c.code(**{k: none[k]}) == B.DADAM_EINVAL
     assert c.code(n=0, params=[0] * ROWS, **none) == B.DADAM_EINVAL and c.code(n=0, **dict(none, hidden=None)) == B.DADAM_EINVAL
     B.dadam_destroy(h)
+
+
+def test_matrices_of_other_row_distances_share_a_tensor_but_no_element():
+    """A matrix may lie between another's rows with a distance of its own (of one row: whatever the distance); against a map of the tensor's elements."""
+    h = handle()
+    apart = [[(3, 200, 100, 300), (3, 1, 100, 100, 100)], [(3, 1, 100, 100, 100), (3, 200, 100, 300)], [(3, 200, 100, 300), (3, 100, 200, 600, 100), (3, 100, 200, 600, 400)]]
+    for good in apart:
+        B.dadam_set_matrices(h, good)
+        assert B.dadam_ortho_get_info(h).n_matrices == len(good)
+    rng = np.random.default_rng(3)
+    seen = [0, 0]
+    for _ in range(3000):
+        ms = []
+        for _ in range(2):
+            ld = int(rng.integers(1, 40))
+            cols, rows = int(rng.integers(1, ld + 1)), int(rng.integers(1, 20))
+            first = int(rng.integers(0, 40)) * ld + int(rng.integers(0, ld - cols + 1))
+            ms.append((2, rows, cols, ld, first))
+        reached = [m[4] + (m[1] - 1) * m[3] + m[2] for m in ms]
+        if max(reached) > SIZES[2]:
+            continue
+        taken = [np.zeros(SIZES[2], dtype=bool) for _ in ms]
+        for t, (_, rows, cols, ld, first) in zip(taken, ms):
+            np.lib.stride_tricks.as_strided(t[first:], (rows, cols), (ld, 1))[:] = True
+        shared = bool((taken[0] & taken[1]).any())
+        seen[shared] += 1
+        assert code(lambda: B.dadam_set_matrices(h, ms)) == (B.DADAM_EINVAL if shared else B.DADAM_OK), (ms, shared)
+    assert min(seen) > 300
+    B.dadam_destroy(h)
