@@ -431,6 +431,7 @@ int run_lone(dadam_handle* h, const Call& call, const Powers& pw, void* stream) 
 int check_workspace(const dadam_handle* h, const void* workspace, uint64_t bytes, uint64_t least) {
   if (!workspace && least) return fail(h, DADAM_EINVAL, "workspace is null");
   if ((uintptr_t)workspace & 255u) return fail(h, DADAM_EALIGN, "workspace is not 256-byte aligned");
+  if (bytes && ((uintptr_t)workspace >= kHighest || bytes > kHighest - (uintptr_t)workspace)) return fail(h, DADAM_EINVAL, "workspace reaches above address 2^52");
   if (bytes < least) return fail(h, DADAM_EINVAL, "workspace has %llu bytes, %llu are needed", (unsigned long long)bytes, (unsigned long long)least);
   return DADAM_OK;
 }

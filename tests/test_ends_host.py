@@ -287,3 +287,18 @@ def test_matrices_of_other_row_distances_share_a_tensor_but_no_element():
         assert code(lambda: B.dadam_set_matrices(h, ms)) == (B.DADAM_EINVAL if shared else B.DADAM_OK), (ms, shared)
     assert min(seen) > 300
     B.dadam_destroy(h)
+
+
+def test_workspaces_that_reach_beyond_memory():
+    """More bytes than addresses: the end wraps, and would lie before the buffers that the workspace overlaps."""
+    h = handle(accum_s=2)
+    B.dadam_set_matrices(h, GOOD)
+    g, work = addresses(ROWS, 1 << 24), 8 << 24
+    src, dst, m, v, acc = (addresses(ROWS, (k + 2) << 24) for k in range(5))
+    B.dadam_bind(h, src, dst, m, v, acc)
+    for at, n_bytes in ((1 << 20, 2 ** 64 - 256), (work, 2 ** 64 - 1), (work, 2 ** 64 - work), (1 << 52, 1 << 24), (work, (1 << 52) - work + 1)):
+        assert code(lambda: B.dadam_ortho_step(h, 0, g, 1, 0, (at, n_bytes))) == B.DADAM_EINVAL, (at, n_bytes)
+        assert code(lambda: B.dadam_orthogonalize(h, g, dst, (at, n_bytes))) == B.DADAM_EINVAL, (at, n_bytes)
+        assert Loss(h).code(workspace=(at, n_bytes)) == B.DADAM_EINVAL, (at, n_bytes)
+    assert code(lambda: B.dadam_ortho_step(h, 0, g, 1, 0, (work, (1 << 52) - work))) == B.DADAM_ESTATE and b"device" in B.lib.dadam_last_error(h)
+    B.dadam_destroy(h)
