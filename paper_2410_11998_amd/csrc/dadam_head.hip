@@ -40,7 +40,8 @@ struct Types<F32, B16> : Types<F32, F32> {};
 
 __device__ __forceinline__ uint32_t left(uint32_t n, uint32_t at) { return at < n ? n - at : 0; }
 
-constexpr int kHeldAt = 13;  // operands of two planes are brought to at most 2^13, an eighth of what a half can hold
+// Operands of two planes are brought to at most 2^15, half of what a half can hold: its smallest step is then 2^-38 of the largest or less, rounded 2^-39.
+constexpr int kHeldAt = 15;
 
 // The power of two that brings what is at most `most` (the bits of a finite float) to at most 2^kHeldAt.
 __device__ __forceinline__ int held_power(uint32_t most) {
