@@ -115,3 +115,29 @@ def test_tiles_of_matrices_go_by_the_workspace(driver, name, kind, step):
         a, = ask(driver, [ortho(4, kind, LARGE[name], step, share=share)])
         assert a.code == 0 and {x.args[1] for x in a.of("k_ortho_gram")} == {edge}
         assert {x.args[1] for x in a.of("k_ortho_next")} == {x.args[2] for x in a.of("k_ortho_end")} == {"256"}
+
+
+# (replicas, tokens, words, width, where the head begins, hundredths of the workspace that is asked for, with gradients), and the modes of k_head_logits (0: statistics, 1:
+# exponentials kept, 2: the logits' gradient) and edges of the head's gradient that go with them
+LOSSES = {
+    "value": ((32, 512, 1000, 250, 6, 100, False), {"0"}, set()),
+    "value of a few replicas at a time": ((32, 512, 1000, 250, 6, 30, False), {"0"}, set()),
+    "pieces": ((1, 1024, 20000, 1024, 6, 90, True), {"0", "2"}, {"256"}),
+    "pieces of a head as it lies": ((1, 1024, 20000, 1024, 8, 90, True), {"0", "2"}, {"256"}),
+    "a head as it lies": ((4, 512, 8448, 256, 8, 100, True), {"1"}, {"256"}),
+    "a remainder by small tiles": ((2, 1000, 8440, 1000, 6, 100, True), {"1"}, {"256", "128"}),
+}
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("name", LOSSES)
+def test_losses_by_large_tiles(driver, name, kind):
+    """What tests/test_head_loss_tiles.py compares goes by the kernels that it is about."""
+    (rows, tokens, vocab, width, before, share, gradient), modes, edges = LOSSES[name]
+    a, = ask(driver, [loss(rows, kind, tokens, vocab, width, before=before, gradient=gradient, share=share)])
+    check_head_gradient(a, rows, vocab, width, name)
+    assert {x.args[2] for x in a.of("k_head_logits")} == {"256"} and {x.args[4] for x in a.of("k_head_logits")} == modes
+    assert {x.args[2] for x in a.of("k_head_dhead")} == edges and {x.args[1] for x in a.of("k_head_dhidden")} == ({"256"} if gradient else set())
+    straight = kind == "bf16" and before == 8
+    assert a.of("k_head_operands")[0].grid[1] == (1 if straight else 2)        # hidden vectors only, or the head's as well
+    assert len({x.words[0] for x in a.of("k_head_dhead")}) == (2 if "pieces" in name else 1 if gradient else 0)

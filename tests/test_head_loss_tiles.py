@@ -6,6 +6,7 @@ import copy
 import numpy as np
 import pytest
 import torch
+from test_ends_calls import LOSSES
 from test_head_loss import KINDS, SENTINEL, Head, host
 
 from paper_2410_11998_amd import binding as B
@@ -27,6 +28,24 @@ def test_a_vocabulary_of_one_row_of_tiles(kind):
     c = Head(2048, 256, 2304, kind, rows=32, seed=21)
     c.run()
     check_some(c, (0, 17, 31))
+    c.close()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("name", LOSSES)
+def test_losses_by_large_tiles(name, kind):
+    (rows, tokens, vocab, width, at, share, gradient), _, _ = LOSSES[name]
+    c = Head(tokens, vocab, width, kind, rows=rows, bias=True, seed=24, before=at - 1)
+    assert c.at == at
+    work = c.workspace(max(c.info(gradient).least_bytes, c.info(gradient).bytes * share // 100))
+    c.run(gradient=gradient, work=work)
+    some = sorted({0, rows // 2, rows - 1})
+    check_some(c, some, gradient=gradient)
+    if gradient:
+        before = torch.randn(c.g.shape, device=c.g.device).to(c.g.dtype)
+        c.g.copy_(before)
+        c.run(flags=B.DADAM_HEAD_MEAN | B.DADAM_HEAD_ADD, work=work)
+        check_some(c, some[:1], before=before)
     c.close()
 
 
