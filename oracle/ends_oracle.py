@@ -45,6 +45,65 @@ def orthogonalised_error(m, planes, schedule=SCHEDULE):
     return e + 2.0 ** -22 * f(x)
 
 
+def _halves(v):
+    """(high, low): 11 bits each of float32 values, of whatever size."""
+    fraction, exponent = np.frexp(v.astype(np.float64))
+    high = np.ldexp(np.rint(fraction * 2048) / 2048, exponent).astype(np.float32)
+    fraction, exponent = np.frexp(v.astype(np.float64) - high)
+    return high, np.ldexp(np.rint(fraction * 2048) / 2048, exponent).astype(np.float32)
+
+
+def orthogonalised_with_roundings(m, planes, schedule=SCHEDULE):
+    """orthogonalised(m) with the operands' bits that the library states: X in two halves, A and B in one half (planes 1) or two, B's diagonal apart in float32; products
+    of one half a side or of two without low times low, sums in float32."""
+    m = np.asarray(m, dtype=np.float64)
+    x = m.T if m.shape[0] > m.shape[1] else m
+    x = x.astype(np.float32) * np.float32(1 / (np.sqrt((x * x).sum()) + 1e-7))
+
+    def product(p, q):
+        return p[0] @ q[0] + (p[0] @ q[1] + p[1] @ q[0]) if planes == 2 else p[0] @ q[0]
+
+    for a, b, c in np.asarray(schedule, dtype=np.float32):
+        h = _halves(x)
+        g = _halves(product(h, (h[0].T, h[1].T)))
+        B = b * (g[0] + g[1] if planes == 2 else g[0]) + c * product(g, g)
+        diagonal = np.diag(B).copy()
+        np.fill_diagonal(B, 0)
+        x = (h[0] + h[1]) * (a + diagonal)[:, None] + product(_halves(B), h)
+    return x.T if m.shape[0] > m.shape[1] else x
+
+
+def orthogonalised_spread(m, planes, schedule=SCHEDULE, draws=4, seed=0):
+    """How far (2-norm) the roundings of orthogonalised_with_roundings take the result, at most, over m and copies of it whose elements differ in their last places: the
+    library's sums are in another order, which leaves roundings as large but turns some the other way."""
+    rng, m = np.random.default_rng(seed), np.asarray(m, dtype=np.float64)
+    want, most = orthogonalised(m, schedule), 0.0
+    for k in range(draws):
+        near = m if k == 0 else m * (1 + rng.uniform(-1, 1, m.shape) * 2.0 ** -22)
+        most = max(most, np.linalg.norm(orthogonalised_with_roundings(near, planes, schedule) - want))
+    return most
+
+
+def orthogonalised_error_of_a_row(m, planes, schedule=SCHEDULE):
+    """A bound like orthogonalised_error's for a matrix of one row or column, whose roundings are too few to say anything about another draw of them.
+
+    X is s times a unit vector, so A = s^2 and B, all diagonal, are numbers.  An operand is off by u = 2^-22 of itself, or of the products' 2^-11 with one plane; a sum of K
+    products by 4 sqrt(K) roundings of 2^-24.  A is off by 2 u A and its sum, and by u A as it is held; B = b A + c A A by |b + 2 c A| times that, the product's sum and two roundings; a X +
+    B X by u of X, by s times what B is off and by three roundings.  What X is off already grows by the polynomial's slope along X and by p(s) / s across it."""
+    s = np.linalg.norm(np.asarray(m, dtype=np.float64))
+    s, size = s / (s + 1e-7), np.asarray(m).size
+    u, e = 2.0 ** -11 if planes == 1 else 2.0 ** -22, 2.0 ** -23
+    for a, b, c in schedule:
+        A = s * s
+        B = b * A + c * A * A
+        dA = (3 * u + 4 * np.sqrt(size) * 2.0 ** -24) * A
+        dB = abs(b + 2 * c * A) * dA + abs(c) * (dA * dA + 4 * 2.0 ** -24 * A * A) + 2.0 ** -23 * (abs(b) * A + abs(c) * A * A)
+        local = 2.0 ** -22 * s * abs(a + B) + s * dB + 3 * 2.0 ** -24 * s * (abs(a) + abs(B))
+        e = max(abs(a + 3 * b * A + 5 * c * A * A), abs(a + B)) * e + local
+        s = s * abs(a + B)
+    return 1.01 * e
+
+
 def head_loss(hidden, head, bias, targets, scale=1.0, mean=True):
     """{"loss", "nll", "dz", "dhidden", "dhead", "dbias"} of one replica; tokens without a target take no part."""
     with np.errstate(invalid="ignore", over="ignore"):
