@@ -440,9 +440,9 @@ __global__ __launch_bounds__(2 * EDGE) void k_head_dhead(HeadArgs a) {
 }
 
 // The same where there are so few tiles that the chip would wait for the tokens' sums: a part of the tokens (blockIdx.y), 32 bits, by rows of words.
-template <typename TY, int BUFFERS>
+template <typename TY>
 __global__ __launch_bounds__(256) void k_head_dhead_part(HeadArgs a) {
-  using T = TileOf<typename TY::op, TY::planes, 128, BUFFERS, true, true>;
+  using T = TileOf<typename TY::op, TY::planes, 128, 4, true, true>;
   const uint64_t base = base_of(a), b = 2 * TY::planes;
   const uint32_t across = a.s.D / T::kM, i = blockIdx.x % across, j = blockIdx.x / across, stages = a.s.T * TY::planes / 64;
   const uint32_t from = (uint32_t)((uint64_t)stages * blockIdx.y / a.s.parts), to = (uint32_t)((uint64_t)stages * (blockIdx.y + 1) / a.s.parts);
@@ -634,10 +634,10 @@ int launch_head_dhead(int xdt, int gdt, uint32_t edge, const HeadArgs& a, uint32
 }
 int launch_head_dhead_parts(int xdt, int gdt, const HeadArgs& a, uint32_t rows, void* stream) {
   const dim3 grid(upto(a.words, 128) * (a.s.D / 128), a.s.parts, rows);
-  const int e = with_tiles(xdt, gdt, 128, grid.x * grid.y * rows, [&](auto, auto, auto ty, auto, auto buffers) {
+  const int e = with_types(xdt, gdt, [&](auto, auto, auto ty) {  // (parts make no more tiles than compute units: four stages)
     using TY = decltype(ty);
-    using T = TileOf<typename TY::op, TY::planes, 128, decltype(buffers)::value, true, true>;
-    return launch<k_head_dhead_part<TY, decltype(buffers)::value>>(grid, T::kThreads, T::kLds, stream, a);
+    using T = TileOf<typename TY::op, TY::planes, 128, 4, true, true>;
+    return launch<k_head_dhead_part<TY>>(grid, T::kThreads, T::kLds, stream, a);
   });
   const dim3 pieces(upto((uint64_t)a.words * (a.s.D / 8), 256), 1, rows);
   return e ? e : with_types(xdt, gdt, [&](auto, auto g, auto ty) { return launch<k_head_join<decltype(g), decltype(ty)>>(pieces, 256, 0, stream, a); });

@@ -3,8 +3,9 @@
 // each, and prints one line for each: the command, the call's answer, the launches (kernel, grid x block, bytes of LDS) that it made, behind those of the head's gradient
 // the piece's first word, its words and how many of them the launch leaves out.  tests/test_ends_calls.py builds and runs it.
 //
-//   loss ROWS PARAM_TYPE GRAD_TYPE TOKENS VOCAB WIDTH BEFORE GRADIENT WORKSPACE    one handle and call; BEFORE elements lie before the head
+//   loss ROWS PARAM_TYPE GRAD_TYPE TOKENS VOCAB WIDTH BEFORE GRADIENT WORKSPACE BIAS   one handle and call; BEFORE elements lie before the head
 //   ortho ROWS PARAM_TYPE GRAD_TYPE STEP WORKSPACE ROWSxCOLS ...                   one handle, its matrices, and dadam_orthogonalize or (STEP 1) dadam_ortho_step
+//   kernels                                                                            the kernels of these calls that the library has
 // WORKSPACE: how many hundredths of the bytes that the information call asks for, at least the least.
 #include "dadam.h"
 #include "dadam_head.h"
@@ -83,17 +84,18 @@ static dadam_config config(uint32_t rows, uint64_t d, const std::vector<dadam_te
 }
 
 static int loss(std::istringstream& line, std::string* text) {
-  uint32_t rows, pt, gt, tokens, vocab, width, gradient;
+  uint32_t rows, pt, gt, tokens, vocab, width, gradient, bias;
   uint64_t before, hundredths;
-  line >> rows >> pt >> gt >> tokens >> vocab >> width >> before >> gradient >> hundredths;
-  const uint64_t n = (uint64_t)vocab * width, d = before + n;
+  line >> rows >> pt >> gt >> tokens >> vocab >> width >> before >> gradient >> hundredths >> bias;
+  const uint64_t n = (uint64_t)vocab * width, d = before + n + (bias ? vocab : 0);
   std::vector<dadam_tensor_desc> ts;
   if (before) ts.push_back({0, before, 0.f, 0});
   ts.push_back({before, n, 0.f, 0});
+  if (bias) ts.push_back({before + n, vocab, 0.f, 0});
   const dadam_config cfg = config(rows, d, ts, pt, gt);
   dadam_handle* h = nullptr;
   if (const int rc = dadam_init(&cfg, &h)) return rc;
-  const dadam_head head = {before ? 1u : 0u, DADAM_HEAD_NO_BIAS, vocab, width};
+  const dadam_head head = {before ? 1u : 0u, bias ? (uint32_t)ts.size() - 1 : DADAM_HEAD_NO_BIAS, vocab, width};
   dadam_head_info info{};
   int rc = dadam_head_get_info(h, &head, tokens, gradient, &info);
   const uint64_t bytes = part(hundredths, info.least_bytes, info.bytes), vectors = (uint64_t)tokens * width * 4;
@@ -153,7 +155,14 @@ int main() {
     words >> what;
     events.clear();
     next_address = 1ull << 32;
-    const int rc = what == "loss" ? loss(words, &text) : what == "ortho" ? ortho(words, &text) : -100;
+    int rc = -100;
+    if (what == "loss") rc = loss(words, &text);
+    if (what == "ortho") rc = ortho(words, &text);
+    if (what == "kernels") {
+      rc = 0;
+      for (const auto& k : kernels())
+        if (k.second.find("k_head_") != std::string::npos || k.second.find("k_few_") != std::string::npos || k.second.find("k_ortho_") != std::string::npos) events += " | kernel " + k.second;
+    }
     std::cout << line << ": " << rc << (rc < 0 ? " " + text : "") << events << "\n";
   }
   return 0;

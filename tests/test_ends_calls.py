@@ -2,6 +2,7 @@
 runtime that refuses what the real one refuses)."""
 
 import os
+import random
 import re
 import subprocess
 
@@ -27,6 +28,10 @@ def driver(tmp_path_factory):
     return exe
 
 
+def plain_kernel(text):
+    return re.sub(r"^(void|int) |dadam::|\(anonymous namespace\)::", "", text).split("(")[0]
+
+
 class Launch:
     """A kernel, its template arguments, grid, and of the head's gradient (the piece's first word, its words, how many of them are left out)."""
 
@@ -43,7 +48,9 @@ class Answer:
     def __init__(self, line):
         head, *events = line.split(": ", 1)[1].split(" | ")
         self.code, _, self.text = head.partition(" ")
-        self.code, self.launches = int(self.code), [Launch(e) for e in events]
+        self.code, self.launches = int(self.code), [Launch(e) for e in events if e.startswith("launch")]
+        self.kernels = {plain_kernel(e[len("kernel "):]) for e in events if e.startswith("kernel")}
+        self.reached = {plain_kernel(e[len("launch "):]) for e in events if e.startswith("launch")}
 
     def of(self, kernel):
         return [x for x in self.launches if x.kernel == kernel]
@@ -57,8 +64,8 @@ def ask(exe, commands):
     return [Answer(x) for x in plain]
 
 
-def loss(rows, kind, tokens, vocab, width, grad=None, before=0, gradient=True, share=100):
-    return f"loss {rows} {TYPES[kind]} {TYPES[grad or kind]} {tokens} {vocab} {width} {before} {int(gradient)} {share}"
+def loss(rows, kind, tokens, vocab, width, grad=None, before=0, gradient=True, share=100, bias=False):
+    return f"loss {rows} {TYPES[kind]} {TYPES[grad or kind]} {tokens} {vocab} {width} {before} {int(gradient)} {share} {int(bias)}"
 
 
 def check_head_gradient(a, rows, vocab, width, what):
@@ -141,3 +148,29 @@ def test_losses_by_large_tiles(driver, name, kind):
     straight = kind == "bf16" and before == 8
     assert a.of("k_head_operands")[0].grid[1] == (1 if straight else 2)        # hidden vectors only, or the head's as well
     assert len({x.words[0] for x in a.of("k_head_dhead")}) == (2 if "pieces" in name else 1 if gradient else 0)
+
+
+def test_every_kernel_is_reached(driver):
+    """By calls of every size, type, workspace and number of replicas, drawn once, and those above in every pair of types."""
+    rng = random.Random(1)
+    calls = [loss(rows, kind, tokens, vocab, width, grad, before, gradient, share) for (rows, tokens, vocab, width, before, share, gradient), _, _ in LOSSES.values() for kind in TYPES for grad in TYPES]
+
+    def log(low, high):
+        return int(2 ** rng.uniform(low, high))
+
+    for _ in range(600):
+        rows, tokens, vocab, width = rng.choice([1, 2, 4, 8, 17, 32, 40]), log(0, 14), log(0, 17), log(1, 12)
+        if rng.random() < 0.4:
+            tokens, vocab, width = rng.choice([1024, 2048, 4096]), rng.choice([50257, 8448, 20000]), rng.choice([256, 512, 1024])
+        calls.append(loss(rows, rng.choice(list(TYPES)), tokens, vocab, width, rng.choice(list(TYPES)), rng.choice([6, 8]), rng.random() < 0.8, rng.choice([100, 100, 60, 30, 1]), rng.random() < 0.5))
+    for _ in range(250):
+        rows, n, kind = rng.choice([1, 2, 4, 17, 20, 70]), rng.choice([3, 20, 60]), rng.random()
+        if kind < 0.7:
+            shapes = [(log(0, 5 if kind < 0.3 else 10), log(0, 6 if kind < 0.3 else 11)) for _ in range(n)]
+        else:
+            shapes = [(512, 512)] * rng.choice([5, 22, 64]) if kind < 0.9 else [(100, 60000), (64, 64)]
+        calls.append(ortho(rows, rng.choice(list(TYPES)), shapes, rng.random() < 0.5, rng.choice(list(TYPES)), rng.choice([100, 20, 0])))
+    there, *answers = ask(driver, ["kernels"] + calls)
+    assert all(a.code == 0 for a in answers) and len(there.kernels) > 150
+    reached = set().union(*(a.reached for a in answers))
+    assert reached == there.kernels, there.kernels - reached
