@@ -559,7 +559,7 @@ typedef struct {
 } dadam_matrix_desc;
 
 /* Register the matrices that the two calls below are about, in place of those registered before; n may be 0.  matrices[n] is a HOST array and is
- * copied.  Allocates and uploads 160 bytes a matrix and up to 16 bytes for every 128 x 128 elements, and may wait for the device: not for use under stream capture, and
+ * copied.  Allocates and uploads 144 bytes a matrix and up to 16 bytes for every 128 x 128 elements, and may wait for the device: not for use under stream capture, and
  * only while no launched work still uses the old ones. */
 int dadam_set_matrices(dadam_handle* h, const dadam_matrix_desc* matrices, uint32_t n);
 

@@ -1,7 +1,8 @@
 // The loss of a language model's head for few tokens (up to kFewTokens): what there is to read and write of the head counts, so it is read as it lies, once for the
 // logits and once for the hidden vectors' gradients, and its gradient is written; nothing of its size is copied.
 //
-// Wavefronts by themselves, without LDS.  Logits: 32 words by 32 tokens, every lane its own row's pieces of 16 bytes from memory.  dW: 32 words by 128 columns, summed over
+// Operands come to the registers straight from memory; LDS holds the sums of wavefronts that share a row's width, and the tokens' values for softmax.
+// Logits: 32 words by 32 tokens, every lane its own row's pieces of 16 bytes.  dW: 32 words by 128 columns, summed over
 // the tokens; dh: the tokens by 128 columns, summed over a range of words, whose rows the lanes read four columns each.  In both, column 4 n + j belongs to block j of 32,
 // so that a lane's four blocks' elements of a row are side by side in memory.  The logits (4 bytes for a token and a word, at most 64 of 2 or 4 bytes times the width) are kept.
 // bfloat16 parameters and gradients: 16 summed elements an instruction, softmax - e[target] rounded to bfloat16.  Otherwise float32 instructions, whose sixteenth part
